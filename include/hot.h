@@ -535,6 +535,99 @@ int hot_stats_whole(const float *yhat, int64_t m, int64_t ld, int32_t s, int32_t
                     float *std_out, void *stream);
 
 /*
+ * Around a network's head: layer norm, and a linear head's loss over a vocabulary without logits in memory.  What the sample layer
+ * draws ([S_loc, N]) holds the weights of both, one set per sample, as views; networks whose weights are no samples use the same
+ * calls with one set.  Tensors are float32, bfloat16 or float16; sums, statistics and losses are held in 32 bits or more, and a result is
+ * rounded to its type once.  Pointers need the alignment of their elements.  Runs on the current device; DEVICE pointers;
+ * workspaces are the caller's scratch (16-byte aligned, contents free before and after).
+ */
+#define HOT_F32 0
+#define HOT_BF16 1
+#define HOT_F16 2
+
+/*
+ * Layer norm over the last axis.  x: rows of `width` elements, `ldx` apart (0: every row the same), samples `x_sample` apart; y and dx are
+ * dense [samples, rows, width].  weight, bias: [width] for every sample, w_sample elements apart (0: one set for all; then their
+ * gradients are summed over all samples too).  ldy, y_sample: pitches of dy (backward call).  width <= 2^31.
+ */
+typedef struct hot_norm_desc {
+    int64_t rows;          /* of one sample, >= 0 */
+    int64_t width;         /* >= 1 */
+    int64_t ldx, x_sample; /* in elements */
+    int64_t ldy, y_sample;
+    int64_t w_sample;
+    double eps;            /* >= 0 */
+    int32_t samples;       /* 1 .. 65535 */
+    int32_t dtype;         /* of x, y, dy, dx */
+    int32_t weight_dtype;  /* of weight, bias and their gradients */
+    int32_t reserved;
+} hot_norm_desc;
+
+/*
+ * y = (x - m) r weight + bias with m = mean x, r = 1/sqrt(mean (x - m)^2 + eps) of each row.  weight and bias may be NULL (ones, zeros).
+ * mean, rstd: fp32 [samples, rows] for the backward call, both NULL to leave them out.
+ */
+int hot_norm_forward(const hot_norm_desc *desc, const void *x, const void *weight, const void *bias, void *y, float *mean,
+                     float *rstd, void *stream);
+
+/*
+ * With h = (x - m) r and u = dy weight:  dx = r (u - mean u - h mean(u h)),  grad_weight = sum over rows dy h,
+ * grad_bias = sum over rows dy.  dx, grad_weight, grad_bias: NULL leaves one out.  The sums are formed in a fixed order through the
+ * workspace (hot_norm_backward_workspace_bytes; NULL where neither sum is asked for).
+ */
+int64_t hot_norm_backward_workspace_bytes(const hot_norm_desc *desc);
+int hot_norm_backward(const hot_norm_desc *desc, const void *x, const void *weight, const float *mean, const float *rstd,
+                      const void *dy, void *dx, void *grad_weight, void *grad_bias, void *workspace, int64_t workspace_bytes,
+                      void *stream);
+
+/*
+ * A linear head over a vocabulary and its loss:  z[r, v] = x[r] . weight[v] + bias[v],  q = softmax(z / T).
+ *   top = 0: index[r] is row r's label, loss = -ln q[label]; T = 1.  Rows whose label is ignore_index have loss 0 and no gradient, whatever
+ *            x holds there; any other label outside the vocabulary gives NaN.
+ *   top > 0: index[r, 0 .. top-1] and logit[r, ..] are a teacher's likeliest words, p = softmax(logit / T) over those with index >= 0 (the
+ *            others, and words of logit -inf, are not there; a word may stand twice), loss = T^2 sum_j p_j (ln p_j - ln q[index_j]).  A
+ *            row that lists nothing has loss 0 and no gradient; an index >= vocab or a logit that is NaN or +inf gives NaN.
+ * x: rows `ldx` elements apart, samples `x_sample` apart (0: all samples see the same rows, whose gradients are then summed over the
+ * samples).  weight: [vocab] rows `ldw` apart, samples `w_sample` apart; bias: [vocab], samples `bias_sample` apart, may be NULL (-inf
+ * takes a word out).  All of dtype.  index: int64, entries of a row adjacent, rows `index_row` and samples `index_sample` apart (0: one
+ * set of targets for all samples); logit likewise, of logit_dtype.  Where |x| or |weight| exceeds 3.389e38 or is not finite, results of the
+ * rows concerned are not finite.  Limits: rows 2^22, width 2^19, vocab 2^24, top 1024, samples 4096, rows x vocab 2^38.
+ */
+typedef struct hot_head_desc {
+    int64_t rows;                      /* of one sample, >= 0 */
+    int64_t width, vocab;              /* >= 1 */
+    int64_t ldx, x_sample;             /* in elements, as all pitches */
+    int64_t ldw, w_sample;             /* ldw >= width; samples > 1: each has weights of its own */
+    int64_t bias_sample;
+    int64_t index_row, index_sample;
+    int64_t logit_row, logit_sample;
+    int64_t ignore_index;
+    double temperature;                /* T, 1e-4 .. 1e4 */
+    int32_t top;                       /* 0: labels */
+    int32_t samples;
+    int32_t dtype, logit_dtype;
+    int32_t w_aligned;                 /* weight is 16-byte aligned (16-bit types are then read as they lie where pitches allow) */
+    int32_t reserved;
+} hot_head_desc;
+
+/* Scratch of a call: which = 0 forward, 1 backward with dx, 2 backward without. */
+int64_t hot_head_workspace_bytes(const hot_head_desc *desc, int which);
+
+/* loss: fp32 [samples, rows].  lse: fp64 [samples, rows], ln sum_v exp(z / T) (0 for rows that do not count), for the backward call; may be NULL. */
+int hot_head_forward(const hot_head_desc *desc, const void *x, const void *weight, const void *bias, const int64_t *index,
+                     const void *logit, float *loss, double *lse, void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * grad_loss: fp32, the gradients of the rows' losses, rows `grad_row` and samples `grad_sample` elements apart (0: all the same).
+ * With dz = grad_loss T (q - sum_j p_j at index_j):  dx = dz weight (dense [samples, rows, width], or [rows, width] where x_sample = 0 and
+ * samples > 1),  grad_weight = dz^T x (dense [samples, vocab, width]),  grad_bias = sum over rows dz (dense [samples, vocab]); NULL
+ * leaves one out.  dz is formed from the logits again, a piece of the vocabulary at a time.
+ */
+int hot_head_backward(const hot_head_desc *desc, const void *x, const void *weight, const void *bias, const int64_t *index,
+                      const void *logit, const double *lse, const float *grad_loss, int64_t grad_sample, int64_t grad_row, void *dx,
+                      void *grad_weight, void *grad_bias, void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
  * Measurement aid, not a step of the paper's path: copies `bytes` (a multiple of 16;
  * both DEVICE pointers 16-byte aligned, ranges disjoint) on the current device with
  * the same 16-byte accesses the kernels use.  Its traffic is known exactly (bytes

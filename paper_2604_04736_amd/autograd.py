@@ -229,3 +229,132 @@ class BayesianModule(torch.nn.Module):
             sampled = {name: w[s, a:b].view(shape) for name, a, b, shape in self._slices}
             outs.append(torch.func.functional_call(self.module, sampled, inputs))
         return torch.stack(outs), kl
+
+
+# ------------------------------------------------------------------ layer norm, and a head's loss over a vocabulary
+
+def _adjacent(t):
+    """t, or a copy whose last axis is adjacent in memory."""
+    return t if t.shape[-1] < 2 or t.stride(-1) == 1 else t.contiguous()
+
+
+class _Norm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps, per_sample):
+        samples = x.shape[0] if per_sample else 1
+        x3 = _adjacent(x).reshape(samples, -1, x.shape[-1])
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        keep = any(ctx.needs_input_grad[:3])
+        mean, rstd = torch.empty(2, *x3.shape[:2], dtype=torch.float32, device=x.device) if keep else (None, None)
+        hot.hot_norm_forward(x3, weight, bias, eps, y.view(x3.shape), mean, rstd)
+        if keep:
+            ctx.save_for_backward(x3, weight, bias, mean, rstd)
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x3, weight, bias, mean, rstd = ctx.saved_tensors
+        want_x, want_w, want_b = ctx.needs_input_grad[:3]
+        dx = torch.empty(dy.shape, dtype=x3.dtype, device=dy.device) if want_x else None
+        dw = torch.empty_like(weight) if want_w else None
+        db = torch.empty_like(bias) if want_b else None
+        ws = None
+        if want_w or want_b:
+            ws = torch.empty(hot.hot_norm_backward_workspace_bytes(x3, weight if weight is not None else bias) // 4, dtype=torch.float32, device=dy.device)
+        hot.hot_norm_backward(x3, weight, mean, rstd, _adjacent(dy).reshape(x3.shape), dx.view(x3.shape) if want_x else None, dw, db, ws)
+        return dx, dw, db, None, None
+
+
+def layer_norm(x, weight=None, bias=None, eps: float = 1e-5) -> torch.Tensor:
+    """Layer norm of x [..., width] over the last axis, differentiable in x, weight and bias.  weight and bias: [width], or
+    [S, width] with x [S, ..., width], where weight sample s (a row of what GaussianSampleLayer draws) belongs to x[s]; either may be
+    None.  x: float32, bfloat16 or float16, which y has too; weight and bias: of x's type or float32.  Statistics and sums are float32."""
+    if x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError(f"x: need [..., width] with a width, got {tuple(x.shape)}")
+    shaped = weight if weight is not None else bias
+    per_sample = shaped is not None and shaped.dim() == 2
+    if per_sample and (x.dim() < 2 or shaped.shape[0] != x.shape[0]):
+        raise ValueError(f"weights of {shaped.shape[0]} samples need x [{shaped.shape[0]}, ..., width], got {tuple(x.shape)}")
+    weight, bias = (t.contiguous() if t is not None else None for t in (weight, bias))
+    return _Norm.apply(x, weight, bias, float(eps), per_sample)
+
+
+class _Head(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, index, logit, ignore_index, temperature):
+        loss = torch.empty(weight.shape[0], x.shape[1], dtype=torch.float32, device=x.device)
+        keep = any(ctx.needs_input_grad[:3])
+        lse = torch.empty(loss.shape, dtype=torch.float64, device=x.device) if keep else None
+        hot.hot_head_forward(x, weight, bias, index, logit, loss, lse, ignore_index, temperature)
+        if keep:
+            ctx.save_for_backward(x, weight, bias, index, logit, lse)
+            ctx.rule = (ignore_index, temperature)
+        return loss
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad_loss):
+        x, weight, bias, index, logit, lse = ctx.saved_tensors
+        dx, dw, db = (torch.empty(t.shape, dtype=t.dtype, device=t.device) if want else None for t, want in zip((x, weight, bias), ctx.needs_input_grad[:3]))
+        hot.hot_head_backward(x, weight, bias, index, logit, lse, grad_loss, dx, dw, db, *ctx.rule)
+        return dx, dw, db, None, None, None, None
+
+
+def _head(x, weight, bias, index, logit, ignore_index, temperature, entries: int):
+    """Shapes of a user's call to those of the binding; `entries`: axes of index behind the rows'."""
+    if not isinstance(weight, torch.Tensor) or weight.dim() not in (2, 3):
+        raise ValueError("weight: need [vocab, width] or [S, vocab, width]")
+    if x.dim() < 1 or x.shape[-1] != weight.shape[-1]:
+        raise ValueError(f"x: need [..., {weight.shape[-1]}], got {tuple(x.shape)}")
+    if bias is not None and bias.shape != weight.shape[:-1]:
+        raise ValueError(f"bias: need {tuple(weight.shape[:-1])}, got {tuple(bias.shape)}")
+    width, tail = x.shape[-1], index.shape[index.dim() - entries:]
+    x, weight = _adjacent(x), _adjacent(weight)
+    if weight.dim() == 2:
+        shape = x.shape[:-1]
+        if index.shape[:index.dim() - entries] != shape:
+            raise ValueError(f"targets: need {tuple(shape)} rows, got {tuple(index.shape)}")
+        x3, weight = x.reshape(1, -1, width), weight.unsqueeze(0)
+        bias = bias.unsqueeze(0) if bias is not None else None
+        index = index.reshape(1, -1, *tail)
+        logit = logit.reshape(index.shape) if logit is not None else None
+    else:
+        # [rows, width]: the same rows for every sample; [S, ..., width]: its own; targets for all samples or for each
+        samples = weight.shape[0]
+        own = x.dim() > 2
+        if own and x.shape[0] != samples:
+            raise ValueError(f"x: need [{samples}, ..., width] or [rows, width], got {tuple(x.shape)}")
+        rows = x.shape[1:-1] if own else x.shape[:-1]
+        x3 = x.reshape(samples if own else 1, -1, width)
+        shape = (samples, *rows)
+        lead = index.shape[:index.dim() - entries]
+        if lead not in (torch.Size(rows), torch.Size(shape)):
+            raise ValueError(f"targets: need {tuple(rows)} or {tuple(shape)} rows, got {tuple(index.shape)}")
+        sets = samples if len(lead) == len(shape) else 1
+        index = index.reshape(sets, -1, *tail)
+        logit = logit.reshape(index.shape) if logit is not None else None
+    if logit is not None:
+        index, logit = _adjacent(index), _adjacent(logit)
+    bias = _adjacent(bias) if bias is not None else None
+    return _Head.apply(x3, weight, bias, index, logit, int(ignore_index), float(temperature)).reshape(shape)
+
+
+def head_cross_entropy(x, weight, target, bias=None, ignore_index: int = -100) -> torch.Tensor:
+    """Cross entropy of the rows of a linear head, float32, from the features in front of it: ln sum_v exp(z_v) - z_target with
+    z = x weight^T + bias, without logits in memory; differentiable in x, weight and bias.  x [..., width], weight [vocab, width],
+    bias [vocab] or None, target int64 [...]; or one head per weight sample: weight [S, vocab, width], bias [S, vocab], x
+    [S, ..., width] or [rows, width] (which every sample then sees), target with or without the samples' axis.  Rows whose target is
+    ignore_index have loss 0 and take no part; a loss over the others is loss.sum() / their number.  x, weight and bias have one type:
+    float32, bfloat16 or float16."""
+    return _head(x, weight, bias, target, None, ignore_index, 1.0, 0)
+
+
+def head_distillation(x, weight, top_index, top_logit, bias=None, temperature: float = 1.0) -> torch.Tensor:
+    """T^2 KL(p || softmax(z / T)) of the rows of a linear head (see head_cross_entropy for x, weight, bias and samples), float32, where
+    p = softmax(top_logit / T) over a teacher's likeliest words top_index (int64 [..., top], negative: not there); differentiable in
+    x, weight and bias, not in the teacher.  Words that are not listed have p = 0 but count in the student's softmax.  A row that lists
+    nothing has loss 0 and takes no part."""
+    if top_index.dim() < 1 or top_index.shape != top_logit.shape:
+        raise ValueError(f"top_index and top_logit: need one shape, got {tuple(top_index.shape)} and {tuple(top_logit.shape)}")
+    return _head(x, weight, bias, top_index, top_logit.detach(), -100, temperature, 1)

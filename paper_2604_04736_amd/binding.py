@@ -33,13 +33,20 @@ EXPORTS = ("hot_create", "hot_forward", "hot_backward", "hot_destroy", "hot_set_
            "hot_backward_dropout_units_rng", "hot_stats_whole", "hot_adam_forward", "hot_backward_adam_forward",
            "hot_linear_backward_rng_ws", "hot_linear_backward_workspace_bytes", "hot_forward_static",
            "hot_linear_launch_shape", "hot_linear_kernel_shape", "hot_linear_planes_shape",
-           "hot_linear_forward_rng_ws", "hot_linear_planes_workspace_bytes", "hot_kl_layer")
+           "hot_linear_forward_rng_ws", "hot_linear_planes_workspace_bytes", "hot_kl_layer",
+           "hot_norm_forward", "hot_norm_backward", "hot_norm_backward_workspace_bytes", "hot_head_forward",
+           "hot_head_backward", "hot_head_workspace_bytes")
 
 
 # Return types of the entry points that do not return an int status (as declared in include/hot.h).
 RESTYPES = {"hot_strerror": ctypes.c_char_p, "hot_recommended_ld": ctypes.c_int64,
             "hot_linear_backward_workspace_bytes": ctypes.c_int64, "hot_linear_kernel_shape": ctypes.c_int64,
-            "hot_linear_planes_workspace_bytes": ctypes.c_int64}
+            "hot_linear_planes_workspace_bytes": ctypes.c_int64, "hot_norm_backward_workspace_bytes": ctypes.c_int64,
+            "hot_head_workspace_bytes": ctypes.c_int64}
+
+# Element types of the norm and the head (HOT_F32, HOT_BF16, HOT_F16).
+HOT_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+HOT_HEAD_MOST_TOP = 1024
 
 
 class hot_desc(ctypes.Structure):
@@ -68,6 +75,21 @@ class hot_adam(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
                 ("eps", ctypes.c_double), ("grad_scale", ctypes.c_double), ("sigma_min", ctypes.c_double),
                 ("step", ctypes.c_int64)]
+
+
+class hot_norm_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("width", ctypes.c_int64), ("ldx", ctypes.c_int64), ("x_sample", ctypes.c_int64),
+                ("ldy", ctypes.c_int64), ("y_sample", ctypes.c_int64), ("w_sample", ctypes.c_int64), ("eps", ctypes.c_double),
+                ("samples", ctypes.c_int32), ("dtype", ctypes.c_int32), ("weight_dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class hot_head_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("width", ctypes.c_int64), ("vocab", ctypes.c_int64), ("ldx", ctypes.c_int64),
+                ("x_sample", ctypes.c_int64), ("ldw", ctypes.c_int64), ("w_sample", ctypes.c_int64), ("bias_sample", ctypes.c_int64),
+                ("index_row", ctypes.c_int64), ("index_sample", ctypes.c_int64), ("logit_row", ctypes.c_int64),
+                ("logit_sample", ctypes.c_int64), ("ignore_index", ctypes.c_int64), ("temperature", ctypes.c_double),
+                ("top", ctypes.c_int32), ("samples", ctypes.c_int32), ("dtype", ctypes.c_int32), ("logit_dtype", ctypes.c_int32),
+                ("w_aligned", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 class HotError(RuntimeError):
@@ -150,6 +172,16 @@ def lib() -> ctypes.CDLL:
     L.hot_stats_merge.argtypes = [vp, vp, ctypes.POINTER(ctypes.c_int32), ctypes.c_int32, ctypes.c_int64,
                                   ctypes.c_int64, ctypes.c_int32, vp, vp, vp]
     L.hot_stats_merge.restype = ctypes.c_int
+    np = ctypes.POINTER(hot_norm_desc)
+    L.hot_norm_forward.argtypes = [np] + [vp] * 7
+    L.hot_norm_backward.argtypes = [np] + [vp] * 9 + [ctypes.c_int64, vp]
+    L.hot_norm_backward_workspace_bytes.argtypes = [np]
+    L.hot_norm_backward_workspace_bytes.restype = ctypes.c_int64
+    hp = ctypes.POINTER(hot_head_desc)
+    L.hot_head_forward.argtypes = [hp] + [vp] * 8 + [ctypes.c_int64, vp]
+    L.hot_head_backward.argtypes = [hp] + [vp] * 7 + [ctypes.c_int64] * 2 + [vp] * 4 + [ctypes.c_int64, vp]
+    L.hot_head_workspace_bytes.argtypes = [hp, ctypes.c_int]
+    L.hot_head_workspace_bytes.restype = ctypes.c_int64
     for name in EXPORTS:
         if name not in RESTYPES:
             getattr(L, name).restype = ctypes.c_int
@@ -747,3 +779,183 @@ def hot_backward_adam_forward(plan: Plan, rng: hot_rng, rng_next: hot_rng, param
                                            _vec(m_sigma, n, dev, "m_sigma"), _vec(v_sigma, n, dev, "v_sigma"),
                                            _mat(w, d.s_local, n, d.ld, dev, "w"), _kl_ptr(plan, kl_out), _stream(dev))
     _check(code, "hot_backward_adam_forward", plan)
+
+
+# ------------------------------------------------------------------ layer norm, and a head's loss over a vocabulary
+
+def _ptr(t):
+    return t.data_ptr() if t is not None else None
+
+
+def _typed(t, name: str, like=None) -> int:
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in HOT_TYPES):
+        raise TypeError(f"{name}: need a float32, bfloat16 or float16 tensor on a GPU")
+    if like is not None and t.device != like.device:
+        raise TypeError(f"{name}: need a tensor on {like.device}")
+    return HOT_TYPES[t.dtype]
+
+
+def _dense(t, shape, dtype, like, name: str) -> None:
+    if t is not None and not (t.is_cuda and t.device == like.device and t.dtype == dtype and tuple(t.shape) == tuple(shape) and t.is_contiguous()):
+        raise TypeError(f"{name}: need a contiguous {dtype} tensor of shape {tuple(shape)} on {like.device}")
+
+
+def _scratch_of(workspace, like):
+    if workspace is None:
+        return None, 0
+    if not (workspace.is_cuda and workspace.device == like.device and workspace.is_contiguous()):
+        raise TypeError(f"workspace: need a contiguous tensor on {like.device}")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _pitch(t, dim: int) -> int:
+    return t.stride(dim) if t.shape[dim] > 1 else 0
+
+
+def _norm_desc(x, weight, bias, eps: float, dy=None) -> hot_norm_desc:
+    """x [samples, rows, width], weight and bias [samples, width] or [width], dy like x."""
+    kind = _typed(x, "x")
+    if x.dim() != 3 or x.shape[2] < 1 or (x.shape[2] > 1 and x.stride(2) != 1):
+        raise ValueError(f"x: need [samples, rows, width] with adjacent elements, got {tuple(x.shape)} strides {x.stride()}")
+    samples, rows, width = x.shape
+    given = [(t, n) for t, n in ((weight, "weight"), (bias, "bias")) if t is not None]
+    weight_kind = kind
+    for t, name in given:
+        weight_kind = _typed(t, name, x)
+        if weight_kind not in (kind, 0):
+            raise TypeError(f"{name}: need x's type or float32")
+        if tuple(t.shape) not in ((width,), (samples, width)) or not t.is_contiguous():
+            raise ValueError(f"{name}: need a contiguous [{width}] or [{samples}, {width}], got {tuple(t.shape)} strides {t.stride()}")
+    if len(given) == 2 and (weight.shape != bias.shape or weight.dtype != bias.dtype):
+        raise ValueError("weight and bias: need one shape and type")
+    if dy is not None:
+        if _typed(dy, "dy", x) != kind or dy.shape != x.shape or (width > 1 and dy.stride(2) != 1):
+            raise ValueError(f"dy: need x's shape and type and adjacent elements, got {tuple(dy.shape)} strides {dy.stride()}")
+    d = dy if dy is not None else x
+    return hot_norm_desc(rows, width, _pitch(x, 1), _pitch(x, 0), _pitch(d, 1), _pitch(d, 0), width if given and given[0][0].dim() == 2 else 0,
+                         float(eps), samples, kind, weight_kind, 0)
+
+
+def hot_norm_forward(x, weight, bias, eps: float, y, mean=None, rstd=None) -> None:
+    """y = layer norm of x [samples, rows, width] over the last axis (see include/hot.h); weight, bias: [width], [samples, width] or
+    None; mean, rstd: float32 [samples, rows] for the backward call, or None."""
+    d = _norm_desc(x, weight, bias, eps)
+    _dense(y, x.shape, x.dtype, x, "y")
+    for t, name in ((mean, "mean"), (rstd, "rstd")):
+        _dense(t, x.shape[:2], torch.float32, x, name)
+    dev = x.device.index
+    with _on(dev):
+        code = lib().hot_norm_forward(ctypes.byref(d), x.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), _ptr(mean), _ptr(rstd), _stream(dev))
+    _check_planless(code, "hot_norm_forward")
+
+
+def hot_norm_backward_workspace_bytes(x, weight=None) -> int:
+    """Bytes of scratch that hot_norm_backward asks for where it forms gradients of weight or bias."""
+    d = _norm_desc(x, weight, None, 0.0)
+    n = lib().hot_norm_backward_workspace_bytes(ctypes.byref(d))
+    if n < 0:
+        _check_planless(int(n), "hot_norm_backward_workspace_bytes")
+    return int(n)
+
+
+def hot_norm_backward(x, weight, mean, rstd, dy, dx=None, grad_weight=None, grad_bias=None, workspace=None) -> None:
+    """Gradients of hot_norm_forward's x, weight and bias (each may be None and is then left out); dy: of x's shape and type."""
+    shaped = weight if weight is not None else (grad_weight if grad_weight is not None else grad_bias)
+    d = _norm_desc(x, shaped, None, 0.0, dy)
+    for t, name in ((mean, "mean"), (rstd, "rstd")):
+        _dense(t, x.shape[:2], torch.float32, x, name)
+    _dense(dx, x.shape, x.dtype, x, "dx")
+    for t, name in ((grad_weight, "grad_weight"), (grad_bias, "grad_bias")):
+        _dense(t, shaped.shape if t is not None else (), shaped.dtype if t is not None else None, x, name)
+    ws, ws_bytes = _scratch_of(workspace, x)
+    dev = x.device.index
+    with _on(dev):
+        code = lib().hot_norm_backward(ctypes.byref(d), x.data_ptr(), _ptr(weight), mean.data_ptr(), rstd.data_ptr(), dy.data_ptr(), _ptr(dx),
+                                       _ptr(grad_weight), _ptr(grad_bias), ws, ws_bytes, _stream(dev))
+    _check_planless(code, "hot_norm_backward")
+
+
+def _head_desc(x, weight, bias, index, logit, ignore_index: int, temperature: float) -> hot_head_desc:
+    """x [samples or 1, rows, width], weight [samples, vocab, width], bias [samples, vocab] or None; index [samples or 1, rows] (labels) or
+    [samples or 1, rows, top] with logit of that shape.  A leading 1 among several samples: the same for all."""
+    kind = _typed(x, "x")
+    if x.dim() != 3 or weight.dim() != 3 or x.shape[2] != weight.shape[2] or x.shape[0] not in (1, weight.shape[0]):
+        raise ValueError(f"x and weight: need [samples or 1, rows, width] and [samples, vocab, width], got {tuple(x.shape)} and {tuple(weight.shape)}")
+    samples, vocab, width = weight.shape
+    rows = x.shape[1]
+    if _typed(weight, "weight", x) != kind:
+        raise TypeError("weight: need x's type")
+    for t, name in ((x, "x"), (weight, "weight")):
+        if width > 1 and t.stride(2) != 1:
+            raise ValueError(f"{name}: need adjacent elements, got strides {t.stride()}")
+    if vocab > 1 and weight.stride(1) < width:
+        raise ValueError(f"weight: rows overlap (strides {weight.stride()})")
+    if bias is not None and (_typed(bias, "bias", x) != kind or tuple(bias.shape) != (samples, vocab) or (vocab > 1 and bias.stride(1) != 1)):
+        raise ValueError(f"bias: need x's type, shape {(samples, vocab)} and adjacent elements, got {tuple(bias.shape)}")
+    want = 2 if logit is None else 3
+    if not (index.is_cuda and index.device == x.device and index.dtype == torch.int64):
+        raise TypeError(f"index: need an int64 tensor on {x.device}")
+    if index.dim() != want or index.shape[0] not in (1, samples) or index.shape[1] != rows:
+        raise ValueError(f"index: need [samples or 1, rows{', top' if want == 3 else ''}], got {tuple(index.shape)}")
+    top, logit_kind = 0, 0
+    if logit is not None:
+        logit_kind, top = _typed(logit, "logit", x), index.shape[2]
+        if logit.shape != index.shape or not 1 <= top <= HOT_HEAD_MOST_TOP:
+            raise ValueError(f"logit: need index's shape with 1 to {HOT_HEAD_MOST_TOP} words a row, got {tuple(logit.shape)}")
+        if top > 1 and (index.stride(2) != 1 or logit.stride(2) != 1):
+            raise ValueError("index and logit: need adjacent words")
+    return hot_head_desc(rows, width, vocab, _pitch(x, 1), _pitch(x, 0), weight.stride(1) if vocab > 1 else width, _pitch(weight, 0),
+                         _pitch(bias, 0) if bias is not None else 0, _pitch(index, 1), _pitch(index, 0), _pitch(logit, 1) if top else 0,
+                         _pitch(logit, 0) if top else 0, int(ignore_index), float(temperature), top, samples, kind, logit_kind,
+                         int(weight.data_ptr() % 16 == 0), 0)
+
+
+def _head_workspace(d: hot_head_desc, which: int) -> int:
+    n = lib().hot_head_workspace_bytes(ctypes.byref(d), which)
+    if n < 0:
+        _check_planless(int(n), "hot_head_workspace_bytes")
+    return int(n)
+
+
+def hot_head_workspace_bytes(x, weight, bias, index, logit=None, which: int = 0, temperature: float = 1.0) -> int:
+    """Bytes of scratch of hot_head_forward (which = 0) and hot_head_backward (1 with dx, 2 without)."""
+    return _head_workspace(_head_desc(x, weight, bias, index, logit, -100, temperature), which)
+
+
+def hot_head_forward(x, weight, bias, index, logit, loss, lse=None, ignore_index: int = -100, temperature: float = 1.0, workspace=None) -> None:
+    """The rows' losses (float32 [samples, rows]) and, for the backward call, lse (float64) of a linear head; see include/hot.h and
+    _head_desc for the shapes.  workspace: scratch of hot_head_workspace_bytes, allocated here where it is None."""
+    d = _head_desc(x, weight, bias, index, logit, ignore_index, temperature)
+    shape = (d.samples, d.rows)
+    _dense(loss, shape, torch.float32, x, "loss")
+    _dense(lse, shape, torch.float64, x, "lse")
+    if workspace is None:
+        workspace = torch.empty(_head_workspace(d, 0), dtype=torch.uint8, device=x.device)
+    ws, ws_bytes = _scratch_of(workspace, x)
+    dev = x.device.index
+    with _on(dev):
+        code = lib().hot_head_forward(ctypes.byref(d), x.data_ptr(), weight.data_ptr(), _ptr(bias), index.data_ptr(), _ptr(logit), loss.data_ptr(),
+                                      _ptr(lse), ws, ws_bytes, _stream(dev))
+    _check_planless(code, "hot_head_forward")
+
+
+def hot_head_backward(x, weight, bias, index, logit, lse, grad_loss, dx=None, grad_weight=None, grad_bias=None, ignore_index: int = -100,
+                      temperature: float = 1.0, workspace=None) -> None:
+    """Gradients of the features (x's shape), the weights [samples, vocab, width] and the bias [samples, vocab] from those of the rows'
+    losses (grad_loss, float32 [samples, rows], any strides); each result may be None and is then left out."""
+    d = _head_desc(x, weight, bias, index, logit, ignore_index, temperature)
+    _dense(lse, (d.samples, d.rows), torch.float64, x, "lse")
+    if not (grad_loss.is_cuda and grad_loss.device == x.device and grad_loss.dtype == torch.float32 and tuple(grad_loss.shape) == (d.samples, d.rows)):
+        raise TypeError(f"grad_loss: need a float32 tensor of shape {(d.samples, d.rows)} on {x.device}")
+    _dense(dx, x.shape, x.dtype, x, "dx")
+    _dense(grad_weight, weight.shape, x.dtype, x, "grad_weight")
+    _dense(grad_bias, (d.samples, d.vocab), x.dtype, x, "grad_bias")
+    if workspace is None:
+        workspace = torch.empty(_head_workspace(d, 1 if dx is not None else 2), dtype=torch.uint8, device=x.device)
+    ws, ws_bytes = _scratch_of(workspace, x)
+    dev = x.device.index
+    with _on(dev):
+        code = lib().hot_head_backward(ctypes.byref(d), x.data_ptr(), weight.data_ptr(), _ptr(bias), index.data_ptr(), _ptr(logit), lse.data_ptr(),
+                                       grad_loss.data_ptr(), _pitch(grad_loss, 0), _pitch(grad_loss, 1), _ptr(dx), _ptr(grad_weight),
+                                       _ptr(grad_bias), ws, ws_bytes, _stream(dev))
+    _check_planless(code, "hot_head_backward")

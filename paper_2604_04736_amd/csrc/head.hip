@@ -1,0 +1,1251 @@
+// libhot: a linear head's loss over a vocabulary and its gradients, from the features in front of the head, without logits in memory.
+//
+//   z[r, v] = x[r] . W[v] + b[v],  q = softmax(z / T),  a row's targets are entries (i_j, p_j) with sum p_j = 1:
+//   loss[r] = T^2 sum_j p_j (ln p_j - ln q[i_j]) = T^2 (sum_j p_j ln p_j + lse(z / T) - sum_j p_j z[i_j] / T)
+//   dz = g T (q - sum_j p_j delta_(i_j)),  dx = dz W,  dW = dz^T x,  db = sum_r dz
+// A label is one entry of weight one at T = 1 (the cross entropy); a teacher's top logits t give p = softmax(t / T) over the words listed.
+//
+// The forward pass multiplies tiles of vocabulary by tiles of rows; a tile leaves per row its largest logit, its sum of exponentials and its
+// share of sum_j p_j z, which a second kernel joins.  The backward pass walks the vocabulary in pieces: it forms a piece's logits again,
+// leaves dz of that piece in scratch memory (16 bits, or three bf16 pieces of float32) and multiplies it with W and with x.  Its
+// products are 2 R V K operations each, one forward and three backward; what bounds them is the matrix pipes from some hundred rows
+// on, below that reading W.
+// Rows without entries are left out before anything is multiplied, so what they hold (NaN too) reaches no result and costs nothing.
+#include <hip/hip_runtime.h>
+
+#include "hot.h"
+#include "vec.h"
+#include "element.h"
+#include "tile.h"
+
+namespace {
+
+constexpr int kComputeUnits = 256;
+constexpr int kMostTop = 1024;           // entries of a row (they are sorted in LDS)
+constexpr int kStartStep = 128;          // words between the marks into a row's sorted entries
+constexpr float kHalfScale = 4096.0f;    // fp16 logits' gradients are held times this: a probability of 1e-11 still counts, 16 x 4096 does not overflow
+
+inline __host__ __device__ long up(long n, long to) { return (n + to - 1) / to * to; }
+
+// --------------------------------------------------------------------------- a teacher's entries
+
+struct ListArgs {
+    long lists, rows;                  // lists = rows x (samples or one)
+    long idx_sample, idx_row, logit_sample, logit_row;
+    int top, logit_type, marks;        // marks = vocabulary / kStartStep, rounded up
+    long vocab;
+    float inv_temperature;
+    const int64_t *index;
+    const void *logit;
+    int *word;                         // [lists, top] ascending
+    float *weight;                     // [lists, top]
+    int *count;                        // [lists]
+    double *sums;                      // [lists, 2]: sum p ln p, sum p
+    unsigned short *start;             // [lists, marks + 1]: entries below word kStartStep * k
+};
+
+constexpr int kListWaves = 4;
+
+__device__ __forceinline__ float wave_max(float v)
+{
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off));
+    return v;
+}
+
+__device__ __forceinline__ double wave_total(double v)
+{
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
+    return v;
+}
+
+// One wave to a row: softmax of what is listed, entries of weight zero dropped, the others sorted by word (rank by comparison with all).
+__global__ void __launch_bounds__(64 * kListWaves)
+hot_head_lists_kernel(ListArgs a)
+{
+    __shared__ int words[kListWaves][kMostTop], sorted[kListWaves][kMostTop];
+    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
+    const long list = (long)blockIdx.x * kListWaves + wave;
+    int *const w = words[wave], *const in_order = sorted[wave];
+    if (list < a.lists) {
+        const long s = list / a.rows, row = list % a.rows;
+        const int64_t *const index = a.index + s * a.idx_sample + row * a.idx_row;
+        const long logit0 = s * a.logit_sample + row * a.logit_row;
+        auto logit = [&](int j) {
+            typedef float F1 __attribute__((ext_vector_type(1)));
+            return load_as<1, F1>(a.logit, a.logit_type, logit0 + j, logit0 + a.top)[0] * a.inv_temperature;
+        };
+        float most = -__builtin_inff();
+        bool outside = false, nan = false;
+        for (int j = lane; j < a.top; j += 64) {
+            const int64_t i = index[j];
+            if (i < 0) continue;
+            outside |= i >= a.vocab;
+            const float t = logit(j);
+            nan |= t != t;
+            most = fmaxf(most, t);
+        }
+        most = wave_max(most);
+        double total = 0.0;
+        for (int j = lane; j < a.top; j += 64)
+            if (index[j] >= 0) total += (double)expf(logit(j) - most);
+        total = wave_total(total);
+        // a word outside the vocabulary or a logit that is no number leaves a row that is none; nothing listed, or nothing but -inf, no entries
+        const bool broken = __builtin_amdgcn_ballot_w64(outside || nan) != 0 || most == __builtin_inff();
+        const bool empty = !broken && most == -__builtin_inff();
+        double entropy = 0.0, sum = 0.0;
+        const double log_total = log(total);
+        for (int j = lane; j < a.top; j += 64) {
+            const int64_t i = index[j];
+            float p = 0.0f;
+            if (!broken && !empty && i >= 0) {
+                const float t = logit(j);
+                p = (float)((double)expf(t - most) / total);
+                if (p > 0.0f) {
+                    entropy += (double)p * ((double)(t - most) - log_total);
+                    sum += (double)p;
+                }
+            }
+            w[j] = p > 0.0f ? (int)i : -1;
+        }
+        entropy = wave_total(entropy);
+        sum = wave_total(sum);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        int kept = 0;
+        for (int j0 = 0; j0 < a.top; j0 += 64) {
+            const int j = j0 + lane, mine = j < a.top ? w[j] : -1;
+            kept += __builtin_popcountll(__builtin_amdgcn_ballot_w64(mine >= 0));
+            if (mine < 0) continue;
+            int rank = 0;
+            for (int k = 0; k < a.top; ++k) rank += w[k] >= 0 && (w[k] < mine || (w[k] == mine && k < j));
+            in_order[rank] = mine;
+            a.word[list * a.top + rank] = mine;
+            a.weight[list * a.top + rank] = (float)((double)expf(logit(j) - most) / total);
+        }
+        if (broken) {
+            if (lane == 0) {
+                in_order[0] = 0;
+                a.word[list * a.top] = 0;
+                a.weight[list * a.top] = __builtin_nanf("");
+            }
+            kept = 1;
+            entropy = sum = (double)__builtin_nanf("");
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (lane == 0) {
+            a.count[list] = kept;
+            a.sums[2 * list] = entropy;
+            a.sums[2 * list + 1] = sum;
+        }
+        for (int m = lane; m <= a.marks; m += 64) {
+            const int word = m * kStartStep;
+            int lo = 0, hi = kept;
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                if (in_order[mid] < word) lo = mid + 1;
+                else hi = mid;
+            }
+            a.start[list * (a.marks + 1) + m] = (unsigned short)lo;
+        }
+    }
+}
+
+// --------------------------------------------------------------------------- the rows that count
+
+struct RowArgs {
+    long rows, vocab;
+    long idx_sample, idx_row;
+    int64_t ignore;
+    const int64_t *index;          // labels, or
+    const int *list_count;         // entries of every list
+    long list_sample;              // lists between samples
+    const double *lse;             // backward: [samples, rows] and the gradients of the losses
+    const float *g;
+    long g_sample, g_row;
+    float scale_to;                // what the largest gradient is held as
+    int *count;                    // [samples]
+    int *row_of, *place_of;        // [samples, rows]: the row at a place, the place of a row (-1: left out)
+    int *label;                    // [samples, rows] by place (-1: no word)
+    float *hi, *lo, *grad;         // by place: lse in base 2 as two floats, the row's gradient
+    float *scale;                  // [samples, 2]: what gradients are multiplied with, and what results are multiplied with in turn
+};
+
+constexpr int kRowBlock = 1024;
+
+__global__ void __launch_bounds__(kRowBlock)
+hot_head_rows_kernel(RowArgs a)
+{
+    __shared__ int totals[kRowBlock / 64];
+    __shared__ float most[kRowBlock / 64];
+    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
+    const long s = blockIdx.x, base = s * a.rows;
+    int before = 0;
+    float largest = 0.0f;
+    for (long r0 = 0; r0 < a.rows; r0 += kRowBlock) {
+        const long row = r0 + threadIdx.x;
+        bool counts = false;
+        int label = -1;
+        if (row < a.rows) {
+            if (a.list_count) counts = a.list_count[s * a.list_sample + row] > 0;
+            else {
+                const int64_t t = a.index[s * a.idx_sample + row * a.idx_row];
+                counts = t != a.ignore;
+                label = t >= 0 && t < a.vocab ? (int)t : -1;
+            }
+        }
+        const unsigned long long mask = __builtin_amdgcn_ballot_w64(counts);
+        if (lane == 0) totals[wave] = __builtin_popcountll(mask);
+        __syncthreads();
+        int at = before + __builtin_popcountll(mask & ((1ull << lane) - 1));
+#pragma unroll
+        for (int i = 0; i < kRowBlock / 64; ++i) {
+            if (i < wave) at += totals[i];
+            before += totals[i];
+        }
+        if (row < a.rows) {
+            a.place_of[base + row] = counts ? at : -1;
+            if (counts) {
+                a.row_of[base + at] = (int)row;
+                if (a.label) a.label[base + at] = label;
+                if (a.lse) {
+                    const double two = a.lse[base + row] * (1.0 / 0.69314718055994530942);
+                    const float hi = (float)two;
+                    a.hi[base + at] = hi;
+                    a.lo[base + at] = __builtin_isfinite(hi) ? (float)(two - (double)hi) : 0.0f;
+                    float g = a.g[s * a.g_sample + row * a.g_row];
+                    if (!a.list_count && label < 0) g = __builtin_nanf("");
+                    a.grad[base + at] = g;
+                    largest = fmaxf(largest, __builtin_fabsf(g));
+                }
+            }
+        }
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) a.count[s] = before;
+    if (!a.lse) return;
+    largest = wave_max(largest);
+    if (lane == 0) most[wave] = largest;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+#pragma unroll
+    for (int i = 0; i < kRowBlock / 64; ++i) largest = fmaxf(largest, most[i]);
+    const bool usable = largest > 1e-30f && largest < 1e30f;
+    a.scale[2 * s] = usable ? a.scale_to / largest : a.scale_to;
+    a.scale[2 * s + 1] = usable ? largest / a.scale_to : 1.0f / a.scale_to;
+}
+
+// --------------------------------------------------------------------------- operands as the tiles read them
+
+struct PackArgs {
+    const void *from;
+    long from_row, from_sample;    // elements
+    const int *row_of;             // [samples, rows] or null: rows as they are
+    const int *count;              // with row_of: how many of them
+    long rows, map_sample;
+    int width, chunks;             // chunks = width / 8, rounded up
+    char *to;                      // [samples][rows][chunks * 16 bytes], pieces `plane` apart
+    long to_sample, plane;
+};
+
+// the three bf16 pieces of a float, whose sum it is up to 2^-25 of it; what is not finite stays in the first
+__device__ __forceinline__ void split_bf16(float x, __bf16 (&p)[3])
+{
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        p[i] = (__bf16)x;
+        const float back = (float)p[i];
+        x = __builtin_isfinite(back) ? x - back : 0.0f;
+    }
+}
+
+template <class T>
+__global__ void __launch_bounds__(256)
+hot_head_pack_kernel(PackArgs a)
+{
+    const long s = blockIdx.y, n = a.row_of ? a.count[s] : a.rows;
+    const long items = n * a.chunks;
+    for (long item = (long)blockIdx.x * 256 + threadIdx.x; item < items; item += (long)gridDim.x * 256) {
+        const long place = item / a.chunks;
+        const int chunk = (int)(item - place * a.chunks);
+        const long row = a.row_of ? a.row_of[s * a.map_sample + place] : place;
+        const T *const from = static_cast<const T *>(a.from) + (size_t)s * (size_t)a.from_sample + (size_t)row * (size_t)a.from_row;
+        char *const to = a.to + (size_t)s * (size_t)a.to_sample + ((size_t)place * (size_t)a.chunks + (size_t)chunk) * 16;
+        if constexpr (sizeof(T) == 2) {
+            typedef T V __attribute__((ext_vector_type(8)));
+            *reinterpret_cast<V *>(to) = __builtin_convertvector(Piece<T>::load(from, chunk * 8L, a.width), V);
+        } else {
+            typedef __bf16 V __attribute__((ext_vector_type(8)));
+            V p[3];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const typename Piece<T>::F v = Piece<T>::load(from, chunk * 8L + 4 * h, a.width);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    __bf16 q[3];
+                    split_bf16(v[j], q);
+#pragma unroll
+                    for (int i = 0; i < 3; ++i) p[i][4 * h + j] = q[i];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 3; ++i) *reinterpret_cast<V *>(to + (size_t)i * (size_t)a.plane) = p[i];
+        }
+    }
+}
+
+// --------------------------------------------------------------------------- logits: statistics, or their gradients
+
+struct HeadArgs {
+    const char *w, *x;             // rows of 16-bit elements (pieces `plane` apart); w begins at word v_begin
+    long w_pitch, w_plane, w_sample, x_pitch, x_plane, x_sample;      // bytes
+    int width;
+    int vocab, v_begin, v_count;   // the piece of the vocabulary
+    long rows, places;             // rows a sample, and that rounded up to 256
+    const int *count, *row_of, *label;
+    const void *bias;
+    long bias_sample;
+    int bias_type;
+    float scale;                   // log2(e) / temperature
+    // a teacher's entries
+    const int *word;
+    const float *weight;
+    const unsigned short *start;
+    int top, marks;
+    long list_sample;
+    // forward: partials[sample][tile][3][place]
+    float *partials;
+    int v_tiles;
+    // backward
+    const float *hi, *lo, *grad, *to_scale;
+    char *dz;                      // [sample][place][dz_pitch]
+    long dz_pitch, dz_plane, dz_sample;
+};
+
+// Walks the targets of this lane's rows that lie in the wave's words: f(nb, m, i, mine, weight) is called for every result (m, i) that
+// some lane's target may be, `mine` where it is this lane's.
+template <class TILE, bool LISTS, class F>
+__device__ __forceinline__ void for_targets(const HeadArgs &a, long s, int v0, const int (&place)[TILE::NB], const bool (&live)[TILE::NB], const F &f)
+{
+    const int first = v0 + TILE::m0(), low = 4 * (TILE::lane() >> 5);
+    auto meet = [&](int nb, int word, float weight) {
+        const int in = word - first;
+#pragma unroll
+        for (int m = 0; m < TILE::MB; ++m) {
+            if (__builtin_amdgcn_ballot_w64(in >= 32 * m && in < 32 * m + 32) == 0) continue;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) f(nb, m, i, in - low == 32 * m + 8 * (i >> 2) + (i & 3), weight);
+        }
+    };
+#pragma unroll
+    for (int nb = 0; nb < TILE::NB; ++nb) {
+        if constexpr (!LISTS) meet(nb, live[nb] ? a.label[s * a.rows + place[nb]] : -1, 1.0f);
+        else {
+            int e = 0, end = 0;
+            const int *words = a.word;
+            const float *weights = a.weight;
+            if (live[nb]) {
+                const long list = s * a.list_sample + a.row_of[s * a.rows + place[nb]];
+                const unsigned short *const start = a.start + list * (a.marks + 1);
+                const int mark = v0 / kStartStep, last = mark + TILE::BM / kStartStep;
+                e = start[mark];
+                end = start[last < a.marks ? last : a.marks];
+                words += list * a.top;
+                weights += list * a.top;
+            }
+            while (__builtin_amdgcn_ballot_w64(e < end) != 0) {
+                const bool more = e < end;
+                meet(nb, more ? words[e] : -1, more ? weights[e] : 0.0f);
+                ++e;
+            }
+        }
+    }
+}
+
+// acc -> logits in units of ln 2 / T, less `minus` of their row; words beyond the vocabulary -inf
+template <class TILE>
+__device__ __forceinline__ void to_scores(const HeadArgs &a, long s, int v0, const float (&minus)[TILE::NB], f16v (&acc)[TILE::MB][TILE::NB])
+{
+    const bool ragged = v0 + TILE::BM > a.vocab;
+#pragma unroll
+    for (int m = 0; m < TILE::MB; ++m)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float bias = 0.0f;
+            const int v = v0 + TILE::m0() + 32 * m + TILE::row(i);
+            if (a.bias) {
+                typedef float F1 __attribute__((ext_vector_type(1)));
+                bias = load_as<1, F1>(a.bias, a.bias_type, s * a.bias_sample + v, s * a.bias_sample + a.vocab)[0] * a.scale;
+            }
+            const bool none = ragged && v >= a.vocab;
+#pragma unroll
+            for (int n = 0; n < TILE::NB; ++n) {
+                const float z = __builtin_fmaf(acc[m][n][i], a.scale, bias - minus[n]);
+                acc[m][n][i] = none ? -__builtin_inff() : z;
+            }
+        }
+}
+
+template <class TILE>
+__device__ __forceinline__ bool head_product(const HeadArgs &a, lds_char *lds, long s, int &v0, int &r0, f16v (&acc)[TILE::MB][TILE::NB])
+{
+    const int count = a.count[s];
+    const Place at = place((int)blockIdx.x, (a.v_count + TILE::BM - 1) / TILE::BM, (count + TILE::BN - 1) / TILE::BN);
+    if (!at.any) return false;
+    const int in = at.m * TILE::BM;
+    v0 = a.v_begin + in;
+    r0 = at.n * TILE::BN;
+    const Operand w = {a.w + (size_t)s * (size_t)a.w_sample + (size_t)in * (size_t)a.w_pitch, a.w_pitch, a.w_plane, a.v_begin + a.v_count - v0, a.width};
+    const Operand x = {a.x + (size_t)s * (size_t)a.x_sample + (size_t)r0 * (size_t)a.x_pitch, a.x_pitch, a.x_plane, count - r0, a.width};
+    TILE::product(lds, w, x, a.width, acc);
+    return true;
+}
+
+template <class TILE, bool LISTS>
+__global__ void __launch_bounds__(TILE::THREADS)
+hot_head_forward_kernel(HeadArgs a)
+{
+    constexpr int NEED = 3 * TILE::WAVES_M * TILE::BN * 4;
+    __shared__ __attribute__((aligned(1024))) char memory[TILE::kLds > NEED ? TILE::kLds : NEED];
+    const long s = blockIdx.y;
+    int v0, r0;
+    f16v acc[TILE::MB][TILE::NB];
+    if (!head_product<TILE>(a, (lds_char *)memory, s, v0, r0, acc)) return;
+    const float zero[TILE::NB] = {};
+    to_scores<TILE>(a, s, v0, zero, acc);
+    float dot[TILE::NB] = {};
+    int at[TILE::NB];
+    bool live[TILE::NB];
+#pragma unroll
+    for (int n = 0; n < TILE::NB; ++n) {
+        at[n] = r0 + TILE::n0() + 32 * n + (TILE::lane() & 31);
+        live[n] = at[n] < a.count[s];
+    }
+    for_targets<TILE, LISTS>(a, s, v0, at, live, [&](int n, int m, int i, bool mine, float weight) { dot[n] += mine ? weight * acc[m][n][i] : 0.0f; });
+    float (*const part)[TILE::WAVES_M][TILE::BN] = reinterpret_cast<float (*)[TILE::WAVES_M][TILE::BN]>(memory);
+#pragma unroll
+    for (int n = 0; n < TILE::NB; ++n) {
+        float most = acc[0][n][0];
+#pragma unroll
+        for (int m = 0; m < TILE::MB; ++m)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) most = fmaxf(most, acc[m][n][i]);
+        most = fmaxf(most, __shfl_xor(most, 32));
+        const float from = most == -__builtin_inff() ? 0.0f : most;        // (nothing but -inf: a sum of zero)
+        float sum = 0.0f;
+#pragma unroll
+        for (int m = 0; m < TILE::MB; ++m)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sum += __builtin_amdgcn_exp2f(acc[m][n][i] - from);
+        sum += __shfl_xor(sum, 32);
+        dot[n] += __shfl_xor(dot[n], 32);
+        if (TILE::lane() < 32) {
+            const int wm = TILE::wave() / TILE::WAVES_N, col = TILE::n0() + 32 * n + TILE::lane();
+            part[0][wm][col] = most;
+            part[1][wm][col] = sum;
+            part[2][wm][col] = dot[n];
+        }
+    }
+    __syncthreads();
+    for (int col = (int)threadIdx.x; col < TILE::BN; col += TILE::THREADS) {
+        if (r0 + col >= a.count[s]) break;
+        float most = part[0][0][col];
+#pragma unroll
+        for (int k = 1; k < TILE::WAVES_M; ++k) most = fmaxf(most, part[0][k][col]);
+        float sum = 0.0f, d = 0.0f;
+#pragma unroll
+        for (int k = 0; k < TILE::WAVES_M; ++k) {
+            // (a largest logit of -inf: a sum of zero, or none where a logit is no number)
+            sum += part[0][k][col] == -__builtin_inff() ? part[1][k][col] : part[1][k][col] * __builtin_amdgcn_exp2f(part[0][k][col] - most);
+            d += part[2][k][col];
+        }
+        float *const out = a.partials + (((size_t)s * (size_t)a.v_tiles + (size_t)(v0 / TILE::BM)) * 3) * (size_t)a.places + (size_t)(r0 + col);
+        out[0] = most;
+        out[a.places] = sum;
+        out[2 * a.places] = d;
+    }
+}
+
+template <class TILE, bool LISTS>
+__global__ void __launch_bounds__(TILE::THREADS)
+hot_head_dz_kernel(HeadArgs a)
+{
+    constexpr int PITCH = TILE::BM * 2 + 16, NEED = TILE::BN * PITCH;       // (16 bytes on: rows of a column of lanes lie in different banks)
+    __shared__ __attribute__((aligned(1024))) char memory[TILE::kLds > NEED ? TILE::kLds : NEED];
+    const long s = blockIdx.y;
+    int v0, r0;
+    f16v acc[TILE::MB][TILE::NB];
+    if (!head_product<TILE>(a, (lds_char *)memory, s, v0, r0, acc)) return;
+    int at[TILE::NB];
+    bool live[TILE::NB];
+    float hi[TILE::NB], lo[TILE::NB], g[TILE::NB];
+    const float to_scale = a.to_scale[2 * s];
+#pragma unroll
+    for (int n = 0; n < TILE::NB; ++n) {
+        at[n] = r0 + TILE::n0() + 32 * n + (TILE::lane() & 31);
+        live[n] = at[n] < a.count[s];
+        hi[n] = live[n] ? a.hi[s * a.rows + at[n]] : __builtin_inff();
+        lo[n] = live[n] ? a.lo[s * a.rows + at[n]] : 0.0f;
+        g[n] = live[n] ? a.grad[s * a.rows + at[n]] * to_scale : 0.0f;
+    }
+    to_scores<TILE>(a, s, v0, hi, acc);
+#pragma unroll
+    for (int m = 0; m < TILE::MB; ++m)
+#pragma unroll
+        for (int n = 0; n < TILE::NB; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                // (the low part of lse is below the rounding of 16-bit results)
+                const float z = TILE::PIECES == 1 ? acc[m][n][i] : acc[m][n][i] - lo[n];
+                acc[m][n][i] = __builtin_amdgcn_exp2f(z);
+            }
+    for_targets<TILE, LISTS>(a, s, v0, at, live, [&](int n, int m, int i, bool mine, float weight) { acc[m][n][i] -= mine ? weight : 0.0f; });
+    // to rows of words, piece by piece, through LDS
+    typedef typename TILE::T T;
+    typedef T V4 __attribute__((ext_vector_type(4)));
+    typedef T V8 __attribute__((ext_vector_type(8)));
+    char *const out = a.dz + (size_t)s * (size_t)a.dz_sample + (size_t)r0 * (size_t)a.dz_pitch + (size_t)(v0 - a.v_begin) * 2;
+#pragma unroll
+    for (int p = 0; p < TILE::PIECES; ++p) {
+        if (p) __syncthreads();
+#pragma unroll
+        for (int n = 0; n < TILE::NB; ++n)
+#pragma unroll
+            for (int m = 0; m < TILE::MB; ++m)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    V4 o;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float v = p == 0 ? acc[m][n][4 * q + i] * g[n] : acc[m][n][4 * q + i];
+                        o[i] = (T)v;
+                        if constexpr (TILE::PIECES > 1) acc[m][n][4 * q + i] = __builtin_isfinite((float)o[i]) ? v - (float)o[i] : 0.0f;
+                    }
+                    *reinterpret_cast<V4 *>(memory + (TILE::n0() + 32 * n + (TILE::lane() & 31)) * PITCH + (TILE::m0() + 32 * m + TILE::row(4 * q)) * 2) = o;
+                }
+        __syncthreads();
+        constexpr int CHUNKS = TILE::BM / 8;
+#pragma unroll 4
+        for (int k = (int)threadIdx.x; k < TILE::BN * CHUNKS; k += TILE::THREADS) {
+            const int row = k / CHUNKS, chunk = k % CHUNKS;
+            *reinterpret_cast<V8 *>(out + (size_t)p * (size_t)a.dz_plane + (size_t)row * (size_t)a.dz_pitch + chunk * 16) =
+                *reinterpret_cast<const V8 *>(memory + row * PITCH + chunk * 16);
+        }
+    }
+}
+
+// --------------------------------------------------------------------------- joining a row's partial statistics
+
+struct JoinArgs {
+    long rows, places;
+    int tiles, lanes;              // lanes: threads to a row
+    const float *partials;
+    const int *place_of, *label;
+    const double *sums;            // of the lists, or null
+    long list_sample;
+    double temperature;
+    float *loss;
+    double *lse;
+};
+
+__global__ void __launch_bounds__(256)
+hot_head_join_kernel(JoinArgs a)
+{
+    __shared__ float sm[3][256];
+    const int per = 256 / a.lanes, r = (int)threadIdx.x % per, lane = (int)threadIdx.x / per;
+    const long s = blockIdx.y, row = (long)blockIdx.x * per + r;
+    const int at = row < a.rows ? a.place_of[s * a.rows + row] : -1;
+    float most = -__builtin_inff(), sum = 0.0f, dot = 0.0f;
+    if (at >= 0)
+        for (int k = lane; k < a.tiles; k += a.lanes) {
+            const float *const p = a.partials + ((size_t)s * (size_t)a.tiles + (size_t)k) * 3 * (size_t)a.places + (size_t)at;
+            const float m = p[0], v = p[a.places], top = m > most || m != m ? m : most;
+            sum = top == -__builtin_inff() ? sum + v : sum * __builtin_amdgcn_exp2f(most - top) + v * __builtin_amdgcn_exp2f(m - top);
+            most = top;
+            dot += p[2 * a.places];
+        }
+    sm[0][threadIdx.x] = most;
+    sm[1][threadIdx.x] = sum;
+    sm[2][threadIdx.x] = dot;
+    __syncthreads();
+    if (lane || row >= a.rows) return;
+    float loss = 0.0f;
+    double lse = 0.0;
+    if (at >= 0) {
+        for (int k = 1; k < a.lanes; ++k) {
+            const float m = sm[0][k * per + r];
+            most = m > most || m != m ? m : most;
+        }
+        double total = 0.0, d = 0.0;
+        for (int k = 0; k < a.lanes; ++k) {
+            const float m = sm[0][k * per + r];
+            total += (double)sm[1][k * per + r] * (m == most ? 1.0 : exp2((double)m - (double)most));
+            d += (double)sm[2][k * per + r];
+        }
+        const double two = (double)most + log2(total);
+        lse = two * 0.69314718055994530942;
+        double entropy = 0.0, weight = 1.0;
+        if (a.sums) {
+            const long list = s * a.list_sample + row;
+            entropy = a.sums[2 * list];
+            weight = a.sums[2 * list + 1];
+        } else if (a.label[s * a.rows + at] < 0) entropy = (double)__builtin_nanf("");
+        loss = (float)(a.temperature * a.temperature * (entropy + weight * lse - d * 0.69314718055994530942));
+    }
+    a.loss[s * a.rows + row] = loss;
+    if (a.lse) a.lse[s * a.rows + row] = lse;
+}
+
+// --------------------------------------------------------------------------- gradients of features, weights and bias
+
+struct GradArgs {
+    const char *dz, *other;        // other: W (from word v_begin) or the packed features
+    long dz_pitch, dz_plane, dz_sample, pitch, plane, sample;
+    int width, vocab, v_begin, v_count;
+    long rows;
+    const int *count;
+    int samples, splits, split_depth;
+    bool first;                    // of the pieces: sums begin with it
+    float *sums;                   // dx: [split][sample][place][width]
+    void *out;                     // dW
+    long out_sample;
+    const float *scale;            // [samples, 2]
+    float temperature;
+};
+
+// dx's share of one piece of the vocabulary (and of one run of it): rows x width, contracted over words
+template <class TILE>
+__global__ void __launch_bounds__(TILE::THREADS)
+hot_head_dx_kernel(GradArgs a)
+{
+    __shared__ __attribute__((aligned(1024))) char memory[TILE::kLds];
+    const long s = blockIdx.y;
+    const int split = (int)blockIdx.z, count = a.count[s];
+    const Place at = place((int)blockIdx.x, (a.width + TILE::BN - 1) / TILE::BN, (count + TILE::BM - 1) / TILE::BM);
+    if (!at.any) return;
+    const int r0 = at.n * TILE::BM, k0 = at.m * TILE::BN, v = split * a.split_depth;
+    const int depth = a.v_count - v < a.split_depth ? a.v_count - v : a.split_depth;
+    f16v acc[TILE::MB][TILE::NB];
+    const Operand dz = {a.dz + (size_t)s * (size_t)a.dz_sample + (size_t)r0 * (size_t)a.dz_pitch + (size_t)v * 2, a.dz_pitch, a.dz_plane, count - r0, depth};
+    const Operand w = {a.other + (size_t)s * (size_t)a.sample + (size_t)v * (size_t)a.pitch + (size_t)k0 * 2, a.pitch, a.plane, a.width - k0, depth};
+    TILE::product((lds_char *)memory, dz, w, depth, acc);
+    float *const sums = a.sums + ((size_t)split * (size_t)a.samples + (size_t)s) * (size_t)a.rows * (size_t)a.width;
+#pragma unroll
+    for (int m = 0; m < TILE::MB; ++m)
+#pragma unroll
+        for (int n = 0; n < TILE::NB; ++n) {
+            const int k = k0 + TILE::n0() + 32 * n + (TILE::lane() & 31);
+            if (k >= a.width) continue;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int r = r0 + TILE::m0() + 32 * m + TILE::row(i);
+                if (r >= count) continue;
+                float *const p = sums + (size_t)r * (size_t)a.width + (size_t)k;
+                *p = a.first ? acc[m][n][i] : *p + acc[m][n][i];
+            }
+        }
+}
+
+// dW of one piece of the vocabulary: words x width, contracted over rows.  M = width, so that a lane's neighbouring results are
+// neighbours in memory; OUT: the type of W.
+template <class TILE, class OUT>
+__global__ void __launch_bounds__(TILE::THREADS)
+hot_head_dw_kernel(GradArgs a)
+{
+    constexpr int PITCH = TILE::BM * (int)sizeof(OUT) + 16, NEED = TILE::BN * PITCH;
+    __shared__ __attribute__((aligned(1024))) char memory[TILE::kLds > NEED ? TILE::kLds : NEED];
+    const long s = blockIdx.y;
+    const int count = a.count[s];
+    const Place at = place((int)blockIdx.x, (a.v_count + TILE::BN - 1) / TILE::BN, (a.width + TILE::BM - 1) / TILE::BM);
+    if (!at.any) return;
+    const int in = at.m * TILE::BN, k0 = at.n * TILE::BM;
+    f16v acc[TILE::MB][TILE::NB];
+    const Operand x = {a.other + (size_t)s * (size_t)a.sample + (size_t)k0 * 2, a.pitch, a.plane, a.width - k0, count};
+    const Operand dz = {a.dz + (size_t)s * (size_t)a.dz_sample + (size_t)in * 2, a.dz_pitch, a.dz_plane, a.v_count - in, count};
+    TILE::product((lds_char *)memory, x, dz, count, acc);
+    const float scale = a.scale[2 * s + 1] * a.temperature;
+    typedef OUT V4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int n = 0; n < TILE::NB; ++n)
+#pragma unroll
+        for (int m = 0; m < TILE::MB; ++m)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                V4 o;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[i] = (OUT)(acc[m][n][4 * q + i] * scale);
+                *reinterpret_cast<V4 *>(memory + (TILE::n0() + 32 * n + (TILE::lane() & 31)) * PITCH + (TILE::m0() + 32 * m + TILE::row(4 * q)) * (int)sizeof(OUT)) = o;
+            }
+    __syncthreads();
+    constexpr int N = Piece<OUT>::N, CHUNKS = TILE::BM / N;
+    OUT *const out = static_cast<OUT *>(a.out) + (size_t)s * (size_t)a.out_sample + (size_t)(a.v_begin + in) * (size_t)a.width;
+    for (int k = (int)threadIdx.x; k < TILE::BN * CHUNKS; k += TILE::THREADS) {
+        const int row = k / CHUNKS, col = k0 + k % CHUNKS * N;
+        if (in + row >= a.v_count || col >= a.width) continue;
+        OUT *const to = out + (size_t)row * (size_t)a.width;
+        const typename Piece<OUT>::V v = *reinterpret_cast<const typename Piece<OUT>::V *>(memory + row * PITCH + k % CHUNKS * 16);
+        if (col + N <= a.width) *reinterpret_cast<typename Piece<OUT>::Loose *>(to + col) = v;
+        else
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if (col + j < a.width) to[col + j] = v[j];
+    }
+}
+
+// db of one piece: sums of dz over the rows, 128 words and 16 runs of rows to a workgroup
+struct BiasArgs {
+    const char *dz;
+    long dz_pitch, dz_plane, dz_sample;
+    int v_begin, v_count;
+    const int *count;
+    const float *scale;
+    float temperature;
+    void *out;
+    long out_sample;
+    int type;
+};
+
+template <class T, int PIECES>
+__global__ void __launch_bounds__(256)
+hot_head_db_kernel(BiasArgs a)
+{
+    __shared__ float runs[16][128];
+    typedef T V8 __attribute__((ext_vector_type(8)));
+    const long s = blockIdx.y;
+    const int lane = (int)threadIdx.x & 15, run = (int)threadIdx.x >> 4, in = (int)blockIdx.x * 128 + lane * 8, count = a.count[s];
+    float sum[8] = {};
+    if (in < a.v_count)        // (rows of dz reach to the next multiple of 256 words)
+        for (int r = run; r < count; r += 16)
+#pragma unroll
+            for (int p = PIECES - 1; p >= 0; --p) {
+                const V8 v = *reinterpret_cast<const V8 *>(a.dz + (size_t)s * (size_t)a.dz_sample + (size_t)p * (size_t)a.dz_plane + (size_t)r * (size_t)a.dz_pitch + (size_t)in * 2);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum[j] += (float)v[j];
+            }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) runs[run][lane * 8 + j] = sum[j];
+    __syncthreads();
+    const int word = (int)blockIdx.x * 128 + (int)threadIdx.x;
+    if (threadIdx.x >= 128 || word >= a.v_count) return;
+    float total = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) total += runs[k][threadIdx.x];
+    store_as(a.out, a.type, s * a.out_sample + a.v_begin + word, total * (a.scale[2 * s + 1] * a.temperature));
+}
+
+struct FeatureArgs {
+    const float *sums;             // [split][sample][place][width]
+    const int *place_of;
+    const float *scale;
+    float temperature;
+    long rows, width;
+    int samples, splits;
+    bool shared;                   // all samples have the same features: their gradients are added
+    void *out;
+};
+
+template <class T>
+__global__ void __launch_bounds__(256)
+hot_head_features_kernel(FeatureArgs a)
+{
+    constexpr int N = Piece<T>::N;
+    const long chunks = (a.width + N - 1) / N, items = a.rows * chunks;
+    for (long item = (long)blockIdx.x * 256 + threadIdx.x; item < items; item += (long)gridDim.x * 256) {
+        const long row = item / chunks, col = (item - row * chunks) * N;
+        const long s0 = a.shared ? 0 : (long)blockIdx.y, s1 = a.shared ? a.samples : s0 + 1;
+        typename Piece<T>::F total = typename Piece<T>::F(0.0f);
+        for (long s = s0; s < s1; ++s) {
+            const int at = a.place_of[s * a.rows + row];
+            if (at < 0) continue;
+            typename Piece<T>::F sum = typename Piece<T>::F(0.0f);
+            for (int k = 0; k < a.splits; ++k) {
+                const float *const p = a.sums + (((size_t)k * (size_t)a.samples + (size_t)s) * (size_t)a.rows + (size_t)at) * (size_t)a.width;
+#pragma unroll
+                for (int h = 0; h < N; h += 4) {
+                    const Piece<float>::F v = Piece<float>::load(p, col + h, a.width);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) sum[h + j] += v[j];
+                }
+            }
+            total += sum * (a.scale[2 * s + 1] * a.temperature);
+        }
+        Piece<T>::store(static_cast<T *>(a.out) + ((size_t)s0 * (size_t)a.rows + (size_t)row) * (size_t)a.width, col, a.width, total);
+    }
+}
+
+__global__ void __launch_bounds__(256) hot_head_zero_kernel(char *p, long bytes)
+{
+    for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < bytes; i += (long)gridDim.x * 256) p[i] = 0;
+}
+
+// ---------------------------------------------------------------------------------
+// Host side.
+
+constexpr long kMostTiles = 1L << 22;                    // of 256 x 256 logits (one grid dimension holds fewer than 2^32 threads)
+constexpr int64_t kPieceBytes = (int64_t)256 << 20;      // of dz and packed weights: what the memory-side cache holds
+
+struct HeadPlan {
+    int pieces;              // of an element
+    bool pack_w;
+    int chunks;              // 16-byte chunks of a packed row
+    long places;
+    int v_piece, v_pieces;   // words of a piece
+    int size;                // 0: tiles for few rows, 1: 128 x 128, 2: large ones
+    int v_tile;              // words of a tile of logits
+    int splits, split_depth;
+    // where things lie in the workspace
+    int64_t word, weight, list_count, sums, start, count, row_of, place_of, label, hi, lo, grad, scale, x, w, dz, partials, dx, bytes;
+};
+
+struct Layout {
+    int64_t at = 0;
+    int64_t take(int64_t bytes)
+    {
+        const int64_t here = at;
+        at += (bytes + 255) / 256 * 256;
+        return here;
+    }
+};
+
+bool head_ok(const hot_head_desc *d)
+{
+    if (!d || d->rows < 0 || d->rows > (1L << 22) || d->width < 1 || d->width > (1L << 19) || d->vocab < 1 || d->vocab > (1L << 24) || d->samples < 1 || d->samples > 4096 ||
+        !known_type(d->dtype) || d->ldx < 0 || d->x_sample < 0 || d->ldw < d->width || d->w_sample < 0 || d->bias_sample < 0 || d->index_row < 0 || d->index_sample < 0)
+        return false;
+    if (d->samples > 1 && (d->w_sample < (d->vocab - 1) * d->ldw + d->width || (d->bias_sample != 0 && d->bias_sample < d->vocab))) return false;
+    if (d->top < 0 || d->top > kMostTop || d->samples * d->rows > (1L << 30)) return false;
+    if (d->top > 0 && (!known_type(d->logit_dtype) || d->logit_row < 0 || d->logit_sample < 0)) return false;
+    if (up(d->rows, 256) / 256 * (up(d->vocab, 256) / 256) > kMostTiles) return false;
+    if (!(d->temperature > 0.0) || !(d->temperature <= 1e4) || !(d->temperature >= 1e-4) || (d->top == 0 && d->temperature != 1.0)) return false;
+    return true;
+}
+
+HeadPlan head_plan(const hot_head_desc &d, bool backward, bool with_dx)
+{
+    HeadPlan p = {};
+    const long S = d.samples, R = d.rows, V = d.vocab, K = d.width;
+    p.pieces = d.dtype == HOT_F32 ? 3 : 1;
+    p.pack_w = p.pieces == 3 || !d.w_aligned || K % 8 || d.ldw % 8 || (S > 1 && d.w_sample % 8) || d.ldw > (1L << 21);
+    p.chunks = (int)((K + 7) / 8);
+    p.places = up(R, 256);
+    // Tiles of 256 x 256 (256 x 128 in three pieces) where they fill the chip, of 128 x 128 below, of 256 x 32 for up to 32 rows.
+    const long large = ((V + 255) / 256) * ((R + 255) / 256) * S;
+    p.size = R <= 32 ? 0 : (large >= kComputeUnits ? 2 : 1);
+    p.v_tile = p.size == 1 ? 128 : 256;
+    long piece = up(V, 256);
+    if (backward || p.pack_w) {
+        const int64_t per_word = S * ((backward ? p.places * 2 * p.pieces : 0) + (p.pack_w ? p.chunks * 16L * p.pieces : 0));
+        const long most = kPieceBytes / per_word / 256 * 256;
+        const long least = 1024;
+        const long n = (piece + (most > least ? most : least) - 1) / (most > least ? most : least);
+        piece = up((V + n - 1) / n, 256);
+    }
+    p.v_piece = (int)piece;
+    p.v_pieces = (int)((V + piece - 1) / piece);
+    // the features' gradients of few tiles: several workgroups share the words of a piece
+    const int bm = p.size == 0 ? 32 : (p.size == 1 || p.pieces == 3 ? 128 : 256), bn = p.size == 1 ? 128 : 256;
+    const long tiles = ((R + bm - 1) / bm) * ((K + bn - 1) / bn) * S;
+    long splits = (2 * kComputeUnits + tiles - 1) / tiles, most_splits = piece / 256;
+    if (tiles >= kComputeUnits) splits = 1;
+    splits = splits < 1 ? 1 : (splits > most_splits ? most_splits : splits);
+    if (splits > 64) splits = 64;
+    p.split_depth = (int)up((piece + splits - 1) / splits, 64);
+    p.splits = (int)((piece + p.split_depth - 1) / p.split_depth);
+
+    Layout l;
+    const long lists = d.top > 0 ? (d.index_sample > 0 || d.logit_sample > 0 ? S : 1) * R : 0, marks = (V + kStartStep - 1) / kStartStep;
+    p.word = l.take(lists * d.top * 4);
+    p.weight = l.take(lists * d.top * 4);
+    p.list_count = l.take(lists * 4);
+    p.sums = l.take(lists * 16);
+    p.start = l.take(lists * (marks + 1) * 2);
+    p.count = l.take(S * 4);
+    p.row_of = l.take(S * R * 4);
+    p.place_of = l.take(S * R * 4);
+    p.label = l.take(d.top > 0 ? 0 : S * R * 4);
+    if (backward) {
+        p.hi = l.take(S * R * 4);
+        p.lo = l.take(S * R * 4);
+        p.grad = l.take(S * R * 4);
+        p.scale = l.take(S * 8);
+    }
+    p.x = l.take(S * p.places * p.chunks * 16 * p.pieces);
+    p.w = l.take(p.pack_w ? S * piece * p.chunks * 16 * p.pieces : 0);
+    if (backward) {
+        p.dz = l.take(S * p.places * piece * 2 * p.pieces);
+        if (with_dx) p.dx = l.take((int64_t)p.splits * S * R * K * 4);
+    } else {
+        p.partials = l.take(S * ((V + p.v_tile - 1) / p.v_tile) * 3 * p.places * 4);
+    }
+    p.bytes = l.at;
+    return p;
+}
+
+struct HeadCall {
+    const hot_head_desc &d;
+    const HeadPlan &p;
+    char *ws;
+    hipStream_t stream;
+    const void *x, *w, *bias;
+    const int64_t *index;
+    const void *logit;
+    long list_sample;
+
+    template <class V>
+    V *in(int64_t at) const { return reinterpret_cast<V *>(ws + at); }
+};
+
+unsigned grid_for(long items, long most = 8192)
+{
+    const long n = (items + 255) / 256;
+    return (unsigned)(n < 1 ? 1 : (n < most ? n : most));
+}
+
+void head_rows(const HeadCall &c, const double *lse, const float *g, long g_sample, long g_row)
+{
+    const hot_head_desc &d = c.d;
+    const HeadPlan &p = c.p;
+    if (d.top > 0) {
+        ListArgs a;
+        a.rows = d.rows;
+        a.lists = d.rows * (c.list_sample > 0 ? d.samples : 1);
+        a.idx_sample = d.index_sample;
+        a.idx_row = d.index_row;
+        a.logit_sample = d.logit_sample;
+        a.logit_row = d.logit_row;
+        a.top = (int)d.top;
+        a.logit_type = d.logit_dtype;
+        a.marks = (int)((d.vocab + kStartStep - 1) / kStartStep);
+        a.vocab = d.vocab;
+        a.inv_temperature = (float)(1.0 / d.temperature);
+        a.index = c.index;
+        a.logit = c.logit;
+        a.word = c.in<int>(p.word);
+        a.weight = c.in<float>(p.weight);
+        a.count = c.in<int>(p.list_count);
+        a.sums = c.in<double>(p.sums);
+        a.start = c.in<unsigned short>(p.start);
+        hot_head_lists_kernel<<<dim3((unsigned)((a.lists + kListWaves - 1) / kListWaves)), 64 * kListWaves, 0, c.stream>>>(a);
+    }
+    RowArgs a = {};
+    a.rows = d.rows;
+    a.vocab = d.vocab;
+    a.idx_sample = d.index_sample;
+    a.idx_row = d.index_row;
+    a.ignore = d.ignore_index;
+    a.index = c.index;
+    a.list_count = d.top > 0 ? c.in<int>(p.list_count) : nullptr;
+    a.list_sample = c.list_sample;
+    a.lse = lse;
+    a.g = g;
+    a.g_sample = g_sample;
+    a.g_row = g_row;
+    a.scale_to = d.dtype == HOT_F16 ? kHalfScale : 1.0f;
+    a.count = c.in<int>(p.count);
+    a.row_of = c.in<int>(p.row_of);
+    a.place_of = c.in<int>(p.place_of);
+    a.label = d.top > 0 ? nullptr : c.in<int>(p.label);
+    a.hi = c.in<float>(p.hi);
+    a.lo = c.in<float>(p.lo);
+    a.grad = c.in<float>(p.grad);
+    a.scale = c.in<float>(p.scale);
+    hot_head_rows_kernel<<<dim3((unsigned)d.samples), kRowBlock, 0, c.stream>>>(a);
+}
+
+template <class T>
+void head_pack_x(const HeadCall &c)
+{
+    PackArgs a;
+    a.from = c.x;
+    a.from_row = c.d.ldx;
+    a.from_sample = c.d.x_sample;
+    a.row_of = c.in<int>(c.p.row_of);
+    a.count = c.in<int>(c.p.count);
+    a.rows = c.d.rows;
+    a.map_sample = c.d.rows;
+    a.width = (int)c.d.width;
+    a.chunks = c.p.chunks;
+    a.to = c.in<char>(c.p.x);
+    a.to_sample = c.p.places * c.p.chunks * 16L;
+    a.plane = c.d.samples * a.to_sample;
+    hot_head_pack_kernel<T><<<dim3(grid_for(c.d.rows * a.chunks), (unsigned)c.d.samples), 256, 0, c.stream>>>(a);
+}
+
+template <class T>
+void head_pack_w(const HeadCall &c, long v_begin, long v_count)
+{
+    PackArgs a = {};
+    a.from = static_cast<const T *>(c.w) + (size_t)v_begin * (size_t)c.d.ldw;
+    a.from_row = c.d.ldw;
+    a.from_sample = c.d.w_sample;
+    a.rows = v_count;
+    a.width = (int)c.d.width;
+    a.chunks = c.p.chunks;
+    a.to = c.in<char>(c.p.w);
+    a.to_sample = c.p.v_piece * (long)c.p.chunks * 16L;
+    a.plane = c.d.samples * a.to_sample;
+    hot_head_pack_kernel<T><<<dim3(grid_for(v_count * a.chunks), (unsigned)c.d.samples), 256, 0, c.stream>>>(a);
+}
+
+// the weights' part of a kernel's arguments: as they lie, or packed
+struct Weights {
+    const char *at;
+    long pitch, plane, sample;
+};
+
+Weights head_weights(const HeadCall &c, long v_begin)
+{
+    if (!c.p.pack_w) return {static_cast<const char *>(c.w) + (size_t)v_begin * (size_t)c.d.ldw * 2, c.d.ldw * 2, 0, c.d.w_sample * 2};
+    const long sample = c.p.v_piece * (long)c.p.chunks * 16L;
+    return {c.in<char>(c.p.w), c.p.chunks * 16L, c.d.samples * sample, sample};
+}
+
+HeadArgs head_args(const HeadCall &c, long v_begin, long v_count)
+{
+    const hot_head_desc &d = c.d;
+    const HeadPlan &p = c.p;
+    HeadArgs a = {};
+    const Weights w = head_weights(c, v_begin);
+    a.w = w.at;
+    a.w_pitch = w.pitch;
+    a.w_plane = w.plane;
+    a.w_sample = w.sample;
+    a.x = c.in<char>(p.x);
+    a.x_pitch = p.chunks * 16L;
+    a.x_sample = p.places * a.x_pitch;
+    a.x_plane = d.samples * a.x_sample;
+    a.width = (int)d.width;
+    a.vocab = (int)d.vocab;
+    a.v_begin = (int)v_begin;
+    a.v_count = (int)v_count;
+    a.rows = d.rows;
+    a.places = p.places;
+    a.count = c.in<int>(p.count);
+    a.row_of = c.in<int>(p.row_of);
+    a.label = c.in<int>(p.label);
+    a.bias = c.bias;
+    a.bias_sample = d.bias_sample;
+    a.bias_type = d.dtype;
+    a.scale = (float)(1.44269504088896340736 / d.temperature);
+    a.word = c.in<int>(p.word);
+    a.weight = c.in<float>(p.weight);
+    a.start = c.in<unsigned short>(p.start);
+    a.top = (int)d.top;
+    a.marks = (int)((d.vocab + kStartStep - 1) / kStartStep);
+    a.list_sample = c.list_sample;
+    a.partials = c.in<float>(p.partials);
+    a.v_tiles = (int)((d.vocab + p.v_tile - 1) / p.v_tile);
+    a.hi = c.in<float>(p.hi);
+    a.lo = c.in<float>(p.lo);
+    a.grad = c.in<float>(p.grad);
+    a.to_scale = c.in<float>(p.scale);
+    a.dz = c.in<char>(p.dz);
+    a.dz_pitch = p.v_piece * 2L;
+    a.dz_sample = p.places * a.dz_pitch;
+    a.dz_plane = d.samples * a.dz_sample;
+    return a;
+}
+
+template <class TILE>
+void head_logits(const HeadCall &c, const HeadArgs &a, bool backward)
+{
+    const dim3 grid((unsigned)place_blocks((a.v_count + TILE::BM - 1) / TILE::BM, (c.d.rows + TILE::BN - 1) / TILE::BN), (unsigned)c.d.samples), block(TILE::THREADS);
+    if (c.d.top > 0) {
+        if (backward) hot_head_dz_kernel<TILE, true><<<grid, block, 0, c.stream>>>(a);
+        else hot_head_forward_kernel<TILE, true><<<grid, block, 0, c.stream>>>(a);
+    } else {
+        if (backward) hot_head_dz_kernel<TILE, false><<<grid, block, 0, c.stream>>>(a);
+        else hot_head_forward_kernel<TILE, false><<<grid, block, 0, c.stream>>>(a);
+    }
+}
+
+template <class T, int PIECES>
+void head_logits(const HeadCall &c, const HeadArgs &a, bool backward)
+{
+    if (c.p.size == 0) head_logits<Tile<T, PIECES, true, true, 256, 32, 8, 1>>(c, a, backward);
+    else if (c.p.size == 1) head_logits<Tile<T, PIECES, true, true, 128, 128, 2, 2>>(c, a, backward);
+    else if constexpr (PIECES == 1) head_logits<Tile<T, PIECES, true, true, 256, 256, 2, 4>>(c, a, backward);
+    else head_logits<Tile<T, PIECES, true, true, 256, 128, 4, 2>>(c, a, backward);
+}
+
+template <class TILE>
+void head_dx(const HeadCall &c, const GradArgs &a)
+{
+    hot_head_dx_kernel<TILE><<<dim3((unsigned)place_blocks((c.d.width + TILE::BN - 1) / TILE::BN, (c.d.rows + TILE::BM - 1) / TILE::BM), (unsigned)c.d.samples, (unsigned)a.splits),
+                               TILE::THREADS, 0, c.stream>>>(a);
+}
+
+template <class TILE, class OUT>
+void head_dw(const HeadCall &c, const GradArgs &a)
+{
+    hot_head_dw_kernel<TILE, OUT><<<dim3((unsigned)place_blocks((a.v_count + TILE::BN - 1) / TILE::BN, (c.d.width + TILE::BM - 1) / TILE::BM), (unsigned)c.d.samples),
+                                    TILE::THREADS, 0, c.stream>>>(a);
+}
+
+// T: the type of the tensors; E: of the tiles' elements
+template <class T, class E, int PIECES>
+void head_forward(const HeadCall &c, float *loss, double *lse)
+{
+    head_rows(c, nullptr, nullptr, 0, 0);
+    head_pack_x<T>(c);
+    for (long v = 0; v < c.d.vocab; v += c.p.v_piece) {
+        const long n = c.d.vocab - v < c.p.v_piece ? c.d.vocab - v : c.p.v_piece;
+        if (c.p.pack_w) head_pack_w<T>(c, v, n);
+        head_logits<E, PIECES>(c, head_args(c, v, n), false);
+    }
+    JoinArgs a;
+    a.rows = c.d.rows;
+    a.places = c.p.places;
+    a.tiles = (int)((c.d.vocab + c.p.v_tile - 1) / c.p.v_tile);
+    a.lanes = 4;
+    while (a.lanes < 256 && (c.d.rows + 256 / a.lanes - 1) / (256 / a.lanes) * c.d.samples < kComputeUnits && a.lanes * 4 < a.tiles) a.lanes *= 2;
+    a.partials = c.in<float>(c.p.partials);
+    a.place_of = c.in<int>(c.p.place_of);
+    a.label = c.in<int>(c.p.label);
+    a.sums = c.d.top > 0 ? c.in<double>(c.p.sums) : nullptr;
+    a.list_sample = c.list_sample;
+    a.temperature = c.d.temperature;
+    a.loss = loss;
+    a.lse = lse;
+    hot_head_join_kernel<<<dim3((unsigned)((c.d.rows + 256 / a.lanes - 1) / (256 / a.lanes)), (unsigned)c.d.samples), 256, 0, c.stream>>>(a);
+}
+
+template <class T, class E, int PIECES>
+void head_backward(const HeadCall &c, const double *lse, const float *g, long g_sample, long g_row, void *dx, void *dw, void *db)
+{
+    head_rows(c, lse, g, g_sample, g_row);
+    head_pack_x<T>(c);
+    const float *const scale = c.in<float>(c.p.scale);
+    for (long v = 0; v < c.d.vocab; v += c.p.v_piece) {
+        const long n = c.d.vocab - v < c.p.v_piece ? c.d.vocab - v : c.p.v_piece;
+        if (c.p.pack_w) head_pack_w<T>(c, v, n);
+        const HeadArgs h = head_args(c, v, n);
+        head_logits<E, PIECES>(c, h, true);
+        GradArgs a = {};
+        a.dz = h.dz;
+        a.dz_pitch = h.dz_pitch;
+        a.dz_plane = h.dz_plane;
+        a.dz_sample = h.dz_sample;
+        a.width = h.width;
+        a.vocab = h.vocab;
+        a.v_begin = h.v_begin;
+        a.v_count = h.v_count;
+        a.rows = h.rows;
+        a.count = h.count;
+        a.samples = c.d.samples;
+        a.splits = c.p.splits;
+        a.split_depth = c.p.split_depth;
+        a.first = v == 0;
+        a.sums = c.in<float>(c.p.dx);
+        a.scale = scale;
+        a.temperature = (float)c.d.temperature;
+        if (dx) {
+            a.other = h.w;
+            a.pitch = h.w_pitch;
+            a.plane = h.w_plane;
+            a.sample = h.w_sample;
+            if (c.p.size == 0) head_dx<Tile<E, PIECES, true, false, 32, 256, 1, 8>>(c, a);
+            else if (c.p.size == 1) head_dx<Tile<E, PIECES, true, false, 128, 128, 2, 2>>(c, a);
+            else if constexpr (PIECES == 1) head_dx<Tile<E, PIECES, true, false, 256, 256, 2, 4>>(c, a);
+            else head_dx<Tile<E, PIECES, true, false, 128, 256, 2, 4>>(c, a);
+        }
+        if (dw) {
+            a.other = h.x;
+            a.pitch = h.x_pitch;
+            a.plane = h.x_plane;
+            a.sample = h.x_sample;
+            a.out = dw;
+            a.out_sample = c.d.vocab * c.d.width;
+            if (c.p.size < 2) head_dw<Tile<E, PIECES, false, false, 128, 128, 2, 2>, T>(c, a);
+            else if constexpr (PIECES == 1) head_dw<Tile<E, PIECES, false, false, 256, 256, 2, 4>, T>(c, a);
+            else head_dw<Tile<E, PIECES, false, false, 256, 128, 4, 2>, T>(c, a);
+        }
+        if (db) {
+            const BiasArgs b = {h.dz, h.dz_pitch, h.dz_plane, h.dz_sample, h.v_begin, h.v_count, h.count, scale, a.temperature, db, c.d.vocab, c.d.dtype};
+            hot_head_db_kernel<E, PIECES><<<dim3((unsigned)((n + 127) / 128), (unsigned)c.d.samples), 256, 0, c.stream>>>(b);
+        }
+    }
+    if (dx) {
+        FeatureArgs a;
+        a.sums = c.in<float>(c.p.dx);
+        a.place_of = c.in<int>(c.p.place_of);
+        a.scale = scale;
+        a.temperature = (float)c.d.temperature;
+        a.rows = c.d.rows;
+        a.width = c.d.width;
+        a.samples = c.d.samples;
+        a.splits = (int)((c.p.v_piece + c.p.split_depth - 1) / c.p.split_depth);
+        a.shared = c.d.samples > 1 && c.d.x_sample == 0;
+        a.out = dx;
+        hot_head_features_kernel<T><<<dim3(grid_for(c.d.rows * ((c.d.width + Piece<T>::N - 1) / Piece<T>::N)), a.shared ? 1u : (unsigned)c.d.samples), 256, 0, c.stream>>>(a);
+    }
+}
+
+bool head_inputs_ok(const hot_head_desc &d, const void *x, const void *w, const void *bias, const int64_t *index, const void *logit)
+{
+    if (!w || !on_element(w, d.dtype) || !on_element(bias, d.dtype)) return false;
+    if (bias && d.samples > 1 && d.bias_sample == 0) return false;
+    if (d.w_aligned && !aligned16(w)) return false;
+    if (d.rows == 0) return true;
+    if (!x || !on_element(x, d.dtype) || !index || (reinterpret_cast<uintptr_t>(index) & 7u)) return false;
+    if (d.top > 0 && (!logit || !on_element(logit, d.logit_dtype))) return false;
+    return true;
+}
+
+HeadCall head_call(const hot_head_desc &d, const HeadPlan &p, const void *x, const void *w, const void *bias, const int64_t *index, const void *logit, void *workspace,
+                   void *stream)
+{
+    return {d, p, static_cast<char *>(workspace), static_cast<hipStream_t>(stream), x, w, bias, index, logit, d.index_sample > 0 || d.logit_sample > 0 ? d.rows : 0};
+}
+
+bool workspace_ok(const HeadPlan &p, const void *workspace, int64_t bytes) { return workspace && aligned16(workspace) && bytes >= p.bytes; }
+
+}  // namespace
+
+extern "C" {
+
+int64_t hot_head_workspace_bytes(const hot_head_desc *desc, int which)
+{
+    if (!head_ok(desc) || which < 0 || which > 2) return HOT_EINVAL;
+    if (desc->rows == 0) return 0;
+    return head_plan(*desc, which > 0, which == 1).bytes;
+}
+
+int hot_head_forward(const hot_head_desc *desc, const void *x, const void *weight, const void *bias, const int64_t *index, const void *logit, float *loss,
+                     double *lse, void *workspace, int64_t workspace_bytes, void *stream)
+{
+    if (!head_ok(desc) || !head_inputs_ok(*desc, x, weight, bias, index, logit)) return HOT_EINVAL;
+    if (desc->rows == 0) return HOT_OK;
+    const HeadPlan p = head_plan(*desc, false, false);
+    if (!loss || !aligned4(loss) || (reinterpret_cast<uintptr_t>(lse) & 7u) || !workspace_ok(p, workspace, workspace_bytes)) return HOT_EINVAL;
+    const HeadCall c = head_call(*desc, p, x, weight, bias, index, logit, workspace, stream);
+    if (desc->dtype == HOT_F32) head_forward<float, __bf16, 3>(c, loss, lse);
+    else if (desc->dtype == HOT_BF16) head_forward<__bf16, __bf16, 1>(c, loss, lse);
+    else head_forward<_Float16, _Float16, 1>(c, loss, lse);
+    return hot_detail::note_hip(hipGetLastError());
+}
+
+int hot_head_backward(const hot_head_desc *desc, const void *x, const void *weight, const void *bias, const int64_t *index, const void *logit,
+                      const double *lse, const float *grad_loss, int64_t grad_sample, int64_t grad_row, void *dx, void *grad_weight, void *grad_bias,
+                      void *workspace, int64_t workspace_bytes, void *stream)
+{
+    if (!head_ok(desc) || !head_inputs_ok(*desc, x, weight, bias, index, logit) || grad_sample < 0 || grad_row < 0) return HOT_EINVAL;
+    if (!on_element(dx, desc->dtype) || !on_element(grad_weight, desc->dtype) || !on_element(grad_bias, desc->dtype)) return HOT_EINVAL;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (desc->rows == 0) {        // sums over no rows
+        const int64_t words = desc->samples * desc->vocab, size = type_bytes(desc->dtype);
+        if (grad_weight) hot_head_zero_kernel<<<grid_for(words * desc->width * size), 256, 0, s>>>(static_cast<char *>(grad_weight), words * desc->width * size);
+        if (grad_bias) hot_head_zero_kernel<<<grid_for(words * size), 256, 0, s>>>(static_cast<char *>(grad_bias), words * size);
+        return hot_detail::note_hip(hipGetLastError());
+    }
+    if (!dx && !grad_weight && !grad_bias) return HOT_OK;
+    const HeadPlan p = head_plan(*desc, true, dx != nullptr);
+    if (!lse || (reinterpret_cast<uintptr_t>(lse) & 7u) || !grad_loss || !aligned4(grad_loss) || !workspace_ok(p, workspace, workspace_bytes)) return HOT_EINVAL;
+    const HeadCall c = head_call(*desc, p, x, weight, bias, index, logit, workspace, stream);
+    if (desc->dtype == HOT_F32) head_backward<float, __bf16, 3>(c, lse, grad_loss, grad_sample, grad_row, dx, grad_weight, grad_bias);
+    else if (desc->dtype == HOT_BF16) head_backward<__bf16, __bf16, 1>(c, lse, grad_loss, grad_sample, grad_row, dx, grad_weight, grad_bias);
+    else head_backward<_Float16, _Float16, 1>(c, lse, grad_loss, grad_sample, grad_row, dx, grad_weight, grad_bias);
+    return hot_detail::note_hip(hipGetLastError());
+}
+
+}  // extern "C"

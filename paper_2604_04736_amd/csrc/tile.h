@@ -1,0 +1,228 @@
+// Tiles of a matrix product on the 16-bit matrix instruction, for the kernels of head.hip: BM x BN results of a workgroup, both
+// operands staged through LDS straight from memory, sixteen bytes a lane, while the tile before is multiplied.
+//
+// An operand lies in memory with its contraction index running along its rows (ALONG: weights and features for the logits, their gradients
+// for the features' gradients) or across them (weights for the features' gradients, features and the logits' gradients for the weights').
+// Along, a lane's eight contraction indices are one 16-byte read of LDS; across, two transposing reads, so no operand is ever
+// transposed in memory.  Sixteen-byte pieces of LDS are permuted so that neither form of reading meets its own banks.
+// PIECES = 3: float32 operands as three bf16 pieces each (planes of equal layout), multiplied as the six products that carry 24 bits, from the
+// smallest on; PIECES = 1: bf16 and fp16 operands as they are.
+#ifndef HOT_TILE_H
+#define HOT_TILE_H
+
+#include <hip/hip_runtime.h>
+
+namespace {
+
+typedef short s4v __attribute__((ext_vector_type(4)));
+typedef short s8v __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f16v __attribute__((ext_vector_type(16)));
+typedef __attribute__((address_space(3))) char lds_char;
+typedef __attribute__((address_space(3))) s4v lds_s4v;
+typedef __attribute__((address_space(3))) s8v lds_s8v;
+
+constexpr unsigned kBeyond = 0x80000000u;        // an offset outside every window: such lanes receive zeros
+
+// The wait states between a run of matrix instructions and the first read of their results: 32, which the scheduler may not move
+// (the compiler's own can be missing where a branch lies between).  Accumulators hand their registers out only against one of these.
+struct TileSettled {
+    __device__ __forceinline__ TileSettled()
+    {
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    TileSettled(const TileSettled &) = delete;
+    TileSettled &operator=(const TileSettled &) = delete;
+};
+
+// 32 x 32 results, sixteen to a lane, over sixteen contraction indices an instruction
+template <class T>
+class TileAcc {
+    f16v v_;
+
+public:
+    __device__ __forceinline__ TileAcc() : v_(0.0f) {}
+    __device__ __forceinline__ void mac(s8v a, s8v b)
+    {
+        if constexpr (__is_same(T, _Float16)) v_ = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), v_, 0, 0, 0);
+        else v_ = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), v_, 0, 0, 0);
+    }
+    __device__ __forceinline__ f16v read(const TileSettled &) const { return v_; }
+};
+
+// One operand's part of a tile: T of its rows or columns ("lines": what is not contracted) from `at` on.
+struct Operand {
+    const char *at;      // first line, first contraction index
+    long pitch;          // bytes between rows in memory
+    long plane;          // bytes between pieces
+    int lines;           // how many lines there are; the tile's others are zeros
+    int depth;           // how many contraction indices there are; the others are zeros
+};
+
+// Lines and indices are taken eight at a time along memory: a row may be read up to the next multiple of eight, and must be finite there or
+// meet zeros of the other operand.
+template <int T, int BK, bool ALONG, int PIECES, int WAVES>
+struct Stage {
+    static constexpr int kBytes = T * BK * 2;                              // of one piece
+    static constexpr int kPerRow = (ALONG ? BK : T) * 2 / 16;              // 16-byte chunks in a row of LDS
+    static constexpr int kRows = 64 / kPerRow;                             // rows that one instruction of a wave fills
+    static constexpr int kLoads = kBytes / 1024, kEach = (kLoads + WAVES - 1) / WAVES;
+    static_assert(kPerRow <= 64 && kBytes % 1024 == 0 && (ALONG || T >= 128), "");
+
+    unsigned off[kEach];
+    int index[ALONG ? 1 : kEach];          // the contraction index of this lane's loads in a tile
+    int wave;
+
+    static __device__ __forceinline__ int permuted(int row)
+    {
+        if constexpr (!ALONG) return (row & 3) << 1;
+        else if constexpr (BK == 64) return row & 7;
+        else return row >> 1 & 3;
+    }
+
+    __device__ __forceinline__ Stage(const Operand &o, int wave_, int lane) : wave(wave_)
+    {
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const int row = (wave + j * WAVES) * kRows + lane / kPerRow, chunk = lane % kPerRow ^ permuted(row);
+            const int line = ALONG ? row : chunk * 8;
+            off[j] = line < o.lines ? (unsigned)(row * o.pitch + chunk * 16) : kBeyond;
+            if constexpr (ALONG) index[0] = chunk * 8;
+            else index[j] = row;
+        }
+    }
+
+    // sends for the tile that begins at contraction index k0
+    __device__ __forceinline__ void ask(const Operand &o, int k0, lds_char *to) const
+    {
+        const int left = o.depth - k0;
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) {
+            const char *const from = o.at + p * o.plane + (ALONG ? (long)k0 * 2 : (long)k0 * o.pitch);
+            const __amdgpu_buffer_rsrc_t win = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(from), 0, (int)kBeyond, 0x00020000);
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) {
+                if (kLoads % WAVES != 0 && wave + j * WAVES >= kLoads) break;
+                const unsigned at = index[ALONG ? 0 : j] < left ? off[j] : kBeyond;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(win, (__attribute__((address_space(3))) void *)(to + p * kBytes + (wave + j * WAVES) * 1024), 16, (int)at, 0, 0, 0);
+            }
+        }
+    }
+};
+
+// Lane l's operand of the matrix instruction: line l % 32 of a block of 32, contraction indices 8 (l / 32) .. + 7 of sixteen.
+template <int T, int BK, bool ALONG>
+__device__ __forceinline__ s8v fragment(const lds_char *tile, int line0, int ks, int lane)
+{
+    const int half = lane >> 5;
+    if constexpr (ALONG) {
+        const int row = line0 + (lane & 31), chunk = ks * 2 + half;
+        return *(const lds_s8v *)(tile + row * (BK * 2) + ((chunk ^ (BK == 64 ? row & 7 : row >> 1 & 3)) << 4));
+    } else {
+        const int i = lane & 15, row = ks * 16 + half * 8 + (i >> 2);
+        const int byte = (line0 + (lane & 16) + (i & 3) * 4) * 2 ^ (i >> 2) << 5;
+        const s4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v *)(tile + row * (T * 2) + byte));
+        const s4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v *)(tile + (row + 4) * (T * 2) + byte));
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+}
+
+template <class T_, int PIECES_, bool A_ALONG_, bool B_ALONG_, int BM_, int BN_, int WAVES_M_, int WAVES_N_>
+struct Tile {
+    typedef T_ T;
+    static constexpr int PIECES = PIECES_, BM = BM_, BN = BN_, WAVES_M = WAVES_M_, WAVES_N = WAVES_N_;
+    static constexpr bool A_ALONG = A_ALONG_, B_ALONG = B_ALONG_;
+    static constexpr int BK = PIECES == 1 ? 64 : 32;
+    static constexpr int WAVES = WAVES_M * WAVES_N, THREADS = 64 * WAVES, WM = BM / WAVES_M, WN = BN / WAVES_N, MB = WM / 32, NB = WN / 32;
+    typedef Stage<BM, BK, A_ALONG, PIECES, WAVES> StageA;
+    typedef Stage<BN, BK, B_ALONG, PIECES, WAVES> StageB;
+    static constexpr int kA = PIECES * StageA::kBytes, kStage = kA + PIECES * StageB::kBytes, kLds = 2 * kStage;
+
+    static __device__ __forceinline__ int lane() { return (int)threadIdx.x & 63; }
+    static __device__ __forceinline__ int wave() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }
+    // where this wave's results begin, and the row within a block of 32 x 32 of result i of a lane (its column is lane % 32)
+    static __device__ __forceinline__ int m0() { return wave() / WAVES_N * WM; }
+    static __device__ __forceinline__ int n0() { return wave() % WAVES_N * WN; }
+    static __device__ __forceinline__ int row(int i) { return 8 * (i >> 2) + 4 * (lane() >> 5) + (i & 3); }
+
+    // everything sent for has come, to all waves
+    static __device__ __forceinline__ void arrive() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+    // results = A B over `depth` contraction indices; LDS is free when it returns
+    static __device__ __forceinline__ void product(lds_char *lds, const Operand &a, const Operand &b, int depth, f16v (&results)[MB][NB])
+    {
+        const int l = lane(), w = wave();
+        const StageA sa(a, w, l);
+        const StageB sb(b, w, l);
+        TileAcc<T> acc[MB][NB];
+        if (depth > 0) {
+            sa.ask(a, 0, lds);
+            sb.ask(b, 0, lds + kA);
+        }
+        arrive();
+        int now = 0;
+        for (int k0 = 0; k0 < depth; k0 += BK) {
+            lds_char *const here = lds + now * kStage, *const next = lds + (now ^ 1) * kStage;
+            if (k0 + BK < depth) {
+                sa.ask(a, k0 + BK, next);
+                sb.ask(b, k0 + BK, next + kA);
+            }
+#pragma unroll
+            for (int ks = 0; ks < BK / 16; ++ks) {
+                s8v fa[PIECES][MB], fb[PIECES][NB];
+#pragma unroll
+                for (int p = 0; p < PIECES; ++p) {
+#pragma unroll
+                    for (int m = 0; m < MB; ++m) fa[p][m] = fragment<BM, BK, A_ALONG>(here + p * StageA::kBytes, m0() + 32 * m, ks, l);
+#pragma unroll
+                    for (int n = 0; n < NB; ++n) fb[p][n] = fragment<BN, BK, B_ALONG>(here + kA + p * StageB::kBytes, n0() + 32 * n, ks, l);
+                }
+                if constexpr (PIECES == 1) {
+#pragma unroll
+                    for (int m = 0; m < MB; ++m)
+#pragma unroll
+                        for (int n = 0; n < NB; ++n) acc[m][n].mac(fa[0][m], fb[0][n]);
+                } else {
+                    constexpr int PA[6] = {2, 1, 0, 1, 0, 0}, PB[6] = {0, 1, 2, 0, 1, 0};
+#pragma unroll
+                    for (int i = 0; i < 6; ++i)
+#pragma unroll
+                        for (int m = 0; m < MB; ++m)
+#pragma unroll
+                            for (int n = 0; n < NB; ++n) acc[m][n].mac(fa[PA[i]][m], fb[PB[i]][n]);
+                }
+            }
+            arrive();
+            now ^= 1;
+        }
+        const TileSettled settled;
+#pragma unroll
+        for (int m = 0; m < MB; ++m)
+#pragma unroll
+            for (int n = 0; n < NB; ++n) results[m][n] = acc[m][n].read(settled);
+    }
+};
+
+// Which tile a workgroup takes.  Workgroups go to the eight dies in turn; each die gets a run of tiles and walks it with up to eight
+// tiles of the second dimension side by side, so that tiles that run together share their operands in the die's L2.
+struct Place {
+    int m, n;
+    bool any;
+};
+
+__device__ __forceinline__ Place place(int id, int m_tiles, int n_tiles)
+{
+    const int items = m_tiles * n_tiles, per_die = (items + 7) / 8, item = id % 8 * per_die + id / 8;
+    if (id / 8 >= per_die || item >= items) return {0, 0, false};
+    const int group = item / (8 * m_tiles), first = group * 8, wide = n_tiles - first < 8 ? n_tiles - first : 8, in = item - group * 8 * m_tiles;
+    return {in / wide, first + in % wide, true};
+}
+
+inline long place_blocks(long m_tiles, long n_tiles) { return (m_tiles * n_tiles + 7) / 8 * 8; }
+
+}  // namespace
+
+#endif  // HOT_TILE_H
