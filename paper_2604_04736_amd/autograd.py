@@ -270,6 +270,10 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5) -> torch.Tensor:
     """Layer norm of x [..., width] over the last axis, differentiable in x, weight and bias.  weight and bias: [width], or
     [S, width] with x [S, ..., width], where weight sample s (a row of what GaussianSampleLayer draws) belongs to x[s]; either may be
     None.  x: float32, bfloat16 or float16, which y has too; weight and bias: of x's type or float32.  Statistics and sums are float32."""
+    if x.is_cuda:
+        y = hot.host().layer_norm(x, weight, bias, eps, torch.cuda.current_device())
+        if y is not None:           # (dense and on the current device: the call, its checks and its backward pass in native code)
+            return y
     if x.dim() < 1 or x.shape[-1] < 1:
         raise ValueError(f"x: need [..., width] with a width, got {tuple(x.shape)}")
     shaped = weight if weight is not None else bias
@@ -303,6 +307,10 @@ class _Head(torch.autograd.Function):
 
 def _head(x, weight, bias, index, logit, ignore_index, temperature, entries: int):
     """Shapes of a user's call to those of the binding; `entries`: axes of index behind the rows'."""
+    if x.is_cuda:
+        loss = hot.host().head_loss(x, weight, bias, index, logit, ignore_index, temperature, torch.cuda.current_device())
+        if loss is not None:
+            return loss
     if not isinstance(weight, torch.Tensor) or weight.dim() not in (2, 3):
         raise ValueError("weight: need [vocab, width] or [S, vocab, width]")
     if x.dim() < 1 or x.shape[-1] != weight.shape[-1]:

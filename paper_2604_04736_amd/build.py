@@ -46,10 +46,11 @@ def build_host_ops(verbose: bool = False) -> str:
     import torch
     from torch.utils import cpp_extension
     torch_lib = os.path.join(os.path.dirname(torch.__file__), "lib")
-    includes = cpp_extension.include_paths() + [sysconfig.get_paths()["include"], os.path.join(ROOT, "include")]
-    _run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall",
+    includes = cpp_extension.include_paths() + [sysconfig.get_paths()["include"], os.path.join(ROOT, "include"),
+                                                os.path.join(os.path.dirname(os.path.dirname(HIPCC)), "include")]
+    _run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall", "-D__HIP_PLATFORM_AMD__",
           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *("-I" + p for p in includes), "-o", HOST_LIB,
-          os.path.join(HERE, "csrc", "host_ops.cpp"), "-L" + HERE, "-lhot", "-Wl,-rpath,$ORIGIN", "-L" + torch_lib, "-lc10",
+          os.path.join(HERE, "csrc", "host_ops.cpp"), "-L" + HERE, "-lhot", "-Wl,-rpath,$ORIGIN", "-L" + torch_lib, "-lc10", "-lc10_hip",
           "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath," + torch_lib], verbose)
     return HOST_LIB
 
