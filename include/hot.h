@@ -591,7 +591,7 @@ int hot_norm_backward(const hot_norm_desc *desc, const void *x, const void *weig
  * samples).  weight: [vocab] rows `ldw` apart, samples `w_sample` apart; bias: [vocab], samples `bias_sample` apart, may be NULL (-inf
  * takes a word out).  All of dtype.  index: int64, entries of a row adjacent, rows `index_row` and samples `index_sample` apart (0: one
  * set of targets for all samples); logit likewise, of logit_dtype.  Where |x| or |weight| exceeds 3.389e38 or is not finite, results of the
- * rows concerned are not finite.  Limits: rows 2^22, width 2^19, vocab 2^24, top 1024, samples 4096, rows x vocab 2^38.
+ * rows concerned are not finite.  Limits: rows 2^20, width 2^19, vocab 2^24, top 1024, samples 4096, rows x vocab 2^38.
  */
 typedef struct hot_head_desc {
     int64_t rows;                      /* of one sample, >= 0 */

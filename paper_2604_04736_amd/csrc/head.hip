@@ -244,8 +244,9 @@ struct PackArgs {
     const int *count;              // with row_of: how many of them
     long rows, map_sample;
     int width, chunks;             // chunks = width / 8, rounded up
-    char *to;                      // [samples][rows][chunks * 16 bytes], pieces `plane` apart
-    long to_sample, plane;
+    char *to;                      // [samples], pieces `plane` apart: blocks of `columns` columns, each all rows
+    long to_sample, plane, block;
+    int columns;
 };
 
 // the three bf16 pieces of a float, whose sum it is up to 2^-25 of it; what is not finite stays in the first
@@ -270,7 +271,7 @@ hot_head_pack_kernel(PackArgs a)
         const int chunk = (int)(item - place * a.chunks);
         const long row = a.row_of ? a.row_of[s * a.map_sample + place] : place;
         const T *const from = static_cast<const T *>(a.from) + (size_t)s * (size_t)a.from_sample + (size_t)row * (size_t)a.from_row;
-        char *const to = a.to + (size_t)s * (size_t)a.to_sample + ((size_t)place * (size_t)a.chunks + (size_t)chunk) * 16;
+        char *const to = a.to + (size_t)s * (size_t)a.to_sample + (size_t)(chunk * 8 / a.columns) * (size_t)a.block + (size_t)place * (size_t)(a.columns * 2) + (size_t)(chunk * 8 % a.columns * 2);
         if constexpr (sizeof(T) == 2) {
             typedef T V __attribute__((ext_vector_type(8)));
             *reinterpret_cast<V *>(to) = __builtin_convertvector(Piece<T>::load(from, chunk * 8L, a.width), V);
@@ -297,8 +298,8 @@ hot_head_pack_kernel(PackArgs a)
 // --------------------------------------------------------------------------- logits: statistics, or their gradients
 
 struct HeadArgs {
-    const char *w, *x;             // rows of 16-bit elements (pieces `plane` apart); w begins at word v_begin
-    long w_pitch, w_plane, w_sample, x_pitch, x_plane, x_sample;      // bytes
+    Matrix w, x;                   // 16-bit elements; w begins at word v_begin
+    long w_sample, x_sample;       // bytes
     int width;
     int vocab, v_begin, v_count;   // the piece of the vocabulary
     long rows, places;             // rows a sample, and that rounded up to 256
@@ -318,8 +319,8 @@ struct HeadArgs {
     int v_tiles;
     // backward
     const float *hi, *lo, *grad, *to_scale;
-    char *dz;                      // [sample][place][dz_pitch]
-    long dz_pitch, dz_plane, dz_sample;
+    char *dz;                      // [sample] blocks of BK words, each all places
+    long dz_block, dz_plane, dz_sample;
 };
 
 // Walks the targets of this lane's rows that lie in the wave's words: f(nb, m, i, mine, weight) is called for every result (m, i) that
@@ -386,6 +387,8 @@ __device__ __forceinline__ void to_scores(const HeadArgs &a, long s, int v0, con
         }
 }
 
+__device__ __forceinline__ Matrix part(const Matrix &m, long bytes) { return {m.at + bytes, m.pitch, m.block, m.plane}; }
+
 template <class TILE>
 __device__ __forceinline__ bool head_product(const HeadArgs &a, lds_char *lds, long s, int &v0, int &r0, f16v (&acc)[TILE::MB][TILE::NB])
 {
@@ -395,8 +398,8 @@ __device__ __forceinline__ bool head_product(const HeadArgs &a, lds_char *lds, l
     const int in = at.m * TILE::BM;
     v0 = a.v_begin + in;
     r0 = at.n * TILE::BN;
-    const Operand w = {a.w + (size_t)s * (size_t)a.w_sample + (size_t)in * (size_t)a.w_pitch, a.w_pitch, a.w_plane, a.v_begin + a.v_count - v0, a.width};
-    const Operand x = {a.x + (size_t)s * (size_t)a.x_sample + (size_t)r0 * (size_t)a.x_pitch, a.x_pitch, a.x_plane, count - r0, a.width};
+    const Operand w = {part(a.w, s * a.w_sample + in * a.w.pitch), a.v_begin + a.v_count - v0, a.width};
+    const Operand x = {part(a.x, s * a.x_sample + r0 * a.x.pitch), count - r0, a.width};
     TILE::product(lds, w, x, a.width, acc);
     return true;
 }
@@ -504,7 +507,8 @@ hot_head_dz_kernel(HeadArgs a)
     typedef typename TILE::T T;
     typedef T V4 __attribute__((ext_vector_type(4)));
     typedef T V8 __attribute__((ext_vector_type(8)));
-    char *const out = a.dz + (size_t)s * (size_t)a.dz_sample + (size_t)r0 * (size_t)a.dz_pitch + (size_t)(v0 - a.v_begin) * 2;
+    constexpr int BK = TILE::BK;
+    char *const out = a.dz + (size_t)s * (size_t)a.dz_sample + (size_t)((v0 - a.v_begin) / BK) * (size_t)a.dz_block + (size_t)r0 * (BK * 2);
 #pragma unroll
     for (int p = 0; p < TILE::PIECES; ++p) {
         if (p) __syncthreads();
@@ -527,9 +531,9 @@ hot_head_dz_kernel(HeadArgs a)
         constexpr int CHUNKS = TILE::BM / 8;
 #pragma unroll 4
         for (int k = (int)threadIdx.x; k < TILE::BN * CHUNKS; k += TILE::THREADS) {
-            const int row = k / CHUNKS, chunk = k % CHUNKS;
-            *reinterpret_cast<V8 *>(out + (size_t)p * (size_t)a.dz_plane + (size_t)row * (size_t)a.dz_pitch + chunk * 16) =
-                *reinterpret_cast<const V8 *>(memory + row * PITCH + chunk * 16);
+            const int block = k / (TILE::BN * BK / 8), in = k % (TILE::BN * BK / 8), row = in / (BK / 8), chunk = in % (BK / 8);
+            *reinterpret_cast<V8 *>(out + (size_t)p * (size_t)a.dz_plane + (size_t)block * (size_t)a.dz_block + in * 16) =
+                *reinterpret_cast<const V8 *>(memory + row * PITCH + block * (BK * 2) + chunk * 16);
         }
     }
 }
@@ -599,8 +603,8 @@ hot_head_join_kernel(JoinArgs a)
 // --------------------------------------------------------------------------- gradients of features, weights and bias
 
 struct GradArgs {
-    const char *dz, *other;        // other: W (from word v_begin) or the packed features
-    long dz_pitch, dz_plane, dz_sample, pitch, plane, sample;
+    Matrix dz, other;              // other: W (from word v_begin) or the packed features
+    long dz_sample, sample;
     int width, vocab, v_begin, v_count;
     long rows;
     const int *count;
@@ -626,8 +630,8 @@ hot_head_dx_kernel(GradArgs a)
     const int r0 = at.n * TILE::BM, k0 = at.m * TILE::BN, v = split * a.split_depth;
     const int depth = a.v_count - v < a.split_depth ? a.v_count - v : a.split_depth;
     f16v acc[TILE::MB][TILE::NB];
-    const Operand dz = {a.dz + (size_t)s * (size_t)a.dz_sample + (size_t)r0 * (size_t)a.dz_pitch + (size_t)v * 2, a.dz_pitch, a.dz_plane, count - r0, depth};
-    const Operand w = {a.other + (size_t)s * (size_t)a.sample + (size_t)v * (size_t)a.pitch + (size_t)k0 * 2, a.pitch, a.plane, a.width - k0, depth};
+    const Operand dz = {part(a.dz, s * a.dz_sample + v / TILE::BK * a.dz.block + r0 * a.dz.pitch), count - r0, depth};
+    const Operand w = {part(a.other, s * a.sample + v * a.other.pitch + k0 / TILE::BK * a.other.block), a.width - k0, depth};
     TILE::product((lds_char *)memory, dz, w, depth, acc);
     float *const sums = a.sums + ((size_t)split * (size_t)a.samples + (size_t)s) * (size_t)a.rows * (size_t)a.width;
 #pragma unroll
@@ -660,8 +664,8 @@ hot_head_dw_kernel(GradArgs a)
     if (!at.any) return;
     const int in = at.m * TILE::BN, k0 = at.n * TILE::BM;
     f16v acc[TILE::MB][TILE::NB];
-    const Operand x = {a.other + (size_t)s * (size_t)a.sample + (size_t)k0 * 2, a.pitch, a.plane, a.width - k0, count};
-    const Operand dz = {a.dz + (size_t)s * (size_t)a.dz_sample + (size_t)in * 2, a.dz_pitch, a.dz_plane, a.v_count - in, count};
+    const Operand x = {part(a.other, s * a.sample + k0 / TILE::BK * a.other.block), a.width - k0, count};
+    const Operand dz = {part(a.dz, s * a.dz_sample + in / TILE::BK * a.dz.block), a.v_count - in, count};
     TILE::product((lds_char *)memory, x, dz, count, acc);
     const float scale = a.scale[2 * s + 1] * a.temperature;
     typedef OUT V4 __attribute__((ext_vector_type(4)));
@@ -694,8 +698,8 @@ hot_head_dw_kernel(GradArgs a)
 
 // db of one piece: sums of dz over the rows, 128 words and 16 runs of rows to a workgroup
 struct BiasArgs {
-    const char *dz;
-    long dz_pitch, dz_plane, dz_sample;
+    Matrix dz;
+    long dz_sample;
     int v_begin, v_count;
     const int *count;
     const float *scale;
@@ -705,7 +709,7 @@ struct BiasArgs {
     int type;
 };
 
-template <class T, int PIECES>
+template <class T, int PIECES, int BK>
 __global__ void __launch_bounds__(256)
 hot_head_db_kernel(BiasArgs a)
 {
@@ -718,7 +722,7 @@ hot_head_db_kernel(BiasArgs a)
         for (int r = run; r < count; r += 16)
 #pragma unroll
             for (int p = PIECES - 1; p >= 0; --p) {
-                const V8 v = *reinterpret_cast<const V8 *>(a.dz + (size_t)s * (size_t)a.dz_sample + (size_t)p * (size_t)a.dz_plane + (size_t)r * (size_t)a.dz_pitch + (size_t)in * 2);
+                const V8 v = *reinterpret_cast<const V8 *>(a.dz.at + s * a.dz_sample + p * a.dz.plane + in / BK * a.dz.block + r * a.dz.pitch + in % BK * 2);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) sum[j] += (float)v[j];
             }
@@ -788,11 +792,13 @@ struct HeadPlan {
     int pieces;              // of an element
     bool pack_w;
     int chunks;              // 16-byte chunks of a packed row
+    int columns;             // of a block of what is packed
+    long row_bytes;          // of a packed row: whole blocks
     long places;
     int v_piece, v_pieces;   // words of a piece
     int size;                // 0: tiles for few rows, 1: 128 x 128, 2: large ones
     int v_tile;              // words of a tile of logits
-    int splits, split_depth;
+    int splits, split_depth; // runs of words of a piece, and their length
     // where things lie in the workspace
     int64_t word, weight, list_count, sums, start, count, row_of, place_of, label, hi, lo, grad, scale, x, w, dz, partials, dx, bytes;
 };
@@ -809,7 +815,7 @@ struct Layout {
 
 bool head_ok(const hot_head_desc *d)
 {
-    if (!d || d->rows < 0 || d->rows > (1L << 22) || d->width < 1 || d->width > (1L << 19) || d->vocab < 1 || d->vocab > (1L << 24) || d->samples < 1 || d->samples > 4096 ||
+    if (!d || d->rows < 0 || d->rows > (1L << 20) || d->width < 1 || d->width > (1L << 19) || d->vocab < 1 || d->vocab > (1L << 24) || d->samples < 1 || d->samples > 4096 ||
         !known_type(d->dtype) || d->ldx < 0 || d->x_sample < 0 || d->ldw < d->width || d->w_sample < 0 || d->bias_sample < 0 || d->index_row < 0 || d->index_sample < 0)
         return false;
     if (d->samples > 1 && (d->w_sample < (d->vocab - 1) * d->ldw + d->width || (d->bias_sample != 0 && d->bias_sample < d->vocab))) return false;
@@ -827,6 +833,8 @@ HeadPlan head_plan(const hot_head_desc &d, bool backward, bool with_dx)
     p.pieces = d.dtype == HOT_F32 ? 3 : 1;
     p.pack_w = p.pieces == 3 || !d.w_aligned || K % 8 || d.ldw % 8 || (S > 1 && d.w_sample % 8) || d.ldw > (1L << 21);
     p.chunks = (int)((K + 7) / 8);
+    p.columns = p.pieces == 3 ? 32 : 64;
+    p.row_bytes = up(K, p.columns) * 2;
     p.places = up(R, 256);
     // Tiles of 256 x 256 (256 x 128 in three pieces) where they fill the chip, of 128 x 128 below, of 256 x 32 for up to 32 rows.
     const long large = ((V + 255) / 256) * ((R + 255) / 256) * S;
@@ -834,7 +842,7 @@ HeadPlan head_plan(const hot_head_desc &d, bool backward, bool with_dx)
     p.v_tile = p.size == 1 ? 128 : 256;
     long piece = up(V, 256);
     if (backward || p.pack_w) {
-        const int64_t per_word = S * ((backward ? p.places * 2 * p.pieces : 0) + (p.pack_w ? p.chunks * 16L * p.pieces : 0));
+        const int64_t per_word = S * ((backward ? p.places * 2 * p.pieces : 0) + (p.pack_w ? p.row_bytes * p.pieces : 0));
         const long most = kPieceBytes / per_word / 256 * 256;
         const long least = 1024;
         const long n = (piece + (most > least ? most : least) - 1) / (most > least ? most : least);
@@ -842,14 +850,18 @@ HeadPlan head_plan(const hot_head_desc &d, bool backward, bool with_dx)
     }
     p.v_piece = (int)piece;
     p.v_pieces = (int)((V + piece - 1) / piece);
-    // the features' gradients of few tiles: several workgroups share the words of a piece
+    // The features' gradients: a run of the piece's words to a workgroup.  A round of workgroups takes its steps of 64 words, and as long as some
+    // twenty of them for its start and for adding to the sums in memory; the number of runs with the fewest such steps is taken.
     const int bm = p.size == 0 ? 32 : (p.size == 1 || p.pieces == 3 ? 128 : 256), bn = p.size == 1 ? 128 : 256;
-    const long tiles = ((R + bm - 1) / bm) * ((K + bn - 1) / bn) * S;
-    long splits = (2 * kComputeUnits + tiles - 1) / tiles, most_splits = piece / 256;
-    if (tiles >= kComputeUnits) splits = 1;
-    splits = splits < 1 ? 1 : (splits > most_splits ? most_splits : splits);
-    if (splits > 64) splits = 64;
-    p.split_depth = (int)up((piece + splits - 1) / splits, 64);
+    const long tiles = ((R + bm - 1) / bm) * ((K + bn - 1) / bn) * S, at_once = kComputeUnits * (p.size == 2 || p.pieces == 3 ? 1 : 2);
+    long best = 0;
+    for (long runs = 1; runs <= 64 && (runs == 1 || runs * 256 <= piece); ++runs) {
+        const long depth = up((piece + runs - 1) / runs, 64), cost = (tiles * runs + at_once - 1) / at_once * (depth / 64 + 20);
+        if (runs == 1 || cost < best) {
+            best = cost;
+            p.split_depth = (int)depth;
+        }
+    }
     p.splits = (int)((piece + p.split_depth - 1) / p.split_depth);
 
     Layout l;
@@ -869,8 +881,8 @@ HeadPlan head_plan(const hot_head_desc &d, bool backward, bool with_dx)
         p.grad = l.take(S * R * 4);
         p.scale = l.take(S * 8);
     }
-    p.x = l.take(S * p.places * p.chunks * 16 * p.pieces);
-    p.w = l.take(p.pack_w ? S * piece * p.chunks * 16 * p.pieces : 0);
+    p.x = l.take(S * p.places * p.row_bytes * p.pieces);
+    p.w = l.take(p.pack_w ? S * piece * p.row_bytes * p.pieces : 0);
     if (backward) {
         p.dz = l.take(S * p.places * piece * 2 * p.pieces);
         if (with_dx) p.dx = l.take((int64_t)p.splits * S * R * K * 4);
@@ -966,7 +978,9 @@ void head_pack_x(const HeadCall &c)
     a.width = (int)c.d.width;
     a.chunks = c.p.chunks;
     a.to = c.in<char>(c.p.x);
-    a.to_sample = c.p.places * c.p.chunks * 16L;
+    a.columns = c.p.columns;
+    a.block = c.p.places * c.p.columns * 2L;
+    a.to_sample = c.p.places * c.p.row_bytes;
     a.plane = c.d.samples * a.to_sample;
     hot_head_pack_kernel<T><<<dim3(grid_for(c.d.rows * a.chunks), (unsigned)c.d.samples), 256, 0, c.stream>>>(a);
 }
@@ -982,22 +996,20 @@ void head_pack_w(const HeadCall &c, long v_begin, long v_count)
     a.width = (int)c.d.width;
     a.chunks = c.p.chunks;
     a.to = c.in<char>(c.p.w);
-    a.to_sample = c.p.v_piece * (long)c.p.chunks * 16L;
+    a.columns = c.p.columns;
+    a.block = c.p.v_piece * c.p.columns * 2L;
+    a.to_sample = c.p.v_piece * c.p.row_bytes;
     a.plane = c.d.samples * a.to_sample;
     hot_head_pack_kernel<T><<<dim3(grid_for(v_count * a.chunks), (unsigned)c.d.samples), 256, 0, c.stream>>>(a);
 }
 
-// the weights' part of a kernel's arguments: as they lie, or packed
-struct Weights {
-    const char *at;
-    long pitch, plane, sample;
-};
-
-Weights head_weights(const HeadCall &c, long v_begin)
+// the weights from word v_begin on as the kernels read them: as they lie, or packed
+Matrix head_weights(const HeadCall &c, long v_begin, long &sample)
 {
-    if (!c.p.pack_w) return {static_cast<const char *>(c.w) + (size_t)v_begin * (size_t)c.d.ldw * 2, c.d.ldw * 2, 0, c.d.w_sample * 2};
-    const long sample = c.p.v_piece * (long)c.p.chunks * 16L;
-    return {c.in<char>(c.p.w), c.p.chunks * 16L, c.d.samples * sample, sample};
+    const long columns = c.p.columns;
+    sample = c.p.pack_w ? c.p.v_piece * c.p.row_bytes : c.d.w_sample * 2;
+    if (!c.p.pack_w) return {static_cast<const char *>(c.w) + (size_t)v_begin * (size_t)c.d.ldw * 2, c.d.ldw * 2, columns * 2, 0};
+    return {c.in<char>(c.p.w), columns * 2, c.p.v_piece * columns * 2, c.d.samples * sample};
 }
 
 HeadArgs head_args(const HeadCall &c, long v_begin, long v_count)
@@ -1005,15 +1017,9 @@ HeadArgs head_args(const HeadCall &c, long v_begin, long v_count)
     const hot_head_desc &d = c.d;
     const HeadPlan &p = c.p;
     HeadArgs a = {};
-    const Weights w = head_weights(c, v_begin);
-    a.w = w.at;
-    a.w_pitch = w.pitch;
-    a.w_plane = w.plane;
-    a.w_sample = w.sample;
-    a.x = c.in<char>(p.x);
-    a.x_pitch = p.chunks * 16L;
-    a.x_sample = p.places * a.x_pitch;
-    a.x_plane = d.samples * a.x_sample;
+    a.w = head_weights(c, v_begin, a.w_sample);
+    a.x_sample = p.places * p.row_bytes;
+    a.x = {c.in<char>(p.x), p.columns * 2L, p.places * p.columns * 2L, d.samples * a.x_sample};
     a.width = (int)d.width;
     a.vocab = (int)d.vocab;
     a.v_begin = (int)v_begin;
@@ -1040,8 +1046,8 @@ HeadArgs head_args(const HeadCall &c, long v_begin, long v_count)
     a.grad = c.in<float>(p.grad);
     a.to_scale = c.in<float>(p.scale);
     a.dz = c.in<char>(p.dz);
-    a.dz_pitch = p.v_piece * 2L;
-    a.dz_sample = p.places * a.dz_pitch;
+    a.dz_block = p.places * p.columns * 2L;
+    a.dz_sample = p.places * p.v_piece * 2L;
     a.dz_plane = d.samples * a.dz_sample;
     return a;
 }
@@ -1122,9 +1128,7 @@ void head_backward(const HeadCall &c, const double *lse, const float *g, long g_
         const HeadArgs h = head_args(c, v, n);
         head_logits<E, PIECES>(c, h, true);
         GradArgs a = {};
-        a.dz = h.dz;
-        a.dz_pitch = h.dz_pitch;
-        a.dz_plane = h.dz_plane;
+        a.dz = {h.dz, c.p.columns * 2L, h.dz_block, h.dz_plane};
         a.dz_sample = h.dz_sample;
         a.width = h.width;
         a.vocab = h.vocab;
@@ -1141,8 +1145,6 @@ void head_backward(const HeadCall &c, const double *lse, const float *g, long g_
         a.temperature = (float)c.d.temperature;
         if (dx) {
             a.other = h.w;
-            a.pitch = h.w_pitch;
-            a.plane = h.w_plane;
             a.sample = h.w_sample;
             if (c.p.size == 0) head_dx<Tile<E, PIECES, true, false, 32, 256, 1, 8>>(c, a);
             else if (c.p.size == 1) head_dx<Tile<E, PIECES, true, false, 128, 128, 2, 2>>(c, a);
@@ -1151,8 +1153,6 @@ void head_backward(const HeadCall &c, const double *lse, const float *g, long g_
         }
         if (dw) {
             a.other = h.x;
-            a.pitch = h.x_pitch;
-            a.plane = h.x_plane;
             a.sample = h.x_sample;
             a.out = dw;
             a.out_sample = c.d.vocab * c.d.width;
@@ -1161,8 +1161,8 @@ void head_backward(const HeadCall &c, const double *lse, const float *g, long g_
             else head_dw<Tile<E, PIECES, false, false, 256, 128, 4, 2>, T>(c, a);
         }
         if (db) {
-            const BiasArgs b = {h.dz, h.dz_pitch, h.dz_plane, h.dz_sample, h.v_begin, h.v_count, h.count, scale, a.temperature, db, c.d.vocab, c.d.dtype};
-            hot_head_db_kernel<E, PIECES><<<dim3((unsigned)((n + 127) / 128), (unsigned)c.d.samples), 256, 0, c.stream>>>(b);
+            const BiasArgs b = {a.dz, a.dz_sample, h.v_begin, h.v_count, h.count, scale, a.temperature, db, c.d.vocab, c.d.dtype};
+            hot_head_db_kernel<E, PIECES, PIECES == 3 ? 32 : 64><<<dim3((unsigned)((n + 127) / 128), (unsigned)c.d.samples), 256, 0, c.stream>>>(b);
         }
     }
     if (dx) {
@@ -1174,7 +1174,7 @@ void head_backward(const HeadCall &c, const double *lse, const float *g, long g_
         a.rows = c.d.rows;
         a.width = c.d.width;
         a.samples = c.d.samples;
-        a.splits = (int)((c.p.v_piece + c.p.split_depth - 1) / c.p.split_depth);
+        a.splits = c.p.splits;
         a.shared = c.d.samples > 1 && c.d.x_sample == 0;
         a.out = dx;
         hot_head_features_kernel<T><<<dim3(grid_for(c.d.rows * ((c.d.width + Piece<T>::N - 1) / Piece<T>::N)), a.shared ? 1u : (unsigned)c.d.samples), 256, 0, c.stream>>>(a);

@@ -53,11 +53,17 @@ public:
     __device__ __forceinline__ f16v read(const TileSettled &) const { return v_; }
 };
 
+// A matrix in memory: element (row, col) at col / BK * block + row * pitch + col % BK * 2, `plane` bytes between pieces.  Rows as they usually
+// lie have a block of BK * 2 bytes; what is written here for the tiles to read has rows of BK elements, one block of columns after another, so
+// that a tile's loads are one run of memory (or four): read across 32 KB rows instead, the features' gradients took 1.2 times as long.
+struct Matrix {
+    const char *at;
+    long pitch, block, plane;
+};
+
 // One operand's part of a tile: T of its rows or columns ("lines": what is not contracted) from `at` on.
 struct Operand {
-    const char *at;      // first line, first contraction index
-    long pitch;          // bytes between rows in memory
-    long plane;          // bytes between pieces
+    Matrix m;            // from the first line and the first contraction index on (a multiple of BK if it is a column)
     int lines;           // how many lines there are; the tile's others are zeros
     int depth;           // how many contraction indices there are; the others are zeros
 };
@@ -89,27 +95,22 @@ struct Stage {
         for (int j = 0; j < kEach; ++j) {
             const int row = (wave + j * WAVES) * kRows + lane / kPerRow, chunk = lane % kPerRow ^ permuted(row);
             const int line = ALONG ? row : chunk * 8;
-            off[j] = line < o.lines ? (unsigned)(row * o.pitch + chunk * 16) : kBeyond;
+            off[j] = line < o.lines ? (unsigned)(chunk * 8 / BK * o.m.block + row * o.m.pitch + chunk * 8 % BK * 2) : kBeyond;
             if constexpr (ALONG) index[0] = chunk * 8;
             else index[j] = row;
         }
     }
 
-    // sends for the tile that begins at contraction index k0
-    __device__ __forceinline__ void ask(const Operand &o, int k0, lds_char *to) const
+    // Sends for load `j` of kEach * PIECES of the tile that begins at contraction index k0 (beyond the last index: for zeros).
+    static constexpr int kAll = kEach * PIECES;
+    __device__ __forceinline__ void ask(const Operand &o, int k0, lds_char *to, int j) const
     {
-        const int left = o.depth - k0;
-#pragma unroll
-        for (int p = 0; p < PIECES; ++p) {
-            const char *const from = o.at + p * o.plane + (ALONG ? (long)k0 * 2 : (long)k0 * o.pitch);
-            const __amdgpu_buffer_rsrc_t win = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(from), 0, (int)kBeyond, 0x00020000);
-#pragma unroll
-            for (int j = 0; j < kEach; ++j) {
-                if (kLoads % WAVES != 0 && wave + j * WAVES >= kLoads) break;
-                const unsigned at = index[ALONG ? 0 : j] < left ? off[j] : kBeyond;
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(win, (__attribute__((address_space(3))) void *)(to + p * kBytes + (wave + j * WAVES) * 1024), 16, (int)at, 0, 0, 0);
-            }
-        }
+        const int p = j / kEach, i = j % kEach;
+        if (kLoads % WAVES != 0 && wave + i * WAVES >= kLoads) return;
+        const char *const from = o.m.at + p * o.m.plane + (ALONG ? k0 / BK * o.m.block : k0 * o.m.pitch);
+        const __amdgpu_buffer_rsrc_t win = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(from), 0, (int)kBeyond, 0x00020000);
+        const unsigned at = index[ALONG ? 0 : i] < o.depth - k0 ? off[i] : kBeyond;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(win, (__attribute__((address_space(3))) void *)(to + p * kBytes + (wave + i * WAVES) * 1024), 16, (int)at, 0, 0, 0);
     }
 };
 
@@ -151,53 +152,102 @@ struct Tile {
     // everything sent for has come, to all waves
     static __device__ __forceinline__ void arrive() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-    // results = A B over `depth` contraction indices; LDS is free when it returns
+    // The operands of one matrix step of sixteen contraction indices: those of B, then those of A
+    struct Operands {
+        s8v a[PIECES][MB], b[PIECES][NB];
+        __device__ __forceinline__ void read(const lds_char *tile, int ks, int i)
+        {
+            const int l = lane();
+            if (i < PIECES * NB) b[i / NB][i % NB] = fragment<BN, BK, B_ALONG>(tile + kA + i / NB * StageB::kBytes, n0() + 32 * (i % NB), ks, l);
+            else {
+                i -= PIECES * NB;
+                a[i / MB][i % MB] = fragment<BM, BK, A_ALONG>(tile + i / MB * StageA::kBytes, m0() + 32 * (i % MB), ks, l);
+            }
+        }
+    };
+    static constexpr int kReads = PIECES * (MB + NB), kLoads = StageA::kAll + StageB::kAll;
+    // a step's products in parts, between which reads and loads are issued: rows of blocks, or the six products of the pieces
+    static constexpr int kParts = PIECES == 1 ? MB : 6;
+
+    static __device__ __forceinline__ void multiply(const Operands &o, TileAcc<T> (&acc)[MB][NB], int part)
+    {
+        if constexpr (PIECES == 1) {
+#pragma unroll
+            for (int n = 0; n < NB; ++n) acc[part][n].mac(o.a[0][part], o.b[0][n]);
+        } else {
+            constexpr int PA[6] = {2, 1, 0, 1, 0, 0}, PB[6] = {0, 1, 2, 0, 1, 0};
+#pragma unroll
+            for (int m = 0; m < MB; ++m)
+#pragma unroll
+                for (int n = 0; n < NB; ++n) acc[m][n].mac(o.a[PA[part]][m], o.b[PB[part]][n]);
+        }
+    }
+
+    // One tile of contraction indices: the tile `here`, while the next is on its way
+    static constexpr int kSteps = BK / 16, kEarly = (kLoads + 1) / 2;
+    static __device__ __forceinline__ void step(lds_char *__restrict here, lds_char *__restrict next, const Operand &a, const Operand &b, const StageA &sa, const StageB &sb,
+                                                int k0, Operands (&now)[2], TileAcc<T> (&acc)[MB][NB])
+    {
+        auto ask = [&](int from, lds_char *to, int j) {
+            if (j < StageA::kAll) sa.ask(a, from, to, j);
+            else sb.ask(b, from, to + kA, j - StageA::kAll);
+        };
+#pragma unroll
+        for (int ks = 0; ks < kSteps; ++ks) {
+            const bool last = ks + 1 == kSteps;
+            __builtin_amdgcn_sched_barrier(0);
+            if (last) arrive();
+#pragma unroll
+            for (int part = 0; part < kParts; ++part) {
+                // reads in the first half of the parts, loads in all of them
+                constexpr int HALF = (kParts + 1) / 2;
+#pragma unroll
+                for (int i = 0; i < kReads; ++i)
+                    if (i * HALF / kReads == part) {
+                        if (last) now[(ks + 1) & 1].read(next, 0, i);
+                        else now[(ks + 1) & 1].read(here, ks + 1, i);
+                    }
+                if (last)
+#pragma unroll
+                    for (int j = 0; j < kEarly; ++j)
+                        if (j * kParts / kEarly == part) ask(k0 + 2 * BK, here, j);
+                if (ks == 0)
+#pragma unroll
+                    for (int j = kEarly; j < kLoads; ++j)
+                        if ((j - kEarly) * kParts / (kLoads - kEarly) == part) ask(k0 + BK, next, j);
+                multiply(now[ks & 1], acc, part);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    }
+
+    // results = A B over `depth` contraction indices; LDS is free when it returns.  Two tiles in LDS, two sets of operands in registers.  Between
+    // the parts of a step's products the next step's operands are read; the last step of a tile begins with the barrier behind which
+    // the tile's room is free: the loads for the tile after the next are issued in that step and the one behind it.
     static __device__ __forceinline__ void product(lds_char *lds, const Operand &a, const Operand &b, int depth, f16v (&results)[MB][NB])
     {
         const int l = lane(), w = wave();
         const StageA sa(a, w, l);
         const StageB sb(b, w, l);
         TileAcc<T> acc[MB][NB];
-        if (depth > 0) {
-            sa.ask(a, 0, lds);
-            sb.ask(b, 0, lds + kA);
+        Operands now[2];
+        auto ask = [&](int from, lds_char *to, int j) {
+            if (j < StageA::kAll) sa.ask(a, from, to, j);
+            else sb.ask(b, from, to + kA, j - StageA::kAll);
+        };
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) ask(0, lds, j);
+        arrive();
+#pragma unroll
+        for (int j = 0; j < kEarly; ++j) ask(BK, lds + kStage, j);
+#pragma unroll
+        for (int i = 0; i < kReads; ++i) now[0].read(lds, 0, i);         // (of zeros where depth is 0)
+        int at = 0;
+        for (int k0 = 0; k0 < depth; k0 += BK) {
+            step(lds + at, lds + (kStage - at), a, b, sa, sb, k0, now, acc);
+            at = kStage - at;
         }
         arrive();
-        int now = 0;
-        for (int k0 = 0; k0 < depth; k0 += BK) {
-            lds_char *const here = lds + now * kStage, *const next = lds + (now ^ 1) * kStage;
-            if (k0 + BK < depth) {
-                sa.ask(a, k0 + BK, next);
-                sb.ask(b, k0 + BK, next + kA);
-            }
-#pragma unroll
-            for (int ks = 0; ks < BK / 16; ++ks) {
-                s8v fa[PIECES][MB], fb[PIECES][NB];
-#pragma unroll
-                for (int p = 0; p < PIECES; ++p) {
-#pragma unroll
-                    for (int m = 0; m < MB; ++m) fa[p][m] = fragment<BM, BK, A_ALONG>(here + p * StageA::kBytes, m0() + 32 * m, ks, l);
-#pragma unroll
-                    for (int n = 0; n < NB; ++n) fb[p][n] = fragment<BN, BK, B_ALONG>(here + kA + p * StageB::kBytes, n0() + 32 * n, ks, l);
-                }
-                if constexpr (PIECES == 1) {
-#pragma unroll
-                    for (int m = 0; m < MB; ++m)
-#pragma unroll
-                        for (int n = 0; n < NB; ++n) acc[m][n].mac(fa[0][m], fb[0][n]);
-                } else {
-                    constexpr int PA[6] = {2, 1, 0, 1, 0, 0}, PB[6] = {0, 1, 2, 0, 1, 0};
-#pragma unroll
-                    for (int i = 0; i < 6; ++i)
-#pragma unroll
-                        for (int m = 0; m < MB; ++m)
-#pragma unroll
-                            for (int n = 0; n < NB; ++n) acc[m][n].mac(fa[PA[i]][m], fb[PB[i]][n]);
-                }
-            }
-            arrive();
-            now ^= 1;
-        }
         const TileSettled settled;
 #pragma unroll
         for (int m = 0; m < MB; ++m)
