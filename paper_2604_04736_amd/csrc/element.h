@@ -18,14 +18,15 @@ struct Piece {
     typedef float F __attribute__((ext_vector_type(N)));
 
     // elements at .. at + N - 1 of a row of n; zeros behind its end
-    static __device__ __forceinline__ F load(const T *row, long at, long n)
+    static __device__ __forceinline__ V take(const T *row, long at, long n)
     {
-        if (at + N <= n) return __builtin_convertvector(V(*reinterpret_cast<const Loose *>(row + at)), F);
-        F v;
+        if (at + N <= n) return *reinterpret_cast<const Loose *>(row + at);
+        V v;
 #pragma unroll
-        for (int j = 0; j < N; ++j) v[j] = at + j < n ? (float)row[at + j] : 0.0f;
+        for (int j = 0; j < N; ++j) v[j] = at + j < n ? row[at + j] : (T)0.0f;
         return v;
     }
+    static __device__ __forceinline__ F load(const T *row, long at, long n) { return __builtin_convertvector(take(row, at, n), F); }
     static __device__ __forceinline__ void store(T *row, long at, long n, F v)
     {
         const V o = __builtin_convertvector(v, V);

@@ -3,9 +3,10 @@
 //   forward   m = mean x,  r = 1/sqrt(mean (x - m)^2 + eps),  h = (x - m) r,  y = h w + b
 //   backward  u = dy w,  dx = r (u - mean u - h mean(u h)),  dw = sum over rows dy h,  db = sum over rows dy
 //
-// What bounds both is memory: a row is read once, kept in registers through mean, variance and result, and written once.  TPR threads
-// share a row, each with VPT pieces of sixteen bytes; rows shorter than a wavefront's reach share one (TPR = 16), longer ones take
-// a workgroup.  Mean, then variance of what was read (two passes over registers, no cancellation), in fp32.
+// What bounds both is memory: a row is read once, kept in registers through mean, variance and result, and written once, while the next
+// row of the same threads is on its way.  32768 x 8192 in bf16: forward 244 us (4.4 TB/s), backward 314 (5.1); a copy of that size runs at
+// 4.8 to 5.2.  TPR threads share a row, each with VPT pieces of sixteen bytes; rows shorter than a wavefront's reach share one
+// (TPR = 16), longer ones take a workgroup.  Mean, then variance of what was read (two passes over registers, no cancellation), in fp32.
 // The sums for dw and db stay in registers of the threads that own the columns while a workgroup walks its rows; every workgroup
 // leaves one row of partial sums in scratch memory and a second kernel adds them in a fixed order.
 #include <hip/hip_runtime.h>
@@ -60,55 +61,72 @@ __device__ __forceinline__ void row_sum(float (&v)[N], float (*slots)[N], int &t
     }
 }
 
+// zeros behind the row's end, where a piece reaches there
+template <int N, class F>
+__device__ __forceinline__ void clip(F &v, int valid)
+{
+    if (valid >= N) return;
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+        if (j >= valid) v[j] = 0.0f;
+}
+
 template <class T, int TPR, int VPT>
 __global__ void __launch_bounds__(TPR > kNormBlock ? TPR : kNormBlock)
 hot_norm_forward_kernel(NormArgs a)
 {
     typedef Piece<T> P;
+    typedef typename P::F F;
     constexpr int N = P::N, BLOCK = TPR > kNormBlock ? TPR : kNormBlock, GROUPS = BLOCK / TPR;
     __shared__ float slots[2 * (TPR > 64 ? TPR / 64 : 1)][1];
     int turn = 0;
-    const int t = (int)threadIdx.x % TPR, s = (int)blockIdx.y;
-    const long n = a.width;
+    const int t = (int)threadIdx.x % TPR, s = (int)blockIdx.y, n = (int)a.width;
     const T *const xs = static_cast<const T *>(a.x) + (size_t)s * (size_t)a.x_sample;
     T *const ys = static_cast<T *>(a.out) + (size_t)s * (size_t)a.rows * (size_t)n;
-    typename P::F w[VPT], b[VPT];
+    const long stride = (long)gridDim.x * GROUPS;
+    long row = (long)blockIdx.x * GROUPS + threadIdx.x / TPR;
+    typename P::V next[VPT];
+    auto ask = [&](long r) {
+        if (r >= a.rows) return;
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) next[i] = P::take(xs + (size_t)r * (size_t)a.ldx, (i * TPR + t) * N, n);
+    };
+    ask(row);
+    F w[VPT], b[VPT];
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-        const long at = (long)(i * TPR + t) * N;
-        w[i] = b[i] = typename P::F(0.0f);
-        if (a.w) w[i] = load_as<N, typename P::F>(a.w, a.w_type, s * a.w_sample + at, s * a.w_sample + n);
-        else w[i] = typename P::F(1.0f);
-        if (a.b) b[i] = load_as<N, typename P::F>(a.b, a.w_type, s * a.w_sample + at, s * a.w_sample + n);
+        const long at = s * a.w_sample + (i * TPR + t) * N, end = s * a.w_sample + n;
+        w[i] = a.w ? load_as<N, F>(a.w, a.w_type, at, end) : F(1.0f);
+        b[i] = a.b ? load_as<N, F>(a.b, a.w_type, at, end) : F(0.0f);
     }
-    for (long row = (long)blockIdx.x * GROUPS + threadIdx.x / TPR; row < a.rows; row += (long)gridDim.x * GROUPS) {
-        const T *const x = xs + (size_t)row * (size_t)a.ldx;
-        typename P::F v[VPT];
+    for (; row < a.rows; row += stride) {
+        F v[VPT];
         float sum[1] = {0.0f};
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            v[i] = P::load(x, (long)(i * TPR + t) * N, n);
+            v[i] = __builtin_convertvector(next[i], F);
 #pragma unroll
             for (int j = 0; j < N; ++j) sum[0] += v[i][j];
         }
+        ask(row + stride);
         row_sum<TPR, 1>(sum, slots, turn);
         const float mean = sum[0] * a.inv_width;
         float sq[1] = {0.0f};
 #pragma unroll
-        for (int i = 0; i < VPT; ++i)
+        for (int i = 0; i < VPT; ++i) {
+            v[i] -= mean;
+            clip<N>(v[i], n - (i * TPR + t) * N);
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
-                v[i][j] = (long)(i * TPR + t) * N + j < n ? v[i][j] - mean : 0.0f;
-                sq[0] = __builtin_fmaf(v[i][j], v[i][j], sq[0]);
-            }
+            for (int j = 0; j < N; ++j) sq[0] = __builtin_fmaf(v[i][j], v[i][j], sq[0]);
+        }
         row_sum<TPR, 1>(sq, slots, turn);
         const float rstd = 1.0f / __builtin_sqrtf(__builtin_fmaf(sq[0], a.inv_width, a.eps));
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            typename P::F o;
+            F o;
 #pragma unroll
             for (int j = 0; j < N; ++j) o[j] = __builtin_fmaf(v[i][j] * rstd, w[i][j], b[i][j]);
-            P::store(ys + (size_t)row * (size_t)n, (long)(i * TPR + t) * N, n, o);
+            P::store(ys + (size_t)row * (size_t)n, (i * TPR + t) * N, n, o);
         }
         if (t == 0 && a.mean) {
             a.mean[s * a.rows + row] = mean;
@@ -122,39 +140,52 @@ __global__ void __launch_bounds__(TPR > kNormBlock ? TPR : kNormBlock)
 hot_norm_backward_kernel(NormArgs a)
 {
     typedef Piece<T> P;
+    typedef typename P::F F;
     constexpr int N = P::N, BLOCK = TPR > kNormBlock ? TPR : kNormBlock, GROUPS = BLOCK / TPR, COLS = TPR * VPT * N;
     __shared__ float slots[2 * (TPR > 64 ? TPR / 64 : 1)][2];
     __shared__ float joined[TPR <= 64 ? BLOCK / 64 * COLS : 1];
     int turn = 0;
-    const int t = (int)threadIdx.x % TPR, s = (int)blockIdx.y;
-    const long n = a.width;
+    const int t = (int)threadIdx.x % TPR, s = (int)blockIdx.y, n = (int)a.width;
     const T *const xs = static_cast<const T *>(a.x) + (size_t)s * (size_t)a.x_sample;
     const T *const dys = static_cast<const T *>(a.dy) + (size_t)s * (size_t)a.y_sample;
     T *const dxs = static_cast<T *>(a.out) + (size_t)s * (size_t)a.rows * (size_t)n;
-    typename P::F w[VPT], dw[VPT], db[VPT];
+    const long stride = (long)gridDim.x * GROUPS;
+    long row = (long)blockIdx.x * GROUPS + threadIdx.x / TPR;
+    typename P::V next_x[VPT], next_dy[VPT];
+    float next_mean = 0.0f, next_rstd = 0.0f;
+    auto ask = [&](long r) {
+        if (r >= a.rows) return;
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) {
+            next_x[i] = P::take(xs + (size_t)r * (size_t)a.ldx, (i * TPR + t) * N, n);
+            next_dy[i] = P::take(dys + (size_t)r * (size_t)a.ldy, (i * TPR + t) * N, n);
+        }
+        next_mean = a.mean[s * a.rows + r];
+        next_rstd = a.rstd[s * a.rows + r];
+    };
+    ask(row);
+    F w[VPT], dw[VPT], db[VPT];
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-        const long at = (long)(i * TPR + t) * N;
-        dw[i] = db[i] = typename P::F(0.0f);
-        if (a.w) w[i] = load_as<N, typename P::F>(a.w, a.w_type, s * a.w_sample + at, s * a.w_sample + n);
-        else w[i] = typename P::F(1.0f);
+        dw[i] = db[i] = F(0.0f);
+        w[i] = a.w ? load_as<N, F>(a.w, a.w_type, s * a.w_sample + (i * TPR + t) * N, s * a.w_sample + n) : F(1.0f);
     }
-    for (long row = (long)blockIdx.x * GROUPS + threadIdx.x / TPR; row < a.rows; row += (long)gridDim.x * GROUPS) {
-        const T *const x = xs + (size_t)row * (size_t)a.ldx, *const dy = dys + (size_t)row * (size_t)a.ldy;
-        const float mean = a.mean[s * a.rows + row], rstd = a.rstd[s * a.rows + row];
-        typename P::F h[VPT], u[VPT];
+    for (; row < a.rows; row += stride) {
+        F h[VPT], u[VPT];
+        const float mean = next_mean, rstd = next_rstd;
         float sum[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            h[i] = P::load(x, (long)(i * TPR + t) * N, n);
-            u[i] = P::load(dy, (long)(i * TPR + t) * N, n);
+            u[i] = __builtin_convertvector(next_dy[i], F);
+            h[i] = (__builtin_convertvector(next_x[i], F) - mean) * rstd;
+            // (behind the row's end dy is zero, and h is made so: the row's own statistics need not be finite)
+            clip<N>(h[i], n - (i * TPR + t) * N);
         }
+        ask(row + stride);
 #pragma unroll
         for (int i = 0; i < VPT; ++i)
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                // (behind the row's end dy is zero, and h is made so: the row's own statistics need not be finite)
-                h[i][j] = (long)(i * TPR + t) * N + j < n ? (h[i][j] - mean) * rstd : 0.0f;
                 db[i][j] += u[i][j];
                 dw[i][j] = __builtin_fmaf(u[i][j], h[i][j], dw[i][j]);
                 u[i][j] *= w[i][j];
@@ -166,17 +197,17 @@ hot_norm_backward_kernel(NormArgs a)
         const float c1 = sum[0] * a.inv_width, c2 = sum[1] * a.inv_width;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            typename P::F o;
+            F o;
 #pragma unroll
             for (int j = 0; j < N; ++j) o[j] = rstd * (u[i][j] - __builtin_fmaf(h[i][j], c2, c1));
-            P::store(dxs + (size_t)row * (size_t)n, (long)(i * TPR + t) * N, n, o);
+            P::store(dxs + (size_t)row * (size_t)n, (i * TPR + t) * N, n, o);
         }
     }
     if (!a.parts) return;
     float *const part = a.parts + ((size_t)s * gridDim.x + blockIdx.x) * 2 * (size_t)n;
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
-        typename P::F (&v)[VPT] = which ? db : dw;
+        F (&v)[VPT] = which ? db : dw;
         if constexpr (TPR > 64) {
 #pragma unroll
             for (int i = 0; i < VPT; ++i)
@@ -343,21 +374,23 @@ hot_norm_join_kernel(const float *__restrict__ parts, long count, long width, lo
 
 // ---------------------------------------------------------------------------------
 // Host side.  Threads to a row and pieces to a thread: the fewest threads, since a thread's own additions are cheaper than those across
-// threads, as long as at most four pieces lie in its registers.
+// threads, as long as its elements fit its registers (65536 x 1024 bf16 backward: 64 threads 87 us, 256 threads 106).
 
 struct NormShape {
     int tpr, vpt;        // 0: the wide kernels
     long groups;         // rows that a workgroup holds at once
 };
 
-// (the backward pass holds five numbers per element where the forward pass holds three: with 1024 threads eight elements a thread fit)
-constexpr bool norm_fits(bool backward, int tpr, int vpt, int per) { return !backward || tpr < 1024 || vpt * per <= 8; }
+// Elements of a thread that fit: the backward pass holds seven numbers for each, the forward pass four.  In workgroups of 256 threads on
+// the backward pass takes eight (65536 x 4096 bf16 on 512 x 8: 310 us; sixteen on 256 threads spill where four waves share a
+// SIMD, 529 us, and leave two waves otherwise; 32768 x 8192 on 256 x 32 499 us, on 1024 x 8 314), the forward pass sixteen (eight: 262 us for 244).
+constexpr bool norm_fits(bool backward, int tpr, int vpt, int per) { return vpt * per <= (tpr < 256 ? 16 : (backward ? 8 : 16)); }
 
 NormShape norm_shape(bool backward, int type, long width)
 {
     const int per = 16 / type_bytes(type);
     const long pieces = (width + per - 1) / per;
-    for (int tpr : {16, 64, 256, 1024})
+    for (int tpr : {16, 64, 256, 512, 1024})
         for (int vpt : {1, 2, 4})
             if (pieces <= (long)tpr * vpt && norm_fits(backward, tpr, vpt, per)) return {tpr, vpt, tpr < kNormBlock ? kNormBlock / tpr : 1};
     return {0, 0, 1};
@@ -371,7 +404,7 @@ long norm_backward_blocks(const hot_norm_desc &d)
     const NormShape h = norm_shape(true, d.dtype, d.width);
     if (!h.tpr) return d.rows < kWideRowRuns ? (d.rows > 0 ? d.rows : 1) : kWideRowRuns;
     const long want = (d.rows + h.groups - 1) / h.groups;
-    const long resident = (h.tpr > kNormBlock ? 1 : 4) * (long)kComputeUnits;
+    const long resident = (h.tpr > 512 ? 1 : (h.tpr > kNormBlock ? 2 : 4)) * (long)kComputeUnits;
     const long most = (resident + d.samples - 1) / d.samples;
     return want < 1 ? 1 : (want < most ? want : most);
 }
@@ -405,7 +438,7 @@ void norm_go(bool backward, const NormArgs &a, long blocks, int samples, hipStre
     const dim3 grid((unsigned)blocks, (unsigned)samples), block(TPR > kNormBlock ? TPR : kNormBlock);
     if (backward) {
         if constexpr (norm_fits(true, TPR, VPT, Piece<T>::N)) hot_norm_backward_kernel<T, TPR, VPT><<<grid, block, 0, s>>>(a);
-    } else hot_norm_forward_kernel<T, TPR, VPT><<<grid, block, 0, s>>>(a);
+    } else if constexpr (norm_fits(false, TPR, VPT, Piece<T>::N)) hot_norm_forward_kernel<T, TPR, VPT><<<grid, block, 0, s>>>(a);
 }
 
 template <class T, int TPR>
@@ -442,6 +475,7 @@ void norm_run(const hot_norm_desc &d, bool backward, const NormArgs &a, hipStrea
     if (h.tpr == 16) norm_go<T, 16>(h.vpt, backward, a, blocks, d.samples, s);
     else if (h.tpr == 64) norm_go<T, 64>(h.vpt, backward, a, blocks, d.samples, s);
     else if (h.tpr == 256) norm_go<T, 256>(h.vpt, backward, a, blocks, d.samples, s);
+    else if (h.tpr == 512) norm_go<T, 512>(h.vpt, backward, a, blocks, d.samples, s);
     else norm_go<T, 1024>(h.vpt, backward, a, blocks, d.samples, s);
 }
 
