@@ -323,85 +323,113 @@ struct HeadArgs {
     long dz_block, dz_plane, dz_sample;
 };
 
-// Walks the targets of this lane's rows that lie in the wave's words: f(nb, m, i, mine, weight) is called for every result (m, i) that
-// some lane's target may be, `mine` where it is this lane's.
-template <class TILE, bool LISTS, class F>
-__device__ __forceinline__ void for_targets(const HeadArgs &a, long s, int v0, const int (&place)[TILE::NB], const bool (&live)[TILE::NB], const F &f)
-{
-    const int first = v0 + TILE::m0(), low = 4 * (TILE::lane() >> 5);
-    auto meet = [&](int nb, int word, float weight) {
-        const int in = word - first;
+// This lane's rows (one in each block of 32) and where their targets are, read before the product so that nothing waits for them behind it.
+template <class TILE, bool LISTS>
+struct Rows {
+    bool live[TILE::NB];
+    int place[TILE::NB];
+    int word[TILE::NB];            // the label, or the first entry in the tile
+    float weight[TILE::NB];
+    long entry[TILE::NB];          // of the list
+    int left[TILE::NB];
+
+    __device__ __forceinline__ Rows(const HeadArgs &a, long s, int count, int v0, int r0)
+    {
 #pragma unroll
-        for (int m = 0; m < TILE::MB; ++m) {
-            if (__builtin_amdgcn_ballot_w64(in >= 32 * m && in < 32 * m + 32) == 0) continue;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) f(nb, m, i, in - low == 32 * m + 8 * (i >> 2) + (i & 3), weight);
-        }
-    };
-#pragma unroll
-    for (int nb = 0; nb < TILE::NB; ++nb) {
-        if constexpr (!LISTS) meet(nb, live[nb] ? a.label[s * a.rows + place[nb]] : -1, 1.0f);
-        else {
-            int e = 0, end = 0;
-            const int *words = a.word;
-            const float *weights = a.weight;
-            if (live[nb]) {
-                const long list = s * a.list_sample + a.row_of[s * a.rows + place[nb]];
+        for (int n = 0; n < TILE::NB; ++n) {
+            place[n] = r0 + TILE::n0() + 32 * n + (TILE::lane() & 31);
+            live[n] = place[n] < count;
+            word[n] = -1;
+            weight[n] = 0.0f;
+            entry[n] = 0;
+            left[n] = 0;
+            if (!live[n]) continue;
+            if constexpr (!LISTS) word[n] = a.label[s * a.rows + place[n]];
+            else {
+                const long list = s * a.list_sample + a.row_of[s * a.rows + place[n]];
                 const unsigned short *const start = a.start + list * (a.marks + 1);
-                const int mark = v0 / kStartStep, last = mark + TILE::BM / kStartStep;
-                e = start[mark];
-                end = start[last < a.marks ? last : a.marks];
-                words += list * a.top;
-                weights += list * a.top;
-            }
-            while (__builtin_amdgcn_ballot_w64(e < end) != 0) {
-                const bool more = e < end;
-                meet(nb, more ? words[e] : -1, more ? weights[e] : 0.0f);
-                ++e;
+                const int mark = v0 / kStartStep, last = mark + TILE::BM / kStartStep, first = start[mark];
+                entry[n] = list * a.top + first;
+                left[n] = start[last < a.marks ? last : a.marks] - first;
+                if (left[n] > 0) {
+                    word[n] = a.word[entry[n]];
+                    weight[n] = a.weight[entry[n]];
+                }
             }
         }
     }
-}
 
-// acc -> logits in units of ln 2 / T, less `minus` of their row; words beyond the vocabulary -inf
+    // f(n, m, i, mine, weight) for every result (m, n, i) of the wave that some lane's target may be; `mine` where it is this lane's
+    template <class F>
+    __device__ __forceinline__ void targets(const HeadArgs &a, int v0, const F &f)
+    {
+        const int first = v0 + TILE::m0(), low = 4 * (TILE::lane() >> 5);
+#pragma unroll
+        for (int n = 0; n < TILE::NB; ++n) {
+            auto meet = [&](int in, float w) {
+#pragma unroll
+                for (int m = 0; m < TILE::MB; ++m) {
+                    if (__builtin_amdgcn_ballot_w64(in >= 32 * m && in < 32 * m + 32) == 0) continue;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) f(n, m, i, in - low == 32 * m + 8 * (i >> 2) + (i & 3), w);
+                }
+            };
+            if constexpr (!LISTS) meet(word[n] - first, 1.0f);
+            else
+                while (__builtin_amdgcn_ballot_w64(left[n] > 0) != 0) {
+                    const int in = left[n] > 0 ? word[n] - first : -1;
+                    const float w = weight[n];
+                    ++entry[n];
+                    if (--left[n] > 0) {
+                        word[n] = a.word[entry[n]];
+                        weight[n] = a.weight[entry[n]];
+                    }
+                    meet(in, w);
+                }
+        }
+    }
+};
+
+// The bias added, words beyond the vocabulary taken out: nothing to do for most tiles
 template <class TILE>
-__device__ __forceinline__ void to_scores(const HeadArgs &a, long s, int v0, const float (&minus)[TILE::NB], f16v (&acc)[TILE::MB][TILE::NB])
+__device__ __forceinline__ void with_bias(const HeadArgs &a, long s, int v0, f16v (&acc)[TILE::MB][TILE::NB])
 {
-    const bool ragged = v0 + TILE::BM > a.vocab;
+    if (!a.bias && v0 + TILE::BM <= a.vocab) return;
 #pragma unroll
     for (int m = 0; m < TILE::MB; ++m)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            float bias = 0.0f;
+            typedef float F1 __attribute__((ext_vector_type(1)));
             const int v = v0 + TILE::m0() + 32 * m + TILE::row(i);
-            if (a.bias) {
-                typedef float F1 __attribute__((ext_vector_type(1)));
-                bias = load_as<1, F1>(a.bias, a.bias_type, s * a.bias_sample + v, s * a.bias_sample + a.vocab)[0] * a.scale;
-            }
-            const bool none = ragged && v >= a.vocab;
+            float bias = v < a.vocab ? 0.0f : -__builtin_inff();
+            if (a.bias && v < a.vocab) bias = load_as<1, F1>(a.bias, a.bias_type, s * a.bias_sample + v, s * a.bias_sample + a.vocab)[0];
 #pragma unroll
-            for (int n = 0; n < TILE::NB; ++n) {
-                const float z = __builtin_fmaf(acc[m][n][i], a.scale, bias - minus[n]);
-                acc[m][n][i] = none ? -__builtin_inff() : z;
-            }
+            for (int n = 0; n < TILE::NB; ++n) acc[m][n][i] += bias;
         }
 }
 
 __device__ __forceinline__ Matrix part(const Matrix &m, long bytes) { return {m.at + bytes, m.pitch, m.block, m.plane}; }
 
+// where a workgroup's tile of logits begins
+struct TileOf {
+    bool any;
+    int v0, r0;
+};
+
 template <class TILE>
-__device__ __forceinline__ bool head_product(const HeadArgs &a, lds_char *lds, long s, int &v0, int &r0, f16v (&acc)[TILE::MB][TILE::NB])
+__device__ __forceinline__ TileOf tile_of(const HeadArgs &a, int count)
 {
-    const int count = a.count[s];
     const Place at = place((int)blockIdx.x, (a.v_count + TILE::BM - 1) / TILE::BM, (count + TILE::BN - 1) / TILE::BN);
-    if (!at.any) return false;
-    const int in = at.m * TILE::BM;
-    v0 = a.v_begin + in;
-    r0 = at.n * TILE::BN;
-    const Operand w = {part(a.w, s * a.w_sample + in * a.w.pitch), a.v_begin + a.v_count - v0, a.width};
-    const Operand x = {part(a.x, s * a.x_sample + r0 * a.x.pitch), count - r0, a.width};
+    return {at.any, a.v_begin + at.m * TILE::BM, at.n * TILE::BN};
+}
+
+template <class TILE>
+__device__ __forceinline__ void logits(const HeadArgs &a, lds_char *lds, long s, int count, const TileOf &t, f16v (&acc)[TILE::MB][TILE::NB])
+{
+    const Operand w = {part(a.w, s * a.w_sample + (t.v0 - a.v_begin) * a.w.pitch), a.v_begin + a.v_count - t.v0, a.width};
+    const Operand x = {part(a.x, s * a.x_sample + t.r0 * a.x.pitch), count - t.r0, a.width};
     TILE::product(lds, w, x, a.width, acc);
-    return true;
+    with_bias<TILE>(a, s, t.v0, acc);
 }
 
 template <class TILE, bool LISTS>
@@ -411,20 +439,15 @@ hot_head_forward_kernel(HeadArgs a)
     constexpr int NEED = 3 * TILE::WAVES_M * TILE::BN * 4;
     __shared__ __attribute__((aligned(1024))) char memory[TILE::kLds > NEED ? TILE::kLds : NEED];
     const long s = blockIdx.y;
-    int v0, r0;
+    const int count = a.count[s];
+    const TileOf tile = tile_of<TILE>(a, count);
+    if (!tile.any) return;
+    Rows<TILE, LISTS> rows(a, s, count, tile.v0, tile.r0);
     f16v acc[TILE::MB][TILE::NB];
-    if (!head_product<TILE>(a, (lds_char *)memory, s, v0, r0, acc)) return;
-    const float zero[TILE::NB] = {};
-    to_scores<TILE>(a, s, v0, zero, acc);
+    logits<TILE>(a, (lds_char *)memory, s, count, tile, acc);
+    const int r0 = tile.r0, v0 = tile.v0;
     float dot[TILE::NB] = {};
-    int at[TILE::NB];
-    bool live[TILE::NB];
-#pragma unroll
-    for (int n = 0; n < TILE::NB; ++n) {
-        at[n] = r0 + TILE::n0() + 32 * n + (TILE::lane() & 31);
-        live[n] = at[n] < a.count[s];
-    }
-    for_targets<TILE, LISTS>(a, s, v0, at, live, [&](int n, int m, int i, bool mine, float weight) { dot[n] += mine ? weight * acc[m][n][i] : 0.0f; });
+    rows.targets(a, v0, [&](int n, int m, int i, bool mine, float weight) { dot[n] += mine ? weight * acc[m][n][i] : 0.0f; });
     float (*const part)[TILE::WAVES_M][TILE::BN] = reinterpret_cast<float (*)[TILE::WAVES_M][TILE::BN]>(memory);
 #pragma unroll
     for (int n = 0; n < TILE::NB; ++n) {
@@ -433,15 +456,15 @@ hot_head_forward_kernel(HeadArgs a)
         for (int m = 0; m < TILE::MB; ++m)
 #pragma unroll
             for (int i = 0; i < 16; ++i) most = fmaxf(most, acc[m][n][i]);
-        most = fmaxf(most, __shfl_xor(most, 32));
+        most = fmaxf(most, __shfl_xor(most, 32)) * a.scale;
         const float from = most == -__builtin_inff() ? 0.0f : most;        // (nothing but -inf: a sum of zero)
         float sum = 0.0f;
 #pragma unroll
         for (int m = 0; m < TILE::MB; ++m)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sum += __builtin_amdgcn_exp2f(acc[m][n][i] - from);
+            for (int i = 0; i < 16; ++i) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[m][n][i], a.scale, -from));
         sum += __shfl_xor(sum, 32);
-        dot[n] += __shfl_xor(dot[n], 32);
+        dot[n] = (dot[n] + __shfl_xor(dot[n], 32)) * a.scale;
         if (TILE::lane() < 32) {
             const int wm = TILE::wave() / TILE::WAVES_N, col = TILE::n0() + 32 * n + TILE::lane();
             part[0][wm][col] = most;
@@ -451,7 +474,7 @@ hot_head_forward_kernel(HeadArgs a)
     }
     __syncthreads();
     for (int col = (int)threadIdx.x; col < TILE::BN; col += TILE::THREADS) {
-        if (r0 + col >= a.count[s]) break;
+        if (r0 + col >= count) break;
         float most = part[0][0][col];
 #pragma unroll
         for (int k = 1; k < TILE::WAVES_M; ++k) most = fmaxf(most, part[0][k][col]);
@@ -476,33 +499,33 @@ hot_head_dz_kernel(HeadArgs a)
     constexpr int PITCH = TILE::BM * 2 + 16, NEED = TILE::BN * PITCH;       // (16 bytes on: rows of a column of lanes lie in different banks)
     __shared__ __attribute__((aligned(1024))) char memory[TILE::kLds > NEED ? TILE::kLds : NEED];
     const long s = blockIdx.y;
-    int v0, r0;
-    f16v acc[TILE::MB][TILE::NB];
-    if (!head_product<TILE>(a, (lds_char *)memory, s, v0, r0, acc)) return;
-    int at[TILE::NB];
-    bool live[TILE::NB];
+    const int count = a.count[s];
+    const TileOf tile = tile_of<TILE>(a, count);
+    if (!tile.any) return;
+    Rows<TILE, LISTS> rows(a, s, count, tile.v0, tile.r0);
     float hi[TILE::NB], lo[TILE::NB], g[TILE::NB];
     const float to_scale = a.to_scale[2 * s];
 #pragma unroll
     for (int n = 0; n < TILE::NB; ++n) {
-        at[n] = r0 + TILE::n0() + 32 * n + (TILE::lane() & 31);
-        live[n] = at[n] < a.count[s];
-        hi[n] = live[n] ? a.hi[s * a.rows + at[n]] : __builtin_inff();
-        lo[n] = live[n] ? a.lo[s * a.rows + at[n]] : 0.0f;
-        g[n] = live[n] ? a.grad[s * a.rows + at[n]] * to_scale : 0.0f;
+        const long at = s * a.rows + rows.place[n];
+        hi[n] = rows.live[n] ? a.hi[at] : __builtin_inff();
+        lo[n] = rows.live[n] ? a.lo[at] : 0.0f;
+        g[n] = rows.live[n] ? a.grad[at] * to_scale : 0.0f;
     }
-    to_scores<TILE>(a, s, v0, hi, acc);
+    f16v acc[TILE::MB][TILE::NB];
+    logits<TILE>(a, (lds_char *)memory, s, count, tile, acc);
+    const int v0 = tile.v0, r0 = tile.r0;
 #pragma unroll
     for (int m = 0; m < TILE::MB; ++m)
 #pragma unroll
         for (int n = 0; n < TILE::NB; ++n)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
+                const float z = __builtin_fmaf(acc[m][n][i], a.scale, -hi[n]);
                 // (the low part of lse is below the rounding of 16-bit results)
-                const float z = TILE::PIECES == 1 ? acc[m][n][i] : acc[m][n][i] - lo[n];
-                acc[m][n][i] = __builtin_amdgcn_exp2f(z);
+                acc[m][n][i] = __builtin_amdgcn_exp2f(TILE::PIECES == 1 ? z : z - lo[n]);
             }
-    for_targets<TILE, LISTS>(a, s, v0, at, live, [&](int n, int m, int i, bool mine, float weight) { acc[m][n][i] -= mine ? weight : 0.0f; });
+    rows.targets(a, v0, [&](int n, int m, int i, bool mine, float weight) { acc[m][n][i] -= mine ? weight : 0.0f; });
     // to rows of words, piece by piece, through LDS
     typedef typename TILE::T T;
     typedef T V4 __attribute__((ext_vector_type(4)));
