@@ -22,7 +22,7 @@ namespace {
 
 constexpr int kComputeUnits = 256;
 constexpr int kMostTop = 1024;           // entries of a row (they are sorted in LDS)
-constexpr int kStartStep = 128;          // words between the marks into a row's sorted entries
+constexpr int kStartStep = 64;           // words between the marks into a row's sorted entries
 constexpr float kHalfScale = 4096.0f;    // fp16 logits' gradients are held times this: a probability of 1e-11 still counts, 16 x 4096 does not overflow
 
 inline __host__ __device__ long up(long n, long to) { return (n + to - 1) / to * to; }
@@ -171,18 +171,17 @@ struct RowArgs {
     float *scale;                  // [samples, 2]: what gradients are multiplied with, and what results are multiplied with in turn
 };
 
-constexpr int kRowBlock = 1024;
-
-__global__ void __launch_bounds__(kRowBlock)
-hot_head_rows_kernel(RowArgs a)
+// The rows of sample s that count, in order: how many, and (WRITE) the arrays by place.  `map` (LDS, rows of them, or null): the row at a place.
+template <int BLOCK, bool WRITE>
+__device__ __forceinline__ int find_rows(const RowArgs &a, long s, unsigned short *map)
 {
-    __shared__ int totals[kRowBlock / 64];
-    __shared__ float most[kRowBlock / 64];
+    __shared__ int totals[2][BLOCK / 64];
+    __shared__ float most[BLOCK / 64];
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
-    const long s = blockIdx.x, base = s * a.rows;
-    int before = 0;
+    const long base = s * a.rows;
+    int before = 0, turn = 0;
     float largest = 0.0f;
-    for (long r0 = 0; r0 < a.rows; r0 += kRowBlock) {
+    for (long r0 = 0; r0 < a.rows; r0 += BLOCK) {
         const long row = r0 + threadIdx.x;
         bool counts = false;
         int label = -1;
@@ -195,45 +194,56 @@ hot_head_rows_kernel(RowArgs a)
             }
         }
         const unsigned long long mask = __builtin_amdgcn_ballot_w64(counts);
-        if (lane == 0) totals[wave] = __builtin_popcountll(mask);
+        if (lane == 0) totals[turn][wave] = __builtin_popcountll(mask);
         __syncthreads();
         int at = before + __builtin_popcountll(mask & ((1ull << lane) - 1));
 #pragma unroll
-        for (int i = 0; i < kRowBlock / 64; ++i) {
-            if (i < wave) at += totals[i];
-            before += totals[i];
+        for (int i = 0; i < BLOCK / 64; ++i) {
+            if (i < wave) at += totals[turn][i];
+            before += totals[turn][i];
         }
-        if (row < a.rows) {
-            a.place_of[base + row] = counts ? at : -1;
-            if (counts) {
-                a.row_of[base + at] = (int)row;
-                if (a.label) a.label[base + at] = label;
-                if (a.lse) {
-                    const double two = a.lse[base + row] * (1.0 / 0.69314718055994530942);
-                    const float hi = (float)two;
-                    a.hi[base + at] = hi;
-                    a.lo[base + at] = __builtin_isfinite(hi) ? (float)(two - (double)hi) : 0.0f;
-                    float g = a.g[s * a.g_sample + row * a.g_row];
-                    if (!a.list_count && label < 0) g = __builtin_nanf("");
-                    a.grad[base + at] = g;
-                    largest = fmaxf(largest, __builtin_fabsf(g));
+        turn ^= 1;
+        if (row < a.rows && counts && map) map[at] = (unsigned short)row;
+        if constexpr (WRITE)
+            if (row < a.rows) {
+                a.place_of[base + row] = counts ? at : -1;
+                if (counts) {
+                    a.row_of[base + at] = (int)row;
+                    if (a.label) a.label[base + at] = label;
+                    if (a.lse) {
+                        const double two = a.lse[base + row] * (1.0 / 0.69314718055994530942);
+                        const float hi = (float)two;
+                        a.hi[base + at] = hi;
+                        a.lo[base + at] = __builtin_isfinite(hi) ? (float)(two - (double)hi) : 0.0f;
+                        float g = a.g[s * a.g_sample + row * a.g_row];
+                        if (!a.list_count && label < 0) g = __builtin_nanf("");
+                        a.grad[base + at] = g;
+                        largest = fmaxf(largest, __builtin_fabsf(g));
+                    }
                 }
             }
-        }
-        __syncthreads();
     }
-    if (threadIdx.x == 0) a.count[s] = before;
-    if (!a.lse) return;
-    largest = wave_max(largest);
-    if (lane == 0) most[wave] = largest;
-    __syncthreads();
-    if (threadIdx.x != 0) return;
+    if constexpr (WRITE) {
+        if (threadIdx.x == 0) a.count[s] = before;
+        if (a.lse) {
+            largest = wave_max(largest);
+            if (lane == 0) most[wave] = largest;
+            __syncthreads();
+            if (threadIdx.x == 0) {
 #pragma unroll
-    for (int i = 0; i < kRowBlock / 64; ++i) largest = fmaxf(largest, most[i]);
-    const bool usable = largest > 1e-30f && largest < 1e30f;
-    a.scale[2 * s] = usable ? a.scale_to / largest : a.scale_to;
-    a.scale[2 * s + 1] = usable ? largest / a.scale_to : 1.0f / a.scale_to;
+                for (int i = 0; i < BLOCK / 64; ++i) largest = fmaxf(largest, most[i]);
+                const bool usable = largest > 1e-30f && largest < 1e30f;
+                a.scale[2 * s] = usable ? a.scale_to / largest : a.scale_to;
+                a.scale[2 * s + 1] = usable ? largest / a.scale_to : 1.0f / a.scale_to;
+            }
+        }
+    }
+    return before;
 }
+
+constexpr int kRowBlock = 1024;
+
+__global__ void __launch_bounds__(kRowBlock) hot_head_rows_kernel(RowArgs a) { find_rows<kRowBlock, true>(a, blockIdx.x, nullptr); }
 
 // --------------------------------------------------------------------------- operands as the tiles read them
 
@@ -242,8 +252,8 @@ struct PackArgs {
     long from_row, from_sample;    // elements
     const int *row_of;             // [samples, rows] or null: rows as they are
     const int *count;              // with row_of: how many of them
-    long rows, map_sample;
-    int width, chunks;             // chunks = width / 8, rounded up
+    long rows;
+    int width;
     char *to;                      // [samples], pieces `plane` apart: blocks of `columns` columns, each all rows
     long to_sample, plane, block;
     int columns;
@@ -260,27 +270,29 @@ __device__ __forceinline__ void split_bf16(float x, __bf16 (&p)[3])
     }
 }
 
+// Workgroup `first` of `blocks`.  A wave packs a run of rows of one block of columns: what it writes is one run of memory.
 template <class T>
-__global__ void __launch_bounds__(256)
-hot_head_pack_kernel(PackArgs a)
+__device__ __forceinline__ void pack(const PackArgs &a, long s, long n, const unsigned short *map, long first, long blocks)
 {
-    const long s = blockIdx.y, n = a.row_of ? a.count[s] : a.rows;
-    const long items = n * a.chunks;
-    for (long item = (long)blockIdx.x * 256 + threadIdx.x; item < items; item += (long)gridDim.x * 256) {
-        const long place = item / a.chunks;
-        const int chunk = (int)(item - place * a.chunks);
-        const long row = a.row_of ? a.row_of[s * a.map_sample + place] : place;
+    const int per_row = a.columns / 8, in_block = (int)threadIdx.x % per_row;
+    const int column_blocks = (a.width + a.columns - 1) / a.columns;
+    const long rows_at_once = 256 / per_row, row_groups = (n + rows_at_once - 1) / rows_at_once, items = row_groups * column_blocks;
+    for (long item = first; item < items; item += blocks) {
+        const long place = item / column_blocks * rows_at_once + threadIdx.x / per_row, block = item % column_blocks;
+        const int col = (int)block * a.columns + in_block * 8;
+        if (place >= n || col >= a.width) continue;
+        const long row = map ? map[place] : (a.row_of ? a.row_of[s * a.rows + place] : place);
         const T *const from = static_cast<const T *>(a.from) + (size_t)s * (size_t)a.from_sample + (size_t)row * (size_t)a.from_row;
-        char *const to = a.to + (size_t)s * (size_t)a.to_sample + (size_t)(chunk * 8 / a.columns) * (size_t)a.block + (size_t)place * (size_t)(a.columns * 2) + (size_t)(chunk * 8 % a.columns * 2);
+        char *const to = a.to + (size_t)s * (size_t)a.to_sample + (size_t)block * (size_t)a.block + ((size_t)place * (size_t)per_row + (size_t)in_block) * 16;
         if constexpr (sizeof(T) == 2) {
             typedef T V __attribute__((ext_vector_type(8)));
-            *reinterpret_cast<V *>(to) = __builtin_convertvector(Piece<T>::load(from, chunk * 8L, a.width), V);
+            *reinterpret_cast<V *>(to) = Piece<T>::take(from, col, a.width);
         } else {
             typedef __bf16 V __attribute__((ext_vector_type(8)));
             V p[3];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const typename Piece<T>::F v = Piece<T>::load(from, chunk * 8L + 4 * h, a.width);
+                const typename Piece<T>::F v = Piece<T>::load(from, col + 4 * h, a.width);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     __bf16 q[3];
@@ -293,6 +305,28 @@ hot_head_pack_kernel(PackArgs a)
             for (int i = 0; i < 3; ++i) *reinterpret_cast<V *>(to + (size_t)i * (size_t)a.plane) = p[i];
         }
     }
+}
+
+template <class T>
+__global__ void __launch_bounds__(256) hot_head_pack_kernel(PackArgs a)
+{
+    const long s = blockIdx.y;
+    pack<T>(a, s, a.row_of ? a.count[s] : a.rows, nullptr, blockIdx.x, gridDim.x);
+}
+
+// Up to kFewRows rows: rows found, features packed and (the first piece's) weights packed in one launch.  Every workgroup that packs
+// features finds the rows by itself; the first one writes them down.
+constexpr int kFewRows = 1024;
+
+template <class T>
+__global__ void __launch_bounds__(256) hot_head_prepare_kernel(RowArgs rows, PackArgs x, PackArgs w, int x_blocks)
+{
+    __shared__ unsigned short map[kFewRows];
+    const long s = blockIdx.y;
+    if ((int)blockIdx.x >= x_blocks) return pack<T>(w, s, w.rows, nullptr, (int)blockIdx.x - x_blocks, (int)gridDim.x - x_blocks);
+    const int count = blockIdx.x == 0 ? find_rows<256, true>(rows, s, map) : find_rows<256, false>(rows, s, map);
+    __syncthreads();
+    pack<T>(x, s, count, map, blockIdx.x, x_blocks);
 }
 
 // --------------------------------------------------------------------------- logits: statistics, or their gradients
@@ -321,6 +355,8 @@ struct HeadArgs {
     const float *hi, *lo, *grad, *to_scale;
     char *dz;                      // [sample] blocks of BK words, each all places
     long dz_block, dz_plane, dz_sample;
+    float *sums;                   // for db, or null: dz summed over a tile's rows, [sample][tile of rows][word of the piece]
+    int row_tiles, v_piece;
 };
 
 // This lane's rows (one in each block of 32) and where their targets are, read before the product so that nothing waits for them behind it.
@@ -349,6 +385,7 @@ struct Rows {
                 const long list = s * a.list_sample + a.row_of[s * a.rows + place[n]];
                 const unsigned short *const start = a.start + list * (a.marks + 1);
                 const int mark = v0 / kStartStep, last = mark + TILE::BM / kStartStep, first = start[mark];
+                static_assert(TILE::BM % kStartStep == 0, "");
                 entry[n] = list * a.top + first;
                 left[n] = start[last < a.marks ? last : a.marks] - first;
                 if (left[n] > 0) {
@@ -390,21 +427,31 @@ struct Rows {
     }
 };
 
-// The bias added, words beyond the vocabulary taken out: nothing to do for most tiles
+// The bias of a tile's words, -inf for words beyond the vocabulary: loaded before the product, added behind it; most tiles have neither
 template <class TILE>
-__device__ __forceinline__ void with_bias(const HeadArgs &a, long s, int v0, f16v (&acc)[TILE::MB][TILE::NB])
+__device__ __forceinline__ bool ask_bias(const HeadArgs &a, long s, int v0, float *bias)
 {
-    if (!a.bias && v0 + TILE::BM <= a.vocab) return;
+    if (!a.bias && v0 + TILE::BM <= a.vocab) return false;
+    for (int i = (int)threadIdx.x; i < TILE::BM; i += TILE::THREADS) {
+        typedef float F1 __attribute__((ext_vector_type(1)));
+        const int v = v0 + i;
+        float b = v < a.vocab ? 0.0f : -__builtin_inff();
+        if (a.bias && v < a.vocab) b = load_as<1, F1>(a.bias, a.bias_type, s * a.bias_sample + v, s * a.bias_sample + a.vocab)[0];
+        bias[i] = b;
+    }
+    return true;
+}
+
+template <class TILE>
+__device__ __forceinline__ void add_bias(const float *bias, f16v (&acc)[TILE::MB][TILE::NB])
+{
 #pragma unroll
     for (int m = 0; m < TILE::MB; ++m)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            typedef float F1 __attribute__((ext_vector_type(1)));
-            const int v = v0 + TILE::m0() + 32 * m + TILE::row(i);
-            float bias = v < a.vocab ? 0.0f : -__builtin_inff();
-            if (a.bias && v < a.vocab) bias = load_as<1, F1>(a.bias, a.bias_type, s * a.bias_sample + v, s * a.bias_sample + a.vocab)[0];
+            const float b = bias[TILE::m0() + 32 * m + TILE::row(i)];
 #pragma unroll
-            for (int n = 0; n < TILE::NB; ++n) acc[m][n][i] += bias;
+            for (int n = 0; n < TILE::NB; ++n) acc[m][n][i] += b;
         }
 }
 
@@ -424,12 +471,13 @@ __device__ __forceinline__ TileOf tile_of(const HeadArgs &a, int count)
 }
 
 template <class TILE>
-__device__ __forceinline__ void logits(const HeadArgs &a, lds_char *lds, long s, int count, const TileOf &t, f16v (&acc)[TILE::MB][TILE::NB])
+__device__ __forceinline__ void logits(const HeadArgs &a, char *lds, float *bias, long s, int count, const TileOf &t, f16v (&acc)[TILE::MB][TILE::NB])
 {
+    const bool biased = ask_bias<TILE>(a, s, t.v0, bias);
     const Operand w = {part(a.w, s * a.w_sample + (t.v0 - a.v_begin) * a.w.pitch), a.v_begin + a.v_count - t.v0, a.width};
     const Operand x = {part(a.x, s * a.x_sample + t.r0 * a.x.pitch), count - t.r0, a.width};
-    TILE::product(lds, w, x, a.width, acc);
-    with_bias<TILE>(a, s, t.v0, acc);
+    TILE::product((lds_char *)lds, w, x, a.width, acc);        // (with barriers between the writing of the bias and this)
+    if (biased) add_bias<TILE>(bias, acc);
 }
 
 template <class TILE, bool LISTS>
@@ -437,14 +485,16 @@ __global__ void __launch_bounds__(TILE::THREADS)
 hot_head_forward_kernel(HeadArgs a)
 {
     constexpr int NEED = 3 * TILE::WAVES_M * TILE::BN * 4;
-    __shared__ __attribute__((aligned(1024))) char memory[TILE::kLds > NEED ? TILE::kLds : NEED];
+    // (one array: beside a second one the compiler would wait for every load in flight before it reads either)
+    constexpr int ROOM = TILE::kLds > NEED ? TILE::kLds : NEED;
+    __shared__ __attribute__((aligned(1024))) char memory[ROOM + TILE::BM * 4];
     const long s = blockIdx.y;
     const int count = a.count[s];
     const TileOf tile = tile_of<TILE>(a, count);
     if (!tile.any) return;
     Rows<TILE, LISTS> rows(a, s, count, tile.v0, tile.r0);
     f16v acc[TILE::MB][TILE::NB];
-    logits<TILE>(a, (lds_char *)memory, s, count, tile, acc);
+    logits<TILE>(a, memory, reinterpret_cast<float *>(memory + ROOM), s, count, tile, acc);
     const int r0 = tile.r0, v0 = tile.v0;
     float dot[TILE::NB] = {};
     rows.targets(a, v0, [&](int n, int m, int i, bool mine, float weight) { dot[n] += mine ? weight * acc[m][n][i] : 0.0f; });
@@ -497,7 +547,9 @@ __global__ void __launch_bounds__(TILE::THREADS)
 hot_head_dz_kernel(HeadArgs a)
 {
     constexpr int PITCH = TILE::BM * 2 + 16, NEED = TILE::BN * PITCH;       // (16 bytes on: rows of a column of lanes lie in different banks)
-    __shared__ __attribute__((aligned(1024))) char memory[TILE::kLds > NEED ? TILE::kLds : NEED];
+    // (one array: beside a second one the compiler would wait for every load in flight before it reads either)
+    constexpr int ROOM = TILE::kLds > NEED ? TILE::kLds : NEED;
+    __shared__ __attribute__((aligned(1024))) char memory[ROOM + TILE::BM * 4];
     const long s = blockIdx.y;
     const int count = a.count[s];
     const TileOf tile = tile_of<TILE>(a, count);
@@ -513,7 +565,7 @@ hot_head_dz_kernel(HeadArgs a)
         g[n] = rows.live[n] ? a.grad[at] * to_scale : 0.0f;
     }
     f16v acc[TILE::MB][TILE::NB];
-    logits<TILE>(a, (lds_char *)memory, s, count, tile, acc);
+    logits<TILE>(a, memory, reinterpret_cast<float *>(memory + ROOM), s, count, tile, acc);
     const int v0 = tile.v0, r0 = tile.r0;
 #pragma unroll
     for (int m = 0; m < TILE::MB; ++m)
@@ -531,6 +583,8 @@ hot_head_dz_kernel(HeadArgs a)
     typedef T V4 __attribute__((ext_vector_type(4)));
     typedef T V8 __attribute__((ext_vector_type(8)));
     constexpr int BK = TILE::BK;
+    constexpr int PAIRS = TILE::BM / 2, RUNS = TILE::THREADS / PAIRS;
+    float sum[2] = {0.0f, 0.0f};
     char *const out = a.dz + (size_t)s * (size_t)a.dz_sample + (size_t)((v0 - a.v_begin) / BK) * (size_t)a.dz_block + (size_t)r0 * (BK * 2);
 #pragma unroll
     for (int p = 0; p < TILE::PIECES; ++p) {
@@ -558,6 +612,29 @@ hot_head_dz_kernel(HeadArgs a)
             *reinterpret_cast<V8 *>(out + (size_t)p * (size_t)a.dz_plane + (size_t)block * (size_t)a.dz_block + in * 16) =
                 *reinterpret_cast<const V8 *>(memory + row * PITCH + block * (BK * 2) + chunk * 16);
         }
+        if (a.sums) {       // two words to a thread, a run of rows each
+            typedef T V2 __attribute__((ext_vector_type(2)));
+            const int pair = (int)threadIdx.x % PAIRS, run = (int)threadIdx.x / PAIRS;
+#pragma unroll 8
+            for (int r = run; r < TILE::BN; r += RUNS) {
+                const V2 v = *reinterpret_cast<const V2 *>(memory + r * PITCH + pair * 4);
+                sum[0] += (float)v[0];
+                sum[1] += (float)v[1];
+            }
+        }
+    }
+    if (!a.sums) return;
+    __syncthreads();
+    float (*const runs)[TILE::BM] = reinterpret_cast<float (*)[TILE::BM]>(memory);
+    const int pair = (int)threadIdx.x % PAIRS;
+    runs[threadIdx.x / PAIRS][2 * pair] = sum[0];
+    runs[threadIdx.x / PAIRS][2 * pair + 1] = sum[1];
+    __syncthreads();
+    for (int i = (int)threadIdx.x; i < TILE::BM; i += TILE::THREADS) {
+        float total = 0.0f;
+#pragma unroll
+        for (int k = 0; k < RUNS; ++k) total += runs[k][i];
+        a.sums[((size_t)s * (size_t)a.row_tiles + (size_t)(r0 / TILE::BN)) * (size_t)a.v_piece + (size_t)(v0 - a.v_begin + i)] = total;
     }
 }
 
@@ -578,37 +655,44 @@ struct JoinArgs {
 __global__ void __launch_bounds__(256)
 hot_head_join_kernel(JoinArgs a)
 {
-    __shared__ float sm[3][256];
+    __shared__ float tops[256];
+    __shared__ double totals[256], dots[256];
     const int per = 256 / a.lanes, r = (int)threadIdx.x % per, lane = (int)threadIdx.x / per;
     const long s = blockIdx.y, row = (long)blockIdx.x * per + r;
     const int at = row < a.rows ? a.place_of[s * a.rows + row] : -1;
-    float most = -__builtin_inff(), sum = 0.0f, dot = 0.0f;
+    float most = -__builtin_inff(), sum = 0.0f, partial = 0.0f;
     if (at >= 0)
+#pragma unroll 4
         for (int k = lane; k < a.tiles; k += a.lanes) {
             const float *const p = a.partials + ((size_t)s * (size_t)a.tiles + (size_t)k) * 3 * (size_t)a.places + (size_t)at;
             const float m = p[0], v = p[a.places], top = m > most || m != m ? m : most;
             sum = top == -__builtin_inff() ? sum + v : sum * __builtin_amdgcn_exp2f(most - top) + v * __builtin_amdgcn_exp2f(m - top);
             most = top;
-            dot += p[2 * a.places];
+            partial += p[2 * a.places];
         }
-    sm[0][threadIdx.x] = most;
-    sm[1][threadIdx.x] = sum;
-    sm[2][threadIdx.x] = dot;
-    __syncthreads();
+    double total = (double)sum, d = (double)partial;
+    // the row's threads, in halves
+    for (int half = a.lanes / 2; half > 0; half /= 2) {
+        if (lane >= half && lane < 2 * half) {
+            tops[threadIdx.x] = most;
+            totals[threadIdx.x] = total;
+            dots[threadIdx.x] = d;
+        }
+        __syncthreads();
+        if (lane < half) {
+            const int other = (int)threadIdx.x + half * per;
+            const float m = tops[other], top = m > most || m != m ? m : most;
+            total = top == -__builtin_inff() ? total + totals[other]
+                                             : total * (double)__builtin_amdgcn_exp2f(most - top) + totals[other] * (double)__builtin_amdgcn_exp2f(m - top);
+            most = top;
+            d += dots[other];
+        }
+        __syncthreads();
+    }
     if (lane || row >= a.rows) return;
     float loss = 0.0f;
     double lse = 0.0;
     if (at >= 0) {
-        for (int k = 1; k < a.lanes; ++k) {
-            const float m = sm[0][k * per + r];
-            most = m > most || m != m ? m : most;
-        }
-        double total = 0.0, d = 0.0;
-        for (int k = 0; k < a.lanes; ++k) {
-            const float m = sm[0][k * per + r];
-            total += (double)sm[1][k * per + r] * (m == most ? 1.0 : exp2((double)m - (double)most));
-            d += (double)sm[2][k * per + r];
-        }
         const double two = (double)most + log2(total);
         lse = two * 0.69314718055994530942;
         double entropy = 0.0, weight = 1.0;
@@ -719,11 +803,10 @@ hot_head_dw_kernel(GradArgs a)
     }
 }
 
-// db of one piece: sums of dz over the rows, 128 words and 16 runs of rows to a workgroup
+// db of one piece: the sums of its tiles of rows added up
 struct BiasArgs {
-    Matrix dz;
-    long dz_sample;
-    int v_begin, v_count;
+    const float *sums;
+    int row_tiles, tile_rows, v_piece, v_begin, v_count;
     const int *count;
     const float *scale;
     float temperature;
@@ -732,31 +815,15 @@ struct BiasArgs {
     int type;
 };
 
-template <class T, int PIECES, int BK>
 __global__ void __launch_bounds__(256)
 hot_head_db_kernel(BiasArgs a)
 {
-    __shared__ float runs[16][128];
-    typedef T V8 __attribute__((ext_vector_type(8)));
     const long s = blockIdx.y;
-    const int lane = (int)threadIdx.x & 15, run = (int)threadIdx.x >> 4, in = (int)blockIdx.x * 128 + lane * 8, count = a.count[s];
-    float sum[8] = {};
-    if (in < a.v_count)        // (rows of dz reach to the next multiple of 256 words)
-        for (int r = run; r < count; r += 16)
-#pragma unroll
-            for (int p = PIECES - 1; p >= 0; --p) {
-                const V8 v = *reinterpret_cast<const V8 *>(a.dz.at + s * a.dz_sample + p * a.dz.plane + in / BK * a.dz.block + r * a.dz.pitch + in % BK * 2);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) sum[j] += (float)v[j];
-            }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) runs[run][lane * 8 + j] = sum[j];
-    __syncthreads();
-    const int word = (int)blockIdx.x * 128 + (int)threadIdx.x;
-    if (threadIdx.x >= 128 || word >= a.v_count) return;
+    const int word = (int)blockIdx.x * 256 + (int)threadIdx.x, tiles = (a.count[s] + a.tile_rows - 1) / a.tile_rows;
+    if (word >= a.v_count) return;
     float total = 0.0f;
-#pragma unroll
-    for (int k = 0; k < 16; ++k) total += runs[k][threadIdx.x];
+#pragma unroll 8
+    for (int k = 0; k < tiles; ++k) total += a.sums[((size_t)s * (size_t)a.row_tiles + (size_t)k) * (size_t)a.v_piece + (size_t)word];
     store_as(a.out, a.type, s * a.out_sample + a.v_begin + word, total * (a.scale[2 * s + 1] * a.temperature));
 }
 
@@ -808,22 +875,27 @@ __global__ void __launch_bounds__(256) hot_head_zero_kernel(char *p, long bytes)
 // ---------------------------------------------------------------------------------
 // Host side.
 
+constexpr long kSmallTiles = 128;                        // tiles of 128 x 128 below which 64 x 64 are taken
 constexpr long kMostTiles = 1L << 22;                    // of 256 x 256 logits (one grid dimension holds fewer than 2^32 threads)
 constexpr int64_t kPieceBytes = (int64_t)256 << 20;      // of dz and packed weights: what the memory-side cache holds
+
+// Sizes of tiles (of logits: words x rows): 256 x 32 for up to 32 rows, 64 x 64 and 128 x 128 where larger ones leave the chip empty, 256 x 256
+// (256 x 128 in three pieces).
+enum { kFew, kSmall, kMiddle, kLarge };
 
 struct HeadPlan {
     int pieces;              // of an element
     bool pack_w;
-    int chunks;              // 16-byte chunks of a packed row
     int columns;             // of a block of what is packed
     long row_bytes;          // of a packed row: whole blocks
     long places;
     int v_piece, v_pieces;   // words of a piece
-    int size;                // 0: tiles for few rows, 1: 128 x 128, 2: large ones
-    int v_tile;              // words of a tile of logits
+    int size;                // kFew ... kLarge
+    int v_tile, r_tile;      // words and rows of a tile of logits
+    int row_tiles;
     int splits, split_depth; // runs of words of a piece, and their length
     // where things lie in the workspace
-    int64_t word, weight, list_count, sums, start, count, row_of, place_of, label, hi, lo, grad, scale, x, w, dz, partials, dx, bytes;
+    int64_t word, weight, list_count, sums, start, count, row_of, place_of, label, hi, lo, grad, scale, x, w, dz, partials, dx, db, bytes;
 };
 
 struct Layout {
@@ -855,14 +927,15 @@ HeadPlan head_plan(const hot_head_desc &d, bool backward, bool with_dx)
     const long S = d.samples, R = d.rows, V = d.vocab, K = d.width;
     p.pieces = d.dtype == HOT_F32 ? 3 : 1;
     p.pack_w = p.pieces == 3 || !d.w_aligned || K % 8 || d.ldw % 8 || (S > 1 && d.w_sample % 8) || d.ldw > (1L << 21);
-    p.chunks = (int)((K + 7) / 8);
     p.columns = p.pieces == 3 ? 32 : 64;
     p.row_bytes = up(K, p.columns) * 2;
     p.places = up(R, 256);
-    // Tiles of 256 x 256 (256 x 128 in three pieces) where they fill the chip, of 128 x 128 below, of 256 x 32 for up to 32 rows.
-    const long large = ((V + 255) / 256) * ((R + 255) / 256) * S;
-    p.size = R <= 32 ? 0 : (large >= kComputeUnits ? 2 : 1);
-    p.v_tile = p.size == 1 ? 128 : 256;
+    auto tiles_of = [&](long v, long r) { return ((V + v - 1) / v) * ((R + r - 1) / r) * S; };
+    p.size = R <= 32 ? kFew : (tiles_of(256, 256) >= kComputeUnits ? kLarge : (tiles_of(128, 128) >= kSmallTiles ? kMiddle : kSmall));
+    constexpr int V_TILE[] = {256, 64, 128, 256}, R_TILE[] = {32, 64, 128, 256};
+    p.v_tile = V_TILE[p.size];
+    p.r_tile = p.size == kLarge && p.pieces == 3 ? 128 : R_TILE[p.size];
+    p.row_tiles = (int)((R + p.r_tile - 1) / p.r_tile);
     long piece = up(V, 256);
     if (backward || p.pack_w) {
         const int64_t per_word = S * ((backward ? p.places * 2 * p.pieces : 0) + (p.pack_w ? p.row_bytes * p.pieces : 0));
@@ -875,8 +948,8 @@ HeadPlan head_plan(const hot_head_desc &d, bool backward, bool with_dx)
     p.v_pieces = (int)((V + piece - 1) / piece);
     // The features' gradients: a run of the piece's words to a workgroup.  A round of workgroups takes its steps of 64 words, and as long as some
     // twenty of them for its start and for adding to the sums in memory; the number of runs with the fewest such steps is taken.
-    const int bm = p.size == 0 ? 32 : (p.size == 1 || p.pieces == 3 ? 128 : 256), bn = p.size == 1 ? 128 : 256;
-    const long tiles = ((R + bm - 1) / bm) * ((K + bn - 1) / bn) * S, at_once = kComputeUnits * (p.size == 2 || p.pieces == 3 ? 1 : 2);
+    const int bm = p.r_tile, bn = V_TILE[p.size];
+    const long tiles = ((R + bm - 1) / bm) * ((K + bn - 1) / bn) * S, at_once = kComputeUnits * (p.size == kLarge || p.pieces == 3 ? 1 : 2);
     long best = 0;
     for (long runs = 1; runs <= 64 && (runs == 1 || runs * 256 <= piece); ++runs) {
         const long depth = up((piece + runs - 1) / runs, 64), cost = (tiles * runs + at_once - 1) / at_once * (depth / 64 + 20);
@@ -908,6 +981,7 @@ HeadPlan head_plan(const hot_head_desc &d, bool backward, bool with_dx)
     p.w = l.take(p.pack_w ? S * piece * p.row_bytes * p.pieces : 0);
     if (backward) {
         p.dz = l.take(S * p.places * piece * 2 * p.pieces);
+        p.db = l.take(S * p.row_tiles * piece * 4);
         if (with_dx) p.dx = l.take((int64_t)p.splits * S * R * K * 4);
     } else {
         p.partials = l.take(S * ((V + p.v_tile - 1) / p.v_tile) * 3 * p.places * 4);
@@ -936,32 +1010,37 @@ unsigned grid_for(long items, long most = 8192)
     return (unsigned)(n < 1 ? 1 : (n < most ? n : most));
 }
 
-void head_rows(const HeadCall &c, const double *lse, const float *g, long g_sample, long g_row)
+void head_lists(const HeadCall &c)
 {
     const hot_head_desc &d = c.d;
     const HeadPlan &p = c.p;
-    if (d.top > 0) {
-        ListArgs a;
-        a.rows = d.rows;
-        a.lists = d.rows * (c.list_sample > 0 ? d.samples : 1);
-        a.idx_sample = d.index_sample;
-        a.idx_row = d.index_row;
-        a.logit_sample = d.logit_sample;
-        a.logit_row = d.logit_row;
-        a.top = (int)d.top;
-        a.logit_type = d.logit_dtype;
-        a.marks = (int)((d.vocab + kStartStep - 1) / kStartStep);
-        a.vocab = d.vocab;
-        a.inv_temperature = (float)(1.0 / d.temperature);
-        a.index = c.index;
-        a.logit = c.logit;
-        a.word = c.in<int>(p.word);
-        a.weight = c.in<float>(p.weight);
-        a.count = c.in<int>(p.list_count);
-        a.sums = c.in<double>(p.sums);
-        a.start = c.in<unsigned short>(p.start);
-        hot_head_lists_kernel<<<dim3((unsigned)((a.lists + kListWaves - 1) / kListWaves)), 64 * kListWaves, 0, c.stream>>>(a);
-    }
+    if (d.top == 0) return;
+    ListArgs a;
+    a.rows = d.rows;
+    a.lists = d.rows * (c.list_sample > 0 ? d.samples : 1);
+    a.idx_sample = d.index_sample;
+    a.idx_row = d.index_row;
+    a.logit_sample = d.logit_sample;
+    a.logit_row = d.logit_row;
+    a.top = (int)d.top;
+    a.logit_type = d.logit_dtype;
+    a.marks = (int)((d.vocab + kStartStep - 1) / kStartStep);
+    a.vocab = d.vocab;
+    a.inv_temperature = (float)(1.0 / d.temperature);
+    a.index = c.index;
+    a.logit = c.logit;
+    a.word = c.in<int>(p.word);
+    a.weight = c.in<float>(p.weight);
+    a.count = c.in<int>(p.list_count);
+    a.sums = c.in<double>(p.sums);
+    a.start = c.in<unsigned short>(p.start);
+    hot_head_lists_kernel<<<dim3((unsigned)((a.lists + kListWaves - 1) / kListWaves)), 64 * kListWaves, 0, c.stream>>>(a);
+}
+
+RowArgs head_rows(const HeadCall &c, const double *lse, const float *g, long g_sample, long g_row)
+{
+    const hot_head_desc &d = c.d;
+    const HeadPlan &p = c.p;
     RowArgs a = {};
     a.rows = d.rows;
     a.vocab = d.vocab;
@@ -984,11 +1063,10 @@ void head_rows(const HeadCall &c, const double *lse, const float *g, long g_samp
     a.lo = c.in<float>(p.lo);
     a.grad = c.in<float>(p.grad);
     a.scale = c.in<float>(p.scale);
-    hot_head_rows_kernel<<<dim3((unsigned)d.samples), kRowBlock, 0, c.stream>>>(a);
+    return a;
 }
 
-template <class T>
-void head_pack_x(const HeadCall &c)
+PackArgs head_pack_x(const HeadCall &c)
 {
     PackArgs a;
     a.from = c.x;
@@ -997,33 +1075,58 @@ void head_pack_x(const HeadCall &c)
     a.row_of = c.in<int>(c.p.row_of);
     a.count = c.in<int>(c.p.count);
     a.rows = c.d.rows;
-    a.map_sample = c.d.rows;
     a.width = (int)c.d.width;
-    a.chunks = c.p.chunks;
     a.to = c.in<char>(c.p.x);
     a.columns = c.p.columns;
     a.block = c.p.places * c.p.columns * 2L;
     a.to_sample = c.p.places * c.p.row_bytes;
     a.plane = c.d.samples * a.to_sample;
-    hot_head_pack_kernel<T><<<dim3(grid_for(c.d.rows * a.chunks), (unsigned)c.d.samples), 256, 0, c.stream>>>(a);
+    return a;
 }
 
-template <class T>
-void head_pack_w(const HeadCall &c, long v_begin, long v_count)
+PackArgs head_pack_w(const HeadCall &c, long v_begin, long v_count)
 {
     PackArgs a = {};
-    a.from = static_cast<const T *>(c.w) + (size_t)v_begin * (size_t)c.d.ldw;
+    a.from = static_cast<const char *>(c.w) + (size_t)v_begin * (size_t)c.d.ldw * (size_t)type_bytes(c.d.dtype);
     a.from_row = c.d.ldw;
     a.from_sample = c.d.w_sample;
     a.rows = v_count;
     a.width = (int)c.d.width;
-    a.chunks = c.p.chunks;
     a.to = c.in<char>(c.p.w);
     a.columns = c.p.columns;
     a.block = c.p.v_piece * c.p.columns * 2L;
     a.to_sample = c.p.v_piece * c.p.row_bytes;
     a.plane = c.d.samples * a.to_sample;
-    hot_head_pack_kernel<T><<<dim3(grid_for(v_count * a.chunks), (unsigned)c.d.samples), 256, 0, c.stream>>>(a);
+    return a;
+}
+
+// workgroups that pack an array: a run of rows of a block of columns to each, as long as that leaves enough of them
+long pack_blocks(const PackArgs &a)
+{
+    const long at_once = 256 / (a.columns / 8), items = (a.rows + at_once - 1) / at_once * ((a.width + a.columns - 1) / a.columns);
+    return items < 8192 ? items : 8192;
+}
+
+template <class T>
+void head_pack(const HeadCall &c, const PackArgs &a)
+{
+    hot_head_pack_kernel<T><<<dim3((unsigned)pack_blocks(a), (unsigned)c.d.samples), 256, 0, c.stream>>>(a);
+}
+
+// Everything in front of the products: entries, rows, the packed features and the first piece's packed weights
+template <class T>
+void head_prepare(const HeadCall &c, const RowArgs &rows, long first_words)
+{
+    head_lists(c);
+    const PackArgs x = head_pack_x(c), w = head_pack_w(c, 0, first_words);
+    const long xb = pack_blocks(x), wb = c.p.pack_w ? pack_blocks(w) : 0;
+    if (c.d.rows <= kFewRows) {
+        hot_head_prepare_kernel<T><<<dim3((unsigned)(xb + wb), (unsigned)c.d.samples), 256, 0, c.stream>>>(rows, x, w, (int)xb);
+        return;
+    }
+    hot_head_rows_kernel<<<dim3((unsigned)c.d.samples), kRowBlock, 0, c.stream>>>(rows);
+    head_pack<T>(c, x);
+    if (c.p.pack_w) head_pack<T>(c, w);
 }
 
 // the weights from word v_begin on as the kernels read them: as they lie, or packed
@@ -1068,6 +1171,8 @@ HeadArgs head_args(const HeadCall &c, long v_begin, long v_count)
     a.lo = c.in<float>(p.lo);
     a.grad = c.in<float>(p.grad);
     a.to_scale = c.in<float>(p.scale);
+    a.row_tiles = p.row_tiles;
+    a.v_piece = p.v_piece;
     a.dz = c.in<char>(p.dz);
     a.dz_block = p.places * p.columns * 2L;
     a.dz_sample = p.places * p.v_piece * 2L;
@@ -1091,8 +1196,9 @@ void head_logits(const HeadCall &c, const HeadArgs &a, bool backward)
 template <class T, int PIECES>
 void head_logits(const HeadCall &c, const HeadArgs &a, bool backward)
 {
-    if (c.p.size == 0) head_logits<Tile<T, PIECES, true, true, 256, 32, 8, 1>>(c, a, backward);
-    else if (c.p.size == 1) head_logits<Tile<T, PIECES, true, true, 128, 128, 2, 2>>(c, a, backward);
+    if (c.p.size == kFew) head_logits<Tile<T, PIECES, true, true, 256, 32, 8, 1>>(c, a, backward);
+    else if (c.p.size == kSmall) head_logits<Tile<T, PIECES, true, true, 64, 64, 2, 2>>(c, a, backward);
+    else if (c.p.size == kMiddle) head_logits<Tile<T, PIECES, true, true, 128, 128, 2, 2>>(c, a, backward);
     else if constexpr (PIECES == 1) head_logits<Tile<T, PIECES, true, true, 256, 256, 2, 4>>(c, a, backward);
     else head_logits<Tile<T, PIECES, true, true, 256, 128, 4, 2>>(c, a, backward);
 }
@@ -1115,11 +1221,10 @@ void head_dw(const HeadCall &c, const GradArgs &a)
 template <class T, class E, int PIECES>
 void head_forward(const HeadCall &c, float *loss, double *lse)
 {
-    head_rows(c, nullptr, nullptr, 0, 0);
-    head_pack_x<T>(c);
+    head_prepare<T>(c, head_rows(c, nullptr, nullptr, 0, 0), c.d.vocab < c.p.v_piece ? c.d.vocab : c.p.v_piece);
     for (long v = 0; v < c.d.vocab; v += c.p.v_piece) {
         const long n = c.d.vocab - v < c.p.v_piece ? c.d.vocab - v : c.p.v_piece;
-        if (c.p.pack_w) head_pack_w<T>(c, v, n);
+        if (c.p.pack_w && v > 0) head_pack<T>(c, head_pack_w(c, v, n));
         head_logits<E, PIECES>(c, head_args(c, v, n), false);
     }
     JoinArgs a;
@@ -1127,7 +1232,7 @@ void head_forward(const HeadCall &c, float *loss, double *lse)
     a.places = c.p.places;
     a.tiles = (int)((c.d.vocab + c.p.v_tile - 1) / c.p.v_tile);
     a.lanes = 4;
-    while (a.lanes < 256 && (c.d.rows + 256 / a.lanes - 1) / (256 / a.lanes) * c.d.samples < kComputeUnits && a.lanes * 4 < a.tiles) a.lanes *= 2;
+    while (a.lanes < 256 && (c.d.rows + 256 / a.lanes - 1) / (256 / a.lanes) * c.d.samples < kComputeUnits && a.lanes * 2 <= a.tiles) a.lanes *= 2;
     a.partials = c.in<float>(c.p.partials);
     a.place_of = c.in<int>(c.p.place_of);
     a.label = c.in<int>(c.p.label);
@@ -1142,13 +1247,13 @@ void head_forward(const HeadCall &c, float *loss, double *lse)
 template <class T, class E, int PIECES>
 void head_backward(const HeadCall &c, const double *lse, const float *g, long g_sample, long g_row, void *dx, void *dw, void *db)
 {
-    head_rows(c, lse, g, g_sample, g_row);
-    head_pack_x<T>(c);
+    head_prepare<T>(c, head_rows(c, lse, g, g_sample, g_row), c.d.vocab < c.p.v_piece ? c.d.vocab : c.p.v_piece);
     const float *const scale = c.in<float>(c.p.scale);
     for (long v = 0; v < c.d.vocab; v += c.p.v_piece) {
         const long n = c.d.vocab - v < c.p.v_piece ? c.d.vocab - v : c.p.v_piece;
-        if (c.p.pack_w) head_pack_w<T>(c, v, n);
-        const HeadArgs h = head_args(c, v, n);
+        if (c.p.pack_w && v > 0) head_pack<T>(c, head_pack_w(c, v, n));
+        HeadArgs h = head_args(c, v, n);
+        if (db) h.sums = c.in<float>(c.p.db);
         head_logits<E, PIECES>(c, h, true);
         GradArgs a = {};
         a.dz = {h.dz, c.p.columns * 2L, h.dz_block, h.dz_plane};
@@ -1169,8 +1274,9 @@ void head_backward(const HeadCall &c, const double *lse, const float *g, long g_
         if (dx) {
             a.other = h.w;
             a.sample = h.w_sample;
-            if (c.p.size == 0) head_dx<Tile<E, PIECES, true, false, 32, 256, 1, 8>>(c, a);
-            else if (c.p.size == 1) head_dx<Tile<E, PIECES, true, false, 128, 128, 2, 2>>(c, a);
+            if (c.p.size == kFew) head_dx<Tile<E, PIECES, true, false, 32, 256, 1, 8>>(c, a);
+            else if (c.p.size == kSmall) head_dx<Tile<E, PIECES, true, false, 64, 64, 2, 2>>(c, a);
+            else if (c.p.size == kMiddle) head_dx<Tile<E, PIECES, true, false, 128, 128, 2, 2>>(c, a);
             else if constexpr (PIECES == 1) head_dx<Tile<E, PIECES, true, false, 256, 256, 2, 4>>(c, a);
             else head_dx<Tile<E, PIECES, true, false, 128, 256, 2, 4>>(c, a);
         }
@@ -1179,13 +1285,14 @@ void head_backward(const HeadCall &c, const double *lse, const float *g, long g_
             a.sample = h.x_sample;
             a.out = dw;
             a.out_sample = c.d.vocab * c.d.width;
-            if (c.p.size < 2) head_dw<Tile<E, PIECES, false, false, 128, 128, 2, 2>, T>(c, a);
+            if (c.p.size == kSmall) head_dw<Tile<E, PIECES, false, false, 64, 64, 2, 2>, T>(c, a);
+            else if (c.p.size < kLarge) head_dw<Tile<E, PIECES, false, false, 128, 128, 2, 2>, T>(c, a);
             else if constexpr (PIECES == 1) head_dw<Tile<E, PIECES, false, false, 256, 256, 2, 4>, T>(c, a);
             else head_dw<Tile<E, PIECES, false, false, 256, 128, 4, 2>, T>(c, a);
         }
         if (db) {
-            const BiasArgs b = {a.dz, a.dz_sample, h.v_begin, h.v_count, h.count, scale, a.temperature, db, c.d.vocab, c.d.dtype};
-            hot_head_db_kernel<E, PIECES, PIECES == 3 ? 32 : 64><<<dim3((unsigned)((n + 127) / 128), (unsigned)c.d.samples), 256, 0, c.stream>>>(b);
+            const BiasArgs b = {h.sums, c.p.row_tiles, c.p.r_tile, c.p.v_piece, h.v_begin, h.v_count, h.count, scale, a.temperature, db, c.d.vocab, c.d.dtype};
+            hot_head_db_kernel<<<dim3((unsigned)((n + 255) / 256), (unsigned)c.d.samples), 256, 0, c.stream>>>(b);
         }
     }
     if (dx) {

@@ -76,7 +76,7 @@ struct Stage {
     static constexpr int kPerRow = (ALONG ? BK : T) * 2 / 16;              // 16-byte chunks in a row of LDS
     static constexpr int kRows = 64 / kPerRow;                             // rows that one instruction of a wave fills
     static constexpr int kLoads = kBytes / 1024, kEach = (kLoads + WAVES - 1) / WAVES;
-    static_assert(kPerRow <= 64 && kBytes % 1024 == 0 && (ALONG || T >= 128), "");
+    static_assert(kPerRow <= 64 && kBytes % 1024 == 0 && (ALONG || T >= 64), "");
 
     unsigned off[kEach];
     int index[ALONG ? 1 : kEach];          // the contraction index of this lane's loads in a tile
