@@ -542,7 +542,7 @@ hot_head_forward_kernel(HeadArgs a)
     }
 }
 
-template <class TILE, bool LISTS>
+template <class TILE, bool LISTS, int PIECES>
 __global__ void __launch_bounds__(TILE::THREADS)
 hot_head_dz_kernel(HeadArgs a)
 {
@@ -575,7 +575,7 @@ hot_head_dz_kernel(HeadArgs a)
             for (int i = 0; i < 16; ++i) {
                 const float z = __builtin_fmaf(acc[m][n][i], a.scale, -hi[n]);
                 // (the low part of lse is below the rounding of 16-bit results)
-                acc[m][n][i] = __builtin_amdgcn_exp2f(TILE::PIECES == 1 ? z : z - lo[n]);
+                acc[m][n][i] = __builtin_amdgcn_exp2f(TILE::PIECES_A == 1 ? z : z - lo[n]);
             }
     rows.targets(a, v0, [&](int n, int m, int i, bool mine, float weight) { acc[m][n][i] -= mine ? weight : 0.0f; });
     // to rows of words, piece by piece, through LDS
@@ -587,7 +587,7 @@ hot_head_dz_kernel(HeadArgs a)
     float sum[2] = {0.0f, 0.0f};
     char *const out = a.dz + (size_t)s * (size_t)a.dz_sample + (size_t)((v0 - a.v_begin) / BK) * (size_t)a.dz_block + (size_t)r0 * (BK * 2);
 #pragma unroll
-    for (int p = 0; p < TILE::PIECES; ++p) {
+    for (int p = 0; p < PIECES; ++p) {
         if (p) __syncthreads();
 #pragma unroll
         for (int n = 0; n < TILE::NB; ++n)
@@ -600,7 +600,7 @@ hot_head_dz_kernel(HeadArgs a)
                     for (int i = 0; i < 4; ++i) {
                         const float v = p == 0 ? acc[m][n][4 * q + i] * g[n] : acc[m][n][4 * q + i];
                         o[i] = (T)v;
-                        if constexpr (TILE::PIECES > 1) acc[m][n][4 * q + i] = __builtin_isfinite((float)o[i]) ? v - (float)o[i] : 0.0f;
+                        if constexpr (PIECES > 1) acc[m][n][4 * q + i] = __builtin_isfinite((float)o[i]) ? v - (float)o[i] : 0.0f;
                     }
                     *reinterpret_cast<V4 *>(memory + (TILE::n0() + 32 * n + (TILE::lane() & 31)) * PITCH + (TILE::m0() + 32 * m + TILE::row(4 * q)) * 2) = o;
                 }
@@ -815,11 +815,9 @@ struct BiasArgs {
     int type;
 };
 
-__global__ void __launch_bounds__(256)
-hot_head_db_kernel(BiasArgs a)
+__device__ __forceinline__ void bias_gradient(const BiasArgs &a, long s, int first)
 {
-    const long s = blockIdx.y;
-    const int word = (int)blockIdx.x * 256 + (int)threadIdx.x, tiles = (a.count[s] + a.tile_rows - 1) / a.tile_rows;
+    const int word = first * 256 + (int)threadIdx.x, tiles = (a.count[s] + a.tile_rows - 1) / a.tile_rows;
     if (word >= a.v_count) return;
     float total = 0.0f;
 #pragma unroll 8
@@ -838,15 +836,16 @@ struct FeatureArgs {
     void *out;
 };
 
+// dx: the sums of its runs of words, at the rows' own places, and zeros for the rows that were left out
 template <class T>
-__global__ void __launch_bounds__(256)
-hot_head_features_kernel(FeatureArgs a)
+__device__ __forceinline__ void feature_gradient(const FeatureArgs &a, long sample, long first, long blocks)
 {
     constexpr int N = Piece<T>::N;
+    if (a.shared && sample > 0) return;
     const long chunks = (a.width + N - 1) / N, items = a.rows * chunks;
-    for (long item = (long)blockIdx.x * 256 + threadIdx.x; item < items; item += (long)gridDim.x * 256) {
+    for (long item = first * 256 + threadIdx.x; item < items; item += blocks * 256) {
         const long row = item / chunks, col = (item - row * chunks) * N;
-        const long s0 = a.shared ? 0 : (long)blockIdx.y, s1 = a.shared ? a.samples : s0 + 1;
+        const long s0 = a.shared ? 0 : sample, s1 = a.shared ? a.samples : s0 + 1;
         typename Piece<T>::F total = typename Piece<T>::F(0.0f);
         for (long s = s0; s < s1; ++s) {
             const int at = a.place_of[s * a.rows + row];
@@ -867,6 +866,15 @@ hot_head_features_kernel(FeatureArgs a)
     }
 }
 
+// both, behind a piece's products: the first x_blocks workgroups have dx (behind the last piece)
+template <class T>
+__global__ void __launch_bounds__(256) hot_head_finish_kernel(FeatureArgs x, BiasArgs b, int x_blocks)
+{
+    const long s = blockIdx.y;
+    if ((int)blockIdx.x < x_blocks) feature_gradient<T>(x, s, blockIdx.x, x_blocks);
+    else bias_gradient(b, s, (int)blockIdx.x - x_blocks);
+}
+
 __global__ void __launch_bounds__(256) hot_head_zero_kernel(char *p, long bytes)
 {
     for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < bytes; i += (long)gridDim.x * 256) p[i] = 0;
@@ -884,7 +892,7 @@ constexpr int64_t kPieceBytes = (int64_t)256 << 20;      // of dz and packed wei
 enum { kFew, kSmall, kMiddle, kLarge };
 
 struct HeadPlan {
-    int pieces;              // of an element
+    int pieces, dz_pieces;   // of an element, and of dz
     bool pack_w;
     int columns;             // of a block of what is packed
     long row_bytes;          // of a packed row: whole blocks
@@ -932,13 +940,14 @@ HeadPlan head_plan(const hot_head_desc &d, bool backward, bool with_dx)
     p.places = up(R, 256);
     auto tiles_of = [&](long v, long r) { return ((V + v - 1) / v) * ((R + r - 1) / r) * S; };
     p.size = R <= 32 ? kFew : (tiles_of(256, 256) >= kComputeUnits ? kLarge : (tiles_of(128, 128) >= kSmallTiles ? kMiddle : kSmall));
+    p.dz_pieces = p.size == kFew && p.pieces == 1 ? 2 : p.pieces;
     constexpr int V_TILE[] = {256, 64, 128, 256}, R_TILE[] = {32, 64, 128, 256};
     p.v_tile = V_TILE[p.size];
     p.r_tile = p.size == kLarge && p.pieces == 3 ? 128 : R_TILE[p.size];
     p.row_tiles = (int)((R + p.r_tile - 1) / p.r_tile);
     long piece = up(V, 256);
     if (backward || p.pack_w) {
-        const int64_t per_word = S * ((backward ? p.places * 2 * p.pieces : 0) + (p.pack_w ? p.row_bytes * p.pieces : 0));
+        const int64_t per_word = S * ((backward ? p.places * 2 * p.dz_pieces : 0) + (p.pack_w ? p.row_bytes * p.pieces : 0));
         const long most = kPieceBytes / per_word / 256 * 256;
         const long least = 1024;
         const long n = (piece + (most > least ? most : least) - 1) / (most > least ? most : least);
@@ -980,7 +989,7 @@ HeadPlan head_plan(const hot_head_desc &d, bool backward, bool with_dx)
     p.x = l.take(S * p.places * p.row_bytes * p.pieces);
     p.w = l.take(p.pack_w ? S * piece * p.row_bytes * p.pieces : 0);
     if (backward) {
-        p.dz = l.take(S * p.places * piece * 2 * p.pieces);
+        p.dz = l.take(S * p.places * piece * 2 * p.dz_pieces);
         p.db = l.take(S * p.row_tiles * piece * 4);
         if (with_dx) p.dx = l.take((int64_t)p.splits * S * R * K * 4);
     } else {
@@ -1180,15 +1189,21 @@ HeadArgs head_args(const HeadCall &c, long v_begin, long v_count)
     return a;
 }
 
-template <class TILE>
-void head_logits(const HeadCall &c, const HeadArgs &a, bool backward)
+// Pieces in which dz of few rows is held.  A weight's gradient is then a handful of products, and one rounding of dz to 16 bits would show in it
+// beside its own (up to three times the error); reading W bounds these calls, so the second piece costs nothing.  With many rows the roundings
+// of dz average out.
+template <int PIECES>
+constexpr int kDz = PIECES == 1 ? 2 : PIECES;
+
+template <class TILE, int DZ>
+void logits_go(const HeadCall &c, const HeadArgs &a, bool backward)
 {
     const dim3 grid((unsigned)place_blocks((a.v_count + TILE::BM - 1) / TILE::BM, (c.d.rows + TILE::BN - 1) / TILE::BN), (unsigned)c.d.samples), block(TILE::THREADS);
     if (c.d.top > 0) {
-        if (backward) hot_head_dz_kernel<TILE, true><<<grid, block, 0, c.stream>>>(a);
+        if (backward) hot_head_dz_kernel<TILE, true, DZ><<<grid, block, 0, c.stream>>>(a);
         else hot_head_forward_kernel<TILE, true><<<grid, block, 0, c.stream>>>(a);
     } else {
-        if (backward) hot_head_dz_kernel<TILE, false><<<grid, block, 0, c.stream>>>(a);
+        if (backward) hot_head_dz_kernel<TILE, false, DZ><<<grid, block, 0, c.stream>>>(a);
         else hot_head_forward_kernel<TILE, false><<<grid, block, 0, c.stream>>>(a);
     }
 }
@@ -1196,11 +1211,11 @@ void head_logits(const HeadCall &c, const HeadArgs &a, bool backward)
 template <class T, int PIECES>
 void head_logits(const HeadCall &c, const HeadArgs &a, bool backward)
 {
-    if (c.p.size == kFew) head_logits<Tile<T, PIECES, true, true, 256, 32, 8, 1>>(c, a, backward);
-    else if (c.p.size == kSmall) head_logits<Tile<T, PIECES, true, true, 64, 64, 2, 2>>(c, a, backward);
-    else if (c.p.size == kMiddle) head_logits<Tile<T, PIECES, true, true, 128, 128, 2, 2>>(c, a, backward);
-    else if constexpr (PIECES == 1) head_logits<Tile<T, PIECES, true, true, 256, 256, 2, 4>>(c, a, backward);
-    else head_logits<Tile<T, PIECES, true, true, 256, 128, 4, 2>>(c, a, backward);
+    if (c.p.size == kFew) logits_go<Tile<T, PIECES, PIECES, true, true, 256, 32, 8, 1>, kDz<PIECES>>(c, a, backward);
+    else if (c.p.size == kSmall) logits_go<Tile<T, PIECES, PIECES, true, true, 64, 64, 2, 2>, PIECES>(c, a, backward);
+    else if (c.p.size == kMiddle) logits_go<Tile<T, PIECES, PIECES, true, true, 128, 128, 2, 2>, PIECES>(c, a, backward);
+    else if constexpr (PIECES == 1) logits_go<Tile<T, PIECES, PIECES, true, true, 256, 256, 2, 4>, PIECES>(c, a, backward);
+    else logits_go<Tile<T, PIECES, PIECES, true, true, 256, 128, 4, 2>, PIECES>(c, a, backward);
 }
 
 template <class TILE>
@@ -1274,40 +1289,30 @@ void head_backward(const HeadCall &c, const double *lse, const float *g, long g_
         if (dx) {
             a.other = h.w;
             a.sample = h.w_sample;
-            if (c.p.size == kFew) head_dx<Tile<E, PIECES, true, false, 32, 256, 1, 8>>(c, a);
-            else if (c.p.size == kSmall) head_dx<Tile<E, PIECES, true, false, 64, 64, 2, 2>>(c, a);
-            else if (c.p.size == kMiddle) head_dx<Tile<E, PIECES, true, false, 128, 128, 2, 2>>(c, a);
-            else if constexpr (PIECES == 1) head_dx<Tile<E, PIECES, true, false, 256, 256, 2, 4>>(c, a);
-            else head_dx<Tile<E, PIECES, true, false, 128, 256, 2, 4>>(c, a);
+            if (c.p.size == kFew) head_dx<Tile<E, kDz<PIECES>, PIECES, true, false, 32, 256, 1, 8>>(c, a);
+            else if (c.p.size == kSmall) head_dx<Tile<E, PIECES, PIECES, true, false, 64, 64, 2, 2>>(c, a);
+            else if (c.p.size == kMiddle) head_dx<Tile<E, PIECES, PIECES, true, false, 128, 128, 2, 2>>(c, a);
+            else if constexpr (PIECES == 1) head_dx<Tile<E, PIECES, PIECES, true, false, 256, 256, 2, 4>>(c, a);
+            else head_dx<Tile<E, PIECES, PIECES, true, false, 128, 256, 2, 4>>(c, a);
         }
         if (dw) {
             a.other = h.x;
             a.sample = h.x_sample;
             a.out = dw;
             a.out_sample = c.d.vocab * c.d.width;
-            if (c.p.size == kSmall) head_dw<Tile<E, PIECES, false, false, 64, 64, 2, 2>, T>(c, a);
-            else if (c.p.size < kLarge) head_dw<Tile<E, PIECES, false, false, 128, 128, 2, 2>, T>(c, a);
-            else if constexpr (PIECES == 1) head_dw<Tile<E, PIECES, false, false, 256, 256, 2, 4>, T>(c, a);
-            else head_dw<Tile<E, PIECES, false, false, 256, 128, 4, 2>, T>(c, a);
+            if (c.p.size == kSmall) head_dw<Tile<E, PIECES, PIECES, false, false, 64, 64, 2, 2>, T>(c, a);
+            else if (c.p.size == kFew) head_dw<Tile<E, PIECES, kDz<PIECES>, false, false, 128, 128, 2, 2>, T>(c, a);
+            else if (c.p.size == kMiddle) head_dw<Tile<E, PIECES, PIECES, false, false, 128, 128, 2, 2>, T>(c, a);
+            else if constexpr (PIECES == 1) head_dw<Tile<E, PIECES, PIECES, false, false, 256, 256, 2, 4>, T>(c, a);
+            else head_dw<Tile<E, PIECES, PIECES, false, false, 256, 128, 4, 2>, T>(c, a);
         }
-        if (db) {
-            const BiasArgs b = {h.sums, c.p.row_tiles, c.p.r_tile, c.p.v_piece, h.v_begin, h.v_count, h.count, scale, a.temperature, db, c.d.vocab, c.d.dtype};
-            hot_head_db_kernel<<<dim3((unsigned)((n + 255) / 256), (unsigned)c.d.samples), 256, 0, c.stream>>>(b);
-        }
-    }
-    if (dx) {
-        FeatureArgs a;
-        a.sums = c.in<float>(c.p.dx);
-        a.place_of = c.in<int>(c.p.place_of);
-        a.scale = scale;
-        a.temperature = (float)c.d.temperature;
-        a.rows = c.d.rows;
-        a.width = c.d.width;
-        a.samples = c.d.samples;
-        a.splits = c.p.splits;
-        a.shared = c.d.samples > 1 && c.d.x_sample == 0;
-        a.out = dx;
-        hot_head_features_kernel<T><<<dim3(grid_for(c.d.rows * ((c.d.width + Piece<T>::N - 1) / Piece<T>::N)), a.shared ? 1u : (unsigned)c.d.samples), 256, 0, c.stream>>>(a);
+        const bool finish_x = dx && v + n >= c.d.vocab;
+        if (!db && !finish_x) continue;
+        const BiasArgs b = {h.sums, c.p.row_tiles, c.p.r_tile, c.p.v_piece, h.v_begin, h.v_count, h.count, scale, a.temperature, db, c.d.vocab, c.d.dtype};
+        const FeatureArgs f = {c.in<float>(c.p.dx), c.in<int>(c.p.place_of), scale, a.temperature, c.d.rows, c.d.width, c.d.samples, c.p.splits,
+                               c.d.samples > 1 && c.d.x_sample == 0, dx};
+        const unsigned xb = finish_x ? grid_for(c.d.rows * ((c.d.width + Piece<T>::N - 1) / Piece<T>::N)) : 0, bb = db ? (unsigned)((n + 255) / 256) : 0;
+        hot_head_finish_kernel<T><<<dim3(xb + bb, (unsigned)c.d.samples), 256, 0, c.stream>>>(f, b, (int)xb);
     }
 }
 

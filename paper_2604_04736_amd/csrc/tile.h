@@ -5,8 +5,8 @@
 // for the features' gradients) or across them (weights for the features' gradients, features and the logits' gradients for the weights').
 // Along, a lane's eight contraction indices are one 16-byte read of LDS; across, two transposing reads, so no operand is ever
 // transposed in memory.  Sixteen-byte pieces of LDS are permuted so that neither form of reading meets its own banks.
-// PIECES = 3: float32 operands as three bf16 pieces each (planes of equal layout), multiplied as the six products that carry 24 bits, from the
-// smallest on; PIECES = 1: bf16 and fp16 operands as they are.
+// Pieces of an operand (planes of equal layout): three bf16 pieces of float32 in both, multiplied as the six products that carry 24 bits, from
+// the smallest on; one of bf16 and fp16 operands as they are; two where an operand is a result that is held in twice its type's bits.
 #ifndef HOT_TILE_H
 #define HOT_TILE_H
 
@@ -131,16 +131,16 @@ __device__ __forceinline__ s8v fragment(const lds_char *tile, int line0, int ks,
     }
 }
 
-template <class T_, int PIECES_, bool A_ALONG_, bool B_ALONG_, int BM_, int BN_, int WAVES_M_, int WAVES_N_>
+template <class T_, int PIECES_A_, int PIECES_B_, bool A_ALONG_, bool B_ALONG_, int BM_, int BN_, int WAVES_M_, int WAVES_N_>
 struct Tile {
     typedef T_ T;
-    static constexpr int PIECES = PIECES_, BM = BM_, BN = BN_, WAVES_M = WAVES_M_, WAVES_N = WAVES_N_;
+    static constexpr int PIECES_A = PIECES_A_, PIECES_B = PIECES_B_, BM = BM_, BN = BN_, WAVES_M = WAVES_M_, WAVES_N = WAVES_N_;
     static constexpr bool A_ALONG = A_ALONG_, B_ALONG = B_ALONG_;
-    static constexpr int BK = PIECES == 1 ? 64 : 32;
+    static constexpr int BK = PIECES_A == 3 ? 32 : 64;
     static constexpr int WAVES = WAVES_M * WAVES_N, THREADS = 64 * WAVES, WM = BM / WAVES_M, WN = BN / WAVES_N, MB = WM / 32, NB = WN / 32;
-    typedef Stage<BM, BK, A_ALONG, PIECES, WAVES> StageA;
-    typedef Stage<BN, BK, B_ALONG, PIECES, WAVES> StageB;
-    static constexpr int kA = PIECES * StageA::kBytes, kStage = kA + PIECES * StageB::kBytes, kLds = 2 * kStage;
+    typedef Stage<BM, BK, A_ALONG, PIECES_A, WAVES> StageA;
+    typedef Stage<BN, BK, B_ALONG, PIECES_B, WAVES> StageB;
+    static constexpr int kA = PIECES_A * StageA::kBytes, kStage = kA + PIECES_B * StageB::kBytes, kLds = 2 * kStage;
 
     static __device__ __forceinline__ int lane() { return (int)threadIdx.x & 63; }
     static __device__ __forceinline__ int wave() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }
@@ -154,32 +154,35 @@ struct Tile {
 
     // The operands of one matrix step of sixteen contraction indices: those of B, then those of A
     struct Operands {
-        s8v a[PIECES][MB], b[PIECES][NB];
+        s8v a[PIECES_A][MB], b[PIECES_B][NB];
         __device__ __forceinline__ void read(const lds_char *tile, int ks, int i)
         {
             const int l = lane();
-            if (i < PIECES * NB) b[i / NB][i % NB] = fragment<BN, BK, B_ALONG>(tile + kA + i / NB * StageB::kBytes, n0() + 32 * (i % NB), ks, l);
+            if (i < PIECES_B * NB) b[i / NB][i % NB] = fragment<BN, BK, B_ALONG>(tile + kA + i / NB * StageB::kBytes, n0() + 32 * (i % NB), ks, l);
             else {
-                i -= PIECES * NB;
+                i -= PIECES_B * NB;
                 a[i / MB][i % MB] = fragment<BM, BK, A_ALONG>(tile + i / MB * StageA::kBytes, m0() + 32 * (i % MB), ks, l);
             }
         }
     };
-    static constexpr int kReads = PIECES * (MB + NB), kLoads = StageA::kAll + StageB::kAll;
-    // a step's products in parts, between which reads and loads are issued: rows of blocks, or the six products of the pieces
-    static constexpr int kParts = PIECES == 1 ? MB : 6;
+    static constexpr int kReads = PIECES_A * MB + PIECES_B * NB, kLoads = StageA::kAll + StageB::kAll;
+    // a step's products in parts, between which reads and loads are issued: rows of blocks, or the products of the pieces
+    static constexpr bool kPlain = PIECES_A == 1 && PIECES_B == 1;
+    static constexpr int kParts = kPlain ? MB : (PIECES_A == 3 ? 6 : 2);
+    static_assert(kPlain || PIECES_A * PIECES_B == 2 || (PIECES_A == 3 && PIECES_B == 3), "");
 
     static __device__ __forceinline__ void multiply(const Operands &o, TileAcc<T> (&acc)[MB][NB], int part)
     {
-        if constexpr (PIECES == 1) {
+        if constexpr (kPlain) {
 #pragma unroll
             for (int n = 0; n < NB; ++n) acc[part][n].mac(o.a[0][part], o.b[0][n]);
         } else {
             constexpr int PA[6] = {2, 1, 0, 1, 0, 0}, PB[6] = {0, 1, 2, 0, 1, 0};
+            const int pa = PIECES_A == 3 ? PA[part] : (PIECES_A == 2 ? 1 - part : 0), pb = PIECES_B == 3 ? PB[part] : (PIECES_B == 2 ? 1 - part : 0);
 #pragma unroll
             for (int m = 0; m < MB; ++m)
 #pragma unroll
-                for (int n = 0; n < NB; ++n) acc[m][n].mac(o.a[PA[part]][m], o.b[PB[part]][n]);
+                for (int n = 0; n < NB; ++n) acc[m][n].mac(o.a[pa][m], o.b[pb][n]);
         }
     }
 
