@@ -365,4 +365,6 @@ def head_distillation(x, weight, top_index, top_logit, bias=None, temperature: f
     nothing has loss 0 and takes no part."""
     if top_index.dim() < 1 or top_index.shape != top_logit.shape:
         raise ValueError(f"top_index and top_logit: need one shape, got {tuple(top_index.shape)} and {tuple(top_logit.shape)}")
+    if not 1 <= top_index.shape[-1] <= hot.HOT_HEAD_MOST_TOP:
+        raise ValueError(f"top_index: need 1 to {hot.HOT_HEAD_MOST_TOP} words a row, got {top_index.shape[-1]}")
     return _head(x, weight, bias, top_index, top_logit.detach(), -100, temperature, 1)

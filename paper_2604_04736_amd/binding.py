@@ -890,8 +890,11 @@ def _head_desc(x, weight, bias, index, logit, ignore_index: int, temperature: fl
             raise ValueError(f"{name}: need adjacent elements, got strides {t.stride()}")
     if vocab > 1 and weight.stride(1) < width:
         raise ValueError(f"weight: rows overlap (strides {weight.stride()})")
-    if bias is not None and (_typed(bias, "bias", x) != kind or tuple(bias.shape) != (samples, vocab) or (vocab > 1 and bias.stride(1) != 1)):
-        raise ValueError(f"bias: need x's type, shape {(samples, vocab)} and adjacent elements, got {tuple(bias.shape)}")
+    if bias is not None:
+        if _typed(bias, "bias", x) != kind:
+            raise TypeError("bias: need x's type")
+        if tuple(bias.shape) != (samples, vocab) or (vocab > 1 and bias.stride(1) != 1):
+            raise ValueError(f"bias: need shape {(samples, vocab)} and adjacent elements, got {tuple(bias.shape)}, strides {bias.stride()}")
     want = 2 if logit is None else 3
     if not (index.is_cuda and index.device == x.device and index.dtype == torch.int64):
         raise TypeError(f"index: need an int64 tensor on {x.device}")

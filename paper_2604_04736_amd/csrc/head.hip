@@ -232,8 +232,10 @@ __device__ __forceinline__ int find_rows(const RowArgs &a, long s, unsigned shor
             if (threadIdx.x == 0) {
 #pragma unroll
                 for (int i = 0; i < BLOCK / 64; ++i) largest = fmaxf(largest, most[i]);
-                const bool usable = largest > 1e-30f && largest < 1e30f;
-                a.scale[2 * s] = usable ? a.scale_to / largest : a.scale_to;
+                // (where that factor would leave the normal numbers, and where nothing but zeros or infinities come in, it is scale_to)
+                const float by = a.scale_to / largest;
+                const bool usable = by >= 0x1p-126f && by <= 0x1p127f;
+                a.scale[2 * s] = usable ? by : a.scale_to;
                 a.scale[2 * s + 1] = usable ? largest / a.scale_to : 1.0f / a.scale_to;
             }
         }
