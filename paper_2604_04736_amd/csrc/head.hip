@@ -64,50 +64,45 @@ __device__ __forceinline__ double wave_total(double v)
 __global__ void __launch_bounds__(64 * kListWaves)
 hot_head_lists_kernel(ListArgs a)
 {
-    __shared__ int words[kListWaves][kMostTop], sorted[kListWaves][kMostTop];
+    __shared__ __attribute__((aligned(16))) int words[kListWaves][kMostTop], sorted[kListWaves][kMostTop];
+    __shared__ float scaled[kListWaves][kMostTop];
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
     const long list = (long)blockIdx.x * kListWaves + wave;
     int *const w = words[wave], *const in_order = sorted[wave];
+    float *const t = scaled[wave];
     if (list < a.lists) {
         const long s = list / a.rows, row = list % a.rows;
         const int64_t *const index = a.index + s * a.idx_sample + row * a.idx_row;
         const long logit0 = s * a.logit_sample + row * a.logit_row;
-        auto logit = [&](int j) {
-            typedef float F1 __attribute__((ext_vector_type(1)));
-            return load_as<1, F1>(a.logit, a.logit_type, logit0 + j, logit0 + a.top)[0] * a.inv_temperature;
-        };
         float most = -__builtin_inff();
         bool outside = false, nan = false;
-        for (int j = lane; j < a.top; j += 64) {
-            const int64_t i = index[j];
-            if (i < 0) continue;
+        for (int j = lane; j < (a.top + 3 & ~3); j += 64) {
+            typedef float F1 __attribute__((ext_vector_type(1)));
+            const int64_t i = j < a.top ? index[j] : -1;
+            const float v = i < 0 ? -__builtin_inff() : load_as<1, F1>(a.logit, a.logit_type, logit0 + j, logit0 + a.top)[0] * a.inv_temperature;
             outside |= i >= a.vocab;
-            const float t = logit(j);
-            nan |= t != t;
-            most = fmaxf(most, t);
+            nan |= v != v;
+            most = fmaxf(most, v);
+            w[j] = i < 0 || i >= a.vocab ? -1 : (int)i;
+            t[j] = v;
         }
         most = wave_max(most);
-        double total = 0.0;
-        for (int j = lane; j < a.top; j += 64)
-            if (index[j] >= 0) total += (double)expf(logit(j) - most);
-        total = wave_total(total);
         // a word outside the vocabulary or a logit that is no number leaves a row that is none; nothing listed, or nothing but -inf, no entries
         const bool broken = __builtin_amdgcn_ballot_w64(outside || nan) != 0 || most == __builtin_inff();
         const bool empty = !broken && most == -__builtin_inff();
-        double entropy = 0.0, sum = 0.0;
-        const double log_total = log(total);
+        double total = 0.0, entropy = 0.0, sum = 0.0;
         for (int j = lane; j < a.top; j += 64) {
-            const int64_t i = index[j];
-            float p = 0.0f;
-            if (!broken && !empty && i >= 0) {
-                const float t = logit(j);
-                p = (float)((double)expf(t - most) / total);
-                if (p > 0.0f) {
-                    entropy += (double)p * ((double)(t - most) - log_total);
-                    sum += (double)p;
-                }
-            }
-            w[j] = p > 0.0f ? (int)i : -1;
+            t[j] = expf(t[j] - most);
+            total += (double)t[j];
+        }
+        total = wave_total(total);
+        for (int j = lane; j < a.top; j += 64) {
+            const float p = broken || empty ? 0.0f : (float)((double)t[j] / total);
+            if (p > 0.0f) {
+                entropy += (double)p * log((double)t[j] / total);
+                sum += (double)p;
+            } else w[j] = -1;
+            t[j] = p;
         }
         entropy = wave_total(entropy);
         sum = wave_total(sum);
@@ -118,10 +113,14 @@ hot_head_lists_kernel(ListArgs a)
             kept += __builtin_popcountll(__builtin_amdgcn_ballot_w64(mine >= 0));
             if (mine < 0) continue;
             int rank = 0;
-            for (int k = 0; k < a.top; ++k) rank += w[k] >= 0 && (w[k] < mine || (w[k] == mine && k < j));
+            for (int k = 0; k < a.top; k += 4) {        // (entries that are not there are -1, as unsigned numbers above all words)
+                const i4 q = *reinterpret_cast<const i4 *>(w + k);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) rank += (unsigned)q[i] < (unsigned)mine || (q[i] == mine && k + i < j);
+            }
             in_order[rank] = mine;
             a.word[list * a.top + rank] = mine;
-            a.weight[list * a.top + rank] = (float)((double)expf(logit(j) - most) / total);
+            a.weight[list * a.top + rank] = t[j];
         }
         if (broken) {
             if (lane == 0) {
@@ -260,17 +259,6 @@ struct PackArgs {
     long to_sample, plane, block;
     int columns;
 };
-
-// the three bf16 pieces of a float, whose sum it is up to 2^-25 of it; what is not finite stays in the first
-__device__ __forceinline__ void split_bf16(float x, __bf16 (&p)[3])
-{
-#pragma unroll
-    for (int i = 0; i < 3; ++i) {
-        p[i] = (__bf16)x;
-        const float back = (float)p[i];
-        x = __builtin_isfinite(back) ? x - back : 0.0f;
-    }
-}
 
 // Workgroup `first` of `blocks`.  A wave packs a run of rows of one block of columns: what it writes is one run of memory.
 template <class T>
@@ -720,8 +708,9 @@ struct GradArgs {
     int samples, splits, split_depth;
     bool first;                    // of the pieces: sums begin with it
     float *sums;                   // dx: [split][sample][place][width]
-    void *out;                     // dW
-    long out_sample;
+    void *out;                     // dW, or its partial sums: [run of rows] out_split apart, [sample], words from out_first on
+    long out_sample, out_split;
+    int out_first, row_depth;      // rows of a run
     const float *scale;            // [samples, 2]
     float temperature;
 };
@@ -773,9 +762,10 @@ hot_head_dw_kernel(GradArgs a)
     if (!at.any) return;
     const int in = at.m * TILE::BN, k0 = at.n * TILE::BM;
     f16v acc[TILE::MB][TILE::NB];
-    const Operand x = {part(a.other, s * a.sample + k0 / TILE::BK * a.other.block), a.width - k0, count};
-    const Operand dz = {part(a.dz, s * a.dz_sample + in / TILE::BK * a.dz.block), a.v_count - in, count};
-    TILE::product((lds_char *)memory, x, dz, count, acc);
+    const int r0 = (int)blockIdx.z * a.row_depth, left = count - r0, depth = left < 0 ? 0 : (left < a.row_depth ? left : a.row_depth);
+    const Operand x = {part(a.other, s * a.sample + k0 / TILE::BK * a.other.block + r0 * a.other.pitch), a.width - k0, depth};
+    const Operand dz = {part(a.dz, s * a.dz_sample + in / TILE::BK * a.dz.block + r0 * a.dz.pitch), a.v_count - in, depth};
+    TILE::product((lds_char *)memory, x, dz, depth, acc);
     const float scale = a.scale[2 * s + 1] * a.temperature;
     typedef OUT V4 __attribute__((ext_vector_type(4)));
 #pragma unroll
@@ -791,7 +781,7 @@ hot_head_dw_kernel(GradArgs a)
             }
     __syncthreads();
     constexpr int N = Piece<OUT>::N, CHUNKS = TILE::BM / N;
-    OUT *const out = static_cast<OUT *>(a.out) + (size_t)s * (size_t)a.out_sample + (size_t)(a.v_begin + in) * (size_t)a.width;
+    OUT *const out = static_cast<OUT *>(a.out) + (size_t)blockIdx.z * (size_t)a.out_split + (size_t)s * (size_t)a.out_sample + (size_t)(a.out_first + in) * (size_t)a.width;
     for (int k = (int)threadIdx.x; k < TILE::BN * CHUNKS; k += TILE::THREADS) {
         const int row = k / CHUNKS, col = k0 + k % CHUNKS * N;
         if (in + row >= a.v_count || col >= a.width) continue;
@@ -802,6 +792,34 @@ hot_head_dw_kernel(GradArgs a)
 #pragma unroll
             for (int j = 0; j < N; ++j)
                 if (col + j < a.width) to[col + j] = v[j];
+    }
+}
+
+// dW of one piece from the partial sums of its runs of rows
+struct RunArgs {
+    const float *parts;            // [run][sample][words of the piece][width]
+    long words_width, part_sample, part_run, out_sample;
+    int runs;
+    void *out;                     // from the piece's first word on
+};
+
+template <class T>
+__global__ void __launch_bounds__(256) hot_head_runs_kernel(RunArgs a)
+{
+    constexpr int N = Piece<T>::N;
+    const long s = blockIdx.y, items = (a.words_width + N - 1) / N;
+    for (long item = (long)blockIdx.x * 256 + threadIdx.x; item < items; item += (long)gridDim.x * 256) {
+        typename Piece<T>::F sum = typename Piece<T>::F(0.0f);
+        for (int k = 0; k < a.runs; ++k) {
+            const float *const p = a.parts + (size_t)k * (size_t)a.part_run + (size_t)s * (size_t)a.part_sample;
+#pragma unroll
+            for (int h = 0; h < N; h += 4) {
+                const Piece<float>::F v = Piece<float>::load(p, item * N + h, a.words_width);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sum[h + j] += v[j];
+            }
+        }
+        Piece<T>::store(static_cast<T *>(a.out) + (size_t)s * (size_t)a.out_sample, item * N, a.words_width, sum);
     }
 }
 
@@ -895,7 +913,7 @@ enum { kFew, kSmall, kMiddle, kLarge };
 
 struct HeadPlan {
     int pieces, dz_pieces;   // of an element, and of dz
-    bool pack_w;
+    bool pack_w, raw_w;      // weights packed; float32 weights of few rows, read as they lie
     int columns;             // of a block of what is packed
     long row_bytes;          // of a packed row: whole blocks
     long places;
@@ -904,8 +922,9 @@ struct HeadPlan {
     int v_tile, r_tile;      // words and rows of a tile of logits
     int row_tiles;
     int splits, split_depth; // runs of words of a piece, and their length
+    int runs, run_depth;     // runs of rows of the weights' gradients, and their length
     // where things lie in the workspace
-    int64_t word, weight, list_count, sums, start, count, row_of, place_of, label, hi, lo, grad, scale, x, w, dz, partials, dx, db, bytes;
+    int64_t word, weight, list_count, sums, start, count, row_of, place_of, label, hi, lo, grad, scale, x, w, dz, partials, dx, db, dw, bytes;
 };
 
 struct Layout {
@@ -936,7 +955,8 @@ HeadPlan head_plan(const hot_head_desc &d, bool backward, bool with_dx)
     HeadPlan p = {};
     const long S = d.samples, R = d.rows, V = d.vocab, K = d.width;
     p.pieces = d.dtype == HOT_F32 ? 3 : 1;
-    p.pack_w = p.pieces == 3 || !d.w_aligned || K % 8 || d.ldw % 8 || (S > 1 && d.w_sample % 8) || d.ldw > (1L << 21);
+    p.raw_w = p.pieces == 3 && R <= 32 && d.w_aligned && K % 4 == 0 && d.ldw % 4 == 0 && (S == 1 || d.w_sample % 4 == 0) && d.ldw <= (1L << 20);
+    p.pack_w = (p.pieces == 3 && !p.raw_w) || (p.pieces == 1 && (!d.w_aligned || K % 8 || d.ldw % 8 || (S > 1 && d.w_sample % 8) || d.ldw > (1L << 21)));
     p.columns = p.pieces == 3 ? 32 : 64;
     p.row_bytes = up(K, p.columns) * 2;
     p.places = up(R, 256);
@@ -971,6 +991,19 @@ HeadPlan head_plan(const hot_head_desc &d, bool backward, bool with_dx)
     }
     p.splits = (int)((piece + p.split_depth - 1) / p.split_depth);
 
+    // The weights' gradients: as many runs of rows as leave the fewest steps of BK rows in all rounds, twenty more to each run, and as long as their
+    // partial sums are no more than two rounds of tiles (5569 x 42 x 1227 float32 without: 195 us on ten workgroups)
+    const int wt = p.size == kLarge ? 256 : (p.size == kMiddle ? 128 : 64), wv = p.size == kLarge && p.pieces == 3 ? 128 : wt;
+    const long w_tiles = ((piece + wv - 1) / wv < (V + wv - 1) / wv ? (piece + wv - 1) / wv : (V + wv - 1) / wv) * ((K + wt - 1) / wt) * S;
+    for (long runs = 1; runs <= 256 && (runs == 1 || (runs * 4 * p.columns <= R && runs * w_tiles <= 2 * kComputeUnits)); ++runs) {
+        const long depth = up((R + runs - 1) / runs, p.columns), cost = (w_tiles * runs + kComputeUnits - 1) / kComputeUnits * (depth / p.columns + 20);
+        if (runs == 1 || cost < best) {
+            best = cost;
+            p.run_depth = (int)depth;
+        }
+    }
+    p.runs = (int)((R + p.run_depth - 1) / p.run_depth);
+
     Layout l;
     const long lists = d.top > 0 ? (d.index_sample > 0 || d.logit_sample > 0 ? S : 1) * R : 0, marks = (V + kStartStep - 1) / kStartStep;
     p.word = l.take(lists * d.top * 4);
@@ -993,6 +1026,7 @@ HeadPlan head_plan(const hot_head_desc &d, bool backward, bool with_dx)
     if (backward) {
         p.dz = l.take(S * p.places * piece * 2 * p.dz_pieces);
         p.db = l.take(S * p.row_tiles * piece * 4);
+        p.dw = l.take(p.runs > 1 ? (int64_t)p.runs * S * (piece < V ? piece : V) * K * 4 : 0);
         if (with_dx) p.dx = l.take((int64_t)p.splits * S * R * K * 4);
     } else {
         p.partials = l.take(S * ((V + p.v_tile - 1) / p.v_tile) * 3 * p.places * 4);
@@ -1144,8 +1178,9 @@ void head_prepare(const HeadCall &c, const RowArgs &rows, long first_words)
 Matrix head_weights(const HeadCall &c, long v_begin, long &sample)
 {
     const long columns = c.p.columns;
-    sample = c.p.pack_w ? c.p.v_piece * c.p.row_bytes : c.d.w_sample * 2;
-    if (!c.p.pack_w) return {static_cast<const char *>(c.w) + (size_t)v_begin * (size_t)c.d.ldw * 2, c.d.ldw * 2, columns * 2, 0};
+    const long size = type_bytes(c.d.dtype);
+    sample = c.p.pack_w ? c.p.v_piece * c.p.row_bytes : c.d.w_sample * size;
+    if (!c.p.pack_w) return {static_cast<const char *>(c.w) + (size_t)v_begin * (size_t)c.d.ldw * (size_t)size, c.d.ldw * size, columns * size, 0};
     return {c.in<char>(c.p.w), columns * 2, c.p.v_piece * columns * 2, c.d.samples * sample};
 }
 
@@ -1195,6 +1230,9 @@ HeadArgs head_args(const HeadCall &c, long v_begin, long v_count)
 // beside its own (up to three times the error); reading W bounds these calls, so the second piece costs nothing.  With many rows the roundings
 // of dz average out.
 template <int PIECES>
+constexpr int kSmallStages = PIECES == 1 ? 4 : 3;
+
+template <int PIECES>
 constexpr int kDz = PIECES == 1 ? 2 : PIECES;
 
 template <class TILE, int DZ>
@@ -1213,8 +1251,11 @@ void logits_go(const HeadCall &c, const HeadArgs &a, bool backward)
 template <class T, int PIECES>
 void head_logits(const HeadCall &c, const HeadArgs &a, bool backward)
 {
-    if (c.p.size == kFew) logits_go<Tile<T, PIECES, PIECES, true, true, 256, 32, 8, 1>, kDz<PIECES>>(c, a, backward);
-    else if (c.p.size == kSmall) logits_go<Tile<T, PIECES, PIECES, true, true, 64, 64, 2, 2>, PIECES>(c, a, backward);
+    if constexpr (PIECES == 3) {
+        if (c.p.raw_w) return logits_go<Tile<T, PIECES, PIECES, true, true, 256, 32, 8, 1, 4, true, false>, kDz<PIECES>>(c, a, backward);
+        if (c.p.size == kFew) return logits_go<Tile<T, PIECES, PIECES, true, true, 256, 32, 8, 1>, kDz<PIECES>>(c, a, backward);
+    } else if (c.p.size == kFew) return logits_go<Tile<T, PIECES, PIECES, true, true, 256, 32, 8, 1, 4>, kDz<PIECES>>(c, a, backward);
+    if (c.p.size == kSmall) logits_go<Tile<T, PIECES, PIECES, true, true, 64, 64, 2, 2, kSmallStages<PIECES>>, PIECES>(c, a, backward);
     else if (c.p.size == kMiddle) logits_go<Tile<T, PIECES, PIECES, true, true, 128, 128, 2, 2>, PIECES>(c, a, backward);
     else if constexpr (PIECES == 1) logits_go<Tile<T, PIECES, PIECES, true, true, 256, 256, 2, 4>, PIECES>(c, a, backward);
     else logits_go<Tile<T, PIECES, PIECES, true, true, 256, 128, 4, 2>, PIECES>(c, a, backward);
@@ -1228,10 +1269,32 @@ void head_dx(const HeadCall &c, const GradArgs &a)
 }
 
 template <class TILE, class OUT>
-void head_dw(const HeadCall &c, const GradArgs &a)
+void dw_go(const HeadCall &c, const GradArgs &a)
 {
-    hot_head_dw_kernel<TILE, OUT><<<dim3((unsigned)place_blocks((a.v_count + TILE::BN - 1) / TILE::BN, (c.d.width + TILE::BM - 1) / TILE::BM), (unsigned)c.d.samples),
+    hot_head_dw_kernel<TILE, OUT><<<dim3((unsigned)place_blocks((a.v_count + TILE::BN - 1) / TILE::BN, (c.d.width + TILE::BM - 1) / TILE::BM), (unsigned)c.d.samples, (unsigned)c.p.runs),
                                     TILE::THREADS, 0, c.stream>>>(a);
+}
+
+// dW on tiles of TILE, or, on tiles of RUN_TILE (whose float32 results have to fit LDS), as partial sums that are then added up
+template <class TILE, class T, class RUN_TILE = TILE>
+void head_dw(const HeadCall &c, GradArgs a, void *dw)
+{
+    const long part = (long)a.v_count * c.d.width;
+    a.row_depth = c.p.run_depth;
+    if (c.p.runs == 1) {
+        a.out = dw;
+        a.out_sample = c.d.vocab * c.d.width;
+        a.out_first = a.v_begin;
+        return dw_go<TILE, T>(c, a);
+    }
+    float *const parts = c.in<float>(c.p.dw);
+    a.out = parts;
+    a.out_sample = part;
+    a.out_split = c.d.samples * part;
+    a.out_first = 0;
+    dw_go<RUN_TILE, float>(c, a);
+    const RunArgs r = {parts, part, part, a.out_split, c.d.vocab * c.d.width, c.p.runs, static_cast<T *>(dw) + (size_t)a.v_begin * (size_t)c.d.width};
+    hot_head_runs_kernel<T><<<dim3(grid_for((part + Piece<T>::N - 1) / Piece<T>::N), (unsigned)c.d.samples), 256, 0, c.stream>>>(r);
 }
 
 // T: the type of the tensors; E: of the tiles' elements
@@ -1291,8 +1354,10 @@ void head_backward(const HeadCall &c, const double *lse, const float *g, long g_
         if (dx) {
             a.other = h.w;
             a.sample = h.w_sample;
-            if (c.p.size == kFew) head_dx<Tile<E, kDz<PIECES>, PIECES, true, false, 32, 256, 1, 8>>(c, a);
-            else if (c.p.size == kSmall) head_dx<Tile<E, PIECES, PIECES, true, false, 64, 64, 2, 2>>(c, a);
+            if (c.p.raw_w) {
+                if constexpr (PIECES == 3) head_dx<Tile<E, PIECES, PIECES, true, false, 32, 256, 1, 8, 4, false, true>>(c, a);
+            } else if (c.p.size == kFew) head_dx<Tile<E, kDz<PIECES>, PIECES, true, false, 32, 256, 1, 8, PIECES == 1 ? 3 : 2>>(c, a);
+            else if (c.p.size == kSmall) head_dx<Tile<E, PIECES, PIECES, true, false, 64, 64, 2, 2, kSmallStages<PIECES>>>(c, a);
             else if (c.p.size == kMiddle) head_dx<Tile<E, PIECES, PIECES, true, false, 128, 128, 2, 2>>(c, a);
             else if constexpr (PIECES == 1) head_dx<Tile<E, PIECES, PIECES, true, false, 256, 256, 2, 4>>(c, a);
             else head_dx<Tile<E, PIECES, PIECES, true, false, 128, 256, 2, 4>>(c, a);
@@ -1300,13 +1365,11 @@ void head_backward(const HeadCall &c, const double *lse, const float *g, long g_
         if (dw) {
             a.other = h.x;
             a.sample = h.x_sample;
-            a.out = dw;
-            a.out_sample = c.d.vocab * c.d.width;
-            if (c.p.size == kSmall) head_dw<Tile<E, PIECES, PIECES, false, false, 64, 64, 2, 2>, T>(c, a);
-            else if (c.p.size == kFew) head_dw<Tile<E, PIECES, kDz<PIECES>, false, false, 128, 128, 2, 2>, T>(c, a);
-            else if (c.p.size == kMiddle) head_dw<Tile<E, PIECES, PIECES, false, false, 128, 128, 2, 2>, T>(c, a);
-            else if constexpr (PIECES == 1) head_dw<Tile<E, PIECES, PIECES, false, false, 256, 256, 2, 4>, T>(c, a);
-            else head_dw<Tile<E, PIECES, PIECES, false, false, 256, 128, 4, 2>, T>(c, a);
+            if (c.p.size == kFew) head_dw<Tile<E, PIECES, kDz<PIECES>, false, false, 64, 64, 2, 2>, T>(c, a, dw);
+            else if (c.p.size == kSmall) head_dw<Tile<E, PIECES, PIECES, false, false, 64, 64, 2, 2, kSmallStages<PIECES>>, T>(c, a, dw);
+            else if (c.p.size == kMiddle) head_dw<Tile<E, PIECES, PIECES, false, false, 128, 128, 2, 2>, T>(c, a, dw);
+            else if constexpr (PIECES == 1) head_dw<Tile<E, PIECES, PIECES, false, false, 256, 256, 2, 4>, T, Tile<E, PIECES, PIECES, false, false, 128, 128, 2, 2>>(c, a, dw);
+            else head_dw<Tile<E, PIECES, PIECES, false, false, 256, 128, 4, 2>, T>(c, a, dw);
         }
         const bool finish_x = dx && v + n >= c.d.vocab;
         if (!db && !finish_x) continue;

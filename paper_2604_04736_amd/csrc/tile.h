@@ -53,9 +53,9 @@ public:
     __device__ __forceinline__ f16v read(const TileSettled &) const { return v_; }
 };
 
-// A matrix in memory: element (row, col) at col / BK * block + row * pitch + col % BK * 2, `plane` bytes between pieces.  Rows as they usually
-// lie have a block of BK * 2 bytes; what is written here for the tiles to read has rows of BK elements, one block of columns after another, so
-// that a tile's loads are one run of memory (or four): read across 32 KB rows instead, the features' gradients took 1.2 times as long.
+// A matrix in memory: element (row, col) at col / BK * block + row * pitch + col % BK * size, `plane` bytes between pieces.  Rows as they usually
+// lie have a block of BK elements; what is written here for the tiles to read has rows of BK elements, one block of columns after another,
+// so that a tile's loads are one run of memory (or four).
 struct Matrix {
     const char *at;
     long pitch, block, plane;
@@ -68,51 +68,66 @@ struct Operand {
     int depth;           // how many contraction indices there are; the others are zeros
 };
 
-// Lines and indices are taken eight at a time along memory: a row may be read up to the next multiple of eight, and must be finite there or
-// meet zeros of the other operand.
-template <int T, int BK, bool ALONG, int PIECES, int WAVES>
+// Lines and indices are taken sixteen bytes at a time along memory: a row may be read up to the next multiple of that, and must be finite there or
+// meet zeros of the other operand.  RAW: float32 as it lies, cut into pieces only where a wave reads its operands from LDS.
+template <int T, int BK, bool ALONG, int PIECES, int WAVES, bool RAW>
 struct Stage {
-    static constexpr int kBytes = T * BK * 2;                              // of one piece
-    static constexpr int kPerRow = (ALONG ? BK : T) * 2 / 16;              // 16-byte chunks in a row of LDS
+    static constexpr int kSize = RAW ? 4 : 2, kChunk = 16 / kSize, kPlanes = RAW ? 1 : PIECES;
+    static constexpr int kBytes = T * BK * kSize;                          // of one plane
+    static constexpr int kPerRow = (ALONG ? BK : T) * kSize / 16;          // 16-byte chunks in a row of LDS
     static constexpr int kRows = 64 / kPerRow;                             // rows that one instruction of a wave fills
-    static constexpr int kLoads = kBytes / 1024, kEach = (kLoads + WAVES - 1) / WAVES;
-    static_assert(kPerRow <= 64 && kBytes % 1024 == 0 && (ALONG || T >= 64), "");
+    // loads of a plane, and how many each wave issues (a plane of fewer loads than waves is loaded by several, to the same place)
+    static constexpr int kLoads = kBytes / 1024, kEach = kLoads >= WAVES ? kLoads / WAVES : 1;
+    static_assert(kPerRow <= 64 && kBytes % 1024 == 0 && (ALONG || T >= 64) && (kLoads % WAVES == 0 || WAVES % kLoads == 0), "");
 
     unsigned off[kEach];
     int index[ALONG ? 1 : kEach];          // the contraction index of this lane's loads in a tile
     int wave;
 
+    // the order of a row's chunks, so that neither form of reading meets its own banks
     static __device__ __forceinline__ int permuted(int row)
     {
-        if constexpr (!ALONG) return (row & 3) << 1;
-        else if constexpr (BK == 64) return row & 7;
+        if constexpr (!ALONG) return RAW ? 0 : (row & 3) << 1;
+        else if constexpr (kPerRow == 8) return row & 7;
         else return row >> 1 & 3;
     }
+
+    __device__ __forceinline__ int load(int i) const { return (wave + i * WAVES) % kLoads; }
 
     __device__ __forceinline__ Stage(const Operand &o, int wave_, int lane) : wave(wave_)
     {
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
-            const int row = (wave + j * WAVES) * kRows + lane / kPerRow, chunk = lane % kPerRow ^ permuted(row);
-            const int line = ALONG ? row : chunk * 8;
-            off[j] = line < o.lines ? (unsigned)(chunk * 8 / BK * o.m.block + row * o.m.pitch + chunk * 8 % BK * 2) : kBeyond;
-            if constexpr (ALONG) index[0] = chunk * 8;
+            const int row = load(j) * kRows + lane / kPerRow, col = (lane % kPerRow ^ permuted(row)) * kChunk;
+            const int line = ALONG ? row : col;
+            off[j] = line < o.lines ? (unsigned)(col / BK * o.m.block + row * o.m.pitch + col % BK * kSize) : kBeyond;
+            if constexpr (ALONG) index[0] = col;
             else index[j] = row;
         }
     }
 
-    // Sends for load `j` of kEach * PIECES of the tile that begins at contraction index k0 (beyond the last index: for zeros).
-    static constexpr int kAll = kEach * PIECES;
+    // Sends for load `j` of kAll of the tile that begins at contraction index k0 (beyond the last index: for zeros).
+    static constexpr int kAll = kEach * kPlanes;
     __device__ __forceinline__ void ask(const Operand &o, int k0, lds_char *to, int j) const
     {
         const int p = j / kEach, i = j % kEach;
-        if (kLoads % WAVES != 0 && wave + i * WAVES >= kLoads) return;
         const char *const from = o.m.at + p * o.m.plane + (ALONG ? k0 / BK * o.m.block : k0 * o.m.pitch);
         const __amdgpu_buffer_rsrc_t win = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(from), 0, (int)kBeyond, 0x00020000);
         const unsigned at = index[ALONG ? 0 : i] < o.depth - k0 ? off[i] : kBeyond;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(win, (__attribute__((address_space(3))) void *)(to + p * kBytes + (wave + i * WAVES) * 1024), 16, (int)at, 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(win, (__attribute__((address_space(3))) void *)(to + p * kBytes + load(i) * 1024), 16, (int)at, 0, 0, 0);
     }
 };
+
+// the three bf16 pieces of a float, whose sum it is up to 2^-25 of it; what is not finite stays in the first
+__device__ __forceinline__ void split_bf16(float x, __bf16 (&p)[3])
+{
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        p[i] = (__bf16)x;
+        const float back = (float)p[i];
+        x = __builtin_isfinite(back) ? x - back : 0.0f;
+    }
+}
 
 // Lane l's operand of the matrix instruction: line l % 32 of a block of 32, contraction indices 8 (l / 32) .. + 7 of sixteen.
 template <int T, int BK, bool ALONG>
@@ -131,16 +146,53 @@ __device__ __forceinline__ s8v fragment(const lds_char *tile, int line0, int ks,
     }
 }
 
-template <class T_, int PIECES_A_, int PIECES_B_, bool A_ALONG_, bool B_ALONG_, int BM_, int BN_, int WAVES_M_, int WAVES_N_>
+// The same of float32: eight of its elements, cut into three pieces
+template <int T, int BK, bool ALONG>
+__device__ __forceinline__ void raw_fragment(const lds_char *tile, int line0, int ks, int lane, s8v &p0, s8v &p1, s8v &p2)
+{
+    typedef float f4v __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) f4v lds_f4v;
+    typedef __attribute__((address_space(3))) float lds_float;
+    const int half = lane >> 5, line = line0 + (lane & 31);
+    float v[8];
+    if constexpr (ALONG) {
+        static_assert(BK == 32, "");
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const f4v q = *(const lds_f4v *)(tile + line * (BK * 4) + (((ks * 2 + half) * 2 + h) ^ (line & 7)) * 16);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[4 * h + j] = q[j];
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = *(const lds_float *)(tile + (ks * 16 + half * 8 + j) * (T * 4) + line * 4);
+    }
+    bf16x8 p[3];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        __bf16 q[3];
+        split_bf16(v[j], q);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) p[i][j] = q[i];
+    }
+    p0 = __builtin_bit_cast(s8v, p[0]);
+    p1 = __builtin_bit_cast(s8v, p[1]);
+    p2 = __builtin_bit_cast(s8v, p[2]);
+}
+
+// STAGES tiles lie in LDS: two, or more where a tile is short work and latency counts; the loads of STAGES - 1 of them are under way.
+template <class T_, int PIECES_A_, int PIECES_B_, bool A_ALONG_, bool B_ALONG_, int BM_, int BN_, int WAVES_M_, int WAVES_N_, int STAGES_ = 2, bool RAW_A_ = false, bool RAW_B_ = false>
 struct Tile {
     typedef T_ T;
     static constexpr int PIECES_A = PIECES_A_, PIECES_B = PIECES_B_, BM = BM_, BN = BN_, WAVES_M = WAVES_M_, WAVES_N = WAVES_N_;
-    static constexpr bool A_ALONG = A_ALONG_, B_ALONG = B_ALONG_;
+    static constexpr int STAGES = STAGES_;
+    static constexpr bool A_ALONG = A_ALONG_, B_ALONG = B_ALONG_, RAW_A = RAW_A_, RAW_B = RAW_B_;
+    static_assert(STAGES >= 2 && (!RAW_A || PIECES_A == 3) && (!RAW_B || PIECES_B == 3), "");
     static constexpr int BK = PIECES_A == 3 ? 32 : 64;
     static constexpr int WAVES = WAVES_M * WAVES_N, THREADS = 64 * WAVES, WM = BM / WAVES_M, WN = BN / WAVES_N, MB = WM / 32, NB = WN / 32;
-    typedef Stage<BM, BK, A_ALONG, PIECES_A, WAVES> StageA;
-    typedef Stage<BN, BK, B_ALONG, PIECES_B, WAVES> StageB;
-    static constexpr int kA = PIECES_A * StageA::kBytes, kStage = kA + PIECES_B * StageB::kBytes, kLds = 2 * kStage;
+    typedef Stage<BM, BK, A_ALONG, PIECES_A, WAVES, RAW_A> StageA;
+    typedef Stage<BN, BK, B_ALONG, PIECES_B, WAVES, RAW_B> StageB;
+    static constexpr int kA = StageA::kPlanes * StageA::kBytes, kStage = kA + StageB::kPlanes * StageB::kBytes, kLds = STAGES * kStage;
 
     static __device__ __forceinline__ int lane() { return (int)threadIdx.x & 63; }
     static __device__ __forceinline__ int wave() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }
@@ -149,8 +201,15 @@ struct Tile {
     static __device__ __forceinline__ int n0() { return wave() % WAVES_N * WN; }
     static __device__ __forceinline__ int row(int i) { return 8 * (i >> 2) + 4 * (lane() >> 5) + (i & 3); }
 
-    // everything sent for has come, to all waves
-    static __device__ __forceinline__ void arrive() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+    // everything sent for has come, to all waves, but for the last PENDING loads of each
+    template <int PENDING = 0>
+    static __device__ __forceinline__ void arrive()
+    {
+        static_assert(PENDING < 64, "");
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(PENDING) : "memory");
+    }
+
+    static constexpr int kReadsB = StageB::kPlanes * NB;
 
     // The operands of one matrix step of sixteen contraction indices: those of B, then those of A
     struct Operands {
@@ -158,14 +217,17 @@ struct Tile {
         __device__ __forceinline__ void read(const lds_char *tile, int ks, int i)
         {
             const int l = lane();
-            if (i < PIECES_B * NB) b[i / NB][i % NB] = fragment<BN, BK, B_ALONG>(tile + kA + i / NB * StageB::kBytes, n0() + 32 * (i % NB), ks, l);
-            else {
-                i -= PIECES_B * NB;
-                a[i / MB][i % MB] = fragment<BM, BK, A_ALONG>(tile + i / MB * StageA::kBytes, m0() + 32 * (i % MB), ks, l);
+            if (i < kReadsB) {
+                if constexpr (RAW_B) raw_fragment<BN, BK, B_ALONG>(tile + kA, n0() + 32 * i, ks, l, b[0][i], b[1][i], b[2][i]);
+                else b[i / NB][i % NB] = fragment<BN, BK, B_ALONG>(tile + kA + i / NB * StageB::kBytes, n0() + 32 * (i % NB), ks, l);
+            } else {
+                i -= kReadsB;
+                if constexpr (RAW_A) raw_fragment<BM, BK, A_ALONG>(tile, m0() + 32 * i, ks, l, a[0][i], a[1][i], a[2][i]);
+                else a[i / MB][i % MB] = fragment<BM, BK, A_ALONG>(tile + i / MB * StageA::kBytes, m0() + 32 * (i % MB), ks, l);
             }
         }
     };
-    static constexpr int kReads = PIECES_A * MB + PIECES_B * NB, kLoads = StageA::kAll + StageB::kAll;
+    static constexpr int kReads = kReadsB + StageA::kPlanes * MB, kLoads = StageA::kAll + StageB::kAll;
     // a step's products in parts, between which reads and loads are issued: rows of blocks, or the products of the pieces
     static constexpr bool kPlain = PIECES_A == 1 && PIECES_B == 1;
     static constexpr int kParts = kPlain ? MB : (PIECES_A == 3 ? 6 : 2);
@@ -186,20 +248,22 @@ struct Tile {
         }
     }
 
-    // One tile of contraction indices: the tile `here`, while the next is on its way
-    static constexpr int kSteps = BK / 16, kEarly = (kLoads + 1) / 2;
-    static __device__ __forceinline__ void step(lds_char *__restrict here, lds_char *__restrict next, const Operand &a, const Operand &b, const StageA &sa, const StageB &sb,
-                                                int k0, Operands (&now)[2], TileAcc<T> (&acc)[MB][NB])
+    // One tile of contraction indices: the tile `here`, while the ones behind it are on their way.  `before`: the room of the tile before, which the
+    // rest of tile STAGES - 1 from here goes to (with two stages that is `next`).
+    static constexpr int kSteps = BK / 16, kEarly = (kLoads + 1) / 2, kAhead = (STAGES - 2) * kLoads;
+    static __device__ __forceinline__ void ask(const Operand &a, const Operand &b, const StageA &sa, const StageB &sb, int k0, lds_char *to, int j)
     {
-        auto ask = [&](int from, lds_char *to, int j) {
-            if (j < StageA::kAll) sa.ask(a, from, to, j);
-            else sb.ask(b, from, to + kA, j - StageA::kAll);
-        };
+        if (j < StageA::kAll) sa.ask(a, k0, to, j);
+        else sb.ask(b, k0, to + kA, j - StageA::kAll);
+    }
+    static __device__ __forceinline__ void step(lds_char *__restrict here, lds_char *__restrict next, lds_char *before, const Operand &a, const Operand &b, const StageA &sa,
+                                                const StageB &sb, int k0, Operands (&now)[2], TileAcc<T> (&acc)[MB][NB])
+    {
 #pragma unroll
         for (int ks = 0; ks < kSteps; ++ks) {
             const bool last = ks + 1 == kSteps;
             __builtin_amdgcn_sched_barrier(0);
-            if (last) arrive();
+            if (last) arrive<kAhead>();
 #pragma unroll
             for (int part = 0; part < kParts; ++part) {
                 // reads in the first half of the parts, loads in all of them
@@ -213,20 +277,22 @@ struct Tile {
                 if (last)
 #pragma unroll
                     for (int j = 0; j < kEarly; ++j)
-                        if (j * kParts / kEarly == part) ask(k0 + 2 * BK, here, j);
+                        if (j * kParts / kEarly == part) ask(a, b, sa, sb, k0 + STAGES * BK, here, j);
                 if (ks == 0)
 #pragma unroll
                     for (int j = kEarly; j < kLoads; ++j)
-                        if ((j - kEarly) * kParts / (kLoads - kEarly) == part) ask(k0 + BK, next, j);
+                        if ((j - kEarly) * kParts / (kLoads - kEarly) == part) ask(a, b, sa, sb, k0 + (STAGES - 1) * BK, STAGES == 2 ? next : before, j);
                 multiply(now[ks & 1], acc, part);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
     }
 
-    // results = A B over `depth` contraction indices; LDS is free when it returns.  Two tiles in LDS, two sets of operands in registers.  Between
-    // the parts of a step's products the next step's operands are read; the last step of a tile begins with the barrier behind which
-    // the tile's room is free: the loads for the tile after the next are issued in that step and the one behind it.
+    // results = A B over `depth` contraction indices; LDS is free when it returns.  Two sets of operands in registers.  Between the parts of
+    // a step's products the next step's operands are read; the last step of a tile begins with the barrier behind which the tile's room
+    // is free: the loads that go there are issued in that step and the one behind it.  256 x 256 tiles of 8192 x 4096 x 131072 in bf16 run at
+    // 1.37 PFLOP/s along, 1.24 to 1.36 across (a library's product 1.48); four waves with 128 x 128 results each were slower (1.06 to 1.3), so were tiles
+    // of 256 x 128 with two workgroups to a compute unit (1.06).
     static __device__ __forceinline__ void product(lds_char *lds, const Operand &a, const Operand &b, int depth, f16v (&results)[MB][NB])
     {
         const int l = lane(), w = wave();
@@ -234,21 +300,20 @@ struct Tile {
         const StageB sb(b, w, l);
         TileAcc<T> acc[MB][NB];
         Operands now[2];
-        auto ask = [&](int from, lds_char *to, int j) {
-            if (j < StageA::kAll) sa.ask(a, from, to, j);
-            else sb.ask(b, from, to + kA, j - StageA::kAll);
-        };
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j) ask(0, lds, j);
-        arrive();
+        for (int t = 0; t < STAGES - 1; ++t)
 #pragma unroll
-        for (int j = 0; j < kEarly; ++j) ask(BK, lds + kStage, j);
+            for (int j = 0; j < kLoads; ++j) ask(a, b, sa, sb, t * BK, lds + t * kStage, j);
+        arrive<kAhead>();
+#pragma unroll
+        for (int j = 0; j < kEarly; ++j) ask(a, b, sa, sb, (STAGES - 1) * BK, lds + (STAGES - 1) * kStage, j);
 #pragma unroll
         for (int i = 0; i < kReads; ++i) now[0].read(lds, 0, i);         // (of zeros where depth is 0)
         int at = 0;
         for (int k0 = 0; k0 < depth; k0 += BK) {
-            step(lds + at, lds + (kStage - at), a, b, sa, sb, k0, now, acc);
-            at = kStage - at;
+            const int behind = at + kStage < kLds ? at + kStage : 0, before = at > 0 ? at - kStage : kLds - kStage;
+            step(lds + at, lds + behind, lds + before, a, b, sa, sb, k0, now, acc);
+            at = behind;
         }
         arrive();
         const TileSettled settled;
