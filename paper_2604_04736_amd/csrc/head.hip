@@ -22,7 +22,7 @@ namespace {
 
 constexpr int kComputeUnits = 256;
 constexpr int kMostTop = 1024;           // entries of a row (they are sorted in LDS)
-constexpr int kStartStep = 64;           // words between the marks into a row's sorted entries
+constexpr int kStartStep = 128;          // words between the marks into a row's sorted entries
 constexpr float kHalfScale = 4096.0f;    // fp16 logits' gradients are held times this: a probability of 1e-11 still counts, 16 x 4096 does not overflow
 
 inline __host__ __device__ long up(long n, long to) { return (n + to - 1) / to * to; }
@@ -61,11 +61,13 @@ __device__ __forceinline__ double wave_total(double v)
 }
 
 // One wave to a row: softmax of what is listed, entries of weight zero dropped, the others sorted by word (rank by comparison with all).
+// MOST: the longest list that fits (12 bytes of LDS an entry decide how many rows a compute unit has under way).
+template <int MOST>
 __global__ void __launch_bounds__(64 * kListWaves)
 hot_head_lists_kernel(ListArgs a)
 {
-    __shared__ __attribute__((aligned(16))) int words[kListWaves][kMostTop], sorted[kListWaves][kMostTop];
-    __shared__ float scaled[kListWaves][kMostTop];
+    __shared__ __attribute__((aligned(16))) int words[kListWaves][MOST], sorted[kListWaves][MOST];
+    __shared__ float scaled[kListWaves][MOST];
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
     const long list = (long)blockIdx.x * kListWaves + wave;
     int *const w = words[wave], *const in_order = sorted[wave];
@@ -113,6 +115,7 @@ hot_head_lists_kernel(ListArgs a)
             kept += __builtin_popcountll(__builtin_amdgcn_ballot_w64(mine >= 0));
             if (mine < 0) continue;
             int rank = 0;
+#pragma unroll 4
             for (int k = 0; k < a.top; k += 4) {        // (entries that are not there are -1, as unsigned numbers above all words)
                 const i4 q = *reinterpret_cast<const i4 *>(w + k);
 #pragma unroll
@@ -139,13 +142,13 @@ hot_head_lists_kernel(ListArgs a)
         }
         for (int m = lane; m <= a.marks; m += 64) {
             const int word = m * kStartStep;
-            int lo = 0, hi = kept;
-            while (lo < hi) {
-                const int mid = (lo + hi) >> 1;
-                if (in_order[mid] < word) lo = mid + 1;
+            int at = 0, hi = kept;
+            while (at < hi) {
+                const int mid = (at + hi) >> 1;
+                if (in_order[mid] < word) at = mid + 1;
                 else hi = mid;
             }
-            a.start[list * (a.marks + 1) + m] = (unsigned short)lo;
+            a.start[list * (a.marks + 1) + m] = (unsigned short)at;
         }
     }
 }
@@ -374,8 +377,8 @@ struct Rows {
             else {
                 const long list = s * a.list_sample + a.row_of[s * a.rows + place[n]];
                 const unsigned short *const start = a.start + list * (a.marks + 1);
-                const int mark = v0 / kStartStep, last = mark + TILE::BM / kStartStep, first = start[mark];
-                static_assert(TILE::BM % kStartStep == 0, "");
+                // (a tile of 64 words walks the entries of its neighbour too, which match none of its results)
+                const int mark = v0 / kStartStep, last = (v0 + TILE::BM + kStartStep - 1) / kStartStep, first = start[mark];
                 entry[n] = list * a.top + first;
                 left[n] = start[last < a.marks ? last : a.marks] - first;
                 if (left[n] > 0) {
@@ -456,7 +459,7 @@ struct TileOf {
 template <class TILE>
 __device__ __forceinline__ TileOf tile_of(const HeadArgs &a, int count)
 {
-    const Place at = place((int)blockIdx.x, (a.v_count + TILE::BM - 1) / TILE::BM, (count + TILE::BN - 1) / TILE::BN);
+    const Place at = place((a.v_count + TILE::BM - 1) / TILE::BM, (count + TILE::BN - 1) / TILE::BN);
     return {at.any, a.v_begin + at.m * TILE::BM, at.n * TILE::BN};
 }
 
@@ -532,6 +535,15 @@ hot_head_forward_kernel(HeadArgs a)
     }
 }
 
+// A product that is rounded to float32 wherever it is used.  (The compiler fuses a product with the conversion of the result to fp16, in one of its uses:
+// the first piece was then rounded once, and the second formed from what a piece rounded twice left, near the middle of two numbers another one.)
+__device__ __forceinline__ float rounded_product(float a, float b)
+{
+    float v = a * b;
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
 template <class TILE, bool LISTS, int PIECES>
 __global__ void __launch_bounds__(TILE::THREADS)
 hot_head_dz_kernel(HeadArgs a)
@@ -588,7 +600,7 @@ hot_head_dz_kernel(HeadArgs a)
                     V4 o;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const float v = p == 0 ? acc[m][n][4 * q + i] * g[n] : acc[m][n][4 * q + i];
+                        const float v = p == 0 ? rounded_product(acc[m][n][4 * q + i], g[n]) : acc[m][n][4 * q + i];
                         o[i] = (T)v;
                         if constexpr (PIECES > 1) acc[m][n][4 * q + i] = __builtin_isfinite((float)o[i]) ? v - (float)o[i] : 0.0f;
                     }
@@ -723,7 +735,7 @@ hot_head_dx_kernel(GradArgs a)
     __shared__ __attribute__((aligned(1024))) char memory[TILE::kLds];
     const long s = blockIdx.y;
     const int split = (int)blockIdx.z, count = a.count[s];
-    const Place at = place((int)blockIdx.x, (a.width + TILE::BN - 1) / TILE::BN, (count + TILE::BM - 1) / TILE::BM);
+    const Place at = place((a.width + TILE::BN - 1) / TILE::BN, (count + TILE::BM - 1) / TILE::BM);
     if (!at.any) return;
     const int r0 = at.n * TILE::BM, k0 = at.m * TILE::BN, v = split * a.split_depth;
     const int depth = a.v_count - v < a.split_depth ? a.v_count - v : a.split_depth;
@@ -758,7 +770,7 @@ hot_head_dw_kernel(GradArgs a)
     __shared__ __attribute__((aligned(1024))) char memory[TILE::kLds > NEED ? TILE::kLds : NEED];
     const long s = blockIdx.y;
     const int count = a.count[s];
-    const Place at = place((int)blockIdx.x, (a.v_count + TILE::BN - 1) / TILE::BN, (a.width + TILE::BM - 1) / TILE::BM);
+    const Place at = place((a.v_count + TILE::BN - 1) / TILE::BN, (a.width + TILE::BM - 1) / TILE::BM);
     if (!at.any) return;
     const int in = at.m * TILE::BN, k0 = at.n * TILE::BM;
     f16v acc[TILE::MB][TILE::NB];
@@ -903,13 +915,14 @@ __global__ void __launch_bounds__(256) hot_head_zero_kernel(char *p, long bytes)
 // ---------------------------------------------------------------------------------
 // Host side.
 
-constexpr long kSmallTiles = 128;                        // tiles of 128 x 128 below which 64 x 64 are taken
 constexpr long kMostTiles = 1L << 22;                    // of 256 x 256 logits (one grid dimension holds fewer than 2^32 threads)
 constexpr int64_t kPieceBytes = (int64_t)256 << 20;      // of dz and packed weights: what the memory-side cache holds
 
 // Sizes of tiles (of logits: words x rows): 256 x 32 for up to 32 rows, 64 x 64 and 128 x 128 where larger ones leave the chip empty, 256 x 256
 // (256 x 128 in three pieces).
-enum { kFew, kSmall, kMiddle, kLarge };
+// Float32 heads of up to 128 rows with 256 tiles of words have 256 x 128 with the weights read as they lie (128 x 1024 x 65536: 971 us packed, 646 so; with half as
+// many tiles, 64 x 768 x 32768, whose packed weights stay in the memory-side cache, 278 packed, 289 so).
+enum { kFew, kSmall, kMiddle, kLarge, kTall };
 
 struct HeadPlan {
     int pieces, dz_pieces;   // of an element, and of dz
@@ -955,15 +968,20 @@ HeadPlan head_plan(const hot_head_desc &d, bool backward, bool with_dx)
     HeadPlan p = {};
     const long S = d.samples, R = d.rows, V = d.vocab, K = d.width;
     p.pieces = d.dtype == HOT_F32 ? 3 : 1;
-    p.raw_w = p.pieces == 3 && R <= 32 && d.w_aligned && K % 4 == 0 && d.ldw % 4 == 0 && (S == 1 || d.w_sample % 4 == 0) && d.ldw <= (1L << 20);
+    const bool whole = d.w_aligned && K % 4 == 0 && d.ldw % 4 == 0 && (S == 1 || d.w_sample % 4 == 0) && d.ldw <= (1L << 20);
+    p.raw_w = p.pieces == 3 && whole && (R <= 32 || (R <= 128 && up(V, 256) / 256 * S >= kComputeUnits));
     p.pack_w = (p.pieces == 3 && !p.raw_w) || (p.pieces == 1 && (!d.w_aligned || K % 8 || d.ldw % 8 || (S > 1 && d.w_sample % 8) || d.ldw > (1L << 21)));
     p.columns = p.pieces == 3 ? 32 : 64;
     p.row_bytes = up(K, p.columns) * 2;
     p.places = up(R, 256);
-    auto tiles_of = [&](long v, long r) { return ((V + v - 1) / v) * ((R + r - 1) / r) * S; };
-    p.size = R <= 32 ? kFew : (tiles_of(256, 256) >= kComputeUnits ? kLarge : (tiles_of(128, 128) >= kSmallTiles ? kMiddle : kSmall));
+    // The time of a size: rounds of workgroups times what a round takes (a round of large tiles is one; smaller tiles run at lower rates, two of them
+    // to a compute unit but for three pieces of 128 x 128).
+    auto rounds = [&](long v, long r, long to_a_unit) { return (double)((((V + v - 1) / v) * ((R + r - 1) / r) * S + to_a_unit * kComputeUnits - 1) / (to_a_unit * kComputeUnits)); };
+    const bool three = p.pieces == 3;
+    const double large = rounds(256, three ? 128 : 256, 1), middle = rounds(128, 128, three ? 1 : 2) * (three ? 0.62 : 0.67), small = rounds(64, 64, 2) * (three ? 0.42 : 0.25);
+    p.size = R <= 32 ? kFew : p.raw_w ? kTall : (large <= middle && large <= small ? kLarge : (middle <= small ? kMiddle : kSmall));
     p.dz_pieces = p.size == kFew && p.pieces == 1 ? 2 : p.pieces;
-    constexpr int V_TILE[] = {256, 64, 128, 256}, R_TILE[] = {32, 64, 128, 256};
+    constexpr int V_TILE[] = {256, 64, 128, 256, 256}, R_TILE[] = {32, 64, 128, 256, 128};
     p.v_tile = V_TILE[p.size];
     p.r_tile = p.size == kLarge && p.pieces == 3 ? 128 : R_TILE[p.size];
     p.row_tiles = (int)((R + p.r_tile - 1) / p.r_tile);
@@ -993,7 +1011,7 @@ HeadPlan head_plan(const hot_head_desc &d, bool backward, bool with_dx)
 
     // The weights' gradients: as many runs of rows as leave the fewest steps of BK rows in all rounds, twenty more to each run, and as long as their
     // partial sums are no more than two rounds of tiles (5569 x 42 x 1227 float32 without: 195 us on ten workgroups)
-    const int wt = p.size == kLarge ? 256 : (p.size == kMiddle ? 128 : 64), wv = p.size == kLarge && p.pieces == 3 ? 128 : wt;
+    const int wt = p.size >= kLarge ? 256 : (p.size == kMiddle ? 128 : 64), wv = p.size >= kLarge && p.pieces == 3 ? 128 : wt;
     const long w_tiles = ((piece + wv - 1) / wv < (V + wv - 1) / wv ? (piece + wv - 1) / wv : (V + wv - 1) / wv) * ((K + wt - 1) / wt) * S;
     for (long runs = 1; runs <= 256 && (runs == 1 || (runs * 4 * p.columns <= R && runs * w_tiles <= 2 * kComputeUnits)); ++runs) {
         const long depth = up((R + runs - 1) / runs, p.columns), cost = (w_tiles * runs + kComputeUnits - 1) / kComputeUnits * (depth / p.columns + 20);
@@ -1079,7 +1097,10 @@ void head_lists(const HeadCall &c)
     a.count = c.in<int>(p.list_count);
     a.sums = c.in<double>(p.sums);
     a.start = c.in<unsigned short>(p.start);
-    hot_head_lists_kernel<<<dim3((unsigned)((a.lists + kListWaves - 1) / kListWaves)), 64 * kListWaves, 0, c.stream>>>(a);
+    const dim3 grid((unsigned)((a.lists + kListWaves - 1) / kListWaves)), block(64 * kListWaves);
+    if (a.top <= 64) hot_head_lists_kernel<64><<<grid, block, 0, c.stream>>>(a);
+    else if (a.top <= 256) hot_head_lists_kernel<256><<<grid, block, 0, c.stream>>>(a);
+    else hot_head_lists_kernel<kMostTop><<<grid, block, 0, c.stream>>>(a);
 }
 
 RowArgs head_rows(const HeadCall &c, const double *lse, const float *g, long g_sample, long g_row)
@@ -1252,6 +1273,7 @@ template <class T, int PIECES>
 void head_logits(const HeadCall &c, const HeadArgs &a, bool backward)
 {
     if constexpr (PIECES == 3) {
+        if (c.p.size == kTall) return logits_go<Tile<T, PIECES, PIECES, true, true, 256, 128, 8, 1, 2, true, false>, PIECES>(c, a, backward);
         if (c.p.raw_w) return logits_go<Tile<T, PIECES, PIECES, true, true, 256, 32, 8, 1, 4, true, false>, kDz<PIECES>>(c, a, backward);
         if (c.p.size == kFew) return logits_go<Tile<T, PIECES, PIECES, true, true, 256, 32, 8, 1>, kDz<PIECES>>(c, a, backward);
     } else if (c.p.size == kFew) return logits_go<Tile<T, PIECES, PIECES, true, true, 256, 32, 8, 1, 4>, kDz<PIECES>>(c, a, backward);
@@ -1354,7 +1376,9 @@ void head_backward(const HeadCall &c, const double *lse, const float *g, long g_
         if (dx) {
             a.other = h.w;
             a.sample = h.w_sample;
-            if (c.p.raw_w) {
+            if (c.p.size == kTall) {
+                if constexpr (PIECES == 3) head_dx<Tile<E, PIECES, PIECES, true, false, 128, 256, 1, 8, 2, false, true>>(c, a);
+            } else if (c.p.raw_w) {
                 if constexpr (PIECES == 3) head_dx<Tile<E, PIECES, PIECES, true, false, 32, 256, 1, 8, 4, false, true>>(c, a);
             } else if (c.p.size == kFew) head_dx<Tile<E, kDz<PIECES>, PIECES, true, false, 32, 256, 1, 8, PIECES == 1 ? 3 : 2>>(c, a);
             else if (c.p.size == kSmall) head_dx<Tile<E, PIECES, PIECES, true, false, 64, 64, 2, 2, kSmallStages<PIECES>>>(c, a);

@@ -325,15 +325,17 @@ struct Tile {
 };
 
 // Which tile a workgroup takes.  Workgroups go to the eight dies in turn; each die gets a run of tiles and walks it with up to eight
-// tiles of the second dimension side by side, so that tiles that run together share their operands in the die's L2.
+// tiles of the second dimension side by side, so that tiles that run together share their operands in the die's L2.  Where the grid's other
+// dimensions (whose steps are multiples of eight workgroups) have few tiles each, the die that begins turns with them.
 struct Place {
     int m, n;
     bool any;
 };
 
-__device__ __forceinline__ Place place(int id, int m_tiles, int n_tiles)
+__device__ __forceinline__ Place place(int m_tiles, int n_tiles)
 {
-    const int items = m_tiles * n_tiles, per_die = (items + 7) / 8, item = id % 8 * per_die + id / 8;
+    const int id = (int)blockIdx.x, die = (id + (int)blockIdx.y + (int)(blockIdx.z * gridDim.y)) % 8;
+    const int items = m_tiles * n_tiles, per_die = (items + 7) / 8, item = die * per_die + id / 8;
     if (id / 8 >= per_die || item >= items) return {0, 0, false};
     const int group = item / (8 * m_tiles), first = group * 8, wide = n_tiles - first < 8 ? n_tiles - first : 8, in = item - group * 8 * m_tiles;
     return {in / wide, first + in % wide, true};

@@ -78,7 +78,7 @@ def _lists(g, rows, vocab, top, lead=(), ragged=True):
 
 # (rows, width, vocabulary): every size of tile, its edges, odd sizes, one of each
 SIZES = [(1, 1, 1), (1, 8, 2), (2, 16, 31), (5, 24, 300), (31, 40, 257), (32, 64, 256), (33, 64, 64), (40, 7, 65), (64, 33, 130), (65, 192, 10), (129, 72, 1000), (128, 128, 4000),
-         (257, 65, 3000), (300, 520, 5000), (513, 96, 16400), (1030, 48, 20000), (700, 200, 33000)]
+         (257, 65, 3000), (300, 520, 5000), (513, 96, 16400), (1030, 48, 20000), (700, 200, 33000), (20, 36, 40000), (70, 44, 33001), (128, 33, 40000)]
 
 
 @pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])

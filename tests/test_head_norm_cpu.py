@@ -64,7 +64,8 @@ def test_scratch_of_many_shapes(hot):
         places = (rows + 255) // 256 * 256
         fixed = samples * places * (width + 64) * 2 * pieces + samples * rows * (40 + top * 12) + samples * rows * (vocab // 64 + 8) * 2 + 65536
         least_piece = samples * 1280 * (places * 4 * max(2, pieces) + (width + 64) * 2 * pieces)
-        assert got[2] <= fixed + max(least_piece, 300 << 20) + samples * vocab * 4 * (places // 32 + 1), (rows, width, vocab, samples, top, dtype, got)
+        runs = 1024 * 256 * 256 * 4                 # partial sums of the weights' gradients: at most two rounds of tiles, each four times over where they are cut
+        assert got[2] <= fixed + max(least_piece, 300 << 20) + runs + samples * vocab * 4 * (places // 32 + 1), (rows, width, vocab, samples, top, dtype, got)
     for _ in range(2000):
         d = _norm(hot, int(2 ** r.uniform(0, 20)), int(2 ** r.uniform(0, 17)), r.choice([1, 3, 16]))
         n = hot.lib().hot_norm_backward_workspace_bytes(ctypes.byref(d))
