@@ -13,6 +13,8 @@
 // Rows without entries are left out before anything is multiplied, so what they hold (NaN too) reaches no result and costs nothing.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "hot.h"
 #include "vec.h"
 #include "element.h"
@@ -1297,26 +1299,28 @@ void dw_go(const HeadCall &c, const GradArgs &a)
                                     TILE::THREADS, 0, c.stream>>>(a);
 }
 
-// dW on tiles of TILE, or, on tiles of RUN_TILE (whose float32 results have to fit LDS), as partial sums that are then added up
+// dW on tiles of TILE, or, on tiles of RUN_TILE (whose float32 results have to fit LDS), as partial sums that are then added up; void: one run only
 template <class TILE, class T, class RUN_TILE = TILE>
 void head_dw(const HeadCall &c, GradArgs a, void *dw)
 {
     const long part = (long)a.v_count * c.d.width;
     a.row_depth = c.p.run_depth;
-    if (c.p.runs == 1) {
+    if (std::is_void_v<RUN_TILE> || c.p.runs == 1) {
         a.out = dw;
         a.out_sample = c.d.vocab * c.d.width;
         a.out_first = a.v_begin;
         return dw_go<TILE, T>(c, a);
     }
-    float *const parts = c.in<float>(c.p.dw);
-    a.out = parts;
-    a.out_sample = part;
-    a.out_split = c.d.samples * part;
-    a.out_first = 0;
-    dw_go<RUN_TILE, float>(c, a);
-    const RunArgs r = {parts, part, part, a.out_split, c.d.vocab * c.d.width, c.p.runs, static_cast<T *>(dw) + (size_t)a.v_begin * (size_t)c.d.width};
-    hot_head_runs_kernel<T><<<dim3(grid_for((part + Piece<T>::N - 1) / Piece<T>::N), (unsigned)c.d.samples), 256, 0, c.stream>>>(r);
+    if constexpr (!std::is_void_v<RUN_TILE>) {
+        float *const parts = c.in<float>(c.p.dw);
+        a.out = parts;
+        a.out_sample = part;
+        a.out_split = c.d.samples * part;
+        a.out_first = 0;
+        dw_go<RUN_TILE, float>(c, a);
+        const RunArgs r = {parts, part, part, a.out_split, c.d.vocab * c.d.width, c.p.runs, static_cast<T *>(dw) + (size_t)a.v_begin * (size_t)c.d.width};
+        hot_head_runs_kernel<T><<<dim3(grid_for((part + Piece<T>::N - 1) / Piece<T>::N), (unsigned)c.d.samples), 256, 0, c.stream>>>(r);
+    }
 }
 
 // T: the type of the tensors; E: of the tiles' elements
@@ -1389,7 +1393,7 @@ void head_backward(const HeadCall &c, const double *lse, const float *g, long g_
         if (dw) {
             a.other = h.x;
             a.sample = h.x_sample;
-            if (c.p.size == kFew) head_dw<Tile<E, PIECES, kDz<PIECES>, false, false, 64, 64, 2, 2>, T>(c, a, dw);
+            if (c.p.size == kFew) head_dw<Tile<E, PIECES, kDz<PIECES>, false, false, 256, 64, 4, 1, 1>, T, void>(c, a, dw);
             else if (c.p.size == kSmall) head_dw<Tile<E, PIECES, PIECES, false, false, 64, 64, 2, 2, kSmallStages<PIECES>>, T>(c, a, dw);
             else if (c.p.size == kMiddle) head_dw<Tile<E, PIECES, PIECES, false, false, 128, 128, 2, 2>, T>(c, a, dw);
             else if constexpr (PIECES == 1) head_dw<Tile<E, PIECES, PIECES, false, false, 256, 256, 2, 4>, T, Tile<E, PIECES, PIECES, false, false, 128, 128, 2, 2>>(c, a, dw);

@@ -180,14 +180,15 @@ __device__ __forceinline__ void raw_fragment(const lds_char *tile, int line0, in
     p2 = __builtin_bit_cast(s8v, p[2]);
 }
 
-// STAGES tiles lie in LDS: two, or more where a tile is short work and latency counts; the loads of STAGES - 1 of them are under way.
+// STAGES tiles lie in LDS: two, or more where a tile is short work and latency counts; the loads of STAGES - 1 of them are under way.  One: the
+// contraction has no more than BK indices.
 template <class T_, int PIECES_A_, int PIECES_B_, bool A_ALONG_, bool B_ALONG_, int BM_, int BN_, int WAVES_M_, int WAVES_N_, int STAGES_ = 2, bool RAW_A_ = false, bool RAW_B_ = false>
 struct Tile {
     typedef T_ T;
     static constexpr int PIECES_A = PIECES_A_, PIECES_B = PIECES_B_, BM = BM_, BN = BN_, WAVES_M = WAVES_M_, WAVES_N = WAVES_N_;
     static constexpr int STAGES = STAGES_;
     static constexpr bool A_ALONG = A_ALONG_, B_ALONG = B_ALONG_, RAW_A = RAW_A_, RAW_B = RAW_B_;
-    static_assert(STAGES >= 2 && (!RAW_A || PIECES_A == 3) && (!RAW_B || PIECES_B == 3), "");
+    static_assert(STAGES >= 1 && (!RAW_A || PIECES_A == 3) && (!RAW_B || PIECES_B == 3), "");
     static constexpr int BK = PIECES_A == 3 ? 32 : 64;
     static constexpr int WAVES = WAVES_M * WAVES_N, THREADS = 64 * WAVES, WM = BM / WAVES_M, WN = BN / WAVES_N, MB = WM / 32, NB = WN / 32;
     typedef Stage<BM, BK, A_ALONG, PIECES_A, WAVES, RAW_A> StageA;
@@ -250,7 +251,7 @@ struct Tile {
 
     // One tile of contraction indices: the tile `here`, while the ones behind it are on their way.  `before`: the room of the tile before, which the
     // rest of tile STAGES - 1 from here goes to (with two stages that is `next`).
-    static constexpr int kSteps = BK / 16, kEarly = (kLoads + 1) / 2, kAhead = (STAGES - 2) * kLoads;
+    static constexpr int kSteps = BK / 16, kEarly = (kLoads + 1) / 2, kAhead = STAGES > 2 ? (STAGES - 2) * kLoads : 0;
     static __device__ __forceinline__ void ask(const Operand &a, const Operand &b, const StageA &sa, const StageB &sb, int k0, lds_char *to, int j)
     {
         if (j < StageA::kAll) sa.ask(a, k0, to, j);
@@ -300,20 +301,33 @@ struct Tile {
         const StageB sb(b, w, l);
         TileAcc<T> acc[MB][NB];
         Operands now[2];
+        if constexpr (STAGES == 1) {
 #pragma unroll
-        for (int t = 0; t < STAGES - 1; ++t)
+            for (int j = 0; j < kLoads; ++j) ask(a, b, sa, sb, 0, lds, j);
+            arrive();
 #pragma unroll
-            for (int j = 0; j < kLoads; ++j) ask(a, b, sa, sb, t * BK, lds + t * kStage, j);
-        arrive<kAhead>();
+            for (int ks = 0; ks < kSteps; ++ks) {
 #pragma unroll
-        for (int j = 0; j < kEarly; ++j) ask(a, b, sa, sb, (STAGES - 1) * BK, lds + (STAGES - 1) * kStage, j);
+                for (int i = 0; i < kReads; ++i) now[ks & 1].read(lds, ks, i);
 #pragma unroll
-        for (int i = 0; i < kReads; ++i) now[0].read(lds, 0, i);         // (of zeros where depth is 0)
-        int at = 0;
-        for (int k0 = 0; k0 < depth; k0 += BK) {
-            const int behind = at + kStage < kLds ? at + kStage : 0, before = at > 0 ? at - kStage : kLds - kStage;
-            step(lds + at, lds + behind, lds + before, a, b, sa, sb, k0, now, acc);
-            at = behind;
+                for (int part = 0; part < kParts; ++part) multiply(now[ks & 1], acc, part);
+            }
+        } else {
+#pragma unroll
+            for (int t = 0; t < STAGES - 1; ++t)
+#pragma unroll
+                for (int j = 0; j < kLoads; ++j) ask(a, b, sa, sb, t * BK, lds + t * kStage, j);
+            arrive<kAhead>();
+#pragma unroll
+            for (int j = 0; j < kEarly; ++j) ask(a, b, sa, sb, (STAGES - 1) * BK, lds + (STAGES - 1) * kStage, j);
+#pragma unroll
+            for (int i = 0; i < kReads; ++i) now[0].read(lds, 0, i);         // (of zeros where depth is 0)
+            int at = 0;
+            for (int k0 = 0; k0 < depth; k0 += BK) {
+                const int behind = at + kStage < kLds ? at + kStage : 0, before = at > 0 ? at - kStage : kLds - kStage;
+                step(lds + at, lds + behind, lds + before, a, b, sa, sb, k0, now, acc);
+                at = behind;
+            }
         }
         arrive();
         const TileSettled settled;

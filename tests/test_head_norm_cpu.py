@@ -138,7 +138,7 @@ def test_product_loops_wait_once_for_a_tile(tmp_path):
     subprocess.run([build.HIPCC] + build.FLAGS + ["-S", "--cuda-device-only", "-o", str(out), src], check=True, capture_output=True)
     text, loops = out.read_text(), 0
     for m in re.finditer(r"^(_Z\w+):[^\n]*\n(.*?)\.Lfunc_end", text, re.S | re.M):
-        if "v_mfma" not in m.group(2):
+        if "v_mfma" not in m.group(2) or re.search(r"ELi\d+ELi\d+ELi1ELb[01]ELb[01]EEE", m.group(1)):       # (one tile: no loop)
             continue
         blocks = re.split(r"^\.LBB\S+:", m.group(2), flags=re.M)
         at = [i for i, b in enumerate(blocks) if "v_mfma" in b]         # (where some waves load and others do not, the loop has branches)
