@@ -68,6 +68,22 @@ struct Operand {
     int depth;           // how many contraction indices there are; the others are zeros
 };
 
+// Which of a row's chunks lies where (exclusive or), so that the lanes that LDS serves at once, 256 bytes, are in different banks: sixteen rows read sixteen bytes
+// each along; across, four rows 64 bytes each, or, of float32, two rows eight apart.  (With only eight rows and 128 bytes told apart, half of the cycles that
+// LDS worked were conflicts.)
+template <int PER_ROW>
+__device__ __forceinline__ int chunk_along(int row)
+{
+    return PER_ROW == 8 ? row >> 1 & 7 : row >> 2 & 3;
+}
+
+template <int T, bool RAW>
+__device__ __forceinline__ int chunk_across(int row)
+{
+    static_assert(T >= 64, "a row holds the chunks told apart");
+    return RAW ? (row >> 3 & 1) << 3 : (T >= 128 ? (row & 3) << 2 : (row >> 1 & 1) << 2);
+}
+
 // Lines and indices are taken sixteen bytes at a time along memory: a row may be read up to the next multiple of that, and must be finite there or
 // meet zeros of the other operand.  RAW: float32 as it lies, cut into pieces only where a wave reads its operands from LDS.
 template <int T, int BK, bool ALONG, int PIECES, int WAVES, bool RAW>
@@ -84,12 +100,11 @@ struct Stage {
     int index[ALONG ? 1 : kEach];          // the contraction index of this lane's loads in a tile
     int wave;
 
-    // the order of a row's chunks, so that neither form of reading meets its own banks
+    // the order of a row's chunks
     static __device__ __forceinline__ int permuted(int row)
     {
-        if constexpr (!ALONG) return RAW ? 0 : (row & 3) << 1;
-        else if constexpr (kPerRow == 8) return row & 7;
-        else return row >> 1 & 3;
+        if constexpr (ALONG) return chunk_along<kPerRow>(row);
+        else return chunk_across<T, RAW>(row);
     }
 
     __device__ __forceinline__ int load(int i) const { return (wave + i * WAVES) % kLoads; }
@@ -136,10 +151,10 @@ __device__ __forceinline__ s8v fragment(const lds_char *tile, int line0, int ks,
     const int half = lane >> 5;
     if constexpr (ALONG) {
         const int row = line0 + (lane & 31), chunk = ks * 2 + half;
-        return *(const lds_s8v *)(tile + row * (BK * 2) + ((chunk ^ (BK == 64 ? row & 7 : row >> 1 & 3)) << 4));
+        return *(const lds_s8v *)(tile + row * (BK * 2) + ((chunk ^ chunk_along<BK / 8>(row)) << 4));
     } else {
         const int i = lane & 15, row = ks * 16 + half * 8 + (i >> 2);
-        const int byte = (line0 + (lane & 16) + (i & 3) * 4) * 2 ^ (i >> 2) << 5;
+        const int byte = (line0 + (lane & 16) + (i & 3) * 4) * 2 ^ chunk_across<T, false>(i >> 2) << 4;        // (the same for row + 4)
         const s4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v *)(tile + row * (T * 2) + byte));
         const s4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v *)(tile + (row + 4) * (T * 2) + byte));
         return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -159,13 +174,13 @@ __device__ __forceinline__ void raw_fragment(const lds_char *tile, int line0, in
         static_assert(BK == 32, "");
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const f4v q = *(const lds_f4v *)(tile + line * (BK * 4) + (((ks * 2 + half) * 2 + h) ^ (line & 7)) * 16);
+            const f4v q = *(const lds_f4v *)(tile + line * (BK * 4) + (((ks * 2 + half) * 2 + h) ^ chunk_along<8>(line)) * 16);
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[4 * h + j] = q[j];
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = *(const lds_float *)(tile + (ks * 16 + half * 8 + j) * (T * 4) + line * 4);
+        for (int j = 0; j < 8; ++j) v[j] = *(const lds_float *)(tile + (ks * 16 + half * 8 + j) * (T * 4) + (line * 4 ^ chunk_across<T, true>(half * 8) << 4));
     }
     bf16x8 p[3];
 #pragma unroll
