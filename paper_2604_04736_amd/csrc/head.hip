@@ -13,6 +13,7 @@
 // Rows without entries are left out before anything is multiplied, so what they hold (NaN too) reaches no result and costs nothing.
 #include <hip/hip_runtime.h>
 
+#include <climits>
 #include <type_traits>
 
 #include "hot.h"
@@ -157,6 +158,44 @@ hot_head_lists_kernel(ListArgs a)
 
 // --------------------------------------------------------------------------- the rows that count
 
+// The features' gradients: a run of a piece's words to a workgroup.  A round of workgroups takes its steps of 64 words, and as long as some twenty
+// of them for its start and for adding to the sums in memory; of the numbers of runs up to 64 the one with the fewest such steps is taken, by the host for all
+// rows (workgroups and sums of that many), and by the device for the rows that count within what the host gave (all passes of
+// 900 x 768 x 20000 float32 of which 65 % are left out: 354 -> 324 us, 2048 x 1024 x 30000 bf16, 70 %: 257 -> 244).
+struct WordRuns {
+    int rows_log, at_once_log;     // rows of a tile and workgroups that run at once, powers of two
+    int width_tiles, samples, piece;
+    long workgroups, sums;         // of one sample: workgroups, rows of sums
+    int *depth;                    // [samples]: words of a run; null in the forward pass
+};
+
+__host__ __device__ inline long up_shift(long n, int log) { return (n + (1L << log) - 1) >> log; }
+
+__host__ __device__ inline int run_depth(int piece, int runs) { return (int)(((unsigned)(piece + runs - 1) / (unsigned)runs + 63) & ~63u); }
+
+__host__ __device__ inline bool run_possible(const WordRuns &a, long rows, int runs)
+{
+    return runs == 1 || (runs * 256 <= a.piece && runs * place_blocks(a.width_tiles, up_shift(rows, a.rows_log)) <= a.workgroups && runs * rows <= a.sums);
+}
+
+__host__ __device__ inline long run_steps(const WordRuns &a, long rows, int runs)
+{
+    return up_shift(up_shift(rows, a.rows_log) * a.width_tiles * a.samples * runs, a.at_once_log) * (run_depth(a.piece, runs) / 64 + 20);
+}
+
+// by one wave, a number of runs to a lane
+__device__ __forceinline__ void choose_runs(const WordRuns &a, long s, int rows)
+{
+    const int runs = ((int)threadIdx.x & 63) + 1;
+    unsigned long long best = run_possible(a, rows, runs) ? (unsigned long long)run_steps(a, rows, runs) << 6 | (unsigned)(runs - 1) : ~0ull;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const unsigned long long other = __shfl_xor(best, d);
+        best = other < best ? other : best;
+    }
+    if (runs == 1) a.depth[s] = run_depth(a.piece, (int)(best & 63) + 1);
+}
+
 struct RowArgs {
     long rows, vocab;
     long idx_sample, idx_row;
@@ -173,6 +212,7 @@ struct RowArgs {
     int *label;                    // [samples, rows] by place (-1: no word)
     float *hi, *lo, *grad;         // by place: lse in base 2 as two floats, the row's gradient
     float *scale;                  // [samples, 2]: what gradients are multiplied with, and what results are multiplied with in turn
+    WordRuns runs;
 };
 
 // The rows of sample s that count, in order: how many, and (WRITE) the arrays by place.  `map` (LDS, rows of them, or null): the row at a place.
@@ -229,6 +269,7 @@ __device__ __forceinline__ int find_rows(const RowArgs &a, long s, unsigned shor
     }
     if constexpr (WRITE) {
         if (threadIdx.x == 0) a.count[s] = before;
+        if (wave == 0 && a.runs.depth) choose_runs(a.runs, s, before);
         if (a.lse) {
             largest = wave_max(largest);
             if (lane == 0) most[wave] = largest;
@@ -719,9 +760,9 @@ struct GradArgs {
     int width, vocab, v_begin, v_count;
     long rows;
     const int *count;
-    int samples, splits, split_depth;
+    WordRuns runs;                 // of words
     bool first;                    // of the pieces: sums begin with it
-    float *sums;                   // dx: [split][sample][place][width]
+    float *sums;                   // dx: [sample], its runs.sums rows: [run][place][width]
     void *out;                     // dW, or its partial sums: [run of rows] out_split apart, [sample], words from out_first on
     long out_sample, out_split;
     int out_first, row_depth;      // rows of a run
@@ -736,16 +777,17 @@ hot_head_dx_kernel(GradArgs a)
 {
     __shared__ __attribute__((aligned(1024))) char memory[TILE::kLds];
     const long s = blockIdx.y;
-    const int split = (int)blockIdx.z, count = a.count[s];
-    const Place at = place((a.width + TILE::BN - 1) / TILE::BN, (count + TILE::BM - 1) / TILE::BM);
-    if (!at.any) return;
-    const int r0 = at.n * TILE::BM, k0 = at.m * TILE::BN, v = split * a.split_depth;
-    const int depth = a.v_count - v < a.split_depth ? a.v_count - v : a.split_depth;
+    const int count = a.count[s], each = a.runs.depth[s], k_tiles = (a.width + TILE::BN - 1) / TILE::BN, r_tiles = (count + TILE::BM - 1) / TILE::BM;
+    if (count == 0) return;
+    const int id = (int)(blockIdx.x + gridDim.x * blockIdx.z), tiles = (int)place_blocks(k_tiles, r_tiles), run = id / tiles;
+    const Place at = place(k_tiles, r_tiles, id - run * tiles, (int)blockIdx.y + run * (int)gridDim.y);
+    if (run >= (a.runs.piece + each - 1) / each || !at.any) return;
+    const int r0 = at.n * TILE::BM, k0 = at.m * TILE::BN, v = run * each, depth = a.v_count - v < each ? a.v_count - v : each;
     f16v acc[TILE::MB][TILE::NB];
     const Operand dz = {part(a.dz, s * a.dz_sample + v / TILE::BK * a.dz.block + r0 * a.dz.pitch), count - r0, depth};
     const Operand w = {part(a.other, s * a.sample + v * a.other.pitch + k0 / TILE::BK * a.other.block), a.width - k0, depth};
     TILE::product((lds_char *)memory, dz, w, depth, acc);
-    float *const sums = a.sums + ((size_t)split * (size_t)a.samples + (size_t)s) * (size_t)a.rows * (size_t)a.width;
+    float *const sums = a.sums + ((size_t)s * (size_t)a.runs.sums + (size_t)run * (size_t)count) * (size_t)a.width;
 #pragma unroll
     for (int m = 0; m < TILE::MB; ++m)
 #pragma unroll
@@ -860,12 +902,13 @@ __device__ __forceinline__ void bias_gradient(const BiasArgs &a, long s, int fir
 }
 
 struct FeatureArgs {
-    const float *sums;             // [split][sample][place][width]
-    const int *place_of;
+    const float *sums;             // as above
+    const int *place_of, *count;
+    WordRuns runs;
     const float *scale;
     float temperature;
     long rows, width;
-    int samples, splits;
+    int samples;
     bool shared;                   // all samples have the same features: their gradients are added
     void *out;
 };
@@ -885,8 +928,9 @@ __device__ __forceinline__ void feature_gradient(const FeatureArgs &a, long samp
             const int at = a.place_of[s * a.rows + row];
             if (at < 0) continue;
             typename Piece<T>::F sum = typename Piece<T>::F(0.0f);
-            for (int k = 0; k < a.splits; ++k) {
-                const float *const p = a.sums + (((size_t)k * (size_t)a.samples + (size_t)s) * (size_t)a.rows + (size_t)at) * (size_t)a.width;
+            const int runs = (a.runs.piece + a.runs.depth[s] - 1) / a.runs.depth[s], count = a.count[s];
+            for (int k = 0; k < runs; ++k) {
+                const float *const p = a.sums + ((size_t)s * (size_t)a.runs.sums + (size_t)k * (size_t)count + (size_t)at) * (size_t)a.width;
 #pragma unroll
                 for (int h = 0; h < N; h += 4) {
                     const Piece<float>::F v = Piece<float>::load(p, col + h, a.width);
@@ -936,10 +980,11 @@ struct HeadPlan {
     int size;                // kFew ... kLarge
     int v_tile, r_tile;      // words and rows of a tile of logits
     int row_tiles;
-    int splits, split_depth; // runs of words of a piece, and their length
+    WordRuns word_runs;       // runs of words of the features' gradients
+    int most_word_runs;
     int runs, run_depth;     // runs of rows of the weights' gradients, and their length
     // where things lie in the workspace
-    int64_t word, weight, list_count, sums, start, count, row_of, place_of, label, hi, lo, grad, scale, x, w, dz, partials, dx, db, dw, bytes;
+    int64_t word, weight, list_count, sums, start, count, word_run, row_of, place_of, label, hi, lo, grad, scale, x, w, dz, partials, dx, db, dw, bytes;
 };
 
 struct Layout {
@@ -997,19 +1042,18 @@ HeadPlan head_plan(const hot_head_desc &d, bool backward, bool with_dx)
     }
     p.v_piece = (int)piece;
     p.v_pieces = (int)((V + piece - 1) / piece);
-    // The features' gradients: a run of the piece's words to a workgroup.  A round of workgroups takes its steps of 64 words, and as long as some
-    // twenty of them for its start and for adding to the sums in memory; the number of runs with the fewest such steps is taken.
-    const int bm = p.r_tile, bn = V_TILE[p.size];
-    const long tiles = ((R + bm - 1) / bm) * ((K + bn - 1) / bn) * S, at_once = kComputeUnits * (p.size == kLarge || p.pieces == 3 ? 1 : 2);
+    // as many workgroups and sums as the best number of runs needs for all rows
+    WordRuns &w = p.word_runs;
+    static_assert(kComputeUnits == 256, "");
+    w = {__builtin_ctz((unsigned)p.r_tile), p.size == kLarge || p.pieces == 3 ? 8 : 9, (int)((K + V_TILE[p.size] - 1) / V_TILE[p.size]), (int)S, (int)piece, LONG_MAX, LONG_MAX, nullptr};
+    int best_runs = 1;
+    for (int runs = 2; runs <= 64 && run_possible(w, R, runs); ++runs)
+        if (run_steps(w, R, runs) < run_steps(w, R, best_runs)) best_runs = runs;
+    best_runs = (int)((piece + run_depth((int)piece, best_runs) - 1) / run_depth((int)piece, best_runs));
+    p.most_word_runs = best_runs;
+    w.workgroups = best_runs * place_blocks(w.width_tiles, (R + p.r_tile - 1) / p.r_tile);
+    w.sums = best_runs * R;
     long best = 0;
-    for (long runs = 1; runs <= 64 && (runs == 1 || runs * 256 <= piece); ++runs) {
-        const long depth = up((piece + runs - 1) / runs, 64), cost = (tiles * runs + at_once - 1) / at_once * (depth / 64 + 20);
-        if (runs == 1 || cost < best) {
-            best = cost;
-            p.split_depth = (int)depth;
-        }
-    }
-    p.splits = (int)((piece + p.split_depth - 1) / p.split_depth);
 
     // The weights' gradients: as many runs of rows as leave the fewest steps of BK rows in all rounds, twenty more to each run, and as long as their
     // partial sums are no more than two rounds of tiles (5569 x 42 x 1227 float32 without: 195 us on ten workgroups)
@@ -1032,6 +1076,7 @@ HeadPlan head_plan(const hot_head_desc &d, bool backward, bool with_dx)
     p.sums = l.take(lists * 16);
     p.start = l.take(lists * (marks + 1) * 2);
     p.count = l.take(S * 4);
+    p.word_run = l.take(S * 4);
     p.row_of = l.take(S * R * 4);
     p.place_of = l.take(S * R * 4);
     p.label = l.take(d.top > 0 ? 0 : S * R * 4);
@@ -1047,7 +1092,7 @@ HeadPlan head_plan(const hot_head_desc &d, bool backward, bool with_dx)
         p.dz = l.take(S * p.places * piece * 2 * p.dz_pieces);
         p.db = l.take(S * p.row_tiles * piece * 4);
         p.dw = l.take(p.runs > 1 ? (int64_t)p.runs * S * (piece < V ? piece : V) * K * 4 : 0);
-        if (with_dx) p.dx = l.take((int64_t)p.splits * S * R * K * 4);
+        if (with_dx) p.dx = l.take(p.word_runs.sums * S * K * 4);
     } else {
         p.partials = l.take(S * ((V + p.v_tile - 1) / p.v_tile) * 3 * p.places * 4);
     }
@@ -1105,6 +1150,13 @@ void head_lists(const HeadCall &c)
     else hot_head_lists_kernel<kMostTop><<<grid, block, 0, c.stream>>>(a);
 }
 
+WordRuns head_runs(const HeadCall &c)
+{
+    WordRuns a = c.p.word_runs;
+    a.depth = c.in<int>(c.p.word_run);
+    return a;
+}
+
 RowArgs head_rows(const HeadCall &c, const double *lse, const float *g, long g_sample, long g_row)
 {
     const hot_head_desc &d = c.d;
@@ -1131,6 +1183,7 @@ RowArgs head_rows(const HeadCall &c, const double *lse, const float *g, long g_s
     a.lo = c.in<float>(p.lo);
     a.grad = c.in<float>(p.grad);
     a.scale = c.in<float>(p.scale);
+    if (lse) a.runs = head_runs(c);
     return a;
 }
 
@@ -1288,7 +1341,7 @@ void head_logits(const HeadCall &c, const HeadArgs &a, bool backward)
 template <class TILE>
 void head_dx(const HeadCall &c, const GradArgs &a)
 {
-    hot_head_dx_kernel<TILE><<<dim3((unsigned)place_blocks((c.d.width + TILE::BN - 1) / TILE::BN, (c.d.rows + TILE::BM - 1) / TILE::BM), (unsigned)c.d.samples, (unsigned)a.splits),
+    hot_head_dx_kernel<TILE><<<dim3((unsigned)place_blocks((c.d.width + TILE::BN - 1) / TILE::BN, (c.d.rows + TILE::BM - 1) / TILE::BM), (unsigned)c.d.samples, (unsigned)c.p.most_word_runs),
                                TILE::THREADS, 0, c.stream>>>(a);
 }
 
@@ -1370,9 +1423,7 @@ void head_backward(const HeadCall &c, const double *lse, const float *g, long g_
         a.v_count = h.v_count;
         a.rows = h.rows;
         a.count = h.count;
-        a.samples = c.d.samples;
-        a.splits = c.p.splits;
-        a.split_depth = c.p.split_depth;
+        a.runs = head_runs(c);
         a.first = v == 0;
         a.sums = c.in<float>(c.p.dx);
         a.scale = scale;
@@ -1402,7 +1453,7 @@ void head_backward(const HeadCall &c, const double *lse, const float *g, long g_
         const bool finish_x = dx && v + n >= c.d.vocab;
         if (!db && !finish_x) continue;
         const BiasArgs b = {h.sums, c.p.row_tiles, c.p.r_tile, c.p.v_piece, h.v_begin, h.v_count, h.count, scale, a.temperature, db, c.d.vocab, c.d.dtype};
-        const FeatureArgs f = {c.in<float>(c.p.dx), c.in<int>(c.p.place_of), scale, a.temperature, c.d.rows, c.d.width, c.d.samples, c.p.splits,
+        const FeatureArgs f = {c.in<float>(c.p.dx), c.in<int>(c.p.place_of), h.count, a.runs, scale, a.temperature, c.d.rows, c.d.width, (int)c.d.samples,
                                c.d.samples > 1 && c.d.x_sample == 0, dx};
         const unsigned xb = finish_x ? grid_for(c.d.rows * ((c.d.width + Piece<T>::N - 1) / Piece<T>::N)) : 0, bb = db ? (unsigned)((n + 255) / 256) : 0;
         hot_head_finish_kernel<T><<<dim3(xb + bb, (unsigned)c.d.samples), 256, 0, c.stream>>>(f, b, (int)xb);

@@ -361,16 +361,18 @@ struct Place {
     bool any;
 };
 
-__device__ __forceinline__ Place place(int m_tiles, int n_tiles)
+__device__ __forceinline__ Place place(int m_tiles, int n_tiles, int id, int turn)
 {
-    const int id = (int)blockIdx.x, die = (id + (int)blockIdx.y + (int)(blockIdx.z * gridDim.y)) % 8;
+    const int die = (id + turn) % 8;
     const int items = m_tiles * n_tiles, per_die = (items + 7) / 8, item = die * per_die + id / 8;
     if (id / 8 >= per_die || item >= items) return {0, 0, false};
     const int group = item / (8 * m_tiles), first = group * 8, wide = n_tiles - first < 8 ? n_tiles - first : 8, in = item - group * 8 * m_tiles;
     return {in / wide, first + in % wide, true};
 }
 
-inline long place_blocks(long m_tiles, long n_tiles) { return (m_tiles * n_tiles + 7) / 8 * 8; }
+__device__ __forceinline__ Place place(int m_tiles, int n_tiles) { return place(m_tiles, n_tiles, (int)blockIdx.x, (int)(blockIdx.y + blockIdx.z * gridDim.y)); }
+
+__host__ __device__ inline long place_blocks(long m_tiles, long n_tiles) { return (m_tiles * n_tiles + 7) & ~7L; }
 
 }  // namespace
 

@@ -173,6 +173,19 @@ def test_rows_left_out_take_no_part(kind, rows):
     assert all(torch.equal(got[n], clean[n]) for n in got)
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("shared_x", [False, True])
+@pytest.mark.parametrize("rows,width,vocab", [(30, 40, 9000), (300, 72, 5000), (1500, 40, 20001)])
+def test_as_many_rows_as_count_choose_the_runs_of_words(kind, shared_x, rows, width, vocab):
+    """Samples of which all, a third, one, and none of the rows are labelled: each has runs of its own for its features' gradients."""
+    x, w, b, up, g = _inputs(kind, rows, width, vocab, 4, False, shared_x)
+    labels = torch.randint(0, vocab, (4, rows), device=DEV, generator=g)
+    place = torch.rand(4, rows, device=DEV, generator=g).argsort(1)
+    for s, kept in enumerate((rows, rows // 3, 1, 0)):
+        labels[s, place[s, kept:]] = -100
+    _check(x, w, b, up, labels)
+
+
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
 def test_no_row_counts_and_no_rows(kind):
     for rows in (0, 1, 33, 1100):
