@@ -300,6 +300,8 @@ class _Head(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, grad_loss):
         x, weight, bias, index, logit, lse = ctx.saved_tensors
+        if ctx.needs_input_grad[0] and x.shape[0] > 1 and x.stride(0) == 0:
+            x = x.contiguous()          # (features expanded over the samples: on one memory the call forms one gradient for all of them)
         dx, dw, db = (torch.empty(t.shape, dtype=t.dtype, device=t.device) if want else None for t, want in zip((x, weight, bias), ctx.needs_input_grad[:3]))
         hot.hot_head_backward(x, weight, bias, index, logit, lse, grad_loss, dx, dw, db, *ctx.rule)
         return dx, dw, db, None, None, None, None

@@ -945,8 +945,11 @@ def hot_head_forward(x, weight, bias, index, logit, loss, lse=None, ignore_index
 def hot_head_backward(x, weight, bias, index, logit, lse, grad_loss, dx=None, grad_weight=None, grad_bias=None, ignore_index: int = -100,
                       temperature: float = 1.0, workspace=None) -> None:
     """Gradients of the features (x's shape), the weights [samples, vocab, width] and the bias [samples, vocab] from those of the rows'
-    losses (grad_loss, float32 [samples, rows], any strides); each result may be None and is then left out."""
+    losses (grad_loss, float32 [samples, rows], any strides); each result may be None and is then left out.  Features that all samples
+    share are x [1, rows, width], and so is their gradient, summed over the samples."""
     d = _head_desc(x, weight, bias, index, logit, ignore_index, temperature)
+    if dx is not None and x.shape[0] > 1 and d.x_sample == 0:
+        raise ValueError("x: the samples lie on one memory, whose gradient is [1, rows, width]; need x[:1], or a copy for a gradient of each")
     _dense(lse, (d.samples, d.rows), torch.float64, x, "lse")
     if not (grad_loss.is_cuda and grad_loss.device == x.device and grad_loss.dtype == torch.float32 and tuple(grad_loss.shape) == (d.samples, d.rows)):
         raise TypeError(f"grad_loss: need a float32 tensor of shape {(d.samples, d.rows)} on {x.device}")
