@@ -538,7 +538,8 @@ int hot_stats_whole(const float *yhat, int64_t m, int64_t ld, int32_t s, int32_t
  * Around a network's head: layer norm, and a linear head's loss over a vocabulary without logits in memory.  What the sample layer
  * draws ([S_loc, N]) holds the weights of both, one set per sample, as views; networks whose weights are no samples use the same
  * calls with one set.  Tensors are float32, bfloat16 or float16; sums, statistics and losses are held in 32 bits or more, and a result is
- * rounded to its type once.  Pointers need the alignment of their elements.  Runs on the current device; DEVICE pointers;
+ * rounded to its type once.  The gradients of logits, which are operands of matrix products, are held in pieces of 16 bits: three for
+ * float32, two for bfloat16 (2^-16 of each) and float16 (2^-22, or steps of 2^-39 of a sample's largest grad_loss).  Pointers need the alignment of their elements.  Runs on the current device; DEVICE pointers;
  * workspaces are the caller's scratch (16-byte aligned, contents free before and after).
  */
 #define HOT_F32 0

@@ -7,14 +7,13 @@
 //
 // The forward pass multiplies tiles of vocabulary by tiles of rows; a tile leaves per row its largest logit, its sum of exponentials and its
 // share of sum_j p_j z, which a second kernel joins.  The backward pass walks the vocabulary in pieces: it forms a piece's logits again,
-// leaves dz of that piece in scratch memory (16 bits, or three bf16 pieces of float32) and multiplies it with W and with x.  Its
-// products are 2 R V K operations each, one forward and three backward; what bounds them is the matrix pipes from some hundred rows
-// on, below that reading W.
+// leaves dz of that piece in scratch memory (two 16-bit pieces, or three bf16 pieces of float32) and multiplies it with W and with x.  Its
+// products are 2 R V K operations each, one forward and five backward (the two with dz twice over); what bounds them is the matrix pipes from
+// some hundred rows on, below that reading W.
 // Rows without entries are left out before anything is multiplied, so what they hold (NaN too) reaches no result and costs nothing.
 #include <hip/hip_runtime.h>
 
 #include <climits>
-#include <type_traits>
 
 #include "hot.h"
 #include "vec.h"
@@ -26,7 +25,8 @@ namespace {
 constexpr int kComputeUnits = 256;
 constexpr int kMostTop = 1024;           // entries of a row (they are sorted in LDS)
 constexpr int kStartStep = 128;          // words between the marks into a row's sorted entries
-constexpr float kHalfScale = 4096.0f;    // fp16 logits' gradients are held times this: a probability of 1e-11 still counts, 16 x 4096 does not overflow
+// fp16: dz is held in units of 2^-15 of a sample's largest gradient (|q - p| <= 1: no overflow), its two pieces in steps of 2^-39 of it
+constexpr float kHalfScale = 32768.0f;
 
 inline __host__ __device__ long up(long n, long to) { return (n + to - 1) / to * to; }
 
@@ -591,7 +591,8 @@ template <class TILE, bool LISTS, int PIECES>
 __global__ void __launch_bounds__(TILE::THREADS)
 hot_head_dz_kernel(HeadArgs a)
 {
-    constexpr int PITCH = TILE::BM * 2 + 16, NEED = TILE::BN * PITCH;       // (16 bytes on: rows of a column of lanes lie in different banks)
+    constexpr int PITCH = TILE::BM * 2 + 16;       // (16 bytes on: rows of a column of lanes lie in different banks)
+    constexpr int ROWS = TILE::WAVES_N * 32, NEED = PIECES * ROWS * PITCH;
     // (one array: beside a second one the compiler would wait for every load in flight before it reads either)
     constexpr int ROOM = TILE::kLds > NEED ? TILE::kLds : NEED;
     __shared__ __attribute__((aligned(1024))) char memory[ROOM + TILE::BM * 4];
@@ -623,45 +624,46 @@ hot_head_dz_kernel(HeadArgs a)
                 acc[m][n][i] = __builtin_amdgcn_exp2f(TILE::PIECES_A == 1 ? z : z - lo[n]);
             }
     rows.targets(a, v0, [&](int n, int m, int i, bool mine, float weight) { acc[m][n][i] -= mine ? weight : 0.0f; });
-    // to rows of words, piece by piece, through LDS
+    // to rows of words through LDS, all pieces of a block of rows of every wave at once
     typedef typename TILE::T T;
     typedef T V4 __attribute__((ext_vector_type(4)));
     typedef T V8 __attribute__((ext_vector_type(8)));
-    constexpr int BK = TILE::BK;
-    constexpr int PAIRS = TILE::BM / 2, RUNS = TILE::THREADS / PAIRS;
+    constexpr int BK = TILE::BK, PAIRS = TILE::BM / 2, RUNS = TILE::THREADS / PAIRS, CHUNKS = TILE::BM / 8;
     float sum[2] = {0.0f, 0.0f};
     char *const out = a.dz + (size_t)s * (size_t)a.dz_sample + (size_t)((v0 - a.v_begin) / BK) * (size_t)a.dz_block + (size_t)r0 * (BK * 2);
+    const int mine = TILE::n0() / TILE::WN * 32 + (TILE::lane() & 31);
 #pragma unroll
-    for (int p = 0; p < PIECES; ++p) {
-        if (p) __syncthreads();
+    for (int n = 0; n < TILE::NB; ++n) {
+        if (n) __syncthreads();
 #pragma unroll
-        for (int n = 0; n < TILE::NB; ++n)
+        for (int m = 0; m < TILE::MB; ++m)
 #pragma unroll
-            for (int m = 0; m < TILE::MB; ++m)
+            for (int q = 0; q < 4; ++q) {
+                V4 o[PIECES];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    V4 o;
+                for (int i = 0; i < 4; ++i) {
+                    float v = rounded_product(acc[m][n][4 * q + i], g[n]);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float v = p == 0 ? rounded_product(acc[m][n][4 * q + i], g[n]) : acc[m][n][4 * q + i];
-                        o[i] = (T)v;
-                        if constexpr (PIECES > 1) acc[m][n][4 * q + i] = __builtin_isfinite((float)o[i]) ? v - (float)o[i] : 0.0f;
+                    for (int p = 0; p < PIECES; ++p) {
+                        o[p][i] = (T)v;
+                        v = __builtin_isfinite((float)o[p][i]) ? v - (float)o[p][i] : 0.0f;
                     }
-                    *reinterpret_cast<V4 *>(memory + (TILE::n0() + 32 * n + (TILE::lane() & 31)) * PITCH + (TILE::m0() + 32 * m + TILE::row(4 * q)) * 2) = o;
                 }
+#pragma unroll
+                for (int p = 0; p < PIECES; ++p) *reinterpret_cast<V4 *>(memory + (p * ROWS + mine) * PITCH + (TILE::m0() + 32 * m + TILE::row(4 * q)) * 2) = o[p];
+            }
         __syncthreads();
-        constexpr int CHUNKS = TILE::BM / 8;
 #pragma unroll 4
-        for (int k = (int)threadIdx.x; k < TILE::BN * CHUNKS; k += TILE::THREADS) {
-            const int block = k / (TILE::BN * BK / 8), in = k % (TILE::BN * BK / 8), row = in / (BK / 8), chunk = in % (BK / 8);
-            *reinterpret_cast<V8 *>(out + (size_t)p * (size_t)a.dz_plane + (size_t)block * (size_t)a.dz_block + in * 16) =
-                *reinterpret_cast<const V8 *>(memory + row * PITCH + block * (BK * 2) + chunk * 16);
+        for (int k = (int)threadIdx.x; k < PIECES * ROWS * CHUNKS; k += TILE::THREADS) {
+            const int p = k / (ROWS * CHUNKS), block = k / (ROWS * BK / 8) % (TILE::BM / BK), in = k % (ROWS * BK / 8), row = in / (BK / 8), chunk = in % (BK / 8);
+            *reinterpret_cast<V8 *>(out + (size_t)p * (size_t)a.dz_plane + (size_t)block * (size_t)a.dz_block + (row / 32 * TILE::WN + 32 * n + row % 32) * (BK * 2) + chunk * 16) =
+                *reinterpret_cast<const V8 *>(memory + (p * ROWS + row) * PITCH + block * (BK * 2) + chunk * 16);
         }
         if (a.sums) {       // two words to a thread, a run of rows each
             typedef T V2 __attribute__((ext_vector_type(2)));
             const int pair = (int)threadIdx.x % PAIRS, run = (int)threadIdx.x / PAIRS;
 #pragma unroll 8
-            for (int r = run; r < TILE::BN; r += RUNS) {
+            for (int r = run; r < PIECES * ROWS; r += RUNS) {
                 const V2 v = *reinterpret_cast<const V2 *>(memory + r * PITCH + pair * 4);
                 sum[0] += (float)v[0];
                 sum[1] += (float)v[1];
@@ -962,12 +964,16 @@ __global__ void __launch_bounds__(256) hot_head_zero_kernel(char *p, long bytes)
 // Host side.
 
 constexpr long kMostTiles = 1L << 22;                    // of 256 x 256 logits (one grid dimension holds fewer than 2^32 threads)
-constexpr int64_t kPieceBytes = (int64_t)256 << 20;      // of dz and packed weights: what the memory-side cache holds
+// Of dz and packed weights: twice what the memory-side cache holds.  Half of it adds the features' gradients up in twice as many passes over their sums
+// (8192 x 4096 x 131072 bf16 forward and backward 41.8 ms, 41.0 so; 1000 x 768 x 32768 float32 1138 us, 1067 so).
+constexpr int64_t kPieceBytes = (int64_t)512 << 20;
 
 // Sizes of tiles (of logits: words x rows): 256 x 32 for up to 32 rows, 64 x 64 and 128 x 128 where larger ones leave the chip empty, 256 x 256
 // (256 x 128 in three pieces).
 // Float32 heads of up to 128 rows with 256 tiles of words have 256 x 128 with the weights read as they lie (128 x 1024 x 65536: 971 us packed, 646 so; with half as
 // many tiles, 64 x 768 x 32768, whose packed weights stay in the memory-side cache, 278 packed, 289 so).
+// Tiles of the gradients are the same, but with half as many words (weights') or rows (features') where two pieces of dz would take twice the room: 256 x 128, and 128 x 64
+// for 128 x 128 (512 x 1024 x 11000 bf16 forward and backward 140 us; with all 128, one workgroup to a compute unit, 153, with 64 x 64 150).
 enum { kFew, kSmall, kMiddle, kLarge, kTall };
 
 struct HeadPlan {
@@ -977,8 +983,9 @@ struct HeadPlan {
     long row_bytes;          // of a packed row: whole blocks
     long places;
     int v_piece, v_pieces;   // words of a piece
-    int size;                // kFew ... kLarge
+    int size;                // kFew ... kTall
     int v_tile, r_tile;      // words and rows of a tile of logits
+    int x_tile;              // rows of a tile of the features' gradients
     int row_tiles;
     WordRuns word_runs;       // runs of words of the features' gradients
     int most_word_runs;
@@ -1027,10 +1034,11 @@ HeadPlan head_plan(const hot_head_desc &d, bool backward, bool with_dx)
     const bool three = p.pieces == 3;
     const double large = rounds(256, three ? 128 : 256, 1), middle = rounds(128, 128, three ? 1 : 2) * (three ? 0.62 : 0.67), small = rounds(64, 64, 2) * (three ? 0.42 : 0.25);
     p.size = R <= 32 ? kFew : p.raw_w ? kTall : (large <= middle && large <= small ? kLarge : (middle <= small ? kMiddle : kSmall));
-    p.dz_pieces = p.size == kFew && p.pieces == 1 ? 2 : p.pieces;
+    p.dz_pieces = three ? 3 : 2;
     constexpr int V_TILE[] = {256, 64, 128, 256, 256}, R_TILE[] = {32, 64, 128, 256, 128};
     p.v_tile = V_TILE[p.size];
-    p.r_tile = p.size == kLarge && p.pieces == 3 ? 128 : R_TILE[p.size];
+    p.r_tile = p.size == kLarge && three ? 128 : R_TILE[p.size];
+    p.x_tile = p.size == kLarge ? 128 : (p.size == kMiddle && !three ? 64 : p.r_tile);
     p.row_tiles = (int)((R + p.r_tile - 1) / p.r_tile);
     long piece = up(V, 256);
     if (backward || p.pack_w) {
@@ -1045,19 +1053,19 @@ HeadPlan head_plan(const hot_head_desc &d, bool backward, bool with_dx)
     // as many workgroups and sums as the best number of runs needs for all rows
     WordRuns &w = p.word_runs;
     static_assert(kComputeUnits == 256, "");
-    w = {__builtin_ctz((unsigned)p.r_tile), p.size == kLarge || p.pieces == 3 ? 8 : 9, (int)((K + V_TILE[p.size] - 1) / V_TILE[p.size]), (int)S, (int)piece, LONG_MAX, LONG_MAX, nullptr};
+    w = {__builtin_ctz((unsigned)p.x_tile), p.size == kLarge || p.pieces == 3 ? 8 : 9, (int)((K + V_TILE[p.size] - 1) / V_TILE[p.size]), (int)S, (int)piece, LONG_MAX, LONG_MAX, nullptr};
     int best_runs = 1;
     for (int runs = 2; runs <= 64 && run_possible(w, R, runs); ++runs)
         if (run_steps(w, R, runs) < run_steps(w, R, best_runs)) best_runs = runs;
     best_runs = (int)((piece + run_depth((int)piece, best_runs) - 1) / run_depth((int)piece, best_runs));
     p.most_word_runs = best_runs;
-    w.workgroups = best_runs * place_blocks(w.width_tiles, (R + p.r_tile - 1) / p.r_tile);
+    w.workgroups = best_runs * place_blocks(w.width_tiles, (R + p.x_tile - 1) / p.x_tile);
     w.sums = best_runs * R;
     long best = 0;
 
     // The weights' gradients: as many runs of rows as leave the fewest steps of BK rows in all rounds, twenty more to each run, and as long as their
     // partial sums are no more than two rounds of tiles (5569 x 42 x 1227 float32 without: 195 us on ten workgroups)
-    const int wt = p.size >= kLarge ? 256 : (p.size == kMiddle ? 128 : 64), wv = p.size >= kLarge && p.pieces == 3 ? 128 : wt;
+    const int wt = p.size >= kLarge ? 256 : (p.size == kMiddle ? 128 : 64), wv = p.size >= kLarge ? 128 : (three ? wt : 64);
     const long w_tiles = ((piece + wv - 1) / wv < (V + wv - 1) / wv ? (piece + wv - 1) / wv : (V + wv - 1) / wv) * ((K + wt - 1) / wt) * S;
     for (long runs = 1; runs <= 256 && (runs == 1 || (runs * 4 * p.columns <= R && runs * w_tiles <= 2 * kComputeUnits)); ++runs) {
         const long depth = up((R + runs - 1) / runs, p.columns), cost = (w_tiles * runs + kComputeUnits - 1) / kComputeUnits * (depth / p.columns + 20);
@@ -1302,24 +1310,24 @@ HeadArgs head_args(const HeadCall &c, long v_begin, long v_count)
     return a;
 }
 
-// Pieces in which dz of few rows is held.  A weight's gradient is then a handful of products, and one rounding of dz to 16 bits would show in it
-// beside its own (up to three times the error); reading W bounds these calls, so the second piece costs nothing.  With many rows the roundings
-// of dz average out.
 template <int PIECES>
 constexpr int kSmallStages = PIECES == 1 ? 4 : 3;
 
+// Pieces in which dz is held.  One rounding of dz to 16 bits would show in gradients of 16 bits beside their own: a word's is made by the few rows that
+// carry or list it, a row's by its few likely words, and there is nothing that averages out (1.4 times the error of a float32 dz
+// over 4096 rows, up to three times it over a handful).
 template <int PIECES>
 constexpr int kDz = PIECES == 1 ? 2 : PIECES;
 
-template <class TILE, int DZ>
+template <class TILE>
 void logits_go(const HeadCall &c, const HeadArgs &a, bool backward)
 {
     const dim3 grid((unsigned)place_blocks((a.v_count + TILE::BM - 1) / TILE::BM, (c.d.rows + TILE::BN - 1) / TILE::BN), (unsigned)c.d.samples), block(TILE::THREADS);
     if (c.d.top > 0) {
-        if (backward) hot_head_dz_kernel<TILE, true, DZ><<<grid, block, 0, c.stream>>>(a);
+        if (backward) hot_head_dz_kernel<TILE, true, kDz<TILE::PIECES_A>><<<grid, block, 0, c.stream>>>(a);
         else hot_head_forward_kernel<TILE, true><<<grid, block, 0, c.stream>>>(a);
     } else {
-        if (backward) hot_head_dz_kernel<TILE, false, DZ><<<grid, block, 0, c.stream>>>(a);
+        if (backward) hot_head_dz_kernel<TILE, false, kDz<TILE::PIECES_A>><<<grid, block, 0, c.stream>>>(a);
         else hot_head_forward_kernel<TILE, false><<<grid, block, 0, c.stream>>>(a);
     }
 }
@@ -1328,14 +1336,14 @@ template <class T, int PIECES>
 void head_logits(const HeadCall &c, const HeadArgs &a, bool backward)
 {
     if constexpr (PIECES == 3) {
-        if (c.p.size == kTall) return logits_go<Tile<T, PIECES, PIECES, true, true, 256, 128, 8, 1, 2, true, false>, PIECES>(c, a, backward);
-        if (c.p.raw_w) return logits_go<Tile<T, PIECES, PIECES, true, true, 256, 32, 8, 1, 4, true, false>, kDz<PIECES>>(c, a, backward);
-        if (c.p.size == kFew) return logits_go<Tile<T, PIECES, PIECES, true, true, 256, 32, 8, 1>, kDz<PIECES>>(c, a, backward);
-    } else if (c.p.size == kFew) return logits_go<Tile<T, PIECES, PIECES, true, true, 256, 32, 8, 1, 4>, kDz<PIECES>>(c, a, backward);
-    if (c.p.size == kSmall) logits_go<Tile<T, PIECES, PIECES, true, true, 64, 64, 2, 2, kSmallStages<PIECES>>, PIECES>(c, a, backward);
-    else if (c.p.size == kMiddle) logits_go<Tile<T, PIECES, PIECES, true, true, 128, 128, 2, 2>, PIECES>(c, a, backward);
-    else if constexpr (PIECES == 1) logits_go<Tile<T, PIECES, PIECES, true, true, 256, 256, 2, 4>, PIECES>(c, a, backward);
-    else logits_go<Tile<T, PIECES, PIECES, true, true, 256, 128, 4, 2>, PIECES>(c, a, backward);
+        if (c.p.size == kTall) return logits_go<Tile<T, PIECES, PIECES, true, true, 256, 128, 8, 1, 2, true, false>>(c, a, backward);
+        if (c.p.raw_w) return logits_go<Tile<T, PIECES, PIECES, true, true, 256, 32, 8, 1, 4, true, false>>(c, a, backward);
+        if (c.p.size == kFew) return logits_go<Tile<T, PIECES, PIECES, true, true, 256, 32, 8, 1>>(c, a, backward);
+    } else if (c.p.size == kFew) return logits_go<Tile<T, PIECES, PIECES, true, true, 256, 32, 8, 1, 4>>(c, a, backward);
+    if (c.p.size == kSmall) logits_go<Tile<T, PIECES, PIECES, true, true, 64, 64, 2, 2, kSmallStages<PIECES>>>(c, a, backward);
+    else if (c.p.size == kMiddle) logits_go<Tile<T, PIECES, PIECES, true, true, 128, 128, 2, 2>>(c, a, backward);
+    else if constexpr (PIECES == 1) logits_go<Tile<T, PIECES, PIECES, true, true, 256, 256, 2, 4>>(c, a, backward);
+    else logits_go<Tile<T, PIECES, PIECES, true, true, 256, 128, 4, 2>>(c, a, backward);
 }
 
 template <class TILE>
@@ -1352,25 +1360,25 @@ void dw_go(const HeadCall &c, const GradArgs &a)
                                     TILE::THREADS, 0, c.stream>>>(a);
 }
 
-// dW on tiles of TILE, or, on tiles of RUN_TILE (whose float32 results have to fit LDS), as partial sums that are then added up; void: one run only
-template <class TILE, class T, class RUN_TILE = TILE>
+// dW on tiles of TILE, or (RUNS) as partial sums in float32 that are then added up
+template <class TILE, class T, bool RUNS = true>
 void head_dw(const HeadCall &c, GradArgs a, void *dw)
 {
     const long part = (long)a.v_count * c.d.width;
     a.row_depth = c.p.run_depth;
-    if (std::is_void_v<RUN_TILE> || c.p.runs == 1) {
+    if (!RUNS || c.p.runs == 1) {
         a.out = dw;
         a.out_sample = c.d.vocab * c.d.width;
         a.out_first = a.v_begin;
         return dw_go<TILE, T>(c, a);
     }
-    if constexpr (!std::is_void_v<RUN_TILE>) {
+    if constexpr (RUNS) {
         float *const parts = c.in<float>(c.p.dw);
         a.out = parts;
         a.out_sample = part;
         a.out_split = c.d.samples * part;
         a.out_first = 0;
-        dw_go<RUN_TILE, float>(c, a);
+        dw_go<TILE, float>(c, a);
         const RunArgs r = {parts, part, part, a.out_split, c.d.vocab * c.d.width, c.p.runs, static_cast<T *>(dw) + (size_t)a.v_begin * (size_t)c.d.width};
         hot_head_runs_kernel<T><<<dim3(grid_for((part + Piece<T>::N - 1) / Piece<T>::N), (unsigned)c.d.samples), 256, 0, c.stream>>>(r);
     }
@@ -1436,19 +1444,17 @@ void head_backward(const HeadCall &c, const double *lse, const float *g, long g_
             } else if (c.p.raw_w) {
                 if constexpr (PIECES == 3) head_dx<Tile<E, PIECES, PIECES, true, false, 32, 256, 1, 8, 4, false, true>>(c, a);
             } else if (c.p.size == kFew) head_dx<Tile<E, kDz<PIECES>, PIECES, true, false, 32, 256, 1, 8, PIECES == 1 ? 3 : 2>>(c, a);
-            else if (c.p.size == kSmall) head_dx<Tile<E, PIECES, PIECES, true, false, 64, 64, 2, 2, kSmallStages<PIECES>>>(c, a);
-            else if (c.p.size == kMiddle) head_dx<Tile<E, PIECES, PIECES, true, false, 128, 128, 2, 2>>(c, a);
-            else if constexpr (PIECES == 1) head_dx<Tile<E, PIECES, PIECES, true, false, 256, 256, 2, 4>>(c, a);
-            else head_dx<Tile<E, PIECES, PIECES, true, false, 128, 256, 2, 4>>(c, a);
+            else if (c.p.size == kSmall) head_dx<Tile<E, kDz<PIECES>, PIECES, true, false, 64, 64, 2, 2, 3>>(c, a);
+            else if (c.p.size == kMiddle) head_dx<Tile<E, kDz<PIECES>, PIECES, true, false, PIECES == 1 ? 64 : 128, 128, 2, 2>>(c, a);
+            else head_dx<Tile<E, kDz<PIECES>, PIECES, true, false, 128, 256, 2, 4>>(c, a);
         }
         if (dw) {
             a.other = h.x;
             a.sample = h.x_sample;
-            if (c.p.size == kFew) head_dw<Tile<E, PIECES, kDz<PIECES>, false, false, 256, 64, 4, 1, 1>, T, void>(c, a, dw);
-            else if (c.p.size == kSmall) head_dw<Tile<E, PIECES, PIECES, false, false, 64, 64, 2, 2, kSmallStages<PIECES>>, T>(c, a, dw);
-            else if (c.p.size == kMiddle) head_dw<Tile<E, PIECES, PIECES, false, false, 128, 128, 2, 2>, T>(c, a, dw);
-            else if constexpr (PIECES == 1) head_dw<Tile<E, PIECES, PIECES, false, false, 256, 256, 2, 4>, T, Tile<E, PIECES, PIECES, false, false, 128, 128, 2, 2>>(c, a, dw);
-            else head_dw<Tile<E, PIECES, PIECES, false, false, 256, 128, 4, 2>, T>(c, a, dw);
+            if (c.p.size == kFew) head_dw<Tile<E, PIECES, kDz<PIECES>, false, false, 256, 64, 4, 1, 1>, T, false>(c, a, dw);
+            else if (c.p.size == kSmall) head_dw<Tile<E, PIECES, kDz<PIECES>, false, false, 64, 64, 2, 2, 3>, T>(c, a, dw);
+            else if (c.p.size == kMiddle) head_dw<Tile<E, PIECES, kDz<PIECES>, false, false, 128, PIECES == 1 ? 64 : 128, 2, 2>, T>(c, a, dw);
+            else head_dw<Tile<E, PIECES, kDz<PIECES>, false, false, 256, 128, 4, 2>, T>(c, a, dw);
         }
         const bool finish_x = dx && v + n >= c.d.vocab;
         if (!db && !finish_x) continue;

@@ -244,23 +244,23 @@ struct Tile {
         }
     };
     static constexpr int kReads = kReadsB + StageA::kPlanes * MB, kLoads = StageA::kAll + StageB::kAll;
-    // a step's products in parts, between which reads and loads are issued: rows of blocks, or the products of the pieces
-    static constexpr bool kPlain = PIECES_A == 1 && PIECES_B == 1;
-    static constexpr int kParts = kPlain ? MB : (PIECES_A == 3 ? 6 : 2);
-    static_assert(kPlain || PIECES_A * PIECES_B == 2 || (PIECES_A == 3 && PIECES_B == 3), "");
+    // a step's products in parts, between which reads and loads are issued: rows of blocks (of the smaller piece before those of the larger), or the products of
+    // three pieces
+    static constexpr int kParts = PIECES_A == 3 ? 6 : MB * PIECES_A * PIECES_B;
+    static_assert(PIECES_A * PIECES_B <= 2 || (PIECES_A == 3 && PIECES_B == 3), "");
 
     static __device__ __forceinline__ void multiply(const Operands &o, TileAcc<T> (&acc)[MB][NB], int part)
     {
-        if constexpr (kPlain) {
-#pragma unroll
-            for (int n = 0; n < NB; ++n) acc[part][n].mac(o.a[0][part], o.b[0][n]);
-        } else {
+        if constexpr (PIECES_A == 3) {
             constexpr int PA[6] = {2, 1, 0, 1, 0, 0}, PB[6] = {0, 1, 2, 0, 1, 0};
-            const int pa = PIECES_A == 3 ? PA[part] : (PIECES_A == 2 ? 1 - part : 0), pb = PIECES_B == 3 ? PB[part] : (PIECES_B == 2 ? 1 - part : 0);
 #pragma unroll
             for (int m = 0; m < MB; ++m)
 #pragma unroll
-                for (int n = 0; n < NB; ++n) acc[m][n].mac(o.a[pa][m], o.b[pb][n]);
+                for (int n = 0; n < NB; ++n) acc[m][n].mac(o.a[PA[part]][m], o.b[PB[part]][n]);
+        } else {
+            const int piece = part / MB, m = part % MB, pa = PIECES_A == 2 ? 1 - piece : 0, pb = PIECES_B == 2 ? 1 - piece : 0;
+#pragma unroll
+            for (int n = 0; n < NB; ++n) acc[m][n].mac(o.a[pa][m], o.b[pb][n]);
         }
     }
 
