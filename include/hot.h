@@ -539,7 +539,8 @@ int hot_stats_whole(const float *yhat, int64_t m, int64_t ld, int32_t s, int32_t
  * draws ([S_loc, N]) holds the weights of both, one set per sample, as views; networks whose weights are no samples use the same
  * calls with one set.  Tensors are float32, bfloat16 or float16; sums, statistics and losses are held in 32 bits or more, and a result is
  * rounded to its type once.  The gradients of logits, which are operands of matrix products, are held in pieces of 16 bits: three for
- * float32, two for bfloat16 (2^-16 of each) and float16 (2^-22, or steps of 2^-39 of a sample's largest grad_loss).  Pointers need the alignment of their elements.  Runs on the current device; DEVICE pointers;
+ * float32, two for bfloat16 (2^-16 of each) and float16 (2^-22, or steps of 2^-39 of a sample's largest grad_loss); what is below
+ * 2^-126 of the largest is zero.  Pointers need the alignment of their elements.  Runs on the current device; DEVICE pointers;
  * workspaces are the caller's scratch (16-byte aligned, contents free before and after).
  */
 #define HOT_F32 0
@@ -614,7 +615,11 @@ typedef struct hot_head_desc {
 /* Scratch of a call: which = 0 forward, 1 backward with dx, 2 backward without. */
 int64_t hot_head_workspace_bytes(const hot_head_desc *desc, int which);
 
-/* loss: fp32 [samples, rows].  lse: fp64 [samples, rows], ln sum_v exp(z / T) (0 for rows that do not count), for the backward call; may be NULL. */
+/*
+ * loss: fp32 [samples, rows].  lse: fp64 [samples, rows], ln sum_v exp(z / T) (0 for rows that do not count), for the backward call; may be NULL.
+ * Where |max z| / T is 2^27 or more (all words masked with the type's lowest value, say) that logarithm would not show beside it; lse then is max z
+ * times 2^200, with 2^24 ln sum_v exp((z - max z) / T) in the 29 lowest bits.
+ */
 int hot_head_forward(const hot_head_desc *desc, const void *x, const void *weight, const void *bias, const int64_t *index,
                      const void *logit, float *loss, double *lse, void *workspace, int64_t workspace_bytes, void *stream);
 

@@ -5,8 +5,9 @@
 //   dz = g T (q - sum_j p_j delta_(i_j)),  dx = dz W,  dW = dz^T x,  db = sum_r dz
 // A label is one entry of weight one at T = 1 (the cross entropy); a teacher's top logits t give p = softmax(t / T) over the words listed.
 //
-// The forward pass multiplies tiles of vocabulary by tiles of rows; a tile leaves per row its largest logit, its sum of exponentials and its
-// share of sum_j p_j z, which a second kernel joins.  The backward pass walks the vocabulary in pieces: it forms a piece's logits again,
+// The forward pass multiplies tiles of vocabulary by tiles of rows; a tile leaves per row its largest logit m, its sum of exponentials of (z - m) / T, its
+// share of sum_j p_j (z - m) and of sum_j p_j, which a second kernel joins.  Logits are subtracted before anything multiplies them, so that words masked with the
+// type's lowest value, or all logits together, may lie anywhere.  The backward pass walks the vocabulary in pieces: it forms a piece's logits again,
 // leaves dz of that piece in scratch memory (two 16-bit pieces, or three bf16 pieces of float32) and multiplies it with W and with x.  Its
 // products are 2 R V K operations each, one forward and five backward (the two with dz twice over); what bounds them is the matrix pipes from
 // some hundred rows on, below that reading W.
@@ -196,8 +197,38 @@ __device__ __forceinline__ void choose_runs(const WordRuns &a, long s, int rows)
     if (runs == 1) a.depth[s] = run_depth(a.piece, (int)(best & 63) + 1);
 }
 
+// A row's largest logit, as what others are taken from: zero where nothing but -inf is there
+__device__ __forceinline__ float level(float most) { return most == -__builtin_inff() ? 0.0f : most; }
+
+// lse = largest / T + ln_sum in 64 bits holds ln_sum to 2^-26 as long as largest / T is below 2^27.  Beyond (every word masked with the lowest value, say) the two
+// lie side by side: the float's value times 2^200, and in the 29 bits that a float leaves free in a double 2^24 ln_sum (at most ln 2^24).
+constexpr unsigned long long kFreeBits = (1ull << 29) - 1;
+
+__device__ __forceinline__ double put_lse(float largest, double ln_sum, double temperature)
+{
+    const double at = (double)largest / temperature;
+    if (!(__builtin_fabs(at) >= 0x1p27) || __builtin_isinf(largest) || !(ln_sum >= 0.0)) return at + ln_sum;
+    return __builtin_bit_cast(double, __builtin_bit_cast(unsigned long long, (double)largest * 0x1p200) | (unsigned long long)(ln_sum * 0x1p24 + 0.5));
+}
+
+// (z - base) log2(e) / T - rest is the logarithm to base 2 of a word's probability
+__device__ __forceinline__ void get_lse(double lse, double temperature, float &base, float &rest)
+{
+    constexpr double LOG2E = 1.44269504088896340736;
+    if (__builtin_fabs(lse) >= 0x1p160 && __builtin_isfinite(lse)) {
+        const unsigned long long bits = __builtin_bit_cast(unsigned long long, lse);
+        base = (float)(__builtin_bit_cast(double, bits & ~kFreeBits) * 0x1p-200);
+        rest = (float)((double)(bits & kFreeBits) * 0x1p-24 * LOG2E);
+        return;
+    }
+    const double at = lse * temperature;
+    base = (float)at;
+    rest = __builtin_isfinite(base) ? (float)((at - (double)base) * LOG2E / temperature) : 0.0f;
+}
+
 struct RowArgs {
     long rows, vocab;
+    double temperature;
     long idx_sample, idx_row;
     int64_t ignore;
     const int64_t *index;          // labels, or
@@ -210,7 +241,7 @@ struct RowArgs {
     int *count;                    // [samples]
     int *row_of, *place_of;        // [samples, rows]: the row at a place, the place of a row (-1: left out)
     int *label;                    // [samples, rows] by place (-1: no word)
-    float *hi, *lo, *grad;         // by place: lse in base 2 as two floats, the row's gradient
+    float *base, *rest, *grad;     // by place: lse as get_lse gives it, the row's gradient
     float *scale;                  // [samples, 2]: what gradients are multiplied with, and what results are multiplied with in turn
     WordRuns runs;
 };
@@ -255,10 +286,7 @@ __device__ __forceinline__ int find_rows(const RowArgs &a, long s, unsigned shor
                     a.row_of[base + at] = (int)row;
                     if (a.label) a.label[base + at] = label;
                     if (a.lse) {
-                        const double two = a.lse[base + row] * (1.0 / 0.69314718055994530942);
-                        const float hi = (float)two;
-                        a.hi[base + at] = hi;
-                        a.lo[base + at] = __builtin_isfinite(hi) ? (float)(two - (double)hi) : 0.0f;
+                        get_lse(a.lse[base + row], a.temperature, a.base[base + at], a.rest[base + at]);
                         float g = a.g[s * a.g_sample + row * a.g_row];
                         if (!a.list_count && label < 0) g = __builtin_nanf("");
                         a.grad[base + at] = g;
@@ -384,11 +412,11 @@ struct HeadArgs {
     const unsigned short *start;
     int top, marks;
     long list_sample;
-    // forward: partials[sample][tile][3][place]
+    // forward: partials[sample][tile][4][place]
     float *partials;
     int v_tiles;
     // backward
-    const float *hi, *lo, *grad, *to_scale;
+    const float *base, *rest, *grad, *to_scale;
     char *dz;                      // [sample] blocks of BK words, each all places
     long dz_block, dz_plane, dz_sample;
     float *sums;                   // for db, or null: dz summed over a tile's rows, [sample][tile of rows][word of the piece]
@@ -404,6 +432,7 @@ struct Rows {
     float weight[TILE::NB];
     long entry[TILE::NB];          // of the list
     int left[TILE::NB];
+    float covered[TILE::NB];       // weight of the targets that targets() met in this wave's words
 
     __device__ __forceinline__ Rows(const HeadArgs &a, long s, int count, int v0, int r0)
     {
@@ -415,6 +444,7 @@ struct Rows {
             weight[n] = 0.0f;
             entry[n] = 0;
             left[n] = 0;
+            covered[n] = 0.0f;
             if (!live[n]) continue;
             if constexpr (!LISTS) word[n] = a.label[s * a.rows + place[n]];
             else {
@@ -440,6 +470,7 @@ struct Rows {
 #pragma unroll
         for (int n = 0; n < TILE::NB; ++n) {
             auto meet = [&](int in, float w) {
+                covered[n] += in >= 0 && in < TILE::WM ? w : 0.0f;
 #pragma unroll
                 for (int m = 0; m < TILE::MB; ++m) {
                     if (__builtin_amdgcn_ballot_w64(in >= 32 * m && in < 32 * m + 32) == 0) continue;
@@ -520,7 +551,7 @@ template <class TILE, bool LISTS>
 __global__ void __launch_bounds__(TILE::THREADS)
 hot_head_forward_kernel(HeadArgs a)
 {
-    constexpr int NEED = 3 * TILE::WAVES_M * TILE::BN * 4;
+    constexpr int NEED = 4 * TILE::WAVES_M * TILE::BN * 4;
     // (one array: beside a second one the compiler would wait for every load in flight before it reads either)
     constexpr int ROOM = TILE::kLds > NEED ? TILE::kLds : NEED;
     __shared__ __attribute__((aligned(1024))) char memory[ROOM + TILE::BM * 4];
@@ -532,49 +563,60 @@ hot_head_forward_kernel(HeadArgs a)
     f16v acc[TILE::MB][TILE::NB];
     logits<TILE>(a, memory, reinterpret_cast<float *>(memory + ROOM), s, count, tile, acc);
     const int r0 = tile.r0, v0 = tile.v0;
-    float dot[TILE::NB] = {};
+    float most[TILE::NB], dot[TILE::NB] = {};
+#pragma unroll
+    for (int n = 0; n < TILE::NB; ++n) {
+        most[n] = acc[0][n][0];
+#pragma unroll
+        for (int m = 0; m < TILE::MB; ++m)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) most[n] = fmaxf(most[n], acc[m][n][i]);
+        most[n] = fmaxf(most[n], __shfl_xor(most[n], 32));
+        const float from = level(most[n]);        // (nothing but -inf: a sum of zero)
+#pragma unroll
+        for (int m = 0; m < TILE::MB; ++m)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[m][n][i] -= from;
+    }
     rows.targets(a, v0, [&](int n, int m, int i, bool mine, float weight) { dot[n] += mine ? weight * acc[m][n][i] : 0.0f; });
     float (*const part)[TILE::WAVES_M][TILE::BN] = reinterpret_cast<float (*)[TILE::WAVES_M][TILE::BN]>(memory);
 #pragma unroll
     for (int n = 0; n < TILE::NB; ++n) {
-        float most = acc[0][n][0];
-#pragma unroll
-        for (int m = 0; m < TILE::MB; ++m)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) most = fmaxf(most, acc[m][n][i]);
-        most = fmaxf(most, __shfl_xor(most, 32)) * a.scale;
-        const float from = most == -__builtin_inff() ? 0.0f : most;        // (nothing but -inf: a sum of zero)
         float sum = 0.0f;
 #pragma unroll
         for (int m = 0; m < TILE::MB; ++m)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[m][n][i], a.scale, -from));
+            for (int i = 0; i < 16; ++i) sum += __builtin_amdgcn_exp2f(acc[m][n][i] * a.scale);
         sum += __shfl_xor(sum, 32);
-        dot[n] = (dot[n] + __shfl_xor(dot[n], 32)) * a.scale;
+        dot[n] += __shfl_xor(dot[n], 32);
         if (TILE::lane() < 32) {
             const int wm = TILE::wave() / TILE::WAVES_N, col = TILE::n0() + 32 * n + TILE::lane();
-            part[0][wm][col] = most;
+            part[0][wm][col] = most[n];
             part[1][wm][col] = sum;
             part[2][wm][col] = dot[n];
+            part[3][wm][col] = rows.covered[n];
         }
     }
     __syncthreads();
     for (int col = (int)threadIdx.x; col < TILE::BN; col += TILE::THREADS) {
         if (r0 + col >= count) break;
-        float most = part[0][0][col];
+        float top = part[0][0][col];
 #pragma unroll
-        for (int k = 1; k < TILE::WAVES_M; ++k) most = fmaxf(most, part[0][k][col]);
-        float sum = 0.0f, d = 0.0f;
+        for (int k = 1; k < TILE::WAVES_M; ++k) top = fmaxf(top, part[0][k][col]);
+        float sum = 0.0f, d = 0.0f, covered = 0.0f;
 #pragma unroll
         for (int k = 0; k < TILE::WAVES_M; ++k) {
+            const float m = part[0][k][col], w = part[3][k][col];
             // (a largest logit of -inf: a sum of zero, or none where a logit is no number)
-            sum += part[0][k][col] == -__builtin_inff() ? part[1][k][col] : part[1][k][col] * __builtin_amdgcn_exp2f(part[0][k][col] - most);
-            d += part[2][k][col];
+            sum += m == -__builtin_inff() ? part[1][k][col] : part[1][k][col] * __builtin_amdgcn_exp2f((m - top) * a.scale);
+            d += part[2][k][col] + (w > 0.0f ? w * (level(m) - level(top)) : 0.0f);
+            covered += w;
         }
-        float *const out = a.partials + (((size_t)s * (size_t)a.v_tiles + (size_t)(v0 / TILE::BM)) * 3) * (size_t)a.places + (size_t)(r0 + col);
-        out[0] = most;
+        float *const out = a.partials + (((size_t)s * (size_t)a.v_tiles + (size_t)(v0 / TILE::BM)) * 4) * (size_t)a.places + (size_t)(r0 + col);
+        out[0] = top;
         out[a.places] = sum;
         out[2 * a.places] = d;
+        out[3 * a.places] = covered;
     }
 }
 
@@ -601,13 +643,13 @@ hot_head_dz_kernel(HeadArgs a)
     const TileOf tile = tile_of<TILE>(a, count);
     if (!tile.any) return;
     Rows<TILE, LISTS> rows(a, s, count, tile.v0, tile.r0);
-    float hi[TILE::NB], lo[TILE::NB], g[TILE::NB];
+    float base[TILE::NB], rest[TILE::NB], g[TILE::NB];
     const float to_scale = a.to_scale[2 * s];
 #pragma unroll
     for (int n = 0; n < TILE::NB; ++n) {
         const long at = s * a.rows + rows.place[n];
-        hi[n] = rows.live[n] ? a.hi[at] : __builtin_inff();
-        lo[n] = rows.live[n] ? a.lo[at] : 0.0f;
+        base[n] = rows.live[n] ? a.base[at] : __builtin_inff();
+        rest[n] = rows.live[n] ? a.rest[at] : 0.0f;
         g[n] = rows.live[n] ? a.grad[at] * to_scale : 0.0f;
     }
     f16v acc[TILE::MB][TILE::NB];
@@ -618,11 +660,7 @@ hot_head_dz_kernel(HeadArgs a)
 #pragma unroll
         for (int n = 0; n < TILE::NB; ++n)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float z = __builtin_fmaf(acc[m][n][i], a.scale, -hi[n]);
-                // (the low part of lse is below the rounding of 16-bit results)
-                acc[m][n][i] = __builtin_amdgcn_exp2f(TILE::PIECES_A == 1 ? z : z - lo[n]);
-            }
+            for (int i = 0; i < 16; ++i) acc[m][n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[m][n][i] - base[n], a.scale, -rest[n]));
     rows.targets(a, v0, [&](int n, int m, int i, bool mine, float weight) { acc[m][n][i] -= mine ? weight : 0.0f; });
     // to rows of words through LDS, all pieces of a block of rows of every wave at once
     typedef typename TILE::T T;
@@ -690,6 +728,7 @@ hot_head_dz_kernel(HeadArgs a)
 struct JoinArgs {
     long rows, places;
     int tiles, lanes;              // lanes: threads to a row
+    float scale;                   // log2(e) / temperature
     const float *partials;
     const int *place_of, *label;
     const double *sums;            // of the lists, or null
@@ -699,56 +738,64 @@ struct JoinArgs {
     double *lse;
 };
 
+// What some of a row's words leave: largest logit, sum of exp2((z - most) scale), sum of p (z - most), sum of p
+template <class SUM>
+struct Share {
+    float most;
+    SUM sum;
+    double dot, covered;
+
+    template <class OTHER>
+    __device__ __forceinline__ void join(const Share<OTHER> &o, float scale)
+    {
+        const float top = o.most > most || o.most != o.most ? o.most : most;
+        const SUM there = (SUM)o.sum;
+        sum = top == -__builtin_inff() ? sum + there : sum * (SUM)__builtin_amdgcn_exp2f((most - top) * scale) + there * (SUM)__builtin_amdgcn_exp2f((o.most - top) * scale);
+        dot = moved(dot, covered, most, top) + moved(o.dot, o.covered, o.most, top);
+        covered += o.covered;
+        most = top;
+    }
+    static __device__ __forceinline__ double moved(double dot, double covered, float from, float to)
+    {
+        return covered > 0.0 ? dot + covered * ((double)level(from) - (double)level(to)) : dot;
+    }
+};
+
 __global__ void __launch_bounds__(256)
 hot_head_join_kernel(JoinArgs a)
 {
-    __shared__ float tops[256];
-    __shared__ double totals[256], dots[256];
+    __shared__ Share<double> shares[256];
     const int per = 256 / a.lanes, r = (int)threadIdx.x % per, lane = (int)threadIdx.x / per;
     const long s = blockIdx.y, row = (long)blockIdx.x * per + r;
     const int at = row < a.rows ? a.place_of[s * a.rows + row] : -1;
-    float most = -__builtin_inff(), sum = 0.0f, partial = 0.0f;
+    Share<float> mine = {-__builtin_inff(), 0.0f, 0.0, 0.0};
     if (at >= 0)
 #pragma unroll 4
         for (int k = lane; k < a.tiles; k += a.lanes) {
-            const float *const p = a.partials + ((size_t)s * (size_t)a.tiles + (size_t)k) * 3 * (size_t)a.places + (size_t)at;
-            const float m = p[0], v = p[a.places], top = m > most || m != m ? m : most;
-            sum = top == -__builtin_inff() ? sum + v : sum * __builtin_amdgcn_exp2f(most - top) + v * __builtin_amdgcn_exp2f(m - top);
-            most = top;
-            partial += p[2 * a.places];
+            const float *const p = a.partials + ((size_t)s * (size_t)a.tiles + (size_t)k) * 4 * (size_t)a.places + (size_t)at;
+            mine.join(Share<float>{p[0], p[a.places], (double)p[2 * a.places], (double)p[3 * a.places]}, a.scale);
         }
-    double total = (double)sum, d = (double)partial;
+    Share<double> all = {mine.most, (double)mine.sum, mine.dot, mine.covered};
     // the row's threads, in halves
     for (int half = a.lanes / 2; half > 0; half /= 2) {
-        if (lane >= half && lane < 2 * half) {
-            tops[threadIdx.x] = most;
-            totals[threadIdx.x] = total;
-            dots[threadIdx.x] = d;
-        }
+        if (lane >= half && lane < 2 * half) shares[threadIdx.x] = all;
         __syncthreads();
-        if (lane < half) {
-            const int other = (int)threadIdx.x + half * per;
-            const float m = tops[other], top = m > most || m != m ? m : most;
-            total = top == -__builtin_inff() ? total + totals[other]
-                                             : total * (double)__builtin_amdgcn_exp2f(most - top) + totals[other] * (double)__builtin_amdgcn_exp2f(m - top);
-            most = top;
-            d += dots[other];
-        }
+        if (lane < half) all.join(shares[(int)threadIdx.x + half * per], a.scale);
         __syncthreads();
     }
     if (lane || row >= a.rows) return;
     float loss = 0.0f;
     double lse = 0.0;
     if (at >= 0) {
-        const double two = (double)most + log2(total);
-        lse = two * 0.69314718055994530942;
+        const double ln_sum = log2(all.sum) * 0.69314718055994530942;
+        lse = put_lse(all.most, ln_sum, a.temperature);
         double entropy = 0.0, weight = 1.0;
         if (a.sums) {
             const long list = s * a.list_sample + row;
             entropy = a.sums[2 * list];
             weight = a.sums[2 * list + 1];
         } else if (a.label[s * a.rows + at] < 0) entropy = (double)__builtin_nanf("");
-        loss = (float)(a.temperature * a.temperature * (entropy + weight * lse - d * 0.69314718055994530942));
+        loss = (float)(a.temperature * a.temperature * (entropy + weight * ln_sum - all.dot / a.temperature));
     }
     a.loss[s * a.rows + row] = loss;
     if (a.lse) a.lse[s * a.rows + row] = lse;
@@ -991,7 +1038,7 @@ struct HeadPlan {
     int most_word_runs;
     int runs, run_depth;     // runs of rows of the weights' gradients, and their length
     // where things lie in the workspace
-    int64_t word, weight, list_count, sums, start, count, word_run, row_of, place_of, label, hi, lo, grad, scale, x, w, dz, partials, dx, db, dw, bytes;
+    int64_t word, weight, list_count, sums, start, count, word_run, row_of, place_of, label, base, rest, grad, scale, x, w, dz, partials, dx, db, dw, bytes;
 };
 
 struct Layout {
@@ -1089,8 +1136,8 @@ HeadPlan head_plan(const hot_head_desc &d, bool backward, bool with_dx)
     p.place_of = l.take(S * R * 4);
     p.label = l.take(d.top > 0 ? 0 : S * R * 4);
     if (backward) {
-        p.hi = l.take(S * R * 4);
-        p.lo = l.take(S * R * 4);
+        p.base = l.take(S * R * 4);
+        p.rest = l.take(S * R * 4);
         p.grad = l.take(S * R * 4);
         p.scale = l.take(S * 8);
     }
@@ -1102,7 +1149,7 @@ HeadPlan head_plan(const hot_head_desc &d, bool backward, bool with_dx)
         p.dw = l.take(p.runs > 1 ? (int64_t)p.runs * S * (piece < V ? piece : V) * K * 4 : 0);
         if (with_dx) p.dx = l.take(p.word_runs.sums * S * K * 4);
     } else {
-        p.partials = l.take(S * ((V + p.v_tile - 1) / p.v_tile) * 3 * p.places * 4);
+        p.partials = l.take(S * ((V + p.v_tile - 1) / p.v_tile) * 4 * p.places * 4);
     }
     p.bytes = l.at;
     return p;
@@ -1172,6 +1219,7 @@ RowArgs head_rows(const HeadCall &c, const double *lse, const float *g, long g_s
     RowArgs a = {};
     a.rows = d.rows;
     a.vocab = d.vocab;
+    a.temperature = d.temperature;
     a.idx_sample = d.index_sample;
     a.idx_row = d.index_row;
     a.ignore = d.ignore_index;
@@ -1187,8 +1235,8 @@ RowArgs head_rows(const HeadCall &c, const double *lse, const float *g, long g_s
     a.row_of = c.in<int>(p.row_of);
     a.place_of = c.in<int>(p.place_of);
     a.label = d.top > 0 ? nullptr : c.in<int>(p.label);
-    a.hi = c.in<float>(p.hi);
-    a.lo = c.in<float>(p.lo);
+    a.base = c.in<float>(p.base);
+    a.rest = c.in<float>(p.rest);
     a.grad = c.in<float>(p.grad);
     a.scale = c.in<float>(p.scale);
     if (lse) a.runs = head_runs(c);
@@ -1297,8 +1345,8 @@ HeadArgs head_args(const HeadCall &c, long v_begin, long v_count)
     a.list_sample = c.list_sample;
     a.partials = c.in<float>(p.partials);
     a.v_tiles = (int)((d.vocab + p.v_tile - 1) / p.v_tile);
-    a.hi = c.in<float>(p.hi);
-    a.lo = c.in<float>(p.lo);
+    a.base = c.in<float>(p.base);
+    a.rest = c.in<float>(p.rest);
     a.grad = c.in<float>(p.grad);
     a.to_scale = c.in<float>(p.scale);
     a.row_tiles = p.row_tiles;
@@ -1400,6 +1448,7 @@ void head_forward(const HeadCall &c, float *loss, double *lse)
     a.tiles = (int)((c.d.vocab + c.p.v_tile - 1) / c.p.v_tile);
     a.lanes = 4;
     while (a.lanes < 256 && (c.d.rows + 256 / a.lanes - 1) / (256 / a.lanes) * c.d.samples < kComputeUnits && a.lanes * 2 <= a.tiles) a.lanes *= 2;
+    a.scale = (float)(1.44269504088896340736 / c.d.temperature);
     a.partials = c.in<float>(c.p.partials);
     a.place_of = c.in<int>(c.p.place_of);
     a.label = c.in<int>(c.p.label);
