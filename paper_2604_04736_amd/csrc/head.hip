@@ -85,7 +85,7 @@ hot_head_lists_kernel(ListArgs a)
         for (int j = lane; j < (a.top + 3 & ~3); j += 64) {
             typedef float F1 __attribute__((ext_vector_type(1)));
             const int64_t i = j < a.top ? index[j] : -1;
-            const float v = i < 0 ? -__builtin_inff() : load_as<1, F1>(a.logit, a.logit_type, logit0 + j, logit0 + a.top)[0] * a.inv_temperature;
+            const float v = i < 0 ? -__builtin_inff() : load_as<1, F1>(a.logit, a.logit_type, logit0 + j, logit0 + a.top)[0];
             outside |= i >= a.vocab;
             nan |= v != v;
             most = fmaxf(most, v);
@@ -98,7 +98,7 @@ hot_head_lists_kernel(ListArgs a)
         const bool empty = !broken && most == -__builtin_inff();
         double total = 0.0, entropy = 0.0, sum = 0.0;
         for (int j = lane; j < a.top; j += 64) {
-            t[j] = expf(t[j] - most);
+            t[j] = expf((t[j] - most) * a.inv_temperature);         // (in this order: the lowest value of a type, over a small T, is no infinity)
             total += (double)t[j];
         }
         total = wave_total(total);

@@ -122,3 +122,25 @@ def test_logits_far_from_zero(offset, temperature, rows, vocab):
         target = targets[0][:, 0]
         p, p_log_p, _ = U.labels(target, vocab)
         _same_distance(x, w, b, up, target, p, p_log_p, 1.0, z - z.max())
+
+
+@pytest.mark.parametrize("offset", [0.0, -1e5, 2.0 ** 22, -2.0 ** 33, 1e30, "lowest"])
+@pytest.mark.parametrize("temperature", [0.5, 1.0, 3.0])
+@pytest.mark.parametrize("rows,vocab,top", [(9, 300, 3), (70, 3000, 90)])
+def test_a_teachers_logits_far_from_zero(offset, temperature, rows, vocab, top):
+    """Only a teacher's distances count; words that all have the lowest value are as likely as each other."""
+    x, w, b, up, g = _inputs("f32", rows, 24, vocab)
+    index = torch.randint(vocab, (rows, top), device=DEV, generator=g)
+    if offset == "lowest":
+        logit, distance = torch.full((rows, top), torch.finfo(torch.float32).min, device=DEV), torch.zeros(rows, top, device=DEV, dtype=torch.float64)
+    else:
+        step = max(math.ulp(abs(offset)) * 2 ** 29, 2.0 ** -6)
+        distance = torch.randint(0, 8, (rows, top), device=DEV, generator=g).double() * step
+        logit = (offset + distance).float()
+        assert torch.equal(logit.double() - logit.double().max(), distance - distance.max())
+    got = _pass(x, w, b, up, (index, logit), temperature)
+    distance -= distance.amax(1, keepdim=True)
+    want = U.head_plain(x[None], w[None], b[None], U.teacher(index[None], distance[None], temperature, vocab), up[None], temperature)
+    for n in got:
+        ref, bound = (t[0] for t in want[n])
+        U.within(got[n], ref, bound, n)
