@@ -34,7 +34,7 @@ inline __host__ __device__ long up(long n, long to) { return (n + to - 1) / to *
 // --------------------------------------------------------------------------- a teacher's entries
 
 struct ListArgs {
-    long lists, rows;                  // lists = rows x (samples or one)
+    long rows;                         // lists = rows x (samples or one)
     long idx_sample, idx_row, logit_sample, logit_row;
     int top, logit_type, marks;        // marks = vocabulary / kStartStep, rounded up
     long vocab;
@@ -73,11 +73,10 @@ hot_head_lists_kernel(ListArgs a)
     __shared__ __attribute__((aligned(16))) int words[kListWaves][MOST], sorted[kListWaves][MOST];
     __shared__ float scaled[kListWaves][MOST];
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
-    const long list = (long)blockIdx.x * kListWaves + wave;
+    const long s = blockIdx.y, row = (long)blockIdx.x * kListWaves + wave, list = s * a.rows + row;
     int *const w = words[wave], *const in_order = sorted[wave];
     float *const t = scaled[wave];
-    if (list < a.lists) {
-        const long s = list / a.rows, row = list % a.rows;
+    if (row < a.rows) {
         const int64_t *const index = a.index + s * a.idx_sample + row * a.idx_row;
         const long logit0 = s * a.logit_sample + row * a.logit_row;
         float most = -__builtin_inff();
@@ -1182,7 +1181,6 @@ void head_lists(const HeadCall &c)
     if (d.top == 0) return;
     ListArgs a;
     a.rows = d.rows;
-    a.lists = d.rows * (c.list_sample > 0 ? d.samples : 1);
     a.idx_sample = d.index_sample;
     a.idx_row = d.index_row;
     a.logit_sample = d.logit_sample;
@@ -1199,7 +1197,8 @@ void head_lists(const HeadCall &c)
     a.count = c.in<int>(p.list_count);
     a.sums = c.in<double>(p.sums);
     a.start = c.in<unsigned short>(p.start);
-    const dim3 grid((unsigned)((a.lists + kListWaves - 1) / kListWaves)), block(64 * kListWaves);
+    // (samples along y: a grid's dimension holds fewer than 2^32 threads)
+    const dim3 grid((unsigned)((a.rows + kListWaves - 1) / kListWaves), c.list_sample > 0 ? (unsigned)d.samples : 1u), block(64 * kListWaves);
     if (a.top <= 64) hot_head_lists_kernel<64><<<grid, block, 0, c.stream>>>(a);
     else if (a.top <= 256) hot_head_lists_kernel<256><<<grid, block, 0, c.stream>>>(a);
     else hot_head_lists_kernel<kMostTop><<<grid, block, 0, c.stream>>>(a);
