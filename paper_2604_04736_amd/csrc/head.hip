@@ -1009,7 +1009,7 @@ __global__ void __launch_bounds__(256) hot_head_zero_kernel(char *p, long bytes)
 // ---------------------------------------------------------------------------------
 // Host side.
 
-constexpr long kMostTiles = 1L << 22;                    // of 256 x 256 logits (one grid dimension holds fewer than 2^32 threads)
+constexpr long kMostTiles = 1L << 22;                    // of up to 512 threads in a launch (one grid dimension holds fewer than 2^32), and of 256 x 256 logits in a call
 // Of dz and packed weights: twice what the memory-side cache holds.  Half of it adds the features' gradients up in twice as many passes over their sums
 // (8192 x 4096 x 131072 bf16 forward and backward 41.8 ms, 41.0 so; 1000 x 768 x 32768 float32 1138 us, 1067 so).
 constexpr int64_t kPieceBytes = (int64_t)512 << 20;
@@ -1094,6 +1094,11 @@ HeadPlan head_plan(const hot_head_desc &d, bool backward, bool with_dx)
         const long n = (piece + (most > least ? most : least) - 1) / (most > least ? most : least);
         piece = up((V + n - 1) / n, 256);
     }
+    // tiles of the weights' gradients: width and words
+    const int wt = p.size >= kLarge ? 256 : (p.size == kMiddle ? 128 : 64), wv = p.size >= kLarge ? 128 : (three ? wt : 64);
+    // (float32, 2^20 rows and 2^18 words: 2^23 tiles of logits)
+    const long logits = kMostTiles / p.row_tiles * p.v_tile, weights = kMostTiles / ((K + wt - 1) / wt) * wv, most = (logits < weights || !backward ? logits : weights) / 256 * 256;
+    piece = piece < most ? piece : most;
     p.v_piece = (int)piece;
     p.v_pieces = (int)((V + piece - 1) / piece);
     // as many workgroups and sums as the best number of runs needs for all rows
@@ -1111,7 +1116,6 @@ HeadPlan head_plan(const hot_head_desc &d, bool backward, bool with_dx)
 
     // The weights' gradients: as many runs of rows as leave the fewest steps of BK rows in all rounds, twenty more to each run, and as long as their
     // partial sums are no more than two rounds of tiles (5569 x 42 x 1227 float32 without: 195 us on ten workgroups)
-    const int wt = p.size >= kLarge ? 256 : (p.size == kMiddle ? 128 : 64), wv = p.size >= kLarge ? 128 : (three ? wt : 64);
     const long w_tiles = ((piece + wv - 1) / wv < (V + wv - 1) / wv ? (piece + wv - 1) / wv : (V + wv - 1) / wv) * ((K + wt - 1) / wt) * S;
     for (long runs = 1; runs <= 256 && (runs == 1 || (runs * 4 * p.columns <= R && runs * w_tiles <= 2 * kComputeUnits)); ++runs) {
         const long depth = up((R + runs - 1) / runs, p.columns), cost = (w_tiles * runs + kComputeUnits - 1) / kComputeUnits * (depth / p.columns + 20);

@@ -27,3 +27,18 @@ def test_lists_of_many_rows_of_many_samples():
         want = torch.where(at[:, 0] >= 0, (torch.logsumexp(z, 1, keepdim=True) - z.gather(1, at.clamp(min=0)))[:, 0], 0.0)
         # |z| below 2^5; a loss of a few additions of numbers of that size
         assert z.abs().max() < 32 and (got[s].double() - want).abs().max() < 16 * 32 * U.U32, s
+
+
+def test_as_many_logits_as_a_call_takes():
+    """float32, 2^20 rows and 2^18 words: more tiles than one launch holds."""
+    rows, vocab = 1 << 20, 1 << 18
+    g = torch.Generator(device=DEV).manual_seed(4)
+    few = torch.randn(8, 1, device=DEV, generator=g)
+    w = torch.randn(vocab, 1, device=DEV, generator=g)
+    which = torch.randint(8, (rows,), device=DEV, generator=g)
+    target = torch.randint(vocab, (rows,), device=DEV, generator=g)
+    got = _ops().head_cross_entropy(few[which], w, target)
+    z = few.double() @ w.double().T
+    want = torch.logsumexp(z, 1)[which] - few.double()[which, 0] * w.double()[target, 0]
+    # |z| below 2^5, logarithms of sums below 2^5: a few roundings of numbers of that size
+    assert z.abs().max() < 32 and (got.double() - want).abs().max() < 32 * 32 * U.U32
