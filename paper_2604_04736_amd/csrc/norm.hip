@@ -342,34 +342,39 @@ hot_norm_wide_weights_kernel(NormArgs a)
         }
 }
 
-// dw and db: the sums of `parts` rows of partial sums, 64 columns and 16 runs of rows to a workgroup.
+// dw and db: the sums of `parts` rows of partial sums, 64 columns and 16 runs of rows to a workgroup (that takes several blocks of columns beyond kMostJoinBlocks:
+// a grid's dimension holds fewer than 2^32 threads).
 constexpr int kJoinRuns = 16;
+constexpr long kMostJoinBlocks = 1L << 20;
 
 __global__ void __launch_bounds__(64 * kJoinRuns)
 hot_norm_join_kernel(const float *__restrict__ parts, long count, long width, long out_sample, int type, void *dw, void *db)
 {
     __shared__ float runs[kJoinRuns][64];
     const int lane = (int)threadIdx.x & 63, run = (int)threadIdx.x >> 6, which = (int)blockIdx.y, s = (int)blockIdx.z;
-    const long col = (long)blockIdx.x * 64 + lane;
     void *const out = which ? db : dw;
     if (!out) return;                    // (the whole workgroup)
-    float sum = 0.0f;
-    if (col < width) {
-        const float *p = parts + ((size_t)s * (size_t)count * 2 + (size_t)which) * (size_t)width + (size_t)col;
-        for (long k = run; k < count; k += 4 * kJoinRuns) {
-            float v[4];
+    for (long first = (long)blockIdx.x * 64; first < width; first += (long)gridDim.x * 64) {
+        const long col = first + lane;
+        float sum = 0.0f;
+        if (col < width) {
+            const float *p = parts + ((size_t)s * (size_t)count * 2 + (size_t)which) * (size_t)width + (size_t)col;
+            for (long k = run; k < count; k += 4 * kJoinRuns) {
+                float v[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = k + i * kJoinRuns < count ? p[(size_t)(k + i * kJoinRuns) * 2 * (size_t)width] : 0.0f;
+                for (int i = 0; i < 4; ++i) v[i] = k + i * kJoinRuns < count ? p[(size_t)(k + i * kJoinRuns) * 2 * (size_t)width] : 0.0f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sum += v[i];
+                for (int i = 0; i < 4; ++i) sum += v[i];
+            }
         }
-    }
-    runs[run][lane] = sum;
-    __syncthreads();
-    if (run || col >= width) return;
+        if (first != (long)blockIdx.x * 64) __syncthreads();
+        runs[run][lane] = sum;
+        __syncthreads();
+        if (run || col >= width) continue;
 #pragma unroll
-    for (int i = 1; i < kJoinRuns; ++i) sum += runs[i][lane];
-    store_as(out, type, s * out_sample + col, sum);
+        for (int i = 1; i < kJoinRuns; ++i) sum += runs[i][lane];
+        store_as(out, type, s * out_sample + col, sum);
+    }
 }
 
 // ---------------------------------------------------------------------------------
@@ -539,7 +544,8 @@ int hot_norm_backward(const hot_norm_desc *desc, const void *x, const void *weig
         // (no rows: no partial sums to add, which gives zeros)
         const long blocks = desc->rows > 0 ? norm_backward_blocks(*desc) : 0;
         const bool own = desc->w_sample > 0;
-        hot_norm_join_kernel<<<dim3((unsigned)((desc->width + 63) / 64), 2, own ? (unsigned)desc->samples : 1u), 64 * kJoinRuns, 0, s>>>(
+        const long columns = (desc->width + 63) / 64;
+        hot_norm_join_kernel<<<dim3((unsigned)(columns < kMostJoinBlocks ? columns : kMostJoinBlocks), 2, own ? (unsigned)desc->samples : 1u), 64 * kJoinRuns, 0, s>>>(
             a.parts, own ? blocks : blocks * desc->samples, desc->width, desc->w_sample, desc->weight_dtype, grad_weight, grad_bias);
     }
     return hot_detail::note_hip(hipGetLastError());

@@ -42,3 +42,21 @@ def test_as_many_logits_as_a_call_takes():
     want = torch.logsumexp(z, 1)[which] - few.double()[which, 0] * w.double()[target, 0]
     # |z| below 2^5, logarithms of sums below 2^5: a few roundings of numbers of that size
     assert z.abs().max() < 32 and (got.double() - want).abs().max() < 32 * 32 * U.U32
+
+
+def test_weights_gradients_of_the_widest_rows():
+    """Two rows of 2^28 + 65 elements: more blocks of columns than one launch of a workgroup each holds."""
+    width = (1 << 28) + 65
+    g = torch.Generator(device=DEV).manual_seed(5)
+    x = torch.randn(2, width, device=DEV, generator=g)
+    w, b = torch.ones(width, device=DEV, requires_grad=True), torch.zeros(width, device=DEV, requires_grad=True)
+    dy = torch.randn(2, width, device=DEV, generator=g)
+    dw, db = torch.autograd.grad(_ops().layer_norm(x, w, b), (w, b), dy)
+    stats = [(float(x[r].double().mean()), float((x[r].double().var(correction=0) + 1e-5).rsqrt())) for r in range(2)]
+    for at in (slice(0, 1 << 20), slice((1 << 26) - 500, (1 << 26) + 500), slice(width - (1 << 20), width)):
+        d = dy[:, at].double()
+        h = torch.stack([(x[r, at].double() - stats[r][0]) * stats[r][1] for r in range(2)])
+        # sums of 2^28 elements over 1024 threads, each a chain of 2^18: mean and variance good for 2^18 U32 of their terms at worst, and two rows
+        off = (1 << 18) * U.U32
+        U.within(dw[at], (d * h).sum(0), (d.abs() * (off * (1 + h.abs()) + 8 * U.U32 * h.abs())).sum(0) + 1e-30, "dw")
+        U.within(db[at], d.sum(0), 4 * U.U32 * d.abs().sum(0) + 1e-30, "db")
