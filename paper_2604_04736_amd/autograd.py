@@ -354,7 +354,7 @@ def head_cross_entropy(x, weight, target, bias=None, ignore_index: int = -100) -
     """Cross entropy of the rows of a linear head, float32, from the features in front of it: ln sum_v exp(z_v) - z_target with
     z = x weight^T + bias, without logits in memory; differentiable in x, weight and bias.  x [..., width], weight [vocab, width],
     bias [vocab] or None, target int64 [...]; or one head per weight sample: weight [S, vocab, width], bias [S, vocab], x
-    [S, ..., width] or [rows, width] (which every sample then sees), target with or without the samples' axis.  Rows whose target is
+    [S, ..., width] or [rows, width] (which every sample then sees, and whose gradient is formed once), target with or without the samples' axis.  Rows whose target is
     ignore_index have loss 0 and take no part; a loss over the others is loss.sum() / their number.  x, weight and bias have one type:
     float32, bfloat16 or float16."""
     return _head(x, weight, bias, target, None, ignore_index, 1.0, 0)

@@ -161,7 +161,7 @@ hot_head_lists_kernel(ListArgs a)
 // The features' gradients: a run of a piece's words to a workgroup.  A round of workgroups takes its steps of 64 words, and as long as some twenty
 // of them for its start and for adding to the sums in memory; of the numbers of runs up to 64 the one with the fewest such steps is taken, by the host for all
 // rows (workgroups and sums of that many), and by the device for the rows that count within what the host gave (all passes of
-// 900 x 768 x 20000 float32 of which 65 % are left out: 354 -> 324 us, 2048 x 1024 x 30000 bf16, 70 %: 257 -> 244).
+// 900 x 768 x 20000 float32 of which 65 % are left out: 383 -> 357 us, 2048 x 1024 x 30000 bf16, 70 %: 388 -> 337).
 struct WordRuns {
     int rows_log, at_once_log;     // rows of a tile and workgroups that run at once, powers of two
     int width_tiles, samples, piece;
@@ -805,8 +805,7 @@ hot_head_join_kernel(JoinArgs a)
 struct GradArgs {
     Matrix dz, other;              // other: W (from word v_begin) or the packed features
     long dz_sample, sample;
-    int width, vocab, v_begin, v_count;
-    long rows;
+    int width, v_begin, v_count;
     const int *count;
     WordRuns runs;                 // of words
     bool first;                    // of the pieces: sums begin with it
@@ -1016,8 +1015,8 @@ constexpr int64_t kPieceBytes = (int64_t)512 << 20;
 
 // Sizes of tiles (of logits: words x rows): 256 x 32 for up to 32 rows, 64 x 64 and 128 x 128 where larger ones leave the chip empty, 256 x 256
 // (256 x 128 in three pieces).
-// Float32 heads of up to 128 rows with 256 tiles of words have 256 x 128 with the weights read as they lie (128 x 1024 x 65536: 971 us packed, 646 so; with half as
-// many tiles, 64 x 768 x 32768, whose packed weights stay in the memory-side cache, 278 packed, 289 so).
+// Float32 heads of up to 128 rows with 256 tiles of words have 256 x 128 with the weights read as they lie (128 x 1024 x 65536 forward and backward: 842 us packed, 585 so; with half as
+// many tiles, 64 x 768 x 32768, whose packed weights stay in the memory-side cache, 281 packed, 278 so).
 // Tiles of the gradients are the same, but with half as many words (weights') or rows (features') where two pieces of dz would take twice the room: 256 x 128, and 128 x 64
 // for 128 x 128 (512 x 1024 x 11000 bf16 forward and backward 140 us; with all 128, one workgroup to a compute unit, 153, with 64 x 64 150).
 enum { kFew, kSmall, kMiddle, kLarge, kTall };
@@ -1028,7 +1027,7 @@ struct HeadPlan {
     int columns;             // of a block of what is packed
     long row_bytes;          // of a packed row: whole blocks
     long places;
-    int v_piece, v_pieces;   // words of a piece
+    int v_piece;             // words of a piece
     int size;                // kFew ... kTall
     int v_tile, r_tile;      // words and rows of a tile of logits
     int x_tile;              // rows of a tile of the features' gradients
@@ -1100,7 +1099,6 @@ HeadPlan head_plan(const hot_head_desc &d, bool backward, bool with_dx)
     const long logits = kMostTiles / p.row_tiles * p.v_tile, weights = kMostTiles / ((K + wt - 1) / wt) * wv, most = (logits < weights || !backward ? logits : weights) / 256 * 256;
     piece = piece < most ? piece : most;
     p.v_piece = (int)piece;
-    p.v_pieces = (int)((V + piece - 1) / piece);
     // as many workgroups and sums as the best number of runs needs for all rows
     WordRuns &w = p.word_runs;
     static_assert(kComputeUnits == 256, "");
@@ -1115,7 +1113,7 @@ HeadPlan head_plan(const hot_head_desc &d, bool backward, bool with_dx)
     long best = 0;
 
     // The weights' gradients: as many runs of rows as leave the fewest steps of BK rows in all rounds, twenty more to each run, and as long as their
-    // partial sums are no more than two rounds of tiles (5569 x 42 x 1227 float32 without: 195 us on ten workgroups)
+    // partial sums are no more than two rounds of tiles (5569 x 42 x 1227 float32, forward and backward: 403 us on ten workgroups, 153 so)
     const long w_tiles = ((piece + wv - 1) / wv < (V + wv - 1) / wv ? (piece + wv - 1) / wv : (V + wv - 1) / wv) * ((K + wt - 1) / wt) * S;
     for (long runs = 1; runs <= 256 && (runs == 1 || (runs * 4 * p.columns <= R && runs * w_tiles <= 2 * kComputeUnits)); ++runs) {
         const long depth = up((R + runs - 1) / runs, p.columns), cost = (w_tiles * runs + kComputeUnits - 1) / kComputeUnits * (depth / p.columns + 20);
@@ -1478,10 +1476,8 @@ void head_backward(const HeadCall &c, const double *lse, const float *g, long g_
         a.dz = {h.dz, c.p.columns * 2L, h.dz_block, h.dz_plane};
         a.dz_sample = h.dz_sample;
         a.width = h.width;
-        a.vocab = h.vocab;
         a.v_begin = h.v_begin;
         a.v_count = h.v_count;
-        a.rows = h.rows;
         a.count = h.count;
         a.runs = head_runs(c);
         a.first = v == 0;

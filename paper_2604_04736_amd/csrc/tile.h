@@ -306,9 +306,9 @@ struct Tile {
 
     // results = A B over `depth` contraction indices; LDS is free when it returns.  Two sets of operands in registers.  Between the parts of
     // a step's products the next step's operands are read; the last step of a tile begins with the barrier behind which the tile's room
-    // is free: the loads that go there are issued in that step and the one behind it.  256 x 256 tiles of 8192 x 4096 x 131072 in bf16 run at
-    // 1.37 PFLOP/s along, 1.24 to 1.36 across (a library's product 1.48); four waves with 128 x 128 results each were slower (1.06 to 1.3), so were tiles
-    // of 256 x 128 with two workgroups to a compute unit (1.06).
+    // is free: the loads that go there are issued in that step and the one behind it.  Tiles of 8192 x 4096 x 131072 in bf16 run at 1.33 to
+    // 1.37 PFLOP/s along (256 x 256), 1.23 and 1.26 across (256 x 128, two pieces; a library's product 1.48).  For one piece four waves with 128 x 128 results each
+    // were slower (1.06 to 1.3), so were tiles of 256 x 128 with two workgroups to a compute unit (1.06).
     static __device__ __forceinline__ void product(lds_char *lds, const Operand &a, const Operand &b, int depth, f16v (&results)[MB][NB])
     {
         const int l = lane(), w = wave();
