@@ -238,6 +238,15 @@ def _adjacent(t):
     return t if t.shape[-1] < 2 or t.stride(-1) == 1 else t.contiguous()
 
 
+def _apart(weight):
+    """weight [..., vocab, width], or a copy where its rows or samples lie between each other (one set for all samples is left as it is)."""
+    weight = _adjacent(weight)
+    vocab, width = weight.shape[-2:]
+    rows = weight.stride(-2) if vocab > 1 else width
+    between = rows < width or (weight.dim() == 3 and weight.shape[0] > 1 and 0 < weight.stride(0) < (vocab - 1) * rows + width)
+    return weight.contiguous() if between else weight
+
+
 class _Norm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, eps, per_sample):
@@ -320,7 +329,7 @@ def _head(x, weight, bias, index, logit, ignore_index, temperature, entries: int
     if bias is not None and bias.shape != weight.shape[:-1]:
         raise ValueError(f"bias: need {tuple(weight.shape[:-1])}, got {tuple(bias.shape)}")
     width, tail = x.shape[-1], index.shape[index.dim() - entries:]
-    x, weight = _adjacent(x), _adjacent(weight)
+    x, weight = _adjacent(x), _apart(weight)
     if weight.dim() == 2:
         shape = x.shape[:-1]
         if index.shape[:index.dim() - entries] != shape:

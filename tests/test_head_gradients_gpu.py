@@ -124,3 +124,20 @@ def test_rows_of_very_different_weights():
     for r in range(rows):
         want, bound = U.head_plain(x[r:r + 1][None], w[None], b[None], U.labels(target[r:r + 1][None], vocab), up[r:r + 1][None])["dx"]
         U.within(got[r:r + 1], want[0], bound[0] + 1.01 * step / 2 * w.double().abs().sum(0), f"row {r}")
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_weights_that_lie_between_each_other(kind):
+    """Samples whose rows alternate in memory, and rows that are one row, give what copies of them give."""
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x, target = torch.randn(2, 40, 32, device=DEV, generator=g).to(U.TYPES[kind]), torch.randint(90, (40,), device=DEV, generator=g)
+    alternate = torch.randn(90, 2, 32, device=DEV, generator=g).to(U.TYPES[kind])
+    one = alternate[:1, 0]
+    for x, base, view in ((x, alternate, lambda t: t.permute(1, 0, 2)), (x[0], one, lambda t: t.expand(90, 32))):
+        got = {}
+        for name in ("as they lie", "copied"):
+            leaves = [t.detach().requires_grad_() for t in (x, base)]
+            w = view(leaves[1])
+            loss = _loss(leaves[0], w if name == "as they lie" else w.contiguous(), None, target)
+            got[name] = [loss.detach(), *torch.autograd.grad(loss.sum(), leaves)]
+        assert all(torch.equal(a, c) for a, c in zip(*got.values()))
