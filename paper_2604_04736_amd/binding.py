@@ -948,7 +948,7 @@ def hot_head_backward(x, weight, bias, index, logit, lse, grad_loss, dx=None, gr
     losses (grad_loss, float32 [samples, rows], any strides); each result may be None and is then left out.  Features that all samples
     share are x [1, rows, width], and so is their gradient, summed over the samples."""
     d = _head_desc(x, weight, bias, index, logit, ignore_index, temperature)
-    if dx is not None and x.shape[0] > 1 and d.x_sample == 0:
+    if dx is not None and x.shape[0] > 1 and d.x_sample == 0 and d.rows > 0:
         raise ValueError("x: the samples lie on one memory, whose gradient is [1, rows, width]; need x[:1], or a copy for a gradient of each")
     _dense(lse, (d.samples, d.rows), torch.float64, x, "lse")
     if not (grad_loss.is_cuda and grad_loss.device == x.device and grad_loss.dtype == torch.float32 and tuple(grad_loss.shape) == (d.samples, d.rows)):

@@ -141,3 +141,10 @@ def test_weights_that_lie_between_each_other(kind):
             loss = _loss(leaves[0], w if name == "as they lie" else w.contiguous(), None, target)
             got[name] = [loss.detach(), *torch.autograd.grad(loss.sum(), leaves)]
         assert all(torch.equal(a, c) for a, c in zip(*got.values()))
+
+
+def test_no_rows_expanded_over_samples():
+    base, drawn = torch.zeros(0, 8, device=DEV, requires_grad=True), torch.randn(2, 100, device=DEV, requires_grad=True)
+    loss = _loss(base.expand(2, 0, 8), drawn[:, 3:75].unflatten(1, (9, 8)), None, torch.zeros(0, dtype=torch.long, device=DEV))
+    dx, dw = torch.autograd.grad(loss.sum(), (base, drawn))
+    assert loss.shape == (2, 0) and dx.shape == (0, 8) and not dw.any()
