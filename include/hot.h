@@ -634,6 +634,111 @@ int hot_head_backward(const hot_head_desc *desc, const void *x, const void *weig
                       void *grad_weight, void *grad_bias, void *workspace, int64_t workspace_bytes, void *stream);
 
 /*
+ * Dropout of activations: element c of row r of sample s stays where sixteen bits of the generator lie below T = round(65536 keep) (a tie to the
+ * even number, at least 1), and is multiplied by 65536 / T; the others are zeros, whatever they were.  The bits are number c mod 2 (from the low end) of word
+ * (c mod 8) / 2 of Philox-4x32-10 under rng's seed at counter (i, first_sample + s, step) with i = 2^63 + offset + r ceil(width / 8) + c div 8: no
+ * mask is stored, the same call on a gradient is the backward pass, and no counter is one that the draw of weights uses.  Layers of one network take disjoint
+ * ranges of `offset`, which counts in calls of the generator (eight elements each).  x and y: dense [samples, rows, width]; y may be x.
+ */
+typedef struct hot_dropout_desc {
+    int64_t rows;      /* of one sample, >= 0 */
+    int64_t width;     /* >= 1 */
+    int64_t offset;    /* >= 0 */
+    double keep;       /* 0 < keep <= 1 */
+    int32_t samples;   /* 1 .. 65535 */
+    int32_t dtype;
+} hot_dropout_desc;
+
+int hot_dropout(const hot_dropout_desc *desc, const hot_rng *rng, const void *x, void *y, void *stream);
+
+/*
+ * The end of a block fused with the norm that begins the next:
+ *   t = norm'(branch),  d = dropout(t) (as hot_dropout; keep = 1: none),  h = x + scale gate d,  y = norm(h)
+ * norm and norm': HOT_NORM_LAYER (as hot_norm_forward), HOT_NORM_RMS (x / sqrt(mean x^2 + eps)) or HOT_NORM_NONE, then without weight, bias, and, for norm,
+ * without y.  x, branch, h, y and their gradients: dense [samples, rows, width], width <= HOT_BLOCK_MOST_WIDTH.  Vectors: [width] for every
+ * sample, *_sample elements apart (0: one for all; then its gradient is summed over all samples too); any of them may be NULL (ones, or zeros
+ * for biases).  y is the norm of h before h is rounded to its type.  stats: fp32 [samples, rows, 4], 16-byte aligned, for the backward call, or NULL.
+ */
+#define HOT_NORM_NONE 0
+#define HOT_NORM_LAYER 1
+#define HOT_NORM_RMS 2
+#define HOT_BLOCK_MOST_WIDTH 16384
+
+typedef struct hot_block_desc {
+    int64_t rows;      /* of one sample, >= 0 */
+    int64_t width;
+    int64_t weight_sample, bias_sample, gate_sample, branch_weight_sample, branch_bias_sample; /* 0 or >= width */
+    int64_t offset;    /* as in hot_dropout_desc */
+    double scale, keep, eps;
+    int32_t samples;   /* 1 .. 65535 */
+    int32_t dtype;
+    int32_t vector_dtype;      /* of all vectors and their gradients: dtype or HOT_F32 */
+    int32_t norm, branch_norm;
+    int32_t reserved;
+} hot_block_desc;
+
+int hot_block_forward(const hot_block_desc *desc, const hot_rng *rng, const void *x, const void *branch, const void *weight, const void *bias,
+                      const void *gate, const void *branch_weight, const void *branch_bias, void *h, void *y, float *stats, void *stream);
+
+/*
+ * dh, dy: gradients of h and y, NULL for zeros.  Any result may be NULL and is then left out; those of vectors are formed in a fixed order through the
+ * workspace (hot_block_backward_workspace_bytes; NULL where no vector's gradient is asked for).  rng is NULL only where keep = 1.
+ */
+int64_t hot_block_backward_workspace_bytes(const hot_block_desc *desc);
+int hot_block_backward(const hot_block_desc *desc, const hot_rng *rng, const void *x, const void *branch, const void *weight, const void *gate,
+                       const void *branch_weight, const void *branch_bias, const float *stats, const void *dh, const void *dy, void *dx,
+                       void *dbranch, void *grad_weight, void *grad_bias, void *grad_gate, void *grad_branch_weight, void *grad_branch_bias,
+                       void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * Attention with a learned relative position bias by buckets.  Query i of head h in entry b of the batch sees key j with
+ *   z = scale q[i] . k[j] + table[bucket[query_code[first_query + i] - key_code[j]], h],   o[i] = sum_j softmax_j(z) v[j]
+ * over the keys that it may see: j <= i + keys - queries where causal, and query_groups[i] = key_groups[j] >= 0 where there are groups.  A query that sees
+ * nothing has o = 0 and gradients 0; what rows of negative groups hold reaches nothing.  Query head h reads key and value head h / (heads / kv_heads).
+ * q, o and their gradients: [batch, heads, queries, width], k and v [batch, kv_heads, keys, width], each with pitches of its own in elements
+ * (batch, head, row; elements of a row adjacent).  table: dense [tables, buckets, heads] of table_dtype (dtype or HOT_F32), entry b taking table
+ * b / (batch / tables); tables = 0: no bias, and no codes.  query_code, key_code: int32, such that differences lie in 0 .. codes - 1; bucket: int32
+ * [codes]; key_range: int32 [ceil(keys / 64), 2], the smallest and largest key code of 64 keys each.  (Indices outside are taken as the last.)  Groups: int32
+ * [groups, queries] and [groups, keys], entry b taking row b mod groups; groups = 0: none.
+ * Limits: HOT_ATTENTION_MOST_*; batch x heads x max(queries, keys) below 2^31.
+ */
+#define HOT_ATTENTION_MOST_WIDTH 128
+#define HOT_ATTENTION_MOST_BUCKETS 4096
+#define HOT_ATTENTION_MOST_CODES 4194304
+
+typedef struct hot_pitch {
+    int64_t batch, head, row;
+} hot_pitch;
+
+typedef struct hot_attention_desc {
+    int64_t queries, keys;                     /* of an entry, >= 0 */
+    hot_pitch q, k, v, o;
+    hot_pitch grad_o, grad_q, grad_k, grad_v;  /* backward call */
+    double scale;
+    int32_t batch, heads, kv_heads, width;
+    int32_t tables, buckets, codes, first_query;
+    int32_t groups, causal;
+    int32_t dtype, table_dtype;
+} hot_attention_desc;
+
+/* Scratch of a call: which = 0 forward, 1 backward. */
+int64_t hot_attention_workspace_bytes(const hot_attention_desc *desc, int which);
+
+/*
+ * stats: fp32 [batch, heads, queries, 2], and rest (o's pitches and type; 16-bit types only): what o's rounding left over.  Both are for the backward call; NULL leaves
+ * them out.
+ */
+int hot_attention_forward(const hot_attention_desc *desc, const void *q, const void *k, const void *v, const void *table, const int32_t *query_code,
+                          const int32_t *key_code, const int32_t *key_range, const int32_t *bucket, const int32_t *query_groups,
+                          const int32_t *key_groups, void *o, void *rest, float *stats, void *workspace, int64_t workspace_bytes, void *stream);
+
+/* All of grad_q, grad_k and grad_v are written (each may be NULL), grad_table (dense, table_dtype) where it is not NULL, every sum in a fixed order. */
+int hot_attention_backward(const hot_attention_desc *desc, const void *q, const void *k, const void *v, const void *table, const int32_t *query_code,
+                           const int32_t *key_code, const int32_t *key_range, const int32_t *bucket, const int32_t *query_groups,
+                           const int32_t *key_groups, const void *o, const void *rest, const float *stats, const void *grad_o, void *grad_q,
+                           void *grad_k, void *grad_v, void *grad_table, void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
  * Measurement aid, not a step of the paper's path: copies `bytes` (a multiple of 16;
  * both DEVICE pointers 16-byte aligned, ranges disjoint) on the current device with
  * the same 16-byte accesses the kernels use.  Its traffic is known exactly (bytes

@@ -19,6 +19,7 @@ caller's scaling).
 from __future__ import annotations
 
 import functools
+import math
 import operator
 
 import torch
@@ -379,3 +380,123 @@ def head_distillation(x, weight, top_index, top_logit, bias=None, temperature: f
     if not 1 <= top_index.shape[-1] <= hot.HOT_HEAD_MOST_TOP:
         raise ValueError(f"top_index: need 1 to {hot.HOT_HEAD_MOST_TOP} words a row, got {top_index.shape[-1]}")
     return _head(x, weight, bias, top_index, top_logit.detach(), -100, temperature, 1)
+
+
+# ------------------------------------------------------------------ dropout, the end of a block, attention
+
+def _counter(rng, keep: float):
+    if rng is None:
+        if keep != 1.0:
+            raise ValueError("rng: dropout needs a hot_rng")
+        return 0, 0, 0
+    return rng.seed, rng.step, rng.first_sample
+
+
+def dropout(x, keep: float, rng, samples: int = 0, offset: int = 0) -> torch.Tensor:
+    """Dropout of activations x [..., width] (with samples = S: [S, ..., width], one mask per Monte-Carlo sample): an element stays with probability keep, in
+    steps of 2^-16, and is divided by it; the others are zeros.  Which ones stay follows from rng (binding.hot_rng: seed, step, first_sample, the
+    global number of sample 0) and the element's place alone, so no mask is stored, the backward pass draws it again, and GPUs that share a seed draw
+    different samples.  Layers of one network take disjoint ranges of offset: dropout_calls(x, samples) calls of the generator each.
+    float32, bfloat16 or float16; differentiable any number of times."""
+    if not isinstance(rng, hot.hot_rng):
+        raise TypeError("rng: need a hot_rng")
+    return hot.host().dropout(x, float(keep), rng.seed, rng.step, rng.first_sample, int(samples), int(offset))
+
+
+def dropout_calls(x, samples: int = 0) -> int:
+    """Calls of the generator that a sample of x [..., width] takes: the next layer's offset lies that much further."""
+    width = x.shape[-1]
+    return x.numel() // width // (samples or 1) * ((width + 7) // 8)
+
+
+def residual_norm(x, branch, weight=None, bias=None, *, norm: str | None = "layer", gate=None, scale: float = 1.0, branch_norm: str | None = None, branch_weight=None,
+                  branch_bias=None, keep: float = 1.0, rng=None, samples: int = 0, offset: int = 0, eps: float = 1e-5):
+    """The end of a block and the norm that begins the next: (h, y) with h = x + scale gate dropout(norm'(branch)) and y = norm(h), in one pass, differentiable
+    in all tensors.  norm, branch_norm (norm'): "layer", "rms" or None (norm None: y is None).  x, branch: [..., width] of one type, float32, bfloat16 or float16,
+    width up to 16384; weight, bias, gate, branch_weight, branch_bias: [width], or with samples = S and x [S, ..., width] also [S, width], x's type or float32
+    (all of them one), None for ones and zeros.  keep, rng, samples, offset: as in dropout; keep = 1 leaves it out.  y is the norm of h before h is rounded
+    to x's type."""
+    for kind, name in ((norm, "norm"), (branch_norm, "branch_norm")):
+        if kind not in hot.HOT_NORMS:
+            raise ValueError(f"{name}: need 'layer', 'rms' or None, got {kind!r}")
+    if rng is not None and not isinstance(rng, hot.hot_rng):
+        raise TypeError("rng: need a hot_rng")
+    out = hot.host().block_end(x, branch, weight, bias, gate, branch_weight, branch_bias, hot.HOT_NORMS[norm], hot.HOT_NORMS[branch_norm], float(scale), float(keep),
+                               float(eps), *_counter(rng, keep), int(samples), int(offset))
+    return out[0], (out[1] if len(out) > 1 else None)
+
+
+class RelativePositions:
+    """Where queries and keys stand, for attention's bias: whole-number codes of both, and for every difference query code - key code, from the smallest on,
+    which of `buckets` rows of the table it takes.  Made once and kept; distances() and windows() make the usual ones."""
+
+    def __init__(self, query_codes, key_codes, bucket_of, buckets: int, device):
+        query, key, bucket = (torch.as_tensor(t).detach().cpu() for t in (query_codes, key_codes, bucket_of))
+        for t, name in ((query, "query_codes"), (key, "key_codes"), (bucket, "bucket_of")):
+            if t.dim() != 1 or t.numel() < 1 or t.is_floating_point() or t.is_complex() or t.dtype == torch.bool:
+                raise ValueError(f"{name}: need a vector of whole numbers, got {tuple(t.shape)} of {t.dtype}")
+        query, key, bucket = query.long(), key.long(), bucket.long()
+        codes = int(query.max()) - int(key.min()) - (int(query.min()) - int(key.max())) + 1
+        if not 1 <= codes <= hot.HOT_ATTENTION_MOST_CODES:
+            raise ValueError(f"codes: need at most {hot.HOT_ATTENTION_MOST_CODES} differences, got {codes}")
+        if bucket.numel() != codes:
+            raise ValueError(f"bucket_of: need a bucket for each of {codes} differences, got {bucket.numel()}")
+        if not 1 <= buckets <= hot.HOT_ATTENTION_MOST_BUCKETS:
+            raise ValueError(f"buckets: need 1 to {hot.HOT_ATTENTION_MOST_BUCKETS}, got {buckets}")
+        if int(bucket.min()) < 0 or int(bucket.max()) >= buckets:
+            raise ValueError(f"bucket_of: need 0 to {buckets - 1}, got {int(bucket.min())} to {int(bucket.max())}")
+        self.queries, self.keys, self.buckets = query.numel(), key.numel(), int(buckets)
+        shifted = key - key.max()
+        tiles = torch.nn.functional.pad(shifted, (0, -len(shifted) % 64), value=int(shifted[-1])).view(-1, 64)
+        ranges = torch.stack([tiles.amin(1), tiles.amax(1)], 1)
+        self.query_code, self.key_code, self.key_range, self.bucket = (
+            t.to(torch.int32).contiguous().to(device) for t in (query - query.min(), shifted, ranges, bucket))
+
+    @classmethod
+    def distances(cls, queries: int, keys: int, buckets: int, furthest: int, device, both_sides: bool = True, first_query: int = 0):
+        """Tokens on a line, query i at first_query + i, key j at j: half of the buckets (of a side, where both_sides) for one distance each, the others for ranges that
+        grow with the logarithm up to `furthest` and hold what is further.  One-sided, keys behind the query share the bucket of distance 0."""
+        side = buckets // 2 if both_sides else buckets
+        near = side // 2
+        if near < 1 or furthest <= near or (both_sides and buckets % 2):
+            raise ValueError(f"buckets and furthest: need an even number of buckets of at least {4 if both_sides else 2} and a distance beyond {max(near, 1)}, got {buckets} and {furthest}")
+        if queries < 1 or keys < 1:
+            raise ValueError(f"queries and keys: need at least one, got {queries} and {keys}")
+        query, key = torch.arange(queries) + first_query, torch.arange(keys)
+        distance = torch.arange(int(query[0]) - int(key[-1]), int(query[-1]) + 1)
+        away = distance.abs() if both_sides else distance.clamp(min=0)
+        far = near + (torch.log(away.clamp(min=1).double() / near) / math.log(furthest / near) * (side - near)).long()
+        bucket = torch.where(away < near, away, far.clamp(max=side - 1))
+        return cls(query, key, bucket + side * (distance < 0) if both_sides else bucket, buckets, device)
+
+    @classmethod
+    def windows(cls, *extent: int, device):
+        """The tokens of a window of extent[0] x extent[1] x ... in order of memory, a row of the table for every difference of places: prod(2 extent - 1) buckets, in
+        order of the differences from the smallest on, the last axis fastest."""
+        if not extent or min(extent) < 1:
+            raise ValueError(f"extent: need at least one axis of at least one token, got {extent}")
+        place, code = torch.meshgrid(*(torch.arange(n) for n in extent), indexing="ij"), 0
+        for axis, n in zip(place, extent):
+            code = code * (2 * n - 1) + axis
+        code = code.reshape(-1)
+        span = 2 * int(code[-1]) + 1
+        return cls(code, code, torch.arange(span), span, device)
+
+
+def attention(q, k, v, table=None, positions: RelativePositions | None = None, *, scale: float | None = None, causal: bool = False, query_groups=None, key_groups=None,
+              first_query: int = 0) -> torch.Tensor:
+    """softmax over the keys of scale q k^T + bias, times v, without scores in memory; differentiable in q, k, v and table.
+    q [..., heads, queries, width], k and v [..., kv heads, keys, width], kv heads dividing heads, width up to 128; float32, bfloat16 or float16, any strides with adjacent
+    elements of a row (the result's and the gradients' tokens lie as [..., tokens, heads, width] where q, k and v are no dense arrays of their own).  scale: 1 / sqrt(width) where None.
+    The bias of head h is table[bucket, h] with the bucket of positions for the two tokens' codes: table [buckets, heads], or [S, buckets, heads] with one table per
+    weight sample and q [S, ..., heads, queries, width]; q's type or float32.  Query i is query first_query + i of positions, so one object serves single tokens of a
+    growing text.
+    Causal: query i sees keys up to i + keys - queries.  query_groups, key_groups: int32 [queries] and [keys], or [entries, ...], row b mod entries for entry b of q's
+    flattened leading axes; a query sees the keys of its own group (texts packed into a row, pieces of a shifted window), negative groups are padding
+    and whatever lies there reaches nothing.  key_groups alone: all queries are of group 0.  A query that sees nothing gives zeros and has no gradients."""
+    if table is not None and not isinstance(positions, RelativePositions):
+        raise TypeError("positions: a table needs RelativePositions")
+    if not isinstance(q, torch.Tensor):
+        raise TypeError("q: need a tensor")
+    p = (positions.query_code, positions.key_code, positions.key_range, positions.bucket, positions.buckets) if table is not None else (None,) * 4 + (0,)
+    return hot.host().attention(q, k, v, table, *p, query_groups, key_groups, int(first_query), float(scale if scale is not None else max(q.shape[-1:] or (1,)) ** -0.5), bool(causal))

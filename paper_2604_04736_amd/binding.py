@@ -35,18 +35,23 @@ EXPORTS = ("hot_create", "hot_forward", "hot_backward", "hot_destroy", "hot_set_
            "hot_linear_launch_shape", "hot_linear_kernel_shape", "hot_linear_planes_shape",
            "hot_linear_forward_rng_ws", "hot_linear_planes_workspace_bytes", "hot_kl_layer",
            "hot_norm_forward", "hot_norm_backward", "hot_norm_backward_workspace_bytes", "hot_head_forward",
-           "hot_head_backward", "hot_head_workspace_bytes")
+           "hot_head_backward", "hot_head_workspace_bytes", "hot_dropout", "hot_block_forward", "hot_block_backward",
+           "hot_block_backward_workspace_bytes", "hot_attention_forward", "hot_attention_backward", "hot_attention_workspace_bytes")
 
 
 # Return types of the entry points that do not return an int status (as declared in include/hot.h).
 RESTYPES = {"hot_strerror": ctypes.c_char_p, "hot_recommended_ld": ctypes.c_int64,
             "hot_linear_backward_workspace_bytes": ctypes.c_int64, "hot_linear_kernel_shape": ctypes.c_int64,
             "hot_linear_planes_workspace_bytes": ctypes.c_int64, "hot_norm_backward_workspace_bytes": ctypes.c_int64,
-            "hot_head_workspace_bytes": ctypes.c_int64}
+            "hot_head_workspace_bytes": ctypes.c_int64, "hot_block_backward_workspace_bytes": ctypes.c_int64,
+            "hot_attention_workspace_bytes": ctypes.c_int64}
 
 # Element types of the norm and the head (HOT_F32, HOT_BF16, HOT_F16).
 HOT_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 HOT_HEAD_MOST_TOP = 1024
+HOT_NORMS = {None: 0, "layer": 1, "rms": 2}
+HOT_BLOCK_MOST_WIDTH = 16384
+HOT_ATTENTION_MOST_WIDTH, HOT_ATTENTION_MOST_BUCKETS, HOT_ATTENTION_MOST_CODES = 128, 4096, 1 << 22
 
 
 class hot_desc(ctypes.Structure):
@@ -90,6 +95,31 @@ class hot_head_desc(ctypes.Structure):
                 ("logit_sample", ctypes.c_int64), ("ignore_index", ctypes.c_int64), ("temperature", ctypes.c_double),
                 ("top", ctypes.c_int32), ("samples", ctypes.c_int32), ("dtype", ctypes.c_int32), ("logit_dtype", ctypes.c_int32),
                 ("w_aligned", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class hot_dropout_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("width", ctypes.c_int64), ("offset", ctypes.c_int64), ("keep", ctypes.c_double),
+                ("samples", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class hot_block_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("width", ctypes.c_int64), ("weight_sample", ctypes.c_int64), ("bias_sample", ctypes.c_int64),
+                ("gate_sample", ctypes.c_int64), ("branch_weight_sample", ctypes.c_int64), ("branch_bias_sample", ctypes.c_int64),
+                ("offset", ctypes.c_int64), ("scale", ctypes.c_double), ("keep", ctypes.c_double), ("eps", ctypes.c_double),
+                ("samples", ctypes.c_int32), ("dtype", ctypes.c_int32), ("vector_dtype", ctypes.c_int32), ("norm", ctypes.c_int32),
+                ("branch_norm", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class hot_pitch(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("head", ctypes.c_int64), ("row", ctypes.c_int64)]
+
+
+class hot_attention_desc(ctypes.Structure):
+    _fields_ = [("queries", ctypes.c_int64), ("keys", ctypes.c_int64), ("q", hot_pitch), ("k", hot_pitch), ("v", hot_pitch), ("o", hot_pitch),
+                ("grad_o", hot_pitch), ("grad_q", hot_pitch), ("grad_k", hot_pitch), ("grad_v", hot_pitch), ("scale", ctypes.c_double),
+                ("batch", ctypes.c_int32), ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("width", ctypes.c_int32),
+                ("tables", ctypes.c_int32), ("buckets", ctypes.c_int32), ("codes", ctypes.c_int32), ("first_query", ctypes.c_int32),
+                ("groups", ctypes.c_int32), ("causal", ctypes.c_int32), ("dtype", ctypes.c_int32), ("table_dtype", ctypes.c_int32)]
 
 
 class HotError(RuntimeError):
@@ -182,6 +212,17 @@ def lib() -> ctypes.CDLL:
     L.hot_head_backward.argtypes = [hp] + [vp] * 7 + [ctypes.c_int64] * 2 + [vp] * 4 + [ctypes.c_int64, vp]
     L.hot_head_workspace_bytes.argtypes = [hp, ctypes.c_int]
     L.hot_head_workspace_bytes.restype = ctypes.c_int64
+    L.hot_dropout.argtypes = [ctypes.POINTER(hot_dropout_desc), rp] + [vp] * 3
+    bp = ctypes.POINTER(hot_block_desc)
+    L.hot_block_forward.argtypes = [bp, rp] + [vp] * 11
+    L.hot_block_backward.argtypes = [bp, rp] + [vp] * 17 + [ctypes.c_int64, vp]
+    L.hot_block_backward_workspace_bytes.argtypes = [bp]
+    L.hot_block_backward_workspace_bytes.restype = ctypes.c_int64
+    ap = ctypes.POINTER(hot_attention_desc)
+    L.hot_attention_forward.argtypes = [ap] + [vp] * 14 + [ctypes.c_int64, vp]
+    L.hot_attention_backward.argtypes = [ap] + [vp] * 19 + [ctypes.c_int64, vp]
+    L.hot_attention_workspace_bytes.argtypes = [ap, ctypes.c_int]
+    L.hot_attention_workspace_bytes.restype = ctypes.c_int64
     for name in EXPORTS:
         if name not in RESTYPES:
             getattr(L, name).restype = ctypes.c_int
@@ -965,3 +1006,189 @@ def hot_head_backward(x, weight, bias, index, logit, lse, grad_loss, dx=None, gr
                                        grad_loss.data_ptr(), _pitch(grad_loss, 0), _pitch(grad_loss, 1), _ptr(dx), _ptr(grad_weight),
                                        _ptr(grad_bias), ws, ws_bytes, _stream(dev))
     _check_planless(code, "hot_head_backward")
+
+
+# ------------------------------------------------------------------ dropout, a block's end, attention
+
+def _rng_ref(rng):
+    return ctypes.byref(rng) if rng is not None else None
+
+
+def hot_dropout(rng: hot_rng, keep: float, x, y, offset: int = 0) -> None:
+    """Dropout of x [samples, rows, width] into y (dense, which may be x); see include/hot.h for which elements stay."""
+    kind = _typed(x, "x")
+    if x.dim() != 3 or x.shape[2] < 1 or not x.is_contiguous():
+        raise ValueError(f"x: need a contiguous [samples, rows, width], got {tuple(x.shape)} strides {x.stride()}")
+    _dense(y, x.shape, x.dtype, x, "y")
+    d = hot_dropout_desc(x.shape[1], x.shape[2], int(offset), float(keep), x.shape[0], kind)
+    dev = x.device.index
+    with _on(dev):
+        code = lib().hot_dropout(ctypes.byref(d), _rng_ref(rng), x.data_ptr(), y.data_ptr(), _stream(dev))
+    _check_planless(code, "hot_dropout")
+
+
+def _block_desc(x, branch, vectors: dict, norm, branch_norm, scale: float, keep: float, offset: int, eps: float) -> hot_block_desc:
+    """x and branch [samples, rows, width]; vectors: {name: [width], [samples, width] or None}, all of one type."""
+    kind = _typed(x, "x")
+    if x.dim() != 3 or x.shape[2] < 1 or not x.is_contiguous():
+        raise ValueError(f"x: need a contiguous [samples, rows, width], got {tuple(x.shape)} strides {x.stride()}")
+    _dense(branch, x.shape, x.dtype, x, "branch")
+    samples, rows, width = x.shape
+    vector_kind = None
+    pitch = {}
+    for name, t in vectors.items():
+        pitch[name] = 0
+        if t is None:
+            continue
+        this = _typed(t, name, x)
+        if this not in (kind, 0) or vector_kind not in (None, this):
+            raise TypeError(f"{name}: the vectors need one type, x's or float32")
+        vector_kind = this
+        if tuple(t.shape) not in ((width,), (samples, width)) or not t.is_contiguous():
+            raise ValueError(f"{name}: need a contiguous [{width}] or [{samples}, {width}], got {tuple(t.shape)} strides {t.stride()}")
+        pitch[name] = width if t.dim() == 2 else 0
+    return hot_block_desc(rows, width, pitch["weight"], pitch["bias"], pitch["gate"], pitch["branch_weight"], pitch["branch_bias"], int(offset),
+                          float(scale), float(keep), float(eps), samples, kind, kind if vector_kind is None else vector_kind, HOT_NORMS[norm],
+                          HOT_NORMS[branch_norm], 0)
+
+
+_VECTORS = ("weight", "bias", "gate", "branch_weight", "branch_bias")
+
+
+def hot_block_forward(x, branch, h, y=None, *, weight=None, bias=None, gate=None, branch_weight=None, branch_bias=None, norm="layer", branch_norm=None,
+                      scale: float = 1.0, keep: float = 1.0, rng=None, offset: int = 0, eps: float = 1e-5, stats=None) -> None:
+    """h = x + scale gate dropout(norm'(branch)), y = norm(h) (None without a norm); see include/hot.h.  stats: float32 [samples, rows, 4] or None."""
+    d = _block_desc(x, branch, dict(zip(_VECTORS, (weight, bias, gate, branch_weight, branch_bias))), norm, branch_norm, scale, keep, offset, eps)
+    _dense(h, x.shape, x.dtype, x, "h")
+    _dense(y, x.shape, x.dtype, x, "y")
+    _dense(stats, (*x.shape[:2], 4), torch.float32, x, "stats")
+    dev = x.device.index
+    with _on(dev):
+        code = lib().hot_block_forward(ctypes.byref(d), _rng_ref(rng), x.data_ptr(), branch.data_ptr(), _ptr(weight), _ptr(bias), _ptr(gate), _ptr(branch_weight),
+                                       _ptr(branch_bias), h.data_ptr(), _ptr(y), _ptr(stats), _stream(dev))
+    _check_planless(code, "hot_block_forward")
+
+
+def hot_block_backward(x, branch, stats, dh, dy, dx=None, dbranch=None, grads=None, *, weight=None, bias=None, gate=None, branch_weight=None, branch_bias=None,
+                       norm="layer", branch_norm=None, scale: float = 1.0, keep: float = 1.0, rng=None, offset: int = 0, eps: float = 1e-5, workspace=None) -> None:
+    """Gradients of hot_block_forward's arguments; dh or dy may be None (zeros), each result too (left out).  grads: {name of a vector: where its gradient
+    goes}, of the vector's shape and type.  workspace: scratch of hot_block_backward_workspace_bytes, allocated here where it is None."""
+    vectors = dict(zip(_VECTORS, (weight, bias, gate, branch_weight, branch_bias)))
+    d = _block_desc(x, branch, vectors, norm, branch_norm, scale, keep, offset, eps)
+    grads = grads or {}
+    for t, name in ((dh, "dh"), (dy, "dy"), (dx, "dx"), (dbranch, "dbranch")):
+        _dense(t, x.shape, x.dtype, x, name)
+    _dense(stats, (*x.shape[:2], 4), torch.float32, x, "stats")
+    for name, t in grads.items():
+        if vectors[name] is None:
+            raise ValueError(f"{name}: there is none, so it has no gradient")
+        _dense(t, vectors[name].shape, vectors[name].dtype, x, "gradient of " + name)
+    if workspace is None and any(t is not None for t in grads.values()):
+        n = lib().hot_block_backward_workspace_bytes(ctypes.byref(d))
+        if n < 0:
+            _check_planless(int(n), "hot_block_backward_workspace_bytes")
+        workspace = torch.empty(int(n), dtype=torch.uint8, device=x.device)
+    ws, ws_bytes = _scratch_of(workspace, x)
+    dev = x.device.index
+    with _on(dev):
+        code = lib().hot_block_backward(ctypes.byref(d), _rng_ref(rng), x.data_ptr(), branch.data_ptr(), _ptr(weight), _ptr(gate), _ptr(branch_weight), _ptr(branch_bias),
+                                        stats.data_ptr(), _ptr(dh), _ptr(dy), _ptr(dx), _ptr(dbranch), *(_ptr(grads.get(n)) for n in _VECTORS), ws, ws_bytes, _stream(dev))
+    _check_planless(code, "hot_block_backward")
+
+
+def _heads_of(t, name: str, like=None) -> hot_pitch:
+    if like is not None and (_typed(t, name, like) != HOT_TYPES[like.dtype]):
+        raise TypeError(f"{name}: need q's type")
+    if t.dim() != 4 or (t.shape[3] > 1 and t.stride(3) != 1):
+        raise ValueError(f"{name}: need [batch, heads, tokens, width] with adjacent elements, got {tuple(t.shape)} strides {t.stride()}")
+    return hot_pitch(_pitch(t, 0), _pitch(t, 1), _pitch(t, 2))
+
+
+def _whole(t, shape, like, name: str):
+    if t is not None:
+        _dense(t, shape, torch.int32, like, name)
+    return _ptr(t)
+
+
+def _attention_desc(q, k, v, o, table, positions, scale, causal, query_groups, key_groups, first_query, grads=(None,) * 4):
+    """The description of a call and its pointers up to key_groups.  positions: (query_code, key_code, key_range, bucket) or None."""
+    kind = _typed(q, "q")
+    d = hot_attention_desc()
+    d.q, d.k, d.v = _heads_of(q, "q"), _heads_of(k, "k", q), _heads_of(v, "v", q)
+    batch, heads, queries, width = q.shape
+    if k.shape != v.shape or k.shape[0] != batch or k.shape[3] != width or k.shape[1] < 1 or heads % k.shape[1]:
+        raise ValueError(f"k and v: need [{batch}, kv heads, keys, {width}] with kv heads dividing {heads}, got {tuple(k.shape)} and {tuple(v.shape)}")
+    for t, name, like in ((o, "o", q), (grads[0], "grad_o", q), (grads[1], "grad_q", q), (grads[2], "grad_k", k), (grads[3], "grad_v", v)):
+        if t is not None:
+            setattr(d, name, _heads_of(t, name, q))
+            if t.shape != like.shape:
+                raise ValueError(f"{name}: need {tuple(like.shape)}, got {tuple(t.shape)}")
+    keys = k.shape[2]
+    d.queries, d.keys, d.batch, d.heads, d.kv_heads, d.width, d.scale, d.causal, d.dtype = queries, keys, batch, heads, k.shape[1], width, scale, bool(causal), kind
+    pointers = [q.data_ptr(), k.data_ptr(), v.data_ptr()] + [None] * 5
+    if table is not None:
+        query_code, key_code, key_range, bucket = positions
+        if table.dim() != 3 or table.shape[2] != heads or not table.is_contiguous():
+            raise ValueError(f"table: need a contiguous [tables, buckets, {heads}], got {tuple(table.shape)} strides {table.stride()}")
+        if query_code.shape[0] < first_query + queries or key_code.shape[0] < keys or key_range.shape[0] < (keys + 63) // 64 or first_query < 0:
+            raise ValueError(f"positions: need codes of {first_query + queries} queries and {keys} keys")
+        d.tables, d.buckets, d.codes, d.first_query, d.table_dtype = table.shape[0], table.shape[1], bucket.shape[0], first_query, _typed(table, "table", q)
+        pointers[3:] = [table.data_ptr(), _whole(query_code, query_code.shape[:1], q, "query_code"), _whole(key_code, key_code.shape[:1], q, "key_code"),
+                        _whole(key_range, (key_range.shape[0], 2), q, "key_range"), _whole(bucket, bucket.shape[:1], q, "bucket")]
+    if (query_groups is None) != (key_groups is None):
+        raise ValueError("query_groups and key_groups: need both or neither")
+    if query_groups is not None:
+        d.groups = query_groups.shape[0]
+        if d.groups < 1:
+            raise ValueError("query_groups: need at least one row")
+    return d, pointers + [_whole(query_groups, (d.groups, queries), q, "query_groups"), _whole(key_groups, (d.groups, keys), q, "key_groups")]
+
+
+def _attention_workspace(d: hot_attention_desc, which: int, like):
+    n = lib().hot_attention_workspace_bytes(ctypes.byref(d), which)
+    if n < 0:
+        _check_planless(int(n), "hot_attention_workspace_bytes")
+    return torch.empty(int(n), dtype=torch.uint8, device=like.device)
+
+
+def hot_attention_forward(q, k, v, o, table=None, positions=None, *, scale: float, causal: bool = False, query_groups=None, key_groups=None, first_query: int = 0,
+                          rest=None, stats=None, workspace=None) -> None:
+    """o [batch, heads, queries, width] of attention with a position bias (see include/hot.h); table [tables, buckets, heads] or None; positions:
+    (query_code, key_code, key_range, bucket), int32.  rest (o's layout), stats (float32 [batch, heads, queries, 2]): for the backward call, or None."""
+    d, pointers = _attention_desc(q, k, v, o, table, positions, scale, causal, query_groups, key_groups, first_query)
+    if rest is not None and (rest.shape != o.shape or rest.stride() != o.stride() or rest.dtype != o.dtype):
+        raise ValueError("rest: need o's shape, strides and type")
+    _dense(stats, (*q.shape[:3], 2), torch.float32, q, "stats")
+    ws, ws_bytes = _scratch_of(workspace if workspace is not None else _attention_workspace(d, 0, q), q)
+    dev = q.device.index
+    with _on(dev):
+        code = lib().hot_attention_forward(ctypes.byref(d), *pointers, o.data_ptr(), _ptr(rest), _ptr(stats), ws, ws_bytes, _stream(dev))
+    _check_planless(code, "hot_attention_forward")
+
+
+def hot_attention_backward(q, k, v, o, grad_o, stats, rest=None, table=None, positions=None, *, scale: float, causal: bool = False, query_groups=None, key_groups=None,
+                           first_query: int = 0, grad_q=None, grad_k=None, grad_v=None, grad_table=None, workspace=None) -> None:
+    """Gradients of hot_attention_forward's q, k, v and table; each may be None and is then left out."""
+    d, pointers = _attention_desc(q, k, v, o, table, positions, scale, causal, query_groups, key_groups, first_query, (grad_o, grad_q, grad_k, grad_v))
+    if rest is not None and (rest.shape != o.shape or rest.stride() != o.stride() or rest.dtype != o.dtype):
+        raise ValueError("rest: need o's shape, strides and type")
+    _dense(stats, (*q.shape[:3], 2), torch.float32, q, "stats")
+    if grad_table is not None:
+        if table is None:
+            raise ValueError("grad_table: there is no table")
+        _dense(grad_table, table.shape, table.dtype, q, "grad_table")
+    ws, ws_bytes = _scratch_of(workspace if workspace is not None else _attention_workspace(d, 1, q), q)
+    dev = q.device.index
+    with _on(dev):
+        code = lib().hot_attention_backward(ctypes.byref(d), *pointers, o.data_ptr(), _ptr(rest), stats.data_ptr(), grad_o.data_ptr(), _ptr(grad_q), _ptr(grad_k),
+                                            _ptr(grad_v), _ptr(grad_table), ws, ws_bytes, _stream(dev))
+    _check_planless(code, "hot_attention_backward")
+
+
+def hot_block_backward_workspace_bytes(x, branch, *, weight=None, bias=None, gate=None, branch_weight=None, branch_bias=None, norm="layer", branch_norm=None) -> int:
+    """Bytes of scratch that hot_block_backward asks for where it forms gradients of vectors."""
+    d = _block_desc(x, branch, dict(zip(_VECTORS, (weight, bias, gate, branch_weight, branch_bias))), norm, branch_norm, 1.0, 1.0, 0, 0.0)
+    n = lib().hot_block_backward_workspace_bytes(ctypes.byref(d))
+    if n < 0:
+        _check_planless(int(n), "hot_block_backward_workspace_bytes")
+    return int(n)

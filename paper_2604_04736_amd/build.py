@@ -8,7 +8,8 @@ from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SRCS = [os.path.join(HERE, "csrc", name) for name in ("forward.hip", "backward.hip", "hot.hip", "stats.hip", "linear.hip", "update.hip", "norm.hip", "head.hip")]
+SRCS = [os.path.join(HERE, "csrc", name) for name in ("forward.hip", "backward.hip", "hot.hip", "stats.hip", "linear.hip", "update.hip", "norm.hip", "head.hip", "block.hip",
+                                                      "attention.hip", "attention_f32.hip", "attention_bf16.hip", "attention_f16.hip")]
 LIB = os.path.join(HERE, "libhot.so")
 HOST_LIB = os.path.join(HERE, "_hot_host.so")
 OBJ_DIR = os.path.join(HERE, "_build")

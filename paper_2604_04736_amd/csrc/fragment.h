@@ -1,0 +1,145 @@
+// Blocks of 16 x 16 results of the matrix instruction, for the kernels of attention.h, and their operands out of LDS.
+//
+// An instruction contracts 32 indices: lane l brings line l % 16 of its operand at indices 8 (l / 16) .. + 7, and receives results (4 (l / 16) + i, l % 16),
+// i = 0 .. 3, the second index being B's line.  Two blocks of results, one below the other, thus leave eight rows of one column in a lane, which is the
+// form of an operand that contracts those 32 rows, if the other operand takes them in the same order: index 8 g + i is row 4 g + i of the upper block (i < 4)
+// or 4 g + i - 4 of the lower.  So the softmax's results go from one product into the next without leaving their lanes.
+// float32 is multiplied by the instruction of its own, four indices at a time, on the same operands.
+#ifndef HOT_FRAGMENT_H
+#define HOT_FRAGMENT_H
+
+#include <hip/hip_runtime.h>
+
+#include "vec.h"
+
+namespace {
+
+template <class T>
+struct Eight {
+    typedef T V __attribute__((ext_vector_type(8)));
+};
+template <class T>
+using V8 = typename Eight<T>::V;
+
+typedef short s4v __attribute__((ext_vector_type(4)));
+typedef short s8v __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) char lds_char;
+typedef __attribute__((address_space(3))) s4v lds_s4v;
+
+// The wait states between a run of matrix instructions and the first read of their results: 32, which the scheduler may not move
+// (the compiler's own can be missing where a branch lies between).  Blocks hand their registers out only against one of these.
+struct Settled {
+    __device__ __forceinline__ Settled()
+    {
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    Settled(const Settled &) = delete;
+    Settled &operator=(const Settled &) = delete;
+};
+
+template <class T>
+class Block16 {
+    f4 v_;
+
+public:
+    __device__ __forceinline__ Block16() : v_(0.0f) {}
+    __device__ __forceinline__ void mac(V8<T> a, V8<T> b)
+    {
+        if constexpr (__is_same(T, float)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v_ = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], v_, 0, 0, 0);
+        } else if constexpr (__is_same(T, _Float16)) v_ = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, v_, 0, 0, 0);
+        else v_ = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, v_, 0, 0, 0);
+    }
+    __device__ __forceinline__ f4 read(const Settled &) const { return v_; }
+    __device__ __forceinline__ void scale(const Settled &, float by)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v_[i] *= by;
+    }
+};
+
+// Eight results as an operand: as they are for float32, in two pieces for 16-bit types (bf16: 2^-17 of each is left over; fp16: 2^-23, or half a step of 2^-24)
+template <class T>
+struct Pieces {
+    static constexpr int N = __is_same(T, float) ? 1 : 2;
+    V8<T> p[N];
+
+    __device__ __forceinline__ void set(int i, float x)
+    {
+        if constexpr (N == 1) p[0][i] = x;
+        else {
+            p[0][i] = (T)x;
+            p[1][i] = (T)(x - (float)p[0][i]);
+        }
+    }
+    // c += a (the pieces)
+    __device__ __forceinline__ void mac(Block16<T> &c, V8<T> a) const
+    {
+#pragma unroll
+        for (int k = N - 1; k >= 0; --k) c.mac(a, p[k]);
+    }
+};
+
+// A tile of rows of DP elements in LDS.  Rows are sixteen bytes longer than their elements, so that sixteen of them read at once are in different banks.
+template <class T, int DP>
+struct Rows {
+    static constexpr int kPitch = DP * (int)sizeof(T) + 16;
+
+    // operand of lines row0 .. + 15 at elements 32 ks ..
+    static __device__ __forceinline__ V8<T> along(const char *tile, int row0, int ks, int lane)
+    {
+        const char *const at = tile + (row0 + (lane & 15)) * kPitch + (ks * 32 + (lane >> 4) * 8) * (int)sizeof(T);
+        return *reinterpret_cast<const V8<T> *>(at);
+    }
+    // operand whose lines are elements e0 .. + 15 and whose 32 indices are rows row0 .. + 31, in the order above
+    static __device__ __forceinline__ V8<T> across(const char *tile, int row0, int e0, int lane)
+    {
+        const int g = lane >> 4, i = lane & 15;
+        if constexpr (sizeof(T) == 2) {
+            // (a transposing read: of four rows of sixteen elements that sixteen lanes name, lane i receives element i of each)
+            lds_char *const at = (lds_char *)(tile + (row0 + 4 * g + (i >> 2)) * kPitch + (e0 + (i & 3) * 4) * 2);
+            const s4v up = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v *)at);
+            const s4v low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v *)(at + 16 * kPitch));
+            return __builtin_bit_cast(V8<T>, __builtin_shufflevector(up, low, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            V8<T> v;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = *reinterpret_cast<const T *>(tile + (row0 + 4 * g + (j & 3) + (j >> 2) * 16) * kPitch + (e0 + i) * (int)sizeof(T));
+            return v;
+        }
+    }
+};
+
+// Eight neighbouring elements of a row of n in memory, zeros behind its end, on any element's address
+template <class T>
+__device__ __forceinline__ V8<T> eight(const T *row, int at, int n)
+{
+    typedef V8<T> Loose __attribute__((aligned(sizeof(T))));
+    if (at + 8 <= n) return *reinterpret_cast<const Loose *>(row + at);
+    V8<T> v;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = at + j < n ? row[at + j] : (T)0.0f;
+    return v;
+}
+
+// Four results to a row of n elements
+template <class T>
+__device__ __forceinline__ void four(T *row, int at, int n, f4 v)
+{
+    typedef T F __attribute__((ext_vector_type(4)));
+    typedef F Loose __attribute__((aligned(sizeof(T))));
+    if (at + 4 <= n) {
+        *reinterpret_cast<Loose *>(row + at) = __builtin_convertvector(v, F);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (at + j < n) row[at + j] = (T)v[j];
+}
+
+}  // namespace
+
+#endif  // HOT_FRAGMENT_H

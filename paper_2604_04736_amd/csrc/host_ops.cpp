@@ -5,6 +5,7 @@
 #include <torch/csrc/utils/pybind.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/functions/basic_ops.h>
@@ -376,10 +377,399 @@ py::object head_loss(const Tensor &x, const Tensor &weight, const MaybeTensor &m
     return py::cast(loss);
 }
 
+// ---------------------------------------------------------------------------------
+// Dropout, a block's end and attention: every call goes this way, dense or not, with the checks that name what is wrong.
+
+#define HOT_NEED(condition, ...) TORCH_CHECK_VALUE(condition, __VA_ARGS__)
+
+void on_gpu(const Tensor &t, const char *name, const Tensor &like)
+{
+    TORCH_CHECK_TYPE(t.is_cuda() && t.layout() == at::kStrided && t.has_storage() && !t.key_set().has(c10::DispatchKey::Python), name,
+                     ": need a float32, bfloat16 or float16 tensor on a GPU");
+    TORCH_CHECK_TYPE(t.device() == like.device(), name, ": need a tensor on ", like.device());
+}
+
+void elements(const Tensor &t, const char *name, const Tensor &like)
+{
+    TORCH_CHECK_TYPE(type_of(t) >= 0, name, ": need a float32, bfloat16 or float16 tensor on a GPU");
+    on_gpu(t, name, like);
+}
+
+struct Counter {
+    hot_rng rng;
+    int64_t samples, offset;
+    double keep;
+};
+
+// samples = 0: all rows are of one sample
+int64_t samples_of(const Tensor &x, const char *name, int64_t samples)
+{
+    HOT_NEED(samples >= 0 && samples <= 65535, "samples: need 0 to 65535, got ", samples);
+    HOT_NEED(x.dim() >= (samples ? 2 : 1) && x.size(-1) >= 1, name, ": need [", samples ? "samples, " : "", "..., width] with a width, got ", x.sizes());
+    HOT_NEED(!samples || x.size(0) == samples, name, ": need ", samples, " samples in front, got ", x.sizes());
+    return samples ? samples : 1;
+}
+
+hot_rng counter_rng(uint64_t seed, int64_t step, int64_t first_sample, int64_t samples)
+{
+    HOT_NEED(step >= 0 && step <= UINT32_MAX, "rng: need a step below 2^32, got ", step);
+    HOT_NEED(first_sample >= 0 && first_sample + samples <= (int64_t(1) << 32), "rng: need samples below 2^32, got ", first_sample, " and ", samples, " from there on");
+    hot_rng r = {};
+    r.seed = seed;
+    r.step = (uint32_t)step;
+    r.first_sample = (uint32_t)first_sample;
+    return r;
+}
+
+void check_keep(double keep, int64_t offset)
+{
+    HOT_NEED(keep > 0.0 && keep <= 1.0, "keep: need 0 < keep <= 1, got ", keep);
+    HOT_NEED(offset >= 0, "offset: need at least 0, got ", offset);
+}
+
+struct Dropout : torch::autograd::Function<Dropout> {
+    static Tensor forward(AutogradContext *ctx, const Tensor &x, double keep, int64_t seed, int64_t step, int64_t first_sample, int64_t samples, int64_t offset)
+    {
+        const c10::DeviceGuard guard(x.device());
+        const int64_t sets = samples ? samples : 1, width = x.size(-1);
+        const Tensor from = x.resolve_neg().contiguous(), y = at::empty(x.sizes(), from.options());
+        hot_dropout_desc d = {};
+        d.width = width;
+        d.rows = x.numel() / width / sets;
+        d.offset = offset;
+        d.keep = keep;
+        d.samples = (int32_t)sets;
+        d.dtype = type_of(x);
+        const hot_rng rng = counter_rng((uint64_t)seed, step, first_sample, sets);
+        check(hot_dropout(&d, &rng, raw(from), raw_mut(y), stream_of(x)), "hot_dropout");
+        ctx->saved_data["keep"] = keep;
+        ctx->saved_data["counter"] = std::vector<int64_t>{seed, step, first_sample, samples, offset};
+        return y;
+    }
+
+    // (its own gradient, as often as it is asked for)
+    static variable_list backward(AutogradContext *ctx, variable_list grads)
+    {
+        const auto c = ctx->saved_data["counter"].toIntVector();
+        return {grads[0].defined() ? apply(grads[0], ctx->saved_data["keep"].toDouble(), c[0], c[1], c[2], c[3], c[4]) : Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor()};
+    }
+};
+
+Tensor dropout(const Tensor &x, double keep, uint64_t seed, int64_t step, int64_t first_sample, int64_t samples, int64_t offset)
+{
+    elements(x, "x", x);
+    const int64_t sets = samples_of(x, "x", samples);
+    check_keep(keep, offset);
+    counter_rng(seed, step, first_sample, sets);
+    py::gil_scoped_release others_run;
+    return Dropout::apply(x, keep, (int64_t)seed, step, first_sample, samples, offset);
+}
+
+// What a block's call is described by, beside its tensors
+struct BlockRule {
+    std::vector<int64_t> whole;      // norm, branch_norm, seed, step, first_sample, samples, offset
+    double scale, keep, eps;
+};
+
+int64_t own_pitch(const Tensor &v) { return v.defined() && v.dim() == 2 ? v.size(1) : 0; }
+
+hot_block_desc block_desc(const Tensor &x, const Tensor (&v)[5], const BlockRule &r, hot_rng &rng)
+{
+    hot_block_desc d = {};
+    const int64_t sets = r.whole[5] ? r.whole[5] : 1;
+    d.width = x.size(-1);
+    d.rows = x.numel() / d.width / sets;
+    d.weight_sample = own_pitch(v[0]);
+    d.bias_sample = own_pitch(v[1]);
+    d.gate_sample = own_pitch(v[2]);
+    d.branch_weight_sample = own_pitch(v[3]);
+    d.branch_bias_sample = own_pitch(v[4]);
+    d.offset = r.whole[6];
+    d.scale = r.scale;
+    d.keep = r.keep;
+    d.eps = r.eps;
+    d.samples = (int32_t)sets;
+    d.dtype = type_of(x);
+    d.vector_dtype = d.dtype;
+    for (const Tensor &t : v)
+        if (t.defined()) d.vector_dtype = type_of(t);
+    d.norm = (int32_t)r.whole[0];
+    d.branch_norm = (int32_t)r.whole[1];
+    rng = counter_rng((uint64_t)r.whole[2], r.whole[3], r.whole[4], sets);
+    return d;
+}
+
+struct BlockEnd : torch::autograd::Function<BlockEnd> {
+    static variable_list forward(AutogradContext *ctx, const Tensor &x, const Tensor &branch, const MaybeTensor &weight, const MaybeTensor &bias, const MaybeTensor &gate,
+                                 const MaybeTensor &branch_weight, const MaybeTensor &branch_bias, std::vector<int64_t> whole, double scale, double keep, double eps)
+    {
+        const c10::DeviceGuard guard(x.device());
+        const BlockRule rule = {whole, scale, keep, eps};
+        const Tensor xs = x.resolve_neg().contiguous(), bs = branch.resolve_neg().contiguous();
+        Tensor v[5] = {given(weight), given(bias), given(gate), given(branch_weight), given(branch_bias)};
+        bool wanted = x.requires_grad() || branch.requires_grad();
+        for (Tensor &t : v)
+            if (t.defined()) {
+                wanted = wanted || t.requires_grad();
+                t = t.resolve_neg().contiguous();
+            }
+        hot_rng rng;
+        const hot_block_desc d = block_desc(xs, v, rule, rng);
+        const Tensor h = at::empty(x.sizes(), xs.options()), y = d.norm != HOT_NORM_NONE ? at::empty(x.sizes(), xs.options()) : Tensor();
+        const Tensor stats = wanted ? at::empty({d.samples, d.rows, 4}, xs.options().dtype(at::kFloat)) : Tensor();
+        check(hot_block_forward(&d, &rng, raw(xs), raw(bs), raw(v[0]), raw(v[1]), raw(v[2]), raw(v[3]), raw(v[4]), raw_mut(h), raw_mut(y),
+                                stats.defined() ? stats.mutable_data_ptr<float>() : nullptr, stream_of(x)),
+              "hot_block_forward");
+        if (wanted) {
+            ctx->set_materialize_grads(false);
+            ctx->save_for_backward({xs, bs, v[0], v[1], v[2], v[3], v[4], stats});
+            ctx->saved_data["whole"] = whole;
+            ctx->saved_data["real"] = std::vector<double>{scale, keep, eps};
+        }
+        if (y.defined()) return {h, y};
+        return {h};
+    }
+
+    static variable_list backward(AutogradContext *ctx, variable_list grads)
+    {
+        const variable_list saved = ctx->get_saved_variables();
+        const Tensor &x = saved[0], &branch = saved[1], &stats = saved[7];
+        const c10::DeviceGuard guard(x.device());
+        const Tensor v[5] = {saved[2], saved[3], saved[4], saved[5], saved[6]};
+        const auto real = ctx->saved_data["real"].toDoubleVector();
+        const BlockRule rule = {ctx->saved_data["whole"].toIntVector(), real[0], real[1], real[2]};
+        hot_rng rng;
+        const hot_block_desc d = block_desc(x, v, rule, rng);
+        const Tensor dh = grads[0].defined() ? grads[0].resolve_neg().contiguous() : Tensor();
+        const Tensor dy = grads.size() > 1 && grads[1].defined() ? grads[1].resolve_neg().contiguous() : Tensor();
+        if (!dh.defined() && !dy.defined()) return variable_list(11);
+        size_t input = 0;        // (inputs that are not there are not counted)
+        const Tensor dx = gradient_of(ctx, x, input), dbranch = gradient_of(ctx, branch, input);
+        Tensor dv[5];
+        bool sums = false;
+        for (int k = 0; k < 5; ++k) {
+            dv[k] = gradient_of(ctx, v[k], input);
+            sums = sums || dv[k].defined();
+        }
+        const int64_t bytes = sums ? hot_block_backward_workspace_bytes(&d) : 0;
+        const Tensor ws = bytes > 0 ? at::empty({bytes}, x.options().dtype(at::kByte)) : Tensor();
+        check(hot_block_backward(&d, &rng, raw(x), raw(branch), raw(v[0]), raw(v[2]), raw(v[3]), raw(v[4]), stats.const_data_ptr<float>(), raw(dh), raw(dy), raw_mut(dx),
+                                 raw_mut(dbranch), raw_mut(dv[0]), raw_mut(dv[1]), raw_mut(dv[2]), raw_mut(dv[3]), raw_mut(dv[4]), raw_mut(ws), bytes, stream_of(x)),
+              "hot_block_backward");
+        return once({dx, dbranch, dv[0], dv[1], dv[2], dv[3], dv[4], Tensor(), Tensor(), Tensor(), Tensor()}, "residual_norm");
+    }
+};
+
+// (h, y), or (h,) without a norm
+std::vector<Tensor> block_end(const Tensor &x, const Tensor &branch, const MaybeTensor &weight, const MaybeTensor &bias, const MaybeTensor &gate, const MaybeTensor &branch_weight,
+                              const MaybeTensor &branch_bias, int64_t norm, int64_t branch_norm, double scale, double keep, double eps, uint64_t seed, int64_t step,
+                              int64_t first_sample, int64_t samples, int64_t offset)
+{
+    elements(x, "x", x);
+    elements(branch, "branch", x);
+    const int64_t sets = samples_of(x, "x", samples), width = x.size(-1);
+    HOT_NEED(width <= HOT_BLOCK_MOST_WIDTH, "x: need a width of at most ", HOT_BLOCK_MOST_WIDTH, ", got ", width);
+    TORCH_CHECK_TYPE(branch.scalar_type() == x.scalar_type(), "branch: need x's type");
+    HOT_NEED(branch.sizes() == x.sizes(), "branch: need x's shape ", x.sizes(), ", got ", branch.sizes());
+    check_keep(keep, offset);
+    HOT_NEED(eps >= 0.0 && eps <= 3.0e38, "eps: need at least 0, got ", eps);
+    HOT_NEED(scale >= -3.0e38 && scale <= 3.0e38, "scale: need a finite number, got ", scale);
+    const char *const names[5] = {"weight", "bias", "gate", "branch_weight", "branch_bias"};
+    const Tensor v[5] = {given(weight), given(bias), given(gate), given(branch_weight), given(branch_bias)};
+    at::ScalarType type = at::ScalarType::Undefined;
+    for (int k = 0; k < 5; ++k) {
+        if (!v[k].defined()) continue;
+        elements(v[k], names[k], x);
+        HOT_NEED(k == 2 || (k < 2 ? norm : branch_norm) != HOT_NORM_NONE, names[k], ": there is no norm that it belongs to");
+        TORCH_CHECK_TYPE((v[k].scalar_type() == x.scalar_type() || v[k].scalar_type() == at::kFloat) && (type == at::ScalarType::Undefined || v[k].scalar_type() == type), names[k],
+                         ": the vectors need one type, x's or float32");
+        type = v[k].scalar_type();
+        HOT_NEED((v[k].dim() == 1 || (v[k].dim() == 2 && samples && v[k].size(0) == samples)) && v[k].size(-1) == width, names[k], ": need [", width, "] or [samples, ", width,
+                 "], got ", v[k].sizes());
+    }
+    counter_rng(seed, step, first_sample, sets);
+    py::gil_scoped_release others_run;
+    return BlockEnd::apply(x, branch, weight, bias, gate, branch_weight, branch_bias, std::vector<int64_t>{norm, branch_norm, (int64_t)seed, step, first_sample, samples, offset},
+                           scale, keep, eps);
+}
+
+// [..., heads, tokens, width] as [batch, heads, tokens, width] with adjacent elements: a view, or a copy where the leading axes are no single one
+Tensor four_axes(const Tensor &t)
+{
+    Tensor u = t.resolve_neg();
+    if (u.size(-1) > 1 && u.stride(-1) != 1) u = u.contiguous();
+    return u.dim() == 4 ? u : (u.dim() == 3 ? u.unsqueeze(0) : u.flatten(0, -4));
+}
+
+hot_pitch pitch_of(const Tensor &t)
+{
+    const auto of = [&](int64_t i) { return t.size(i) > 1 ? t.stride(i) : 0; };
+    return {of(0), of(1), of(2)};
+}
+
+// Heads side by side in a token's row, as the products around attention have them
+Tensor token_major(const Tensor &like) { return at::empty({like.size(0), like.size(2), like.size(1), like.size(3)}, like.options()).transpose(1, 2); }
+
+Tensor room_like(const Tensor &t) { return t.is_non_overlapping_and_dense() && (t.size(-1) < 2 || t.stride(-1) == 1) ? at::empty_like(t) : token_major(t); }
+
+hot_attention_desc attention_desc(const Tensor &q, const Tensor &k, const Tensor &v, const Tensor &table, const Tensor &bucket, const Tensor &query_groups, int64_t first_query,
+                                  double scale, bool causal)
+{
+    hot_attention_desc d = {};
+    d.queries = q.size(2);
+    d.keys = k.size(2);
+    d.q = pitch_of(q);
+    d.k = pitch_of(k);
+    d.v = pitch_of(v);
+    d.scale = scale;
+    d.batch = (int32_t)q.size(0);
+    d.heads = (int32_t)q.size(1);
+    d.kv_heads = (int32_t)k.size(1);
+    d.width = (int32_t)q.size(3);
+    if (table.defined()) {
+        d.tables = (int32_t)(table.dim() == 3 ? table.size(0) : 1);
+        d.buckets = (int32_t)table.size(-2);
+        d.codes = (int32_t)bucket.size(0);
+        d.first_query = (int32_t)first_query;
+        d.table_dtype = type_of(table);
+    }
+    d.groups = query_groups.defined() ? (int32_t)query_groups.size(0) : 0;
+    d.causal = causal;
+    d.dtype = type_of(q);
+    return d;
+}
+
+const int32_t *codes(const Tensor &t) { return t.defined() ? t.const_data_ptr<int32_t>() : nullptr; }
+
+Tensor attention_room(const hot_attention_desc &d, int which, const Tensor &like)
+{
+    const int64_t bytes = hot_attention_workspace_bytes(&d, which);
+    TORCH_CHECK(bytes >= 0, "hot_attention_workspace_bytes: ", hot_strerror((int)bytes), " (code ", bytes, ")");
+    return at::empty({bytes}, like.options().dtype(at::kByte));
+}
+
+struct Attention : torch::autograd::Function<Attention> {
+    static Tensor forward(AutogradContext *ctx, const Tensor &q_, const Tensor &k_, const Tensor &v_, const MaybeTensor &maybe_table, const MaybeTensor &query_code,
+                          const MaybeTensor &key_code, const MaybeTensor &key_range, const MaybeTensor &bucket, const MaybeTensor &query_groups, const MaybeTensor &key_groups,
+                          int64_t first_query, double scale, bool causal)
+    {
+        const c10::DeviceGuard guard(q_.device());
+        const Tensor q = four_axes(q_), k = four_axes(k_), v = four_axes(v_);
+        const Tensor table = maybe_table ? maybe_table->resolve_neg().contiguous() : Tensor(), qg = given(query_groups), kg = given(key_groups);
+        hot_attention_desc d = attention_desc(q, k, v, table, given(bucket), qg, first_query, scale, causal);
+        const Tensor o = token_major(q);
+        d.o = pitch_of(o);
+        const bool keep = q_.requires_grad() || k_.requires_grad() || v_.requires_grad() || (maybe_table && maybe_table->requires_grad());
+        const Tensor stats = keep ? at::empty({q.size(0), q.size(1), q.size(2), 2}, q.options().dtype(at::kFloat)) : Tensor();
+        const Tensor rest = keep && d.dtype != HOT_F32 ? token_major(q) : Tensor();
+        const Tensor ws = attention_room(d, 0, q);
+        check(hot_attention_forward(&d, raw(q), raw(k), raw(v), raw(table), codes(given(query_code)), codes(given(key_code)), codes(given(key_range)), codes(given(bucket)), codes(qg),
+                                    codes(kg), raw_mut(o), raw_mut(rest), stats.defined() ? stats.mutable_data_ptr<float>() : nullptr, raw_mut(ws), ws.numel(), stream_of(q)),
+              "hot_attention_forward");
+        if (keep) {
+            ctx->save_for_backward({q, k, v, table, given(query_code), given(key_code), given(key_range), given(bucket), qg, kg, o, rest, stats});
+            ctx->saved_data["whole"] = std::vector<int64_t>{first_query, causal};
+            ctx->saved_data["scale"] = scale;
+            ctx->saved_data["q"] = q_.sizes().vec();
+            ctx->saved_data["k"] = k_.sizes().vec();
+        }
+        return o.reshape(q_.sizes());
+    }
+
+    static variable_list backward(AutogradContext *ctx, variable_list grads)
+    {
+        variable_list none(13);
+        if (!grads[0].defined()) return none;
+        const variable_list s = ctx->get_saved_variables();
+        const Tensor &q = s[0], &k = s[1], &v = s[2], &table = s[3], &o = s[10], &rest = s[11], &stats = s[12];
+        const c10::DeviceGuard guard(q.device());
+        const auto whole = ctx->saved_data["whole"].toIntVector();
+        const Tensor up = four_axes(grads[0]);
+        hot_attention_desc d = attention_desc(q, k, v, table, s[7], s[8], whole[0], ctx->saved_data["scale"].toDouble(), whole[1]);
+        const Tensor dq = ctx->needs_input_grad(0) ? room_like(q) : Tensor(), dk = ctx->needs_input_grad(1) ? room_like(k) : Tensor(), dv = ctx->needs_input_grad(2) ? room_like(v) : Tensor();
+        const Tensor dtable = table.defined() && ctx->needs_input_grad(3) ? at::empty_like(table) : Tensor();
+        d.o = pitch_of(o);
+        d.grad_o = pitch_of(up);
+        if (dq.defined()) d.grad_q = pitch_of(dq);
+        if (dk.defined()) d.grad_k = pitch_of(dk);
+        if (dv.defined()) d.grad_v = pitch_of(dv);
+        const Tensor ws = attention_room(d, 1, q);
+        check(hot_attention_backward(&d, raw(q), raw(k), raw(v), raw(table), codes(s[4]), codes(s[5]), codes(s[6]), codes(s[7]), codes(s[8]), codes(s[9]), raw(o), raw(rest),
+                                     stats.const_data_ptr<float>(), raw(up), raw_mut(dq), raw_mut(dk), raw_mut(dv), raw_mut(dtable), raw_mut(ws), ws.numel(), stream_of(q)),
+              "hot_attention_backward");
+        const auto as = [&](const Tensor &t, const char *name) { return t.defined() ? t.reshape(ctx->saved_data[name].toIntVector()) : t; };
+        none[0] = as(dq, "q");
+        none[1] = as(dk, "k");
+        none[2] = as(dv, "k");
+        none[3] = dtable;
+        return once(none, "attention");
+    }
+};
+
+// Rows of group numbers as int32 [groups, n], or an error
+Tensor group_rows(const MaybeTensor &maybe, const char *name, int64_t n, const Tensor &like)
+{
+    if (!maybe) return Tensor();
+    const Tensor &t = *maybe;
+    TORCH_CHECK_TYPE(t.is_cuda() && t.device() == like.device() && t.scalar_type() == at::kInt && !t.key_set().has(c10::DispatchKey::Python), name, ": need an int32 tensor on ", like.device());
+    HOT_NEED((t.dim() == 1 || t.dim() == 2) && t.size(-1) == n && t.size(0) >= (t.dim() == 2), name, ": need [", n, "] or [entries, ", n, "], got ", t.sizes());
+    return (t.dim() == 1 ? t.unsqueeze(0) : t).contiguous();
+}
+
+Tensor attention(const Tensor &q, const Tensor &k, const Tensor &v, const MaybeTensor &table, const MaybeTensor &query_code, const MaybeTensor &key_code, const MaybeTensor &key_range,
+                 const MaybeTensor &bucket, int64_t buckets, const MaybeTensor &query_groups, const MaybeTensor &key_groups, int64_t first_query, double scale, bool causal)
+{
+    elements(q, "q", q);
+    elements(k, "k", q);
+    elements(v, "v", q);
+    TORCH_CHECK_TYPE(k.scalar_type() == q.scalar_type() && v.scalar_type() == q.scalar_type(), "k and v: need q's type");
+    const int64_t n = q.dim();
+    HOT_NEED(n >= 3 && q.size(-1) >= 1 && q.size(-1) <= HOT_ATTENTION_MOST_WIDTH && q.size(-3) >= 1, "q: need [..., heads, queries, width] with a width of 1 to ",
+             HOT_ATTENTION_MOST_WIDTH, ", got ", q.sizes());
+    HOT_NEED(k.dim() == n && k.sizes() == v.sizes() && k.size(-1) == q.size(-1) && k.sizes().slice(0, n - 3) == q.sizes().slice(0, n - 3), "k and v: need one shape, q's leading axes and width ",
+             q.sizes(), ", got ", k.sizes(), " and ", v.sizes());
+    HOT_NEED(k.size(-3) >= 1 && q.size(-3) % k.size(-3) == 0, "k and v: need a number of heads that divides ", q.size(-3), ", got ", k.size(-3));
+    HOT_NEED(scale >= -1.0e30 && scale <= 1.0e30, "scale: need a number up to 1e30, got ", scale);
+    int64_t batch = 1;
+    for (const int64_t m : q.sizes().slice(0, n - 3)) batch *= m;
+    HOT_NEED((double)batch * (double)q.size(-3) * (double)std::max<int64_t>(1, std::max(q.size(-2), k.size(-2))) < 2147483647.0 && q.size(-3) <= 65535,
+             "q: need fewer than 2^31 rows and 65536 heads, got ", q.sizes());
+    if (table) {
+        elements(*table, "table", q);
+        TORCH_CHECK_TYPE(table->scalar_type() == q.scalar_type() || table->scalar_type() == at::kFloat, "table: need q's type or float32");
+        HOT_NEED(bucket && query_code && key_code && key_range, "table: need positions");
+        HOT_NEED((table->dim() == 2 || (table->dim() == 3 && n >= 4 && table->size(0) == q.size(0) && table->size(0) >= 1 && table->size(0) <= 65535)) && table->size(-1) == q.size(-3) &&
+                     table->size(-2) == buckets,
+                 "table: need [", buckets, ", ", q.size(-3), "], or one for each of q's first axis, got ", table->sizes());
+        for (const MaybeTensor *t : {&query_code, &key_code, &key_range, &bucket})
+            TORCH_CHECK_TYPE((*t)->is_cuda() && (*t)->device() == q.device() && (*t)->scalar_type() == at::kInt && (*t)->is_contiguous(), "positions: need those of ", q.device());
+        HOT_NEED(first_query >= 0 && first_query + q.size(-2) <= query_code->size(0), "first_query: the positions know ", query_code->size(0), " queries, got ", q.size(-2), " from ",
+                 first_query, " on");
+        HOT_NEED(k.size(-2) <= key_code->size(0), "k: the positions know ", key_code->size(0), " keys, got ", k.size(-2));
+    }
+    Tensor qg = group_rows(query_groups, "query_groups", q.size(-2), q), kg = group_rows(key_groups, "key_groups", k.size(-2), q);
+    HOT_NEED(!qg.defined() || kg.defined(), "query_groups: need key_groups too");
+    if (kg.defined()) {
+        if (!qg.defined()) qg = at::zeros({1, q.size(-2)}, kg.options());
+        const int64_t rows = std::max(qg.size(0), kg.size(0));
+        HOT_NEED((qg.size(0) == rows || qg.size(0) == 1) && (kg.size(0) == rows || kg.size(0) == 1) && batch % rows == 0, "query_groups and key_groups: need as many rows, dividing ", batch,
+                 " entries, got ", qg.sizes(), " and ", kg.sizes());
+        qg = qg.expand({rows, qg.size(1)}).contiguous();
+        kg = kg.expand({rows, kg.size(1)}).contiguous();
+    }
+    const auto there = [](const Tensor &t) { return t.defined() ? MaybeTensor(t) : MaybeTensor(); };
+    py::gil_scoped_release others_run;
+    if (!table) return Attention::apply(q, k, v, MaybeTensor(), MaybeTensor(), MaybeTensor(), MaybeTensor(), MaybeTensor(), there(qg), there(kg), 0, scale, causal);
+    return Attention::apply(q, k, v, table, query_code, key_code, key_range, bucket, there(qg), there(kg), first_query, scale, causal);
+}
+
 }  // namespace
 
 PYBIND11_MODULE(_hot_host, m)
 {
+    m.def("dropout", &dropout);
+    m.def("block_end", &block_end);
+    m.def("attention", &attention);
     m.def("layer_norm", &layer_norm);
     m.def("head_loss", &head_loss);
     m.def("linear_forward", &linear_forward);
