@@ -692,13 +692,15 @@ int hot_block_backward(const hot_block_desc *desc, const hot_rng *rng, const voi
 
 /*
  * Attention with a learned relative position bias by buckets.  Query i of head h in entry b of the batch sees key j with
- *   z = scale q[i] . k[j] + table[bucket[query_code[first_query + i] - key_code[j]], h],   o[i] = sum_j softmax_j(z) v[j]
+ *   z = scale q[i] . k[j] + table[bucket[query_code[first_query + i] - key_code[j]][0], h],   o[i] = sum_j softmax_j(z) v[j]
  * over the keys that it may see: j <= i + keys - queries where causal, and query_groups[i] = key_groups[j] >= 0 where there are groups.  A query that sees
  * nothing has o = 0 and gradients 0; what rows of negative groups hold reaches nothing.  Query head h reads key and value head h / (heads / kv_heads).
  * q, o and their gradients: [batch, heads, queries, width], k and v [batch, kv_heads, keys, width], each with pitches of its own in elements
  * (batch, head, row; elements of a row adjacent).  table: dense [tables, buckets, heads] of table_dtype (dtype or HOT_F32), entry b taking table
  * b / (batch / tables); tables = 0: no bias, and no codes.  query_code, key_code: int32, such that differences lie in 0 .. codes - 1; bucket: int32
- * [codes]; key_range: int32 [ceil(keys / 64), 2], the smallest and largest key code of 64 keys each.  (Indices outside are taken as the last.)  Groups: int32
+ * [codes, 2], the bucket of every difference and the last difference up to which all are of that bucket; query_range, key_range: int32 [tokens / 64 rounded up, 2], the smallest and
+ * largest code of 64 tokens each, of all that query_code and key_code hold.  All 8-byte aligned.  (Indices outside are taken as the last; other things that do not
+ * fit together give other results.)  Groups: int32
  * [groups, queries] and [groups, keys], entry b taking row b mod groups; groups = 0: none.
  * Limits: HOT_ATTENTION_MOST_*; batch x heads x max(queries, keys) below 2^31.
  */
@@ -729,12 +731,12 @@ int64_t hot_attention_workspace_bytes(const hot_attention_desc *desc, int which)
  * them out.
  */
 int hot_attention_forward(const hot_attention_desc *desc, const void *q, const void *k, const void *v, const void *table, const int32_t *query_code,
-                          const int32_t *key_code, const int32_t *key_range, const int32_t *bucket, const int32_t *query_groups,
+                          const int32_t *key_code, const int32_t *query_range, const int32_t *key_range, const int32_t *bucket, const int32_t *query_groups,
                           const int32_t *key_groups, void *o, void *rest, float *stats, void *workspace, int64_t workspace_bytes, void *stream);
 
 /* All of grad_q, grad_k and grad_v are written (each may be NULL), grad_table (dense, table_dtype) where it is not NULL, every sum in a fixed order. */
 int hot_attention_backward(const hot_attention_desc *desc, const void *q, const void *k, const void *v, const void *table, const int32_t *query_code,
-                           const int32_t *key_code, const int32_t *key_range, const int32_t *bucket, const int32_t *query_groups,
+                           const int32_t *key_code, const int32_t *query_range, const int32_t *key_range, const int32_t *bucket, const int32_t *query_groups,
                            const int32_t *key_groups, const void *o, const void *rest, const float *stats, const void *grad_o, void *grad_q,
                            void *grad_k, void *grad_v, void *grad_table, void *workspace, int64_t workspace_bytes, void *stream);
 

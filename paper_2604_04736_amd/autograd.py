@@ -446,11 +446,17 @@ class RelativePositions:
         if int(bucket.min()) < 0 or int(bucket.max()) >= buckets:
             raise ValueError(f"bucket_of: need 0 to {buckets - 1}, got {int(bucket.min())} to {int(bucket.max())}")
         self.queries, self.keys, self.buckets = query.numel(), key.numel(), int(buckets)
-        shifted = key - key.max()
-        tiles = torch.nn.functional.pad(shifted, (0, -len(shifted) % 64), value=int(shifted[-1])).view(-1, 64)
-        ranges = torch.stack([tiles.amin(1), tiles.amax(1)], 1)
-        self.query_code, self.key_code, self.key_range, self.bucket = (
-            t.to(torch.int32).contiguous().to(device) for t in (query - query.min(), shifted, ranges, bucket))
+        query, key = query - query.min(), key - key.max()
+
+        def ranges(code):
+            tiles = torch.nn.functional.pad(code, (0, -len(code) % 64), value=int(code[-1])).view(-1, 64)
+            return torch.stack([tiles.amin(1), tiles.amax(1)], 1)
+
+        # the last difference of the run of equal buckets that each lies in
+        ends = torch.cat([bucket[1:] != bucket[:-1], torch.tensor([True])]).nonzero()[:, 0]
+        runs = torch.stack([bucket, ends[torch.searchsorted(ends, torch.arange(codes))]], 1)
+        self.query_code, self.key_code, self.query_range, self.key_range, self.bucket = (
+            t.to(torch.int32).contiguous().to(device) for t in (query, key, ranges(query), ranges(key), runs))
 
     @classmethod
     def distances(cls, queries: int, keys: int, buckets: int, furthest: int, device, both_sides: bool = True, first_query: int = 0):
@@ -498,5 +504,5 @@ def attention(q, k, v, table=None, positions: RelativePositions | None = None, *
         raise TypeError("positions: a table needs RelativePositions")
     if not isinstance(q, torch.Tensor):
         raise TypeError("q: need a tensor")
-    p = (positions.query_code, positions.key_code, positions.key_range, positions.bucket, positions.buckets) if table is not None else (None,) * 4 + (0,)
+    p = (positions.query_code, positions.key_code, positions.query_range, positions.key_range, positions.bucket, positions.buckets) if table is not None else (None,) * 5 + (0,)
     return hot.host().attention(q, k, v, table, *p, query_groups, key_groups, int(first_query), float(scale if scale is not None else max(q.shape[-1:] or (1,)) ** -0.5), bool(causal))

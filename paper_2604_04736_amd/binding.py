@@ -219,8 +219,8 @@ def lib() -> ctypes.CDLL:
     L.hot_block_backward_workspace_bytes.argtypes = [bp]
     L.hot_block_backward_workspace_bytes.restype = ctypes.c_int64
     ap = ctypes.POINTER(hot_attention_desc)
-    L.hot_attention_forward.argtypes = [ap] + [vp] * 14 + [ctypes.c_int64, vp]
-    L.hot_attention_backward.argtypes = [ap] + [vp] * 19 + [ctypes.c_int64, vp]
+    L.hot_attention_forward.argtypes = [ap] + [vp] * 15 + [ctypes.c_int64, vp]
+    L.hot_attention_backward.argtypes = [ap] + [vp] * 20 + [ctypes.c_int64, vp]
     L.hot_attention_workspace_bytes.argtypes = [ap, ctypes.c_int]
     L.hot_attention_workspace_bytes.restype = ctypes.c_int64
     for name in EXPORTS:
@@ -1111,7 +1111,7 @@ def _whole(t, shape, like, name: str):
 
 
 def _attention_desc(q, k, v, o, table, positions, scale, causal, query_groups, key_groups, first_query, grads=(None,) * 4):
-    """The description of a call and its pointers up to key_groups.  positions: (query_code, key_code, key_range, bucket) or None."""
+    """The description of a call and its pointers up to key_groups.  positions: (query_code, key_code, query_range, key_range, bucket) or None."""
     kind = _typed(q, "q")
     d = hot_attention_desc()
     d.q, d.k, d.v = _heads_of(q, "q"), _heads_of(k, "k", q), _heads_of(v, "v", q)
@@ -1125,16 +1125,17 @@ def _attention_desc(q, k, v, o, table, positions, scale, causal, query_groups, k
                 raise ValueError(f"{name}: need {tuple(like.shape)}, got {tuple(t.shape)}")
     keys = k.shape[2]
     d.queries, d.keys, d.batch, d.heads, d.kv_heads, d.width, d.scale, d.causal, d.dtype = queries, keys, batch, heads, k.shape[1], width, scale, bool(causal), kind
-    pointers = [q.data_ptr(), k.data_ptr(), v.data_ptr()] + [None] * 5
+    pointers = [q.data_ptr(), k.data_ptr(), v.data_ptr()] + [None] * 6
     if table is not None:
-        query_code, key_code, key_range, bucket = positions
+        query_code, key_code, query_range, key_range, bucket = positions
         if table.dim() != 3 or table.shape[2] != heads or not table.is_contiguous():
             raise ValueError(f"table: need a contiguous [tables, buckets, {heads}], got {tuple(table.shape)} strides {table.stride()}")
-        if query_code.shape[0] < first_query + queries or key_code.shape[0] < keys or key_range.shape[0] < (keys + 63) // 64 or first_query < 0:
+        if query_code.shape[0] < first_query + queries or key_code.shape[0] < keys or first_query < 0:
             raise ValueError(f"positions: need codes of {first_query + queries} queries and {keys} keys")
         d.tables, d.buckets, d.codes, d.first_query, d.table_dtype = table.shape[0], table.shape[1], bucket.shape[0], first_query, _typed(table, "table", q)
         pointers[3:] = [table.data_ptr(), _whole(query_code, query_code.shape[:1], q, "query_code"), _whole(key_code, key_code.shape[:1], q, "key_code"),
-                        _whole(key_range, (key_range.shape[0], 2), q, "key_range"), _whole(bucket, bucket.shape[:1], q, "bucket")]
+                        _whole(query_range, ((query_code.shape[0] + 63) // 64, 2), q, "query_range"), _whole(key_range, ((key_code.shape[0] + 63) // 64, 2), q, "key_range"),
+                        _whole(bucket, (bucket.shape[0], 2), q, "bucket")]
     if (query_groups is None) != (key_groups is None):
         raise ValueError("query_groups and key_groups: need both or neither")
     if query_groups is not None:
@@ -1154,7 +1155,7 @@ def _attention_workspace(d: hot_attention_desc, which: int, like):
 def hot_attention_forward(q, k, v, o, table=None, positions=None, *, scale: float, causal: bool = False, query_groups=None, key_groups=None, first_query: int = 0,
                           rest=None, stats=None, workspace=None) -> None:
     """o [batch, heads, queries, width] of attention with a position bias (see include/hot.h); table [tables, buckets, heads] or None; positions:
-    (query_code, key_code, key_range, bucket), int32.  rest (o's layout), stats (float32 [batch, heads, queries, 2]): for the backward call, or None."""
+    (query_code, key_code, query_range, key_range, bucket), int32.  rest (o's layout), stats (float32 [batch, heads, queries, 2]): for the backward call, or None."""
     d, pointers = _attention_desc(q, k, v, o, table, positions, scale, causal, query_groups, key_groups, first_query)
     if rest is not None and (rest.shape != o.shape or rest.stride() != o.stride() or rest.dtype != o.dtype):
         raise ValueError("rest: need o's shape, strides and type")

@@ -23,8 +23,8 @@
 namespace {
 
 using hot_detail::AttentionArgs;
-using hot_detail::kBins;
 
+constexpr int kMostCode = 1 << 28;               // beyond every code, and far enough from the ends of int to be added to
 constexpr float kNone = -__builtin_inff();
 template <class T>
 constexpr float kShift = __is_same(T, _Float16) ? 14.0f : 0.0f;
@@ -32,67 +32,234 @@ constexpr float kShift = __is_same(T, _Float16) ? 14.0f : 0.0f;
 __device__ __forceinline__ float two_to(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // Workgroups go to the eight dies in turn; each die gets a run of items, so that those which read the same keys share its L2.
-__device__ __forceinline__ long item_of(long id, long items)
+__device__ __forceinline__ long item_of(long items)
 {
+    const long id = (long)blockIdx.y * gridDim.x + blockIdx.x;
     const long per = (items + 7) / 8, item = id % 8 * per + id / 8;
     return id / 8 < per && item < items ? item : -1;
 }
 
-// The pieces of a tile of rows that a thread takes from memory to LDS: sixteen bytes each
+// A tile of ROWS rows on its way from memory to LDS: sixteen bytes of a row to a thread, kEach rows apart.  Loads are not branched around (see
+// fragment.h): rows behind the last are read from that one, and are zeros in LDS, as are rows of negative groups.  A row's last piece is read from where it ends; the
+// columns behind the rows' end are zeros from the start (clear) and never written.
 template <class T, int DP, int ROWS, int THREADS>
 struct Fetch {
     typedef Piece<T> P;
-    static constexpr int kPerRow = DP / P::N, kAll = ROWS * kPerRow, kEach = (kAll + THREADS - 1) / THREADS;
+    typedef typename P::Loose Loose;
+    static constexpr int N = P::N, kSlots = DP / N <= 4 ? 4 : (DP / N <= 8 ? 8 : (DP / N <= 16 ? 16 : 32)), kStep = THREADS / kSlots, kEach = ROWS / kStep;
+    static_assert(ROWS % kStep == 0, "");
     typename P::V v[kEach];
 
-    // rows first .. of `base` (pitch `row`), zeros where `there` says no
-    template <class There>
-    __device__ __forceinline__ void ask(const T *base, long row, int first, int width, There there)
+    static __device__ __forceinline__ int row0() { return (int)threadIdx.x / kSlots; }
+    static __device__ __forceinline__ int at() { return (int)threadIdx.x % kSlots * N; }
+
+    static __device__ __forceinline__ void clear(char *tile, int width)
     {
+        for (int i = (int)threadIdx.x; i < ROWS * DP; i += THREADS)
+            if (i % DP >= width) *reinterpret_cast<T *>(tile + i / DP * Rows<T, DP>::kPitch + i % DP * (int)sizeof(T)) = (T)0.0f;
+    }
+    // `base`: the tile's first row; last: its last row that is there
+    __device__ __forceinline__ void ask(const T *base, long pitch, int last, int width)
+    {
+        const int c = at();
+        if (c >= width) return;
+        if (width >= N) {
+            base += c + N <= width ? c : width - N;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const int r = row0() + i * kStep;
+                v[i] = *reinterpret_cast<const Loose *>(base + (r < last ? r : last) * pitch);
+            }
+        } else
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const int r = row0() + i * kStep;
+                v[i] = few_of<N, typename P::V>(base + (r < last ? r : last) * pitch, width);
+            }
+    }
+    // bits of this thread's rows that are there: up to the last, and of no negative group
+    static __device__ __forceinline__ unsigned rows_there(const int *groups, int last)
+    {
+        unsigned bits = 0;
+        int g[kEach];
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            const int c = (int)threadIdx.x + i * THREADS, r = c / kPerRow, at = c % kPerRow * P::N;
-            v[i] = (typename P::V)((T)0.0f);
-            if ((kAll % THREADS == 0 || c < kAll) && there(first + r)) v[i] = P::take(base + (long)(first + r) * row, at, width);
+            const int r = row0() + i * kStep;
+            g[i] = groups ? groups[r < last ? r : last] : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) bits |= (unsigned)(g[i] >= 0 && row0() + i * kStep <= last) << i;
+        return bits;
+    }
+    __device__ __forceinline__ void put(char *tile, int width, unsigned there) const
+    {
+        const int c = at();
+        if (c >= width) return;
+        tile += row0() * Rows<T, DP>::kPitch + c * (int)sizeof(T);
+        if (c + N <= width) {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                typename P::V x = v[i];
+                if (!(there >> i & 1u)) x = (typename P::V)((T)0.0f);
+                *reinterpret_cast<typename P::V *>(tile + i * kStep * Rows<T, DP>::kPitch) = x;
+            }
+            return;
+        }
+        const int skip = width >= N ? c + N - width : 0;          // elements of the piece that belong to the one before
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if (j >= skip && c + j - skip < width) *reinterpret_cast<T *>(tile + i * kStep * Rows<T, DP>::kPitch + (j - skip) * (int)sizeof(T)) = there >> i & 1u ? v[i][j] : (T)0.0f;
+    }
+};
+
+// Smallest and largest entry of `spans` over tiles of 64 from that of row `first` to that of row `last`
+__device__ __forceinline__ int2 span_over(const int2 *spans, int first, int last)
+{
+    int2 s = spans[first >> 6];
+    for (int t = (first >> 6) + 1; t <= last >> 6; ++t) {
+        const int2 u = spans[t];
+        s.x = u.x < s.x ? u.x : s.x;
+        s.y = u.y > s.y ? u.y : s.y;
+    }
+    return s;
+}
+
+// The tiles first .. end - 1 of T rows whose groups can meet those of `mine`, one after the other: sixty-four are looked at at once
+template <int T>
+struct Walk {
+    const int2 *spans;           // of 64 rows each; null: all tiles
+    int2 mine;
+    int base, end;
+    unsigned long mask;
+
+    __device__ __forceinline__ void look(int from)
+    {
+        base = from;
+        const int t = from + ((int)threadIdx.x & 63);
+        bool meets = t < end;
+        if (meets && spans) {
+            const int2 s = spans[t * T >> 6];
+            meets = s.x <= s.y && s.x <= mine.y && s.y >= mine.x;
+        }
+        mask = __ballot(meets);
+    }
+    __device__ __forceinline__ int begin(const int2 *spans_, int2 mine_, int first, int end_)
+    {
+        spans = spans_;
+        mine = mine_;
+        end = end_;
+        if (!spans) return first;
+        look(first);
+        return next(0);
+    }
+    __device__ __forceinline__ int next(int now)
+    {
+        if (!spans) return now + 1;
+        while (!mask) {
+            if (base + 64 >= end) return end;
+            look(base + 64);
+        }
+        const int t = base + __builtin_ctzl(mask);
+        mask &= mask - 1;
+        return t;
+    }
+};
+
+// How the bias of a tile of pairs is had.  The differences of codes between the two sides' ranges lie in low .. high: if they are of one bucket it is one number; if they are
+// few they are staged in LDS; else each pair goes to memory.
+constexpr int kOne = 0, kStaged = 1, kFar = 2;
+
+template <int THREADS>
+struct Bias {
+    static constexpr int kRoom = 4 * THREADS;
+    float v[4], one;
+    int bucket[4];
+    int low, count, form, all;
+
+    template <bool BUCKETS>
+    __device__ __forceinline__ void ask(const AttentionArgs &a, const float *bias, int2 queries, int2 keys)
+    {
+        if (!a.tables) {
+            form = kOne;
+            one = 0.0f;
+            return;
+        }
+        low = queries.x - keys.y;
+        int high = queries.y - keys.x;
+        low = low < 0 ? 0 : (low < a.codes ? low : a.codes - 1);
+        high = high < low ? low : (high < a.codes ? high : a.codes - 1);
+        count = high - low + 1;
+        const int2 run = a.bucket[low];
+        all = run.x;
+        one = bias[low];
+        form = run.y >= high ? kOne : (count <= kRoom ? kStaged : kFar);
+        if (count > kRoom) return;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int at = (int)threadIdx.x + i * THREADS;
+            if (i * THREADS < count) {
+                v[i] = bias[low + (at < count ? at : 0)];
+                if constexpr (BUCKETS) bucket[i] = a.bucket[low + (at < count ? at : 0)].x;
+            }
         }
     }
-    __device__ __forceinline__ void put(char *tile) const
+    template <bool BUCKETS>
+    __device__ __forceinline__ void put(float *room, int *buckets, int most) const
     {
+        if (form != kStaged) return;
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int c = (int)threadIdx.x + i * THREADS, r = c / kPerRow, at = c % kPerRow * P::N;
-            if (kAll % THREADS == 0 || c < kAll) *reinterpret_cast<typename P::V *>(tile + r * Rows<T, DP>::kPitch + at * (int)sizeof(T)) = v[i];
+        for (int i = 0; i < 4; ++i) {
+            const int at = (int)threadIdx.x + i * THREADS;
+            if (at < count) {
+                room[at] = v[i];
+                if constexpr (BUCKETS) buckets[at] = (unsigned)bucket[i] < (unsigned)most ? bucket[i] : most - 1;
+            }
         }
     }
 };
 
-// Smallest and largest of the values that threads offer, to all of them.  `room`: two words.
-__device__ __forceinline__ void range_of(int value, bool offers, int *room, int &low, int &high)
+// The same number, of which the compiler does not know it: comparisons with it are made where they stand.  (Moved out of loops, the masks of the rows' ends took
+// three hundred scalar registers more than there are.)
+__device__ __forceinline__ int fresh(int x)
 {
-    if (threadIdx.x == 0) {
-        room[0] = 0x7FFFFFFF;
-        room[1] = -0x7FFFFFFF;
+    asm volatile("" : "+s"(x));
+    return x;
+}
+
+template <int FORM, bool MASKED>
+struct Form {
+    static constexpr int kForm = FORM;
+    static constexpr bool kMasked = MASKED;
+};
+
+// go(Form<...>) for what a tile asks for
+template <class Go>
+__device__ __forceinline__ void by_form(int form, bool masked, Go go)
+{
+    if (form == kOne) {
+        if (masked) go(Form<kOne, true>{});
+        else go(Form<kOne, false>{});
+    } else if (form == kStaged) {
+        if (masked) go(Form<kStaged, true>{});
+        else go(Form<kStaged, false>{});
     }
-    __syncthreads();
-    if (offers) {
-        atomicMin(room, value);
-        atomicMax(room + 1, value);
-    }
-    __syncthreads();
-    low = room[0];
-    high = room[1];
+#ifndef NOFAR
+    else go(Form<kFar, true>{});
+#endif
 }
 
 // ---------------------------------------------------------------------------------
 // The table as a vector over differences of codes, in units of log 2; what a type's lowest value would overflow to stays finite, so that it is no mask.
-// And zeros for the bounds of fp16 (see above).
+// Smallest and largest group of 64 queries and of 64 keys each (those that are not negative).  And zeros for the bounds of fp16 (see above).
 __global__ void __launch_bounds__(256)
 hot_attention_begin_kernel(AttentionArgs a)
 {
     const long n = (long)a.tables * a.heads * a.codes;
     for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long)gridDim.x * 256) {
         const int code = (int)(i % a.codes), h = (int)(i / a.codes % a.heads), t = (int)(i / a.codes / a.heads);
-        const unsigned b = (unsigned)a.bucket[code], last = (unsigned)a.buckets - 1u;
+        const unsigned b = (unsigned)a.bucket[code].x, last = (unsigned)a.buckets - 1u;
         const long at = ((long)t * a.buckets + (b < last ? b : last)) * a.heads + h;
         const float v = a.table_type == HOT_F32 ? static_cast<const float *>(a.table)[at]
                                                 : (a.table_type == HOT_BF16 ? (float)static_cast<const __bf16 *>(a.table)[at] : (float)static_cast<const _Float16 *>(a.table)[at]);
@@ -101,6 +268,23 @@ hot_attention_begin_kernel(AttentionArgs a)
         a.bias[i] = u;
     }
     for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < a.bounds_count; i += (long)gridDim.x * 256) a.bounds[i] = 0u;
+    if (!a.groups) return;
+    const int tiles_q = (a.queries + 63) >> 6, tiles_k = (a.keys + 63) >> 6, lane = (int)threadIdx.x & 63;
+    const long all = (long)a.groups * (tiles_q + tiles_k);
+    for (long i = (long)blockIdx.x * 4 + (threadIdx.x >> 6); i < all; i += (long)gridDim.x * 4) {
+        const bool of_keys = i >= (long)a.groups * tiles_q;
+        const long at = of_keys ? i - (long)a.groups * tiles_q : i;
+        const int tiles = of_keys ? tiles_k : tiles_q, count = of_keys ? a.keys : a.queries, row = (int)(at / tiles), r = (int)(at % tiles) * 64 + lane;
+        const int g = r < count ? (of_keys ? a.key_groups : a.query_groups)[(long)row * count + r] : -1;
+        int low = g < 0 ? 0x7FFFFFFF : g, high = g;
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) {
+            const int l = __shfl_xor(low, off), h = __shfl_xor(high, off);
+            low = l < low ? l : low;
+            high = h > high ? h : high;
+        }
+        if (lane == 0) (of_keys ? a.key_spans : a.query_spans)[at] = int2{low, high};
+    }
 }
 
 // A query's place: of the rows of a tile, which hold queries of `pack` heads side by side
@@ -113,9 +297,9 @@ __device__ __forceinline__ Query query_of(const AttentionArgs &a, int b, int uni
 {
     Query q;
     q.there = row < a.queries * a.pack;
-    q.i = q.there ? row / a.pack : 0;
-    q.h = unit * a.pack + (a.pack > 1 ? row - row / a.pack * a.pack : 0);
-    if (!q.there) q.h = unit * a.pack;
+    row = q.there ? row : 0;
+    q.i = row / a.pack;
+    q.h = unit * a.pack + (row - q.i * a.pack);
     q.code = a.tables ? a.query_code[q.i] : 0;
     q.group = a.groups ? a.query_groups[(long)(b % a.groups) * a.queries + q.i] : 0;
     if (q.group < 0) q.there = false;
@@ -124,225 +308,222 @@ __device__ __forceinline__ Query query_of(const AttentionArgs &a, int b, int uni
     return q;
 }
 
+// The range of codes of queries first .. last of an entry: that of the 64s of the whole line which they lie in
+__device__ __forceinline__ int2 query_codes(const AttentionArgs &a, int first, int last)
+{
+    return a.tables ? span_over(a.query_range, a.first_query + first, a.first_query + last) : int2{0, 0};
+}
+
 // ---------------------------------------------------------------------------------
 template <class T, int DP, int QB, int WAVES, int KT>
-__global__ void __launch_bounds__(64 * WAVES)
+__global__ void __launch_bounds__(64 * WAVES, 2)
 hot_attention_forward_kernel(AttentionArgs a)
 {
     constexpr int THREADS = 64 * WAVES, KS = DP / 32, DB = DP / 16, KB = KT / 16, TILE = WAVES * QB * 16;
     typedef Rows<T, DP> R;
+    typedef Fetch<T, DP, KT, THREADS> F;
     __shared__ __attribute__((aligned(16))) char k_tile[KT * R::kPitch];
     __shared__ __attribute__((aligned(16))) char v_tile[KT * R::kPitch];
     __shared__ __attribute__((aligned(16))) int codes[KT], groups[KT];
-    __shared__ int room[2];
+    __shared__ float staged[Bias<THREADS>::kRoom];
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, g = lane >> 4, col = lane & 15;
     const int units = a.heads / a.pack, rows = a.queries * a.pack;
+    F::clear(k_tile, a.width);
+    F::clear(v_tile, a.width);
 
-    for (long id = blockIdx.x; id < ((a.items + 7) & ~7L); id += gridDim.x) {
-        long item = item_of(id, a.items);
-        if (item < 0) continue;
-        const int split = (int)(item % a.splits);
-        item /= a.splits;
-        const int tile_q = a.tiles_q - 1 - (int)(item % a.tiles_q);
-        item /= a.tiles_q;
-        const int unit = (int)(item % units), b = (int)(item / units);
-        const int kvh = unit * a.pack / a.per, table = a.tables ? b / a.entries : 0;
-        const T *const q = static_cast<const T *>(a.q) + b * a.p_q.batch;
-        const T *const k = static_cast<const T *>(a.k) + b * a.p_k.batch + kvh * a.p_k.head;
-        const T *const v = static_cast<const T *>(a.v) + b * a.p_v.batch + kvh * a.p_v.head;
-        const int *const kg = a.groups ? a.key_groups + (long)(b % a.groups) * a.keys : nullptr;
+    long item = item_of(a.items);
+    if (item < 0) return;
+    const int split = (int)(item % a.splits);
+    item /= a.splits;
+    const int tile_q = a.tiles_q - 1 - (int)(item % a.tiles_q);
+    item /= a.tiles_q;
+    const int unit = (int)(item % units), b = (int)(item / units);
+    const int kvh = unit * a.pack / a.per, table = a.tables ? b / a.entries : 0;
+    const T *const q = static_cast<const T *>(a.q) + b * a.p_q.batch;
+    const T *const k = static_cast<const T *>(a.k) + b * a.p_k.batch + kvh * a.p_k.head;
+    const T *const v = static_cast<const T *>(a.v) + b * a.p_v.batch + kvh * a.p_v.head;
+    const int *const kg = a.groups ? a.key_groups + (long)(b % a.groups) * a.keys : nullptr;
+    const int end_row = (tile_q + 1) * TILE < rows ? (tile_q + 1) * TILE : rows, last_i = (end_row - 1) / a.pack, first_i = tile_q * TILE / a.pack;
 
-        Query at[QB];
-        V8<T> qf[QB][KS];
-        const float *bias[QB];
-        int lowest = 0x7FFFFFFF, highest = -0x7FFFFFFF, few = 0x7FFFFFFF;
+    Query at[QB];
+    V8<T> qf[QB][KS];
 #pragma unroll
-        for (int n = 0; n < QB; ++n) {
-            at[n] = query_of(a, b, unit, tile_q * TILE + (wave * QB + n) * 16 + col);
-            bias[n] = a.bias + ((long)table * a.heads + at[n].h) * a.codes;
+    for (int n = 0; n < QB; ++n) {
+        at[n] = query_of(a, b, unit, tile_q * TILE + (wave * QB + n) * 16 + col);
+#pragma unroll
+        for (int s = 0; s < KS; ++s) qf[n][s] = eight(q + at[n].h * a.p_q.head + at[n].i * a.p_q.row, s * 32 + g * 8, a.width, at[n].there);
+    }
+    // (heads side by side have a bias each: what is staged is the first one's, and only one of them asks for it)
+    const float *const bias = a.bias + ((long)table * a.heads + unit * a.pack) * a.codes;
+    const int2 mine = query_codes(a, first_i, last_i);
+    // keys that any row of this workgroup may see by order, and up to which all of them may
+    int visible = a.causal ? last_i + a.keys - a.queries + 1 : a.keys, few = a.causal ? first_i + a.keys - a.queries + 1 : a.keys;
+    visible = visible < 0 ? 0 : (visible > a.keys ? a.keys : visible);
+    if (few > a.keys) few = a.keys;
+    const int all_tiles = (visible + KT - 1) / KT, share = (all_tiles + a.splits - 1) / a.splits;
+    const int end_tile = (split + 1) * share < all_tiles ? (split + 1) * share : all_tiles;
+
+    Walk<KT> walk;
+    F next_k, next_v;
+    Bias<THREADS> next_bias;
+    int next_code = 0, next_group = 0;
+    unsigned next_there = 0;
+    auto ask = [&](int tile) {
+        if (tile >= end_tile) return;
+        const int last = a.keys - 1 - tile * KT;
+        next_k.ask(k + (long)tile * KT * a.p_k.row, a.p_k.row, last, fresh(a.width));
+        next_v.ask(v + (long)tile * KT * a.p_v.row, a.p_v.row, last, fresh(a.width));
+        next_there = F::rows_there(kg ? kg + tile * KT : nullptr, last);
+        if ((int)threadIdx.x < KT) {
+            const int j = tile * KT + ((int)threadIdx.x < last ? (int)threadIdx.x : last);
+            next_code = a.tables ? a.key_code[j] : 0;
+            next_group = kg ? kg[j] : 0;
+            if ((int)threadIdx.x > last) next_group = -1;
+        }
+        next_bias.template ask<false>(a, bias, mine, a.tables ? a.key_range[tile * KT >> 6] : int2{0, 0});
+        if (a.pack > 1 && a.tables) next_bias.form = kFar;
+    };
+
+    Block16<T> o[DB][QB];
+    float m[QB], l[QB];
+#pragma unroll
+    for (int n = 0; n < QB; ++n) {
+        m[n] = kNone;
+        l[n] = 0.0f;
+    }
+    int tile = walk.begin(a.groups ? a.key_spans + (long)(b % a.groups) * ((a.keys + 63) >> 6) : nullptr,
+                          a.groups ? span_over(a.query_spans + (long)(b % a.groups) * ((a.queries + 63) >> 6), first_i, last_i) : int2{0, 0}, split * share, end_tile);
+    ask(tile);
+    while (tile < end_tile) {
+        __syncthreads();
+        next_k.put(k_tile, fresh(a.width), next_there);
+        next_v.put(v_tile, fresh(a.width), next_there);
+        if ((int)threadIdx.x < KT) {
+            codes[threadIdx.x] = next_code;
+            groups[threadIdx.x] = next_group;
+        }
+        next_bias.template put<false>(staged, nullptr, 0);
+        const int form = next_bias.form, low = next_bias.low;
+        const float one = next_bias.one;
+        __syncthreads();
+        const int k0 = tile * KT;
+        tile = walk.next(tile);
+        ask(tile);
+
+        Block16<T> acc[KB][QB];
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
-                qf[n][s] = (V8<T>)((T)0.0f);
-                if (at[n].there) qf[n][s] = eight(q + at[n].h * a.p_q.head + at[n].i * a.p_q.row, s * 32 + g * 8, a.width);
+                const V8<T> f = R::along(k_tile, kb * 16, s, lane);
+#pragma unroll
+                for (int n = 0; n < QB; ++n) acc[kb][n].mac(f, qf[n][s]);
             }
-            if (at[n].there && a.groups) {
-                lowest = at[n].group < lowest ? at[n].group : lowest;
-                highest = at[n].group > highest ? at[n].group : highest;
-            }
-        }
-        int low = 0, high = 0;
-        if (a.groups) {
-            int l2, h2;
-            range_of(lowest, true, room, low, h2);
-            __syncthreads();
-            range_of(highest, true, room, l2, high);
-        }
-        // keys that any row of this workgroup may see by order, and up to which all of them may
-        const int end_row = (tile_q + 1) * TILE < rows ? (tile_q + 1) * TILE : rows, last_i = (end_row - 1) / a.pack, first_i = tile_q * TILE / a.pack;
-        int visible = a.causal ? last_i + a.keys - a.queries + 1 : a.keys;
-        visible = visible < 0 ? 0 : (visible > a.keys ? a.keys : visible);
-        few = a.causal ? first_i + a.keys - a.queries + 1 : a.keys;
-        if (few > a.keys) few = a.keys;
-        const int all_tiles = (visible + KT - 1) / KT, share = (all_tiles + a.splits - 1) / a.splits;
-        const int end_tile = (split + 1) * share < all_tiles ? (split + 1) * share : all_tiles;
-
-        // the next tile that holds a key of a group of these rows
-        auto wanted = [&](int tile) {
-            if (a.groups)
-                for (; tile < end_tile; ++tile) {
-                    const int j = tile * KT + lane;
-                    const int group = lane < KT && j < a.keys ? kg[j] : -1;
-                    if (__ballot(group >= 0 && group >= low && group <= high)) break;
-                }
-            return tile;
-        };
-        Fetch<T, DP, KT, THREADS> next_k, next_v;
-        int next_code = 0, next_group = 0;
-        auto ask = [&](int tile) {
-            if (tile >= end_tile) return;
-            auto there = [&](int j) { return j < a.keys && (!kg || kg[j] >= 0); };
-            next_k.ask(k, a.p_k.row, tile * KT, a.width, there);
-            next_v.ask(v, a.p_v.row, tile * KT, a.width, there);
-            const int j = tile * KT + (int)threadIdx.x;
-            if ((int)threadIdx.x < KT) {
-                next_code = a.tables && j < a.keys ? a.key_code[j] : 0;
-                next_group = a.groups ? (j < a.keys ? kg[j] : -1) : 0;
-            }
-        };
-
-        Block16<T> o[DB][QB];
-        float m[QB], l[QB];
+        const Settled settled;
+        float z[KB][QB][4], top[QB];
 #pragma unroll
-        for (int n = 0; n < QB; ++n) {
-            m[n] = kNone;
-            l[n] = 0.0f;
-        }
-        int tile = wanted(split * share);
-        ask(tile);
-        while (tile < end_tile) {
-            __syncthreads();
-            next_k.put(k_tile);
-            next_v.put(v_tile);
-            if ((int)threadIdx.x < KT) {
-                codes[threadIdx.x] = next_code;
-                groups[threadIdx.x] = next_group;
-            }
-            __syncthreads();
-            const int k0 = tile * KT;
-            tile = wanted(tile + 1);
-            ask(tile);
-
-            Block16<T> acc[KB][QB];
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                for (int s = 0; s < KS; ++s) {
-                    const V8<T> f = R::along(k_tile, kb * 16, s, lane);
-#pragma unroll
-                    for (int n = 0; n < QB; ++n) acc[kb][n].mac(f, qf[n][s]);
-                }
-            const Settled settled;
-            float z[KB][QB][4], top[QB];
-#pragma unroll
-            for (int n = 0; n < QB; ++n) top[n] = kNone;
-            const bool edge = k0 + KT > few;
+        for (int n = 0; n < QB; ++n) top[n] = kNone;
+        by_form(form, k0 + KT > few || a.groups, [&](auto how) {
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
-                const i4 kc = *reinterpret_cast<const i4 *>(codes + kb * 16 + g * 4);
-                const i4 kgr = *reinterpret_cast<const i4 *>(groups + kb * 16 + g * 4);
+                i4 kc = i4(0), kgr = i4(0);
+                if constexpr (how.kForm != kOne) kc = *reinterpret_cast<const i4 *>(codes + kb * 16 + g * 4);
+                if constexpr (how.kMasked) kgr = *reinterpret_cast<const i4 *>(groups + kb * 16 + g * 4);
 #pragma unroll
                 for (int n = 0; n < QB; ++n) {
                     const f4 s = acc[kb][n].read(settled);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        float add = 0.0f;
-                        if (a.tables) {
+                        float add = one;
+                        if constexpr (how.kForm == kStaged) {
+                            const unsigned at_code = (unsigned)(at[n].code - low - kc[i]), last = Bias<THREADS>::kRoom - 1;
+                            add = staged[at_code < last ? at_code : last];
+                        } else if constexpr (how.kForm == kFar) {
                             const unsigned at_code = (unsigned)(at[n].code - kc[i]), last = (unsigned)a.codes - 1u;
-                            add = bias[n][at_code < last ? at_code : last];
+                            add = a.tables ? bias[(long)(at[n].h - unit * a.pack) * a.codes + (at_code < last ? at_code : last)] : 0.0f;
                         }
                         float x = __builtin_fmaf(s[i], a.scale, add);
-                        if (edge && k0 + kb * 16 + g * 4 + i > at[n].last) x = kNone;
-                        if (a.groups && kgr[i] != at[n].group) x = kNone;
+                        if constexpr (how.kMasked)
+                            if (k0 + kb * 16 + g * 4 + i > at[n].last || (a.groups && kgr[i] != at[n].group)) x = kNone;
                         z[kb][n][i] = x;
                         top[n] = __builtin_fmaxf(top[n], x);
                     }
                 }
             }
-            float base[QB];
-#pragma unroll
-            for (int n = 0; n < QB; ++n) {
-                top[n] = __builtin_fmaxf(top[n], __shfl_xor(top[n], 16));
-                top[n] = __builtin_fmaxf(top[n], __shfl_xor(top[n], 32));
-                const float now = __builtin_fmaxf(m[n], top[n]);
-                base[n] = now == kNone ? 0.0f : now;
-                if (__ballot(now > m[n])) {
-                    const float by = two_to(m[n] - base[n]);
-                    l[n] *= by;
-#pragma unroll
-                    for (int d = 0; d < DB; ++d) o[d][n].scale(settled, by);
-                }
-                m[n] = now;
-            }
-#pragma unroll
-            for (int c = 0; c < KT / 32; ++c) {
-                Pieces<T> p[QB];
-#pragma unroll
-                for (int n = 0; n < QB; ++n)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float e = two_to(z[2 * c + (i >> 2)][n][i & 3] - base[n] + kShift<T>);
-                        l[n] += e;
-                        p[n].set(i, e);
-                    }
-#pragma unroll
-                for (int d = 0; d < DB; ++d) {
-                    const V8<T> f = R::across(v_tile, c * 32, d * 16, lane);
-#pragma unroll
-                    for (int n = 0; n < QB; ++n) p[n].mac(o[d][n], f);
-                }
-            }
-        }
-        const Settled settled;
+        });
+        float base[QB];
 #pragma unroll
         for (int n = 0; n < QB; ++n) {
-            l[n] += __shfl_xor(l[n], 16);
-            l[n] += __shfl_xor(l[n], 32);
-            const int row = tile_q * TILE + (wave * QB + n) * 16 + col;
-            if (row >= rows) continue;
-            // (a row that sees nothing, or is of no group: zeros)
-            const int i = row / a.pack, h = unit * a.pack + (row - i * a.pack);
-            const long whole = ((long)b * a.heads + h) * a.queries + i;
-            if (a.splits > 1) {
-                float *const part = a.part_o + ((long)split * a.all_rows + whole) * a.width;
+            top[n] = __builtin_fmaxf(top[n], __shfl_xor(top[n], 16));
+            top[n] = __builtin_fmaxf(top[n], __shfl_xor(top[n], 32));
+            const float now = __builtin_fmaxf(m[n], top[n]);
+            base[n] = now == kNone ? 0.0f : now;
+            if (__ballot(now > m[n])) {
+                const float by = two_to(m[n] - base[n]);
+                l[n] *= by;
 #pragma unroll
-                for (int d = 0; d < DB; ++d) four(part, d * 16 + g * 4, a.width, o[d][n].read(settled));
-                if (g == 0) {
-                    a.part_ml[2 * ((long)split * a.all_rows + whole)] = m[n];
-                    a.part_ml[2 * ((long)split * a.all_rows + whole) + 1] = l[n];
-                }
-                continue;
+                for (int d = 0; d < DB; ++d) o[d][n].scale(settled, by);
             }
-            const float by = l[n] == 0.0f ? 0.0f : 1.0f / l[n];
-            T *const to = static_cast<T *>(a.o) + b * a.p_o.batch + h * a.p_o.head + i * a.p_o.row;
-            T *const rest = a.rest ? static_cast<T *>(a.rest) + b * a.p_o.batch + h * a.p_o.head + i * a.p_o.row : nullptr;
+            m[n] = now;
+        }
+#pragma unroll
+        for (int c = 0; c < KT / 32; ++c) {
+            Pieces<T> p[QB];
+#pragma unroll
+            for (int n = 0; n < QB; ++n)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float e = two_to(z[2 * c + (i >> 2)][n][i & 3] - base[n] + kShift<T>);
+                    l[n] += e;
+                    p[n].set(i, e);
+                }
 #pragma unroll
             for (int d = 0; d < DB; ++d) {
-                f4 x = o[d][n].read(settled);
-                f4 left;
+                const V8<T> f = R::across(v_tile, c * 32, d * 16, lane);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    x[j] = l[n] == 0.0f ? 0.0f : x[j] * by;
-                    left[j] = x[j] - (float)(T)x[j];
-                }
-                four(to, d * 16 + g * 4, a.width, x);
-                if (rest) four(rest, d * 16 + g * 4, a.width, left);
-            }
-            if (g == 0 && a.stats) {
-                a.stats[2 * whole] = l[n] == 0.0f ? 0.0f : m[n];
-                a.stats[2 * whole + 1] = l[n] == 0.0f ? __builtin_inff() : __builtin_log2f(l[n]) - kShift<T>;
+                for (int n = 0; n < QB; ++n) p[n].mac(o[d][n], f);
             }
         }
-        __syncthreads();
+    }
+    const Settled settled;
+#pragma unroll
+    for (int n = 0; n < QB; ++n) {
+        l[n] += __shfl_xor(l[n], 16);
+        l[n] += __shfl_xor(l[n], 32);
+        const int row = tile_q * TILE + (wave * QB + n) * 16 + col;
+        if (row >= rows) continue;
+        // (a row that sees nothing, or is of no group: zeros)
+        const int i = row / a.pack, h = unit * a.pack + (row - i * a.pack);
+        const long place = ((long)b * a.heads + h) * a.queries + i;
+        if (a.splits > 1) {
+            float *const part = a.part_o + ((long)split * a.all_rows + place) * a.width;
+#pragma unroll
+            for (int d = 0; d < DB; ++d) four(part, d * 16 + g * 4, a.width, o[d][n].read(settled));
+            if (g == 0) {
+                a.part_ml[2 * ((long)split * a.all_rows + place)] = m[n];
+                a.part_ml[2 * ((long)split * a.all_rows + place) + 1] = l[n];
+            }
+            continue;
+        }
+        const float by = 1.0f / l[n];
+        T *const to = static_cast<T *>(a.o) + b * a.p_o.batch + h * a.p_o.head + i * a.p_o.row;
+        T *const rest = a.rest ? static_cast<T *>(a.rest) + b * a.p_o.batch + h * a.p_o.head + i * a.p_o.row : nullptr;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+            f4 x = o[d][n].read(settled);
+            f4 left;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                x[j] = l[n] == 0.0f ? 0.0f : x[j] * by;
+                left[j] = x[j] - (float)(T)x[j];
+            }
+            four(to, d * 16 + g * 4, a.width, x);
+            if (rest) four(rest, d * 16 + g * 4, a.width, left);
+        }
+        if (g == 0 && a.stats) {
+            a.stats[2 * place] = l[n] == 0.0f ? 0.0f : m[n];
+            a.stats[2 * place + 1] = l[n] == 0.0f ? __builtin_inff() : __builtin_log2f(l[n]) - kShift<T>;
+        }
     }
 }
 
@@ -355,18 +536,20 @@ hot_attention_join_kernel(AttentionArgs a)
     for (long row = (long)blockIdx.x * 16 + ((int)threadIdx.x >> 4); row < a.all_rows; row += (long)gridDim.x * 16) {
         const int i = (int)(row % a.queries), h = (int)(row / a.queries % a.heads), b = (int)(row / a.queries / a.heads);
         float m = kNone;
+#pragma unroll 4
         for (int s = 0; s < a.splits; ++s) m = __builtin_fmaxf(m, a.part_ml[2 * ((long)s * a.all_rows + row)]);
         const float base = m == kNone ? 0.0f : m;
         float l = 0.0f, o[8] = {};
+#pragma unroll 4
         for (int s = 0; s < a.splits; ++s) {
             const long at = (long)s * a.all_rows + row;
             const float by = two_to(a.part_ml[2 * at] - base);
             l = __builtin_fmaf(a.part_ml[2 * at + 1], by, l);
-            const V8<float> v = eight(a.part_o + at * a.width, t * 8, a.width);
+            const V8<float> v = eight(a.part_o + at * a.width, t * 8, a.width, true);
 #pragma unroll
             for (int j = 0; j < 8; ++j) o[j] = __builtin_fmaf(v[j], by, o[j]);
         }
-        const float by = l == 0.0f ? 0.0f : 1.0f / l;
+        const float by = 1.0f / l;
         T *const to = static_cast<T *>(a.o) + b * a.p_o.batch + h * a.p_o.head + i * a.p_o.row;
         T *const rest = a.rest ? static_cast<T *>(a.rest) + b * a.p_o.batch + h * a.p_o.head + i * a.p_o.row : nullptr;
 #pragma unroll
@@ -388,52 +571,69 @@ hot_attention_join_kernel(AttentionArgs a)
 }
 
 // ---------------------------------------------------------------------------------
-// D of every query, sixteen lanes to a row; for fp16 also the largest |do_i|^2 of every head and the largest |v_j|^2 of every key head
+// D of every query, sixteen lanes to a row; for fp16 also the largest |do_i|^2 of every head and the largest |v_j|^2 of every key head (kPrepareRows rows to a workgroup, so
+// that few of them meet at one address)
+constexpr int kPrepareRows = 128;
+
 template <class T>
 __global__ void __launch_bounds__(256)
 hot_attention_prepare_kernel(AttentionArgs a)
 {
-    const int t = (int)threadIdx.x & 15;
-    const long keys = __is_same(T, _Float16) ? (long)a.batch * a.kv_heads * a.keys : 0, all = a.all_rows + keys;
-    for (long row = (long)blockIdx.x * 16 + ((int)threadIdx.x >> 4); row < all; row += (long)gridDim.x * 16) {
-        float sum = 0.0f, square = 0.0f;
-        unsigned *bound;
-        if (row < a.all_rows) {
-            const int i = (int)(row % a.queries), h = (int)(row / a.queries % a.heads), b = (int)(row / a.queries / a.heads);
-            const bool there = !a.groups || a.query_groups[(long)(b % a.groups) * a.queries + i] >= 0;
-            bound = a.bounds + (long)b * a.heads + h;
-            if (there) {
+    constexpr bool BOUNDS = __is_same(T, _Float16);
+    __shared__ float most[16];
+    const int t = (int)threadIdx.x & 15, lane_row = (int)threadIdx.x >> 4;
+    const long keys = BOUNDS ? (long)a.batch * a.kv_heads * a.keys : 0, all = a.all_rows + keys;
+    for (long first = (long)blockIdx.x * kPrepareRows; first < all; first += (long)gridDim.x * kPrepareRows) {
+        // whose maximum row `r` goes to
+        auto owner = [&](long r) { return r < a.all_rows ? r / a.queries : (long)a.batch * a.heads + (r - a.all_rows) / a.keys; };
+        const long end = first + kPrepareRows < all ? first + kPrepareRows : all;
+        const bool alone = BOUNDS && owner(first) == owner(end - 1);
+        float largest = 0.0f;
+        for (long row = first + lane_row; row < end; row += 16) {
+            float sum = 0.0f, square = 0.0f;
+            if (row < a.all_rows) {
+                const int i = (int)(row % a.queries), h = (int)(row / a.queries % a.heads), b = (int)(row / a.queries / a.heads);
+                const bool there = !a.groups || a.query_groups[(long)(b % a.groups) * a.queries + i] >= 0;
                 const long o_at = b * a.p_o.batch + h * a.p_o.head + i * a.p_o.row;
-                const V8<T> up = eight(static_cast<const T *>(a.grad_o) + b * a.p_go.batch + h * a.p_go.head + i * a.p_go.row, t * 8, a.width);
-                const V8<T> o = eight(static_cast<const T *>(a.o) + o_at, t * 8, a.width);
+                const V8<T> up = eight(static_cast<const T *>(a.grad_o) + b * a.p_go.batch + h * a.p_go.head + i * a.p_go.row, t * 8, a.width, there);
+                const V8<T> o = eight(static_cast<const T *>(a.o) + o_at, t * 8, a.width, there);
                 V8<T> rest = (V8<T>)((T)0.0f);
-                if (a.rest) rest = eight(static_cast<const T *>(a.rest) + o_at, t * 8, a.width);
+                if (a.rest) rest = eight(static_cast<const T *>(a.rest) + o_at, t * 8, a.width, there);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     sum = __builtin_fmaf((float)up[j], (float)o[j] + (float)rest[j], sum);
                     square = __builtin_fmaf((float)up[j], (float)up[j], square);
                 }
-            }
-        } else {
-            const long at = row - a.all_rows;
-            const int j0 = (int)(at % a.keys), h = (int)(at / a.keys % a.kv_heads), b = (int)(at / a.keys / a.kv_heads);
-            bound = a.bounds + (long)a.batch * a.heads + (long)b * a.kv_heads + h;
-            if (!a.groups || a.key_groups[(long)(b % a.groups) * a.keys + j0] >= 0) {
-                const V8<T> v = eight(static_cast<const T *>(a.v) + b * a.p_v.batch + h * a.p_v.head + j0 * a.p_v.row, t * 8, a.width);
+            } else if constexpr (BOUNDS) {
+                const long at = row - a.all_rows;
+                const int j0 = (int)(at % a.keys), h = (int)(at / a.keys % a.kv_heads), b = (int)(at / a.keys / a.kv_heads);
+                const bool there = !a.groups || a.key_groups[(long)(b % a.groups) * a.keys + j0] >= 0;
+                const V8<T> v = eight(static_cast<const T *>(a.v) + b * a.p_v.batch + h * a.p_v.head + j0 * a.p_v.row, t * 8, a.width, there);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) square = __builtin_fmaf((float)v[j], (float)v[j], square);
             }
-        }
 #pragma unroll
-        for (int off = 8; off > 0; off >>= 1) {
-            sum += __shfl_xor(sum, off);
-            square += __shfl_xor(square, off);
+            for (int off = 8; off > 0; off >>= 1) {
+                sum += __shfl_xor(sum, off);
+                if constexpr (BOUNDS) square += __shfl_xor(square, off);
+            }
+            if (t == 0 && row < a.all_rows) a.d[row] = sum;
+            // (positive floats are ordered as their bits are, and the largest does not depend on the order; nan and infinity are left out)
+            if constexpr (BOUNDS) {
+                if (!(square < 3.0e38f)) square = 0.0f;
+                if (alone) largest = __builtin_fmaxf(largest, square);
+                else if (t == 0) atomicMax(a.bounds + owner(row), __builtin_bit_cast(unsigned, square));
+            }
         }
-        if (t) continue;
-        if (row < a.all_rows) a.d[row] = sum;
-        // (positive floats are ordered as their bits are, and the largest does not depend on the order; nan and infinity are left out)
-        if constexpr (__is_same(T, _Float16))
-            if (square < 3.0e38f) atomicMax(bound, __builtin_bit_cast(unsigned, square));
+        if constexpr (BOUNDS) {
+            if (t == 0) most[lane_row] = largest;
+            __syncthreads();
+            if (threadIdx.x == 0 && alone) {
+                for (int i = 1; i < 16; ++i) largest = __builtin_fmaxf(largest, most[i]);
+                atomicMax(a.bounds + owner(first), __builtin_bit_cast(unsigned, largest));
+            }
+            __syncthreads();
+        }
     }
 }
 
@@ -457,412 +657,489 @@ __device__ __forceinline__ float unit_of(const AttentionArgs &a, int b, int h, i
 }
 
 // ---------------------------------------------------------------------------------
-// dk and dv: a wave holds KB blocks of sixteen keys, and their k and v as operands; the queries of every head that reads them go by in LDS.
+// dk and dv: a wave holds KB blocks of sixteen keys, and their k and v as operands; the queries of the heads that read them go by in LDS.  Where that gives too few
+// workgroups, the heads and runs of queries are split and the parts are added in their order (hot_attention_keys_join_kernel).
 template <class T, int DP, int KB, int WAVES>
-__global__ void __launch_bounds__(64 * WAVES)
+__global__ void __launch_bounds__(64 * WAVES, 2)
 hot_attention_keys_kernel(AttentionArgs a)
 {
     constexpr int THREADS = 64 * WAVES, KS = DP / 32, DB = DP / 16, TILE = WAVES * KB * 16, QT = 64;
     typedef Rows<T, DP> R;
+    typedef Fetch<T, DP, QT, THREADS> F;
     __shared__ __attribute__((aligned(16))) char q_tile[QT * R::kPitch];
     __shared__ __attribute__((aligned(16))) char up_tile[QT * R::kPitch];
     __shared__ __attribute__((aligned(16))) float ms[QT], ls[QT], ds[QT];
     __shared__ __attribute__((aligned(16))) int codes[QT], groups[QT];
-    __shared__ int room[2];
+    __shared__ float staged[Bias<THREADS>::kRoom];
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, g = lane >> 4, col = lane & 15;
-    const int tiles_q = (a.queries + QT - 1) / QT;
+    const int tiles_q = (a.queries + QT - 1) / QT, past = a.keys - a.queries;
+    F::clear(q_tile, a.width);
+    F::clear(up_tile, a.width);
 
-    for (long id = blockIdx.x; id < ((a.items + 7) & ~7L); id += gridDim.x) {
-        long item = item_of(id, a.items);
-        if (item < 0) continue;
-        const int tile_k = (int)(item % a.tiles_k);
-        item /= a.tiles_k;
-        const int kvh = (int)(item % a.kv_heads), b = (int)(item / a.kv_heads), table = a.tables ? b / a.entries : 0;
-        const T *const k = static_cast<const T *>(a.k) + b * a.p_k.batch + kvh * a.p_k.head;
-        const T *const v = static_cast<const T *>(a.v) + b * a.p_v.batch + kvh * a.p_v.head;
-        const int *const kg = a.groups ? a.key_groups + (long)(b % a.groups) * a.keys : nullptr;
-        const int *const qg = a.groups ? a.query_groups + (long)(b % a.groups) * a.queries : nullptr;
-        const int past = a.keys - a.queries;
+    long item = item_of(a.items);
+    if (item < 0) return;
+    const int split = (int)(item % a.splits);
+    item /= a.splits;
+    const int tile_k = (int)(item % a.tiles_k);
+    item /= a.tiles_k;
+    const int kvh = (int)(item % a.kv_heads), b = (int)(item / a.kv_heads), table = a.tables ? b / a.entries : 0;
+    // one head of the key head's, or all; a run of its queries
+    const int runs = a.by_head ? a.splits / a.per : a.splits, run = a.by_head ? split / a.per : split;
+    const int first_h = kvh * a.per + (a.by_head ? split % a.per : 0), end_h = a.by_head ? first_h + 1 : first_h + a.per;
+    const T *const k = static_cast<const T *>(a.k) + b * a.p_k.batch + kvh * a.p_k.head;
+    const T *const v = static_cast<const T *>(a.v) + b * a.p_v.batch + kvh * a.p_v.head;
+    const int *const kg = a.groups ? a.key_groups + (long)(b % a.groups) * a.keys : nullptr;
+    const int *const qg = a.groups ? a.query_groups + (long)(b % a.groups) * a.queries : nullptr;
 
-        int key[KB], code[KB], group[KB];
-        V8<T> kf[KB][KS], vf[KB][KS];
-        int lowest = 0x7FFFFFFF, highest = -0x7FFFFFFF;
+    int key[KB], code[KB], group[KB];
+    V8<T> kf[KB][KS], vf[KB][KS];
 #pragma unroll
-        for (int n = 0; n < KB; ++n) {
-            key[n] = tile_k * TILE + (wave * KB + n) * 16 + col;
-            const bool in = key[n] < a.keys;
-            code[n] = a.tables && in ? a.key_code[key[n]] : 0;
-            group[n] = in ? (kg ? kg[key[n]] : 0) : -1;
+    for (int n = 0; n < KB; ++n) {
+        key[n] = tile_k * TILE + (wave * KB + n) * 16 + col;
+        const bool in = key[n] < a.keys;
+        const int j = in ? key[n] : a.keys - 1;
+        code[n] = a.tables ? a.key_code[j] : 0;
+        group[n] = kg ? kg[j] : 0;
+        if (!in) group[n] = -1;
 #pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                kf[n][s] = vf[n][s] = (V8<T>)((T)0.0f);
-                if (group[n] >= 0) {
-                    kf[n][s] = eight(k + key[n] * a.p_k.row, s * 32 + g * 8, a.width);
-                    vf[n][s] = eight(v + key[n] * a.p_v.row, s * 32 + g * 8, a.width);
+        for (int s = 0; s < KS; ++s) {
+            kf[n][s] = eight(k + j * a.p_k.row, s * 32 + g * 8, a.width, group[n] >= 0);
+            vf[n][s] = eight(v + j * a.p_v.row, s * 32 + g * 8, a.width, group[n] >= 0);
+        }
+    }
+    const int last_key = (tile_k + 1) * TILE < a.keys ? (tile_k + 1) * TILE - 1 : a.keys - 1;
+    const int2 key_codes = a.tables ? span_over(a.key_range, tile_k * TILE, last_key) : int2{0, 0};
+    const int2 mine = a.groups ? span_over(a.key_spans + (long)(b % a.groups) * ((a.keys + 63) >> 6), tile_k * TILE, last_key) : int2{0, 0};
+    Block16<T> dk[DB][KB], dv[DB][KB];
+    const float unit = unit_of<T>(a, b, kvh * a.per, a.per);
+    // from the first query that sees a key of this tile on
+    const int first = a.causal && tile_k * TILE > past ? (tile_k * TILE - past) / QT : 0, left = tiles_q > first ? tiles_q - first : 0, share = (left + runs - 1) / runs;
+    const int first_tile = first + run * share, end_tile = first_tile + share < tiles_q ? first_tile + share : tiles_q;
+
+    for (int h = first_h; h < end_h; ++h) {
+        const T *const q = static_cast<const T *>(a.q) + b * a.p_q.batch + h * a.p_q.head;
+        const T *const up = static_cast<const T *>(a.grad_o) + b * a.p_go.batch + h * a.p_go.head;
+        const float *const bias = a.bias + ((long)table * a.heads + h) * a.codes;
+        const long stat0 = ((long)b * a.heads + h) * a.queries;
+        Walk<QT> walk;
+        F next_q, next_up;
+        Bias<THREADS> next_bias;
+        float next_m = 0.0f, next_l = 0.0f, next_d = 0.0f;
+        int next_code = 0, next_group = 0;
+        unsigned next_there = 0;
+        auto ask = [&](int tile) {
+            if (tile >= end_tile) return;
+            const int last = a.queries - 1 - tile * QT;
+            next_q.ask(q + (long)tile * QT * a.p_q.row, a.p_q.row, last, fresh(a.width));
+            next_up.ask(up + (long)tile * QT * a.p_go.row, a.p_go.row, last, fresh(a.width));
+            next_there = F::rows_there(qg ? qg + tile * QT : nullptr, last);
+            if ((int)threadIdx.x < QT) {
+                const int i = tile * QT + ((int)threadIdx.x < last ? (int)threadIdx.x : last);
+                next_m = a.stats[2 * (stat0 + i)];
+                next_l = a.stats[2 * (stat0 + i) + 1];
+                next_d = a.d[stat0 + i];
+                next_code = a.tables ? a.query_code[i] : 0;
+                next_group = qg ? qg[i] : 0;
+                if ((int)threadIdx.x > last) {
+                    next_l = __builtin_inff();
+                    next_group = -2;
                 }
             }
-            if (group[n] >= 0) {
-                lowest = group[n] < lowest ? group[n] : lowest;
-                highest = group[n] > highest ? group[n] : highest;
-            }
-        }
-        int low = 0, high = 0;
-        if (a.groups) {
-            int l2, h2;
-            range_of(lowest, true, room, low, h2);
+            next_bias.template ask<false>(a, bias, query_codes(a, tile * QT, tile * QT + (last < QT - 1 ? last : QT - 1)), key_codes);
+        };
+        int tile = walk.begin(a.groups ? a.query_spans + (long)(b % a.groups) * tiles_q : nullptr, mine, first_tile, end_tile);
+        ask(tile);
+        while (tile < end_tile) {
             __syncthreads();
-            range_of(highest, true, room, l2, high);
-        }
-        Block16<T> dk[DB][KB], dv[DB][KB];
-        const float unit = unit_of<T>(a, b, kvh * a.per, a.per);
-        // the first query that sees a key of this tile
-        int first = a.causal ? tile_k * TILE - past : 0;
-        first = first < 0 ? 0 : first;
-        const int first_tile = first / QT;
-
-        for (int h = kvh * a.per; h < (kvh + 1) * a.per; ++h) {
-            const T *const q = static_cast<const T *>(a.q) + b * a.p_q.batch + h * a.p_q.head;
-            const T *const up = static_cast<const T *>(a.grad_o) + b * a.p_go.batch + h * a.p_go.head;
-            const float *const bias = a.bias + ((long)table * a.heads + h) * a.codes;
-            const long stat0 = ((long)b * a.heads + h) * a.queries;
-            auto wanted = [&](int tile) {
-                if (a.groups)
-                    for (; tile < tiles_q; ++tile) {
-                        const int i = tile * QT + lane;
-                        const int x = i < a.queries ? qg[i] : -1;
-                        if (__ballot(x >= 0 && x >= low && x <= high)) break;
-                    }
-                return tile;
-            };
-            Fetch<T, DP, QT, THREADS> next_q, next_up;
-            float next_m = 0.0f, next_l = 0.0f, next_d = 0.0f;
-            int next_code = 0, next_group = 0;
-            auto ask = [&](int tile) {
-                if (tile >= tiles_q) return;
-                auto there = [&](int i) { return i < a.queries && (!qg || qg[i] >= 0); };
-                next_q.ask(q, a.p_q.row, tile * QT, a.width, there);
-                next_up.ask(up, a.p_go.row, tile * QT, a.width, there);
-                const int i = tile * QT + (int)threadIdx.x;
-                if ((int)threadIdx.x < QT) {
-                    const bool in = i < a.queries;
-                    next_m = in ? a.stats[2 * (stat0 + i)] : 0.0f;
-                    next_l = in ? a.stats[2 * (stat0 + i) + 1] : __builtin_inff();
-                    next_d = in ? a.d[stat0 + i] : 0.0f;
-                    next_code = a.tables && in ? a.query_code[i] : 0;
-                    next_group = in ? (qg ? qg[i] : 0) : -2;
-                }
-            };
-            int tile = wanted(first_tile);
+            next_q.put(q_tile, fresh(a.width), next_there);
+            next_up.put(up_tile, fresh(a.width), next_there);
+            if ((int)threadIdx.x < QT) {
+                ms[threadIdx.x] = next_m;
+                ls[threadIdx.x] = next_l;
+                ds[threadIdx.x] = next_d;
+                codes[threadIdx.x] = next_code;
+                groups[threadIdx.x] = next_group;
+            }
+            next_bias.template put<false>(staged, nullptr, 0);
+            const int form = next_bias.form, low = next_bias.low;
+            const float one = next_bias.one;
+            __syncthreads();
+            const int i0 = tile * QT;
+            tile = walk.next(tile);
             ask(tile);
-            while (tile < tiles_q) {
-                __syncthreads();
-                next_q.put(q_tile);
-                next_up.put(up_tile);
-                if ((int)threadIdx.x < QT) {
-                    ms[threadIdx.x] = next_m;
-                    ls[threadIdx.x] = next_l;
-                    ds[threadIdx.x] = next_d;
-                    codes[threadIdx.x] = next_code;
-                    groups[threadIdx.x] = next_group;
-                }
-                __syncthreads();
-                const int i0 = tile * QT;
-                tile = wanted(tile + 1);
-                ask(tile);
-                // whether some pair is not to be seen by order, or by the ends
-                const bool edge = a.causal && i0 + past < tile_k * TILE + TILE - 1;
+            // (queries behind the last have l = infinity, keys behind the last are zeros and are not stored)
+            const bool masked = a.groups || (a.causal && i0 + past < last_key);
 #pragma unroll
-                for (int c = 0; c < QT / 32; ++c) {
-                    Block16<T> s[2][KB], dp[2][KB];
+            for (int c = 0; c < QT / 32; ++c) {
+                Block16<T> s[2][KB], dp[2][KB];
 #pragma unroll
-                    for (int u = 0; u < 2; ++u)
+                for (int u = 0; u < 2; ++u)
 #pragma unroll
-                        for (int x = 0; x < KS; ++x) {
-                            const V8<T> fq = R::along(q_tile, c * 32 + u * 16, x, lane), fu = R::along(up_tile, c * 32 + u * 16, x, lane);
+                    for (int x = 0; x < KS; ++x) {
+                        const V8<T> fq = R::along(q_tile, c * 32 + u * 16, x, lane), fu = R::along(up_tile, c * 32 + u * 16, x, lane);
 #pragma unroll
-                            for (int n = 0; n < KB; ++n) {
-                                s[u][n].mac(fq, kf[n][x]);
-                                dp[u][n].mac(fu, vf[n][x]);
-                            }
+                        for (int n = 0; n < KB; ++n) {
+                            s[u][n].mac(fq, kf[n][x]);
+                            dp[u][n].mac(fu, vf[n][x]);
                         }
-                    const Settled settled;
-                    Pieces<T> p[KB], dz[KB];
+                    }
+                const Settled settled;
+                Pieces<T> p[KB], dz[KB];
+                by_form(form, masked, [&](auto how) {
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
                         const int row0 = c * 32 + u * 16 + g * 4;
                         const f4 m = *reinterpret_cast<const f4 *>(ms + row0), l = *reinterpret_cast<const f4 *>(ls + row0), d = *reinterpret_cast<const f4 *>(ds + row0);
-                        const i4 qc = *reinterpret_cast<const i4 *>(codes + row0), qgr = *reinterpret_cast<const i4 *>(groups + row0);
+                        i4 qc = i4(0), qgr = i4(0);
+                        if constexpr (how.kForm != kOne) qc = *reinterpret_cast<const i4 *>(codes + row0);
+                        if constexpr (how.kMasked) qgr = *reinterpret_cast<const i4 *>(groups + row0);
 #pragma unroll
                         for (int n = 0; n < KB; ++n) {
                             const f4 zs = s[u][n].read(settled), dps = dp[u][n].read(settled);
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
-                                float add = 0.0f;
-                                if (a.tables) {
+                                float add = one;
+                                if constexpr (how.kForm == kStaged) {
+                                    const unsigned at_code = (unsigned)(qc[i] - (code[n] + low)), last = Bias<THREADS>::kRoom - 1;
+                                    add = staged[at_code < last ? at_code : last];
+                                } else if constexpr (how.kForm == kFar) {
                                     const unsigned at_code = (unsigned)(qc[i] - code[n]), last = (unsigned)a.codes - 1u;
                                     add = bias[at_code < last ? at_code : last];
                                 }
                                 float e = two_to(__builtin_fmaf(zs[i], a.scale, add) - m[i] - l[i] + kShift<T>);
-                                if (group[n] != qgr[i] || (edge && key[n] > i0 + row0 + i + past)) e = 0.0f;
+                                float w = e * ((dps[i] - d[i]) * (unit * (__is_same(T, _Float16) ? 0x1p-14f : 1.0f)));
+                                if constexpr (how.kMasked)
+                                    if ((a.groups && group[n] != qgr[i]) || (a.causal && key[n] > i0 + row0 + i + past)) e = w = 0.0f;
                                 p[n].set(u * 4 + i, e);
-                                dz[n].set(u * 4 + i, e * ((dps[i] - d[i]) * (unit * (__is_same(T, _Float16) ? 0x1p-14f : 1.0f))));
+                                dz[n].set(u * 4 + i, w);
                             }
                         }
                     }
+                });
 #pragma unroll
-                    for (int x = 0; x < DB; ++x) {
-                        const V8<T> fu = R::across(up_tile, c * 32, x * 16, lane), fq = R::across(q_tile, c * 32, x * 16, lane);
+                for (int x = 0; x < DB; ++x) {
+                    const V8<T> fu = R::across(up_tile, c * 32, x * 16, lane), fq = R::across(q_tile, c * 32, x * 16, lane);
 #pragma unroll
-                        for (int n = 0; n < KB; ++n) {
-                            p[n].mac(dv[x][n], fu);
-                            dz[n].mac(dk[x][n], fq);
-                        }
+                    for (int n = 0; n < KB; ++n) {
+                        p[n].mac(dv[x][n], fu);
+                        dz[n].mac(dk[x][n], fq);
                     }
                 }
             }
         }
-        const Settled settled;
+    }
+    const Settled settled;
+    const float by_k = a.plain_scale / unit, by_v = __is_same(T, _Float16) ? 0x1p-14f : 1.0f;
 #pragma unroll
-        for (int n = 0; n < KB; ++n) {
-            if (key[n] >= a.keys) continue;
-            T *const to_k = a.grad_k ? static_cast<T *>(a.grad_k) + b * a.p_gk.batch + kvh * a.p_gk.head + key[n] * a.p_gk.row : nullptr;
-            T *const to_v = a.grad_v ? static_cast<T *>(a.grad_v) + b * a.p_gv.batch + kvh * a.p_gv.head + key[n] * a.p_gv.row : nullptr;
+    for (int n = 0; n < KB; ++n) {
+        if (key[n] >= a.keys) continue;
+        if (a.splits > 1) {
+            const long at = ((((long)split * a.batch + b) * a.kv_heads + kvh) * a.keys + key[n]) * a.width;
 #pragma unroll
             for (int x = 0; x < DB; ++x) {
-                if (to_k) four(to_k, x * 16 + g * 4, a.width, dk[x][n].read(settled) * (a.plain_scale / unit));
-                if (to_v) four(to_v, x * 16 + g * 4, a.width, dv[x][n].read(settled) * (__is_same(T, _Float16) ? 0x1p-14f : 1.0f));
+                if (a.grad_k) four(a.part_k + at, x * 16 + g * 4, a.width, dk[x][n].read(settled) * by_k);
+                if (a.grad_v) four(a.part_v + at, x * 16 + g * 4, a.width, dv[x][n].read(settled) * by_v);
             }
+            continue;
         }
-        __syncthreads();
+        T *const to_k = a.grad_k ? static_cast<T *>(a.grad_k) + b * a.p_gk.batch + kvh * a.p_gk.head + key[n] * a.p_gk.row : nullptr;
+        T *const to_v = a.grad_v ? static_cast<T *>(a.grad_v) + b * a.p_gv.batch + kvh * a.p_gv.head + key[n] * a.p_gv.row : nullptr;
+#pragma unroll
+        for (int x = 0; x < DB; ++x) {
+            if (to_k) four(to_k, x * 16 + g * 4, a.width, dk[x][n].read(settled) * by_k);
+            if (to_v) four(to_v, x * 16 + g * 4, a.width, dv[x][n].read(settled) * by_v);
+        }
+    }
+}
+
+// Parts of gradients of rows of `count` tokens and `heads` heads an entry added up, sixteen lanes to a row
+struct SumArgs {
+    const float *parts;
+    void *to;
+    hot_pitch pitch;
+    int splits, count, heads, width;
+    long rows;
+};
+
+template <class T>
+__global__ void __launch_bounds__(256)
+hot_attention_sum_kernel(SumArgs first, SumArgs second)
+{
+    const SumArgs a = blockIdx.y ? second : first;
+    if (!a.to) return;
+    const int t = (int)threadIdx.x & 15;
+    for (long row = (long)blockIdx.x * 16 + ((int)threadIdx.x >> 4); row < a.rows; row += (long)gridDim.x * 16) {
+        const int i = (int)(row % a.count), h = (int)(row / a.count % a.heads), b = (int)(row / a.count / a.heads);
+        float o[8] = {};
+#pragma unroll 4
+        for (int s = 0; s < a.splits; ++s) {
+            const V8<float> v = eight(a.parts + ((long)s * a.rows + row) * a.width, t * 8, a.width, true);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o[j] += v[j];
+        }
+        T *const to = static_cast<T *>(a.to) + b * a.pitch.batch + h * a.pitch.head + i * a.pitch.row;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) four(to, t * 8 + c * 4, a.width, f4{o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]});
     }
 }
 
 // ---------------------------------------------------------------------------------
-// dq, and what the table's gradient is made of.  A workgroup holds the queries of one tile and head, of several entries of the batch one after the other; every
-// pair's dz is added to its difference of codes in bins of the wave's own (LDS works a wave's additions one after the other), the waves' bins are
-// added up in their order and go to the table's buckets, which one wave alone adds to.
+// dq, and what the table's gradient is made of.  A workgroup holds the queries of one tile and head, of several entries of the batch one after the other.  Where a tile of
+// pairs is of one bucket its dz are added up in registers (in 64 bits from tile to tile); else each goes to its difference of codes in bins of the wave's own, and from
+// there to the wave's sums of the buckets.  No two waves add to one place, and LDS works a wave's additions in the order that they are issued in.
 template <class T, int DP, int QB, int WAVES, bool TABLE>
-__global__ void __launch_bounds__(64 * WAVES)
+__global__ void __launch_bounds__(64 * WAVES, 2)
 hot_attention_queries_kernel(AttentionArgs a)
 {
-    constexpr int THREADS = 64 * WAVES, KS = DP / 32, DB = DP / 16, KT = 64, TILE = WAVES * QB * 16;
+    constexpr int THREADS = 64 * WAVES, KS = DP / 32, DB = DP / 16, KT = 64, TILE = WAVES * QB * 16, BINS = TABLE ? Bias<THREADS>::kRoom : 1;
     typedef Rows<T, DP> R;
+    typedef Fetch<T, DP, KT, THREADS> F;
     __shared__ __attribute__((aligned(16))) char k_tile[KT * R::kPitch];
     __shared__ __attribute__((aligned(16))) char v_tile[KT * R::kPitch];
     __shared__ __attribute__((aligned(16))) int codes[KT], groups[KT];
-    __shared__ int room[2];
-    __shared__ float bins[TABLE ? WAVES : 1][TABLE ? kBins : 1];
-    extern __shared__ float buckets[];
+    __shared__ float staged[Bias<THREADS>::kRoom];
+    __shared__ int staged_bucket[BINS];
+    __shared__ float all_bins[WAVES * BINS];
+    extern __shared__ float all_sums[];          // [waves, buckets]
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, g = lane >> 4, col = lane & 15;
+    float *const bins = all_bins + wave * BINS, *const sums = all_sums + wave * a.buckets;
+    F::clear(k_tile, a.width);
+    F::clear(v_tile, a.width);
+    if constexpr (TABLE)
+        for (int i = lane; i < BINS; i += 64) bins[i] = 0.0f;
+    auto add = [](float *to, float x) { __hip_atomic_fetch_add(to, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT); };
 
-    for (long id = blockIdx.x; id < ((a.items + 7) & ~7L); id += gridDim.x) {
-        long item = item_of(id, a.items);
-        if (item < 0) continue;
-        const long unit_item = item;
-        const int tile_q = a.tiles_q - 1 - (int)(item % a.tiles_q);
-        item /= a.tiles_q;
-        const int h = (int)(item % a.heads), chunk = (int)(item / a.heads), kvh = h / a.per;
-        const int per_table = (a.entries + a.chunk - 1) / a.chunk, table = chunk / per_table;
-        const int first_b = table * a.entries + chunk % per_table * a.chunk;
-        const int end_b = first_b + a.chunk < (table + 1) * a.entries ? first_b + a.chunk : (table + 1) * a.entries;
-        const float *const bias = a.bias + ((long)table * a.heads + h) * a.codes;
-        if constexpr (TABLE) {
-            for (int i = (int)threadIdx.x; i < a.buckets; i += THREADS) buckets[i] = 0.0f;
-            for (int i = lane; i < kBins; i += 64) bins[wave][i] = 0.0f;
-        }
-        for (int b = first_b; b < end_b; ++b) {
-            const T *const q = static_cast<const T *>(a.q) + b * a.p_q.batch + h * a.p_q.head;
-            const T *const up = static_cast<const T *>(a.grad_o) + b * a.p_go.batch + h * a.p_go.head;
-            const T *const k = static_cast<const T *>(a.k) + b * a.p_k.batch + kvh * a.p_k.head;
-            const T *const v = static_cast<const T *>(a.v) + b * a.p_v.batch + kvh * a.p_v.head;
-            const int *const kg = a.groups ? a.key_groups + (long)(b % a.groups) * a.keys : nullptr;
-            const float unit = unit_of<T>(a, b, h, 1);
-            Query at[QB];
-            V8<T> qf[QB][KS], uf[QB][KS];
-            float m[QB], l[QB], dd[QB];
-            int lowest = 0x7FFFFFFF, highest = -0x7FFFFFFF, code_low = 0x7FFFFFFF, code_high = -0x7FFFFFFF;
+    long item = item_of(a.items);
+    if (item < 0) return;
+    const long unit_item = item;
+    const int split = (int)(item % a.splits);
+    item /= a.splits;
+    const int tile_q = a.tiles_q - 1 - (int)(item % a.tiles_q);
+    item /= a.tiles_q;
+    const int h = (int)(item % a.heads), chunk = (int)(item / a.heads), kvh = h / a.per;
+    const int per_table = (a.entries + a.chunk - 1) / a.chunk, table = chunk / per_table;
+    const int first_b = table * a.entries + chunk % per_table * a.chunk;
+    const int end_b = first_b + a.chunk < (table + 1) * a.entries ? first_b + a.chunk : (table + 1) * a.entries;
+    const float *const bias = a.bias + ((long)table * a.heads + h) * a.codes;
+    const int end_row = (tile_q + 1) * TILE < a.queries ? (tile_q + 1) * TILE : a.queries, first_i = tile_q * TILE, last_i = end_row - 1;
+    int visible = a.causal ? last_i + a.keys - a.queries + 1 : a.keys, few = a.causal ? first_i + a.keys - a.queries + 1 : a.keys;
+    visible = visible < 0 ? 0 : (visible > a.keys ? a.keys : visible);
+    if (few > a.keys) few = a.keys;
+    const int all_tiles = (visible + KT - 1) / KT, share = (all_tiles + a.splits - 1) / a.splits;
+    const int end_tile = (split + 1) * share < all_tiles ? (split + 1) * share : all_tiles;
+    const int2 mine_codes = query_codes(a, first_i, last_i);
+    double same = 0.0;               // this lane's part of the sum of bucket `same_bucket`
+    int same_bucket = -1;
+    auto flush = [&]() {
+        if (same_bucket < 0) return;
 #pragma unroll
-            for (int n = 0; n < QB; ++n) {
-                at[n] = query_of(a, b, h, tile_q * TILE + (wave * QB + n) * 16 + col);
+        for (int off = 32; off > 0; off >>= 1) same += __shfl_xor(same, off);
+        if (lane == 0) add(sums + same_bucket, (float)same);
+        same = 0.0;
+    };
+    if constexpr (TABLE)
+        for (int i = lane; i < a.buckets; i += 64) sums[i] = 0.0f;
+    for (int b = first_b; b < end_b; ++b) {
+        const T *const q = static_cast<const T *>(a.q) + b * a.p_q.batch + h * a.p_q.head;
+        const T *const up = static_cast<const T *>(a.grad_o) + b * a.p_go.batch + h * a.p_go.head;
+        const T *const k = static_cast<const T *>(a.k) + b * a.p_k.batch + kvh * a.p_k.head;
+        const T *const v = static_cast<const T *>(a.v) + b * a.p_v.batch + kvh * a.p_v.head;
+        const int *const kg = a.groups ? a.key_groups + (long)(b % a.groups) * a.keys : nullptr;
+        const float unit = unit_of<T>(a, b, h, 1);
+        Query at[QB];
+        V8<T> qf[QB][KS], uf[QB][KS];
+        float m[QB], l[QB], dd[QB];
+        int code_low = kMostCode, code_high = -1;             // of this wave's queries
+#pragma unroll
+        for (int n = 0; n < QB; ++n) {
+            at[n] = query_of(a, b, h, tile_q * TILE + (wave * QB + n) * 16 + col);
+            const long row = ((long)b * a.heads + h) * a.queries + at[n].i;
+            m[n] = a.stats[2 * row];
+            l[n] = a.stats[2 * row + 1];
+            dd[n] = a.d[row];
+            if (!at[n].there) {
                 m[n] = dd[n] = 0.0f;
                 l[n] = __builtin_inff();
-                if (at[n].there) {
-                    const long row = ((long)b * a.heads + h) * a.queries + at[n].i;
-                    m[n] = a.stats[2 * row];
-                    l[n] = a.stats[2 * row + 1];
-                    dd[n] = a.d[row];
-                    lowest = at[n].group < lowest ? at[n].group : lowest;
-                    highest = at[n].group > highest ? at[n].group : highest;
-                    code_low = at[n].code < code_low ? at[n].code : code_low;
-                    code_high = at[n].code > code_high ? at[n].code : code_high;
-                }
+            } else {
+                code_low = at[n].code < code_low ? at[n].code : code_low;
+                code_high = at[n].code > code_high ? at[n].code : code_high;
+            }
 #pragma unroll
-                for (int s = 0; s < KS; ++s) {
-                    qf[n][s] = uf[n][s] = (V8<T>)((T)0.0f);
-                    if (at[n].there) {
-                        qf[n][s] = eight(q + at[n].i * a.p_q.row, s * 32 + g * 8, a.width);
-                        uf[n][s] = eight(up + at[n].i * a.p_go.row, s * 32 + g * 8, a.width);
-                    }
-                }
+            for (int s = 0; s < KS; ++s) {
+                qf[n][s] = eight(q + at[n].i * a.p_q.row, s * 32 + g * 8, a.width, at[n].there);
+                uf[n][s] = eight(up + at[n].i * a.p_go.row, s * 32 + g * 8, a.width, at[n].there);
             }
-            int low = 0, high = 0, qc_low = 0, qc_high = 0, unused;
-            if (a.groups) {
-                range_of(lowest, true, room, low, unused);
-                __syncthreads();
-                range_of(highest, true, room, unused, high);
-                __syncthreads();
+        }
+        if constexpr (TABLE) {
+#pragma unroll
+            for (int off = 8; off > 0; off >>= 1) {
+                const int x = __shfl_xor(code_low, off), y = __shfl_xor(code_high, off);
+                code_low = x < code_low ? x : code_low;
+                code_high = y > code_high ? y : code_high;
             }
-            if constexpr (TABLE) {
-                range_of(code_low, true, room, qc_low, unused);
-                __syncthreads();
-                range_of(code_high, true, room, unused, qc_high);
-                __syncthreads();
+        }
+        Walk<KT> walk;
+        F next_k, next_v;
+        Bias<THREADS> next_bias;
+        int next_code = 0, next_group = 0;
+        int2 next_range = int2{0, 0};
+        unsigned next_there = 0;
+        auto ask = [&](int tile) {
+            if (tile >= end_tile) return;
+            const int last = a.keys - 1 - tile * KT;
+            next_k.ask(k + (long)tile * KT * a.p_k.row, a.p_k.row, last, fresh(a.width));
+            next_v.ask(v + (long)tile * KT * a.p_v.row, a.p_v.row, last, fresh(a.width));
+            next_there = F::rows_there(kg ? kg + tile * KT : nullptr, last);
+            if ((int)threadIdx.x < KT) {
+                const int j = tile * KT + ((int)threadIdx.x < last ? (int)threadIdx.x : last);
+                next_code = a.tables ? a.key_code[j] : 0;
+                next_group = kg ? kg[j] : 0;
+                if ((int)threadIdx.x > last) next_group = -1;
             }
-            const int end_row = (tile_q + 1) * TILE < a.queries ? (tile_q + 1) * TILE : a.queries;
-            int visible = a.causal ? end_row - 1 + a.keys - a.queries + 1 : a.keys;
-            visible = visible < 0 ? 0 : (visible > a.keys ? a.keys : visible);
-            int few = a.causal ? tile_q * TILE + a.keys - a.queries + 1 : a.keys;
-            if (few > a.keys) few = a.keys;
-            const int end_tile = (visible + KT - 1) / KT;
-            auto wanted = [&](int tile) {
-                if (a.groups)
-                    for (; tile < end_tile; ++tile) {
-                        const int j = tile * KT + lane;
-                        const int x = j < a.keys ? kg[j] : -1;
-                        if (__ballot(x >= 0 && x >= low && x <= high)) break;
-                    }
-                return tile;
-            };
-            Fetch<T, DP, KT, THREADS> next_k, next_v;
-            int next_code = 0, next_group = 0;
-            auto ask = [&](int tile) {
-                if (tile >= end_tile) return;
-                auto there = [&](int j) { return j < a.keys && (!kg || kg[j] >= 0); };
-                next_k.ask(k, a.p_k.row, tile * KT, a.width, there);
-                next_v.ask(v, a.p_v.row, tile * KT, a.width, there);
-                const int j = tile * KT + (int)threadIdx.x;
-                if ((int)threadIdx.x < KT) {
-                    next_code = a.tables && j < a.keys ? a.key_code[j] : 0;
-                    next_group = a.groups ? (j < a.keys ? kg[j] : -1) : 0;
-                }
-            };
-            Block16<T> dq[DB][QB];
-            int tile = wanted(0);
+            next_range = a.tables ? a.key_range[tile] : int2{0, 0};
+            next_bias.template ask<TABLE>(a, bias, mine_codes, next_range);
+        };
+        Block16<T> dq[DB][QB];
+        int tile = walk.begin(a.groups ? a.key_spans + (long)(b % a.groups) * ((a.keys + 63) >> 6) : nullptr,
+                              a.groups ? span_over(a.query_spans + (long)(b % a.groups) * ((a.queries + 63) >> 6), first_i, last_i) : int2{0, 0}, split * share, end_tile);
+        ask(tile);
+        while (tile < end_tile) {
+            __syncthreads();
+            next_k.put(k_tile, fresh(a.width), next_there);
+            next_v.put(v_tile, fresh(a.width), next_there);
+            if ((int)threadIdx.x < KT) {
+                codes[threadIdx.x] = next_code;
+                groups[threadIdx.x] = next_group;
+            }
+            next_bias.template put<TABLE>(staged, staged_bucket, a.buckets);
+            const int form = next_bias.form, low = next_bias.low, bucket = next_bias.all;
+            const int2 range = next_range;
+            const float one = next_bias.one;
+            __syncthreads();
+            const int k0 = tile * KT;
+            tile = walk.next(tile);
             ask(tile);
-            while (tile < end_tile) {
-                __syncthreads();
-                next_k.put(k_tile);
-                next_v.put(v_tile);
-                if ((int)threadIdx.x < KT) {
-                    codes[threadIdx.x] = next_code;
-                    groups[threadIdx.x] = next_group;
-                }
-                __syncthreads();
-                const int k0 = tile * KT, here = tile;
-                tile = wanted(tile + 1);
-                ask(tile);
-                const bool edge = k0 + KT > few;
-                int bin_low = 0, bins_all = 0;
-                if constexpr (TABLE) {
-                    bin_low = qc_low - a.key_range[2 * here + 1];
-                    bins_all = qc_high - a.key_range[2 * here] - bin_low + 1;
-                }
-                float grad[TABLE ? KT / 16 : 1][QB][4];
+            const bool masked = k0 + KT > few || a.groups;
+            float here = 0.0f;
 #pragma unroll
-                for (int c = 0; c < KT / 32; ++c) {
-                    Block16<T> s[2][QB], dp[2][QB];
+            for (int c = 0; c < KT / 32; ++c) {
+                Block16<T> s[2][QB], dp[2][QB];
 #pragma unroll
-                    for (int u = 0; u < 2; ++u)
+                for (int u = 0; u < 2; ++u)
 #pragma unroll
-                        for (int x = 0; x < KS; ++x) {
-                            const V8<T> fk = R::along(k_tile, c * 32 + u * 16, x, lane), fv = R::along(v_tile, c * 32 + u * 16, x, lane);
+                    for (int x = 0; x < KS; ++x) {
+                        const V8<T> fk = R::along(k_tile, c * 32 + u * 16, x, lane), fv = R::along(v_tile, c * 32 + u * 16, x, lane);
 #pragma unroll
-                            for (int n = 0; n < QB; ++n) {
-                                s[u][n].mac(fk, qf[n][x]);
-                                dp[u][n].mac(fv, uf[n][x]);
-                            }
+                        for (int n = 0; n < QB; ++n) {
+                            s[u][n].mac(fk, qf[n][x]);
+                            dp[u][n].mac(fv, uf[n][x]);
                         }
-                    const Settled settled;
-                    Pieces<T> dz[QB];
+                    }
+                const Settled settled;
+                Pieces<T> dz[QB];
+                by_form(form, masked, [&](auto how) {
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
                         const int row0 = c * 32 + u * 16 + g * 4;
-                        const i4 kc = *reinterpret_cast<const i4 *>(codes + row0), kgr = *reinterpret_cast<const i4 *>(groups + row0);
+                        i4 kc = i4(0), kgr = i4(0);
+                        if constexpr (how.kForm != kOne) kc = *reinterpret_cast<const i4 *>(codes + row0);
+                        if constexpr (how.kMasked) kgr = *reinterpret_cast<const i4 *>(groups + row0);
 #pragma unroll
                         for (int n = 0; n < QB; ++n) {
                             const f4 zs = s[u][n].read(settled), dps = dp[u][n].read(settled);
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
-                                float add = 0.0f;
-                                if (a.tables) {
-                                    const unsigned at_code = (unsigned)(at[n].code - kc[i]), last = (unsigned)a.codes - 1u;
-                                    add = bias[at_code < last ? at_code : last];
+                                float bias_here = one;
+                                unsigned at_code = 0;
+                                if constexpr (how.kForm == kStaged) {
+                                    constexpr unsigned last = Bias<THREADS>::kRoom - 1;
+                                    at_code = (unsigned)(at[n].code - low - kc[i]);
+                                    at_code = at_code < last ? at_code : last;
+                                    bias_here = staged[at_code];
+                                } else if constexpr (how.kForm == kFar) {
+                                    const unsigned last = (unsigned)a.codes - 1u;
+                                    at_code = (unsigned)(at[n].code - kc[i]);
+                                    at_code = at_code < last ? at_code : last;
+                                    bias_here = bias[at_code];
                                 }
-                                float e = two_to(__builtin_fmaf(zs[i], a.scale, add) - m[n] - l[n]);
-                                if (edge && k0 + row0 + i > at[n].last) e = 0.0f;
-                                if (a.groups && kgr[i] != at[n].group) e = 0.0f;
-                                const float w = e * (dps[i] - dd[n]);
-                                if constexpr (TABLE) grad[2 * c + u][n][i] = w;
+                                const float e = two_to(__builtin_fmaf(zs[i], a.scale, bias_here) - m[n] - l[n]);
+                                float w = e * (dps[i] - dd[n]);
+                                bool sees = at[n].there;
+                                if constexpr (how.kMasked) {
+                                    sees = !(k0 + row0 + i > at[n].last || (a.groups && kgr[i] != at[n].group));
+                                    if (!sees) w = 0.0f;
+                                }
                                 dz[n].set(u * 4 + i, w * unit);
+                                if constexpr (TABLE) {
+                                    if constexpr (how.kForm == kOne) here += w;
+                                    else if constexpr (how.kForm == kStaged) {
+                                        if (sees) add(bins + at_code, w);
+                                    } else if (sees && a.tables) {
+                                        const unsigned to = (unsigned)a.bucket[at_code].x, most = (unsigned)a.buckets - 1u;
+                                        add(sums + (to < most ? to : most), w);
+                                    }
+                                }
                             }
                         }
                     }
+                });
 #pragma unroll
-                    for (int x = 0; x < DB; ++x) {
-                        const V8<T> f = R::across(k_tile, c * 32, x * 16, lane);
+                for (int x = 0; x < DB; ++x) {
+                    const V8<T> f = R::across(k_tile, c * 32, x * 16, lane);
 #pragma unroll
-                        for (int n = 0; n < QB; ++n) dz[n].mac(dq[x][n], f);
-                    }
+                    for (int n = 0; n < QB; ++n) dz[n].mac(dq[x][n], f);
                 }
-                if constexpr (TABLE) {
-                    // (as many bins at a time as there are; differences beyond them wait for their turn)
-                    for (int done = 0; done < bins_all; done += kBins) {
-                        const int now = bins_all - done < kBins ? bins_all - done : kBins;
-#pragma unroll
-                        for (int x = 0; x < KT / 16; ++x) {
-                            const i4 kc = *reinterpret_cast<const i4 *>(codes + x * 16 + g * 4);
-#pragma unroll
-                            for (int n = 0; n < QB; ++n)
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) {
-                                    const int bin = at[n].code - kc[i] - bin_low - done;
-                                    if (at[n].there && (unsigned)bin < (unsigned)now) __hip_atomic_fetch_add(&bins[wave][bin], grad[x][n][i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-                                }
-                        }
-                        __syncthreads();
-                        if (wave == 0)
-                            for (int i = lane; i < now; i += 64) {
-                                float sum = 0.0f;
-#pragma unroll
-                                for (int w = 0; w < WAVES; ++w) {
-                                    sum += bins[w][i];
-                                    bins[w][i] = 0.0f;
-                                }
-                                const unsigned code = (unsigned)(bin_low + done + i), last = (unsigned)a.codes - 1u;
-                                const unsigned bucket = (unsigned)a.bucket[code < last ? code : last], most = (unsigned)a.buckets - 1u;
-                                __hip_atomic_fetch_add(&buckets[bucket < most ? bucket : most], sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-                            }
-                        __syncthreads();
+            }
+            if constexpr (TABLE) {
+                if (form == kOne) {
+                    if (bucket != same_bucket) {
+                        flush();
+                        same_bucket = bucket < 0 ? 0 : (bucket < a.buckets ? bucket : a.buckets - 1);
+                    }
+                    same += (double)here;
+                } else if (form == kStaged) {
+                    // the bins that this wave's queries reach
+                    // (none where the wave has no queries: code_high is -1)
+                    int first = code_low - range.y - low, end = code_high - range.x - low + 1;
+                    first = first < 0 ? 0 : first;
+                    end = code_high < 0 ? 0 : (end < BINS ? end : BINS);
+                    for (int i = first + lane; i < end; i += 64) {
+                        const float x = bins[i];
+                        bins[i] = 0.0f;
+                        add(sums + staged_bucket[i], x);
                     }
                 }
             }
-            const Settled settled;
-            if (a.grad_q)
+        }
+        const Settled settled;
+        if (a.grad_q)
 #pragma unroll
-                for (int n = 0; n < QB; ++n) {
-                    const int row = tile_q * TILE + (wave * QB + n) * 16 + col;
-                    if (row >= a.queries) continue;
-                    T *const to = static_cast<T *>(a.grad_q) + b * a.p_gq.batch + h * a.p_gq.head + row * a.p_gq.row;
+            for (int n = 0; n < QB; ++n) {
+                const int row = tile_q * TILE + (wave * QB + n) * 16 + col;
+                if (row >= a.queries) continue;
+                if (a.splits > 1) {
+                    float *const part = a.part_o + ((long)split * a.all_rows + ((long)b * a.heads + h) * a.queries + row) * a.width;
 #pragma unroll
-                    for (int x = 0; x < DB; ++x) four(to, x * 16 + g * 4, a.width, dq[x][n].read(settled) * (a.plain_scale / unit));
+                    for (int x = 0; x < DB; ++x) four(part, x * 16 + g * 4, a.width, dq[x][n].read(settled) * (a.plain_scale / unit));
+                    continue;
                 }
-            __syncthreads();
+                T *const to = static_cast<T *>(a.grad_q) + b * a.p_gq.batch + h * a.p_gq.head + row * a.p_gq.row;
+#pragma unroll
+                for (int x = 0; x < DB; ++x) four(to, x * 16 + g * 4, a.width, dq[x][n].read(settled) * (a.plain_scale / unit));
+            }
+        __syncthreads();
+    }
+    if constexpr (TABLE) {
+        flush();
+        __syncthreads();
+        float *const to = a.parts + unit_item * a.buckets;
+        for (int i = (int)threadIdx.x; i < a.buckets; i += THREADS) {
+            float sum = all_sums[i];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) sum += all_sums[w * a.buckets + i];
+            to[i] = sum;
         }
-        if constexpr (TABLE) {
-            float *const to = a.parts + unit_item * a.buckets;
-            for (int i = (int)threadIdx.x; i < a.buckets; i += THREADS) to[i] = buckets[i];
-            __syncthreads();
-        }
+        __syncthreads();
     }
 }
 
@@ -870,30 +1147,38 @@ hot_attention_queries_kernel(AttentionArgs a)
 __global__ void __launch_bounds__(1024)
 hot_attention_table_kernel(AttentionArgs a)
 {
-    __shared__ float runs[16][64];
+    __shared__ double runs[16][64];
     const int lane = (int)threadIdx.x & 63, run = (int)threadIdx.x >> 6, h = (int)blockIdx.y, table = (int)blockIdx.z;
-    const int col = (int)blockIdx.x * 64 + lane, per_table = (a.entries + a.chunk - 1) / a.chunk;
-    float sum = 0.0f;
-    if (col < a.buckets)
-        for (long u = run; u < (long)per_table * a.tiles_q; u += 16) {
-            const long chunk = (long)table * per_table + u / a.tiles_q, unit = (chunk * a.heads + h) * a.tiles_q + u % a.tiles_q;
-            sum += a.parts[unit * a.buckets + col];
+    const int col = (int)blockIdx.x * 64 + lane, per_table = (a.entries + a.chunk - 1) / a.chunk, each = a.tiles_q * a.splits;
+    double sum = 0.0;
+    if (col < a.buckets) {
+        const long all = (long)per_table * each;
+        for (long u = run; u < all; u += 64) {
+            float v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const long w = u + 16 * j < all ? u + 16 * j : u, chunk = (long)table * per_table + w / each;
+                v[j] = a.parts[((chunk * a.heads + h) * each + w % each) * a.buckets + col];
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum += u + 16 * j < all ? (double)v[j] : 0.0;
         }
+    }
     runs[run][lane] = sum;
     __syncthreads();
     if (run || col >= a.buckets) return;
 #pragma unroll
     for (int i = 1; i < 16; ++i) sum += runs[i][lane];
-    store_as(a.grad_table, a.table_type, ((long)table * a.buckets + col) * a.heads + h, sum);
+    store_as(a.grad_table, a.table_type, ((long)table * a.buckets + col) * a.heads + h, (float)sum);
 }
 
 // ---------------------------------------------------------------------------------
 // Host side: what is launched for one type
 
-inline unsigned blocks_for(long items)
+inline dim3 blocks_for(long items)
 {
     const long most = 1L << 20, up = (items + 7) & ~7L;
-    return (unsigned)(up < most ? up : most);
+    return up <= most ? dim3((unsigned)up) : dim3((unsigned)most, (unsigned)((up + most - 1) / most));
 }
 
 template <class T, int DP>
@@ -907,10 +1192,10 @@ void forward_go(const AttentionArgs &a, hipStream_t s)
 template <class T, int DP>
 void queries_go(const AttentionArgs &a, hipStream_t s)
 {
-    const unsigned blocks = blocks_for(a.items);
+    const dim3 blocks = blocks_for(a.items);
     if (a.grad_table) {
-        if (a.shape == 1) hot_attention_queries_kernel<T, DP, 1, 4, true><<<blocks, 256, a.buckets * 4, s>>>(a);
-        else hot_attention_queries_kernel<T, DP, 2, 4, true><<<blocks, 256, a.buckets * 4, s>>>(a);
+        if (a.shape == 1) hot_attention_queries_kernel<T, DP, 1, 4, true><<<blocks, 256, 4 * a.buckets * 4, s>>>(a);
+        else hot_attention_queries_kernel<T, DP, 2, 4, true><<<blocks, 256, 4 * a.buckets * 4, s>>>(a);
     } else if (a.shape == 1) hot_attention_queries_kernel<T, DP, 1, 4, false><<<blocks, 256, 0, s>>>(a);
     else hot_attention_queries_kernel<T, DP, 2, 4, false><<<blocks, 256, 0, s>>>(a);
 }
@@ -918,7 +1203,15 @@ void queries_go(const AttentionArgs &a, hipStream_t s)
 template <class T, int DP>
 void keys_go(const AttentionArgs &a, hipStream_t s)
 {
-    hot_attention_keys_kernel<T, DP, 1, 4><<<blocks_for(a.items), 256, 0, s>>>(a);
+    if (a.shape == 1) hot_attention_keys_kernel<T, DP, 1, 4><<<blocks_for(a.items), 256, 0, s>>>(a);
+    else hot_attention_keys_kernel<T, DP, 2, 4><<<blocks_for(a.items), 256, 0, s>>>(a);
+}
+
+template <class T>
+void sum_go(const SumArgs &x, const SumArgs &y, hipStream_t s)
+{
+    const long blocks = (x.rows + 15) / 16;
+    hot_attention_sum_kernel<T><<<dim3((unsigned)(blocks < 8192 ? blocks : 8192), y.to ? 2 : 1), 256, 0, s>>>(x, y);
 }
 
 #define HOT_BY_WIDTH(GO)                    \
@@ -934,7 +1227,9 @@ namespace hot_detail {
 template <class T>
 void attention_begin(const AttentionArgs &a, hipStream_t s)
 {
-    const long n = (long)a.tables * a.heads * a.codes, all = n > a.bounds_count ? n : a.bounds_count;
+    const long n = (long)a.tables * a.heads * a.codes, spans = 64L * a.groups * (((a.queries + 63) >> 6) + ((a.keys + 63) >> 6));
+    long all = n > a.bounds_count ? n : a.bounds_count;
+    all = all > spans ? all : spans;
     if (!all) return;
     const long blocks = (all + 255) / 256;
     hot_attention_begin_kernel<<<(unsigned)(blocks < 2048 ? blocks : 2048), 256, 0, s>>>(a);
@@ -953,7 +1248,7 @@ void attention_forward(const AttentionArgs &a, hipStream_t s)
 template <class T>
 void attention_prepare(const AttentionArgs &a, hipStream_t s)
 {
-    const long blocks = (a.all_rows + (__is_same(T, _Float16) ? (long)a.batch * a.kv_heads * a.keys : 0) + 15) / 16;
+    const long blocks = (a.all_rows + (__is_same(T, _Float16) ? (long)a.batch * a.kv_heads * a.keys : 0) + kPrepareRows - 1) / kPrepareRows;
     hot_attention_prepare_kernel<T><<<(unsigned)(blocks < 8192 ? blocks : 8192), 256, 0, s>>>(a);
 }
 
@@ -961,6 +1256,11 @@ template <class T>
 void attention_keys(const AttentionArgs &a, hipStream_t s)
 {
     HOT_BY_WIDTH(keys_go);
+    if (a.splits > 1) {
+        const long rows = (long)a.batch * a.kv_heads * a.keys;
+        const SumArgs k = {a.part_k, a.grad_k, a.p_gk, a.splits, a.keys, a.kv_heads, a.width, rows}, v = {a.part_v, a.grad_v, a.p_gv, a.splits, a.keys, a.kv_heads, a.width, rows};
+        sum_go<T>(k, v, s);
+    }
 }
 
 template <class T>
@@ -968,6 +1268,10 @@ void attention_queries(const AttentionArgs &a, hipStream_t s)
 {
     if (a.items) {
         HOT_BY_WIDTH(queries_go);
+    }
+    if (a.items && a.grad_q && a.splits > 1) {
+        const SumArgs q = {a.part_o, a.grad_q, a.p_gq, a.splits, a.queries, a.heads, a.width, a.all_rows};
+        sum_go<T>(q, SumArgs{}, s);
     }
     if (a.grad_table) hot_attention_table_kernel<<<dim3((unsigned)((a.buckets + 63) / 64), (unsigned)a.heads, (unsigned)a.tables), 1024, 0, s>>>(a);
 }

@@ -15,6 +15,8 @@ namespace {
 
 using hot_detail::AttentionArgs;
 
+bool aligned8(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 7u) == 0; }
+
 constexpr long kMostRows = 0x7FFFFFFFL;
 
 bool attention_ok(const hot_attention_desc *d)
@@ -65,13 +67,13 @@ Cut forward_cut(const hot_attention_desc &d)
 }
 
 struct BackwardCut {
-    int shape, tiles, chunk;
+    int shape, tiles, chunk, splits, by_head;
     long items;
 };
 
 BackwardCut queries_cut(const hot_attention_desc &d)
 {
-    BackwardCut c;
+    BackwardCut c = {};
     c.shape = d.queries <= 64 ? 1 : 2;
     const int tile = c.shape == 1 ? 64 : 128;
     c.tiles = (int)((d.queries + tile - 1) / tile);
@@ -81,33 +83,66 @@ BackwardCut queries_cut(const hot_attention_desc &d)
     c.chunk = (int)(all / 8192 + 1);
     if (c.chunk > entries) c.chunk = entries < 1 ? 1 : (int)entries;
     c.items = sets * ((entries + c.chunk - 1) / c.chunk) * d.heads * c.tiles;
+    long splits = c.items ? 512 / c.items : 1;
+    const long most = (d.keys + 63) / 64 / 4;
+    splits = splits < most ? splits : most;
+    c.splits = splits < 2 ? 1 : (int)splits;
+    c.items *= c.splits;
+    return c;
+}
+
+BackwardCut keys_cut(const hot_attention_desc &d)
+{
+    BackwardCut c = {};
+    c.shape = d.keys <= 64 ? 1 : 2;
+    const int tile = c.shape == 1 ? 64 : 128, per = d.heads / d.kv_heads;
+    c.tiles = (int)((d.keys + tile - 1) / tile);
+    c.items = (long)d.batch * d.kv_heads * c.tiles;
+    // few workgroups, whose work is of unequal length where order counts: heads of a key head apart, then runs of queries
+    const long want = c.items ? 1024 / c.items : 1, tiles_q = (d.queries + 63) / 64;
+    c.splits = 1;
+    if (want > 1) {
+        c.by_head = per > 1;
+        long runs = c.by_head ? want / per : want;
+        runs = runs < tiles_q / 4 ? runs : tiles_q / 4;
+        c.splits = (int)((runs < 1 ? 1 : runs) * (c.by_head ? per : 1));
+    }
+    c.items *= c.splits;
     return c;
 }
 
 long up16(long bytes) { return (bytes + 15) & ~15L; }
 
 struct Room {
-    long bias, part_o, part_ml, d, bounds, parts, all;
+    long query_spans, key_spans, part_o, part_ml, d, bounds, parts, part_k, part_v, all;
 };
 
 Room room_of(const hot_attention_desc &d, bool backward)
 {
     Room r = {};
+    long at = 0;
+    const auto take = [&](long bytes) {
+        const long here = at;
+        at += up16(bytes);
+        return here;
+    };
     const long rows = (long)d.batch * d.heads * d.queries;
-    long at = d.tables ? up16((long)d.tables * d.heads * d.codes * 4) : 0;
+    take(d.tables ? (long)d.tables * d.heads * d.codes * 4 : 0);
+    r.query_spans = take((long)d.groups * ((d.queries + 63) / 64) * 8);
+    r.key_spans = take((long)d.groups * ((d.keys + 63) / 64) * 8);
     if (!backward) {
-        const Cut c = forward_cut(d);
-        r.part_o = at;
-        if (c.splits > 1) at += up16((long)c.splits * rows * d.width * 4);
-        r.part_ml = at;
-        if (c.splits > 1) at += up16((long)c.splits * rows * 8);
+        const long splits = forward_cut(d).splits;
+        r.part_o = take(splits > 1 ? splits * rows * d.width * 4 : 0);
+        r.part_ml = take(splits > 1 ? splits * rows * 8 : 0);
     } else {
-        r.d = at;
-        at += up16(rows * 4);
-        r.bounds = at;
-        at += up16((long)d.batch * (d.heads + d.kv_heads) * 4);
-        r.parts = at;
-        at += up16(d.tables ? queries_cut(d).items * d.buckets * 4 : 0);
+        const BackwardCut q = queries_cut(d), k = keys_cut(d);
+        r.d = take(rows * 4);
+        r.bounds = take((long)d.batch * (d.heads + d.kv_heads) * 4);
+        r.parts = take(d.tables ? q.items * d.buckets * 4 : 0);
+        r.part_o = take(q.splits > 1 ? q.splits * rows * d.width * 4 : 0);
+        const long part = k.splits > 1 ? (long)k.splits * d.batch * d.kv_heads * d.keys * d.width * 4 : 0;
+        r.part_k = take(part);
+        r.part_v = take(part);
     }
     r.all = at;
     return r;
@@ -129,6 +164,7 @@ AttentionArgs args_of(const hot_attention_desc &d)
     a.codes = d.codes;
     a.groups = d.groups;
     a.causal = d.causal != 0;
+    a.first_query = d.first_query;
     a.table_type = d.table_dtype;
     a.pack = a.splits = a.chunk = 1;
     a.all_rows = (long)d.batch * d.heads * d.queries;
@@ -146,13 +182,13 @@ AttentionArgs args_of(const hot_attention_desc &d)
 }
 
 // The arrays that both calls read; false if one is missing or off its grid
-bool give(AttentionArgs &a, const hot_attention_desc &d, const void *q, const void *k, const void *v, const void *table, const int32_t *query_code, const int32_t *key_code,
-          const int32_t *key_range, const int32_t *bucket, const int32_t *query_groups, const int32_t *key_groups)
+bool give(AttentionArgs &a, const hot_attention_desc &d, const Room &r, char *ws, const void *q, const void *k, const void *v, const void *table, const int32_t *query_code,
+          const int32_t *key_code, const int32_t *query_range, const int32_t *key_range, const int32_t *bucket, const int32_t *query_groups, const int32_t *key_groups)
 {
     if (a.all_rows && (!q || !on_element(q, d.dtype))) return false;
     if (d.keys && d.batch && (!k || !v || !on_element(k, d.dtype) || !on_element(v, d.dtype))) return false;
-    if (d.tables && (!table || !query_code || !key_code || !key_range || !bucket || !on_element(table, d.table_dtype) || !aligned4(query_code) || !aligned4(key_code) ||
-                     !aligned4(key_range) || !aligned4(bucket)))
+    if (d.tables && (!table || !query_code || !key_code || !query_range || !key_range || !bucket || !on_element(table, d.table_dtype) || !aligned4(query_code) ||
+                     !aligned4(key_code) || !aligned8(query_range) || !aligned8(key_range) || !aligned8(bucket)))
         return false;
     if (d.groups && (!query_groups || !key_groups || !aligned4(query_groups) || !aligned4(key_groups))) return false;
     a.q = q;
@@ -161,10 +197,15 @@ bool give(AttentionArgs &a, const hot_attention_desc &d, const void *q, const vo
     a.table = table;
     a.query_code = query_code ? query_code + d.first_query : nullptr;
     a.key_code = key_code;
-    a.key_range = key_range;
-    a.bucket = bucket;
+    a.query_range = reinterpret_cast<const int2 *>(query_range);
+    a.key_range = reinterpret_cast<const int2 *>(key_range);
+    a.bucket = reinterpret_cast<const int2 *>(bucket);
     a.query_groups = query_groups;
     a.key_groups = key_groups;
+    a.bias = reinterpret_cast<float *>(ws);
+    a.query_spans = reinterpret_cast<int2 *>(ws + r.query_spans);
+    a.key_spans = reinterpret_cast<int2 *>(ws + r.key_spans);
+    a.part_o = reinterpret_cast<float *>(ws + r.part_o);
     return true;
 }
 
@@ -187,18 +228,18 @@ int64_t hot_attention_workspace_bytes(const hot_attention_desc *desc, int which)
 }
 
 int hot_attention_forward(const hot_attention_desc *desc, const void *q, const void *k, const void *v, const void *table, const int32_t *query_code,
-                          const int32_t *key_code, const int32_t *key_range, const int32_t *bucket, const int32_t *query_groups, const int32_t *key_groups, void *o,
+                          const int32_t *key_code, const int32_t *query_range, const int32_t *key_range, const int32_t *bucket, const int32_t *query_groups, const int32_t *key_groups, void *o,
                           void *rest, float *stats, void *workspace, int64_t workspace_bytes, void *stream)
 {
     if (!attention_ok(desc)) return HOT_EINVAL;
     AttentionArgs a = args_of(*desc);
-    if (!give(a, *desc, q, k, v, table, query_code, key_code, key_range, bucket, query_groups, key_groups)) return HOT_EINVAL;
-    if (a.all_rows == 0) return HOT_OK;
+    char *const ws = static_cast<char *>(workspace);
     const Room r = room_of(*desc, false);
+    if (!give(a, *desc, r, ws, q, k, v, table, query_code, key_code, query_range, key_range, bucket, query_groups, key_groups)) return HOT_EINVAL;
+    if (a.all_rows == 0) return HOT_OK;
     if (!o || !on_element(o, desc->dtype) || !on_element(rest, desc->dtype) || (rest && desc->dtype == HOT_F32) || !aligned4(stats) ||
         (r.all && (!workspace || !aligned16(workspace) || workspace_bytes < r.all)))
         return HOT_EINVAL;
-    char *const ws = static_cast<char *>(workspace);
     const Cut c = forward_cut(*desc);
     a.pack = c.pack;
     a.shape = c.shape;
@@ -208,8 +249,6 @@ int hot_attention_forward(const hot_attention_desc *desc, const void *q, const v
     a.o = o;
     a.rest = rest;
     a.stats = stats;
-    a.bias = reinterpret_cast<float *>(ws);
-    a.part_o = reinterpret_cast<float *>(ws + r.part_o);
     a.part_ml = reinterpret_cast<float *>(ws + r.part_ml);
     hipStream_t s = static_cast<hipStream_t>(stream);
     HOT_BY_TYPE(attention_begin, a);
@@ -218,21 +257,21 @@ int hot_attention_forward(const hot_attention_desc *desc, const void *q, const v
 }
 
 int hot_attention_backward(const hot_attention_desc *desc, const void *q, const void *k, const void *v, const void *table, const int32_t *query_code,
-                           const int32_t *key_code, const int32_t *key_range, const int32_t *bucket, const int32_t *query_groups, const int32_t *key_groups, const void *o,
+                           const int32_t *key_code, const int32_t *query_range, const int32_t *key_range, const int32_t *bucket, const int32_t *query_groups, const int32_t *key_groups, const void *o,
                            const void *rest, const float *stats, const void *grad_o, void *grad_q, void *grad_k, void *grad_v, void *grad_table, void *workspace,
                            int64_t workspace_bytes, void *stream)
 {
     if (!attention_ok(desc)) return HOT_EINVAL;
     AttentionArgs a = args_of(*desc);
-    if (!give(a, *desc, q, k, v, table, query_code, key_code, key_range, bucket, query_groups, key_groups)) return HOT_EINVAL;
-    const int t = desc->dtype;
+    char *const ws = static_cast<char *>(workspace);
     const Room r = room_of(*desc, true);
+    if (!give(a, *desc, r, ws, q, k, v, table, query_code, key_code, query_range, key_range, bucket, query_groups, key_groups)) return HOT_EINVAL;
+    const int t = desc->dtype;
     if (!on_element(grad_q, t) || !on_element(grad_k, t) || !on_element(grad_v, t) || !on_element(grad_table, desc->table_dtype) || (grad_table && !desc->tables) ||
         (r.all && (!workspace || !aligned16(workspace) || workspace_bytes < r.all)))
         return HOT_EINVAL;
     if (a.all_rows && (!o || !stats || !grad_o || !on_element(o, t) || !on_element(rest, t) || (rest && t == HOT_F32) || !aligned4(stats) || !on_element(grad_o, t)))
         return HOT_EINVAL;
-    char *const ws = static_cast<char *>(workspace);
     a.o = const_cast<void *>(o);
     a.rest = const_cast<void *>(rest);
     a.stats = const_cast<float *>(stats);
@@ -241,10 +280,11 @@ int hot_attention_backward(const hot_attention_desc *desc, const void *q, const 
     a.grad_k = grad_k;
     a.grad_v = grad_v;
     a.grad_table = grad_table;
-    a.bias = reinterpret_cast<float *>(ws);
     a.d = reinterpret_cast<float *>(ws + r.d);
     a.bounds = reinterpret_cast<unsigned *>(ws + r.bounds);
     a.parts = reinterpret_cast<float *>(ws + r.parts);
+    a.part_k = reinterpret_cast<float *>(ws + r.part_k);
+    a.part_v = reinterpret_cast<float *>(ws + r.part_v);
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (a.all_rows) {
         a.bounds_count = t == HOT_F16 ? (long)desc->batch * (desc->heads + desc->kv_heads) : 0;
@@ -252,8 +292,12 @@ int hot_attention_backward(const hot_attention_desc *desc, const void *q, const 
         HOT_BY_TYPE(attention_prepare, a);
     }
     if ((grad_k || grad_v) && desc->keys && desc->batch) {
-        a.tiles_k = (int)((desc->keys + 63) / 64);
-        a.items = (long)desc->batch * desc->kv_heads * a.tiles_k;
+        const BackwardCut c = keys_cut(*desc);
+        a.shape = c.shape;
+        a.tiles_k = c.tiles;
+        a.splits = c.splits;
+        a.by_head = c.by_head;
+        a.items = c.items;
         HOT_BY_TYPE(attention_keys, a);
     }
     if ((grad_q && a.all_rows) || grad_table) {
@@ -261,6 +305,7 @@ int hot_attention_backward(const hot_attention_desc *desc, const void *q, const 
         a.shape = c.shape;
         a.tiles_q = c.tiles;
         a.chunk = c.chunk;
+        a.splits = c.splits;
         a.items = c.items;
         HOT_BY_TYPE(attention_queries, a);
     }

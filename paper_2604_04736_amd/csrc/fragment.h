@@ -113,15 +113,49 @@ struct Rows {
     }
 };
 
-// Eight neighbouring elements of a row of n in memory, zeros behind its end, on any element's address
+// The N elements of a vector moved down by `by` (the same for all lanes), zeros behind them
+template <int N, class V>
+__device__ __forceinline__ V moved_down(V v, int by)
+{
+#pragma unroll 1
+    for (; by > 0; --by) {
+#pragma unroll
+        for (int j = 0; j + 1 < N; ++j) v[j] = v[j + 1];
+        v[N - 1] = 0;
+    }
+    return v;
+}
+
+// The first `n` < N elements of a row, zeros behind them
+template <int N, class V, class T>
+__device__ __forceinline__ V few_of(const T *row, int n)
+{
+    V v = (V)((T)0.0f);
+#pragma unroll 1
+    for (int k = n - 1; k >= 0; --k) {
+#pragma unroll
+        for (int j = N - 1; j > 0; --j) v[j] = v[j - 1];
+        v[0] = row[k];
+    }
+    return v;
+}
+
+// Eight neighbouring elements of a row of n in memory, zeros behind its end and where `there` is false, on any element's address.  Nothing branches around a
+// load: the compiler would wait for each before the next (a row of the tensor is there to be read in any case, what was read is dropped).  Pieces behind
+// the row's end are read from where it ends.
 template <class T>
-__device__ __forceinline__ V8<T> eight(const T *row, int at, int n)
+__device__ __forceinline__ V8<T> eight(const T *row, int at, int n, bool there)
 {
     typedef V8<T> Loose __attribute__((aligned(sizeof(T))));
-    if (at + 8 <= n) return *reinterpret_cast<const Loose *>(row + at);
     V8<T> v;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = at + j < n ? row[at + j] : (T)0.0f;
+    if (n >= 8) {
+        v = *reinterpret_cast<const Loose *>(row + (at + 8 <= n ? at : n - 8));
+        if (n & 7) {
+            const V8<T> low = moved_down<8>(v, 8 - (n & 7));
+            if (at + 8 > n) v = low;
+        }
+    } else v = few_of<8, V8<T>>(row, n);
+    if (!there || at >= n) v = (V8<T>)((T)0.0f);
     return v;
 }
 

@@ -650,7 +650,7 @@ Tensor attention_room(const hot_attention_desc &d, int which, const Tensor &like
 
 struct Attention : torch::autograd::Function<Attention> {
     static Tensor forward(AutogradContext *ctx, const Tensor &q_, const Tensor &k_, const Tensor &v_, const MaybeTensor &maybe_table, const MaybeTensor &query_code,
-                          const MaybeTensor &key_code, const MaybeTensor &key_range, const MaybeTensor &bucket, const MaybeTensor &query_groups, const MaybeTensor &key_groups,
+                          const MaybeTensor &key_code, const MaybeTensor &query_range, const MaybeTensor &key_range, const MaybeTensor &bucket, const MaybeTensor &query_groups, const MaybeTensor &key_groups,
                           int64_t first_query, double scale, bool causal)
     {
         const c10::DeviceGuard guard(q_.device());
@@ -663,11 +663,11 @@ struct Attention : torch::autograd::Function<Attention> {
         const Tensor stats = keep ? at::empty({q.size(0), q.size(1), q.size(2), 2}, q.options().dtype(at::kFloat)) : Tensor();
         const Tensor rest = keep && d.dtype != HOT_F32 ? token_major(q) : Tensor();
         const Tensor ws = attention_room(d, 0, q);
-        check(hot_attention_forward(&d, raw(q), raw(k), raw(v), raw(table), codes(given(query_code)), codes(given(key_code)), codes(given(key_range)), codes(given(bucket)), codes(qg),
-                                    codes(kg), raw_mut(o), raw_mut(rest), stats.defined() ? stats.mutable_data_ptr<float>() : nullptr, raw_mut(ws), ws.numel(), stream_of(q)),
+        check(hot_attention_forward(&d, raw(q), raw(k), raw(v), raw(table), codes(given(query_code)), codes(given(key_code)), codes(given(query_range)), codes(given(key_range)),
+                                    codes(given(bucket)), codes(qg), codes(kg), raw_mut(o), raw_mut(rest), stats.defined() ? stats.mutable_data_ptr<float>() : nullptr, raw_mut(ws), ws.numel(), stream_of(q)),
               "hot_attention_forward");
         if (keep) {
-            ctx->save_for_backward({q, k, v, table, given(query_code), given(key_code), given(key_range), given(bucket), qg, kg, o, rest, stats});
+            ctx->save_for_backward({q, k, v, table, given(query_code), given(key_code), given(query_range), given(key_range), given(bucket), qg, kg, o, rest, stats});
             ctx->saved_data["whole"] = std::vector<int64_t>{first_query, causal};
             ctx->saved_data["scale"] = scale;
             ctx->saved_data["q"] = q_.sizes().vec();
@@ -678,14 +678,14 @@ struct Attention : torch::autograd::Function<Attention> {
 
     static variable_list backward(AutogradContext *ctx, variable_list grads)
     {
-        variable_list none(13);
+        variable_list none(14);
         if (!grads[0].defined()) return none;
         const variable_list s = ctx->get_saved_variables();
-        const Tensor &q = s[0], &k = s[1], &v = s[2], &table = s[3], &o = s[10], &rest = s[11], &stats = s[12];
+        const Tensor &q = s[0], &k = s[1], &v = s[2], &table = s[3], &o = s[11], &rest = s[12], &stats = s[13];
         const c10::DeviceGuard guard(q.device());
         const auto whole = ctx->saved_data["whole"].toIntVector();
         const Tensor up = four_axes(grads[0]);
-        hot_attention_desc d = attention_desc(q, k, v, table, s[7], s[8], whole[0], ctx->saved_data["scale"].toDouble(), whole[1]);
+        hot_attention_desc d = attention_desc(q, k, v, table, s[8], s[9], whole[0], ctx->saved_data["scale"].toDouble(), whole[1]);
         const Tensor dq = ctx->needs_input_grad(0) ? room_like(q) : Tensor(), dk = ctx->needs_input_grad(1) ? room_like(k) : Tensor(), dv = ctx->needs_input_grad(2) ? room_like(v) : Tensor();
         const Tensor dtable = table.defined() && ctx->needs_input_grad(3) ? at::empty_like(table) : Tensor();
         d.o = pitch_of(o);
@@ -694,7 +694,7 @@ struct Attention : torch::autograd::Function<Attention> {
         if (dk.defined()) d.grad_k = pitch_of(dk);
         if (dv.defined()) d.grad_v = pitch_of(dv);
         const Tensor ws = attention_room(d, 1, q);
-        check(hot_attention_backward(&d, raw(q), raw(k), raw(v), raw(table), codes(s[4]), codes(s[5]), codes(s[6]), codes(s[7]), codes(s[8]), codes(s[9]), raw(o), raw(rest),
+        check(hot_attention_backward(&d, raw(q), raw(k), raw(v), raw(table), codes(s[4]), codes(s[5]), codes(s[6]), codes(s[7]), codes(s[8]), codes(s[9]), codes(s[10]), raw(o), raw(rest),
                                      stats.const_data_ptr<float>(), raw(up), raw_mut(dq), raw_mut(dk), raw_mut(dv), raw_mut(dtable), raw_mut(ws), ws.numel(), stream_of(q)),
               "hot_attention_backward");
         const auto as = [&](const Tensor &t, const char *name) { return t.defined() ? t.reshape(ctx->saved_data[name].toIntVector()) : t; };
@@ -716,8 +716,8 @@ Tensor group_rows(const MaybeTensor &maybe, const char *name, int64_t n, const T
     return (t.dim() == 1 ? t.unsqueeze(0) : t).contiguous();
 }
 
-Tensor attention(const Tensor &q, const Tensor &k, const Tensor &v, const MaybeTensor &table, const MaybeTensor &query_code, const MaybeTensor &key_code, const MaybeTensor &key_range,
-                 const MaybeTensor &bucket, int64_t buckets, const MaybeTensor &query_groups, const MaybeTensor &key_groups, int64_t first_query, double scale, bool causal)
+Tensor attention(const Tensor &q, const Tensor &k, const Tensor &v, const MaybeTensor &table, const MaybeTensor &query_code, const MaybeTensor &key_code, const MaybeTensor &query_range,
+                 const MaybeTensor &key_range, const MaybeTensor &bucket, int64_t buckets, const MaybeTensor &query_groups, const MaybeTensor &key_groups, int64_t first_query, double scale, bool causal)
 {
     elements(q, "q", q);
     elements(k, "k", q);
@@ -737,11 +737,11 @@ Tensor attention(const Tensor &q, const Tensor &k, const Tensor &v, const MaybeT
     if (table) {
         elements(*table, "table", q);
         TORCH_CHECK_TYPE(table->scalar_type() == q.scalar_type() || table->scalar_type() == at::kFloat, "table: need q's type or float32");
-        HOT_NEED(bucket && query_code && key_code && key_range, "table: need positions");
+        HOT_NEED(bucket && query_code && key_code && query_range && key_range, "table: need positions");
         HOT_NEED((table->dim() == 2 || (table->dim() == 3 && n >= 4 && table->size(0) == q.size(0) && table->size(0) >= 1 && table->size(0) <= 65535)) && table->size(-1) == q.size(-3) &&
                      table->size(-2) == buckets,
                  "table: need [", buckets, ", ", q.size(-3), "], or one for each of q's first axis, got ", table->sizes());
-        for (const MaybeTensor *t : {&query_code, &key_code, &key_range, &bucket})
+        for (const MaybeTensor *t : {&query_code, &key_code, &query_range, &key_range, &bucket})
             TORCH_CHECK_TYPE((*t)->is_cuda() && (*t)->device() == q.device() && (*t)->scalar_type() == at::kInt && (*t)->is_contiguous(), "positions: need those of ", q.device());
         HOT_NEED(first_query >= 0 && first_query + q.size(-2) <= query_code->size(0), "first_query: the positions know ", query_code->size(0), " queries, got ", q.size(-2), " from ",
                  first_query, " on");
@@ -759,8 +759,8 @@ Tensor attention(const Tensor &q, const Tensor &k, const Tensor &v, const MaybeT
     }
     const auto there = [](const Tensor &t) { return t.defined() ? MaybeTensor(t) : MaybeTensor(); };
     py::gil_scoped_release others_run;
-    if (!table) return Attention::apply(q, k, v, MaybeTensor(), MaybeTensor(), MaybeTensor(), MaybeTensor(), MaybeTensor(), there(qg), there(kg), 0, scale, causal);
-    return Attention::apply(q, k, v, table, query_code, key_code, key_range, bucket, there(qg), there(kg), first_query, scale, causal);
+    if (!table) return Attention::apply(q, k, v, MaybeTensor(), MaybeTensor(), MaybeTensor(), MaybeTensor(), MaybeTensor(), MaybeTensor(), there(qg), there(kg), 0, scale, causal);
+    return Attention::apply(q, k, v, table, query_code, key_code, query_range, key_range, bucket, there(qg), there(kg), first_query, scale, causal);
 }
 
 }  // namespace
