@@ -702,8 +702,9 @@ int hot_block_backward(const hot_block_desc *desc, const hot_rng *rng, const voi
  * largest code of 64 tokens each, of all that query_code and key_code hold.  All 8-byte aligned.  (Indices outside are taken as the last; other things that do not
  * fit together give other results.)  Groups: int32
  * [groups, queries] and [groups, keys], entry b taking row b mod groups; groups = 0: none.
- * Limits: HOT_ATTENTION_MOST_*; batch x heads x max(queries, keys) below 2^31.
+ * Limits: width 8 to HOT_ATTENTION_MOST_WIDTH, HOT_ATTENTION_MOST_BUCKETS, HOT_ATTENTION_MOST_CODES; batch x heads x max(queries, keys) below 2^31.
  */
+#define HOT_ATTENTION_LEAST_WIDTH 8
 #define HOT_ATTENTION_MOST_WIDTH 128
 #define HOT_ATTENTION_MOST_BUCKETS 4096
 #define HOT_ATTENTION_MOST_CODES 4194304

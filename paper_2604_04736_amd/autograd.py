@@ -492,7 +492,7 @@ class RelativePositions:
 def attention(q, k, v, table=None, positions: RelativePositions | None = None, *, scale: float | None = None, causal: bool = False, query_groups=None, key_groups=None,
               first_query: int = 0) -> torch.Tensor:
     """softmax over the keys of scale q k^T + bias, times v, without scores in memory; differentiable in q, k, v and table.
-    q [..., heads, queries, width], k and v [..., kv heads, keys, width], kv heads dividing heads, width up to 128; float32, bfloat16 or float16, any strides with adjacent
+    q [..., heads, queries, width], k and v [..., kv heads, keys, width], kv heads dividing heads, width 8 to 128; float32, bfloat16 or float16, any strides with adjacent
     elements of a row (the result's and the gradients' tokens lie as [..., tokens, heads, width] where q, k and v are no dense arrays of their own).  scale: 1 / sqrt(width) where None.
     The bias of head h is table[bucket, h] with the bucket of positions for the two tokens' codes: table [buckets, heads], or [S, buckets, heads] with one table per
     weight sample and q [S, ..., heads, queries, width]; q's type or float32.  Query i is query first_query + i of positions, so one object serves single tokens of a

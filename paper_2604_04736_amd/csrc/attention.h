@@ -39,6 +39,20 @@ __device__ __forceinline__ long item_of(long items)
     return id / 8 < per && item < items ? item : -1;
 }
 
+// The same number, of which the compiler does not know it: what is made of it is made where it stands.  (Moved out of loops, the masks of the rows' ends took three hundred scalar
+// registers more than there are, and the places in LDS a hundred vector registers, for which others were spilled.)
+__device__ __forceinline__ int fresh(int x)
+{
+    asm volatile("" : "+s"(x));
+    return x;
+}
+
+__device__ __forceinline__ int fresh_lane(int x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
 // A tile of ROWS rows on its way from memory to LDS: sixteen bytes of a row to a thread, kEach rows apart.  Loads are not branched around (see
 // fragment.h): rows behind the last are read from that one, and are zeros in LDS, as are rows of negative groups.  A row's last piece is read from where it ends; the
 // columns behind the rows' end are zeros from the start (clear) and never written.
@@ -48,69 +62,57 @@ struct Fetch {
     typedef typename P::Loose Loose;
     static constexpr int N = P::N, kSlots = DP / N <= 4 ? 4 : (DP / N <= 8 ? 8 : (DP / N <= 16 ? 16 : 32)), kStep = THREADS / kSlots, kEach = ROWS / kStep;
     static_assert(ROWS % kStep == 0, "");
-    typename P::V v[kEach];
-
-    static __device__ __forceinline__ int row0() { return (int)threadIdx.x / kSlots; }
-    static __device__ __forceinline__ int at() { return (int)threadIdx.x % kSlots * N; }
+    i4 v[kEach];                 // (as whole registers: elements of 16 bits would be taken apart)
 
     static __device__ __forceinline__ void clear(char *tile, int width)
     {
         for (int i = (int)threadIdx.x; i < ROWS * DP; i += THREADS)
-            if (i % DP >= width) *reinterpret_cast<T *>(tile + i / DP * Rows<T, DP>::kPitch + i % DP * (int)sizeof(T)) = (T)0.0f;
+            if (i % DP >= width) *reinterpret_cast<T *>(tile + Rows<T, DP>::place(i / DP, i % DP)) = (T)0.0f;
     }
     // `base`: the tile's first row; last: its last row that is there
     __device__ __forceinline__ void ask(const T *base, long pitch, int last, int width)
     {
-        const int c = at();
+        const int id = fresh_lane((int)threadIdx.x), row0 = id / kSlots, c = id % kSlots * N;
         if (c >= width) return;
-        if (width >= N) {
-            base += c + N <= width ? c : width - N;
+        base += c + N <= width ? c : width - N;
 #pragma unroll
-            for (int i = 0; i < kEach; ++i) {
-                const int r = row0() + i * kStep;
-                v[i] = *reinterpret_cast<const Loose *>(base + (r < last ? r : last) * pitch);
-            }
-        } else
-#pragma unroll
-            for (int i = 0; i < kEach; ++i) {
-                const int r = row0() + i * kStep;
-                v[i] = few_of<N, typename P::V>(base + (r < last ? r : last) * pitch, width);
-            }
+        for (int i = 0; i < kEach; ++i) {
+            const int r = row0 + i * kStep;
+            v[i] = __builtin_bit_cast(i4, (typename P::V)*reinterpret_cast<const Loose *>(base + (r < last ? r : last) * pitch));
+        }
     }
     // bits of this thread's rows that are there: up to the last, and of no negative group
     static __device__ __forceinline__ unsigned rows_there(const int *groups, int last)
     {
         unsigned bits = 0;
         int g[kEach];
+        const int row0 = fresh_lane((int)threadIdx.x) / kSlots;
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            const int r = row0() + i * kStep;
+            const int r = row0 + i * kStep;
             g[i] = groups ? groups[r < last ? r : last] : 0;
         }
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) bits |= (unsigned)(g[i] >= 0 && row0() + i * kStep <= last) << i;
+        for (int i = 0; i < kEach; ++i) bits |= (unsigned)(g[i] >= 0 && row0 + i * kStep <= last) << i;
         return bits;
     }
     __device__ __forceinline__ void put(char *tile, int width, unsigned there) const
     {
-        const int c = at();
+        const int id = fresh_lane((int)threadIdx.x), row0 = id / kSlots, c = id % kSlots * N;
         if (c >= width) return;
-        tile += row0() * Rows<T, DP>::kPitch + c * (int)sizeof(T);
-        if (c + N <= width) {
+        const int skip = c + N > width ? c + N - width : 0;          // elements of the piece that belong to the one before
 #pragma unroll
-            for (int i = 0; i < kEach; ++i) {
-                typename P::V x = v[i];
-                if (!(there >> i & 1u)) x = (typename P::V)((T)0.0f);
-                *reinterpret_cast<typename P::V *>(tile + i * kStep * Rows<T, DP>::kPitch) = x;
+        for (int i = 0; i < kEach; ++i) {
+            const i4 x = there >> i & 1u ? v[i] : i4(0);
+            char *const to = tile + Rows<T, DP>::place(row0 + i * kStep, c);
+            if (!skip) *reinterpret_cast<i4 *>(to) = x;
+            else {
+                const typename P::V e = __builtin_bit_cast(typename P::V, x);
+#pragma unroll
+                for (int j = 1; j < N; ++j)
+                    if (j >= skip) *reinterpret_cast<T *>(to + (j - skip) * (int)sizeof(T)) = e[j];
             }
-            return;
         }
-        const int skip = width >= N ? c + N - width : 0;          // elements of the piece that belong to the one before
-#pragma unroll
-        for (int i = 0; i < kEach; ++i)
-#pragma unroll
-            for (int j = 0; j < N; ++j)
-                if (j >= skip && c + j - skip < width) *reinterpret_cast<T *>(tile + i * kStep * Rows<T, DP>::kPitch + (j - skip) * (int)sizeof(T)) = there >> i & 1u ? v[i][j] : (T)0.0f;
     }
 };
 
@@ -174,18 +176,16 @@ constexpr int kOne = 0, kStaged = 1, kFar = 2;
 template <int THREADS>
 struct Bias {
     static constexpr int kRoom = 4 * THREADS;
-    float v[4], one;
-    int bucket[4];
-    int low, count, form, all;
+    float v, one;
+    int bucket, low, count, form, all;
 
+    // (the first THREADS of what is staged come with the tile's rows; more there are only in wide windows)
     template <bool BUCKETS>
     __device__ __forceinline__ void ask(const AttentionArgs &a, const float *bias, int2 queries, int2 keys)
     {
-        if (!a.tables) {
-            form = kOne;
-            one = 0.0f;
-            return;
-        }
+        form = kOne;
+        one = 0.0f;
+        if (!a.tables) return;
         low = queries.x - keys.y;
         int high = queries.y - keys.x;
         low = low < 0 ? 0 : (low < a.codes ? low : a.codes - 1);
@@ -195,38 +195,26 @@ struct Bias {
         all = run.x;
         one = bias[low];
         form = run.y >= high ? kOne : (count <= kRoom ? kStaged : kFar);
-        if (count > kRoom) return;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int at = (int)threadIdx.x + i * THREADS;
-            if (i * THREADS < count) {
-                v[i] = bias[low + (at < count ? at : 0)];
-                if constexpr (BUCKETS) bucket[i] = a.bucket[low + (at < count ? at : 0)].x;
-            }
-        }
+        const int at = low + ((int)threadIdx.x < count ? (int)threadIdx.x : 0);
+        v = bias[at];
+        if constexpr (BUCKETS) bucket = a.bucket[at].x;
     }
     template <bool BUCKETS>
-    __device__ __forceinline__ void put(float *room, int *buckets, int most) const
+    __device__ __forceinline__ void put(const AttentionArgs &a, const float *bias, float *room, int *buckets) const
     {
         if (form != kStaged) return;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int at = (int)threadIdx.x + i * THREADS;
-            if (at < count) {
-                room[at] = v[i];
-                if constexpr (BUCKETS) buckets[at] = (unsigned)bucket[i] < (unsigned)most ? bucket[i] : most - 1;
-            }
+        const auto within = [&](int b) { return (unsigned)b < (unsigned)a.buckets ? b : a.buckets - 1; };
+        if ((int)threadIdx.x < count) {
+            room[threadIdx.x] = v;
+            if constexpr (BUCKETS) buckets[threadIdx.x] = within(bucket);
+        }
+#pragma unroll 1
+        for (int at = (int)threadIdx.x + THREADS; at < count; at += THREADS) {
+            room[at] = bias[low + at];
+            if constexpr (BUCKETS) buckets[at] = within(a.bucket[low + at].x);
         }
     }
 };
-
-// The same number, of which the compiler does not know it: comparisons with it are made where they stand.  (Moved out of loops, the masks of the rows' ends took
-// three hundred scalar registers more than there are.)
-__device__ __forceinline__ int fresh(int x)
-{
-    asm volatile("" : "+s"(x));
-    return x;
-}
 
 template <int FORM, bool MASKED>
 struct Form {
@@ -319,7 +307,7 @@ template <class T, int DP, int QB, int WAVES, int KT>
 __global__ void __launch_bounds__(64 * WAVES, 2)
 hot_attention_forward_kernel(AttentionArgs a)
 {
-    constexpr int THREADS = 64 * WAVES, KS = DP / 32, DB = DP / 16, KB = KT / 16, TILE = WAVES * QB * 16;
+    constexpr int THREADS = 64 * WAVES, KS = DP / 32, DB = DP / 16, TILE = WAVES * QB * 16;
     typedef Rows<T, DP> R;
     typedef Fetch<T, DP, KT, THREADS> F;
     __shared__ __attribute__((aligned(16))) char k_tile[KT * R::kPitch];
@@ -391,6 +379,10 @@ hot_attention_forward_kernel(AttentionArgs a)
         m[n] = kNone;
         l[n] = 0.0f;
     }
+    bool any = false;
+#pragma unroll
+    for (int n = 0; n < QB; ++n) any = any || at[n].there;
+    const bool busy = __ballot(any) != 0;            // (waves without queries only bring tiles)
     int tile = walk.begin(a.groups ? a.key_spans + (long)(b % a.groups) * ((a.keys + 63) >> 6) : nullptr,
                           a.groups ? span_over(a.query_spans + (long)(b % a.groups) * ((a.queries + 63) >> 6), first_i, last_i) : int2{0, 0}, split * share, end_tile);
     ask(tile);
@@ -402,84 +394,82 @@ hot_attention_forward_kernel(AttentionArgs a)
             codes[threadIdx.x] = next_code;
             groups[threadIdx.x] = next_group;
         }
-        next_bias.template put<false>(staged, nullptr, 0);
-        const int form = next_bias.form, low = next_bias.low;
-        const float one = next_bias.one;
+        next_bias.template put<false>(a, bias, staged, nullptr);
+        const int form = __builtin_amdgcn_readfirstlane(next_bias.form), low = __builtin_amdgcn_readfirstlane(next_bias.low);
+        const float one = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, next_bias.one)));
         __syncthreads();
         const int k0 = tile * KT;
         tile = walk.next(tile);
         ask(tile);
-
-        Block16<T> acc[KB][QB];
+        if (!busy) continue;
+        // 32 keys at a time: their scores and pieces are as many registers as there is room for beside the sums
+#pragma unroll 1
+        for (int c = 0; c < KT / 32; ++c) {
+            const int here = fresh_lane(lane);
+            Block16<T> acc[2][QB];
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                const V8<T> f = R::along(k_tile, kb * 16, s, lane);
+                for (int s = 0; s < KS; ++s) {
+                    const V8<T> f = R::along(k_tile, c * 32 + u * 16, s, here);
 #pragma unroll
-                for (int n = 0; n < QB; ++n) acc[kb][n].mac(f, qf[n][s]);
-            }
-        const Settled settled;
-        float z[KB][QB][4], top[QB];
+                    for (int n = 0; n < QB; ++n) acc[u][n].mac(f, qf[n][s]);
+                }
+            const Settled settled;
+            float z[QB][8], top[QB];
 #pragma unroll
-        for (int n = 0; n < QB; ++n) top[n] = kNone;
-        by_form(form, k0 + KT > few || a.groups, [&](auto how) {
+            for (int n = 0; n < QB; ++n) top[n] = kNone;
+            by_form(form, k0 + KT > few || a.groups, [&](auto how) {
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb) {
-                i4 kc = i4(0), kgr = i4(0);
-                if constexpr (how.kForm != kOne) kc = *reinterpret_cast<const i4 *>(codes + kb * 16 + g * 4);
-                if constexpr (how.kMasked) kgr = *reinterpret_cast<const i4 *>(groups + kb * 16 + g * 4);
+                for (int u = 0; u < 2; ++u) {
+                    const int row0 = c * 32 + u * 16 + g * 4;
+                    i4 kc = i4(0), kgr = i4(0);
+                    if constexpr (how.kForm != kOne) kc = *reinterpret_cast<const i4 *>(codes + row0);
+                    if constexpr (how.kMasked) kgr = *reinterpret_cast<const i4 *>(groups + row0);
 #pragma unroll
-                for (int n = 0; n < QB; ++n) {
-                    const f4 s = acc[kb][n].read(settled);
+                    for (int n = 0; n < QB; ++n) {
+                        const f4 s = acc[u][n].read(settled);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        float add = one;
-                        if constexpr (how.kForm == kStaged) {
-                            const unsigned at_code = (unsigned)(at[n].code - low - kc[i]), last = Bias<THREADS>::kRoom - 1;
-                            add = staged[at_code < last ? at_code : last];
-                        } else if constexpr (how.kForm == kFar) {
-                            const unsigned at_code = (unsigned)(at[n].code - kc[i]), last = (unsigned)a.codes - 1u;
-                            add = a.tables ? bias[(long)(at[n].h - unit * a.pack) * a.codes + (at_code < last ? at_code : last)] : 0.0f;
+                        for (int i = 0; i < 4; ++i) {
+                            float add = one;
+                            if constexpr (how.kForm == kStaged) {
+                                const unsigned at_code = (unsigned)(at[n].code - low - kc[i]), last = Bias<THREADS>::kRoom - 1;
+                                add = staged[at_code < last ? at_code : last];
+                            } else if constexpr (how.kForm == kFar) {
+                                const unsigned at_code = (unsigned)(at[n].code - kc[i]), last = (unsigned)a.codes - 1u;
+                                add = a.tables ? bias[(long)(at[n].h - unit * a.pack) * a.codes + (at_code < last ? at_code : last)] : 0.0f;
+                            }
+                            float x = __builtin_fmaf(s[i], a.scale, add);
+                            if constexpr (how.kMasked) x = (k0 + row0 + i > at[n].last) | (kgr[i] != at[n].group) ? kNone : x;
+                            z[n][u * 4 + i] = x;
+                            top[n] = __builtin_fmaxf(top[n], x);
                         }
-                        float x = __builtin_fmaf(s[i], a.scale, add);
-                        if constexpr (how.kMasked)
-                            if (k0 + kb * 16 + g * 4 + i > at[n].last || (a.groups && kgr[i] != at[n].group)) x = kNone;
-                        z[kb][n][i] = x;
-                        top[n] = __builtin_fmaxf(top[n], x);
                     }
                 }
-            }
-        });
-        float base[QB];
-#pragma unroll
-        for (int n = 0; n < QB; ++n) {
-            top[n] = __builtin_fmaxf(top[n], __shfl_xor(top[n], 16));
-            top[n] = __builtin_fmaxf(top[n], __shfl_xor(top[n], 32));
-            const float now = __builtin_fmaxf(m[n], top[n]);
-            base[n] = now == kNone ? 0.0f : now;
-            if (__ballot(now > m[n])) {
-                const float by = two_to(m[n] - base[n]);
-                l[n] *= by;
-#pragma unroll
-                for (int d = 0; d < DB; ++d) o[d][n].scale(settled, by);
-            }
-            m[n] = now;
-        }
-#pragma unroll
-        for (int c = 0; c < KT / 32; ++c) {
+            });
             Pieces<T> p[QB];
 #pragma unroll
-            for (int n = 0; n < QB; ++n)
+            for (int n = 0; n < QB; ++n) {
+                top[n] = __builtin_fmaxf(top[n], __shfl_xor(top[n], 16));
+                top[n] = __builtin_fmaxf(top[n], __shfl_xor(top[n], 32));
+                const float now = __builtin_fmaxf(m[n], top[n]), base = now == kNone ? 0.0f : now;
+                if (__ballot(now > m[n])) {
+                    const float by = two_to(m[n] - base);
+                    l[n] *= by;
+#pragma unroll
+                    for (int d = 0; d < DB; ++d) o[d][n].scale(settled, by);
+                }
+                m[n] = now;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float e = two_to(z[2 * c + (i >> 2)][n][i & 3] - base[n] + kShift<T>);
+                    const float e = two_to(z[n][i] - base + kShift<T>);
                     l[n] += e;
                     p[n].set(i, e);
                 }
+            }
 #pragma unroll
             for (int d = 0; d < DB; ++d) {
-                const V8<T> f = R::across(v_tile, c * 32, d * 16, lane);
+                const V8<T> f = R::across(v_tile, c * 32, d * 16, here);
 #pragma unroll
                 for (int n = 0; n < QB; ++n) p[n].mac(o[d][n], f);
             }
@@ -672,7 +662,7 @@ hot_attention_keys_kernel(AttentionArgs a)
     __shared__ __attribute__((aligned(16))) int codes[QT], groups[QT];
     __shared__ float staged[Bias<THREADS>::kRoom];
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, g = lane >> 4, col = lane & 15;
-    const int tiles_q = (a.queries + QT - 1) / QT, past = a.keys - a.queries;
+    const int tiles_q = (a.queries + QT - 1) / QT, past = a.keys - a.queries, reach = a.causal ? past : 0x7FFFFF00;        // (added to less than 256)
     F::clear(q_tile, a.width);
     F::clear(up_tile, a.width);
 
@@ -710,6 +700,10 @@ hot_attention_keys_kernel(AttentionArgs a)
     const int last_key = (tile_k + 1) * TILE < a.keys ? (tile_k + 1) * TILE - 1 : a.keys - 1;
     const int2 key_codes = a.tables ? span_over(a.key_range, tile_k * TILE, last_key) : int2{0, 0};
     const int2 mine = a.groups ? span_over(a.key_spans + (long)(b % a.groups) * ((a.keys + 63) >> 6), tile_k * TILE, last_key) : int2{0, 0};
+    bool any = false;
+#pragma unroll
+    for (int n = 0; n < KB; ++n) any = any || group[n] >= 0;
+    const bool busy = __ballot(any) != 0;                // (waves without keys only bring tiles)
     Block16<T> dk[DB][KB], dv[DB][KB];
     const float unit = unit_of<T>(a, b, kvh * a.per, a.per);
     // from the first query that sees a key of this tile on
@@ -760,23 +754,25 @@ hot_attention_keys_kernel(AttentionArgs a)
                 codes[threadIdx.x] = next_code;
                 groups[threadIdx.x] = next_group;
             }
-            next_bias.template put<false>(staged, nullptr, 0);
-            const int form = next_bias.form, low = next_bias.low;
-            const float one = next_bias.one;
+            next_bias.template put<false>(a, bias, staged, nullptr);
+            const int form = __builtin_amdgcn_readfirstlane(next_bias.form), low = __builtin_amdgcn_readfirstlane(next_bias.low);
+            const float one = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, next_bias.one)));
             __syncthreads();
             const int i0 = tile * QT;
             tile = walk.next(tile);
             ask(tile);
+            if (!busy) continue;
             // (queries behind the last have l = infinity, keys behind the last are zeros and are not stored)
             const bool masked = a.groups || (a.causal && i0 + past < last_key);
-#pragma unroll
+#pragma unroll 1
             for (int c = 0; c < QT / 32; ++c) {
+                const int at = fresh_lane(lane);
                 Block16<T> s[2][KB], dp[2][KB];
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
 #pragma unroll
                     for (int x = 0; x < KS; ++x) {
-                        const V8<T> fq = R::along(q_tile, c * 32 + u * 16, x, lane), fu = R::along(up_tile, c * 32 + u * 16, x, lane);
+                        const V8<T> fq = R::along(q_tile, c * 32 + u * 16, x, at), fu = R::along(up_tile, c * 32 + u * 16, x, at);
 #pragma unroll
                         for (int n = 0; n < KB; ++n) {
                             s[u][n].mac(fq, kf[n][x]);
@@ -809,7 +805,7 @@ hot_attention_keys_kernel(AttentionArgs a)
                                 float e = two_to(__builtin_fmaf(zs[i], a.scale, add) - m[i] - l[i] + kShift<T>);
                                 float w = e * ((dps[i] - d[i]) * (unit * (__is_same(T, _Float16) ? 0x1p-14f : 1.0f)));
                                 if constexpr (how.kMasked)
-                                    if ((a.groups && group[n] != qgr[i]) || (a.causal && key[n] > i0 + row0 + i + past)) e = w = 0.0f;
+                                    if ((group[n] != qgr[i]) | (key[n] - i0 > row0 + i + reach)) e = w = 0.0f;
                                 p[n].set(u * 4 + i, e);
                                 dz[n].set(u * 4 + i, w);
                             }
@@ -818,7 +814,7 @@ hot_attention_keys_kernel(AttentionArgs a)
                 });
 #pragma unroll
                 for (int x = 0; x < DB; ++x) {
-                    const V8<T> fu = R::across(up_tile, c * 32, x * 16, lane), fq = R::across(q_tile, c * 32, x * 16, lane);
+                    const V8<T> fu = R::across(up_tile, c * 32, x * 16, at), fq = R::across(q_tile, c * 32, x * 16, at);
 #pragma unroll
                     for (int n = 0; n < KB; ++n) {
                         p[n].mac(dv[x][n], fu);
@@ -897,16 +893,17 @@ hot_attention_queries_kernel(AttentionArgs a)
     __shared__ __attribute__((aligned(16))) char k_tile[KT * R::kPitch];
     __shared__ __attribute__((aligned(16))) char v_tile[KT * R::kPitch];
     __shared__ __attribute__((aligned(16))) int codes[KT], groups[KT];
-    __shared__ float staged[Bias<THREADS>::kRoom];
+    __shared__ float staged[Bias<THREADS>::kRoom + 64];          // (the last 64, and those of the bins, are for pairs that do not count: a place for each lane)
     __shared__ int staged_bucket[BINS];
-    __shared__ float all_bins[WAVES * BINS];
+    __shared__ float all_bins[WAVES * (BINS + 64)];
     extern __shared__ float all_sums[];          // [waves, buckets]
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, g = lane >> 4, col = lane & 15;
-    float *const bins = all_bins + wave * BINS, *const sums = all_sums + wave * a.buckets;
+    float *const bins = all_bins + wave * (BINS + 64), *const sums = all_sums + wave * a.buckets;
     F::clear(k_tile, a.width);
     F::clear(v_tile, a.width);
     if constexpr (TABLE)
-        for (int i = lane; i < BINS; i += 64) bins[i] = 0.0f;
+        for (int i = lane; i < BINS + 64; i += 64) bins[i] = 0.0f;
+    staged[Bias<THREADS>::kRoom + lane] = 0.0f;
     auto add = [](float *to, float x) { __hip_atomic_fetch_add(to, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT); };
 
     long item = item_of(a.items);
@@ -960,6 +957,7 @@ hot_attention_queries_kernel(AttentionArgs a)
             if (!at[n].there) {
                 m[n] = dd[n] = 0.0f;
                 l[n] = __builtin_inff();
+                at[n].code = kMostCode;          // (beyond what is staged)
             } else {
                 code_low = at[n].code < code_low ? at[n].code : code_low;
                 code_high = at[n].code > code_high ? at[n].code : code_high;
@@ -999,6 +997,10 @@ hot_attention_queries_kernel(AttentionArgs a)
             next_range = a.tables ? a.key_range[tile] : int2{0, 0};
             next_bias.template ask<TABLE>(a, bias, mine_codes, next_range);
         };
+        bool any = false;
+#pragma unroll
+        for (int n = 0; n < QB; ++n) any = any || at[n].there;
+        const bool busy = __ballot(any) != 0;            // (waves without queries only bring tiles)
         Block16<T> dq[DB][QB];
         int tile = walk.begin(a.groups ? a.key_spans + (long)(b % a.groups) * ((a.keys + 63) >> 6) : nullptr,
                               a.groups ? span_over(a.query_spans + (long)(b % a.groups) * ((a.queries + 63) >> 6), first_i, last_i) : int2{0, 0}, split * share, end_tile);
@@ -1011,24 +1013,26 @@ hot_attention_queries_kernel(AttentionArgs a)
                 codes[threadIdx.x] = next_code;
                 groups[threadIdx.x] = next_group;
             }
-            next_bias.template put<TABLE>(staged, staged_bucket, a.buckets);
-            const int form = next_bias.form, low = next_bias.low, bucket = next_bias.all;
+            next_bias.template put<TABLE>(a, bias, staged, staged_bucket);
+            const int form = __builtin_amdgcn_readfirstlane(next_bias.form), low = __builtin_amdgcn_readfirstlane(next_bias.low), bucket = __builtin_amdgcn_readfirstlane(next_bias.all);
             const int2 range = next_range;
-            const float one = next_bias.one;
+            const float one = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, next_bias.one)));
             __syncthreads();
             const int k0 = tile * KT;
             tile = walk.next(tile);
             ask(tile);
+            if (!busy) continue;
             const bool masked = k0 + KT > few || a.groups;
             float here = 0.0f;
-#pragma unroll
+#pragma unroll 1
             for (int c = 0; c < KT / 32; ++c) {
+                const int own = fresh_lane(lane);
                 Block16<T> s[2][QB], dp[2][QB];
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
 #pragma unroll
                     for (int x = 0; x < KS; ++x) {
-                        const V8<T> fk = R::along(k_tile, c * 32 + u * 16, x, lane), fv = R::along(v_tile, c * 32 + u * 16, x, lane);
+                        const V8<T> fk = R::along(k_tile, c * 32 + u * 16, x, own), fv = R::along(v_tile, c * 32 + u * 16, x, own);
 #pragma unroll
                         for (int n = 0; n < QB; ++n) {
                             s[u][n].mac(fk, qf[n][x]);
@@ -1051,10 +1055,12 @@ hot_attention_queries_kernel(AttentionArgs a)
                             for (int i = 0; i < 4; ++i) {
                                 float bias_here = one;
                                 unsigned at_code = 0;
+                                const bool sees = !how.kMasked || !((k0 + row0 + i > at[n].last) | (kgr[i] != at[n].group));
                                 if constexpr (how.kForm == kStaged) {
-                                    constexpr unsigned last = Bias<THREADS>::kRoom - 1;
+                                    const unsigned none = (unsigned)(Bias<THREADS>::kRoom + lane);
                                     at_code = (unsigned)(at[n].code - low - kc[i]);
-                                    at_code = at_code < last ? at_code : last;
+                                    at_code = at_code < none ? at_code : none;
+                                    if constexpr (how.kMasked) at_code = sees ? at_code : none;
                                     bias_here = staged[at_code];
                                 } else if constexpr (how.kForm == kFar) {
                                     const unsigned last = (unsigned)a.codes - 1u;
@@ -1064,17 +1070,13 @@ hot_attention_queries_kernel(AttentionArgs a)
                                 }
                                 const float e = two_to(__builtin_fmaf(zs[i], a.scale, bias_here) - m[n] - l[n]);
                                 float w = e * (dps[i] - dd[n]);
-                                bool sees = at[n].there;
-                                if constexpr (how.kMasked) {
-                                    sees = !(k0 + row0 + i > at[n].last || (a.groups && kgr[i] != at[n].group));
-                                    if (!sees) w = 0.0f;
-                                }
+                                if constexpr (how.kMasked) w = sees ? w : 0.0f;
                                 dz[n].set(u * 4 + i, w * unit);
                                 if constexpr (TABLE) {
                                     if constexpr (how.kForm == kOne) here += w;
                                     else if constexpr (how.kForm == kStaged) {
-                                        if (sees) add(bins + at_code, w);
-                                    } else if (sees && a.tables) {
+                                        add(bins + at_code, w);
+                                    } else {
                                         const unsigned to = (unsigned)a.bucket[at_code].x, most = (unsigned)a.buckets - 1u;
                                         add(sums + (to < most ? to : most), w);
                                     }
@@ -1085,7 +1087,7 @@ hot_attention_queries_kernel(AttentionArgs a)
                 });
 #pragma unroll
                 for (int x = 0; x < DB; ++x) {
-                    const V8<T> f = R::across(k_tile, c * 32, x * 16, lane);
+                    const V8<T> f = R::across(k_tile, c * 32, x * 16, own);
 #pragma unroll
                     for (int n = 0; n < QB; ++n) dz[n].mac(dq[x][n], f);
                 }
@@ -1203,8 +1205,7 @@ void queries_go(const AttentionArgs &a, hipStream_t s)
 template <class T, int DP>
 void keys_go(const AttentionArgs &a, hipStream_t s)
 {
-    if (a.shape == 1) hot_attention_keys_kernel<T, DP, 1, 4><<<blocks_for(a.items), 256, 0, s>>>(a);
-    else hot_attention_keys_kernel<T, DP, 2, 4><<<blocks_for(a.items), 256, 0, s>>>(a);
+    hot_attention_keys_kernel<T, DP, 1, 4><<<blocks_for(a.items), 256, 0, s>>>(a);
 }
 
 template <class T>

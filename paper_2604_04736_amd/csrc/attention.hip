@@ -21,7 +21,7 @@ constexpr long kMostRows = 0x7FFFFFFFL;
 
 bool attention_ok(const hot_attention_desc *d)
 {
-    if (!d || d->queries < 0 || d->keys < 0 || d->batch < 0 || d->heads < 1 || d->kv_heads < 1 || d->heads % d->kv_heads || d->width < 1 ||
+    if (!d || d->queries < 0 || d->keys < 0 || d->batch < 0 || d->heads < 1 || d->kv_heads < 1 || d->heads % d->kv_heads || d->width < HOT_ATTENTION_LEAST_WIDTH ||
         d->width > HOT_ATTENTION_MOST_WIDTH || d->groups < 0 || !known_type(d->dtype) || !(d->scale >= -1.0e30 && d->scale <= 1.0e30))
         return false;
     // (65535: the last dimension of a grid)
@@ -94,8 +94,7 @@ BackwardCut queries_cut(const hot_attention_desc &d)
 BackwardCut keys_cut(const hot_attention_desc &d)
 {
     BackwardCut c = {};
-    c.shape = d.keys <= 64 ? 1 : 2;
-    const int tile = c.shape == 1 ? 64 : 128, per = d.heads / d.kv_heads;
+    const int tile = 64, per = d.heads / d.kv_heads;
     c.tiles = (int)((d.keys + tile - 1) / tile);
     c.items = (long)d.batch * d.kv_heads * c.tiles;
     // few workgroups, whose work is of unequal length where order counts: heads of a key head apart, then runs of queries
@@ -293,7 +292,6 @@ int hot_attention_backward(const hot_attention_desc *desc, const void *q, const 
     }
     if ((grad_k || grad_v) && desc->keys && desc->batch) {
         const BackwardCut c = keys_cut(*desc);
-        a.shape = c.shape;
         a.tiles_k = c.tiles;
         a.splits = c.splits;
         a.by_head = c.by_head;

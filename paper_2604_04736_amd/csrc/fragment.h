@@ -83,24 +83,45 @@ struct Pieces {
     }
 };
 
-// A tile of rows of DP elements in LDS.  Rows are sixteen bytes longer than their elements, so that sixteen of them read at once are in different banks.
+// A tile of rows of DP elements in LDS.  LDS serves 256 bytes at once if they are in different banks: sixteen lanes of sixteen bytes, which are those of sixteen rows
+// (along), or eight rows of 32 bytes (the transposing read across).  Rows of 16-bit elements have their sixteen-byte pieces permuted by the row so that
+// both are; rows of float32, which the slower instruction bounds, are sixteen bytes longer than their elements.
 template <class T, int DP>
 struct Rows {
-    static constexpr int kPitch = DP * (int)sizeof(T) + 16;
+    static constexpr bool kPermuted = sizeof(T) == 2;
+    static constexpr int kPitch = kPermuted ? (DP <= 32 ? 64 : (DP <= 64 ? 128 : 256)) : DP * (int)sizeof(T) + 16;
 
-    // operand of lines row0 .. + 15 at elements 32 ks ..
+    static __device__ __forceinline__ int turn(int row)
+    {
+        if constexpr (!kPermuted) return 0;
+        else if constexpr (kPitch == 256) return (row & 7) << 1 | (row >> 3 & 1);
+        else if constexpr (kPitch == 128) return (row >> 1 & 3) << 1 | (row >> 3 & 1);
+        else return (row >> 2 & 1) << 1 | (row >> 3 & 1);
+    }
+    // the byte of element `at` (a multiple of sixteen bytes, if the piece as a whole is meant) of a row
+    static __device__ __forceinline__ int place(int row, int at)
+    {
+        const int byte = at * (int)sizeof(T);
+        return row * kPitch + (byte ^ turn(row) << 4);
+    }
+    // operand of lines row0 .. + 15 (row0 a multiple of sixteen) at elements 32 ks ..
     static __device__ __forceinline__ V8<T> along(const char *tile, int row0, int ks, int lane)
     {
-        const char *const at = tile + (row0 + (lane & 15)) * kPitch + (ks * 32 + (lane >> 4) * 8) * (int)sizeof(T);
-        return *reinterpret_cast<const V8<T> *>(at);
+        const int row = lane & 15, at = ks * 32 + (lane >> 4) * 8;
+        if constexpr (kPermuted) return *reinterpret_cast<const V8<T> *>(tile + row0 * kPitch + place(row, at));
+        else {
+            // (sixteen bytes at a time: rows are on no larger boundary)
+            const f4 low = *reinterpret_cast<const f4 *>(tile + row0 * kPitch + place(row, at)), high = *reinterpret_cast<const f4 *>(tile + row0 * kPitch + place(row, at) + 16);
+            return __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
     }
     // operand whose lines are elements e0 .. + 15 and whose 32 indices are rows row0 .. + 31, in the order above
     static __device__ __forceinline__ V8<T> across(const char *tile, int row0, int e0, int lane)
     {
         const int g = lane >> 4, i = lane & 15;
-        if constexpr (sizeof(T) == 2) {
+        if constexpr (kPermuted) {
             // (a transposing read: of four rows of sixteen elements that sixteen lanes name, lane i receives element i of each)
-            lds_char *const at = (lds_char *)(tile + (row0 + 4 * g + (i >> 2)) * kPitch + (e0 + (i & 3) * 4) * 2);
+            lds_char *const at = (lds_char *)(tile + row0 * kPitch + place(4 * g + (i >> 2), e0 + (i & 3) * 4));
             const s4v up = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v *)at);
             const s4v low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v *)(at + 16 * kPitch));
             return __builtin_bit_cast(V8<T>, __builtin_shufflevector(up, low, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -126,21 +147,7 @@ __device__ __forceinline__ V moved_down(V v, int by)
     return v;
 }
 
-// The first `n` < N elements of a row, zeros behind them
-template <int N, class V, class T>
-__device__ __forceinline__ V few_of(const T *row, int n)
-{
-    V v = (V)((T)0.0f);
-#pragma unroll 1
-    for (int k = n - 1; k >= 0; --k) {
-#pragma unroll
-        for (int j = N - 1; j > 0; --j) v[j] = v[j - 1];
-        v[0] = row[k];
-    }
-    return v;
-}
-
-// Eight neighbouring elements of a row of n in memory, zeros behind its end and where `there` is false, on any element's address.  Nothing branches around a
+// Eight neighbouring elements of a row of n >= 8 in memory, zeros behind its end and where `there` is false, on any element's address.  Nothing branches around a
 // load: the compiler would wait for each before the next (a row of the tensor is there to be read in any case, what was read is dropped).  Pieces behind
 // the row's end are read from where it ends.
 template <class T>
@@ -148,13 +155,11 @@ __device__ __forceinline__ V8<T> eight(const T *row, int at, int n, bool there)
 {
     typedef V8<T> Loose __attribute__((aligned(sizeof(T))));
     V8<T> v;
-    if (n >= 8) {
-        v = *reinterpret_cast<const Loose *>(row + (at + 8 <= n ? at : n - 8));
-        if (n & 7) {
-            const V8<T> low = moved_down<8>(v, 8 - (n & 7));
-            if (at + 8 > n) v = low;
-        }
-    } else v = few_of<8, V8<T>>(row, n);
+    v = *reinterpret_cast<const Loose *>(row + (at + 8 <= n ? at : n - 8));
+    if (n & 7) {
+        const V8<T> low = moved_down<8>(v, 8 - (n & 7));
+        if (at + 8 > n) v = low;
+    }
     if (!there || at >= n) v = (V8<T>)((T)0.0f);
     return v;
 }

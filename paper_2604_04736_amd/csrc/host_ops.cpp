@@ -724,7 +724,7 @@ Tensor attention(const Tensor &q, const Tensor &k, const Tensor &v, const MaybeT
     elements(v, "v", q);
     TORCH_CHECK_TYPE(k.scalar_type() == q.scalar_type() && v.scalar_type() == q.scalar_type(), "k and v: need q's type");
     const int64_t n = q.dim();
-    HOT_NEED(n >= 3 && q.size(-1) >= 1 && q.size(-1) <= HOT_ATTENTION_MOST_WIDTH && q.size(-3) >= 1, "q: need [..., heads, queries, width] with a width of 1 to ",
+    HOT_NEED(n >= 3 && q.size(-1) >= HOT_ATTENTION_LEAST_WIDTH && q.size(-1) <= HOT_ATTENTION_MOST_WIDTH && q.size(-3) >= 1, "q: need [..., heads, queries, width] with a width of 8 to ",
              HOT_ATTENTION_MOST_WIDTH, ", got ", q.sizes());
     HOT_NEED(k.dim() == n && k.sizes() == v.sizes() && k.size(-1) == q.size(-1) && k.sizes().slice(0, n - 3) == q.sizes().slice(0, n - 3), "k and v: need one shape, q's leading axes and width ",
              q.sizes(), ", got ", k.sizes(), " and ", v.sizes());
