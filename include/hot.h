@@ -698,8 +698,9 @@ int hot_block_backward(const hot_block_desc *desc, const hot_rng *rng, const voi
  * q, o and their gradients: [batch, heads, queries, width], k and v [batch, kv_heads, keys, width], each with pitches of its own in elements
  * (batch, head, row; elements of a row adjacent).  table: dense [tables, buckets, heads] of table_dtype (dtype or HOT_F32), entry b taking table
  * b / (batch / tables); tables = 0: no bias, and no codes.  query_code, key_code: int32, such that differences lie in 0 .. codes - 1; bucket: int32
- * [codes, 2], the bucket of every difference and the last difference up to which all are of that bucket; query_range, key_range: int32 [tokens / 64 rounded up, 2], the smallest and
- * largest code of 64 tokens each, of all that query_code and key_code hold.  All 8-byte aligned.  (Indices outside are taken as the last; other things that do not
+ * [codes, 2], the bucket of every difference and the last difference up to which all are of that bucket; query_range, key_range: int32 [tokens / 64 rounded up, 4], of 64 tokens each
+ * of all that query_code and key_code hold the smallest and the largest code, and 1 if codes go up by one from each token to the next (that of the next 64 included), else 0, and 0.
+ * bucket is 8-byte, the ranges are 16-byte aligned.  (Indices outside are taken as the last; other things that do not
  * fit together give other results.)  Groups: int32
  * [groups, queries] and [groups, keys], entry b taking row b mod groups; groups = 0: none.
  * Limits: width 8 to HOT_ATTENTION_MOST_WIDTH, HOT_ATTENTION_MOST_BUCKETS, HOT_ATTENTION_MOST_CODES; batch x heads x max(queries, keys) below 2^31.
@@ -722,12 +723,15 @@ typedef struct hot_attention_desc {
     int32_t tables, buckets, codes, first_query;
     int32_t groups, causal;
     int32_t dtype, table_dtype;
+    int32_t loose;                             /* 1: q, k, v or grad_o may lie off the 4-byte grid (16-bit types) */
+    int32_t reserved;
 } hot_attention_desc;
 
 /* Scratch of a call: which = 0 forward, 1 backward. */
 int64_t hot_attention_workspace_bytes(const hot_attention_desc *desc, int which);
 
 /*
+ * Tensors whose rows are no whole 4-byte words on that grid (odd widths or pitches, loose) are copied into the workspace first.
  * stats: fp32 [batch, heads, queries, 2], and rest (o's pitches and type; 16-bit types only): what o's rounding left over.  Both are for the backward call; NULL leaves
  * them out.
  */

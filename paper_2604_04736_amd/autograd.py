@@ -450,7 +450,9 @@ class RelativePositions:
 
         def ranges(code):
             tiles = torch.nn.functional.pad(code, (0, -len(code) % 64), value=int(code[-1])).view(-1, 64)
-            return torch.stack([tiles.amin(1), tiles.amax(1)], 1)
+            steps = torch.ones_like(tiles).view(-1)             # (whether the code behind a token's is one more; the last token has none behind)
+            steps[:len(code) - 1] = code[1:] - code[:-1] == 1
+            return torch.stack([tiles.amin(1), tiles.amax(1), steps.view(-1, 64).amin(1), torch.zeros(len(tiles), dtype=code.dtype)], 1)
 
         # the last difference of the run of equal buckets that each lies in
         ends = torch.cat([bucket[1:] != bucket[:-1], torch.tensor([True])]).nonzero()[:, 0]

@@ -119,7 +119,8 @@ class hot_attention_desc(ctypes.Structure):
                 ("grad_o", hot_pitch), ("grad_q", hot_pitch), ("grad_k", hot_pitch), ("grad_v", hot_pitch), ("scale", ctypes.c_double),
                 ("batch", ctypes.c_int32), ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("width", ctypes.c_int32),
                 ("tables", ctypes.c_int32), ("buckets", ctypes.c_int32), ("codes", ctypes.c_int32), ("first_query", ctypes.c_int32),
-                ("groups", ctypes.c_int32), ("causal", ctypes.c_int32), ("dtype", ctypes.c_int32), ("table_dtype", ctypes.c_int32)]
+                ("groups", ctypes.c_int32), ("causal", ctypes.c_int32), ("dtype", ctypes.c_int32), ("table_dtype", ctypes.c_int32),
+                ("loose", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 class HotError(RuntimeError):
@@ -1124,6 +1125,7 @@ def _attention_desc(q, k, v, o, table, positions, scale, causal, query_groups, k
             if t.shape != like.shape:
                 raise ValueError(f"{name}: need {tuple(like.shape)}, got {tuple(t.shape)}")
     keys = k.shape[2]
+    d.loose = int(any(t.data_ptr() % 4 for t in (q, k, v, *grads[:1]) if t is not None))
     d.queries, d.keys, d.batch, d.heads, d.kv_heads, d.width, d.scale, d.causal, d.dtype = queries, keys, batch, heads, k.shape[1], width, scale, bool(causal), kind
     pointers = [q.data_ptr(), k.data_ptr(), v.data_ptr()] + [None] * 6
     if table is not None:
@@ -1134,7 +1136,7 @@ def _attention_desc(q, k, v, o, table, positions, scale, causal, query_groups, k
             raise ValueError(f"positions: need codes of {first_query + queries} queries and {keys} keys")
         d.tables, d.buckets, d.codes, d.first_query, d.table_dtype = table.shape[0], table.shape[1], bucket.shape[0], first_query, _typed(table, "table", q)
         pointers[3:] = [table.data_ptr(), _whole(query_code, query_code.shape[:1], q, "query_code"), _whole(key_code, key_code.shape[:1], q, "key_code"),
-                        _whole(query_range, ((query_code.shape[0] + 63) // 64, 2), q, "query_range"), _whole(key_range, ((key_code.shape[0] + 63) // 64, 2), q, "key_range"),
+                        _whole(query_range, ((query_code.shape[0] + 63) // 64, 4), q, "query_range"), _whole(key_range, ((key_code.shape[0] + 63) // 64, 4), q, "key_range"),
                         _whole(bucket, (bucket.shape[0], 2), q, "bucket")]
     if (query_groups is None) != (key_groups is None):
         raise ValueError("query_groups and key_groups: need both or neither")

@@ -31,90 +31,117 @@ constexpr float kShift = __is_same(T, _Float16) ? 14.0f : 0.0f;
 
 __device__ __forceinline__ float two_to(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// Workgroups go to the eight dies in turn; each die gets a run of items, so that those which read the same keys share its L2.
+// Which item a workgroup takes.  Splits of one tile lie side by side, then the heads (of all entries), then the tiles, those with the most work first where causal order
+// makes them unequal: the last ones to finish are short, and since workgroups go to the eight dies in turn, a head's tiles stay on one die where heads are a multiple of eight.
 __device__ __forceinline__ long item_of(long items)
 {
     const long id = (long)blockIdx.y * gridDim.x + blockIdx.x;
-    const long per = (items + 7) / 8, item = id % 8 * per + id / 8;
-    return id / 8 < per && item < items ? item : -1;
+    return id < items ? id : -1;
 }
 
-// The same number, of which the compiler does not know it: what is made of it is made where it stands.  (Moved out of loops, the masks of the rows' ends took three hundred scalar
-// registers more than there are, and the places in LDS a hundred vector registers, for which others were spilled.)
-__device__ __forceinline__ int fresh(int x)
-{
-    asm volatile("" : "+s"(x));
-    return x;
-}
-
+// The same number, of which the compiler does not know it: what is made of it is made where it stands.  (Moved out of loops, places in LDS took a hundred registers, for
+// which others were spilled.)
 __device__ __forceinline__ int fresh_lane(int x)
 {
     asm volatile("" : "+v"(x));
     return x;
 }
 
-// A tile of ROWS rows on its way from memory to LDS: sixteen bytes of a row to a thread, kEach rows apart.  Loads are not branched around (see
-// fragment.h): rows behind the last are read from that one, and are zeros in LDS, as are rows of negative groups.  A row's last piece is read from where it ends; the
-// columns behind the rows' end are zeros from the start (clear) and never written.
-template <class T, int DP, int ROWS, int THREADS>
-struct Fetch {
-    typedef Piece<T> P;
-    typedef typename P::Loose Loose;
-    static constexpr int N = P::N, kSlots = DP / N <= 4 ? 4 : (DP / N <= 8 ? 8 : (DP / N <= 16 ? 16 : 32)), kStep = THREADS / kSlots, kEach = ROWS / kStep;
-    static_assert(ROWS % kStep == 0, "");
-    i4 v[kEach];                 // (as whole registers: elements of 16 bits would be taken apart)
+// Tiles in LDS: two of 16-bit elements, one on its way while the other is worked on; one of float32, whose products take longer than its way
+template <class T>
+constexpr int kStages = sizeof(T) == 2 ? 2 : 1;
 
-    static __device__ __forceinline__ void clear(char *tile, int width)
+// Two tiles of ROWS rows straight from memory to LDS, one behind the other, 1024 bytes of LDS to an instruction of a wave, sixteen of them a lane.  What is no element, rows behind the
+// last and rows of negative groups are zeros: the hardware's answer to an offset outside its window.  A lane's places do not change from tile to tile.
+// What of a row is no whole piece goes through registers (tail).
+constexpr unsigned kBeyond = 0x80000000u;
+typedef __amdgpu_buffer_rsrc_t Window;
+
+template <class T, int DP, int ROWS, int WAVES>
+struct Bring {
+    typedef Rows<T, DP, ROWS> R;
+    static constexpr int N = 16 / (int)sizeof(T), kLoads = R::kBytes / 1024, kEach = (kLoads + WAVES - 1) / WAVES;
+    static_assert(64 * WAVES >= 2 * ROWS, "a thread to a row's tail");
+    int row[kEach];
+    unsigned off[2][kEach];
+    T ends[N - 1];
+
+    __device__ __forceinline__ void begin(long pitch0, long pitch1, int width)
     {
-        for (int i = (int)threadIdx.x; i < ROWS * DP; i += THREADS)
-            if (i % DP >= width) *reinterpret_cast<T *>(tile + Rows<T, DP>::place(i / DP, i % DP)) = (T)0.0f;
-    }
-    // `base`: the tile's first row; last: its last row that is there
-    __device__ __forceinline__ void ask(const T *base, long pitch, int last, int width)
-    {
-        const int id = fresh_lane((int)threadIdx.x), row0 = id / kSlots, c = id % kSlots * N;
-        if (c >= width) return;
-        base += c + N <= width ? c : width - N;
+        const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            const int r = row0 + i * kStep;
-            v[i] = __builtin_bit_cast(i4, (typename P::V)*reinterpret_cast<const Loose *>(base + (r < last ? r : last) * pitch));
+            int at;
+            const bool is = R::at_byte((wave + i * WAVES) * 1024 + lane * 16, row[i], at);
+            off[0][i] = (unsigned)(row[i] * (int)pitch0 + at) * (unsigned)sizeof(T);
+            off[1][i] = (unsigned)(row[i] * (int)pitch1 + at) * (unsigned)sizeof(T);
+            if (!is || at + N > width) row[i] = 0x7FFFFFFF;
         }
     }
-    // bits of this thread's rows that are there: up to the last, and of no negative group
-    static __device__ __forceinline__ unsigned rows_there(const int *groups, int last)
+    // base0, base1: the tiles' first rows; last: their last row that is there; groups: those of the rows, or null
+    __device__ __forceinline__ void ask(const T *base0, long pitch0, const T *base1, long pitch1, int width, int last, const int *groups, lds_char *to)
     {
-        unsigned bits = 0;
+        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+        if (width % N) {
+            const int r = (int)threadIdx.x % ROWS, from = r < last ? r : last;
+            const T *const end = ((int)threadIdx.x < ROWS ? base0 + from * pitch0 : base1 + from * pitch1) + width / N * N;
+#pragma unroll
+            for (int j = 0; j < N - 1; ++j) ends[j] = end[j < width % N ? j : 0];
+            const bool there = (int)threadIdx.x < 2 * ROWS && r <= last && (!groups || groups[from] >= 0);
+#pragma unroll
+            for (int j = 0; j < N - 1; ++j) ends[j] = there ? ends[j] : (T)0.0f;
+        }
         int g[kEach];
-        const int row0 = fresh_lane((int)threadIdx.x) / kSlots;
+        if (groups)
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int r = row0 + i * kStep;
-            g[i] = groups ? groups[r < last ? r : last] : 0;
-        }
+            for (int i = 0; i < kEach; ++i) g[i] = groups[row[i] <= last ? row[i] : 0];
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) bits |= (unsigned)(g[i] >= 0 && row0 + i * kStep <= last) << i;
-        return bits;
-    }
-    __device__ __forceinline__ void put(char *tile, int width, unsigned there) const
-    {
-        const int id = fresh_lane((int)threadIdx.x), row0 = id / kSlots, c = id % kSlots * N;
-        if (c >= width) return;
-        const int skip = c + N > width ? c + N - width : 0;          // elements of the piece that belong to the one before
+        for (int which = 0; which < 2; ++which) {
+            const Window window = __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(which ? base1 : base0), 0, (int)kBeyond, 0x00020000);
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const i4 x = there >> i & 1u ? v[i] : i4(0);
-            char *const to = tile + Rows<T, DP>::place(row0 + i * kStep, c);
-            if (!skip) *reinterpret_cast<i4 *>(to) = x;
-            else {
-                const typename P::V e = __builtin_bit_cast(typename P::V, x);
-#pragma unroll
-                for (int j = 1; j < N; ++j)
-                    if (j >= skip) *reinterpret_cast<T *>(to + (j - skip) * (int)sizeof(T)) = e[j];
+            for (int i = 0; i < kEach; ++i) {
+                if (kLoads % WAVES && wave + i * WAVES >= kLoads) break;
+                bool there = row[i] <= last;
+                if (groups) there = there & (g[i] >= 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(window, (__attribute__((address_space(3))) void *)(to + which * R::kBytes + (wave + i * WAVES) * 1024), 16,
+                                                         there ? (int)off[which][i] : (int)kBeyond, 0, 0, 0);
             }
         }
     }
+    // the rows' tails, once the tiles have arrived (a barrier behind them)
+    __device__ __forceinline__ void tail(lds_char *tile, int width) const
+    {
+        if (width % N == 0) return;
+        const int r = (int)threadIdx.x % ROWS, which = (int)threadIdx.x / ROWS;
+        if (which < 2)
+#pragma unroll
+            for (int j = 0; j < N - 1; ++j)
+                if (j < width % N) *(__attribute__((address_space(3))) T *)(tile + which * R::kBytes + R::place(r, width / N * N + j)) = ends[j];
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    }
 };
+
+// Everything that was sent for has come, to all waves.  (The builtin, not an instruction of our own: the compiler has to know that nothing is on its way any more, or it waits
+// in the loops behind for what came before them.)
+__device__ __forceinline__ void arrive()
+{
+    __builtin_amdgcn_s_waitcnt(0x0F70);          // vmcnt(0)
+    __syncthreads();
+}
+
+// ... of codes, whose entries also say whether codes go up by one from token to token (z)
+__device__ __forceinline__ int2 codes_over(const int4 *ranges, int first, int last, bool &line)
+{
+    int4 s = ranges[first >> 6];
+    for (int t = (first >> 6) + 1; t <= last >> 6; ++t) {
+        const int4 u = ranges[t];
+        s.x = u.x < s.x ? u.x : s.x;
+        s.y = u.y > s.y ? u.y : s.y;
+        s.z &= u.z;
+    }
+    line = s.z != 0;
+    return int2{s.x, s.y};
+}
 
 // Smallest and largest entry of `spans` over tiles of 64 from that of row `first` to that of row `last`
 __device__ __forceinline__ int2 span_over(const int2 *spans, int first, int last)
@@ -173,15 +200,16 @@ struct Walk {
 // few they are staged in LDS; else each pair goes to memory.
 constexpr int kOne = 0, kStaged = 1, kFar = 2;
 
-template <int THREADS>
+// ROOM: how many are staged at most.  640 hold a window of 12 x 12 tokens; beside tiles of 128 16-bit elements 384, so that two workgroups' share a compute unit's LDS.
+template <int THREADS, int ROOM>
 struct Bias {
-    static constexpr int kRoom = 4 * THREADS;
+    static constexpr int kRoom = ROOM;
     float v, one;
     int bucket, low, count, form, all;
 
     // (the first THREADS of what is staged come with the tile's rows; more there are only in wide windows)
     template <bool BUCKETS>
-    __device__ __forceinline__ void ask(const AttentionArgs &a, const float *bias, int2 queries, int2 keys)
+    __device__ __forceinline__ void ask(const AttentionArgs &a, const float *bias, int2 queries, int2 keys, int heads)
     {
         form = kOne;
         one = 0.0f;
@@ -194,16 +222,16 @@ struct Bias {
         const int2 run = a.bucket[low];
         all = run.x;
         one = bias[low];
-        form = run.y >= high ? kOne : (count <= kRoom ? kStaged : kFar);
+        form = run.y >= high ? kOne : (heads == 1 ? (count <= kRoom ? kStaged : kFar) : (count * heads <= kRoom ? kStaged : kFar));
         const int at = low + ((int)threadIdx.x < count ? (int)threadIdx.x : 0);
         v = bias[at];
         if constexpr (BUCKETS) bucket = a.bucket[at].x;
     }
     template <bool BUCKETS>
-    __device__ __forceinline__ void put(const AttentionArgs &a, const float *bias, float *room, int *buckets) const
+    __device__ __forceinline__ void put(const AttentionArgs &a, const float *bias, float *room, unsigned short *buckets, int heads) const
     {
         if (form != kStaged) return;
-        const auto within = [&](int b) { return (unsigned)b < (unsigned)a.buckets ? b : a.buckets - 1; };
+        const auto within = [&](int b) { return (unsigned short)((unsigned)b < (unsigned)a.buckets ? b : a.buckets - 1); };
         if ((int)threadIdx.x < count) {
             room[threadIdx.x] = v;
             if constexpr (BUCKETS) buckets[threadIdx.x] = within(bucket);
@@ -213,6 +241,11 @@ struct Bias {
             room[at] = bias[low + at];
             if constexpr (BUCKETS) buckets[at] = within(a.bucket[low + at].x);
         }
+        // (the biases of further heads behind those of the first)
+#pragma unroll 1
+        for (int h = 1; h < heads; ++h)
+#pragma unroll 1
+            for (int at = (int)threadIdx.x; at < count; at += THREADS) room[h * count + at] = bias[(long)h * a.codes + low + at];
     }
 };
 
@@ -297,9 +330,9 @@ __device__ __forceinline__ Query query_of(const AttentionArgs &a, int b, int uni
 }
 
 // The range of codes of queries first .. last of an entry: that of the 64s of the whole line which they lie in
-__device__ __forceinline__ int2 query_codes(const AttentionArgs &a, int first, int last)
+__device__ __forceinline__ int2 query_codes(const AttentionArgs &a, int first, int last, bool &line)
 {
-    return a.tables ? span_over(a.query_range, a.first_query + first, a.first_query + last) : int2{0, 0};
+    return a.tables ? codes_over(a.query_range, a.first_query + first, a.first_query + last, line) : int2{0, 0};
 }
 
 // ---------------------------------------------------------------------------------
@@ -308,25 +341,23 @@ __global__ void __launch_bounds__(64 * WAVES, 2)
 hot_attention_forward_kernel(AttentionArgs a)
 {
     constexpr int THREADS = 64 * WAVES, KS = DP / 32, DB = DP / 16, TILE = WAVES * QB * 16;
-    typedef Rows<T, DP> R;
-    typedef Fetch<T, DP, KT, THREADS> F;
-    __shared__ __attribute__((aligned(16))) char k_tile[KT * R::kPitch];
-    __shared__ __attribute__((aligned(16))) char v_tile[KT * R::kPitch];
-    __shared__ __attribute__((aligned(16))) int codes[KT], groups[KT];
-    __shared__ float staged[Bias<THREADS>::kRoom];
+    typedef Rows<T, DP, KT> R;
+    typedef Bring<T, DP, KT, WAVES> B;
+    constexpr int STAGES = kStages<T>;
+    typedef Bias<THREADS, THREADS < 256 ? 256 : (sizeof(T) == 2 && DP > 64 ? 384 : 640)> Staging;
+    __shared__ __attribute__((aligned(1024))) char tiles[STAGES * 2 * R::kBytes];
+    __shared__ __attribute__((aligned(16))) int all_codes[STAGES * KT], all_groups[STAGES * KT];
+    __shared__ float all_staged[STAGES * Staging::kRoom];
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, g = lane >> 4, col = lane & 15;
-    const int units = a.heads / a.pack, rows = a.queries * a.pack;
-    F::clear(k_tile, a.width);
-    F::clear(v_tile, a.width);
+    const int rows = a.queries * a.pack;
 
     long item = item_of(a.items);
     if (item < 0) return;
     const int split = (int)(item % a.splits);
     item /= a.splits;
-    const int tile_q = a.tiles_q - 1 - (int)(item % a.tiles_q);
-    item /= a.tiles_q;
-    const int unit = (int)(item % units), b = (int)(item / units);
-    const int kvh = unit * a.pack / a.per, table = a.tables ? b / a.entries : 0;
+    const int units = a.heads / a.pack, unit = (int)(item % units);
+    item /= units;
+    const int b = (int)(item % a.batch), tile_q = a.tiles_q - 1 - (int)(item / a.batch), kvh = unit * a.pack / a.per, table = a.tables ? b / a.entries : 0;
     const T *const q = static_cast<const T *>(a.q) + b * a.p_q.batch;
     const T *const k = static_cast<const T *>(a.k) + b * a.p_k.batch + kvh * a.p_k.head;
     const T *const v = static_cast<const T *>(a.v) + b * a.p_v.batch + kvh * a.p_v.head;
@@ -341,9 +372,10 @@ hot_attention_forward_kernel(AttentionArgs a)
 #pragma unroll
         for (int s = 0; s < KS; ++s) qf[n][s] = eight(q + at[n].h * a.p_q.head + at[n].i * a.p_q.row, s * 32 + g * 8, a.width, at[n].there);
     }
-    // (heads side by side have a bias each: what is staged is the first one's, and only one of them asks for it)
+    // (of the first of heads side by side)
     const float *const bias = a.bias + ((long)table * a.heads + unit * a.pack) * a.codes;
-    const int2 mine = query_codes(a, first_i, last_i);
+    bool line = false;
+    const int2 mine = query_codes(a, first_i, last_i, line);
     // keys that any row of this workgroup may see by order, and up to which all of them may
     int visible = a.causal ? last_i + a.keys - a.queries + 1 : a.keys, few = a.causal ? first_i + a.keys - a.queries + 1 : a.keys;
     visible = visible < 0 ? 0 : (visible > a.keys ? a.keys : visible);
@@ -352,24 +384,25 @@ hot_attention_forward_kernel(AttentionArgs a)
     const int end_tile = (split + 1) * share < all_tiles ? (split + 1) * share : all_tiles;
 
     Walk<KT> walk;
-    F next_k, next_v;
-    Bias<THREADS> next_bias;
+    B bring;
+    bring.begin(a.p_k.row, a.p_v.row, a.width);
+    Staging next_bias;
+    float next_one[QB] = {};
     int next_code = 0, next_group = 0;
-    unsigned next_there = 0;
-    auto ask = [&](int tile) {
+    auto ask = [&](int tile, lds_char *to) {
         if (tile >= end_tile) return;
         const int last = a.keys - 1 - tile * KT;
-        next_k.ask(k + (long)tile * KT * a.p_k.row, a.p_k.row, last, fresh(a.width));
-        next_v.ask(v + (long)tile * KT * a.p_v.row, a.p_v.row, last, fresh(a.width));
-        next_there = F::rows_there(kg ? kg + tile * KT : nullptr, last);
         if ((int)threadIdx.x < KT) {
             const int j = tile * KT + ((int)threadIdx.x < last ? (int)threadIdx.x : last);
             next_code = a.tables ? a.key_code[j] : 0;
             next_group = kg ? kg[j] : 0;
             if ((int)threadIdx.x > last) next_group = -1;
         }
-        next_bias.template ask<false>(a, bias, mine, a.tables ? a.key_range[tile * KT >> 6] : int2{0, 0});
-        if (a.pack > 1 && a.tables) next_bias.form = kFar;
+        next_bias.template ask<false>(a, bias, mine, a.tables ? codes_over(a.key_range, tile * KT, tile * KT, line) : int2{0, 0}, a.pack);
+        if (a.tables)
+#pragma unroll
+            for (int n = 0; n < QB; ++n) next_one[n] = bias[(long)(at[n].h - unit * a.pack) * a.codes + next_bias.low];
+        bring.ask(k + (long)tile * KT * a.p_k.row, a.p_k.row, v + (long)tile * KT * a.p_v.row, a.p_v.row, a.width, last, kg ? kg + tile * KT : nullptr, to);
     };
 
     Block16<T> o[DB][QB];
@@ -385,23 +418,29 @@ hot_attention_forward_kernel(AttentionArgs a)
     const bool busy = __ballot(any) != 0;            // (waves without queries only bring tiles)
     int tile = walk.begin(a.groups ? a.key_spans + (long)(b % a.groups) * ((a.keys + 63) >> 6) : nullptr,
                           a.groups ? span_over(a.query_spans + (long)(b % a.groups) * ((a.queries + 63) >> 6), first_i, last_i) : int2{0, 0}, split * share, end_tile);
-    ask(tile);
-    while (tile < end_tile) {
-        __syncthreads();
-        next_k.put(k_tile, fresh(a.width), next_there);
-        next_v.put(v_tile, fresh(a.width), next_there);
+    // One tile: the products of what is `here`, while the next one comes to `there`
+    auto step = [&](lds_char *__restrict here_tile, lds_char *__restrict there_tile, int buffer) {
+        int *const codes = all_codes + buffer * KT, *const groups = all_groups + buffer * KT;
+        float *const staged = all_staged + buffer * Staging::kRoom;
         if ((int)threadIdx.x < KT) {
             codes[threadIdx.x] = next_code;
             groups[threadIdx.x] = next_group;
         }
-        next_bias.template put<false>(a, bias, staged, nullptr);
+        next_bias.template put<false>(a, bias, staged, nullptr, a.pack);
         const int form = __builtin_amdgcn_readfirstlane(next_bias.form), low = __builtin_amdgcn_readfirstlane(next_bias.low);
-        const float one = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, next_bias.one)));
-        __syncthreads();
+        float one[QB];
+        int own[QB];                     // where the biases of the row's head are staged, from its code on
+#pragma unroll
+        for (int n = 0; n < QB; ++n) {
+            one[n] = next_one[n];
+            own[n] = (at[n].h - unit * a.pack) * next_bias.count + at[n].code - low;
+        }
+        arrive();
+        bring.tail(here_tile, a.width);
         const int k0 = tile * KT;
         tile = walk.next(tile);
-        ask(tile);
-        if (!busy) continue;
+        if constexpr (STAGES == 2) ask(tile, there_tile);
+        if (!busy) return;
         // 32 keys at a time: their scores and pieces are as many registers as there is room for beside the sums
 #pragma unroll 1
         for (int c = 0; c < KT / 32; ++c) {
@@ -411,7 +450,7 @@ hot_attention_forward_kernel(AttentionArgs a)
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int s = 0; s < KS; ++s) {
-                    const V8<T> f = R::along(k_tile, c * 32 + u * 16, s, here);
+                    const V8<T> f = R::along(here_tile, c, u, s, here);
 #pragma unroll
                     for (int n = 0; n < QB; ++n) acc[u][n].mac(f, qf[n][s]);
                 }
@@ -422,7 +461,7 @@ hot_attention_forward_kernel(AttentionArgs a)
             by_form(form, k0 + KT > few || a.groups, [&](auto how) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    const int row0 = c * 32 + u * 16 + g * 4;
+                    const int row0 = R::row_of(c, u, g);
                     i4 kc = i4(0), kgr = i4(0);
                     if constexpr (how.kForm != kOne) kc = *reinterpret_cast<const i4 *>(codes + row0);
                     if constexpr (how.kMasked) kgr = *reinterpret_cast<const i4 *>(groups + row0);
@@ -431,9 +470,9 @@ hot_attention_forward_kernel(AttentionArgs a)
                         const f4 s = acc[u][n].read(settled);
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            float add = one;
+                            float add = one[n];
                             if constexpr (how.kForm == kStaged) {
-                                const unsigned at_code = (unsigned)(at[n].code - low - kc[i]), last = Bias<THREADS>::kRoom - 1;
+                                const unsigned at_code = (unsigned)(own[n] - kc[i]), last = Staging::kRoom - 1;
                                 add = staged[at_code < last ? at_code : last];
                             } else if constexpr (how.kForm == kFar) {
                                 const unsigned at_code = (unsigned)(at[n].code - kc[i]), last = (unsigned)a.codes - 1u;
@@ -469,10 +508,23 @@ hot_attention_forward_kernel(AttentionArgs a)
             }
 #pragma unroll
             for (int d = 0; d < DB; ++d) {
-                const V8<T> f = R::across(v_tile, c * 32, d * 16, here);
+                const V8<T> f = R::across(here_tile + R::kBytes, c, d * 16, here);
 #pragma unroll
                 for (int n = 0; n < QB; ++n) p[n].mac(o[d][n], f);
             }
+        }
+    };
+    lds_char *const lds = (lds_char *)tiles;
+    if constexpr (STAGES == 2) ask(tile, lds);
+    int buffer = 0;
+    while (tile < end_tile) {
+        if constexpr (STAGES == 2) {
+            step(lds + buffer * 2 * R::kBytes, lds + (1 - buffer) * 2 * R::kBytes, buffer);
+            buffer = 1 - buffer;
+        } else {
+            __syncthreads();
+            ask(tile, lds);
+            step(lds, lds, 0);
         }
     }
     const Settled settled;
@@ -654,25 +706,24 @@ __global__ void __launch_bounds__(64 * WAVES, 2)
 hot_attention_keys_kernel(AttentionArgs a)
 {
     constexpr int THREADS = 64 * WAVES, KS = DP / 32, DB = DP / 16, TILE = WAVES * KB * 16, QT = 64;
-    typedef Rows<T, DP> R;
-    typedef Fetch<T, DP, QT, THREADS> F;
-    __shared__ __attribute__((aligned(16))) char q_tile[QT * R::kPitch];
-    __shared__ __attribute__((aligned(16))) char up_tile[QT * R::kPitch];
-    __shared__ __attribute__((aligned(16))) float ms[QT], ls[QT], ds[QT];
-    __shared__ __attribute__((aligned(16))) int codes[QT], groups[QT];
-    __shared__ float staged[Bias<THREADS>::kRoom];
+    typedef Rows<T, DP, QT> R;
+    typedef Bring<T, DP, QT, WAVES> B;
+    constexpr int STAGES = kStages<T>;
+    typedef Bias<THREADS, THREADS < 256 ? 256 : (sizeof(T) == 2 && DP > 64 ? 384 : 640)> Staging;
+    __shared__ __attribute__((aligned(1024))) char tiles[STAGES * 2 * R::kBytes];
+    __shared__ __attribute__((aligned(16))) float all_ms[STAGES * QT], all_ls[STAGES * QT], all_ds[STAGES * QT];
+    __shared__ __attribute__((aligned(16))) int all_codes[STAGES * QT], all_groups[STAGES * QT];
+    __shared__ float all_staged[STAGES * Staging::kRoom];
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, g = lane >> 4, col = lane & 15;
     const int tiles_q = (a.queries + QT - 1) / QT, past = a.keys - a.queries, reach = a.causal ? past : 0x7FFFFF00;        // (added to less than 256)
-    F::clear(q_tile, a.width);
-    F::clear(up_tile, a.width);
 
     long item = item_of(a.items);
     if (item < 0) return;
     const int split = (int)(item % a.splits);
     item /= a.splits;
-    const int tile_k = (int)(item % a.tiles_k);
-    item /= a.tiles_k;
-    const int kvh = (int)(item % a.kv_heads), b = (int)(item / a.kv_heads), table = a.tables ? b / a.entries : 0;
+    const int kvh = (int)(item % a.kv_heads);
+    item /= a.kv_heads;
+    const int b = (int)(item % a.batch), tile_k = (int)(item / a.batch), table = a.tables ? b / a.entries : 0;
     // one head of the key head's, or all; a run of its queries
     const int runs = a.by_head ? a.splits / a.per : a.splits, run = a.by_head ? split / a.per : split;
     const int first_h = kvh * a.per + (a.by_head ? split % a.per : 0), end_h = a.by_head ? first_h + 1 : first_h + a.per;
@@ -698,7 +749,8 @@ hot_attention_keys_kernel(AttentionArgs a)
         }
     }
     const int last_key = (tile_k + 1) * TILE < a.keys ? (tile_k + 1) * TILE - 1 : a.keys - 1;
-    const int2 key_codes = a.tables ? span_over(a.key_range, tile_k * TILE, last_key) : int2{0, 0};
+    bool line = false;
+    const int2 key_codes = a.tables ? codes_over(a.key_range, tile_k * TILE, last_key, line) : int2{0, 0};
     const int2 mine = a.groups ? span_over(a.key_spans + (long)(b % a.groups) * ((a.keys + 63) >> 6), tile_k * TILE, last_key) : int2{0, 0};
     bool any = false;
 #pragma unroll
@@ -710,23 +762,21 @@ hot_attention_keys_kernel(AttentionArgs a)
     const int first = a.causal && tile_k * TILE > past ? (tile_k * TILE - past) / QT : 0, left = tiles_q > first ? tiles_q - first : 0, share = (left + runs - 1) / runs;
     const int first_tile = first + run * share, end_tile = first_tile + share < tiles_q ? first_tile + share : tiles_q;
 
+    B bring;
+    bring.begin(a.p_q.row, a.p_go.row, a.width);
+    lds_char *const lds = (lds_char *)tiles;
     for (int h = first_h; h < end_h; ++h) {
         const T *const q = static_cast<const T *>(a.q) + b * a.p_q.batch + h * a.p_q.head;
         const T *const up = static_cast<const T *>(a.grad_o) + b * a.p_go.batch + h * a.p_go.head;
         const float *const bias = a.bias + ((long)table * a.heads + h) * a.codes;
         const long stat0 = ((long)b * a.heads + h) * a.queries;
         Walk<QT> walk;
-        F next_q, next_up;
-        Bias<THREADS> next_bias;
+        Staging next_bias;
         float next_m = 0.0f, next_l = 0.0f, next_d = 0.0f;
         int next_code = 0, next_group = 0;
-        unsigned next_there = 0;
-        auto ask = [&](int tile) {
+        auto ask = [&](int tile, lds_char *to) {
             if (tile >= end_tile) return;
             const int last = a.queries - 1 - tile * QT;
-            next_q.ask(q + (long)tile * QT * a.p_q.row, a.p_q.row, last, fresh(a.width));
-            next_up.ask(up + (long)tile * QT * a.p_go.row, a.p_go.row, last, fresh(a.width));
-            next_there = F::rows_there(qg ? qg + tile * QT : nullptr, last);
             if ((int)threadIdx.x < QT) {
                 const int i = tile * QT + ((int)threadIdx.x < last ? (int)threadIdx.x : last);
                 next_m = a.stats[2 * (stat0 + i)];
@@ -739,14 +789,14 @@ hot_attention_keys_kernel(AttentionArgs a)
                     next_group = -2;
                 }
             }
-            next_bias.template ask<false>(a, bias, query_codes(a, tile * QT, tile * QT + (last < QT - 1 ? last : QT - 1)), key_codes);
+            next_bias.template ask<false>(a, bias, query_codes(a, tile * QT, tile * QT + (last < QT - 1 ? last : QT - 1), line), key_codes, 1);
+            bring.ask(q + (long)tile * QT * a.p_q.row, a.p_q.row, up + (long)tile * QT * a.p_go.row, a.p_go.row, a.width, last, qg ? qg + tile * QT : nullptr, to);
         };
         int tile = walk.begin(a.groups ? a.query_spans + (long)(b % a.groups) * tiles_q : nullptr, mine, first_tile, end_tile);
-        ask(tile);
-        while (tile < end_tile) {
-            __syncthreads();
-            next_q.put(q_tile, fresh(a.width), next_there);
-            next_up.put(up_tile, fresh(a.width), next_there);
+        // One tile: the products of what is `here`, while the next one comes to `there`
+        auto step = [&](lds_char *__restrict here, lds_char *__restrict there, int buffer) {
+            int *const codes = all_codes + buffer * QT, *const groups = all_groups + buffer * QT;
+            float *const ms = all_ms + buffer * QT, *const ls = all_ls + buffer * QT, *const ds = all_ds + buffer * QT, *const staged = all_staged + buffer * Staging::kRoom;
             if ((int)threadIdx.x < QT) {
                 ms[threadIdx.x] = next_m;
                 ls[threadIdx.x] = next_l;
@@ -754,14 +804,15 @@ hot_attention_keys_kernel(AttentionArgs a)
                 codes[threadIdx.x] = next_code;
                 groups[threadIdx.x] = next_group;
             }
-            next_bias.template put<false>(a, bias, staged, nullptr);
+            next_bias.template put<false>(a, bias, staged, nullptr, 1);
             const int form = __builtin_amdgcn_readfirstlane(next_bias.form), low = __builtin_amdgcn_readfirstlane(next_bias.low);
             const float one = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, next_bias.one)));
-            __syncthreads();
+            arrive();
+            bring.tail(here, a.width);
             const int i0 = tile * QT;
             tile = walk.next(tile);
-            ask(tile);
-            if (!busy) continue;
+            if constexpr (STAGES == 2) ask(tile, there);
+            if (!busy) return;
             // (queries behind the last have l = infinity, keys behind the last are zeros and are not stored)
             const bool masked = a.groups || (a.causal && i0 + past < last_key);
 #pragma unroll 1
@@ -772,7 +823,7 @@ hot_attention_keys_kernel(AttentionArgs a)
                 for (int u = 0; u < 2; ++u)
 #pragma unroll
                     for (int x = 0; x < KS; ++x) {
-                        const V8<T> fq = R::along(q_tile, c * 32 + u * 16, x, at), fu = R::along(up_tile, c * 32 + u * 16, x, at);
+                        const V8<T> fq = R::along(here, c, u, x, at), fu = R::along(here + R::kBytes, c, u, x, at);
 #pragma unroll
                         for (int n = 0; n < KB; ++n) {
                             s[u][n].mac(fq, kf[n][x]);
@@ -784,7 +835,7 @@ hot_attention_keys_kernel(AttentionArgs a)
                 by_form(form, masked, [&](auto how) {
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
-                        const int row0 = c * 32 + u * 16 + g * 4;
+                        const int row0 = R::row_of(c, u, g);
                         const f4 m = *reinterpret_cast<const f4 *>(ms + row0), l = *reinterpret_cast<const f4 *>(ls + row0), d = *reinterpret_cast<const f4 *>(ds + row0);
                         i4 qc = i4(0), qgr = i4(0);
                         if constexpr (how.kForm != kOne) qc = *reinterpret_cast<const i4 *>(codes + row0);
@@ -796,7 +847,7 @@ hot_attention_keys_kernel(AttentionArgs a)
                             for (int i = 0; i < 4; ++i) {
                                 float add = one;
                                 if constexpr (how.kForm == kStaged) {
-                                    const unsigned at_code = (unsigned)(qc[i] - (code[n] + low)), last = Bias<THREADS>::kRoom - 1;
+                                    const unsigned at_code = (unsigned)(qc[i] - (code[n] + low)), last = Staging::kRoom - 1;
                                     add = staged[at_code < last ? at_code : last];
                                 } else if constexpr (how.kForm == kFar) {
                                     const unsigned at_code = (unsigned)(qc[i] - code[n]), last = (unsigned)a.codes - 1u;
@@ -814,13 +865,27 @@ hot_attention_keys_kernel(AttentionArgs a)
                 });
 #pragma unroll
                 for (int x = 0; x < DB; ++x) {
-                    const V8<T> fu = R::across(up_tile, c * 32, x * 16, at), fq = R::across(q_tile, c * 32, x * 16, at);
+                    const V8<T> fu = R::across(here + R::kBytes, c, x * 16, at), fq = R::across(here, c, x * 16, at);
 #pragma unroll
                     for (int n = 0; n < KB; ++n) {
                         p[n].mac(dv[x][n], fu);
                         dz[n].mac(dk[x][n], fq);
                     }
                 }
+            }
+        };
+        // (the waves have done with the last head's tiles)
+        __syncthreads();
+        if constexpr (STAGES == 2) ask(tile, lds);
+        int buffer = 0;
+        while (tile < end_tile) {
+            if constexpr (STAGES == 2) {
+                step(lds + buffer * 2 * R::kBytes, lds + (1 - buffer) * 2 * R::kBytes, buffer);
+                buffer = 1 - buffer;
+            } else {
+                __syncthreads();
+                ask(tile, lds);
+                step(lds, lds, 0);
             }
         }
     }
@@ -879,6 +944,16 @@ hot_attention_sum_kernel(SumArgs first, SumArgs second)
     }
 }
 
+// same_row += sum over e >= E of v[e] of lane L + e of this lane's sixteen, next_row += that of lane L + e - 16
+template <int E>
+__device__ __forceinline__ void sum_along(const float (&v)[8], float &same_row, float &next_row)
+{
+    const int bits = __builtin_bit_cast(int, v[E]);
+    same_row += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, bits, 0x100 | E, 0xF, 0xF, true));
+    next_row += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, bits, 0x110 | (16 - E), 0xF, 0xF, true));
+    if constexpr (E < 7) sum_along<E + 1>(v, same_row, next_row);
+}
+
 // ---------------------------------------------------------------------------------
 // dq, and what the table's gradient is made of.  A workgroup holds the queries of one tile and head, of several entries of the batch one after the other.  Where a tile of
 // pairs is of one bucket its dz are added up in registers (in 64 bits from tile to tile); else each goes to its difference of codes in bins of the wave's own, and from
@@ -887,33 +962,32 @@ template <class T, int DP, int QB, int WAVES, bool TABLE>
 __global__ void __launch_bounds__(64 * WAVES, 2)
 hot_attention_queries_kernel(AttentionArgs a)
 {
-    constexpr int THREADS = 64 * WAVES, KS = DP / 32, DB = DP / 16, KT = 64, TILE = WAVES * QB * 16, BINS = TABLE ? Bias<THREADS>::kRoom : 1;
-    typedef Rows<T, DP> R;
-    typedef Fetch<T, DP, KT, THREADS> F;
-    __shared__ __attribute__((aligned(16))) char k_tile[KT * R::kPitch];
-    __shared__ __attribute__((aligned(16))) char v_tile[KT * R::kPitch];
-    __shared__ __attribute__((aligned(16))) int codes[KT], groups[KT];
-    __shared__ float staged[Bias<THREADS>::kRoom + 64];          // (the last 64, and those of the bins, are for pairs that do not count: a place for each lane)
-    __shared__ int staged_bucket[BINS];
+    constexpr int THREADS = 64 * WAVES, KS = DP / 32, DB = DP / 16, KT = 64, TILE = WAVES * QB * 16;
+    typedef Rows<T, DP, KT> R;
+    typedef Bring<T, DP, KT, WAVES> B;
+    constexpr int STAGES = kStages<T>;
+    typedef Bias<THREADS, THREADS < 256 ? 256 : (sizeof(T) == 2 && DP > 64 ? 384 : 640)> Staging;
+    constexpr int BINS = TABLE ? Staging::kRoom : 1;
+    __shared__ __attribute__((aligned(1024))) char tiles[STAGES * 2 * R::kBytes];
+    __shared__ __attribute__((aligned(16))) int all_codes[STAGES * KT], all_groups[STAGES * KT];
+    __shared__ float all_staged[STAGES * (Staging::kRoom + 64)];          // (the last 64, and those of the bins, are for pairs that do not count: a place for each lane)
+    __shared__ unsigned short all_staged_bucket[STAGES * BINS];
     __shared__ float all_bins[WAVES * (BINS + 64)];
     extern __shared__ float all_sums[];          // [waves, buckets]
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, g = lane >> 4, col = lane & 15;
     float *const bins = all_bins + wave * (BINS + 64), *const sums = all_sums + wave * a.buckets;
-    F::clear(k_tile, a.width);
-    F::clear(v_tile, a.width);
     if constexpr (TABLE)
         for (int i = lane; i < BINS + 64; i += 64) bins[i] = 0.0f;
-    staged[Bias<THREADS>::kRoom + lane] = 0.0f;
+    for (int i = 0; i < STAGES; ++i) all_staged[i * (Staging::kRoom + 64) + Staging::kRoom + lane] = 0.0f;
     auto add = [](float *to, float x) { __hip_atomic_fetch_add(to, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT); };
 
     long item = item_of(a.items);
     if (item < 0) return;
-    const long unit_item = item;
-    const int split = (int)(item % a.splits);
+    const int chunks = (int)(a.items / ((long)a.splits * a.tiles_q * a.heads)), split = (int)(item % a.splits);
     item /= a.splits;
-    const int tile_q = a.tiles_q - 1 - (int)(item % a.tiles_q);
-    item /= a.tiles_q;
-    const int h = (int)(item % a.heads), chunk = (int)(item / a.heads), kvh = h / a.per;
+    const int h = (int)(item % a.heads), kvh = h / a.per;
+    item /= a.heads;
+    const int chunk = (int)(item % chunks), tile_q = a.tiles_q - 1 - (int)(item / chunks);
     const int per_table = (a.entries + a.chunk - 1) / a.chunk, table = chunk / per_table;
     const int first_b = table * a.entries + chunk % per_table * a.chunk;
     const int end_b = first_b + a.chunk < (table + 1) * a.entries ? first_b + a.chunk : (table + 1) * a.entries;
@@ -924,7 +998,9 @@ hot_attention_queries_kernel(AttentionArgs a)
     if (few > a.keys) few = a.keys;
     const int all_tiles = (visible + KT - 1) / KT, share = (all_tiles + a.splits - 1) / a.splits;
     const int end_tile = (split + 1) * share < all_tiles ? (split + 1) * share : all_tiles;
-    const int2 mine_codes = query_codes(a, first_i, last_i);
+    bool line = false;               // whether the queries' codes go up by one
+    const int2 mine_codes = query_codes(a, first_i, last_i, line);
+    const int line_code = TABLE ? a.query_code[first_i] : 0;
     double same = 0.0;               // this lane's part of the sum of bucket `same_bucket`
     int same_bucket = -1;
     auto flush = [&]() {
@@ -936,6 +1012,9 @@ hot_attention_queries_kernel(AttentionArgs a)
     };
     if constexpr (TABLE)
         for (int i = lane; i < a.buckets; i += 64) sums[i] = 0.0f;
+    B bring;
+    bring.begin(a.p_k.row, a.p_v.row, a.width);
+    lds_char *const lds = (lds_char *)tiles;
     for (int b = first_b; b < end_b; ++b) {
         const T *const q = static_cast<const T *>(a.q) + b * a.p_q.batch + h * a.p_q.head;
         const T *const up = static_cast<const T *>(a.grad_o) + b * a.p_go.batch + h * a.p_go.head;
@@ -977,25 +1056,22 @@ hot_attention_queries_kernel(AttentionArgs a)
             }
         }
         Walk<KT> walk;
-        F next_k, next_v;
-        Bias<THREADS> next_bias;
+        Staging next_bias;
         int next_code = 0, next_group = 0;
         int2 next_range = int2{0, 0};
-        unsigned next_there = 0;
-        auto ask = [&](int tile) {
+        bool next_line = false;
+        auto ask = [&](int tile, lds_char *to) {
             if (tile >= end_tile) return;
             const int last = a.keys - 1 - tile * KT;
-            next_k.ask(k + (long)tile * KT * a.p_k.row, a.p_k.row, last, fresh(a.width));
-            next_v.ask(v + (long)tile * KT * a.p_v.row, a.p_v.row, last, fresh(a.width));
-            next_there = F::rows_there(kg ? kg + tile * KT : nullptr, last);
             if ((int)threadIdx.x < KT) {
                 const int j = tile * KT + ((int)threadIdx.x < last ? (int)threadIdx.x : last);
                 next_code = a.tables ? a.key_code[j] : 0;
                 next_group = kg ? kg[j] : 0;
                 if ((int)threadIdx.x > last) next_group = -1;
             }
-            next_range = a.tables ? a.key_range[tile] : int2{0, 0};
-            next_bias.template ask<TABLE>(a, bias, mine_codes, next_range);
+            next_range = a.tables ? codes_over(a.key_range, tile * KT, tile * KT, next_line) : int2{0, 0};
+            next_bias.template ask<TABLE>(a, bias, mine_codes, next_range, 1);
+            bring.ask(k + (long)tile * KT * a.p_k.row, a.p_k.row, v + (long)tile * KT * a.p_v.row, a.p_v.row, a.width, last, kg ? kg + tile * KT : nullptr, to);
         };
         bool any = false;
 #pragma unroll
@@ -1004,24 +1080,26 @@ hot_attention_queries_kernel(AttentionArgs a)
         Block16<T> dq[DB][QB];
         int tile = walk.begin(a.groups ? a.key_spans + (long)(b % a.groups) * ((a.keys + 63) >> 6) : nullptr,
                               a.groups ? span_over(a.query_spans + (long)(b % a.groups) * ((a.queries + 63) >> 6), first_i, last_i) : int2{0, 0}, split * share, end_tile);
-        ask(tile);
-        while (tile < end_tile) {
-            __syncthreads();
-            next_k.put(k_tile, fresh(a.width), next_there);
-            next_v.put(v_tile, fresh(a.width), next_there);
+        // One tile: the products of what is `here`, while the next one comes to `there`
+        auto step = [&](lds_char *__restrict here_tile, lds_char *__restrict there_tile, int buffer) {
+            int *const codes = all_codes + buffer * KT, *const groups = all_groups + buffer * KT;
+            float *const staged = all_staged + buffer * (Staging::kRoom + 64);
+            unsigned short *const staged_bucket = all_staged_bucket + buffer * BINS;
             if ((int)threadIdx.x < KT) {
                 codes[threadIdx.x] = next_code;
                 groups[threadIdx.x] = next_group;
             }
-            next_bias.template put<TABLE>(a, bias, staged, staged_bucket);
+            next_bias.template put<TABLE>(a, bias, staged, staged_bucket, 1);
             const int form = __builtin_amdgcn_readfirstlane(next_bias.form), low = __builtin_amdgcn_readfirstlane(next_bias.low), bucket = __builtin_amdgcn_readfirstlane(next_bias.all);
             const int2 range = next_range;
+            const bool lined = TABLE && line && next_line;
             const float one = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, next_bias.one)));
-            __syncthreads();
+            arrive();
+            bring.tail(here_tile, a.width);
             const int k0 = tile * KT;
             tile = walk.next(tile);
-            ask(tile);
-            if (!busy) continue;
+            if constexpr (STAGES == 2) ask(tile, there_tile);
+            if (!busy) return;
             const bool masked = k0 + KT > few || a.groups;
             float here = 0.0f;
 #pragma unroll 1
@@ -1032,7 +1110,7 @@ hot_attention_queries_kernel(AttentionArgs a)
                 for (int u = 0; u < 2; ++u)
 #pragma unroll
                     for (int x = 0; x < KS; ++x) {
-                        const V8<T> fk = R::along(k_tile, c * 32 + u * 16, x, own), fv = R::along(v_tile, c * 32 + u * 16, x, own);
+                        const V8<T> fk = R::along(here_tile, c, u, x, own), fv = R::along(here_tile + R::kBytes, c, u, x, own);
 #pragma unroll
                         for (int n = 0; n < QB; ++n) {
                             s[u][n].mac(fk, qf[n][x]);
@@ -1041,10 +1119,12 @@ hot_attention_queries_kernel(AttentionArgs a)
                     }
                 const Settled settled;
                 Pieces<T> dz[QB];
+                const unsigned none = (unsigned)(Staging::kRoom + lane);           // where what is beyond the bins goes
+                float counts[TABLE ? QB : 1][8];
                 by_form(form, masked, [&](auto how) {
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
-                        const int row0 = c * 32 + u * 16 + g * 4;
+                        const int row0 = R::row_of(c, u, g);
                         i4 kc = i4(0), kgr = i4(0);
                         if constexpr (how.kForm != kOne) kc = *reinterpret_cast<const i4 *>(codes + row0);
                         if constexpr (how.kMasked) kgr = *reinterpret_cast<const i4 *>(groups + row0);
@@ -1057,10 +1137,8 @@ hot_attention_queries_kernel(AttentionArgs a)
                                 unsigned at_code = 0;
                                 const bool sees = !how.kMasked || !((k0 + row0 + i > at[n].last) | (kgr[i] != at[n].group));
                                 if constexpr (how.kForm == kStaged) {
-                                    const unsigned none = (unsigned)(Bias<THREADS>::kRoom + lane);
                                     at_code = (unsigned)(at[n].code - low - kc[i]);
                                     at_code = at_code < none ? at_code : none;
-                                    if constexpr (how.kMasked) at_code = sees ? at_code : none;
                                     bias_here = staged[at_code];
                                 } else if constexpr (how.kForm == kFar) {
                                     const unsigned last = (unsigned)a.codes - 1u;
@@ -1075,7 +1153,7 @@ hot_attention_queries_kernel(AttentionArgs a)
                                 if constexpr (TABLE) {
                                     if constexpr (how.kForm == kOne) here += w;
                                     else if constexpr (how.kForm == kStaged) {
-                                        add(bins + at_code, w);
+                                        counts[n][u * 4 + i] = w;
                                     } else {
                                         const unsigned to = (unsigned)a.bucket[at_code].x, most = (unsigned)a.buckets - 1u;
                                         add(sums + (to < most ? to : most), w);
@@ -1084,10 +1162,44 @@ hot_attention_queries_kernel(AttentionArgs a)
                             }
                         }
                     }
+                    if constexpr (TABLE && how.kForm == kStaged) {
+                        const int row0 = R::row_of(c, 0, g);
+                        if (lined) {
+                            // Queries L of a block and eight neighbouring keys: distance D + L of the first key is that of key e and query L + e, which is a lane of this
+                            // block's row or, sixteen distances on, one of the next: two sums over eight lanes each, and the blocks' overlap added up.  Three
+                            // additions to LDS where single pairs took sixteen (some 270 cycles each: LDS adds floats one lane after the other).
+                            const int from = line_code + wave * QB * 16 + col - low - codes[row0];
+                            float carry = 0.0f;
+#pragma unroll
+                            for (int n = QB - 1; n >= 0; --n) {
+                                float same_row = counts[n][0], next_row = 0.0f;
+                                sum_along<1>(counts[n], same_row, next_row);
+                                const unsigned bin = (unsigned)(from + n * 16);
+                                add(bins + (bin < none ? bin : none), same_row + carry);
+                                carry = next_row;
+                            }
+                            const unsigned bin = (unsigned)(from - 16);
+                            add(bins + (bin < none ? bin : none), carry);
+                        } else {
+#pragma unroll
+                            for (int u = 0; u < 2; ++u) {
+                                const i4 kc = *reinterpret_cast<const i4 *>(codes + row0 + 4 * u);
+#pragma unroll
+                                for (int n = 0; n < QB; ++n)
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i) {
+                                        const float w = counts[n][u * 4 + i];
+                                        unsigned bin = (unsigned)(at[n].code - low - kc[i]);
+                                        bin = w != 0.0f && bin < none ? bin : none;
+                                        add(bins + bin, w);
+                                    }
+                            }
+                        }
+                    }
                 });
 #pragma unroll
                 for (int x = 0; x < DB; ++x) {
-                    const V8<T> f = R::across(k_tile, c * 32, x * 16, own);
+                    const V8<T> f = R::across(here_tile, c, x * 16, own);
 #pragma unroll
                     for (int n = 0; n < QB; ++n) dz[n].mac(dq[x][n], f);
                 }
@@ -1112,6 +1224,18 @@ hot_attention_queries_kernel(AttentionArgs a)
                     }
                 }
             }
+        };
+        if constexpr (STAGES == 2) ask(tile, lds);
+        int buffer = 0;
+        while (tile < end_tile) {
+            if constexpr (STAGES == 2) {
+                step(lds + buffer * 2 * R::kBytes, lds + (1 - buffer) * 2 * R::kBytes, buffer);
+                buffer = 1 - buffer;
+            } else {
+                __syncthreads();
+                ask(tile, lds);
+                step(lds, lds, 0);
+            }
         }
         const Settled settled;
         if (a.grad_q)
@@ -1134,7 +1258,7 @@ hot_attention_queries_kernel(AttentionArgs a)
     if constexpr (TABLE) {
         flush();
         __syncthreads();
-        float *const to = a.parts + unit_item * a.buckets;
+        float *const to = a.parts + ((((long)chunk * a.heads + h) * a.tiles_q + tile_q) * a.splits + split) * a.buckets;
         for (int i = (int)threadIdx.x; i < a.buckets; i += THREADS) {
             float sum = all_sums[i];
 #pragma unroll
@@ -1179,7 +1303,7 @@ hot_attention_table_kernel(AttentionArgs a)
 
 inline dim3 blocks_for(long items)
 {
-    const long most = 1L << 20, up = (items + 7) & ~7L;
+    const long most = 1L << 20, up = items;
     return up <= most ? dim3((unsigned)up) : dim3((unsigned)most, (unsigned)((up + most - 1) / most));
 }
 

@@ -10,8 +10,32 @@
 #include "vec.h"
 #include "element.h"
 #include "attention_args.h"
+#include "fragment.h"
 
 namespace {
+
+// Rows of `width` elements as rows of `wide`, a multiple of eight, with zeros behind; those of negative groups are zeros.  [batch, heads, tokens, wide]
+template <class T>
+__global__ void __launch_bounds__(256)
+hot_attention_pack_kernel(const T *__restrict__ from, T *__restrict__ to, hot_pitch p, long rows, int heads, int tokens, int width, int wide, const int32_t *groups, int group_rows)
+{
+    const int pieces = wide / 8;
+    for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < rows * pieces; i += (long)gridDim.x * 256) {
+        const long row = i / pieces;
+        const int c = (int)(i % pieces), t = (int)(row % tokens), h = (int)(row / tokens % heads), b = (int)(row / tokens / heads);
+        const bool there = !group_rows || groups[(long)(b % group_rows) * tokens + t] >= 0;
+        *reinterpret_cast<V8<T> *>(to + row * wide + c * 8) = eight(from + b * p.batch + h * p.head + t * p.row, c * 8, width, there);
+    }
+}
+
+void pack_rows(const void *from, void *to, const hot_pitch &p, int batch, int heads, int tokens, int width, int wide, int bytes, const int32_t *groups, int group_rows, hipStream_t s)
+{
+    const long rows = (long)batch * heads * tokens, blocks = (rows * (wide / 8) + 255) / 256;
+    if (!rows) return;
+    const unsigned n = (unsigned)(blocks < 8192 ? blocks : 8192);
+    if (bytes == 2) hot_attention_pack_kernel<_Float16><<<n, 256, 0, s>>>(static_cast<const _Float16 *>(from), static_cast<_Float16 *>(to), p, rows, heads, tokens, width, wide, groups, group_rows);
+    else hot_attention_pack_kernel<float><<<n, 256, 0, s>>>(static_cast<const float *>(from), static_cast<float *>(to), p, rows, heads, tokens, width, wide, groups, group_rows);
+}
 
 using hot_detail::AttentionArgs;
 
@@ -112,7 +136,17 @@ BackwardCut keys_cut(const hot_attention_desc &d)
 
 long up16(long bytes) { return (bytes + 15) & ~15L; }
 
+// Whether a tensor's rows have to be copied before they can go to LDS: 16-bit elements off the 4-byte grid, or 64 rows that 31 bits cannot span
+bool copied(const hot_attention_desc &d, const hot_pitch &p)
+{
+    const long bytes = type_bytes(d.dtype);
+    return (bytes == 2 && (d.loose || (d.width | p.batch | p.head | p.row) % 2)) || p.row >= (1L << 31) / 64 / bytes - d.width;
+}
+
+long packed_width(const hot_attention_desc &d) { return (d.width + 7) / 8 * 8; }
+
 struct Room {
+    long pack_q, pack_k, pack_v, pack_go;        // negative: as they lie
     long query_spans, key_spans, part_o, part_ml, d, bounds, parts, part_k, part_v, all;
 };
 
@@ -129,6 +163,11 @@ Room room_of(const hot_attention_desc &d, bool backward)
     take(d.tables ? (long)d.tables * d.heads * d.codes * 4 : 0);
     r.query_spans = take((long)d.groups * ((d.queries + 63) / 64) * 8);
     r.key_spans = take((long)d.groups * ((d.keys + 63) / 64) * 8);
+    const auto pack = [&](const hot_pitch &p, long heads, long tokens) { return copied(d, p) ? take(d.batch * heads * tokens * packed_width(d) * type_bytes(d.dtype)) : -1L; };
+    r.pack_k = pack(d.k, d.kv_heads, d.keys);
+    r.pack_v = pack(d.v, d.kv_heads, d.keys);
+    r.pack_q = backward ? pack(d.q, d.heads, d.queries) : -1L;
+    r.pack_go = backward ? pack(d.grad_o, d.heads, d.queries) : -1L;
     if (!backward) {
         const long splits = forward_cut(d).splits;
         r.part_o = take(splits > 1 ? splits * rows * d.width * 4 : 0);
@@ -187,7 +226,7 @@ bool give(AttentionArgs &a, const hot_attention_desc &d, const Room &r, char *ws
     if (a.all_rows && (!q || !on_element(q, d.dtype))) return false;
     if (d.keys && d.batch && (!k || !v || !on_element(k, d.dtype) || !on_element(v, d.dtype))) return false;
     if (d.tables && (!table || !query_code || !key_code || !query_range || !key_range || !bucket || !on_element(table, d.table_dtype) || !aligned4(query_code) ||
-                     !aligned4(key_code) || !aligned8(query_range) || !aligned8(key_range) || !aligned8(bucket)))
+                     !aligned4(key_code) || !aligned16(query_range) || !aligned16(key_range) || !aligned8(bucket)))
         return false;
     if (d.groups && (!query_groups || !key_groups || !aligned4(query_groups) || !aligned4(key_groups))) return false;
     a.q = q;
@@ -196,8 +235,8 @@ bool give(AttentionArgs &a, const hot_attention_desc &d, const Room &r, char *ws
     a.table = table;
     a.query_code = query_code ? query_code + d.first_query : nullptr;
     a.key_code = key_code;
-    a.query_range = reinterpret_cast<const int2 *>(query_range);
-    a.key_range = reinterpret_cast<const int2 *>(key_range);
+    a.query_range = reinterpret_cast<const int4 *>(query_range);
+    a.key_range = reinterpret_cast<const int4 *>(key_range);
     a.bucket = reinterpret_cast<const int2 *>(bucket);
     a.query_groups = query_groups;
     a.key_groups = key_groups;
@@ -205,6 +244,34 @@ bool give(AttentionArgs &a, const hot_attention_desc &d, const Room &r, char *ws
     a.query_spans = reinterpret_cast<int2 *>(ws + r.query_spans);
     a.key_spans = reinterpret_cast<int2 *>(ws + r.key_spans);
     a.part_o = reinterpret_cast<float *>(ws + r.part_o);
+    return true;
+}
+
+// The tensors that go to LDS: copied, or as they lie.  False if one is off the grid that the description promises.
+bool place(AttentionArgs &a, const hot_attention_desc &d, const Room &r, char *ws, bool backward, hipStream_t s)
+{
+    struct Part {
+        const void **at;
+        hot_pitch *pitch;
+        long room;
+        int heads, tokens;
+        const int32_t *groups;
+    } parts[4] = {{&a.k, &a.p_k, r.pack_k, a.kv_heads, a.keys, a.key_groups},
+                  {&a.v, &a.p_v, r.pack_v, a.kv_heads, a.keys, a.key_groups},
+                  {&a.q, &a.p_q, r.pack_q, a.heads, a.queries, a.query_groups},
+                  {&a.grad_o, &a.p_go, r.pack_go, a.heads, a.queries, a.query_groups}};
+    for (int i = 0; i < (backward ? 4 : 2); ++i) {
+        const Part &p = parts[i];
+        if (p.room < 0 && !aligned4(*p.at)) return false;
+    }
+    for (int i = 0; i < (backward ? 4 : 2); ++i) {
+        Part &p = parts[i];
+        if (p.room < 0) continue;
+        const long w = packed_width(d);
+        pack_rows(*p.at, ws + p.room, *p.pitch, a.batch, p.heads, p.tokens, a.width, (int)w, type_bytes(d.dtype), p.groups, a.groups, s);
+        *p.at = ws + p.room;
+        *p.pitch = hot_pitch{p.heads * p.tokens * w, p.tokens * w, w};
+    }
     return true;
 }
 
@@ -250,6 +317,7 @@ int hot_attention_forward(const hot_attention_desc *desc, const void *q, const v
     a.stats = stats;
     a.part_ml = reinterpret_cast<float *>(ws + r.part_ml);
     hipStream_t s = static_cast<hipStream_t>(stream);
+    if (!place(a, *desc, r, ws, false, s)) return HOT_EINVAL;
     HOT_BY_TYPE(attention_begin, a);
     HOT_BY_TYPE(attention_forward, a);
     return hot_detail::note_hip(hipGetLastError());
@@ -285,6 +353,7 @@ int hot_attention_backward(const hot_attention_desc *desc, const void *q, const 
     a.part_k = reinterpret_cast<float *>(ws + r.part_k);
     a.part_v = reinterpret_cast<float *>(ws + r.part_v);
     hipStream_t s = static_cast<hipStream_t>(stream);
+    if (!place(a, *desc, r, ws, true, s)) return HOT_EINVAL;
     if (a.all_rows) {
         a.bounds_count = t == HOT_F16 ? (long)desc->batch * (desc->heads + desc->kv_heads) : 0;
         HOT_BY_TYPE(attention_begin, a);

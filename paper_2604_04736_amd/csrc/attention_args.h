@@ -21,7 +21,8 @@ struct AttentionArgs {
     hot_pitch p_q, p_k, p_v, p_o, p_go, p_gq, p_gk, p_gv;
     const void *q, *k, *v, *table, *grad_o;
     const int32_t *query_code, *key_code, *query_groups, *key_groups;
-    const int2 *query_range, *key_range, *bucket;
+    const int4 *query_range, *key_range;
+    const int2 *bucket;
     void *o, *rest, *grad_q, *grad_k, *grad_v, *grad_table;
     float *stats;                      // [all_rows, 2]: the largest z in units of log 2, and log2 of the sum
     float *bias;                       // [tables, heads, codes], in units of log 2

@@ -1,9 +1,8 @@
 // Blocks of 16 x 16 results of the matrix instruction, for the kernels of attention.h, and their operands out of LDS.
 //
 // An instruction contracts 32 indices: lane l brings line l % 16 of its operand at indices 8 (l / 16) .. + 7, and receives results (4 (l / 16) + i, l % 16),
-// i = 0 .. 3, the second index being B's line.  Two blocks of results, one below the other, thus leave eight rows of one column in a lane, which is the
-// form of an operand that contracts those 32 rows, if the other operand takes them in the same order: index 8 g + i is row 4 g + i of the upper block (i < 4)
-// or 4 g + i - 4 of the lower.  So the softmax's results go from one product into the next without leaving their lanes.
+// i = 0 .. 3, the second index being B's line.  Two blocks of results thus leave eight rows of one column in a lane, which is the
+// form of an operand that contracts those 32 rows, if the other operand takes them in the same order (Rows).  So the softmax's results go from one product into the next without leaving their lanes.
 // float32 is multiplied by the instruction of its own, four indices at a time, on the same operands.
 #ifndef HOT_FRAGMENT_H
 #define HOT_FRAGMENT_H
@@ -25,6 +24,7 @@ typedef short s4v __attribute__((ext_vector_type(4)));
 typedef short s8v __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) char lds_char;
 typedef __attribute__((address_space(3))) s4v lds_s4v;
+typedef __attribute__((address_space(3))) f4 lds_f4;
 
 // The wait states between a run of matrix instructions and the first read of their results: 32, which the scheduler may not move
 // (the compiler's own can be missing where a branch lies between).  Blocks hand their registers out only against one of these.
@@ -83,52 +83,73 @@ struct Pieces {
     }
 };
 
-// A tile of rows of DP elements in LDS.  LDS serves 256 bytes at once if they are in different banks: sixteen lanes of sixteen bytes, which are those of sixteen rows
-// (along), or eight rows of 32 bytes (the transposing read across).  Rows of 16-bit elements have their sixteen-byte pieces permuted by the row so that
-// both are; rows of float32, which the slower instruction bounds, are sixteen bytes longer than their elements.
-template <class T, int DP>
+// A tile of ROWS rows of DP elements in LDS, and the order in which products take its rows: line 4 a + b of block u of sixteen lines (two blocks to 32 rows c) is row
+// kSpread a + 8 c + 4 u + b.  A lane thus holds the results of eight neighbouring rows, and the four lanes of one column those of rows kSpread apart, so that
+// where rows and columns are tokens of a line, sixty-four lanes have sixty-four different distances.
+// LDS serves 256 bytes at once if they are in different banks: sixteen bytes each of the sixteen rows of a block (along), or 32 bytes each of eight rows
+// (the transposing read across; float32: 64 bytes of four).  Pieces of sixteen bytes are permuted by the row so that both are.
+template <class T, int DP, int ROWS>
 struct Rows {
-    static constexpr bool kPermuted = sizeof(T) == 2;
-    static constexpr int kPitch = kPermuted ? (DP <= 32 ? 64 : (DP <= 64 ? 128 : 256)) : DP * (int)sizeof(T) + 16;
+    static constexpr bool kSmall = sizeof(T) == 2;
+    static constexpr int kSpread = ROWS / 4;
+    static constexpr int kPitch = kSmall ? (DP <= 32 ? 64 : (DP <= 64 ? 128 : 256)) : DP * 4 + 64;
+    static constexpr int kBytes = (ROWS * kPitch + (kSmall ? 0 : 4 * 64) + 1023) / 1024 * 1024;         // (whole loads of a wave)
 
-    static __device__ __forceinline__ int turn(int row)
-    {
-        if constexpr (!kPermuted) return 0;
-        else if constexpr (kPitch == 256) return (row & 7) << 1 | (row >> 3 & 1);
-        else if constexpr (kPitch == 128) return (row >> 1 & 3) << 1 | (row >> 3 & 1);
-        else return (row >> 2 & 1) << 1 | (row >> 3 & 1);
-    }
-    // the byte of element `at` (a multiple of sixteen bytes, if the piece as a whole is meant) of a row
+    static __device__ __forceinline__ int row_of(int c, int u, int a) { return kSpread * a + 8 * c + 4 * u; }
+
+    // the byte of element `at` of a row
     static __device__ __forceinline__ int place(int row, int at)
     {
-        const int byte = at * (int)sizeof(T);
-        return row * kPitch + (byte ^ turn(row) << 4);
-    }
-    // operand of lines row0 .. + 15 (row0 a multiple of sixteen) at elements 32 ks ..
-    static __device__ __forceinline__ V8<T> along(const char *tile, int row0, int ks, int lane)
-    {
-        const int row = lane & 15, at = ks * 32 + (lane >> 4) * 8;
-        if constexpr (kPermuted) return *reinterpret_cast<const V8<T> *>(tile + row0 * kPitch + place(row, at));
+        const int byte = at * (int)sizeof(T), a = row / kSpread & 3;
+        if constexpr (!kSmall) return row * kPitch + a * 64 + (byte ^ a << 4);
         else {
-            // (sixteen bytes at a time: rows are on no larger boundary)
-            const f4 low = *reinterpret_cast<const f4 *>(tile + row0 * kPitch + place(row, at)), high = *reinterpret_cast<const f4 *>(tile + row0 * kPitch + place(row, at) + 16);
+            const int high = a >> 1, low = a & 1;
+            int turn;
+            if constexpr (kPitch == 256) turn = (row & 3) << 1 | low << 3 | high;
+            else if constexpr (kPitch == 128) turn = (row & 2) | low << 2 | high;
+            else turn = low << 1 | high;
+            return row * kPitch + (byte ^ turn << 4);
+        }
+    }
+    // ... and back: which row and element lie at a byte; false for what belongs to none
+    static __device__ __forceinline__ bool at_byte(int byte, int &row, int &at)
+    {
+        if constexpr (kSmall) {
+            row = byte / kPitch;
+            at = (place(row, 0) - row * kPitch ^ byte % kPitch) / 2;
+            return row < ROWS && at < DP;
+        } else {
+            constexpr int SEGMENT = kSpread * kPitch + 64;
+            const int a = byte / SEGMENT, in = byte % SEGMENT, of_row = in % kPitch;
+            row = a * kSpread + in / kPitch;
+            at = (of_row ^ a << 4) / 4;
+            return a < 4 && in < kSpread * kPitch && of_row < DP * 4;
+        }
+    }
+    // operand of the sixteen lines of block u of rows c at elements 32 ks ..
+    static __device__ __forceinline__ V8<T> along(const lds_char *tile, int c, int u, int ks, int lane)
+    {
+        const int row = row_of(c, u, lane >> 2 & 3) + (lane & 3), at = ks * 32 + (lane >> 4) * 8;
+        if constexpr (kSmall) return *(const __attribute__((address_space(3))) V8<T> *)(tile + place(row, at));
+        else {
+            const f4 low = *(const lds_f4 *)(tile + place(row, at)), high = *(const lds_f4 *)(tile + place(row, at + 4));
             return __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7);
         }
     }
-    // operand whose lines are elements e0 .. + 15 and whose 32 indices are rows row0 .. + 31, in the order above
-    static __device__ __forceinline__ V8<T> across(const char *tile, int row0, int e0, int lane)
+    // operand whose lines are elements e0 .. + 15 and whose 32 indices are rows c, in the order of a lane's results of both blocks
+    static __device__ __forceinline__ V8<T> across(const lds_char *tile, int c, int e0, int lane)
     {
-        const int g = lane >> 4, i = lane & 15;
-        if constexpr (kPermuted) {
+        const int row = row_of(c, 0, lane >> 4), i = lane & 15;
+        if constexpr (kSmall) {
             // (a transposing read: of four rows of sixteen elements that sixteen lanes name, lane i receives element i of each)
-            lds_char *const at = (lds_char *)(tile + row0 * kPitch + place(4 * g + (i >> 2), e0 + (i & 3) * 4));
+            const lds_char *const at = tile + place(row + (i >> 2), e0 + (i & 3) * 4);
             const s4v up = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v *)at);
-            const s4v low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v *)(at + 16 * kPitch));
+            const s4v low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v *)(at + 4 * kPitch));
             return __builtin_bit_cast(V8<T>, __builtin_shufflevector(up, low, 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
             V8<T> v;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = *reinterpret_cast<const T *>(tile + (row0 + 4 * g + (j & 3) + (j >> 2) * 16) * kPitch + (e0 + i) * (int)sizeof(T));
+            for (int j = 0; j < 8; ++j) v[j] = *(const __attribute__((address_space(3))) T *)(tile + place(row, e0 + i) + j * kPitch);
             return v;
         }
     }

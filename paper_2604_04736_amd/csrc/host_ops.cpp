@@ -636,6 +636,7 @@ hot_attention_desc attention_desc(const Tensor &q, const Tensor &k, const Tensor
     d.groups = query_groups.defined() ? (int32_t)query_groups.size(0) : 0;
     d.causal = causal;
     d.dtype = type_of(q);
+    for (const Tensor *t : {&q, &k, &v}) d.loose |= reinterpret_cast<uintptr_t>(t->const_data_ptr()) % 4 != 0;
     return d;
 }
 
@@ -690,6 +691,7 @@ struct Attention : torch::autograd::Function<Attention> {
         const Tensor dtable = table.defined() && ctx->needs_input_grad(3) ? at::empty_like(table) : Tensor();
         d.o = pitch_of(o);
         d.grad_o = pitch_of(up);
+        d.loose |= reinterpret_cast<uintptr_t>(up.const_data_ptr()) % 4 != 0;
         if (dq.defined()) d.grad_q = pitch_of(dq);
         if (dk.defined()) d.grad_k = pitch_of(dk);
         if (dv.defined()) d.grad_v = pitch_of(dv);
