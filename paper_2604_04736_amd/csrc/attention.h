@@ -129,12 +129,31 @@ __device__ __forceinline__ void arrive()
     __syncthreads();
 }
 
+// What all lanes read alike, and nobody writes meanwhile, through the scalar cache: vector loads come back in order, and one that is waited for would wait for the tile on its way
+typedef int i2 __attribute__((ext_vector_type(2)));
+template <class X>
+__device__ __forceinline__ X alike_as(const void *p)
+{
+    return *(const __attribute__((address_space(4))) X *)(uintptr_t)p;
+}
+__device__ __forceinline__ float alike(const float *p) { return alike_as<float>(p); }
+__device__ __forceinline__ int2 alike(const int2 *p)
+{
+    const i2 v = alike_as<i2>(p);
+    return int2{v[0], v[1]};
+}
+__device__ __forceinline__ int4 alike(const int4 *p)
+{
+    const i4 v = alike_as<i4>(p);
+    return int4{v[0], v[1], v[2], v[3]};
+}
+
 // ... of codes, whose entries also say whether codes go up by one from token to token (z)
 __device__ __forceinline__ int2 codes_over(const int4 *ranges, int first, int last, bool &line)
 {
-    int4 s = ranges[first >> 6];
+    int4 s = alike(ranges + (first >> 6));
     for (int t = (first >> 6) + 1; t <= last >> 6; ++t) {
-        const int4 u = ranges[t];
+        const int4 u = alike(ranges + t);
         s.x = u.x < s.x ? u.x : s.x;
         s.y = u.y > s.y ? u.y : s.y;
         s.z &= u.z;
@@ -143,23 +162,27 @@ __device__ __forceinline__ int2 codes_over(const int4 *ranges, int first, int la
     return int2{s.x, s.y};
 }
 
-// Smallest and largest entry of `spans` over tiles of 64 from that of row `first` to that of row `last`
-__device__ __forceinline__ int2 span_over(const int2 *spans, int first, int last)
+// Smallest and largest group of 64 rows each, and whether some are of a negative one (z), from the 64 of row `first` to those of row `last`
+__device__ __forceinline__ int4 span_over(const int4 *spans, int first, int last)
 {
-    int2 s = spans[first >> 6];
+    int4 s = alike(spans + (first >> 6));
     for (int t = (first >> 6) + 1; t <= last >> 6; ++t) {
-        const int2 u = spans[t];
+        const int4 u = alike(spans + t);
         s.x = u.x < s.x ? u.x : s.x;
         s.y = u.y > s.y ? u.y : s.y;
+        s.z |= u.z;
     }
     return s;
 }
 
+// Whether all rows of both spans are of one group: every pair may see each other, by groups
+__device__ __forceinline__ bool together(int4 a, int4 b) { return (a.z | b.z) == 0 && a.x == a.y && b.x == b.y && a.x == b.x; }
+
 // The tiles first .. end - 1 of T rows whose groups can meet those of `mine`, one after the other: sixty-four are looked at at once
 template <int T>
 struct Walk {
-    const int2 *spans;           // of 64 rows each; null: all tiles
-    int2 mine;
+    const int4 *spans;           // of 64 rows each; null: all tiles
+    int4 mine;
     int base, end;
     unsigned long mask;
 
@@ -169,12 +192,12 @@ struct Walk {
         const int t = from + ((int)threadIdx.x & 63);
         bool meets = t < end;
         if (meets && spans) {
-            const int2 s = spans[t * T >> 6];
+            const int4 s = spans[t * T >> 6];
             meets = s.x <= s.y && s.x <= mine.y && s.y >= mine.x;
         }
         mask = __ballot(meets);
     }
-    __device__ __forceinline__ int begin(const int2 *spans_, int2 mine_, int first, int end_)
+    __device__ __forceinline__ int begin(const int4 *spans_, int4 mine_, int first, int end_)
     {
         spans = spans_;
         mine = mine_;
@@ -219,9 +242,9 @@ struct Bias {
         low = low < 0 ? 0 : (low < a.codes ? low : a.codes - 1);
         high = high < low ? low : (high < a.codes ? high : a.codes - 1);
         count = high - low + 1;
-        const int2 run = a.bucket[low];
+        const int2 run = alike(a.bucket + low);
         all = run.x;
-        one = bias[low];
+        one = alike(bias + low);
         form = run.y >= high ? kOne : (heads == 1 ? (count <= kRoom ? kStaged : kFar) : (count * heads <= kRoom ? kStaged : kFar));
         const int at = low + ((int)threadIdx.x < count ? (int)threadIdx.x : 0);
         v = bias[at];
@@ -304,7 +327,8 @@ hot_attention_begin_kernel(AttentionArgs a)
             low = l < low ? l : low;
             high = h > high ? h : high;
         }
-        if (lane == 0) (of_keys ? a.key_spans : a.query_spans)[at] = int2{low, high};
+        const int none = __ballot(r < count && g < 0) != 0;
+        if (lane == 0) (of_keys ? a.key_spans : a.query_spans)[at] = int4{low, high, none, 0};
     }
 }
 
@@ -383,6 +407,9 @@ hot_attention_forward_kernel(AttentionArgs a)
     const int all_tiles = (visible + KT - 1) / KT, share = (all_tiles + a.splits - 1) / a.splits;
     const int end_tile = (split + 1) * share < all_tiles ? (split + 1) * share : all_tiles;
 
+    const int4 *const spans = a.groups ? a.key_spans + (long)(b % a.groups) * ((a.keys + 63) >> 6) : nullptr;
+    const int4 my_groups = a.groups ? span_over(a.query_spans + (long)(b % a.groups) * ((a.queries + 63) >> 6), first_i, last_i) : int4{0, 0, 0, 0};
+    bool next_apart = false;             // whether groups keep some pairs of the next tile apart
     Walk<KT> walk;
     B bring;
     bring.begin(a.p_k.row, a.p_v.row, a.width);
@@ -402,7 +429,9 @@ hot_attention_forward_kernel(AttentionArgs a)
         if (a.tables)
 #pragma unroll
             for (int n = 0; n < QB; ++n) next_one[n] = bias[(long)(at[n].h - unit * a.pack) * a.codes + next_bias.low];
-        bring.ask(k + (long)tile * KT * a.p_k.row, a.p_k.row, v + (long)tile * KT * a.p_v.row, a.p_v.row, a.width, last, kg ? kg + tile * KT : nullptr, to);
+        const int4 span = a.groups ? alike(spans + (tile * KT >> 6)) : int4{0, 0, 0, 0};
+        next_apart = a.groups && !together(span, my_groups);
+        bring.ask(k + (long)tile * KT * a.p_k.row, a.p_k.row, v + (long)tile * KT * a.p_v.row, a.p_v.row, a.width, last, span.z ? kg + tile * KT : nullptr, to);
     };
 
     Block16<T> o[DB][QB];
@@ -416,8 +445,7 @@ hot_attention_forward_kernel(AttentionArgs a)
 #pragma unroll
     for (int n = 0; n < QB; ++n) any = any || at[n].there;
     const bool busy = __ballot(any) != 0;            // (waves without queries only bring tiles)
-    int tile = walk.begin(a.groups ? a.key_spans + (long)(b % a.groups) * ((a.keys + 63) >> 6) : nullptr,
-                          a.groups ? span_over(a.query_spans + (long)(b % a.groups) * ((a.queries + 63) >> 6), first_i, last_i) : int2{0, 0}, split * share, end_tile);
+    int tile = walk.begin(spans, my_groups, split * share, end_tile);
     // One tile: the products of what is `here`, while the next one comes to `there`
     auto step = [&](lds_char *__restrict here_tile, lds_char *__restrict there_tile, int buffer) {
         int *const codes = all_codes + buffer * KT, *const groups = all_groups + buffer * KT;
@@ -435,6 +463,7 @@ hot_attention_forward_kernel(AttentionArgs a)
             one[n] = next_one[n];
             own[n] = (at[n].h - unit * a.pack) * next_bias.count + at[n].code - low;
         }
+        const bool apart = next_apart;
         arrive();
         bring.tail(here_tile, a.width);
         const int k0 = tile * KT;
@@ -458,7 +487,7 @@ hot_attention_forward_kernel(AttentionArgs a)
             float z[QB][8], top[QB];
 #pragma unroll
             for (int n = 0; n < QB; ++n) top[n] = kNone;
-            by_form(form, k0 + KT > few || a.groups, [&](auto how) {
+            by_form(form, k0 + KT > few || apart, [&](auto how) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     const int row0 = R::row_of(c, u, g);
@@ -751,7 +780,9 @@ hot_attention_keys_kernel(AttentionArgs a)
     const int last_key = (tile_k + 1) * TILE < a.keys ? (tile_k + 1) * TILE - 1 : a.keys - 1;
     bool line = false;
     const int2 key_codes = a.tables ? codes_over(a.key_range, tile_k * TILE, last_key, line) : int2{0, 0};
-    const int2 mine = a.groups ? span_over(a.key_spans + (long)(b % a.groups) * ((a.keys + 63) >> 6), tile_k * TILE, last_key) : int2{0, 0};
+    const int4 *const spans = a.groups ? a.query_spans + (long)(b % a.groups) * tiles_q : nullptr;
+    const int4 my_groups = a.groups ? span_over(a.key_spans + (long)(b % a.groups) * ((a.keys + 63) >> 6), tile_k * TILE, last_key) : int4{0, 0, 0, 0};
+    bool next_apart = false;             // whether groups keep some pairs of the next tile apart
     bool any = false;
 #pragma unroll
     for (int n = 0; n < KB; ++n) any = any || group[n] >= 0;
@@ -790,9 +821,11 @@ hot_attention_keys_kernel(AttentionArgs a)
                 }
             }
             next_bias.template ask<false>(a, bias, query_codes(a, tile * QT, tile * QT + (last < QT - 1 ? last : QT - 1), line), key_codes, 1);
-            bring.ask(q + (long)tile * QT * a.p_q.row, a.p_q.row, up + (long)tile * QT * a.p_go.row, a.p_go.row, a.width, last, qg ? qg + tile * QT : nullptr, to);
+            const int4 span = a.groups ? alike(spans + tile) : int4{0, 0, 0, 0};
+            next_apart = a.groups && !together(span, my_groups);
+            bring.ask(q + (long)tile * QT * a.p_q.row, a.p_q.row, up + (long)tile * QT * a.p_go.row, a.p_go.row, a.width, last, span.z ? qg + tile * QT : nullptr, to);
         };
-        int tile = walk.begin(a.groups ? a.query_spans + (long)(b % a.groups) * tiles_q : nullptr, mine, first_tile, end_tile);
+        int tile = walk.begin(spans, my_groups, first_tile, end_tile);
         // One tile: the products of what is `here`, while the next one comes to `there`
         auto step = [&](lds_char *__restrict here, lds_char *__restrict there, int buffer) {
             int *const codes = all_codes + buffer * QT, *const groups = all_groups + buffer * QT;
@@ -807,6 +840,7 @@ hot_attention_keys_kernel(AttentionArgs a)
             next_bias.template put<false>(a, bias, staged, nullptr, 1);
             const int form = __builtin_amdgcn_readfirstlane(next_bias.form), low = __builtin_amdgcn_readfirstlane(next_bias.low);
             const float one = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, next_bias.one)));
+            const bool apart = next_apart;
             arrive();
             bring.tail(here, a.width);
             const int i0 = tile * QT;
@@ -814,7 +848,7 @@ hot_attention_keys_kernel(AttentionArgs a)
             if constexpr (STAGES == 2) ask(tile, there);
             if (!busy) return;
             // (queries behind the last have l = infinity, keys behind the last are zeros and are not stored)
-            const bool masked = a.groups || (a.causal && i0 + past < last_key);
+            const bool masked = apart || (a.causal && i0 + past < last_key);
 #pragma unroll 1
             for (int c = 0; c < QT / 32; ++c) {
                 const int at = fresh_lane(lane);
@@ -1055,6 +1089,9 @@ hot_attention_queries_kernel(AttentionArgs a)
                 code_high = y > code_high ? y : code_high;
             }
         }
+        const int4 *const spans = a.groups ? a.key_spans + (long)(b % a.groups) * ((a.keys + 63) >> 6) : nullptr;
+        const int4 my_groups = a.groups ? span_over(a.query_spans + (long)(b % a.groups) * ((a.queries + 63) >> 6), first_i, last_i) : int4{0, 0, 0, 0};
+        bool next_apart = false;             // whether groups keep some pairs of the next tile apart
         Walk<KT> walk;
         Staging next_bias;
         int next_code = 0, next_group = 0;
@@ -1071,15 +1108,16 @@ hot_attention_queries_kernel(AttentionArgs a)
             }
             next_range = a.tables ? codes_over(a.key_range, tile * KT, tile * KT, next_line) : int2{0, 0};
             next_bias.template ask<TABLE>(a, bias, mine_codes, next_range, 1);
-            bring.ask(k + (long)tile * KT * a.p_k.row, a.p_k.row, v + (long)tile * KT * a.p_v.row, a.p_v.row, a.width, last, kg ? kg + tile * KT : nullptr, to);
+            const int4 span = a.groups ? alike(spans + (tile * KT >> 6)) : int4{0, 0, 0, 0};
+            next_apart = a.groups && !together(span, my_groups);
+            bring.ask(k + (long)tile * KT * a.p_k.row, a.p_k.row, v + (long)tile * KT * a.p_v.row, a.p_v.row, a.width, last, span.z ? kg + tile * KT : nullptr, to);
         };
         bool any = false;
 #pragma unroll
         for (int n = 0; n < QB; ++n) any = any || at[n].there;
         const bool busy = __ballot(any) != 0;            // (waves without queries only bring tiles)
         Block16<T> dq[DB][QB];
-        int tile = walk.begin(a.groups ? a.key_spans + (long)(b % a.groups) * ((a.keys + 63) >> 6) : nullptr,
-                              a.groups ? span_over(a.query_spans + (long)(b % a.groups) * ((a.queries + 63) >> 6), first_i, last_i) : int2{0, 0}, split * share, end_tile);
+        int tile = walk.begin(spans, my_groups, split * share, end_tile);
         // One tile: the products of what is `here`, while the next one comes to `there`
         auto step = [&](lds_char *__restrict here_tile, lds_char *__restrict there_tile, int buffer) {
             int *const codes = all_codes + buffer * KT, *const groups = all_groups + buffer * KT;
@@ -1094,13 +1132,14 @@ hot_attention_queries_kernel(AttentionArgs a)
             const int2 range = next_range;
             const bool lined = TABLE && line && next_line;
             const float one = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, next_bias.one)));
+            const bool apart = next_apart;
             arrive();
             bring.tail(here_tile, a.width);
             const int k0 = tile * KT;
             tile = walk.next(tile);
             if constexpr (STAGES == 2) ask(tile, there_tile);
             if (!busy) return;
-            const bool masked = k0 + KT > few || a.groups;
+            const bool masked = k0 + KT > few || apart;
             float here = 0.0f;
 #pragma unroll 1
             for (int c = 0; c < KT / 32; ++c) {

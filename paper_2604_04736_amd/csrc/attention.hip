@@ -161,8 +161,8 @@ Room room_of(const hot_attention_desc &d, bool backward)
     };
     const long rows = (long)d.batch * d.heads * d.queries;
     take(d.tables ? (long)d.tables * d.heads * d.codes * 4 : 0);
-    r.query_spans = take((long)d.groups * ((d.queries + 63) / 64) * 8);
-    r.key_spans = take((long)d.groups * ((d.keys + 63) / 64) * 8);
+    r.query_spans = take((long)d.groups * ((d.queries + 63) / 64) * 16);
+    r.key_spans = take((long)d.groups * ((d.keys + 63) / 64) * 16);
     const auto pack = [&](const hot_pitch &p, long heads, long tokens) { return copied(d, p) ? take(d.batch * heads * tokens * packed_width(d) * type_bytes(d.dtype)) : -1L; };
     r.pack_k = pack(d.k, d.kv_heads, d.keys);
     r.pack_v = pack(d.v, d.kv_heads, d.keys);
@@ -241,8 +241,8 @@ bool give(AttentionArgs &a, const hot_attention_desc &d, const Room &r, char *ws
     a.query_groups = query_groups;
     a.key_groups = key_groups;
     a.bias = reinterpret_cast<float *>(ws);
-    a.query_spans = reinterpret_cast<int2 *>(ws + r.query_spans);
-    a.key_spans = reinterpret_cast<int2 *>(ws + r.key_spans);
+    a.query_spans = reinterpret_cast<int4 *>(ws + r.query_spans);
+    a.key_spans = reinterpret_cast<int4 *>(ws + r.key_spans);
     a.part_o = reinterpret_cast<float *>(ws + r.part_o);
     return true;
 }

@@ -28,7 +28,7 @@ struct AttentionArgs {
     float *bias;                       // [tables, heads, codes], in units of log 2
     float *part_o, *part_ml;           // [splits, all_rows, width], [splits, all_rows, 2]
     float *part_k, *part_v;            // [splits, batch, kv_heads, keys, width]
-    int2 *query_spans, *key_spans;     // [groups, 64s of queries or keys]
+    int4 *query_spans, *key_spans;     // [groups, 64s of queries or keys]
     float *d;                          // [all_rows]
     float *parts;                      // [items of dq, buckets]
     unsigned *bounds;                  // [batch, heads] and [batch, kv_heads]
