@@ -361,13 +361,14 @@ __device__ __forceinline__ int2 query_codes(const AttentionArgs &a, int first, i
 
 // ---------------------------------------------------------------------------------
 template <class T, int DP, int QB, int WAVES, int KT>
-__global__ void __launch_bounds__(64 * WAVES, 2)
+__global__ void __launch_bounds__(64 * WAVES, WAVES == 8 ? 4 : 2)
 hot_attention_forward_kernel(AttentionArgs a)
 {
     constexpr int THREADS = 64 * WAVES, KS = DP / 32, DB = DP / 16, TILE = WAVES * QB * 16;
     typedef Rows<T, DP, KT> R;
     typedef Bring<T, DP, KT, WAVES> B;
-    constexpr int STAGES = kStages<T>;
+    // (one wave with few rows: twice as many of them to a compute unit bring more than a second tile of each)
+    constexpr int STAGES = WAVES == 1 ? 1 : kStages<T>;
     typedef Bias<THREADS, THREADS < 256 ? 256 : (sizeof(T) == 2 && DP > 64 ? 384 : 640)> Staging;
     __shared__ __attribute__((aligned(1024))) char tiles[STAGES * 2 * R::kBytes];
     __shared__ __attribute__((aligned(16))) int all_codes[STAGES * KT], all_groups[STAGES * KT];
@@ -419,6 +420,9 @@ hot_attention_forward_kernel(AttentionArgs a)
     auto ask = [&](int tile, lds_char *to) {
         if (tile >= end_tile) return;
         const int last = a.keys - 1 - tile * KT;
+        const int4 span = a.groups ? alike(spans + (tile * KT >> 6)) : int4{0, 0, 0, 0};
+        next_apart = a.groups && !together(span, my_groups);
+        bring.ask(k + (long)tile * KT * a.p_k.row, a.p_k.row, v + (long)tile * KT * a.p_v.row, a.p_v.row, a.width, last, span.z ? kg + tile * KT : nullptr, to);
         if ((int)threadIdx.x < KT) {
             const int j = tile * KT + ((int)threadIdx.x < last ? (int)threadIdx.x : last);
             next_code = a.tables ? a.key_code[j] : 0;
@@ -429,9 +433,6 @@ hot_attention_forward_kernel(AttentionArgs a)
         if (a.tables)
 #pragma unroll
             for (int n = 0; n < QB; ++n) next_one[n] = bias[(long)(at[n].h - unit * a.pack) * a.codes + next_bias.low];
-        const int4 span = a.groups ? alike(spans + (tile * KT >> 6)) : int4{0, 0, 0, 0};
-        next_apart = a.groups && !together(span, my_groups);
-        bring.ask(k + (long)tile * KT * a.p_k.row, a.p_k.row, v + (long)tile * KT * a.p_v.row, a.p_v.row, a.width, last, span.z ? kg + tile * KT : nullptr, to);
     };
 
     Block16<T> o[DB][QB];
@@ -471,9 +472,9 @@ hot_attention_forward_kernel(AttentionArgs a)
         if constexpr (STAGES == 2) ask(tile, there_tile);
         if (!busy) return;
         // 32 keys at a time: their scores and pieces are as many registers as there is room for beside the sums
+        const int here = fresh_lane(lane);
 #pragma unroll 1
         for (int c = 0; c < KT / 32; ++c) {
-            const int here = fresh_lane(lane);
             Block16<T> acc[2][QB];
 #pragma unroll
             for (int u = 0; u < 2; ++u)
@@ -598,21 +599,25 @@ hot_attention_forward_kernel(AttentionArgs a)
     }
 }
 
-// The splits' results joined: sixteen lanes to a row
+// The splits' results joined: a workgroup to a row, sixteen lanes to its elements and sixteen runs of splits, whose sums are added in their order
 template <class T>
 __global__ void __launch_bounds__(256)
 hot_attention_join_kernel(AttentionArgs a)
 {
-    const int t = (int)threadIdx.x & 15;
-    for (long row = (long)blockIdx.x * 16 + ((int)threadIdx.x >> 4); row < a.all_rows; row += (long)gridDim.x * 16) {
+    __shared__ float sums[16][16 * 8 + 1], totals[16], tops[16];
+    const int t = (int)threadIdx.x & 15, run = (int)threadIdx.x >> 4;
+    for (long row = blockIdx.x; row < a.all_rows; row += gridDim.x) {
         const int i = (int)(row % a.queries), h = (int)(row / a.queries % a.heads), b = (int)(row / a.queries / a.heads);
         float m = kNone;
-#pragma unroll 4
-        for (int s = 0; s < a.splits; ++s) m = __builtin_fmaxf(m, a.part_ml[2 * ((long)s * a.all_rows + row)]);
+        for (int s = run; s < a.splits; s += 16) m = __builtin_fmaxf(m, a.part_ml[2 * ((long)s * a.all_rows + row)]);
+        if (t == 0) tops[run] = m;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 16; ++k) m = __builtin_fmaxf(m, tops[k]);
         const float base = m == kNone ? 0.0f : m;
         float l = 0.0f, o[8] = {};
 #pragma unroll 4
-        for (int s = 0; s < a.splits; ++s) {
+        for (int s = run; s < a.splits; s += 16) {
             const long at = (long)s * a.all_rows + row;
             const float by = two_to(a.part_ml[2 * at] - base);
             l = __builtin_fmaf(a.part_ml[2 * at + 1], by, l);
@@ -620,24 +625,28 @@ hot_attention_join_kernel(AttentionArgs a)
 #pragma unroll
             for (int j = 0; j < 8; ++j) o[j] = __builtin_fmaf(v[j], by, o[j]);
         }
-        const float by = 1.0f / l;
-        T *const to = static_cast<T *>(a.o) + b * a.p_o.batch + h * a.p_o.head + i * a.p_o.row;
-        T *const rest = a.rest ? static_cast<T *>(a.rest) + b * a.p_o.batch + h * a.p_o.head + i * a.p_o.row : nullptr;
+        if (t == 0) totals[run] = l;
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            f4 x, left;
+        for (int j = 0; j < 8; ++j) sums[run][t * 8 + j] = o[j];
+        __syncthreads();
+        if ((int)threadIdx.x < a.width) {
+            l = 0.0f;
+            float x = 0.0f;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                x[j] = l == 0.0f ? 0.0f : o[4 * c + j] * by;
-                left[j] = x[j] - (float)(T)x[j];
+            for (int k = 0; k < 16; ++k) {
+                l += totals[k];
+                x += sums[k][threadIdx.x];
             }
-            four(to, t * 8 + c * 4, a.width, x);
-            if (rest) four(rest, t * 8 + c * 4, a.width, left);
+            x = l == 0.0f ? 0.0f : x / l;
+            const long to = b * a.p_o.batch + h * a.p_o.head + i * a.p_o.row + (long)threadIdx.x;
+            static_cast<T *>(a.o)[to] = (T)x;
+            if (a.rest) static_cast<T *>(a.rest)[to] = (T)(x - (float)(T)x);
+            if (threadIdx.x == 0 && a.stats) {
+                a.stats[2 * row] = l == 0.0f ? 0.0f : m;
+                a.stats[2 * row + 1] = l == 0.0f ? __builtin_inff() : __builtin_log2f(l) - kShift<T>;
+            }
         }
-        if (t == 0 && a.stats) {
-            a.stats[2 * row] = l == 0.0f ? 0.0f : m;
-            a.stats[2 * row + 1] = l == 0.0f ? __builtin_inff() : __builtin_log2f(l) - kShift<T>;
-        }
+        __syncthreads();
     }
 }
 
@@ -808,6 +817,9 @@ hot_attention_keys_kernel(AttentionArgs a)
         auto ask = [&](int tile, lds_char *to) {
             if (tile >= end_tile) return;
             const int last = a.queries - 1 - tile * QT;
+            const int4 span = a.groups ? alike(spans + tile) : int4{0, 0, 0, 0};
+            next_apart = a.groups && !together(span, my_groups);
+            bring.ask(q + (long)tile * QT * a.p_q.row, a.p_q.row, up + (long)tile * QT * a.p_go.row, a.p_go.row, a.width, last, span.z ? qg + tile * QT : nullptr, to);
             if ((int)threadIdx.x < QT) {
                 const int i = tile * QT + ((int)threadIdx.x < last ? (int)threadIdx.x : last);
                 next_m = a.stats[2 * (stat0 + i)];
@@ -821,9 +833,6 @@ hot_attention_keys_kernel(AttentionArgs a)
                 }
             }
             next_bias.template ask<false>(a, bias, query_codes(a, tile * QT, tile * QT + (last < QT - 1 ? last : QT - 1), line), key_codes, 1);
-            const int4 span = a.groups ? alike(spans + tile) : int4{0, 0, 0, 0};
-            next_apart = a.groups && !together(span, my_groups);
-            bring.ask(q + (long)tile * QT * a.p_q.row, a.p_q.row, up + (long)tile * QT * a.p_go.row, a.p_go.row, a.width, last, span.z ? qg + tile * QT : nullptr, to);
         };
         int tile = walk.begin(spans, my_groups, first_tile, end_tile);
         // One tile: the products of what is `here`, while the next one comes to `there`
@@ -849,9 +858,9 @@ hot_attention_keys_kernel(AttentionArgs a)
             if (!busy) return;
             // (queries behind the last have l = infinity, keys behind the last are zeros and are not stored)
             const bool masked = apart || (a.causal && i0 + past < last_key);
+            const int at = fresh_lane(lane);
 #pragma unroll 1
             for (int c = 0; c < QT / 32; ++c) {
-                const int at = fresh_lane(lane);
                 Block16<T> s[2][KB], dp[2][KB];
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
@@ -1100,6 +1109,9 @@ hot_attention_queries_kernel(AttentionArgs a)
         auto ask = [&](int tile, lds_char *to) {
             if (tile >= end_tile) return;
             const int last = a.keys - 1 - tile * KT;
+            const int4 span = a.groups ? alike(spans + (tile * KT >> 6)) : int4{0, 0, 0, 0};
+            next_apart = a.groups && !together(span, my_groups);
+            bring.ask(k + (long)tile * KT * a.p_k.row, a.p_k.row, v + (long)tile * KT * a.p_v.row, a.p_v.row, a.width, last, span.z ? kg + tile * KT : nullptr, to);
             if ((int)threadIdx.x < KT) {
                 const int j = tile * KT + ((int)threadIdx.x < last ? (int)threadIdx.x : last);
                 next_code = a.tables ? a.key_code[j] : 0;
@@ -1108,9 +1120,6 @@ hot_attention_queries_kernel(AttentionArgs a)
             }
             next_range = a.tables ? codes_over(a.key_range, tile * KT, tile * KT, next_line) : int2{0, 0};
             next_bias.template ask<TABLE>(a, bias, mine_codes, next_range, 1);
-            const int4 span = a.groups ? alike(spans + (tile * KT >> 6)) : int4{0, 0, 0, 0};
-            next_apart = a.groups && !together(span, my_groups);
-            bring.ask(k + (long)tile * KT * a.p_k.row, a.p_k.row, v + (long)tile * KT * a.p_v.row, a.p_v.row, a.width, last, span.z ? kg + tile * KT : nullptr, to);
         };
         bool any = false;
 #pragma unroll
@@ -1351,6 +1360,7 @@ void forward_go(const AttentionArgs &a, hipStream_t s)
 {
     if (a.shape == 0) hot_attention_forward_kernel<T, DP, 1, 1, 32><<<blocks_for(a.items), 64, 0, s>>>(a);
     else if (a.shape == 1) hot_attention_forward_kernel<T, DP, 1, 4, 64><<<blocks_for(a.items), 256, 0, s>>>(a);
+    else if constexpr (DP <= 96 && sizeof(T) == 2) hot_attention_forward_kernel<T, DP, 1, 8, 64><<<blocks_for(a.items), 512, 0, s>>>(a);
     else hot_attention_forward_kernel<T, DP, 2, 4, 64><<<blocks_for(a.items), 256, 0, s>>>(a);
 }
 
@@ -1404,8 +1414,7 @@ void attention_forward(const AttentionArgs &a, hipStream_t s)
 {
     HOT_BY_WIDTH(forward_go);
     if (a.splits > 1) {
-        const long blocks = (a.all_rows + 15) / 16;
-        hot_attention_join_kernel<T><<<(unsigned)(blocks < 4096 ? blocks : 4096), 256, 0, s>>>(a);
+        hot_attention_join_kernel<T><<<(unsigned)(a.all_rows < 8192 ? a.all_rows : 8192), 256, 0, s>>>(a);
     }
 }
 
