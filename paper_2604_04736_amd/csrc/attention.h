@@ -288,10 +288,7 @@ __device__ __forceinline__ void by_form(int form, bool masked, Go go)
     } else if (form == kStaged) {
         if (masked) go(Form<kStaged, true>{});
         else go(Form<kStaged, false>{});
-    }
-#ifndef NOFAR
-    else go(Form<kFar, true>{});
-#endif
+    } else go(Form<kFar, true>{});
 }
 
 // ---------------------------------------------------------------------------------
@@ -586,7 +583,7 @@ hot_attention_forward_kernel(AttentionArgs a)
             f4 left;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                x[j] = l[n] == 0.0f ? 0.0f : x[j] * by;
+                x[j] = as_it_is<T>(l[n] == 0.0f ? 0.0f : x[j] * by);
                 left[j] = x[j] - (float)(T)x[j];
             }
             four(to, d * 16 + g * 4, a.width, x);
@@ -637,7 +634,7 @@ hot_attention_join_kernel(AttentionArgs a)
                 l += totals[k];
                 x += sums[k][threadIdx.x];
             }
-            x = l == 0.0f ? 0.0f : x / l;
+            x = as_it_is<T>(l == 0.0f ? 0.0f : x / l);
             const long to = b * a.p_o.batch + h * a.p_o.head + i * a.p_o.row + (long)threadIdx.x;
             static_cast<T *>(a.o)[to] = (T)x;
             if (a.rest) static_cast<T *>(a.rest)[to] = (T)(x - (float)(T)x);

@@ -81,8 +81,7 @@ Cut forward_cut(const hot_attention_desc &d)
     c.tiles = (int)((rows + tile - 1) / tile);
     c.items = (long)d.batch * (d.heads / c.pack) * c.tiles;
     // workgroups for every place there is, but at least four tiles of keys to each
-    // (twice as many where groups may leave some of them nothing to do)
-    const long places = c.shape == 0 ? (d.groups ? 4096 : 2048) : 512, tiles_k = (d.keys + keys - 1) / keys;
+    const long places = c.shape == 0 ? 2048 : 512, tiles_k = (d.keys + keys - 1) / keys;
     long splits = c.items ? places / c.items : 1;
     if (splits > tiles_k / 4) splits = tiles_k / 4;
     if (splits > 128) splits = 128;

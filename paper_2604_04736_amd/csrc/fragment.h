@@ -61,6 +61,15 @@ public:
     }
 };
 
+// x, once.  The compiler joins a product with its rounding to fp16 (one rounding for two), at some of the product's uses and not at others: two pieces of a number
+// would then be of different numbers, a step of the first piece apart where that is nearly a tie.
+template <class T>
+__device__ __forceinline__ float as_it_is(float x)
+{
+    if constexpr (__is_same(T, _Float16)) asm("" : "+v"(x));
+    return x;
+}
+
 // Eight results as an operand: as they are for float32, in two pieces for 16-bit types (bf16: 2^-17 of each is left over; fp16: 2^-23, or half a step of 2^-24)
 template <class T>
 struct Pieces {
@@ -71,7 +80,8 @@ struct Pieces {
     {
         if constexpr (N == 1) p[0][i] = x;
         else {
-            p[0][i] = (T)x;
+#pragma clang fp contract(off)     // (of the product's rounding in every form of a kernel, or the forms' results differ in the last place)
+            p[0][i] = (T)(x = as_it_is<T>(x));
             p[1][i] = (T)(x - (float)p[0][i]);
         }
     }

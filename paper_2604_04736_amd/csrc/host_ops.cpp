@@ -2,6 +2,8 @@
 // the C call in one native function each, since a small layer's call is bound by the interpreter (a forecast of one row through
 // three layers with 16 samples 69 -> 41 us, of which the GPU works 23; a training pass on 64 rows 456 -> 330).  Every function answers None where an argument is not what it takes without
 // a copy or a conversion; the caller then goes through binding.py, whose checks name what is wrong.  No arithmetic here.
+#include <unordered_set>
+
 #include <torch/csrc/utils/pybind.h>
 
 #include <ATen/ATen.h>
@@ -197,6 +199,32 @@ variable_list once(variable_list grads, const char *name)
 }
 
 Tensor given(const MaybeTensor &t) { return t ? *t : Tensor(); }
+
+// In a backward pass that is being captured: the gradient of a leaf is handed over on the stream that was current when the leaf's first living graph was made.  Where that is
+// the default stream (an eager graph of the leaf lives), the capture becomes invalid and its end ends the process: an error here instead, before that.
+void captured_alone(const Tensor &like, const char *name)
+{
+    const auto stream = c10::hip::getCurrentHIPStream(like.device().index());
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(stream, &status) != hipSuccess || status == hipStreamCaptureStatusNone) return;
+    const c10::StreamId eager = c10::hip::getDefaultHIPStream(like.device().index()).id();
+    const auto self = torch::autograd::get_current_node();
+    std::vector<torch::autograd::Node *> left;
+    std::unordered_set<torch::autograd::Node *> seen;
+    if (self && stream.id() != eager) left.push_back(self.get());
+    while (!left.empty()) {
+        torch::autograd::Node *const node = left.back();
+        left.pop_back();
+        for (uint32_t i = 0; i < node->num_outputs(); ++i) {
+            torch::autograd::Node *const to = node->next_edge(i).function.get();
+            if (!to || !node->task_should_compute_output(i) || !seen.insert(to).second) continue;
+            const auto of = to->stream();
+            TORCH_CHECK(to->num_outputs() != 0 || !of || of->id() != eager, name,
+                        ": this backward pass is being captured while a graph of the same leaves, made on the default stream, lives; drop that graph first");
+            left.push_back(to);
+        }
+    }
+}
 
 // room for the gradient of the next input, where it is wanted
 Tensor gradient_of(AutogradContext *ctx, const Tensor &t, size_t &input)
@@ -451,6 +479,7 @@ struct Dropout : torch::autograd::Function<Dropout> {
     static variable_list backward(AutogradContext *ctx, variable_list grads)
     {
         const auto c = ctx->saved_data["counter"].toIntVector();
+        if (grads[0].defined()) captured_alone(grads[0], "dropout");
         return {grads[0].defined() ? apply(grads[0], ctx->saved_data["keep"].toDouble(), c[0], c[1], c[2], c[3], c[4]) : Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor()};
     }
 };
@@ -501,7 +530,7 @@ hot_block_desc block_desc(const Tensor &x, const Tensor (&v)[5], const BlockRule
 
 struct BlockEnd : torch::autograd::Function<BlockEnd> {
     static variable_list forward(AutogradContext *ctx, const Tensor &x, const Tensor &branch, const MaybeTensor &weight, const MaybeTensor &bias, const MaybeTensor &gate,
-                                 const MaybeTensor &branch_weight, const MaybeTensor &branch_bias, std::vector<int64_t> whole, double scale, double keep, double eps)
+                                 const MaybeTensor &branch_weight, const MaybeTensor &branch_bias, std::vector<int64_t> whole, double scale, double keep, double eps, bool graph)
     {
         const c10::DeviceGuard guard(x.device());
         const BlockRule rule = {whole, scale, keep, eps};
@@ -514,6 +543,7 @@ struct BlockEnd : torch::autograd::Function<BlockEnd> {
                 t = t.resolve_neg().contiguous();
             }
         hot_rng rng;
+        wanted = wanted && graph;
         const hot_block_desc d = block_desc(xs, v, rule, rng);
         const Tensor h = at::empty(x.sizes(), xs.options()), y = d.norm != HOT_NORM_NONE ? at::empty(x.sizes(), xs.options()) : Tensor();
         const Tensor stats = wanted ? at::empty({d.samples, d.rows, 4}, xs.options().dtype(at::kFloat)) : Tensor();
@@ -542,7 +572,8 @@ struct BlockEnd : torch::autograd::Function<BlockEnd> {
         const hot_block_desc d = block_desc(x, v, rule, rng);
         const Tensor dh = grads[0].defined() ? grads[0].resolve_neg().contiguous() : Tensor();
         const Tensor dy = grads.size() > 1 && grads[1].defined() ? grads[1].resolve_neg().contiguous() : Tensor();
-        if (!dh.defined() && !dy.defined()) return variable_list(11);
+        if (!dh.defined() && !dy.defined()) return variable_list(12);
+        captured_alone(x, "residual_norm");
         size_t input = 0;        // (inputs that are not there are not counted)
         const Tensor dx = gradient_of(ctx, x, input), dbranch = gradient_of(ctx, branch, input);
         Tensor dv[5];
@@ -556,7 +587,7 @@ struct BlockEnd : torch::autograd::Function<BlockEnd> {
         check(hot_block_backward(&d, &rng, raw(x), raw(branch), raw(v[0]), raw(v[2]), raw(v[3]), raw(v[4]), stats.const_data_ptr<float>(), raw(dh), raw(dy), raw_mut(dx),
                                  raw_mut(dbranch), raw_mut(dv[0]), raw_mut(dv[1]), raw_mut(dv[2]), raw_mut(dv[3]), raw_mut(dv[4]), raw_mut(ws), bytes, stream_of(x)),
               "hot_block_backward");
-        return once({dx, dbranch, dv[0], dv[1], dv[2], dv[3], dv[4], Tensor(), Tensor(), Tensor(), Tensor()}, "residual_norm");
+        return once({dx, dbranch, dv[0], dv[1], dv[2], dv[3], dv[4], Tensor(), Tensor(), Tensor(), Tensor(), Tensor()}, "residual_norm");
     }
 };
 
@@ -590,7 +621,7 @@ std::vector<Tensor> block_end(const Tensor &x, const Tensor &branch, const Maybe
     counter_rng(seed, step, first_sample, sets);
     py::gil_scoped_release others_run;
     return BlockEnd::apply(x, branch, weight, bias, gate, branch_weight, branch_bias, std::vector<int64_t>{norm, branch_norm, (int64_t)seed, step, first_sample, samples, offset},
-                           scale, keep, eps);
+                           scale, keep, eps, at::GradMode::is_enabled());
 }
 
 // [..., heads, tokens, width] as [batch, heads, tokens, width] with adjacent elements: a view, or a copy where the leading axes are no single one
@@ -652,7 +683,7 @@ Tensor attention_room(const hot_attention_desc &d, int which, const Tensor &like
 struct Attention : torch::autograd::Function<Attention> {
     static Tensor forward(AutogradContext *ctx, const Tensor &q_, const Tensor &k_, const Tensor &v_, const MaybeTensor &maybe_table, const MaybeTensor &query_code,
                           const MaybeTensor &key_code, const MaybeTensor &query_range, const MaybeTensor &key_range, const MaybeTensor &bucket, const MaybeTensor &query_groups, const MaybeTensor &key_groups,
-                          int64_t first_query, double scale, bool causal)
+                          int64_t first_query, double scale, bool causal, bool graph)
     {
         const c10::DeviceGuard guard(q_.device());
         const Tensor q = four_axes(q_), k = four_axes(k_), v = four_axes(v_);
@@ -660,7 +691,7 @@ struct Attention : torch::autograd::Function<Attention> {
         hot_attention_desc d = attention_desc(q, k, v, table, given(bucket), qg, first_query, scale, causal);
         const Tensor o = token_major(q);
         d.o = pitch_of(o);
-        const bool keep = q_.requires_grad() || k_.requires_grad() || v_.requires_grad() || (maybe_table && maybe_table->requires_grad());
+        const bool keep = graph && (q_.requires_grad() || k_.requires_grad() || v_.requires_grad() || (maybe_table && maybe_table->requires_grad()));
         const Tensor stats = keep ? at::empty({q.size(0), q.size(1), q.size(2), 2}, q.options().dtype(at::kFloat)) : Tensor();
         const Tensor rest = keep && d.dtype != HOT_F32 ? token_major(q) : Tensor();
         const Tensor ws = attention_room(d, 0, q);
@@ -679,8 +710,9 @@ struct Attention : torch::autograd::Function<Attention> {
 
     static variable_list backward(AutogradContext *ctx, variable_list grads)
     {
-        variable_list none(14);
+        variable_list none(15);
         if (!grads[0].defined()) return none;
+        captured_alone(grads[0], "attention");
         const variable_list s = ctx->get_saved_variables();
         const Tensor &q = s[0], &k = s[1], &v = s[2], &table = s[3], &o = s[11], &rest = s[12], &stats = s[13];
         const c10::DeviceGuard guard(q.device());
@@ -760,9 +792,10 @@ Tensor attention(const Tensor &q, const Tensor &k, const Tensor &v, const MaybeT
         kg = kg.expand({rows, kg.size(1)}).contiguous();
     }
     const auto there = [](const Tensor &t) { return t.defined() ? MaybeTensor(t) : MaybeTensor(); };
+    const bool graph = at::GradMode::is_enabled();
     py::gil_scoped_release others_run;
-    if (!table) return Attention::apply(q, k, v, MaybeTensor(), MaybeTensor(), MaybeTensor(), MaybeTensor(), MaybeTensor(), MaybeTensor(), there(qg), there(kg), 0, scale, causal);
-    return Attention::apply(q, k, v, table, query_code, key_code, query_range, key_range, bucket, there(qg), there(kg), first_query, scale, causal);
+    if (!table) return Attention::apply(q, k, v, MaybeTensor(), MaybeTensor(), MaybeTensor(), MaybeTensor(), MaybeTensor(), MaybeTensor(), there(qg), there(kg), 0, scale, causal, graph);
+    return Attention::apply(q, k, v, table, query_code, key_code, query_range, key_range, bucket, there(qg), there(kg), first_query, scale, causal, graph);
 }
 
 }  // namespace
