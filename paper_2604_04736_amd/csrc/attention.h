@@ -357,6 +357,13 @@ __device__ __forceinline__ int2 query_codes(const AttentionArgs &a, int first, i
 }
 
 // ---------------------------------------------------------------------------------
+// o, and the rows' statistics.  A wave holds QB blocks of sixteen queries as operands and their o in registers; KT keys and values at a time go by in LDS, the next tile of 16-bit
+// types on its way meanwhile.  Two products of 16 x 16 x DP for a block of sixteen keys, and a third one for p's second piece: with 16 heads x 8192 tokens x 128 bf16 in causal
+// order 0.70 ms, half of the matrix rate that a large product reaches for these three, the rest being what softmax issues beside them.
+// Two blocks of queries to a wave halve LDS's reading at width 128 (one block and eight waves: 0.75 ms); up to 96 elements eight waves of one block have the registers to be four to a
+// unit's quarter (two texts' rows of 3001 x 8 heads x 80 fp16, packed, 93 -> 78 us).
+// One wave and 32 keys where a tile has up to sixteen rows: bound by memory, 335 MB of eight caches of up to 16384 x 8 heads x 128 bf16 in 83 us, 4.0 TB/s (four waves with 64 keys, three of them without
+// rows: 124 us).
 template <class T, int DP, int QB, int WAVES, int KT>
 __global__ void __launch_bounds__(64 * WAVES, WAVES == 8 ? 4 : 2)
 hot_attention_forward_kernel(AttentionArgs a)
@@ -596,7 +603,8 @@ hot_attention_forward_kernel(AttentionArgs a)
     }
 }
 
-// The splits' results joined: a workgroup to a row, sixteen lanes to its elements and sixteen runs of splits, whose sums are added in their order
+// The splits' results joined: a workgroup to a row, sixteen lanes to its elements and sixteen runs of splits, whose sums are added in their order.  Few rows and up to 128 splits, so what
+// counts is how many loads are on their way (256 rows x 32 splits 5 us; sixteen lanes to a row 11).
 template <class T>
 __global__ void __launch_bounds__(256)
 hot_attention_join_kernel(AttentionArgs a)
@@ -649,8 +657,9 @@ hot_attention_join_kernel(AttentionArgs a)
 
 // ---------------------------------------------------------------------------------
 // D of every query, sixteen lanes to a row; for fp16 also the largest |do_i|^2 of every head and the largest |v_j|^2 of every key head (kPrepareRows rows to a workgroup, so
-// that few of them meet at one address)
-constexpr int kPrepareRows = 128;
+// that few of them meet at one address).  Bound by memory and its latency: 16 x 8192 rows of 128 bf16 17 us, 5.8 TB/s with what the caches still hold; four rows to a quarter of a wave,
+// two of them on their way (eight rows one after the other, places by divisions of 64 bits: 18 us, and where there are few rows 22 instead of 16).
+constexpr int kPrepareRows = 64;
 
 template <class T>
 __global__ void __launch_bounds__(256)
@@ -659,17 +668,20 @@ hot_attention_prepare_kernel(AttentionArgs a)
     constexpr bool BOUNDS = __is_same(T, _Float16);
     __shared__ float most[16];
     const int t = (int)threadIdx.x & 15, lane_row = (int)threadIdx.x >> 4;
-    const long keys = BOUNDS ? (long)a.batch * a.kv_heads * a.keys : 0, all = a.all_rows + keys;
-    for (long first = (long)blockIdx.x * kPrepareRows; first < all; first += (long)gridDim.x * kPrepareRows) {
+    const unsigned rows = (unsigned)a.all_rows, all = rows + (BOUNDS ? (unsigned)((long)a.batch * a.kv_heads * a.keys) : 0u);      // (each less than 2^31)
+    const unsigned step = gridDim.x * kPrepareRows;
+    for (unsigned first = blockIdx.x * kPrepareRows; first < all; first = all - first > step ? first + step : all) {
         // whose maximum row `r` goes to
-        auto owner = [&](long r) { return r < a.all_rows ? r / a.queries : (long)a.batch * a.heads + (r - a.all_rows) / a.keys; };
-        const long end = first + kPrepareRows < all ? first + kPrepareRows : all;
+        auto owner = [&](unsigned r) { return r < rows ? (long)(r / (unsigned)a.queries) : (long)a.batch * a.heads + (r - rows) / (unsigned)a.keys; };
+        const unsigned end = all - first > kPrepareRows ? first + kPrepareRows : all;
         const bool alone = BOUNDS && owner(first) == owner(end - 1);
         float largest = 0.0f;
-        for (long row = first + lane_row; row < end; row += 16) {
+#pragma unroll 2
+        for (unsigned row = first + lane_row; row < end; row += 16) {
             float sum = 0.0f, square = 0.0f;
-            if (row < a.all_rows) {
-                const int i = (int)(row % a.queries), h = (int)(row / a.queries % a.heads), b = (int)(row / a.queries / a.heads);
+            if (row < rows) {
+                const unsigned of = row / (unsigned)a.queries;
+                const int i = (int)(row - of * (unsigned)a.queries), h = (int)(of % (unsigned)a.heads), b = (int)(of / (unsigned)a.heads);
                 const bool there = !a.groups || a.query_groups[(long)(b % a.groups) * a.queries + i] >= 0;
                 const long o_at = b * a.p_o.batch + h * a.p_o.head + i * a.p_o.row;
                 const V8<T> up = eight(static_cast<const T *>(a.grad_o) + b * a.p_go.batch + h * a.p_go.head + i * a.p_go.row, t * 8, a.width, there);
@@ -682,8 +694,8 @@ hot_attention_prepare_kernel(AttentionArgs a)
                     square = __builtin_fmaf((float)up[j], (float)up[j], square);
                 }
             } else if constexpr (BOUNDS) {
-                const long at = row - a.all_rows;
-                const int j0 = (int)(at % a.keys), h = (int)(at / a.keys % a.kv_heads), b = (int)(at / a.keys / a.kv_heads);
+                const unsigned at = row - rows, of = at / (unsigned)a.keys;
+                const int j0 = (int)(at - of * (unsigned)a.keys), h = (int)(of % (unsigned)a.kv_heads), b = (int)(of / (unsigned)a.kv_heads);
                 const bool there = !a.groups || a.key_groups[(long)(b % a.groups) * a.keys + j0] >= 0;
                 const V8<T> v = eight(static_cast<const T *>(a.v) + b * a.p_v.batch + h * a.p_v.head + j0 * a.p_v.row, t * 8, a.width, there);
 #pragma unroll
@@ -694,7 +706,7 @@ hot_attention_prepare_kernel(AttentionArgs a)
                 sum += __shfl_xor(sum, off);
                 if constexpr (BOUNDS) square += __shfl_xor(square, off);
             }
-            if (t == 0 && row < a.all_rows) a.d[row] = sum;
+            if (t == 0 && row < rows) a.d[row] = sum;
             // (positive floats are ordered as their bits are, and the largest does not depend on the order; nan and infinity are left out)
             if constexpr (BOUNDS) {
                 if (!(square < 3.0e38f)) square = 0.0f;
@@ -735,7 +747,10 @@ __device__ __forceinline__ float unit_of(const AttentionArgs &a, int b, int h, i
 
 // ---------------------------------------------------------------------------------
 // dk and dv: a wave holds KB blocks of sixteen keys, and their k and v as operands; the queries of the heads that read them go by in LDS.  Where that gives too few
-// workgroups, the heads and runs of queries are split and the parts are added in their order (hot_attention_keys_join_kernel).
+// workgroups, the heads and runs of queries are split and the parts are added in their order (hot_attention_sum_kernel).
+// z and dp, then dv and dk with two pieces of p and dz: six products, of which 16 heads x 8192 tokens x 128 bf16 in causal order do 0.83 TFLOP in 1.25 ms, 54 % of what a large product
+// reaches.  Two waves to a unit's quarter and 32 queries in registers at a time; with KB = 2 (half of the reading of LDS) registers are spilled or one wave is left: 2.1 ms.
+// Eight waves to a tile: 1.31 ms, six and a third wave to a quarter 2.3.
 template <class T, int DP, int KB, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES, 2)
 hot_attention_keys_kernel(AttentionArgs a)
@@ -953,7 +968,7 @@ hot_attention_keys_kernel(AttentionArgs a)
     }
 }
 
-// Parts of gradients of rows of `count` tokens and `heads` heads an entry added up, sixteen lanes to a row
+// Parts of gradients of rows of `count` tokens and `heads` heads an entry added up in their order, sixteen lanes to a row (dk and dv of 8192 x 4 rows x 128 in four parts: 151 MB in 23 us)
 struct SumArgs {
     const float *parts;
     void *to;
@@ -998,6 +1013,9 @@ __device__ __forceinline__ void sum_along(const float (&v)[8], float &same_row, 
 // dq, and what the table's gradient is made of.  A workgroup holds the queries of one tile and head, of several entries of the batch one after the other.  Where a tile of
 // pairs is of one bucket its dz are added up in registers (in 64 bits from tile to tile); else each goes to its difference of codes in bins of the wave's own, and from
 // there to the wave's sums of the buckets.  No two waves add to one place, and LDS works a wave's additions in the order that they are issued in.
+// Four products (z, dp, dz's two pieces times k): 16 heads x 8192 tokens x 128 bf16 in causal order 0.80 ms, 56 % of the rate of a large product; a block of sixteen queries to a wave
+// where there are no more than 64 of them, else two (one at 8192 tokens: 1.10 ms).  Of the sums over one distance each, lines of a tile are summed along lanes first: LDS's own
+// additions of floats take some 270 cycles an instruction.
 template <class T, int DP, int QB, int WAVES, bool TABLE>
 __global__ void __launch_bounds__(64 * WAVES, 2)
 hot_attention_queries_kernel(AttentionArgs a)

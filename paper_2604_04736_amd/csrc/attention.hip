@@ -80,7 +80,7 @@ Cut forward_cut(const hot_attention_desc &d)
     const int tile = c.shape == 0 ? 16 : (c.shape == 1 ? 64 : 128), keys = c.shape == 0 ? 32 : 64;
     c.tiles = (int)((rows + tile - 1) / tile);
     c.items = (long)d.batch * (d.heads / c.pack) * c.tiles;
-    // workgroups for every place there is, but at least four tiles of keys to each
+    // workgroups for every place there is (a wave each: eight to a unit; 64 splits of 16384 keys instead of 32 gained nothing), but at least four tiles of keys to each
     const long places = c.shape == 0 ? 2048 : 512, tiles_k = (d.keys + keys - 1) / keys;
     long splits = c.items ? places / c.items : 1;
     if (splits > tiles_k / 4) splits = tiles_k / 4;

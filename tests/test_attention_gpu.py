@@ -115,6 +115,16 @@ def test_codes_of_any_order(kind, spread):
     _check(*_inputs(kind, 2, 2, 2, nq, nk, 32), _table(kind, 1, buckets, 2), p)
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("buckets", [1, 2, 63, 65, 1023, 4096])
+def test_few_and_many_buckets(kind, buckets):
+    """As many as are allowed: the waves' own sums of them lie in LDS beside the tiles, of the widest rows too."""
+    for nq, nk, width in ((60, 60, 24), (140, 200, 128)):
+        codes = nq + nk - 1
+        p = _ops().RelativePositions(torch.arange(nq), torch.arange(nk), (torch.arange(codes) * 67) % buckets, buckets, DEV)
+        _check(*_inputs(kind, 2, 2, 1, nq, nk, width), _table(kind, 2, buckets, 2), p)
+
+
 def _packed(batch, n, seed, holes=True):
     g = torch.Generator(device=DEV).manual_seed(seed)
     ends = torch.rand(batch, 4, device=DEV, generator=g).sort(1).values * n
