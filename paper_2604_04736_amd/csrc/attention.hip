@@ -63,11 +63,15 @@ bool attention_ok(const hot_attention_desc *d)
     return true;
 }
 
-// How the forward call cuts its work: shape 0 a wave with sixteen rows and 32 keys at a time, 1 and 2 four waves with sixteen or 32 rows each and 64 keys
+// How the forward call cuts its work: shape 0 a wave with sixteen rows and 32 keys at a time, 1 and 2 tiles of 64 and 128 rows and 64 keys
 struct Cut {
     int pack, shape, splits, tiles;
     long items;
 };
+
+// Whether tiles of 128 rows leave some of the two places of 256 compute units empty.  Tiles of 64 are then better, though each of them reads all keys (two texts' rows of 3001 tokens x 8
+// heads x 80 packed, 384 tiles: forward 74 -> 67 us, dq 124 -> 104; 768 entries and heads of 65 tokens, 768 tiles, the other way: dq 39 -> 47).
+bool few(long sets, long rows) { return sets * ((rows + 127) / 128) < 512; }
 
 Cut forward_cut(const hot_attention_desc &d)
 {
@@ -76,7 +80,7 @@ Cut forward_cut(const hot_attention_desc &d)
     // heads of one key head side by side in a tile where one head's queries do not fill it: its keys are then read once for all
     c.pack = d.queries * per <= 64 ? per : 1;
     const long rows = d.queries * c.pack;
-    c.shape = rows <= 16 ? 0 : (rows <= 64 ? 1 : 2);
+    c.shape = rows <= 16 ? 0 : (rows <= 64 || few((long)d.batch * (d.heads / c.pack), rows) ? 1 : 2);
     const int tile = c.shape == 0 ? 16 : (c.shape == 1 ? 64 : 128), keys = c.shape == 0 ? 32 : 64;
     c.tiles = (int)((rows + tile - 1) / tile);
     c.items = (long)d.batch * (d.heads / c.pack) * c.tiles;
@@ -98,7 +102,7 @@ struct BackwardCut {
 BackwardCut queries_cut(const hot_attention_desc &d)
 {
     BackwardCut c = {};
-    c.shape = d.queries <= 64 ? 1 : 2;
+    c.shape = d.queries <= 64 || few((long)d.batch * d.heads, d.queries) ? 1 : 2;
     const int tile = c.shape == 1 ? 64 : 128;
     c.tiles = (int)((d.queries + tile - 1) / tile);
     const long entries = d.tables ? d.batch / d.tables : d.batch, sets = d.tables ? d.tables : 1;

@@ -95,6 +95,23 @@ def test_a_table_for_every_weight_sample(kind, table_kind):
 
 
 @pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("width", [16, 33, 64, 80, 96, 128])
+@pytest.mark.parametrize("heads,kv,nq,nk", [(2, 2, 70, 70), (4, 2, 65, 200), (2, 1, 129, 129), (2, 2, 200, 150)])
+def test_many_entries(kind, width, heads, kv, nq, nk):
+    """Enough tiles for the larger ones (128 queries), whole and in part, with and without a table, order and groups."""
+    batch = 264
+    p = _ops().RelativePositions.distances(nq, nk, 16, 60, DEV, first_query=nk - nq if nk > nq else 0)
+    inputs = _inputs(kind, batch, heads, kv, nq, nk, width)
+    _check(*inputs, _table(kind, 2, 16, heads), p, causal=True)
+    g = torch.Generator(device=DEV).manual_seed(nq)
+    qg, kg = (torch.randint(-1, 3, (12, n), device=DEV, generator=g, dtype=torch.int32).sort(1).values for n in (nq, nk))
+    _check(*inputs, query_groups=qg, key_groups=kg)
+    window = _ops().RelativePositions.windows(10, 7, device=DEV) if nq == nk == 70 else None
+    if window is not None:
+        _check(*inputs, _table(kind, 1, window.buckets, heads), window)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
 def test_no_bias_and_other_scales(kind):
     for scale in (None, 0.0, -0.3, 1.0):
         _check(*_inputs(kind, 2, 2, 1, 66, 70, 24), **({"scale": scale} if scale is not None else {}))
