@@ -31,6 +31,14 @@ constexpr float kShift = __is_same(T, _Float16) ? 14.0f : 0.0f;
 
 __device__ __forceinline__ float two_to(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// ... times 2^kShift (for the other types no addition of zero, which the compiler would keep)
+template <class T>
+__device__ __forceinline__ float shifted(float x)
+{
+    if constexpr (__is_same(T, _Float16)) x += kShift<T>;
+    return two_to(x);
+}
+
 // Which item a workgroup takes.  Splits of one tile lie side by side, then the heads (of all entries), then the tiles, those with the most work first where causal order
 // makes them unequal: the last ones to finish are short, and since workgroups go to the eight dies in turn, a head's tiles stay on one die where heads are a multiple of eight.
 __device__ __forceinline__ long item_of(long items)
@@ -534,10 +542,11 @@ hot_attention_forward_kernel(AttentionArgs a)
                 }
                 m[n] = now;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float e = two_to(z[n][i] - base + kShift<T>);
+                for (int i = 0; i < 8; i += 2) {
+                    const float e = shifted<T>(z[n][i] - base), f = shifted<T>(z[n][i + 1] - base);
                     l[n] += e;
-                    p[n].set(i, e);
+                    l[n] += f;
+                    p[n].set(i, e, f);
                 }
             }
 #pragma unroll
@@ -898,6 +907,7 @@ hot_attention_keys_kernel(AttentionArgs a)
 #pragma unroll
                         for (int n = 0; n < KB; ++n) {
                             const f4 zs = s[u][n].read(settled), dps = dp[u][n].read(settled);
+                            float es[4], ws[4];
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
                                 float add = one;
@@ -908,12 +918,17 @@ hot_attention_keys_kernel(AttentionArgs a)
                                     const unsigned at_code = (unsigned)(qc[i] - code[n]), last = (unsigned)a.codes - 1u;
                                     add = bias[at_code < last ? at_code : last];
                                 }
-                                float e = two_to(__builtin_fmaf(zs[i], a.scale, add) - m[i] - l[i] + kShift<T>);
+                                float e = shifted<T>(__builtin_fmaf(zs[i], a.scale, add) - m[i] - l[i]);
                                 float w = e * ((dps[i] - d[i]) * (unit * (__is_same(T, _Float16) ? 0x1p-14f : 1.0f)));
                                 if constexpr (how.kMasked)
                                     if ((group[n] != qgr[i]) | (key[n] - i0 > row0 + i + reach)) e = w = 0.0f;
-                                p[n].set(u * 4 + i, e);
-                                dz[n].set(u * 4 + i, w);
+                                es[i] = e;
+                                ws[i] = w;
+                            }
+#pragma unroll
+                            for (int i = 0; i < 4; i += 2) {
+                                p[n].set(u * 4 + i, es[i], es[i + 1]);
+                                dz[n].set(u * 4 + i, ws[i], ws[i + 1]);
                             }
                         }
                     }
@@ -1194,6 +1209,7 @@ hot_attention_queries_kernel(AttentionArgs a)
 #pragma unroll
                         for (int n = 0; n < QB; ++n) {
                             const f4 zs = s[u][n].read(settled), dps = dp[u][n].read(settled);
+                            float before = 0.0f;
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
                                 float bias_here = one;
@@ -1212,7 +1228,8 @@ hot_attention_queries_kernel(AttentionArgs a)
                                 const float e = two_to(__builtin_fmaf(zs[i], a.scale, bias_here) - m[n] - l[n]);
                                 float w = e * (dps[i] - dd[n]);
                                 if constexpr (how.kMasked) w = sees ? w : 0.0f;
-                                dz[n].set(u * 4 + i, w * unit);
+                                if (i & 1) dz[n].set(u * 4 + i - 1, before, w * unit);
+                                before = w * unit;
                                 if constexpr (TABLE) {
                                     if constexpr (how.kForm == kOne) here += w;
                                     else if constexpr (how.kForm == kStaged) {

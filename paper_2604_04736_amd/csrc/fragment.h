@@ -76,13 +76,28 @@ struct Pieces {
     static constexpr int N = __is_same(T, float) ? 1 : 2;
     V8<T> p[N];
 
-    __device__ __forceinline__ void set(int i, float x)
+    // results i and i + 1, i even: one conversion for both (one at a time, each was converted once more for its second piece)
+    __device__ __forceinline__ void set(int i, float x, float y)
     {
-        if constexpr (N == 1) p[0][i] = x;
-        else {
+        if constexpr (N == 1) {
+            p[0][i] = x;
+            p[0][i + 1] = y;
+        } else {
 #pragma clang fp contract(off)     // (of the product's rounding in every form of a kernel, or the forms' results differ in the last place)
-            p[0][i] = (T)(x = as_it_is<T>(x));
-            p[1][i] = (T)(x - (float)p[0][i]);
+            typedef T T2 __attribute__((ext_vector_type(2)));
+            typedef float F2 __attribute__((ext_vector_type(2)));
+            typedef unsigned U4 __attribute__((ext_vector_type(4)));
+            const F2 v = {as_it_is<T>(x), as_it_is<T>(y)};
+            const unsigned high = __builtin_bit_cast(unsigned, __builtin_convertvector(v, T2));
+            F2 back;
+            if constexpr (__is_same(T, _Float16)) back = __builtin_convertvector(__builtin_bit_cast(T2, high), F2);
+            else back = F2{__builtin_bit_cast(float, high << 16), __builtin_bit_cast(float, high & 0xffff0000u)};
+            const unsigned low = __builtin_bit_cast(unsigned, __builtin_convertvector((F2){v.x - back.x, v.y - back.y}, T2));
+            U4 first = __builtin_bit_cast(U4, p[0]), second = __builtin_bit_cast(U4, p[1]);
+            first[i / 2] = high;
+            second[i / 2] = low;
+            p[0] = __builtin_bit_cast(V8<T>, first);
+            p[1] = __builtin_bit_cast(V8<T>, second);
         }
     }
     // c += a (the pieces)

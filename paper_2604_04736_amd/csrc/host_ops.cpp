@@ -206,7 +206,11 @@ void captured_alone(const Tensor &like, const char *name)
 {
     const auto stream = c10::hip::getCurrentHIPStream(like.device().index());
     hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
-    if (hipStreamIsCapturing(stream, &status) != hipSuccess || status == hipStreamCaptureStatusNone) return;
+    if (hipStreamIsCapturing(stream, &status) != hipSuccess) {
+        (void)hipGetLastError();             // (the default stream's answer while another one is captured; not to be found by a later call)
+        return;
+    }
+    if (status == hipStreamCaptureStatusNone) return;
     const c10::StreamId eager = c10::hip::getDefaultHIPStream(like.device().index()).id();
     const auto self = torch::autograd::get_current_node();
     std::vector<torch::autograd::Node *> left;
