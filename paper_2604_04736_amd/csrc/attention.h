@@ -367,9 +367,10 @@ __device__ __forceinline__ int2 query_codes(const AttentionArgs &a, int first, i
 // ---------------------------------------------------------------------------------
 // o, and the rows' statistics.  A wave holds QB blocks of sixteen queries as operands and their o in registers; KT keys and values at a time go by in LDS, the next tile of 16-bit
 // types on its way meanwhile.  Two products of 16 x 16 x DP for a block of sixteen keys, and a third one for p's second piece: with 16 heads x 8192 tokens x 128 bf16 in causal
-// order 0.70 ms, half of the matrix rate that a large product reaches for these three, the rest being what softmax issues beside them.
-// Two blocks of queries to a wave halve LDS's reading at width 128 (one block and eight waves: 0.75 ms); up to 96 elements eight waves of one block have the registers to be four to a
-// unit's quarter (two texts' rows of 3001 x 8 heads x 80 fp16, packed, 93 -> 78 us).
+// order 0.64 ms, half of the matrix rate that a large product reaches for these three, the rest being what softmax issues beside them (0.70 with every p converted by itself, and once
+// more for its second piece).
+// Two blocks of queries to a wave halve LDS's reading at width 128 (one block and eight waves: 0.75 ms where this was 0.70); up to 96 elements eight waves of one block have the registers to be four to a
+// unit's quarter (two texts' rows of 3001 x 8 heads x 80 fp16, packed, 93 -> 78 us; such few tiles are 64 rows now).
 // One wave and 32 keys where a tile has up to sixteen rows: bound by memory, 335 MB of eight caches of up to 16384 x 8 heads x 128 bf16 in 83 us, 4.0 TB/s (four waves with 64 keys, three of them without
 // rows: 124 us).
 template <class T, int DP, int QB, int WAVES, int KT>
@@ -757,9 +758,9 @@ __device__ __forceinline__ float unit_of(const AttentionArgs &a, int b, int h, i
 // ---------------------------------------------------------------------------------
 // dk and dv: a wave holds KB blocks of sixteen keys, and their k and v as operands; the queries of the heads that read them go by in LDS.  Where that gives too few
 // workgroups, the heads and runs of queries are split and the parts are added in their order (hot_attention_sum_kernel).
-// z and dp, then dv and dk with two pieces of p and dz: six products, of which 16 heads x 8192 tokens x 128 bf16 in causal order do 0.83 TFLOP in 1.25 ms, 54 % of what a large product
-// reaches.  Two waves to a unit's quarter and 32 queries in registers at a time; with KB = 2 (half of the reading of LDS) registers are spilled or one wave is left: 2.1 ms.
-// Eight waves to a tile: 1.31 ms, six and a third wave to a quarter 2.3.
+// z and dp, then dv and dk with two pieces of p and dz: six products, of which 16 heads x 8192 tokens x 128 bf16 in causal order do 0.83 TFLOP in 1.17 ms, 58 % of what a large product
+// reaches (m and log2 l apart and pieces one at a time: 1.25).  Two waves to a unit's quarter and 32 queries in registers at a time; with KB = 2 (half of the reading of LDS) registers are spilled or one wave is left: 2.1 ms where this was 1.25;
+// eight waves to a tile 1.31, six and a third wave to a quarter 2.3.
 template <class T, int DP, int KB, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES, 2)
 hot_attention_keys_kernel(AttentionArgs a)
@@ -1027,8 +1028,8 @@ __device__ __forceinline__ void sum_along(const float (&v)[8], float &same_row, 
 // dq, and what the table's gradient is made of.  A workgroup holds the queries of one tile and head, of several entries of the batch one after the other.  Where a tile of
 // pairs is of one bucket its dz are added up in registers (in 64 bits from tile to tile); else each goes to its difference of codes in bins of the wave's own, and from
 // there to the wave's sums of the buckets.  No two waves add to one place, and LDS works a wave's additions in the order that they are issued in.
-// Four products (z, dp, dz's two pieces times k): 16 heads x 8192 tokens x 128 bf16 in causal order 0.80 ms, 56 % of the rate of a large product; a block of sixteen queries to a wave
-// where there are no more than 64 of them, else two (one at 8192 tokens: 1.10 ms).  Of the sums over one distance each, lines of a tile are summed along lanes first: LDS's own
+// Four products (z, dp, dz's two pieces times k): 16 heads x 8192 tokens x 128 bf16 in causal order 0.75 ms, 60 % of the rate of a large product; a block of sixteen queries to a wave
+// where there are no more than 64 of them, else two (one at 8192 tokens: 1.10 ms where this was 0.80).  Of the sums over one distance each, lines of a tile are summed along lanes first: LDS's own
 // additions of floats take some 270 cycles an instruction.
 template <class T, int DP, int QB, int WAVES, bool TABLE>
 __global__ void __launch_bounds__(64 * WAVES, 2)
