@@ -4,7 +4,7 @@ import math
 
 import torch
 
-from head_norm_util import DEV, HALF_UNIT, TYPES, U32, rounded, within  # noqa: F401
+from head_norm_util import DEV, HALF_UNIT, TINY, TYPES, U32, rounded, within  # noqa: F401
 
 M0, M1, W0, W1 = 0xD2511F53, 0xCD9E8D57, 0x9E3779B9, 0xBB67AE85
 

@@ -297,6 +297,36 @@ def test_long_caches_are_split_and_joined():
         _check(*_inputs(kind, 1, heads, kv, rows, nk, 128), _table(kind, 1, 32, heads), p)
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+def test_long_texts_with_gradients(kind):
+    """Far fields of one bucket, tiles along the diagonal and many tiles of 128 queries; packed texts too."""
+    n, heads, kv = 2100, 32, 8
+    p = _ops().RelativePositions.distances(n, n, 32, 128, DEV, both_sides=False)
+    inputs = _inputs(kind, 1, heads, kv, n, n, 128)
+    _check(*inputs, _table(kind, 1, 32, heads), p, causal=True)
+    group = (torch.arange(n, device=DEV) // 700).int()
+    _check(*inputs, _table(kind, 1, 32, heads), p, causal=True, query_groups=group[None], key_groups=group[None])
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+def test_one_tensor_for_all_and_calls_at_once(kind):
+    """q, k and v one tensor of three axes: its gradient is the sum of the three; and calls on several streams at the same time."""
+    q, _, _, do = _inputs(kind, 1, 3, 3, 150, 150, 48)
+    apart = _pass(q, q, q, do)
+    leaf = q[0].clone().requires_grad_()
+    grad, = torch.autograd.grad(_ops().attention(leaf, leaf, leaf), leaf, do[0])
+    sizes = sum(apart[m].double().abs() for m in ("dq", "dk", "dv"))[0]
+    assert ((grad.double() - (apart["dq"].double() + apart["dk"].double() + apart["dv"].double())[0]).abs() <= 2.02 * U.HALF_UNIT[grad.dtype] * sizes + U.TINY[grad.dtype]).all()      # (two additions)
+    streams, results = [torch.cuda.Stream() for _ in range(3)], []
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for stream in streams:
+            with torch.cuda.stream(stream):
+                results.append(_pass(q, q, q, do))
+    torch.cuda.synchronize()
+    assert all(torch.equal(r[m], apart[m]) for r in results for m in apart)
+
+
 def test_offsets_beyond_32_bits():
     """A cache of more than 2^32 bytes and 2^31 elements, of which only the last tokens are no padding."""
     nk, width = (1 << 24) + 77, 128
