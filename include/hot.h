@@ -694,15 +694,15 @@ int hot_block_backward(const hot_block_desc *desc, const hot_rng *rng, const voi
  * Attention with a learned relative position bias by buckets.  Query i of head h in entry b of the batch sees key j with
  *   z = scale q[i] . k[j] + table[bucket[query_code[first_query + i] - key_code[j]][0], h],   o[i] = sum_j softmax_j(z) v[j]
  * over the keys that it may see: j <= i + keys - queries where causal, and query_groups[i] = key_groups[j] >= 0 where there are groups.  A query that sees
- * nothing has o = 0 and gradients 0; what rows of negative groups hold reaches nothing.  Query head h reads key and value head h / (heads / kv_heads).
+ * nothing has o = 0 and gradients 0; what rows of negative groups hold reaches nothing (rows that order or another group hides have to be finite).
+ * Query head h reads key and value head h / (heads / kv_heads).
  * q, o and their gradients: [batch, heads, queries, width], k and v [batch, kv_heads, keys, width], each with pitches of its own in elements
  * (batch, head, row; elements of a row adjacent).  table: dense [tables, buckets, heads] of table_dtype (dtype or HOT_F32), entry b taking table
  * b / (batch / tables); tables = 0: no bias, and no codes.  query_code, key_code: int32, such that differences lie in 0 .. codes - 1; bucket: int32
  * [codes, 2], the bucket of every difference and the last difference up to which all are of that bucket; query_range, key_range: int32 [tokens / 64 rounded up, 4], of 64 tokens each
  * of all that query_code and key_code hold the smallest and the largest code, and 1 if codes go up by one from each token to the next (that of the next 64 included), else 0, and 0.
- * bucket is 8-byte, the ranges are 16-byte aligned.  (Indices outside are taken as the last; other things that do not
- * fit together give other results.)  Groups: int32
- * [groups, queries] and [groups, keys], entry b taking row b mod groups; groups = 0: none.
+ * bucket is 8-byte, the ranges are 16-byte aligned.  (Indices outside are taken as the last; other things that do not fit together give other results.)
+ * Groups: int32 [groups, queries] and [groups, keys], entry b taking row b mod groups; groups = 0: none.
  * Limits: width 8 to HOT_ATTENTION_MOST_WIDTH, HOT_ATTENTION_MOST_BUCKETS, HOT_ATTENTION_MOST_CODES; batch x heads x max(queries, keys) below 2^31.
  */
 #define HOT_ATTENTION_LEAST_WIDTH 8

@@ -501,7 +501,9 @@ def attention(q, k, v, table=None, positions: RelativePositions | None = None, *
     growing text.
     Causal: query i sees keys up to i + keys - queries.  query_groups, key_groups: int32 [queries] and [keys], or [entries, ...], row b mod entries for entry b of q's
     flattened leading axes; a query sees the keys of its own group (texts packed into a row, pieces of a shifted window), negative groups are padding
-    and whatever lies there reaches nothing.  key_groups alone: all queries are of group 0.  A query that sees nothing gives zeros and has no gradients."""
+    and whatever lies there reaches nothing (keys and values that order or another group hides have to be finite: their weight is a zero that is multiplied).
+    key_groups alone: all queries are of group 0.  A query that sees nothing gives zeros and has no gradients.
+    A backward pass that is captured into a graph while an eager graph of the same leaves lives raises RuntimeError (dropout's and residual_norm's too)."""
     if table is not None and not isinstance(positions, RelativePositions):
         raise TypeError("positions: a table needs RelativePositions")
     if not isinstance(q, torch.Tensor):
