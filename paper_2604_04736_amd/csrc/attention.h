@@ -55,6 +55,12 @@ __device__ __forceinline__ int fresh_lane(int x)
     return x;
 }
 
+// Whether 32 keys' part of o is added up by itself before it goes to o.  float32's instruction takes four keys, so that o was one chain of 1024 additions over 4096 keys; what they leave off is in D, alike
+// for all keys of a row, and the sums of the table's gradient do not average it out (16 heads x 4096 tokens whose values have a common part: 3 times as far from 64 bits).  Now 128 additions of sums of eight;
+// 16 heads x 4096 x 128 in causal order 0.95 -> 1.00 ms forward.  The instruction of 16-bit types takes 32 keys anyway.
+template <class T>
+constexpr bool kFresh = sizeof(T) == 4;
+
 // Tiles in LDS: two of 16-bit elements, one on its way while the other is worked on; one of float32, whose products take longer than its way
 template <class T>
 constexpr int kStages = sizeof(T) == 2 ? 2 : 1;
@@ -542,19 +548,39 @@ hot_attention_forward_kernel(AttentionArgs a)
                     for (int d = 0; d < DB; ++d) o[d][n].scale(settled, by);
                 }
                 m[n] = now;
+                float sum = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 8; i += 2) {
                     const float e = shifted<T>(z[n][i] - base), f = shifted<T>(z[n][i + 1] - base);
-                    l[n] += e;
-                    l[n] += f;
+                    sum += e;
+                    sum += f;
                     p[n].set(i, e, f);
                 }
+                l[n] += sum;
             }
+            if constexpr (kFresh<T>) {
 #pragma unroll
-            for (int d = 0; d < DB; ++d) {
-                const V8<T> f = R::across(here_tile + R::kBytes, c, d * 16, here);
+                for (int d = 0; d < DB; d += 2) {
+                    Block16<T> part[2][QB];
 #pragma unroll
-                for (int n = 0; n < QB; ++n) p[n].mac(o[d][n], f);
+                    for (int x = 0; x < 2; ++x) {
+                        const V8<T> f = R::across(here_tile + R::kBytes, c, (d + x) * 16, here);
+#pragma unroll
+                        for (int n = 0; n < QB; ++n) p[n].mac(part[x][n], f);
+                    }
+                    const Settled summed;
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int n = 0; n < QB; ++n) o[d + x][n].add(summed, part[x][n]);
+                }
+            } else {
+#pragma unroll
+                for (int d = 0; d < DB; ++d) {
+                    const V8<T> f = R::across(here_tile + R::kBytes, c, d * 16, here);
+#pragma unroll
+                    for (int n = 0; n < QB; ++n) p[n].mac(o[d][n], f);
+                }
             }
         }
     };

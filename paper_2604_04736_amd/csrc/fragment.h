@@ -54,6 +54,11 @@ public:
         else v_ = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, v_, 0, 0, 0);
     }
     __device__ __forceinline__ f4 read(const Settled &) const { return v_; }
+    __device__ __forceinline__ void add(const Settled &, const Block16 &b)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v_[i] += b.v_[i];
+    }
     __device__ __forceinline__ void scale(const Settled &, float by)
     {
 #pragma unroll
