@@ -10,6 +10,8 @@
 // dz are operands of the next product where they are.  Those operands have 16 bits: two pieces of each, since one rounding of p or dz does not average
 // out where few keys count or where keys have a common mean (dz adds up to zero over a row, its roundings do not).
 // D is formed from o and what o's rounding left over, for the same reason.
+// The backward kernels round as the forward one did: z first, then z - m, then - log2 l.  (m + log2 l as one number is shorter by one addition, but where |m| is large, by a bias or a product that a row's keys
+// share, log2 l is lost in it, and z keeps what the forward pass rounded off: p then added up to anything but one.)
 // fp16's pieces end at 2^-24: p is held times 2^14, dz in units of a bound on it, 2 max |do_i| max |v_j| of the head.
 #ifndef HOT_ATTENTION_H
 #define HOT_ATTENTION_H
@@ -785,7 +787,7 @@ __device__ __forceinline__ float unit_of(const AttentionArgs &a, int b, int h, i
 // dk and dv: a wave holds KB blocks of sixteen keys, and their k and v as operands; the queries of the heads that read them go by in LDS.  Where that gives too few
 // workgroups, the heads and runs of queries are split and the parts are added in their order (hot_attention_sum_kernel).
 // z and dp, then dv and dk with two pieces of p and dz: six products, of which 16 heads x 8192 tokens x 128 bf16 in causal order do 0.83 TFLOP in 1.17 ms, 58 % of what a large product
-// reaches (m and log2 l apart and pieces one at a time: 1.25).  Two waves to a unit's quarter and 32 queries in registers at a time; with KB = 2 (half of the reading of LDS) registers are spilled or one wave is left: 2.1 ms where this was 1.25;
+// reaches (pieces one at a time: 1.25).  Two waves to a unit's quarter and 32 queries in registers at a time; with KB = 2 (half of the reading of LDS) registers are spilled or one wave is left: 2.1 ms where this was 1.25;
 // eight waves to a tile 1.31, six and a third wave to a quarter 2.3.
 template <class T, int DP, int KB, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES, 2)
@@ -797,7 +799,7 @@ hot_attention_keys_kernel(AttentionArgs a)
     constexpr int STAGES = kStages<T>;
     typedef Bias<THREADS, THREADS < 256 ? 256 : (sizeof(T) == 2 && DP > 64 ? 384 : 640)> Staging;
     __shared__ __attribute__((aligned(1024))) char tiles[STAGES * 2 * R::kBytes];
-    __shared__ __attribute__((aligned(16))) float all_ms[STAGES * QT], all_ds[STAGES * QT];
+    __shared__ __attribute__((aligned(16))) float all_ms[STAGES * QT], all_ls[STAGES * QT], all_ds[STAGES * QT];
     __shared__ __attribute__((aligned(16))) int all_codes[STAGES * QT], all_groups[STAGES * QT];
     __shared__ float all_staged[STAGES * Staging::kRoom];
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, g = lane >> 4, col = lane & 15;
@@ -886,9 +888,10 @@ hot_attention_keys_kernel(AttentionArgs a)
         // One tile: the products of what is `here`, while the next one comes to `there`
         auto step = [&](lds_char *__restrict here, lds_char *__restrict there, int buffer) {
             int *const codes = all_codes + buffer * QT, *const groups = all_groups + buffer * QT;
-            float *const ms = all_ms + buffer * QT, *const ds = all_ds + buffer * QT, *const staged = all_staged + buffer * Staging::kRoom;
+            float *const ms = all_ms + buffer * QT, *const ls = all_ls + buffer * QT, *const ds = all_ds + buffer * QT, *const staged = all_staged + buffer * Staging::kRoom;
             if ((int)threadIdx.x < QT) {
-                ms[threadIdx.x] = next_m + next_l;
+                ms[threadIdx.x] = next_m;
+                ls[threadIdx.x] = next_l - kShift<T>;
                 ds[threadIdx.x] = next_d;
                 codes[threadIdx.x] = next_code;
                 groups[threadIdx.x] = next_group;
@@ -926,7 +929,7 @@ hot_attention_keys_kernel(AttentionArgs a)
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
                         const int row0 = R::row_of(c, u, g);
-                        const f4 ml = *reinterpret_cast<const f4 *>(ms + row0), d = *reinterpret_cast<const f4 *>(ds + row0);
+                        const f4 m = *reinterpret_cast<const f4 *>(ms + row0), l = *reinterpret_cast<const f4 *>(ls + row0), d = *reinterpret_cast<const f4 *>(ds + row0);
                         i4 qc = i4(0), qgr = i4(0);
                         if constexpr (how.kForm != kOne) qc = *reinterpret_cast<const i4 *>(codes + row0);
                         if constexpr (how.kMasked) qgr = *reinterpret_cast<const i4 *>(groups + row0);
@@ -944,7 +947,7 @@ hot_attention_keys_kernel(AttentionArgs a)
                                     const unsigned at_code = (unsigned)(qc[i] - code[n]), last = (unsigned)a.codes - 1u;
                                     add = bias[at_code < last ? at_code : last];
                                 }
-                                float e = shifted<T>(__builtin_fmaf(zs[i], a.scale, add - ml[i]));
+                                float e = two_to(__builtin_fmaf(zs[i], a.scale, add) - m[i] - l[i]);
                                 float w = e * ((dps[i] - d[i]) * (unit * (__is_same(T, _Float16) ? 0x1p-14f : 1.0f)));
                                 if constexpr (how.kMasked)
                                     if ((group[n] != qgr[i]) | (key[n] - i0 > row0 + i + reach)) e = w = 0.0f;
@@ -1123,17 +1126,18 @@ hot_attention_queries_kernel(AttentionArgs a)
         const float unit = unit_of<T>(a, b, h, 1);
         Query at[QB];
         V8<T> qf[QB][KS], uf[QB][KS];
-        float ml[QB], dd[QB];
+        float m[QB], l[QB], dd[QB];
         int code_low = kMostCode, code_high = -1;             // of this wave's queries
 #pragma unroll
         for (int n = 0; n < QB; ++n) {
             at[n] = query_of(a, b, h, tile_q * TILE + (wave * QB + n) * 16 + col);
             const long row = ((long)b * a.heads + h) * a.queries + at[n].i;
-            ml[n] = a.stats[2 * row] + a.stats[2 * row + 1];
+            m[n] = a.stats[2 * row];
+            l[n] = a.stats[2 * row + 1];
             dd[n] = a.d[row];
             if (!at[n].there) {
-                dd[n] = 0.0f;
-                ml[n] = __builtin_inff();
+                m[n] = dd[n] = 0.0f;
+                l[n] = __builtin_inff();
                 at[n].code = kMostCode;          // (beyond what is staged)
             } else {
                 code_low = at[n].code < code_low ? at[n].code : code_low;
@@ -1250,7 +1254,7 @@ hot_attention_queries_kernel(AttentionArgs a)
                                     at_code = at_code < last ? at_code : last;
                                     bias_here = bias[at_code];
                                 }
-                                const float e = two_to(__builtin_fmaf(zs[i], a.scale, bias_here - ml[n]));
+                                const float e = two_to(__builtin_fmaf(zs[i], a.scale, bias_here) - m[n] - l[n]);
                                 float w = e * (dps[i] - dd[n]);
                                 if constexpr (how.kMasked) w = sees ? w : 0.0f;
                                 if (i & 1) dz[n].set(u * 4 + i - 1, before, w * unit);

@@ -50,3 +50,127 @@ def test_float32_tables_of_long_texts(causal):
         off += float((got[:, h].double() - want).square().sum())
         size += float(want.square().sum())
     assert math.sqrt(off) <= 1.5 * math.sqrt(variance), (math.sqrt(off), math.sqrt(variance), math.sqrt(size))
+
+
+# ------------------------------------------------------------------ scores that lie far from zero together
+
+SIZES = [(2, 80), (2, 300), (130, 129)]          # the last: enough tiles for the larger ones
+
+
+def _inputs(kind, batch, n, width=32, heads=4, kv=2):
+    g = torch.Generator(device=DEV).manual_seed(7 * n + width)
+    return [torch.randn(batch, h, n, width, device=DEV, generator=g).to(U.TYPES[kind]) for h in (heads, kv, kv, heads)]
+
+
+def _whole(kind, batch, n, width=16, heads=4, kv=2):
+    """Queries and keys of small whole numbers: with SCALE scores are eighths in units of ln 2, and no sum of them or with a number of few bits is rounded."""
+    g = torch.Generator(device=DEV).manual_seed(5 * n)
+    q, k = (torch.randint(-2, 3, (batch, h, n, width), device=DEV, generator=g).to(U.TYPES[kind]) for h in (heads, kv))
+    return [q, k] + [torch.randn(batch, h, n, width, device=DEV, generator=g).to(U.TYPES[kind]) for h in (kv, heads)]
+
+
+SCALE = math.log(2) / 8
+
+
+def _positions(form, n):
+    ops = _ops()
+    if form == "line":
+        return ops.RelativePositions.distances(n, n, 8, 30, DEV)
+    if form == "one":                            # a bucket for all
+        return ops.RelativePositions(torch.arange(n), torch.arange(n), torch.zeros(2 * n - 1, dtype=torch.long), 8, DEV)
+    g = torch.Generator().manual_seed(n)         # thousands of differences in a tile
+    query, key = torch.randint(0, 60000, (n,), generator=g), torch.randint(0, 60000, (n,), generator=g)
+    codes = int(query.max() - key.min() - (query.min() - key.max())) + 1
+    return ops.RelativePositions(query, key, torch.randint(0, 8, (codes,), generator=g), 8, DEV)
+
+
+def _pass(q, k, v, do, table=None, positions=None, **more):
+    leaves = {"q": q, "k": k, "v": v, **({"table": table} if table is not None else {})}
+    leaves = {n: t.detach().requires_grad_() for n, t in leaves.items()}
+    o = _ops().attention(leaves["q"], leaves["k"], leaves["v"], leaves.get("table"), positions, **more)
+    return {"o": o.detach(), **{"d" + n: t for n, t in zip(leaves, torch.autograd.grad(o, list(leaves.values()), do))}}
+
+
+def _within(got, want):
+    for name, t in got.items():
+        t = t[None] if name == "dtable" else t
+        U.within(t, *want[name], f"{name} {tuple(t.shape)} {t.dtype}")
+
+
+def _alike(q, k, v, do, table, which, **more):
+    """All scores that a row sees alike: the plain form with q = 0, and dk, which q itself goes into, with k = 0."""
+    none = torch.zeros_like(table)[None]
+    want = U.attention_plain(q * 0, k, v, do, none, which, **more)
+    want["dk"] = U.attention_plain(q, k * 0, v, do, none, which, **more)["dk"]
+    return want
+
+
+@pytest.mark.parametrize("kind,table_kind,value", [("f32", "f32", -1e9), ("f32", "f32", None), ("bf16", "bf16", -1e9), ("bf16", "bf16", None), ("bf16", "f32", -1e9), ("bf16", "f32", None),
+                                                   ("f16", "f32", -1e9), ("f16", "f32", None)])
+@pytest.mark.parametrize("batch,n", SIZES)
+@pytest.mark.parametrize("form", ["line", "one", "any"])
+def test_rows_that_see_masked_keys_alone(kind, table_kind, value, batch, n, form):
+    """A bias of -1e9, or of the type's lowest value, for every key that a row sees: float32 scores are then alike whatever q and k are, and so are the weights, forward and backward."""
+    q, k, v, do = _inputs(kind, batch, n)
+    p = _positions(form, n)
+    value = torch.finfo(U.TYPES[table_kind]).min if value is None else value
+    table = torch.full((8, 4), value, device=DEV, dtype=U.TYPES[table_kind])
+    # half a step at 1.44e9 is 64 in units of ln 2
+    assert float((q.float() @ k.repeat_interleave(2, 1).float().transpose(-1, -2)).abs().max()) / math.sqrt(32) * 1.4427 < 60
+    which = U.buckets_of(p, n, n)
+    group = (torch.arange(n, device=DEV) // 37).int()
+    group[5:9] = -1
+    for more in ({}, {"causal": True}, {"causal": True, "query_groups": group[None], "key_groups": group[None]}):
+        _within(_pass(q, k, v, do, table, p, **more), _alike(q, k, v, do, table, which, **more))
+
+
+@pytest.mark.parametrize("kind,table_kind", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32"), ("f16", "f32")])
+@pytest.mark.parametrize("batch,n", SIZES)
+def test_rows_that_see_masked_keys_alone_beside_others(kind, table_kind, batch, n):
+    """Causal order and distances 0 to 4 masked by the lowest value: rows 0 to 4 see masked keys alone, all others have some that are not."""
+    q, k, v, do = _inputs(kind, batch, n)
+    do[:, :, :5] *= 0.5                          # (fp16's pieces are in units of the largest row, which is then one of the others)
+    p = _ops().RelativePositions(torch.arange(n), torch.arange(n), (torch.arange(2 * n - 1) - (n - 1) > 4).long(), 2, DEV)
+    which = U.buckets_of(p, n, n)
+    g = torch.Generator(device=DEV).manual_seed(n)
+    table = torch.randn(2, 4, device=DEV, generator=g).to(U.TYPES[table_kind])
+    table[0] = torch.finfo(table.dtype).min
+    got = _pass(q, k, v, do, table, p, causal=True)
+    masked = table.clone()
+    masked[0] = -math.inf
+    first, others = do.clone(), do.clone()
+    first[:, :, 5:], others[:, :, :5] = 0, 0
+    one = _alike(q, k, v, first, table, which, causal=True)
+    two = U.attention_plain(q, k, v, others, masked[None], which, causal=True)
+    want = {m: tuple(a + b for a, b in zip(one[m], two[m])) for m in ("dk", "dv", "dtable")}
+    for m in ("o", "dq"):
+        want[m] = tuple(torch.cat([a[:, :, :5], b[:, :, 5:]], 2) for a, b in zip(one[m], two[m]))
+    _within(got, want)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("batch,n", SIZES)
+@pytest.mark.parametrize("form", ["line", "one", "any"])
+def test_a_bias_that_all_keys_share(kind, batch, n, form):
+    """Scores of eighths and one bias for all: no score is rounded, so results are as near to 64 bits as without the bias, whatever its size."""
+    q, k, v, do = _whole(kind, batch, n)
+    p = _positions(form, n)
+    which = U.buckets_of(p, n, n)
+    want = U.attention_plain(q, k, v, do, torch.zeros(1, 8, 4, device=DEV), which, scale=SCALE)
+    for value in (3000.0, -1e4, -65504.0, 1e5):
+        _within(_pass(q, k, v, do, torch.full((8, 4), value, device=DEV), p, scale=SCALE), want)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("batch,n", SIZES)
+@pytest.mark.parametrize("sign", [1, -1])
+def test_products_that_all_keys_share(kind, batch, n, sign):
+    """No bias, and one element of queries and keys that adds 8192 to every score (in units of ln 2): weights, and the gradients of everything else, are as without it."""
+    q, k, v, do = _whole(kind, batch, n)
+    q[..., 0], k[..., 0] = 256, 256 * sign
+    plain_q, plain_k = q.clone(), k.clone()
+    plain_q[..., 0], plain_k[..., 0] = 0, 0
+    for causal in (False, True):
+        want = U.attention_plain(plain_q, k, v, do, scale=SCALE, causal=causal)
+        want["dk"] = U.attention_plain(q, plain_k, v, do, scale=SCALE, causal=causal)["dk"]
+        _within(_pass(q, k, v, do, scale=SCALE, causal=causal), want)
