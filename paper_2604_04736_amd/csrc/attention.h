@@ -965,10 +965,25 @@ hot_attention_keys_kernel(AttentionArgs a)
 #pragma unroll
                 for (int x = 0; x < DB; ++x) {
                     const V8<T> fu = R::across(here + R::kBytes, c, x * 16, at), fq = R::across(here, c, x * 16, at);
+                    if constexpr (kFresh<T>) {
+                        Block16<T> part_v[KB], part_k[KB];
 #pragma unroll
-                    for (int n = 0; n < KB; ++n) {
-                        p[n].mac(dv[x][n], fu);
-                        dz[n].mac(dk[x][n], fq);
+                        for (int n = 0; n < KB; ++n) {
+                            p[n].mac(part_v[n], fu);
+                            dz[n].mac(part_k[n], fq);
+                        }
+                        const Settled summed;
+#pragma unroll
+                        for (int n = 0; n < KB; ++n) {
+                            dv[x][n].add(summed, part_v[n]);
+                            dk[x][n].add(summed, part_k[n]);
+                        }
+                    } else {
+#pragma unroll
+                        for (int n = 0; n < KB; ++n) {
+                            p[n].mac(dv[x][n], fu);
+                            dz[n].mac(dk[x][n], fq);
+                        }
                     }
                 }
             }

@@ -52,6 +52,34 @@ def test_float32_tables_of_long_texts(causal):
     assert math.sqrt(off) <= 1.5 * math.sqrt(variance), (math.sqrt(off), math.sqrt(variance), math.sqrt(size))
 
 
+def test_float32_keys_and_values_of_long_texts():
+    """The gradients of keys and values that two heads of 4096 queries read, where what is added up has one sign: do and q have common parts, so that p do and (dp - D) q of a key do.
+
+    As above: T = 2 x 4096 / 32 sums of 32 queries, growing in proportion, give a variance of (2^-24 dk)^2 T / 9; scaling and rounding at most a third each, and as much again for what p and dz are off,
+    which is another number in every query and averages out.  Thousands of elements leave their norm no room; a fifth is allowed.  One chain, four queries at a time, has 2048 / 9 in the place of 256 / 9:
+    2.7 times this."""
+    n, batch, heads, kv, width = 4096, 2, 16, 8, 32
+    g = torch.Generator(device=DEV).manual_seed(12)
+    q, do = (3 + 0.1 * torch.randn(batch, heads, n, width, device=DEV, generator=g) for _ in range(2))
+    k, v = (torch.randn(batch, kv, n, width, device=DEV, generator=g).requires_grad_() for _ in range(2))
+    got = torch.autograd.grad(_ops().attention(q, k, v), (k, v), do)
+    off, size = [0.0, 0.0], [0.0, 0.0]
+    for b in range(batch):
+        for h in range(kv):
+            kd, vd, want = k.detach()[b, h].double(), v.detach()[b, h].double(), [0.0, 0.0]
+            for i in (2 * h, 2 * h + 1):
+                qd, dod = q[b, i].double(), do[b, i].double()
+                w = torch.softmax(qd @ kd.T / math.sqrt(width), -1)
+                dp = dod @ vd.T
+                want[0] = want[0] + (w * (dp - (w * dp).sum(-1, keepdim=True))).T @ qd / math.sqrt(width)
+                want[1] = want[1] + w.T @ dod
+            for m in range(2):
+                off[m] += float((got[m][b, h].double() - want[m]).square().sum())
+                size[m] += float(want[m].square().sum())
+    for m in range(2):
+        assert math.sqrt(off[m] / size[m]) <= 1.2 * U.U32 * math.sqrt(2 * n / 32 / 9 + 4 / 3), (m, math.sqrt(off[m] / size[m]) / U.U32)
+
+
 # ------------------------------------------------------------------ scores that lie far from zero together
 
 SIZES = [(2, 80), (2, 300), (130, 129)]          # the last: enough tiles for the larger ones
