@@ -702,7 +702,7 @@ int hot_block_backward(const hot_block_desc *desc, const hot_rng *rng, const voi
  * [codes, 2], the bucket of every difference and the last difference up to which all are of that bucket; query_range, key_range: int32 [tokens / 64 rounded up, 4], of 64 tokens each
  * of all that query_code and key_code hold the smallest and the largest code, and 1 if codes go up by one from each token to the next (that of the next 64 included), else 0, and 0.
  * bucket is 8-byte, the ranges are 16-byte aligned.  (Indices outside are taken as the last; other things that do not fit together give other results.)
- * Groups: int32 [groups, queries] and [groups, keys], entry b taking row b mod groups; groups = 0: none.
+ * Groups: int32 [groups, queries] and [groups, keys] (NULL where there are no tokens), entry b taking row b mod groups; groups = 0: none.
  * Limits: width 8 to HOT_ATTENTION_MOST_WIDTH, HOT_ATTENTION_MOST_BUCKETS, HOT_ATTENTION_MOST_CODES; batch x heads x max(queries, keys) below 2^31.
  */
 #define HOT_ATTENTION_LEAST_WIDTH 8

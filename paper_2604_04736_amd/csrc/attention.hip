@@ -232,7 +232,8 @@ bool give(AttentionArgs &a, const hot_attention_desc &d, const Room &r, char *ws
     if (d.tables && (!table || !query_code || !key_code || !query_range || !key_range || !bucket || !on_element(table, d.table_dtype) || !aligned4(query_code) ||
                      !aligned4(key_code) || !aligned16(query_range) || !aligned16(key_range) || !aligned8(bucket)))
         return false;
-    if (d.groups && (!query_groups || !key_groups || !aligned4(query_groups) || !aligned4(key_groups))) return false;
+    // (groups of no tokens need no array: that of an empty tensor is null)
+    if (d.groups && ((d.queries && !query_groups) || (d.keys && !key_groups) || !aligned4(query_groups) || !aligned4(key_groups))) return false;
     a.q = q;
     a.k = k;
     a.v = v;
