@@ -703,12 +703,14 @@ int hot_block_backward(const hot_block_desc *desc, const hot_rng *rng, const voi
  * of all that query_code and key_code hold the smallest and the largest code, and 1 if codes go up by one from each token to the next (that of the next 64 included), else 0, and 0.
  * bucket is 8-byte, the ranges are 16-byte aligned.  (Indices outside are taken as the last; other things that do not fit together give other results.)
  * Groups: int32 [groups, queries] and [groups, keys] (NULL where there are no tokens), entry b taking row b mod groups; groups = 0: none.
- * Limits: width 8 to HOT_ATTENTION_MOST_WIDTH, HOT_ATTENTION_MOST_BUCKETS, HOT_ATTENTION_MOST_CODES; batch x heads x max(queries, keys) below 2^31.
+ * Limits: width 8 to HOT_ATTENTION_MOST_WIDTH, HOT_ATTENTION_MOST_BUCKETS, HOT_ATTENTION_MOST_CODES; at most HOT_ATTENTION_MOST_TOKENS queries and keys, batch x heads x max(queries, keys)
+ * below 2^31 - 1, first_query + queries below 2^31.
  */
 #define HOT_ATTENTION_LEAST_WIDTH 8
 #define HOT_ATTENTION_MOST_WIDTH 128
 #define HOT_ATTENTION_MOST_BUCKETS 4096
 #define HOT_ATTENTION_MOST_CODES 4194304
+#define HOT_ATTENTION_MOST_TOKENS 2147483520 /* 2^31 - 128: the end of the last tile is below 2^31 too */
 
 typedef struct hot_pitch {
     int64_t batch, head, row;

@@ -362,7 +362,7 @@ __device__ __forceinline__ Query query_of(const AttentionArgs &a, int b, int uni
     q.group = a.groups ? a.query_groups[(long)(b % a.groups) * a.queries + q.i] : 0;
     if (q.group < 0) q.there = false;
     if (!q.there) q.group = -3;            // (that of no key)
-    q.last = !q.there ? -1 : (a.causal ? q.i + a.keys - a.queries : a.keys - 1);
+    q.last = !q.there ? -1 : (a.causal ? q.i + (a.keys - a.queries) : a.keys - 1);
     return q;
 }
 
@@ -423,7 +423,7 @@ hot_attention_forward_kernel(AttentionArgs a)
     bool line = false;
     const int2 mine = query_codes(a, first_i, last_i, line);
     // keys that any row of this workgroup may see by order, and up to which all of them may
-    int visible = a.causal ? last_i + a.keys - a.queries + 1 : a.keys, few = a.causal ? first_i + a.keys - a.queries + 1 : a.keys;
+    int visible = a.causal ? last_i + (a.keys - a.queries) + 1 : a.keys, few = a.causal ? first_i + (a.keys - a.queries) + 1 : a.keys;
     visible = visible < 0 ? 0 : (visible > a.keys ? a.keys : visible);
     if (few > a.keys) few = a.keys;
     const int all_tiles = (visible + KT - 1) / KT, share = (all_tiles + a.splits - 1) / a.splits;
@@ -1110,7 +1110,7 @@ hot_attention_queries_kernel(AttentionArgs a)
     const int end_b = first_b + a.chunk < (table + 1) * a.entries ? first_b + a.chunk : (table + 1) * a.entries;
     const float *const bias = a.bias + ((long)table * a.heads + h) * a.codes;
     const int end_row = (tile_q + 1) * TILE < a.queries ? (tile_q + 1) * TILE : a.queries, first_i = tile_q * TILE, last_i = end_row - 1;
-    int visible = a.causal ? last_i + a.keys - a.queries + 1 : a.keys, few = a.causal ? first_i + a.keys - a.queries + 1 : a.keys;
+    int visible = a.causal ? last_i + (a.keys - a.queries) + 1 : a.keys, few = a.causal ? first_i + (a.keys - a.queries) + 1 : a.keys;
     visible = visible < 0 ? 0 : (visible > a.keys ? a.keys : visible);
     if (few > a.keys) few = a.keys;
     const int all_tiles = (visible + KT - 1) / KT, share = (all_tiles + a.splits - 1) / a.splits;

@@ -50,12 +50,12 @@ bool attention_ok(const hot_attention_desc *d)
         return false;
     // (65535: the last dimension of a grid)
     if (d->tables < 0 || d->tables > 65535 || d->heads > 65535) return false;
-    if (d->queries >= kMostRows || d->keys >= kMostRows) return false;
+    if (d->queries > HOT_ATTENTION_MOST_TOKENS || d->keys > HOT_ATTENTION_MOST_TOKENS) return false;
     const double entries = (double)d->batch * (double)d->heads;
     if (entries * (double)d->queries >= (double)kMostRows || entries * (double)d->keys >= (double)kMostRows || entries >= (double)kMostRows) return false;
     if (d->tables) {
         if (d->batch % d->tables || d->buckets < 1 || d->buckets > HOT_ATTENTION_MOST_BUCKETS || d->codes < 1 || d->codes > HOT_ATTENTION_MOST_CODES ||
-            d->first_query < 0 || (d->table_dtype != d->dtype && d->table_dtype != HOT_F32) || (double)d->tables * d->heads * (double)d->codes >= 1.0e12)
+            d->first_query < 0 || d->first_query + d->queries > kMostRows || (d->table_dtype != d->dtype && d->table_dtype != HOT_F32) || (double)d->tables * d->heads * (double)d->codes >= 1.0e12)
             return false;
     }
     for (const hot_pitch *p : {&d->q, &d->k, &d->v, &d->o, &d->grad_o, &d->grad_q, &d->grad_k, &d->grad_v})

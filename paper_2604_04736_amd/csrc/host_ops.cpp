@@ -772,6 +772,7 @@ Tensor attention(const Tensor &q, const Tensor &k, const Tensor &v, const MaybeT
     for (const int64_t m : q.sizes().slice(0, n - 3)) batch *= m;
     HOT_NEED((double)batch * (double)q.size(-3) * (double)std::max<int64_t>(1, std::max(q.size(-2), k.size(-2))) < 2147483647.0 && q.size(-3) <= 65535,
              "q: need fewer than 2^31 rows and 65536 heads, got ", q.sizes());
+    HOT_NEED(std::max(q.size(-2), k.size(-2)) <= HOT_ATTENTION_MOST_TOKENS, "q and k: need at most ", HOT_ATTENTION_MOST_TOKENS, " tokens, got ", q.sizes(), " and ", k.sizes());
     if (table) {
         elements(*table, "table", q);
         TORCH_CHECK_TYPE(table->scalar_type() == q.scalar_type() || table->scalar_type() == at::kFloat, "table: need q's type or float32");

@@ -44,3 +44,21 @@ def test_groups_of_no_tokens(hot):
     assert forward(_desc(hot, groups=2), None, ONE) == hot.HOT_EINVAL
     assert forward(_desc(hot, groups=2), ONE, None) == hot.HOT_EINVAL
     assert forward(_desc(hot, groups=2, queries=0), None, ONE + 2) == hot.HOT_EINVAL
+
+
+def test_the_most_tokens(hot):
+    """2^31 - 128 of either, so that where the last tile ends is a 32-bit number too; one more is refused."""
+    lib, most = hot.lib(), (1 << 31) - 128
+    one = dict(batch=1, heads=1, kv=1, width=8)
+    for which in (0, 1):
+        for sizes in (dict(queries=most, keys=4), dict(queries=4, keys=most), dict(queries=most, keys=most)):
+            assert lib.hot_attention_workspace_bytes(ctypes.byref(_desc(hot, **one, **sizes)), which) > 0, sizes
+            more = {n: size + (size == most) for n, size in sizes.items()}
+            assert lib.hot_attention_workspace_bytes(ctypes.byref(_desc(hot, **one, **more)), which) == hot.HOT_EINVAL, more
+        # rows of all heads of all entries
+        assert lib.hot_attention_workspace_bytes(ctypes.byref(_desc(hot, 2, 1, 1, 4, 1 << 30, 8)), which) == hot.HOT_EINVAL
+        # the line that queries lie on
+        table = dict(tables=1, buckets=4, codes=21)
+        last = (1 << 31) - 1 - 10
+        assert lib.hot_attention_workspace_bytes(ctypes.byref(_desc(hot, first_query=last, **table)), which) > 0
+        assert lib.hot_attention_workspace_bytes(ctypes.byref(_desc(hot, first_query=last + 1, **table)), which) == hot.HOT_EINVAL
