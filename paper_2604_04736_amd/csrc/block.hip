@@ -91,9 +91,10 @@ __device__ __forceinline__ void drop(f8 &v, const bool (&kept)[8], float up)
 // ---------------------------------------------------------------------------------
 // Dropout alone.  `tpr` threads to a row (of one sample, blockIdx.y), each with an octet of every `tpr`; workgroups along z share long rows.
 // Rows of whole octets are one long row.  Bound by memory: 32768 x 4096 bf16 in 98 us, 5.5 TB/s, as fast as they are copied.  (10007 x 1531 fp16, whose rows begin on any element: 15 us.)
+// (x and y may be one array: every thread reads its octet before it writes it, and no other thread's.)
 template <class T>
 __global__ void __launch_bounds__(kBlockThreads)
-hot_dropout_kernel(const T *__restrict__ x, T *__restrict__ y, long rows, long width, long octets, int tpr, Drop d)
+hot_dropout_kernel(const T *x, T *y, long rows, long width, long octets, int tpr, Drop d)
 {
     const int s = (int)blockIdx.y;
     x += (size_t)s * (size_t)rows * (size_t)width;
