@@ -366,7 +366,6 @@ int hot_attention_backward(const hot_attention_desc *desc, const void *q, const 
     }
     if ((grad_k || grad_v) && desc->keys && desc->batch) {
         const BackwardCut c = keys_cut(*desc);
-        a.tiles_k = c.tiles;
         a.splits = c.splits;
         a.by_head = c.by_head;
         a.items = c.items;

@@ -12,7 +12,7 @@ struct AttentionArgs {
     int queries, keys, batch, heads, kv_heads, per, width;         // per: query heads to a key head
     int tables, entries, buckets, codes, groups, causal, table_type; // entries: of the batch, to a table
     int pack;                          // heads side by side in a tile's rows (forward)
-    int shape, splits, tiles_q, tiles_k;
+    int shape, splits, tiles_q;
     int chunk;                         // entries that a workgroup takes one after the other (dq)
     int by_head;                       // splits are of the heads that read a key head (times runs of their queries), not of queries alone (dk and dv)
     int first_query;
