@@ -205,17 +205,17 @@ Tensor given(const MaybeTensor &t) { return t ? *t : Tensor(); }
 void captured_alone(const Tensor &like, const char *name)
 {
     const auto stream = c10::hip::getCurrentHIPStream(like.device().index());
-    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
-    if (hipStreamIsCapturing(stream, &status) != hipSuccess) {
-        (void)hipGetLastError();             // (the default stream's answer while another one is captured; not to be found by a later call)
-        return;
-    }
-    if (status == hipStreamCaptureStatusNone) return;
     const c10::StreamId eager = c10::hip::getDefaultHIPStream(like.device().index()).id();
+    // (the default stream is never captured, and to ask it while another one is would be an error, left for a later call to find)
+    if (stream.id() == eager) return;
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    const hipError_t asked = hipStreamIsCapturing(stream, &status);
+    TORCH_CHECK(asked == hipSuccess, name, ": ", hipGetErrorString(asked));
+    if (status == hipStreamCaptureStatusNone) return;
     const auto self = torch::autograd::get_current_node();
     std::vector<torch::autograd::Node *> left;
     std::unordered_set<torch::autograd::Node *> seen;
-    if (self && stream.id() != eager) left.push_back(self.get());
+    if (self) left.push_back(self.get());
     while (!left.empty()) {
         torch::autograd::Node *const node = left.back();
         left.pop_back();
