@@ -375,11 +375,11 @@ __device__ __forceinline__ int2 query_codes(const AttentionArgs &a, int first, i
 // ---------------------------------------------------------------------------------
 // o, and the rows' statistics.  A wave holds QB blocks of sixteen queries as operands and their o in registers; KT keys and values at a time go by in LDS, the next tile of 16-bit
 // types on its way meanwhile.  Two products of 16 x 16 x DP for a block of sixteen keys, and a third one for p's second piece: with 16 heads x 8192 tokens x 128 bf16 in causal
-// order 0.64 ms, half of the matrix rate that a large product reaches for these three, the rest being what softmax issues beside them (0.70 with every p converted by itself, and once
+// order 0.63 ms, half of the matrix rate that a large product reaches for these three, the rest being what softmax issues beside them (0.70 with every p converted by itself, and once
 // more for its second piece).
 // Two blocks of queries to a wave halve LDS's reading at width 128 (one block and eight waves: 0.75 ms where this was 0.70); up to 96 elements eight waves of one block have the registers to be four to a
 // unit's quarter (two texts' rows of 3001 x 8 heads x 80 fp16, packed, 93 -> 78 us; such few tiles are 64 rows now).
-// One wave and 32 keys where a tile has up to sixteen rows: bound by memory, 335 MB of eight caches of up to 16384 x 8 heads x 128 bf16 in 83 us, 4.0 TB/s (four waves with 64 keys, three of them without
+// One wave and 32 keys where a tile has up to sixteen rows: bound by memory, 335 MB of eight caches of up to 16384 x 8 heads x 128 bf16 in 80 to 83 us, 4.1 TB/s (four waves with 64 keys, three of them without
 // rows: 124 us).
 template <class T, int DP, int QB, int WAVES, int KT>
 __global__ void __launch_bounds__(64 * WAVES, WAVES == 8 ? 4 : 2)
@@ -695,7 +695,7 @@ hot_attention_join_kernel(AttentionArgs a)
 
 // ---------------------------------------------------------------------------------
 // D of every query, sixteen lanes to a row; for fp16 also the largest |do_i|^2 of every head and the largest |v_j|^2 of every key head (kPrepareRows rows to a workgroup, so
-// that few of them meet at one address).  Bound by memory and its latency: 16 x 8192 rows of 128 bf16 17 us, 5.8 TB/s with what the caches still hold; four rows to a quarter of a wave,
+// that few of them meet at one address).  Bound by memory and its latency: 16 x 8192 rows of 128 bf16 18 us, 5.6 TB/s with what the caches still hold; four rows to a quarter of a wave,
 // two of them on their way (eight rows one after the other, places by divisions of 64 bits: 18 us, and where there are few rows 22 instead of 16).
 constexpr int kPrepareRows = 64;
 
@@ -1072,7 +1072,7 @@ __device__ __forceinline__ void sum_along(const float (&v)[8], float &same_row, 
 // dq, and what the table's gradient is made of.  A workgroup holds the queries of one tile and head, of several entries of the batch one after the other.  Where a tile of
 // pairs is of one bucket its dz are added up in registers (in 64 bits from tile to tile); else each goes to its difference of codes in bins of the wave's own, and from
 // there to the wave's sums of the buckets.  No two waves add to one place, and LDS works a wave's additions in the order that they are issued in.
-// Four products (z, dp, dz's two pieces times k): 16 heads x 8192 tokens x 128 bf16 in causal order 0.75 ms, 60 % of the rate of a large product; a block of sixteen queries to a wave
+// Four products (z, dp, dz's two pieces times k): 16 heads x 8192 tokens x 128 bf16 in causal order 0.76 ms, 59 % of the rate of a large product; a block of sixteen queries to a wave
 // where there are no more than 64 of them, else two (one at 8192 tokens: 1.10 ms where this was 0.80).  Of the sums over one distance each, lines of a tile are summed along lanes first: LDS's own
 // additions of floats take some 270 cycles an instruction.
 template <class T, int DP, int QB, int WAVES, bool TABLE>
