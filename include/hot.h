@@ -734,7 +734,7 @@ int64_t hot_attention_workspace_bytes(const hot_attention_desc *desc, int which)
 
 /*
  * Tensors whose rows are no whole 4-byte words on that grid (odd widths or pitches, loose) are copied into the workspace first.
- * stats: fp32 [batch, heads, queries, 2], and rest (o's pitches and type; 16-bit types only): what o's rounding left over.  Both are for the backward call; NULL leaves
+ * stats: fp32 [batch, heads, queries, 2], and rest (o's pitches and type; 16-bit types only): what o's rounding left over (fp16: times 2048).  Both are for the backward call; NULL leaves
  * them out.
  */
 int hot_attention_forward(const hot_attention_desc *desc, const void *q, const void *k, const void *v, const void *table, const int32_t *query_code,

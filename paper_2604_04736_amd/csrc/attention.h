@@ -30,6 +30,9 @@ constexpr int kMostCode = 1 << 28;               // beyond every code, and far e
 constexpr float kNone = -__builtin_inff();
 template <class T>
 constexpr float kShift = __is_same(T, _Float16) ? 14.0f : 0.0f;
+// what o's rounding leaves over is held in units of 1 / kFiner: of fp16 it is at most 16, and at 2^-24 its steps would end where o is some 2^-13
+template <class T>
+constexpr float kFiner = __is_same(T, _Float16) ? 2048.0f : 1.0f;
 
 __device__ __forceinline__ float two_to(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -629,7 +632,7 @@ hot_attention_forward_kernel(AttentionArgs a)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 x[j] = as_it_is<T>(l[n] == 0.0f ? 0.0f : x[j] * by);
-                left[j] = x[j] - (float)(T)x[j];
+                left[j] = (x[j] - (float)(T)x[j]) * kFiner<T>;
             }
             four(to, d * 16 + g * 4, a.width, x);
             if (rest) four(rest, d * 16 + g * 4, a.width, left);
@@ -683,7 +686,7 @@ hot_attention_join_kernel(AttentionArgs a)
             x = as_it_is<T>(l == 0.0f ? 0.0f : x / l);
             const long to = b * a.p_o.batch + h * a.p_o.head + i * a.p_o.row + (long)threadIdx.x;
             static_cast<T *>(a.o)[to] = (T)x;
-            if (a.rest) static_cast<T *>(a.rest)[to] = (T)(x - (float)(T)x);
+            if (a.rest) static_cast<T *>(a.rest)[to] = (T)((x - (float)(T)x) * kFiner<T>);
             if (threadIdx.x == 0 && a.stats) {
                 a.stats[2 * row] = l == 0.0f ? 0.0f : m;
                 a.stats[2 * row + 1] = l == 0.0f ? __builtin_inff() : __builtin_log2f(l) - kShift<T>;
@@ -728,7 +731,7 @@ hot_attention_prepare_kernel(AttentionArgs a)
                 if (a.rest) rest = eight(static_cast<const T *>(a.rest) + o_at, t * 8, a.width, there);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    sum = __builtin_fmaf((float)up[j], (float)o[j] + (float)rest[j], sum);
+                    sum = __builtin_fmaf((float)up[j], __builtin_fmaf((float)rest[j], 1.0f / kFiner<T>, (float)o[j]), sum);
                     square = __builtin_fmaf((float)up[j], (float)up[j], square);
                 }
             } else if constexpr (BOUNDS) {

@@ -202,3 +202,22 @@ def test_products_that_all_keys_share(kind, batch, n, sign):
         want = U.attention_plain(plain_q, k, v, do, scale=SCALE, causal=causal)
         want["dk"] = U.attention_plain(q, plain_k, v, do, scale=SCALE, causal=causal)["dk"]
         _within(_pass(q, k, v, do, scale=SCALE, causal=causal), want)
+
+
+@pytest.mark.parametrize("batch,n", SIZES)
+@pytest.mark.parametrize("power", [11, 14])
+def test_small_values_in_fp16(batch, n, power):
+    """Values 2^power times smaller, few bits each so that all are there in fp16, under gradients 2^8 times as large: every gradient is 2^(8 - power) times that of the values as they were, and as near to it,
+    though o and what its rounding leaves over end in steps of 2^-24.  A float32 table, whose gradient D's error goes into."""
+    q, k, v, do = _inputs("f16", batch, n)
+    v = (v * 8).round() / 8
+    p = _positions("line", n)
+    g = torch.Generator(device=DEV).manual_seed(n)
+    table = torch.randn(8, 4, device=DEV, generator=g)
+    want = U.attention_plain(q, k, v, do, table[None], U.buckets_of(p, n, n))
+    got = _pass(q, k, v * 2.0 ** -power, do * 2.0 ** 8, table, p)
+    for name in ("dq", "dk", "dtable"):
+        # (fp16 results end in steps of 2^-24 too)
+        value, bound = want[name]
+        step = 0.0 if name == "dtable" else 2.0 ** (-25 + power - 8)
+        U.within((got[name][None] if name == "dtable" else got[name]).double() * 2.0 ** (power - 8), value, bound + step, name)
