@@ -1,4 +1,4 @@
-"""How exact attention's results are where plain bounds, which add up every rounding with one sign, say little: long float32 texts."""
+"""How exact attention's results are where plain bounds, which add up every rounding with one sign, say little: long float32 texts, scores that lie far from zero together, small values in fp16."""
 import math
 
 import pytest
@@ -221,3 +221,24 @@ def test_small_values_in_fp16(batch, n, power):
         value, bound = want[name]
         step = 0.0 if name == "dtable" else 2.0 ** (-25 + power - 8)
         U.within((got[name][None] if name == "dtable" else got[name]).double() * 2.0 ** (power - 8), value, bound + step, name)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("width", [8, 33, 64, 96, 128])
+@pytest.mark.parametrize("batch,n", [(4, 3), *SIZES])
+def test_weights_of_the_backward_pass_add_up_to_one(kind, width, batch, n):
+    """Scores that a shared bias rounds to steps of 128 (in units of ln 2), steps up to 2^128 in a weight: every kernel forms the same ones.  The sum of dv over the keys is that of do over the queries."""
+    nk = max(n, 300)
+    g = torch.Generator(device=DEV).manual_seed(width + n)
+    q, k, v, do = (s * torch.randn(batch, h, m, width, device=DEV, generator=g) for s, h, m in ((4, 4, n), (1, 2, nk), (1, 2, nk), (1, 4, n)))
+    q, k, v, do = (t.to(U.TYPES[kind]) for t in (q, k, v, do))
+    p = _ops().RelativePositions.distances(n, nk, 8, 30, DEV)
+    held = {"f32": 0.0, "bf16": 2.0 ** -16, "f16": 2.0 ** -21}[kind]
+    for bias in (-1e9, -1e6, 3e5):
+        got = _pass(q, k, v, do, torch.full((8, 4), bias, device=DEV), p, scale=1.0)
+        assert all(torch.isfinite(t).all() for t in got.values())
+        up = do.double().unflatten(1, (2, 2))
+        dv = got["dv"].double()
+        # dv's own roundings, those of p (its pieces, 2^x, and the sum of all keys), and the additions
+        bound = 1.01 * U.HALF_UNIT[U.TYPES[kind]] * dv.abs().sum(2) + nk * U.TINY[U.TYPES[kind]] + (held + (nk + 72 + 2 * n + 64) * U.U32) * up.abs().sum((2, 3))
+        U.within(dv.sum(2), up.sum((2, 3)), bound, f"{kind} {bias}")
