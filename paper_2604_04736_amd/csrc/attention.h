@@ -60,9 +60,10 @@ __device__ __forceinline__ int fresh_lane(int x)
     return x;
 }
 
-// Whether 32 keys' part of o is added up by itself before it goes to o.  float32's instruction takes four keys, so that o was one chain of 1024 additions over 4096 keys; what they leave off is in D, alike
-// for all keys of a row, and the sums of the table's gradient do not average it out (16 heads x 4096 tokens whose values have a common part: 3 times as far from 64 bits).  Now 128 additions of sums of eight;
-// 16 heads x 4096 x 128 in causal order 0.95 -> 1.00 ms forward.  The instruction of 16-bit types takes 32 keys anyway.
+// Whether 32 keys' part of o, and 32 queries' part of dk and dv, is added up by itself before it goes to the sum.  float32's instruction takes four of them, so that o was one chain of 1024 additions over 4096
+// keys, dk and dv one of all queries of the heads that share a key.  What o's leave off is in D, alike for all keys of a row, and the sums of the table's gradient do not average it out (16 heads x 4096 tokens
+// whose values have a common part: 3 times as far from 64 bits).  Now 128 additions of sums of eight: 16 heads x 4096 x 128 in causal order 0.95 -> 1.00 ms forward, 3.42 -> 3.48 a pass for dk and dv.
+// The instruction of 16-bit types takes 32 keys anyway.
 template <class T>
 constexpr bool kFresh = sizeof(T) == 4;
 
